@@ -477,6 +477,99 @@ int ham_embedder_set_vocab(ham_embedder *e, const void *table, int32_t vocab);
 int ham_embed_tokens(ham_embedder *e, const int32_t *ids, const int32_t *offsets,
                      int32_t batch, int32_t total_tokens, void *out, void *stream);
 
+/* ------------------------------------------------------------------------------------
+ * What follows a macro-step's attention: norm, 8-bit products, the choice of a token
+ * ------------------------------------------------------------------------------------
+ * The rest of a layer and the end of a macro-step, for serving: the output projection, the residual's
+ * addition and norm, the gated feed-forward block, the head and the token.  The paper takes these
+ * from the base model (Sec. 4.1) at its precision; 8-bit operands are this library's own choice, in
+ * the format of its FP8 pools: e4m3 codes with power-of-two scales.  At decoding batches the weights
+ * are most of what is read, and 8 bits halve them.
+ *
+ * 8-bit rows and weights.  A row of k elements (k a multiple of 16) is k code bytes and, for each
+ * block of 128 elements (the last may be shorter), one scale byte s: an element is code * 2^(s - 127)
+ * (E8M0; 255 is NaN).  A row's scale bytes are padded to a multiple of four:
+ *   codes  [rows][k] uint8;   scales [rows][4 * ceil(k / 512)] uint8
+ * A weight [n][k] has one scale for each block of 128 x 128:
+ *   codes  [n][k] uint8;      scales [ceil(n / 128)][4 * ceil(k / 512)] uint8
+ * The library's encoders choose s = E - 8 + 127 for a block's largest magnitude m 2^E (0.5 <= m < 1),
+ * E - 8 within [-124, 119], and s = 127 for a block of zeros; each element is scaled exactly and
+ * rounded once, to nearest with ties to even (infinities become +-448, NaN stays NaN).  They write
+ * 127 into the padding; what it holds is never used.  Codes must be 16-byte aligned, scales 4-byte.
+ *
+ * All calls are asynchronous on `stream`, one launch each (a programmatic dependent launch: it waits
+ * for the kernel before it on the stream before it reads a caller's buffer or writes one); with
+ * rows == 0 they launch nothing and the buffers may be NULL.  Outputs must not overlap inputs or each
+ * other unless a call says otherwise. */
+
+/* Residual addition and root-mean-square norm:
+ *   h = x + residual,  y = h / sqrt(mean_k(h_k^2) + eps) * weight
+ *   sum_out = bf16(h),  out = bf16(y),  codes and scales = the 8-bit row of y
+ * in fp32 from the bf16 inputs (the norm takes the unrounded h), each output rounded once.
+ * x, residual (nullable: 0)  device bf16 [rows][hidden];  weight  device bf16 [hidden]
+ * sum_out, out (nullable)    device bf16 [rows][hidden]; each may be x or residual itself
+ * codes, scales (nullable, together)  an 8-bit output as above; out or codes is required
+ * hidden a multiple of 16, at most 32768.  Host errors: HAM_EINVAL, HAM_ECUDA. */
+int ham_add_norm(const void *x, const void *residual, const void *weight, float eps, int32_t rows,
+                 int32_t hidden, void *sum_out, void *out, void *codes, void *scales, void *stream);
+
+/* bf16 rows [rows][k] -> 8-bit rows (e.g. an attention's output for its projection).
+ * Host errors: HAM_EINVAL, HAM_ECUDA. */
+int ham_fp8_encode(const void *x, int32_t rows, int32_t k, void *codes, void *scales, void *stream);
+
+/* A bf16 weight [n][k] -> codes and 128 x 128 block scales.  Host errors: HAM_EINVAL, HAM_ECUDA. */
+int ham_fp8_encode_weight(const void *w, int32_t n, int32_t k, void *codes, void *scales, void *stream);
+
+typedef struct ham_fp8_weight ham_fp8_weight; /* opaque handle: a weight laid out for the products */
+
+/* Copy a weight (device codes [n][k] and scales, as above) into the products' layout, on the current
+ * CUDA device (synchronous; the caller may free its copy).  With codes_up and scales_up the handle is
+ * a gated weight for ham_fp8_gated: codes the gate's projection, codes_up the up projection, both
+ * [n][k], n a multiple of 16.  Host errors: HAM_EINVAL, HAM_EUNSUPPORTED (the padded size passes
+ * 2^31 rows of 128), HAM_ENOMEM, HAM_ECUDA; *out is NULL on failure. */
+int ham_fp8_weight_alloc(int32_t n, int32_t k, const void *codes, const void *scales, const void *codes_up,
+                         const void *scales_up, ham_fp8_weight **out);
+int ham_fp8_weight_free(ham_fp8_weight *w); /* synchronizes as cudaFree does; NULL is a no-op */
+
+/* out [rows][n] = X W^T: 8-bit rows X [rows][k], products on the block-scaled tensor cores, summed in
+ * fp32 and rounded once to out_dtype (HAM_DTYPE_BF16 or HAM_DTYPE_F32).  The handle is only read:
+ * calls on several streams may share it.  Host errors: HAM_EINVAL (also for a gated weight),
+ * HAM_ECUDA. */
+int ham_fp8_linear(ham_fp8_weight *w, const void *x_codes, const void *x_scales, int32_t rows, void *out,
+                   int32_t out_dtype, void *stream);
+
+/* The first half of a gated feed-forward block, one kernel: G = X W_gate^T, U = X W_up^T (fp32),
+ * H = G / (1 + exp(-G)) * U, encoded as 8-bit rows (codes [rows][n], scales), the input of the second
+ * projection.  Host errors: HAM_EINVAL (also for a weight without an up part), HAM_ECUDA. */
+int ham_fp8_gated(ham_fp8_weight *w, const void *x_codes, const void *x_scales, int32_t rows, void *codes,
+                  void *scales, void *stream);
+
+/* Read and clear the weight's device error word (a bounded wait of a product that ran out;
+ * synchronizes `stream`).  Returns HAM_EDEVICE if it was set, with the code in *device_code. */
+int ham_fp8_weight_status(ham_fp8_weight *w, void *stream, int32_t *device_code);
+
+/* One token for each row of logits, from a given random number.  For a row l with settings T, k, p, m
+ * and the random number u:
+ *   w_i = trunc(2^31 exp((l_i - max l) / T)), x = (l_i - max l) / T in fp32 (0 where l_i = max l)
+ *   tokens are ordered by l, largest first, equal ones by index; kept are the first k of them (top-k),
+ *   of these the shortest prefix whose weights reach p times the weights of the k (top-p), of these
+ *   the ones with w_i >= m 2^31 (min-p: m times the likeliest token's weight)
+ *   token = the first index, in index order, at which the running sum of the kept weights exceeds
+ *   floor(u S), S their whole sum;  prob = w_token / S
+ * The weights are whole numbers and their sums exact, so the token does not depend on batch, launch
+ * shape or the order of additions.  T <= 0 (or NaN) takes the largest logit, ties to the lowest index.
+ * k <= 0 or k >= vocab, p >= 1 and m <= 0 keep all; the likeliest token is always kept.  A NaN logit
+ * counts as -inf (ruled out); a row with nothing but those gives token -1 and prob 0.
+ * logits       device [rows][vocab], bf16 or f32 (logits_dtype), 16-byte aligned; vocab at most 2^18
+ * u            device f32 [rows], in [0, 1)
+ * temperature, top_p, min_p  nullable device f32 [rows];  top_k  nullable device int32 [rows]
+ *              (NULL: temperature 1, the others off)
+ * tokens       device int32 [rows];  probs  nullable device f32 [rows]
+ * Host errors: HAM_EINVAL, HAM_EUNSUPPORTED (vocab above 2^18), HAM_ECUDA. */
+int ham_sample(const void *logits, int32_t logits_dtype, int32_t rows, int32_t vocab, const float *u,
+               const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+               int32_t *tokens, float *probs, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

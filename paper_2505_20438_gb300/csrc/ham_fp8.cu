@@ -1,0 +1,886 @@
+// Products with 8-bit weights (e4m3 codes, a power-of-two scale for each 128 x 128 block) of 8-bit
+// rows (a scale for each 128 elements), on the block-scaled tensor-core products of sm_103a, and the
+// first half of a gated feed-forward block made of two of them:
+//
+//   Y[t][n] = sum_b 2^(sx[t][b] + sw[n / 128][b] - 254) sum_{k in block b} X[t][k] W[n][k]
+//   H[t][f] = silu(G[t][f]) U[t][f],  G = X W_g^T, U = X W_u^T,  encoded as 8-bit rows
+//
+// The scales are E8M0 bytes, so tcgen05 kind::mxf8f6f4 applies them inside the product (its scale
+// blocks are 32 elements of K: four products of a 128-block use the same byte) and a whole sum stays
+// in one fp32 accumulator in tensor memory.  Four consecutive blocks' bytes are one 32-bit word of a
+// row; a word serves four K steps, the instruction descriptor selecting the byte, so that the scales
+// of an operand tile are copied to tensor memory (512 bytes a copy) once every four steps.
+//
+// Weights are laid out once (ham_fp8_weight_alloc) as [tile of 128 rows][K block][128 x 128], each
+// block 16 KiB in the shared-memory layout of the 128-byte swizzle, so that a weight tile's K range is
+// one contiguous stretch of memory (a gated weight: gate and up block after block).
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cstring>
+#include <new>
+
+#include "ham_mx.cuh"
+#include "ham_ops.cuh"
+
+struct ham_fp8_weight {
+  int32_t n = 0, k = 0, parts = 1;   // parts: 2 for a gated weight (gate, up)
+  int32_t tiles = 0, kbs = 0, sk = 0;
+  int device = 0;
+  uint8_t *codes = nullptr;    // [tiles][kbs][parts][128 x 128 swizzled]
+  uint8_t *scales = nullptr;   // [tiles][parts][sk]
+  int32_t *err = nullptr;      // device error word
+  int32_t *host_err = nullptr; // pinned
+  CUtensorMap map;             // codes as [tiles * kbs * parts * 128][128] bytes, boxes of a block
+};
+
+namespace ham {
+namespace {
+
+constexpr int kTile = 128;             // weight rows of a tile
+constexpr int kBlockBytes = 128 * 128; // a tile's K block
+
+// One thread per 16-byte piece of the laid-out weight.
+__global__ void lay_out_weight_kernel(const uint8_t *__restrict__ codes, int n, int k, int part, int parts,
+                                      int kbs, int64_t pieces, uint8_t *__restrict__ dst) {
+  const int64_t p = blockIdx.x * (int64_t)blockDim.x + threadIdx.x;
+  if (p >= pieces) return;
+  const int in = (int)(p % (kBlockBytes / 16)), r = in / 8, c = in % 8;
+  const int64_t block = p / (kBlockBytes / 16);  // tile * kbs + kb
+  const int64_t row = block / kbs * kTile + r;
+  const int col = (int)(block % kbs) * kFp8Block + 16 * c;
+  uint4 v = make_uint4(0, 0, 0, 0);
+  if (row < n && col < k) v = *reinterpret_cast<const uint4 *>(codes + row * k + col);
+  *reinterpret_cast<uint4 *>(dst + (block * parts + part) * kBlockBytes + r * 128 + ((c ^ (r & 7)) << 4)) = v;
+}
+__global__ void lay_out_scales_kernel(const uint8_t *__restrict__ scales, int tiles, int sk, int part,
+                                      int parts, uint8_t *__restrict__ dst) {
+  const int i = blockIdx.x * blockDim.x + threadIdx.x;
+  if (i < tiles * sk) dst[((int64_t)(i / sk) * parts + part) * sk + i % sk] = scales[i];
+}
+
+// Shared memory that a CTA with `cols` columns of tensor memory asks for at least, in kernels whose CTAs
+// wait for one another: an SM's 228 KB then run out before its 512 columns do, so that no CTA of a
+// cluster ever waits for columns that a CTA of another cluster holds (two clusters could otherwise each
+// hold what the other waits for).
+constexpr int smem_floor(int cols) { return (228 * 1024 * (cols / 32) + 16) / 17; }
+
+struct ProductArgs {
+  const uint8_t *w, *ws;   // the handle's layout
+  const uint8_t *xs;       // [rows][sk]
+  void *out;               // [rows][n], or [rows][n] codes of a gated product
+  uint8_t *out_scales;     // gated: [rows][out_sk]
+  int32_t *err;
+  int rows, n, kbs, sk, out_sk;
+  int nt;                  // rows (of X) a CTA of the streaming kernel takes, a multiple of 16
+  int stages, stage_bytes, tmem_cols;
+  int tiles;               // weight tiles
+  int f32;                 // fp32 output
+};
+
+__device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.f + expf(-g)) * u; }
+
+// Four neighbouring outputs of one row from column c (a multiple of 4), within the row's n.
+__device__ __forceinline__ void store4(const ProductArgs &a, int64_t row, int c, float4 v) {
+  const int64_t at = row * a.n + c;
+  if (c + 4 <= a.n && (a.n & 3) == 0) {
+    if (a.f32)
+      *reinterpret_cast<float4 *>(static_cast<float *>(a.out) + at) = v;
+    else
+      *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + at) =
+          make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+    return;
+  }
+  const float f[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (c + i < a.n) {
+      if (a.f32) static_cast<float *>(a.out)[at + i] = f[i];
+      else static_cast<__nv_bfloat16 *>(a.out)[at + i] = __float2bfloat16_rn(f[i]);
+    }
+}
+
+// ------------------------------------------------------------------------------------
+// Few rows: the weights stream
+// ------------------------------------------------------------------------------------
+// A CTA multiplies one weight tile's (128 rows: the product's M; gated: the gate's and the up's tile)
+// K range with nt rows of X (its N).  The K blocks are cut over the CTAs of a cluster, which add their
+// fp32 accumulators through distributed shared memory, in the order of the ranges.  Weight blocks are
+// requested before the dependency wait: nothing on the stream writes them.
+constexpr int kStreamThreads = 256;
+constexpr int kStreamSf = 4;            // scale slots (of four K blocks each)
+constexpr int kStreamSmem = 200 * 1024; // ring budget, one CTA an SM
+constexpr int kStreamSmem2 = 104 * 1024; // ... where two CTAs share an SM
+
+constexpr int kStreamStages = 12;       // at most
+constexpr int kStreamBars = (2 * kStreamStages + 2 * kStreamSf + 1) * 8;
+// Bytes of a scale slot (the weight tiles', the rows') and of everything beside the ring.
+__host__ __device__ constexpr int stream_sf_bytes(int parts) { return (parts + 1) * 512; }
+constexpr int stream_fixed(int parts) { return 1024 + kStreamSf * stream_sf_bytes(parts) + kStreamBars; }
+
+template <int kParts>
+__global__ void __launch_bounds__(kStreamThreads)
+    fp8_stream_kernel(const __grid_constant__ CUtensorMap tx, ProductArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t *sf = ring + (size_t)a.stages * a.stage_bytes;
+  uint64_t *full = reinterpret_cast<uint64_t *>(sf + kStreamSf * stream_sf_bytes(kParts));
+  uint64_t *empty = full + kStreamStages, *sf_full = empty + kStreamStages;
+  uint64_t *sf_empty = sf_full + kStreamSf, *acc_full = sf_empty + kStreamSf;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_shared;
+  volatile int *abort_flag = &abort_shared;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tile = blockIdx.x, splits = gridDim.y, rank = blockIdx.y;  // a cluster: the splits
+  const int n0 = blockIdx.z * a.nt;
+  const int kb0 = (int)((int64_t)rank * a.kbs / splits), kb1 = (int)((int64_t)(rank + 1) * a.kbs / splits);
+  const int nk = kb1 - kb0, stages = a.stages;
+  const int g0 = kb0 >> 2;                            // first scale word
+  const int ng = ((kb1 + 3) >> 2) - g0;
+  if (tid == 0) {
+    for (int s = 0; s < stages; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int s = 0; s < kStreamSf; ++s) {
+      mbar_init(&sf_full[s], 1);
+      mbar_init(&sf_empty[s], 1);
+    }
+    mbar_init(acc_full, 1);
+    abort_shared = 0;
+    fence_mbar_init();
+  }
+  if (warp == 0 && lane == 0) prefetch_tensormap(&tx);
+  if (warp == 1) tmem_alloc_n(&tmem_slot, (uint32_t)a.tmem_cols);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  const uint32_t sf_tmem = tmem + kParts * a.nt;      // two buffers of (kParts + 1) * 4 columns
+  int issued = 0;
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ copies
+    if (lane == 0) {
+      const uint64_t pol_x = policy_evict_last();
+      const uint8_t *src = a.w + ((int64_t)tile * a.kbs + kb0) * (kParts * kBlockBytes);
+      const int xbytes = a.nt * 128;
+      auto load_w = [&](int t, int s) {
+        mbar_arrive_tx(&full[s], (uint32_t)(kParts * kBlockBytes + xbytes));
+        bulk_load(ring + s * a.stage_bytes, src + (int64_t)t * (kParts * kBlockBytes),
+                  (uint32_t)(kParts * kBlockBytes), &full[s]);
+      };
+      const int pre = min(stages, nk);
+      for (int t = 0; t < pre; ++t) load_w(t, t);
+      grid_dependency_wait();
+      for (int t = 0; t < nk; ++t) {
+        const int s = t % stages;
+        if (t >= pre) {
+          if (!thread_wait(&empty[s], (uint32_t)(t / stages - 1) & 1u, abort_flag, true)) break;
+          load_w(t, s);
+        }
+        tma_load_2d(ring + s * a.stage_bytes + kParts * kBlockBytes, &tx, (kb0 + t) * kFp8Block, n0, &full[s],
+                    pol_x);
+        issued = t + 1;
+      }
+      if (issued < nk && !*abort_flag) {
+        record_error(a.err, HAM_DEVERR_TIMEOUT);
+        *abort_flag = 1;
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ products
+    bool ok = true;
+    for (int t = 0; t < nk; ++t) {
+      const int s = t % stages, kb = kb0 + t, g = (kb >> 2) - g0;
+      const bool first = t == 0 || (kb & 3) == 0;     // a new scale word
+      const uint32_t sft = sf_tmem + (uint32_t)((g & 1) * (kParts + 1) * 4);
+      if (first && !warp_wait(&sf_full[g % kStreamSf], (uint32_t)(g / kStreamSf) & 1u, abort_flag)) { ok = false; break; }
+      if (!warp_wait(&full[s], (uint32_t)(t / stages) & 1u, abort_flag)) { ok = false; break; }
+      if (elect_one()) {
+        tc_fence_after();
+        if (first) {
+          const uint32_t from = smem_u32(sf + (g % kStreamSf) * stream_sf_bytes(kParts));
+#pragma unroll
+          for (int p = 0; p <= kParts; ++p) tc_copy_scales<1>(sft + p * 4, from + p * 512);
+          tc_commit(&sf_empty[g % kStreamSf]);
+        }
+        const uint32_t wa = smem_u32(ring + s * a.stage_bytes), xa = wa + kParts * kBlockBytes;
+        const uint32_t idesc = idesc_mx(kTile, a.nt, kb & 3);
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+          for (int p = 0; p < kParts; ++p)
+            tc_mma_mx<1>(tmem + p * a.nt, smem_desc_sw128(wa + p * kBlockBytes + kk * 32, 16, 1024),
+                         smem_desc_sw128(xa + kk * 32, 16, 1024), idesc, sft + p * 4, sft + kParts * 4,
+                         t > 0 || kk > 0);
+        tc_commit(&empty[s]);
+      }
+      __syncwarp();
+    }
+    if (!ok && lane == 0 && !*abort_flag) {
+      record_error(a.err, HAM_DEVERR_TIMEOUT);
+      *abort_flag = 1;
+    }
+    __syncwarp();
+    if (elect_one()) tc_commit(acc_full);  // also after an abort: what was issued completes
+    __syncwarp();
+  } else if (warp == 2) {
+    // ------------------------------------------------------------ scale words
+    uint32_t w[kParts];
+#pragma unroll
+    for (int p = 0; p < kParts; ++p) w[p] = 0;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    for (int g = 0; g < ng; ++g) {
+      const int slot = g % kStreamSf;
+      uint32_t x[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int r = lane + 32 * j;
+        x[j] = 0x7f7f7f7fu;
+        if (r < a.nt && n0 + r < a.rows)
+          x[j] = __ldg(reinterpret_cast<const uint32_t *>(a.xs + (int64_t)(n0 + r) * a.sk) + g0 + g);
+      }
+#pragma unroll
+      for (int p = 0; p < kParts; ++p)
+        w[p] = __ldg(reinterpret_cast<const uint32_t *>(a.ws + ((int64_t)tile * kParts + p) * a.sk) + g0 + g);
+      if (g >= kStreamSf &&
+          !warp_wait(&sf_empty[slot], (uint32_t)(g / kStreamSf - 1) & 1u, abort_flag)) {
+        if (lane == 0 && !*abort_flag) {
+          record_error(a.err, HAM_DEVERR_TIMEOUT);
+          *abort_flag = 1;
+        }
+        break;
+      }
+      uint4 *dst = reinterpret_cast<uint4 *>(sf + slot * stream_sf_bytes(kParts)) + lane;
+#pragma unroll
+      for (int p = 0; p < kParts; ++p) dst[p * 32] = make_uint4(w[p], w[p], w[p], w[p]);
+      dst[kParts * 32] = make_uint4(x[0], x[1], x[2], x[3]);
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sf_full[slot]);
+    }
+  }
+
+  // ---------------------------------------------------------------- epilogue (every warp)
+  // Accumulators -> shared memory [part][row][128 features] (the ring, free by now), then each CTA of
+  // the cluster adds its share of the rows: a warp a row, a lane four features.
+  __syncwarp();
+  bool ok = warp_wait(acc_full, 0u, abort_flag);
+  ok = ok && !__any_sync(kFull, *abort_flag != 0);
+  float *acc = reinterpret_cast<float *>(ring);
+  if (ok) {
+    tc_fence_after();
+    const int quarter = warp & 3;
+    const uint32_t t_row = tmem + ((uint32_t)(quarter * 32) << 16);
+    for (int c = (warp >> 2) * 16; c < kParts * a.nt; c += 32) {
+      uint32_t v[16];
+      tmem_ld16(t_row + c, v);
+      tmem_wait_ld();
+#pragma unroll
+      for (int j = 0; j < 16; ++j) acc[(c + j) * kTile + quarter * 32 + lane] = __uint_as_float(v[j]);
+    }
+  }
+  tc_fence_before();
+  if (splits > 1) cluster_sync_all();
+  else __syncthreads();
+  if (warp == 1) {
+    if (!ok && lane == 0) thread_wait(acc_full, 0u, abort_flag, false);  // products in flight
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc_n(tmem, (uint32_t)a.tmem_cols);
+  }
+  const int live = min(a.nt, a.rows - n0);
+  if (ok) {
+    const uint32_t base = smem_u32(acc) + lane * 16;
+    for (int r = rank * 8 + warp; r < live; r += splits * 8) {
+      float4 v[kParts];
+#pragma unroll
+      for (int p = 0; p < kParts; ++p) {
+        const uint32_t at = base + (uint32_t)((p * a.nt + r) * kTile * 4);
+        if (splits == 1) {
+          v[p] = *reinterpret_cast<const float4 *>(acc + (p * a.nt + r) * kTile + lane * 4);
+        } else {
+          v[p] = ld_cluster_f4(cluster_map_shared(at, 0));
+          for (int q = 1; q < splits; ++q) {
+            const float4 o = ld_cluster_f4(cluster_map_shared(at, q));
+            v[p].x += o.x, v[p].y += o.y, v[p].z += o.z, v[p].w += o.w;
+          }
+        }
+      }
+      const int c = tile * kTile + lane * 4;
+      if constexpr (kParts == 1) {
+        if (c < a.n) store4(a, n0 + r, c, v[0]);
+      } else {
+        const float h[4] = {silu_mul(v[0].x, v[1].x), silu_mul(v[0].y, v[1].y), silu_mul(v[0].z, v[1].z),
+                            silu_mul(v[0].w, v[1].w)};
+        const float m = warp_max_f32(fmaxf(fmaxf(fabsf(h[0]), fabsf(h[1])), fmaxf(fabsf(h[2]), fabsf(h[3]))));
+        const int e = fp8_exponent(m);
+        if (c < a.n)  // (n is a multiple of 16; features past it are zeros)
+          *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(a.out) + (int64_t)(n0 + r) * a.n + c) =
+              fp8_codes4(h[0], h[1], h[2], h[3], fp8_pow2(-e));
+        uint8_t *s = a.out_scales + (int64_t)(n0 + r) * a.out_sk;
+        if (lane == 0) s[tile] = (uint8_t)(e + 127);
+        else if (tile == a.tiles - 1 && lane < a.out_sk - tile) s[tile + lane] = 127;  // padding
+      }
+    }
+  }
+  if (splits > 1) cluster_sync_all();  // (a peer may still read this CTA's accumulators)
+  if (tid == 0 && *abort_flag)  // after an abort, this CTA's copies land before it exits
+    for (int t = max(0, issued - stages); t < issued; ++t)
+      thread_wait(&full[t % stages], (uint32_t)(t / stages) & 1u, abort_flag, false);
+}
+
+// ------------------------------------------------------------------------------------
+// Many rows: pairs of CTAs, tiles of 256 x 256
+// ------------------------------------------------------------------------------------
+// A pair of CTAs (cta_group::2) computes 256 rows of X by two weight tiles (a gated weight: the gate's
+// and the up's tile of the same features): each CTA holds 128 of the rows (its lanes of tensor memory)
+// and loads its rows and one of the two weight tiles, so that every byte of an operand is read from
+// L2 once a pair.  The pairs are persistent.  The two accumulators (256 columns each) share 64 columns,
+// which leaves the columns 448.. for the scales: a tile's epilogue empties the shared columns first,
+// and the next tile's products begin when it has.
+constexpr int kPairThreads = 256;       // warps: copies, products, scales, -, 4 x epilogue
+constexpr int kPairStages = 6;
+constexpr int kPairStageBytes = 2 * kBlockBytes;
+constexpr int kPairSf = 4;
+constexpr int kPairSfBytes = 3 * 512;   // the CTA's 128 rows, both weight tiles
+constexpr int kPairBuf1 = 192, kPairSfCol = 448;
+constexpr int kPairSmem = smem_floor(512);
+static_assert(kPairSmem >= 1024 + kPairStages * kPairStageBytes + kPairSf * kPairSfBytes + 256 &&
+                  kPairSmem <= 227 * 1024, "shared memory");
+
+template <bool kGated>
+__global__ void __launch_bounds__(kPairThreads, 1)
+    fp8_pair_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ CUtensorMap tw,
+                    ProductArgs a, int row_tiles, int col_tiles) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t *sf = ring + kPairStages * kPairStageBytes;
+  uint64_t *full = reinterpret_cast<uint64_t *>(sf + kPairSf * kPairSfBytes);  // of the first CTA
+  uint64_t *empty = full + kPairStages;
+  uint64_t *sf_full = empty + kPairStages;     // of the first CTA: an arrival a CTA
+  uint64_t *sf_empty = sf_full + kPairSf;
+  uint64_t *acc_full = sf_empty + kPairSf;     // [2]
+  uint64_t *acc_shared_free = acc_full + 2;    // of the first CTA: an arrival an epilogue warp
+  uint64_t *drained = acc_shared_free + 1;     // every product issued is complete (after an abort)
+  static_assert((2 * kPairStages + 2 * kPairSf + 4) * 8 <= 256, "barriers");
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_shared;
+  volatile int *abort_flag = &abort_shared;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = (int)cluster_rank();
+  const int pairs = gridDim.x / 2, pair = blockIdx.x / 2;
+  const int total = row_tiles * col_tiles;
+  if (tid == 0) {
+    for (int s = 0; s < kPairStages; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int s = 0; s < kPairSf; ++s) {
+      mbar_init(&sf_full[s], 2);
+      mbar_init(&sf_empty[s], 1);
+    }
+    mbar_init(&acc_full[0], 1);
+    mbar_init(&acc_full[1], 1);
+    mbar_init(acc_shared_free, 8);
+    mbar_init(drained, 1);
+    abort_shared = 0;
+    fence_mbar_init();
+  }
+  if (warp == 0 && lane == 0) {
+    prefetch_tensormap(&tx);
+    prefetch_tensormap(&tw);
+  }
+  if (warp == 1) tmem_alloc_pair<512>(&tmem_slot);
+  tc_fence_before();
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  int issued = 0;
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ copies
+    if (lane == 0) {
+      const uint64_t pol = policy_evict_last();
+      grid_dependency_wait();
+      bool ok = true;
+      int it = 0;
+      for (int w = pair; w < total && ok; w += pairs) {
+        const int rt = w % row_tiles, ct = w / row_tiles;
+        const int x_row = rt * 256 + rank * 128;
+        // the laid-out weight's rows of K block 0 of this CTA's tile
+        const int64_t block = kGated ? (int64_t)ct * a.kbs * 2 + rank : ((int64_t)ct * 2 + rank) * a.kbs;
+        for (int kb = 0; kb < a.kbs; ++kb, ++it) {
+          const int s = it % kPairStages;
+          if (it >= kPairStages &&
+              !thread_wait(&empty[s], (uint32_t)(it / kPairStages - 1) & 1u, abort_flag, true)) {
+            ok = false;
+            break;
+          }
+          if (rank == 0) mbar_arrive_tx(&full[s], 2 * kPairStageBytes);  // both CTAs' copies
+          const uint32_t bar = cluster_map_shared(smem_u32(&full[s]), 0);
+          uint8_t *dst = ring + s * kPairStageBytes;
+          tma_load_2d_pair(dst, &tx, kb * kFp8Block, x_row, bar, pol);
+          tma_load_2d_pair(dst + kBlockBytes, &tw, 0, (int)((block + (int64_t)kb * (kGated ? 2 : 1)) * 128), bar,
+                           pol);
+          issued = it + 1;
+        }
+      }
+      if (!ok && !*abort_flag) {
+        record_error(a.err, HAM_DEVERR_TIMEOUT);
+        *abort_flag = 1;
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ products (first CTA)
+    if (rank == 0) {
+      bool ok = true;
+      int it = 0, gi = 0, n = 0;
+      for (int w = pair; w < total && ok; w += pairs, ++n) {
+        const uint32_t acc = tmem + (uint32_t)((n & 1) * kPairBuf1);
+        if (n > 0 && !warp_wait_cluster(acc_shared_free, (uint32_t)(n - 1) & 1u, abort_flag)) { ok = false; break; }
+        for (int kb = 0; kb < a.kbs; ++kb, ++it) {
+          const int s = it % kPairStages;
+          const bool first = (kb & 3) == 0;
+          const uint32_t sft = tmem + kPairSfCol + (uint32_t)((gi & 1) * 16);
+          if (first && !warp_wait_cluster(&sf_full[gi % kPairSf], (uint32_t)(gi / kPairSf) & 1u, abort_flag)) { ok = false; break; }
+          if (!warp_wait_cluster(&full[s], (uint32_t)(it / kPairStages) & 1u, abort_flag)) { ok = false; break; }
+          if (elect_one()) {
+            tc_fence_after();
+            if (first) {
+              const uint32_t from = smem_u32(sf + (gi % kPairSf) * kPairSfBytes);
+#pragma unroll
+              for (int p = 0; p < 3; ++p) tc_copy_scales<2>(sft + p * 4, from + p * 512);
+              tc_commit_pair(&sf_empty[gi % kPairSf]);
+            }
+            const uint32_t xa = smem_u32(ring + s * kPairStageBytes), wa = xa + kBlockBytes;
+            const uint32_t idesc = idesc_mx(256, 256, kb & 3);
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk)
+              tc_mma_mx<2>(acc, smem_desc_sw128(xa + kk * 32, 16, 1024), smem_desc_sw128(wa + kk * 32, 16, 1024),
+                           idesc, sft, sft + 4, kb > 0 || kk > 0);
+            tc_commit_pair(&empty[s]);
+            if (kb == a.kbs - 1) tc_commit_pair(&acc_full[n & 1]);
+          }
+          __syncwarp();
+          if ((kb & 3) == 3 || kb == a.kbs - 1) ++gi;
+        }
+      }
+      if (!ok) {
+        if (lane == 0 && !*abort_flag) {
+          record_error(a.err, HAM_DEVERR_TIMEOUT);
+          *abort_flag = 1;
+        }
+        __syncwarp();
+        if (elect_one()) {
+          tc_commit_pair(drained);
+          thread_wait(drained, 0u, abort_flag, false);
+        }
+        __syncwarp();
+      }
+    }
+  } else if (warp == 2) {
+    // ------------------------------------------------------------ scale words
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int groups = (a.kbs + 3) / 4;
+    bool ok = true;
+    int gi = 0;
+    for (int w = pair; w < total && ok; w += pairs) {
+      const int rt = w % row_tiles, ct = w / row_tiles;
+      const int x_row = rt * 256 + rank * 128;
+      for (int g = 0; g < groups; ++g, ++gi) {
+        const int slot = gi % kPairSf;
+        uint32_t x[4], ws[2];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int r = x_row + lane + 32 * j;
+          x[j] = r < a.rows ? __ldg(reinterpret_cast<const uint32_t *>(a.xs + (int64_t)r * a.sk) + g) : 0x7f7f7f7fu;
+        }
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {  // the tile's scale rows: [tile][part]
+          const int row = ct * 2 + p;
+          ws[p] = kGated || row < a.tiles
+                      ? __ldg(reinterpret_cast<const uint32_t *>(a.ws + (int64_t)row * a.sk) + g)
+                      : 0x7f7f7f7fu;
+        }
+        if (gi >= kPairSf && !warp_wait(&sf_empty[slot], (uint32_t)(gi / kPairSf - 1) & 1u, abort_flag)) {
+          ok = false;
+          break;
+        }
+        uint4 *dst = reinterpret_cast<uint4 *>(sf + slot * kPairSfBytes) + lane;
+        dst[0] = make_uint4(x[0], x[1], x[2], x[3]);
+        dst[32] = make_uint4(ws[0], ws[0], ws[0], ws[0]);
+        dst[64] = make_uint4(ws[1], ws[1], ws[1], ws[1]);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(cluster_map_shared(smem_u32(&sf_full[slot]), 0));
+      }
+    }
+    if (!ok && lane == 0 && !*abort_flag) {
+      record_error(a.err, HAM_DEVERR_TIMEOUT);
+      *abort_flag = 1;
+    }
+  } else if (warp >= 4) {
+    // ------------------------------------------------------------ epilogue: a thread a row
+    const int quarter = warp & 3;
+    const uint32_t free_bar = cluster_map_shared(smem_u32(acc_shared_free), 0);
+    bool ok = true;
+    int n = 0;
+    for (int w = pair; w < total && ok; w += pairs, ++n) {
+      const int rt = w % row_tiles, ct = w / row_tiles, buf = n & 1;
+      const int row = rt * 256 + rank * 128 + quarter * 32 + lane;
+      const uint32_t acc = tmem + (uint32_t)(buf * kPairBuf1) + ((uint32_t)(quarter * 32) << 16);
+      if (!warp_wait_cluster(&acc_full[buf], (uint32_t)(n >> 1) & 1u, abort_flag)) {
+        if (lane == 0 && !*abort_flag) {
+          record_error(a.err, HAM_DEVERR_TIMEOUT);
+          *abort_flag = 1;
+        }
+        ok = false;
+        break;
+      }
+      tc_fence_after();
+      if constexpr (!kGated) {
+        const int c0 = ct * 256, first = buf ? 0 : 6;  // the shared 64 columns first
+        const bool vec = (a.n & 7) == 0;
+#pragma unroll 1
+        for (int i = 0; i < 8; ++i) {
+          const int ch = (first + i) & 7;
+          uint32_t v[32];
+          tmem_ld32(acc + ch * 32, v);
+          tmem_wait_ld();
+          if (i == 1) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(free_bar);
+          }
+          const int c = c0 + ch * 32;
+          if (row < a.rows && c < a.n) {
+            if (vec && c + 32 <= a.n && !a.f32) {
+              uint4 *dst = reinterpret_cast<uint4 *>(static_cast<uint16_t *>(a.out) + (int64_t)row * a.n + c);
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                const float *f = reinterpret_cast<const float *>(v) + 8 * q;
+                dst[q] = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]),
+                                    pack_bf16x2(f[6], f[7]));
+              }
+            } else {
+#pragma unroll
+              for (int q = 0; q < 8; ++q)
+                if (c + 4 * q < a.n)
+                  store4(a, row, c + 4 * q, make_float4(__uint_as_float(v[4 * q]), __uint_as_float(v[4 * q + 1]),
+                                                        __uint_as_float(v[4 * q + 2]), __uint_as_float(v[4 * q + 3])));
+            }
+          }
+        }
+      } else {
+        // features in two halves of 64, the one that lies in the shared columns first
+        float h[2][64];
+        const int first = buf ? 0 : 1;
+        float m = 0.f;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int half = first ^ i;
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            uint32_t g[32], u[32];
+            tmem_ld32(acc + half * 64 + j * 32, g);
+            tmem_ld32(acc + 128 + half * 64 + j * 32, u);
+            tmem_wait_ld();
+#pragma unroll
+            for (int q = 0; q < 32; ++q) {
+              h[i][j * 32 + q] = silu_mul(__uint_as_float(g[q]), __uint_as_float(u[q]));
+              m = fmaxf(m, fabsf(h[i][j * 32 + q]));
+            }
+          }
+          if (i == 0) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(free_bar);
+          }
+        }
+        const int e = fp8_exponent(m);
+        const float p = fp8_pow2(-e);
+        if (row < a.rows) {
+          uint8_t *dst = static_cast<uint8_t *>(a.out) + (int64_t)row * a.n;
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const int c = ct * kTile + (first ^ i) * 64 + q * 16;
+              const float *f = h[i] + q * 16;
+              if (c < a.n)  // (n is a multiple of 16)
+                *reinterpret_cast<uint4 *>(dst + c) =
+                    make_uint4(fp8_codes4(f[0], f[1], f[2], f[3], p), fp8_codes4(f[4], f[5], f[6], f[7], p),
+                               fp8_codes4(f[8], f[9], f[10], f[11], p), fp8_codes4(f[12], f[13], f[14], f[15], p));
+            }
+          uint8_t *s = a.out_scales + (int64_t)row * a.out_sk;
+          s[ct] = (uint8_t)(e + 127);
+          if (ct == a.tiles - 1)
+            for (int b = a.tiles; b < a.out_sk; ++b) s[b] = 127;  // padding
+        }
+      }
+    }
+    tc_fence_before();
+  }
+  __syncwarp();
+  if (warp == 0 && lane == 0 && rank == 0 && *abort_flag)
+    // after an abort the pair's copies (all count at this CTA's barriers) land before either CTA exits
+    for (int t = max(0, issued - kPairStages); t < issued; ++t)
+      thread_wait(&full[t % kPairStages], (uint32_t)(t / kPairStages) & 1u, abort_flag, false);
+  __syncwarp();
+  cluster_sync_all();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc_pair<512>(tmem);
+  }
+}
+
+// ------------------------------------------------------------------------------------
+// Host side
+// ------------------------------------------------------------------------------------
+template <typename K>
+cudaError_t allow_smem(K kernel, int bytes, bool (&done)[64], int dev) {
+  if (dev >= 0 && dev < 64 && done[dev]) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && dev >= 0 && dev < 64) done[dev] = true;
+  return e;
+}
+
+// Pairs of CTAs that are resident at once (a pair lies within one group of SMs, and an odd group
+// leaves an SM without a partner); a persistent grid is no larger.
+template <typename K>
+int resident_pairs(K kernel, int (&known)[64], int dev) {
+  if (dev >= 0 && dev < 64 && known[dev] > 0) return known[dev];
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(device_sms() / 2 * 2));
+  cfg.blockDim = dim3(kPairThreads);
+  cfg.dynamicSmemBytes = (size_t)kPairSmem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int n = 0;
+  if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
+    cudaGetLastError();
+    n = device_sms() / 2;
+  }
+  if (dev >= 0 && dev < 64) known[dev] = n;
+  return n;
+}
+
+template <int kParts>
+cudaError_t launch_stream(const CUtensorMap &tx, ProductArgs a, int dev, cudaStream_t stream) {
+  static bool done[64] = {};
+  const int sms = device_sms();
+  const int zt = (a.rows + a.nt - 1) / a.nt;
+  int splits = 1;
+  while (splits < 8 && splits * 2 <= a.kbs && (int64_t)a.tiles * zt * splits * 2 <= sms) splits *= 2;
+  a.stage_bytes = kParts * kBlockBytes + a.nt * 128;
+  const int per = (a.kbs + splits - 1) / splits;      // K blocks of a CTA
+  const int budget = (int64_t)a.tiles * zt * splits > sms ? kStreamSmem2 : kStreamSmem;
+  a.stages = std::min(std::min(per, kStreamStages), (budget - stream_fixed(kParts)) / a.stage_bytes);
+  const int acc = kParts * a.nt * kTile * 4;          // the epilogue's, in the ring
+  a.stages = std::max(std::max(a.stages, 2), (acc + a.stage_bytes - 1) / a.stage_bytes);
+  int cols = 32;
+  while (cols < kParts * a.nt + 2 * (kParts + 1) * 4) cols *= 2;
+  a.tmem_cols = cols;
+  const int smem = std::max(a.stages * a.stage_bytes + stream_fixed(kParts), splits > 1 ? smem_floor(cols) : 0);
+  cudaError_t e = allow_smem(fp8_stream_kernel<kParts>, 226 * 1024, done, dev);
+  if (e != cudaSuccess) return e;
+  return launch_after(fp8_stream_kernel<kParts>, dim3((unsigned)a.tiles, (unsigned)splits, (unsigned)zt),
+                      dim3(kStreamThreads), (size_t)smem, dim3(1, (unsigned)splits, 1), stream, tx, a);
+}
+
+template <bool kGated>
+cudaError_t launch_pair(const CUtensorMap &tx, const CUtensorMap &tw, const ProductArgs &a, int dev,
+                        cudaStream_t stream) {
+  static bool done[64] = {};
+  static int resident[64] = {};
+  const int row_tiles = (a.rows + 255) / 256, col_tiles = kGated ? a.tiles : (a.tiles + 1) / 2;
+  cudaError_t e = allow_smem(fp8_pair_kernel<kGated>, kPairSmem, done, dev);
+  if (e != cudaSuccess) return e;
+  const int pairs = std::min(resident_pairs(fp8_pair_kernel<kGated>, resident, dev), row_tiles * col_tiles);
+  return launch_after(fp8_pair_kernel<kGated>, dim3((unsigned)(2 * pairs)), dim3(kPairThreads), (size_t)kPairSmem,
+                      dim3(2, 1, 1), stream, tx, tw, a, row_tiles, col_tiles);
+}
+
+int run_product(ham_fp8_weight *w, const void *x_codes, const void *x_scales, int32_t rows, void *out,
+                void *out_scales, int f32, void *stream) {
+  int dev = 0;
+  cudaGetDevice(&dev);
+  if (dev != w->device) cudaSetDevice(w->device);
+  ProductArgs a{};
+  a.w = w->codes;
+  a.ws = w->scales;
+  a.xs = static_cast<const uint8_t *>(x_scales);
+  a.out = out;
+  a.out_scales = static_cast<uint8_t *>(out_scales);
+  a.err = w->err;
+  a.rows = rows;
+  a.n = w->n;
+  a.kbs = w->kbs;
+  a.sk = w->sk;
+  a.out_sk = fp8_scale_bytes(w->n);
+  a.tiles = w->tiles;
+  a.f32 = f32;
+  const int64_t tiles = (int64_t)((rows + 255) / 256) * (w->parts == 2 ? w->tiles : (w->tiles + 1) / 2);
+  const bool pair = rows > 128 && tiles * 2 >= device_sms();
+  a.nt = std::min(128, (rows + 15) / 16 * 16);
+  CUtensorMap tx;
+  int rc = HAM_OK;
+  if (make_bytes_tensor_map(&tx, x_codes, rows, w->k, kFp8Block, pair ? 128 : a.nt, true) != 0) {
+    rc = op_fail(HAM_ECUDA, "tensor map of the rows");
+  } else {
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const cudaError_t e = pair ? (w->parts == 2 ? launch_pair<true>(tx, w->map, a, w->device, s)
+                                                : launch_pair<false>(tx, w->map, a, w->device, s))
+                               : (w->parts == 2 ? launch_stream<2>(tx, a, w->device, s)
+                                                : launch_stream<1>(tx, a, w->device, s));
+    if (e != cudaSuccess) rc = op_fail(HAM_ECUDA, "product launch: %s", cudaGetErrorString(e));
+  }
+  if (dev != w->device) cudaSetDevice(dev);
+  return rc;
+}
+
+int check_product(const ham_fp8_weight *w, const void *xc, const void *xs, int32_t rows, const void *out) {
+  if (!w) return op_fail(HAM_EINVAL, "null handle");
+  if (rows < 0 || rows > (1 << 24)) return op_fail(HAM_EINVAL, "rows %d outside 0..2^24", rows);
+  if (rows == 0) return HAM_OK;
+  if (!xc || !xs || !out) return op_fail(HAM_EINVAL, "codes, scales and the output are required");
+  if (!op_aligned(xc, 16) || !op_aligned(out, 16) || !op_aligned(xs, 4))
+    return op_fail(HAM_EINVAL, "codes and the output must be 16-byte aligned, scales 4-byte aligned");
+  return HAM_OK;
+}
+
+}  // namespace
+}  // namespace ham
+
+using ham::op_aligned;
+using ham::op_fail;
+using ham::op_overlap;
+
+extern "C" {
+
+int ham_fp8_weight_free(ham_fp8_weight *w) {
+  if (!w) return HAM_OK;
+  int dev = 0;
+  cudaGetDevice(&dev);
+  cudaSetDevice(w->device);
+  cudaFree(w->codes);
+  cudaFree(w->scales);
+  cudaFree(w->err);
+  cudaFreeHost(w->host_err);
+  cudaSetDevice(dev);
+  delete w;
+  return HAM_OK;
+}
+
+int ham_fp8_weight_alloc(int32_t n, int32_t k, const void *codes, const void *scales, const void *codes_up,
+                         const void *scales_up, ham_fp8_weight **out) {
+  if (!out) return op_fail(HAM_EINVAL, "out is required");
+  *out = nullptr;
+  if (n < 1 || n > (1 << 22)) return op_fail(HAM_EINVAL, "n %d outside 1..2^22", n);
+  if (k < 16 || k % 16 != 0 || k > (1 << 20)) return op_fail(HAM_EINVAL, "k %d must be a multiple of 16 in 16..2^20", k);
+  if (!codes || !scales) return op_fail(HAM_EINVAL, "codes and scales are required");
+  if (!codes_up != !scales_up) return op_fail(HAM_EINVAL, "codes_up and scales_up come together");
+  if (codes_up && n % 16 != 0) return op_fail(HAM_EINVAL, "n %d of a gated weight must be a multiple of 16", n);
+  for (const void *p : {codes, codes_up})
+    if (!op_aligned(p, 16)) return op_fail(HAM_EINVAL, "codes must be 16-byte aligned");
+  ham_fp8_weight *w = new (std::nothrow) ham_fp8_weight();
+  if (!w) return op_fail(HAM_ENOMEM, "host allocation failed");
+  w->n = n;
+  w->k = k;
+  w->parts = codes_up ? 2 : 1;
+  w->tiles = (n + ham::kTile - 1) / ham::kTile;
+  w->kbs = (k + ham::kFp8Block - 1) / ham::kFp8Block;
+  w->sk = ham::fp8_scale_bytes(k);
+  cudaGetDevice(&w->device);
+  const int64_t blocks = (int64_t)w->tiles * w->kbs;
+  if (blocks * w->parts * 128 > INT32_MAX) {
+    delete w;
+    return op_fail(HAM_EUNSUPPORTED, "weight of %d x %d is too large", n, k);
+  }
+  cudaError_t e = cudaMalloc(reinterpret_cast<void **>(&w->codes), (size_t)blocks * w->parts * ham::kBlockBytes);
+  if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void **>(&w->scales), (size_t)w->tiles * w->parts * w->sk);
+  if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void **>(&w->err), 4);
+  if (e == cudaSuccess) e = cudaMallocHost(reinterpret_cast<void **>(&w->host_err), 4);
+  if (e != cudaSuccess) {
+    cudaGetLastError();
+    ham_fp8_weight_free(w);
+    return op_fail(HAM_ENOMEM, "weight of %d x %d: %s", n, k, cudaGetErrorString(e));
+  }
+  const int64_t pieces = blocks * (ham::kBlockBytes / 16);
+  for (int p = 0; p < w->parts && e == cudaSuccess; ++p) {
+    ham::lay_out_weight_kernel<<<(unsigned)((pieces + 255) / 256), 256>>>(
+        static_cast<const uint8_t *>(p ? codes_up : codes), n, k, p, w->parts, w->kbs, pieces, w->codes);
+    e = cudaGetLastError();
+    if (e != cudaSuccess) break;
+    ham::lay_out_scales_kernel<<<(unsigned)((w->tiles * w->sk + 255) / 256), 256>>>(
+        static_cast<const uint8_t *>(p ? scales_up : scales), w->tiles, w->sk, p, w->parts, w->scales);
+    e = cudaGetLastError();
+  }
+  if (e == cudaSuccess) e = cudaMemset(w->err, 0, 4);
+  if (e == cudaSuccess) e = cudaDeviceSynchronize();
+  if (e != cudaSuccess || ham::make_bytes_tensor_map(&w->map, w->codes, blocks * w->parts * 128, 128, 128, 128,
+                                                     false) != 0) {
+    cudaGetLastError();
+    ham_fp8_weight_free(w);
+    return op_fail(HAM_ECUDA, "weight layout: %s", cudaGetErrorString(e));
+  }
+  *out = w;
+  return HAM_OK;
+}
+
+int ham_fp8_linear(ham_fp8_weight *w, const void *x_codes, const void *x_scales, int32_t rows, void *out,
+                   int32_t out_dtype, void *stream) {
+  ham::ApiRange nvtx_range("ham_fp8_linear");
+  int rc = ham::check_product(w, x_codes, x_scales, rows, out);
+  if (rc) return rc;
+  if (w->parts != 1) return op_fail(HAM_EINVAL, "a gated weight serves ham_fp8_gated");
+  if (out_dtype != HAM_DTYPE_BF16 && out_dtype != HAM_DTYPE_F32) return op_fail(HAM_EINVAL, "out_dtype %d", out_dtype);
+  if (rows == 0) return HAM_OK;
+  const int f32 = out_dtype == HAM_DTYPE_F32;
+  const size_t ob = (size_t)rows * w->n * (f32 ? 4 : 2);
+  if (op_overlap(out, ob, x_codes, (size_t)rows * w->k) || op_overlap(out, ob, x_scales, (size_t)rows * w->sk))
+    return op_fail(HAM_EINVAL, "out must not overlap the input rows");
+  return ham::run_product(w, x_codes, x_scales, rows, out, nullptr, f32, stream);
+}
+
+int ham_fp8_gated(ham_fp8_weight *w, const void *x_codes, const void *x_scales, int32_t rows, void *codes,
+                  void *scales, void *stream) {
+  ham::ApiRange nvtx_range("ham_fp8_gated");
+  int rc = ham::check_product(w, x_codes, x_scales, rows, codes);
+  if (rc) return rc;
+  if (w->parts != 2) return op_fail(HAM_EINVAL, "ham_fp8_gated takes a gated weight (gate and up)");
+  if (rows == 0) return HAM_OK;
+  if (!scales || !op_aligned(scales, 4)) return op_fail(HAM_EINVAL, "the output's scales are required, 4-byte aligned");
+  const size_t ob = (size_t)rows * w->n, sb = (size_t)rows * ham::fp8_scale_bytes(w->n);
+  const size_t xb = (size_t)rows * w->k, xsb = (size_t)rows * w->sk;
+  if (op_overlap(codes, ob, x_codes, xb) || op_overlap(codes, ob, x_scales, xsb) ||
+      op_overlap(scales, sb, x_codes, xb) || op_overlap(scales, sb, x_scales, xsb) || op_overlap(codes, ob, scales, sb))
+    return op_fail(HAM_EINVAL, "inputs and outputs must not overlap");
+  return ham::run_product(w, x_codes, x_scales, rows, codes, scales, 0, stream);
+}
+
+int ham_fp8_weight_status(ham_fp8_weight *w, void *stream, int32_t *device_code) {
+  if (!w) return op_fail(HAM_EINVAL, "null handle");
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaError_t ce = cudaMemcpyAsync(w->host_err, w->err, 4, cudaMemcpyDeviceToHost, s);
+  if (ce == cudaSuccess) ce = cudaMemsetAsync(w->err, 0, 4, s);
+  if (ce == cudaSuccess) ce = cudaStreamSynchronize(s);
+  if (ce != cudaSuccess) return op_fail(HAM_ECUDA, "status read: %s", cudaGetErrorString(ce));
+  if (device_code) *device_code = *w->host_err;
+  if (*w->host_err != 0) return op_fail(HAM_EDEVICE, "device error word = %d", *w->host_err);
+  return HAM_OK;
+}
+
+}  // extern "C"

@@ -15,6 +15,7 @@
 #include <vector>
 
 #include "ham_internal.cuh"
+#include "ham_ops.cuh"
 #include "ham_front.cuh"
 #include "ham_micro.cuh"
 #include "ham_prefill.cuh"
@@ -461,6 +462,20 @@ int make_fp8_v_tensor_map(CUtensorMap *map, const void *v_codes, int64_t rows_d,
                      strides, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
                      CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+
+int make_bytes_tensor_map(CUtensorMap *map, const void *base, int64_t rows, int64_t cols,
+                          int box_cols, int box_rows, bool swizzle) {
+  EncodeTiled encode = tensor_map_encoder();
+  if (!encode) return -1;
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)cols};  // bytes of a row
+  const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
+  const cuuint32_t estride[2] = {1, 1};
+  return (int)encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims,
+                     strides, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                     swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
 int make_pool_tensor_map(CUtensorMap *map, const void *pool, int64_t rows, int head_dim) {

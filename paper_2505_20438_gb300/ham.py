@@ -101,6 +101,15 @@ _SIGNATURES = {
     "ham_prefill": [_vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _i32, _vp],
     "ham_qkv_append": [_vp, _i32, _vp, _vp, _i32, _vp, _vp, _vp, _vp],
     "ham_micro_step": [_vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp],
+    "ham_add_norm": [_vp, _vp, _vp, ctypes.c_float, _i32, _i32, _vp, _vp, _vp, _vp, _vp],
+    "ham_fp8_encode": [_vp, _i32, _i32, _vp, _vp, _vp],
+    "ham_fp8_encode_weight": [_vp, _i32, _i32, _vp, _vp, _vp],
+    "ham_fp8_weight_alloc": [_i32, _i32, _vp, _vp, _vp, _vp, ctypes.POINTER(_vp)],
+    "ham_fp8_weight_free": [_vp],
+    "ham_fp8_linear": [_vp, _vp, _vp, _i32, _vp, _i32, _vp],
+    "ham_fp8_gated": [_vp, _vp, _vp, _i32, _vp, _vp, _vp],
+    "ham_fp8_weight_status": [_vp, _vp, ctypes.POINTER(_i32)],
+    "ham_sample": [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp],
 }
 _lib = None
 
@@ -151,7 +160,8 @@ _raw_stream = None  # () -> the current device's current stream, as an integer
 
 def _load_dtypes():
     import torch
-    _dtypes.update(bf16=torch.bfloat16, f32=torch.float32, i32=torch.int32, i64=torch.int64)
+    _dtypes.update(bf16=torch.bfloat16, f32=torch.float32, i32=torch.int32, i64=torch.int64,
+                   u8=torch.uint8)
     return _dtypes
 
 
@@ -542,3 +552,131 @@ def ham_embedder_status(e: Embedder, stream=None) -> int:
     if rc not in (HAM_OK, HAM_EDEVICE):
         _check(rc)
     return code.value
+
+
+# ---------------------------------------------------------------------------------------
+# what follows the attention: norm, 8-bit products, the choice of a token
+# ---------------------------------------------------------------------------------------
+
+def fp8_scale_bytes(k: int) -> int:
+    """Scale bytes of an 8-bit row of k elements (one a block of 128, padded to whole words)."""
+    return 4 * (-(-k // 512))
+
+
+def ham_add_norm(x, weight, eps, residual=None, sum_out=None, out=None, codes=None, scales=None,
+                 stream=None):
+    """Residual addition and root-mean-square norm of x [T][H] (bf16): sum_out = x + residual, out
+    and / or (codes, scales) the normed rows in bf16 / in 8 bits."""
+    T, H = x.shape if x is not None and x.dim() == 2 else (0, 0)
+    _check(lib().ham_add_norm(
+        _dev(x, (T, H), "bf16", "x"), _dev(residual, (T, H), "bf16", "residual", nullable=True),
+        _dev(weight, (H,), "bf16", "weight"), eps, T, H,
+        _dev(sum_out, (T, H), "bf16", "sum_out", nullable=True),
+        _dev(out, (T, H), "bf16", "out", nullable=True),
+        _dev(codes, (T, H), "u8", "codes", nullable=True),
+        _dev(scales, (T, fp8_scale_bytes(H)), "u8", "scales", nullable=True), _stream_ptr(stream)))
+
+
+def ham_fp8_encode(x, codes, scales, stream=None):
+    """bf16 rows x [T][K] -> codes uint8 [T][K], scales uint8 [T][fp8_scale_bytes(K)]."""
+    T, K = x.shape if x is not None and x.dim() == 2 else (0, 0)
+    _check(lib().ham_fp8_encode(
+        _dev(x, (T, K), "bf16", "x"), T, K, _dev(codes, (T, K), "u8", "codes"),
+        _dev(scales, (T, fp8_scale_bytes(K)), "u8", "scales"), _stream_ptr(stream)))
+
+
+def ham_fp8_encode_weight(w, codes, scales, stream=None):
+    """bf16 weight w [N][K] -> codes uint8 [N][K], block scales uint8
+    [ceil(N / 128)][fp8_scale_bytes(K)]."""
+    N, K = w.shape if w is not None and w.dim() == 2 else (0, 0)
+    _check(lib().ham_fp8_encode_weight(
+        _dev(w, (N, K), "bf16", "w"), N, K, _dev(codes, (N, K), "u8", "codes"),
+        _dev(scales, (-(-N // 128), fp8_scale_bytes(K)), "u8", "scales"), _stream_ptr(stream)))
+
+
+class Fp8Weight:
+    """Owning handle of one weight laid out for the 8-bit products (ham_fp8_weight*)."""
+
+    def __init__(self, ptr: int, n: int, k: int, gated: bool):
+        self.ptr, self.n, self.k, self.gated = ptr, n, k, gated
+
+    @property
+    def _as_parameter_(self):
+        return ctypes.c_void_p(self.ptr)
+
+    def close(self):
+        if self.ptr:
+            ham_fp8_weight_free(self)
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def ham_fp8_weight_alloc(n, k, codes, scales, codes_up=None, scales_up=None) -> Fp8Weight:
+    """codes uint8 [n][k] and scales uint8 [ceil(n / 128)][fp8_scale_bytes(k)] on the GPU (copied);
+    with codes_up and scales_up a gated weight (codes the gate's projection)."""
+    import torch
+    shape, sshape = (n, k), (-(-n // 128), fp8_scale_bytes(k))
+    out = ctypes.c_void_p()
+    args = (_dev(codes, shape, "u8", "codes"), _dev(scales, sshape, "u8", "scales"),
+            _dev(codes_up, shape, "u8", "codes_up", nullable=True),
+            _dev(scales_up, sshape, "u8", "scales_up", nullable=True))
+    torch.cuda.current_stream().synchronize()   # (the copy runs on the legacy default stream)
+    _check(lib().ham_fp8_weight_alloc(n, k, *args, ctypes.byref(out)))
+    return Fp8Weight(out.value, n, k, codes_up is not None)
+
+
+def ham_fp8_weight_free(w: Fp8Weight):
+    ptr, w.ptr = w.ptr, 0
+    _check(lib().ham_fp8_weight_free(ctypes.c_void_p(ptr)))
+
+
+def ham_fp8_linear(w: Fp8Weight, x_codes, x_scales, out, stream=None):
+    """out [T][n] = X W^T for 8-bit rows X [T][k].  Output dtype follows `out` (bf16 or fp32)."""
+    import torch
+    T = x_codes.shape[0] if x_codes is not None and x_codes.dim() == 2 else 0
+    f32 = out is not None and out.dtype is torch.float32
+    _check(lib().ham_fp8_linear(
+        w, _dev(x_codes, (T, w.k), "u8", "x_codes"),
+        _dev(x_scales, (T, fp8_scale_bytes(w.k)), "u8", "x_scales"), T,
+        _dev(out, (T, w.n), "f32" if f32 else "bf16", "out"),
+        HAM_DTYPE_F32 if f32 else HAM_DTYPE_BF16, _stream_ptr(stream)))
+
+
+def ham_fp8_gated(w: Fp8Weight, x_codes, x_scales, codes, scales, stream=None):
+    """8-bit rows (codes [T][n], scales) of silu(X W_gate^T) * (X W_up^T) for 8-bit rows X [T][k]."""
+    T = x_codes.shape[0] if x_codes is not None and x_codes.dim() == 2 else 0
+    _check(lib().ham_fp8_gated(
+        w, _dev(x_codes, (T, w.k), "u8", "x_codes"),
+        _dev(x_scales, (T, fp8_scale_bytes(w.k)), "u8", "x_scales"), T,
+        _dev(codes, (T, w.n), "u8", "codes"),
+        _dev(scales, (T, fp8_scale_bytes(w.n)), "u8", "scales"), _stream_ptr(stream)))
+
+
+def ham_fp8_weight_status(w: Fp8Weight, stream=None) -> int:
+    """Device error code (HAM_DEVERR_*), read and cleared; does not raise on HAM_EDEVICE."""
+    code = ctypes.c_int32(0)
+    rc = lib().ham_fp8_weight_status(w, _stream_ptr(stream), ctypes.byref(code))
+    if rc not in (HAM_OK, HAM_EDEVICE):
+        _check(rc)
+    return code.value
+
+
+def ham_sample(logits, u, tokens, temperature=None, top_k=None, top_p=None, min_p=None, probs=None,
+               stream=None):
+    """tokens int32 [B] (and probs fp32 [B]) chosen from logits [B][V] (bf16 or fp32) with the given
+    random numbers u fp32 [B]; temperature, top_p, min_p fp32 [B] and top_k int32 [B] are optional."""
+    import torch
+    B, V = logits.shape if logits is not None and logits.dim() == 2 else (0, 0)
+    f32 = logits is not None and logits.dtype is torch.float32
+    row = (B,)
+    _check(lib().ham_sample(
+        _dev(logits, (B, V), "f32" if f32 else "bf16", "logits"),
+        HAM_DTYPE_F32 if f32 else HAM_DTYPE_BF16, B, V, _dev(u, row, "f32", "u"),
+        _dev(temperature, row, "f32", "temperature", nullable=True),
+        _dev(top_k, row, "i32", "top_k", nullable=True), _dev(top_p, row, "f32", "top_p", nullable=True),
+        _dev(min_p, row, "f32", "min_p", nullable=True), _dev(tokens, row, "i32", "tokens"),
+        _dev(probs, row, "f32", "probs", nullable=True), _stream_ptr(stream)))
