@@ -10,20 +10,22 @@
 // Sums are of whole numbers, so that neither the order of the additions nor the launch's shape can
 // change an answer.  Weights are below one part in 2^31 of the likeliest token's where they are 0.
 //
-// A row is held in the shared memory of a cluster of CTAs and read from global memory once.  Nothing is
-// sorted.  A histogram over 2048 bins of (max - l) / T, which grows as the order goes on, of counts (for
-// top-k) or of weights (top-p alone) finds the bin in which the order is cut; every CTA sums its share
-// of the bins over the cluster, so that this costs two cluster barriers.  Then
+// A row is held in the shared memory of a cluster of CTAs and read from global memory once.  A row is
+// never sorted.  A histogram over 512 bins of (max - l) / T, which grows as the order goes on, of counts
+// (for top-k) or of counts and weights (top-p alone) finds the bin in which the order is cut: every CTA
+// adds up the cluster's histograms for itself, 16 bytes a load, so that this costs one cluster barrier
+// (of 2048 bins, added up by shares and read back, it took 8500 cycles against 3000).  Then
 //  - where at most 2048 tokens lie up to that bin (the usual case) they are listed, in index order, in
-//    the first CTA's shared memory, and that CTA makes the exact cuts, ranking only the tokens of the
-//    cuts' bins against one another, and picks the token;
-//  - otherwise the cluster goes on as a whole: histograms over 2048 parts of the bin, then over the
+//    the first CTA's shared memory, and that CTA makes the exact cuts, sorting only the tokens of the
+//    cuts' bins, and picks the token;
+//  - otherwise the cluster goes on as a whole: histograms over 512 parts of the bin, then over the
 //    values of l in the part until one is left, whose equal tokens are kept by index; then the sums of
 //    the kept weights by stretches of the index.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "ham_mx.cuh"
@@ -33,12 +35,12 @@ namespace ham {
 namespace {
 
 constexpr int kSampleThreads = 512, kSampleWarps = kSampleThreads / 32;
-constexpr int kBins = 2048;
+constexpr int kBins = 512;
 constexpr int kList = 2048;             // tokens that one CTA ranks by itself
 constexpr float kFine = 2147483648.f;   // 2^31
 constexpr float kLeast = -21.49f;       // below -31 log 2 = -21.4876 a weight is 0
-constexpr float kBinsPerX = 95.25f;     // bins of x = (l - max) / T: 2047 reach beyond kLeast
-constexpr float kLastBin = 2047.f;
+constexpr float kLastBin = 511.f;
+constexpr float kBinsPerX = 23.78f;     // bins of x = (l - max) / T: 511 reach to -21.4886
 constexpr int kSampleMaxVocab = 1 << 18;
 constexpr int kMaxCluster = 8;           // (8 CTAs hold the largest vocabulary in fp32)
 constexpr int kSampleSmem = 220 * 1024, kSampleSmem2 = 112 * 1024;  // one and two CTAs an SM
@@ -52,21 +54,24 @@ struct SampleArgs {
   int vocab, slice;       // elements of a CTA, a multiple of 8
 };
 
-struct Histogram { uint32_t count[kBins], low[kBins], high[kBins]; };  // weight = high 2^16 + low
+// Weights are added in two halves (weight = high 2^16 + low): at most 2^16 tokens of a CTA keep each
+// half's sum within 32 bits.
+struct __align__(16) Histogram { uint32_t count[kBins], low[kBins], high[kBins]; };
 
-// What a CTA shares with its cluster beside the logits and the running sums of its share of the bins.
+// What a CTA shares with its cluster beside the logits.
 struct SampleShared {
   Histogram h;
   float list_l[kList];                    // first CTA: the listed tokens, by index
   int32_t list_i[kList];
+  uint32_t list_w[kList];
   uint64_t total_mass, warp_mass[kSampleWarps];
-  uint32_t total_count, warp_count[kSampleWarps];
+  uint32_t warp_count[kSampleWarps];
   float best, warp_best[kSampleWarps];
   uint32_t key_max, key_min, warp_max[kSampleWarps], warp_min[kSampleWarps];
   uint64_t kept, warp_kept[kSampleWarps];
   uint32_t ties, warp_ties[kSampleWarps];
   int first;                              // first index of the largest logit
-  uint64_t found_before_mass, found_mass;
+  uint64_t found_before_mass, found_mass, aim;
   uint32_t found_before_count, found_count;
   int found, members;
 };
@@ -82,94 +87,179 @@ __device__ __forceinline__ uint32_t key_of(float l) {
 }
 // A row's temperature, and x = (l - best) / t rounded to nearest as a division is: with r the rounded
 // reciprocal of t, q = a r and its remainder a - q t (exact in a fused multiply-add), q + rem r rounds
-// to the quotient (Markstein, IBM J. Res. Dev. 34, 1990), in the range where nothing underflows.
+// to the quotient (Markstein, IBM J. Res. Dev. 34, 1990).  Where a step leaves fp32's range the weight
+// is right all the same: an x that underflows is one whose exponential is 1, an overflow makes x NaN or
+// -inf, and both weigh 0.  Rows with an infinite largest logit or an extreme t divide instead.
 struct Scale {
   float best, t, r, bins;   // bins = kBinsPerX / t
-  bool plain;               // t within 2^-60 .. 2^60
+  bool plain;
 };
 __device__ __forceinline__ Scale scale_of(float best, float t) {
-  return Scale{best, t, __frcp_rn(t), __fdiv_rn(kBinsPerX, t), t > 0x1p-60f && t < 0x1p60f};
+  return Scale{best, t, __frcp_rn(t), __fdiv_rn(kBinsPerX, t), t > 0x1p-60f && t < 0x1p60f && best < INFINITY};
 }
 __device__ __forceinline__ float x_of(float l, const Scale &c) {
-  if (l == c.best) return 0.f;
   const float a = __fsub_rn(l, c.best);
-  if (!c.plain || a > -0x1p-30f || a < -0x1p30f) return __fdiv_rn(a, c.t);
-  const float q = __fmul_rn(a, c.r);
-  return __fmaf_rn(__fmaf_rn(-q, c.t, a), c.r, q);
+  if (c.plain) {
+    const float q = __fmul_rn(a, c.r);
+    return __fmaf_rn(__fmaf_rn(-q, c.t, a), c.r, q);
+  }
+  return l == c.best ? 0.f : __fdiv_rn(a, c.t);
 }
 __device__ __forceinline__ uint32_t weight_of(float x) {
-  return x >= kLeast ? (uint32_t)(expf(x) * kFine) : 0u;
+  const uint32_t w = (uint32_t)(expf(x) * kFine);
+  return x >= kLeast ? w : 0u;
 }
 // Where l lies in the order, in bins (the fraction: the part of the bin); it grows as l falls, so bins
 // and parts follow the order.  From kLastBin on weights are 0 and the token is left out.
 __device__ __forceinline__ float place_of(float l, const Scale &c) {
-  return l == c.best ? 0.f : __fmul_rn(__fsub_rn(c.best, l), c.bins);
+  const float f = __fmul_rn(__fsub_rn(c.best, l), c.bins);
+  return c.plain || l != c.best ? f : 0.f;
 }
 __device__ __forceinline__ bool has_bin(float place) { return place < kLastBin; }
 __device__ __forceinline__ int part_of(float place, int bin) { return (int)((place - (float)bin) * (float)kBins); }
 
 __device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t a) {
   uint32_t v;
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a));
   return v;
 }
 __device__ __forceinline__ uint64_t ld_cluster_u64(uint32_t a) {
   uint64_t v;
-  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a) : "memory");
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a));
   return v;
 }
 __device__ __forceinline__ void st_cluster_u32(uint32_t a, uint32_t v) {
   asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory");
 }
+__device__ __forceinline__ uint4 ld_cluster_u32x4(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+  return v;
+}
 template <typename T>
 __device__ __forceinline__ uint32_t peer(const T *p, int rank) { return cluster_map_shared(smem_u32(p), (uint32_t)rank); }
 
-// Where the order is cut (depth 0: not at all): kept are the tokens of bins before b1, of b1 those of
-// parts before b2, and of that part all (depth 2) or those with keys above `key` and the first `ties`
-// by index of the ones equal to it (depth 3).
+// Where the order is cut: kept are the tokens whose place is below `end` (a part is 2^-9 of a bin, so
+// that an end between parts is a number of 18 bits), or, with `by_value`, those with logits above
+// `value` and the first `ties` by index of the ones equal to it.
 struct Cut {
-  int depth = 0, b1 = 0, b2 = 0;
-  uint32_t key = 0, ties = 0;
+  float end = INFINITY, value = -INFINITY;
+  bool by_value = false, by_index = false;  // by_index: some of the equal tokens are cut off
+  uint32_t ties = 0;
   uint64_t mass = 0;       // weight of what is kept
-  bool by_index = false;   // some of the equal tokens are cut off
 };
 
-// Inclusive running sums over the block's threads, in thread order, of a count and a weight; the
-// block's sums in `count_all`, `mass_all`.
-__device__ __forceinline__ void block_scan(SampleShared &s, uint32_t &count, uint64_t &mass, uint32_t &count_all,
-                                           uint64_t &mass_all) {
+// Inclusive running sums of a weight over the block's threads, in thread order; `all`: their sum.
+__device__ __forceinline__ uint64_t block_scan(SampleShared &s, uint64_t mass, uint64_t &all) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const uint32_t c = __shfl_up_sync(kFull, count, o);
     const uint64_t m = __shfl_up_sync(kFull, mass, o);
-    if (lane >= o) count += c, mass += m;
+    if (lane >= o) mass += m;
   }
-  __syncthreads();                               // (the arrays' last readers are done)
-  if (lane == 31) s.warp_count[warp] = count, s.warp_mass[warp] = mass;
+  __syncthreads();                               // (the array's last readers are done)
+  if (lane == 31) s.warp_mass[warp] = mass;
   __syncthreads();
-  count_all = 0, mass_all = 0;
+  all = 0;
 #pragma unroll
   for (int q = 0; q < kSampleWarps; ++q) {
-    if (q == warp) count += count_all, mass += mass_all;
-    count_all += s.warp_count[q], mass_all += s.warp_mass[q];
+    if (q == warp) mass += all;
+    all += s.warp_mass[q];
   }
+  return mass;
 }
+
+// A warp's view of one value of each CTA of the cluster: lane q holds that of CTA q (0 past them).
+__device__ __forceinline__ uint32_t sum8(uint32_t v) { return __reduce_add_sync(kFull, v); }
+__device__ __forceinline__ uint64_t sum8(uint64_t v) {
+#pragma unroll
+  for (int o = 4; o > 0; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
+  return __shfl_sync(kFull, v, 0);
+}
+
+// A vector of 16 bytes of logits.
+template <typename T>
+struct Vec {
+  static constexpr int kN = 16 / (int)sizeof(T);
+  float l[kN];
+  __device__ __forceinline__ explicit Vec(const uint4 &v) {
+    const T *e = reinterpret_cast<const T *>(&v);
+#pragma unroll
+    for (int j = 0; j < kN; ++j) l[j] = load_logit(e + j);
+  }
+  // A vector of ruled-out logits.
+  static __device__ __forceinline__ uint4 none() {
+    const uint32_t v = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+    return make_uint4(v, v, v, v);
+  }
+  // The vector with NaN as -inf and -0 as 0; `best`: the largest logit so far.
+  static __device__ __forceinline__ uint4 clean_of(const uint4 &v, float &best) {
+    uint4 o;
+    const T *e = reinterpret_cast<const T *>(&v);
+    T *d = reinterpret_cast<T *>(&o);
+#pragma unroll
+    for (int j = 0; j < kN; ++j) {
+      const float f = clean(load_logit(e + j));
+      best = fmaxf(best, f);
+      if constexpr (sizeof(T) == 4) d[j] = f;
+      else d[j] = (T)(__float_as_uint(f) >> 16);
+    }
+    return o;
+  }
+};
 
 template <typename T>
 struct Row {
+  static constexpr int kN = Vec<T>::kN;
   SampleShared &s;
-  uint64_t *run_mass;      // running sums of this CTA's share of the bins
-  uint32_t *run_count;
-  const T *data;           // this CTA's logits
-  int begin, n, ctas, rank, tid;
+  uint4 *data;             // this CTA's logits, cleaned (-inf before and after them)
+  int first_index;         // index of the first vector's first element
+  int vecs, ctas, rank, tid;
   Scale c;
 
   __device__ void sync() const {
     if (ctas > 1) cluster_sync_all();
     else __syncthreads();
   }
-  __device__ __forceinline__ float logit(int i) const { return clean(load_logit(data + i)); }
+  template <typename V>
+  __device__ __forceinline__ uint32_t lane32(const V *p) const {
+    const int q = tid & 31;
+    return q < ctas ? ld_cluster_u32(peer(p, q)) : 0u;
+  }
+  __device__ __forceinline__ uint64_t lane64(const uint64_t *p) const {
+    const int q = tid & 31;
+    return q < ctas ? ld_cluster_u64(peer(p, q)) : 0ull;
+  }
+  // f(vector) for every vector of this CTA's logits, in any order.
+  template <typename F>
+  __device__ __forceinline__ void each(F f) const {
+#pragma unroll 2
+    for (int v = tid; v < vecs; v += kSampleThreads) f(Vec<T>(data[v]));
+  }
+  // The histogram of the logits in range by the bins of `where` (negative: left out), counts and / or
+  // weights.  Computed for the whole vector first: a vector's chains of arithmetic overlap.
+  template <bool kCounts, bool kMasses, typename W>
+  __device__ __forceinline__ void histogram(W where) const {
+    each([&](const Vec<T> &x) {
+      int bin[kN];
+      uint32_t w[kN];
+#pragma unroll
+      for (int j = 0; j < kN; ++j) {
+        bin[j] = where(x.l[j]);
+        if (kMasses) w[j] = weight_of(x_of(x.l[j], c));
+      }
+#pragma unroll
+      for (int j = 0; j < kN; ++j)
+        if (bin[j] >= 0) {
+          if (kCounts) atomicAdd(&s.h.count[bin[j]], 1u);
+          if (kMasses) add_mass(bin[j], w[j]);
+        }
+    });
+  }
+  __device__ __forceinline__ int bin_of(float l) const {
+    const float f = place_of(l, c);
+    return has_bin(f) ? (int)f : -1;
+  }
   __device__ void clear() const {
     for (int i = tid; i < kBins; i += kSampleThreads) s.h.count[i] = s.h.low[i] = s.h.high[i] = 0;
     __syncthreads();
@@ -178,92 +268,77 @@ struct Row {
     if (w & 0xffffu) atomicAdd(&s.h.low[bin], w & 0xffffu);
     if (w >> 16) atomicAdd(&s.h.high[bin], w >> 16);
   }
-  __device__ __forceinline__ void add(int bin, uint32_t w) const {
-    atomicAdd(&s.h.count[bin], 1u);
-    add_mass(bin, w);
-  }
+  // The share of a row's weight that top-p reaches for: whole numbers from here on (a sum reaches the
+  // fp64 product if it reaches the whole number above).
+  static __device__ uint64_t aim_of(double p, uint64_t mass) { return (uint64_t)ceil(fmax(p * (double)mass, 1.)); }
   // The first bin at which the running count (or weight) of the whole row's histogram, begun at the
-  // given sums, reaches the aim (aim_p > 0: that share of the row's weight, at least 1); s.found (-1:
-  // none), its own and the earlier sums.  All CTAs of the cluster call it.
-  __device__ void find(bool by_mass, uint64_t count0, uint64_t mass0, uint64_t aim_count, double aim_mass,
-                       double aim_p = 0.) const {
+  // given sums, reaches the aim (p > 0: the aim is that share of the row's weight, left in s.aim);
+  // s.found (-1: none), its own and the earlier sums.  All CTAs of the cluster call it; the histograms
+  // must stand until their next barrier.
+  __device__ void find(bool by_mass, bool masses, uint32_t count0, uint64_t mass0, uint64_t aim, double p = 0.) const {
     sync();                                      // every CTA's histogram is complete
-    const int share = kBins / ctas, per = (share + kSampleThreads - 1) / kSampleThreads;
-    uint32_t cn[4], cs = 0, ca;
-    uint64_t m[4], ms = 0, ma;
+    constexpr int kThreads = kBins / 4;          // four bins a thread
+    static_assert(kThreads % 32 == 0 && kThreads <= kSampleThreads, "threads");
+    const int lane = tid & 31, warp = tid >> 5;
+    uint32_t c4[4], c_sum = 0, ci = 0;
+    uint64_t m4[4], m_sum = 0, mi = 0;
+    if (tid < kThreads) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      cn[j] = 0, m[j] = 0;
-      const int i = tid * per + j;
-      if (j < per && i < share) {
-        const int bin = rank * share + i;
-        uint64_t hi = 0, lo = 0;
-#pragma unroll 4
-        for (int q = 0; q < ctas; ++q) {
-          cn[j] += ld_cluster_u32(peer(&s.h.count[bin], q));
-          hi += ld_cluster_u32(peer(&s.h.high[bin], q));
-          lo += ld_cluster_u32(peer(&s.h.low[bin], q));
+      for (int j = 0; j < 4; ++j) c4[j] = 0, m4[j] = 0;
+      const uint32_t at_c = smem_u32(&s.h.count[tid * 4]), at_h = smem_u32(&s.h.high[tid * 4]);
+      const uint32_t at_l = smem_u32(&s.h.low[tid * 4]);
+#pragma unroll
+      for (int q = 0; q < kMaxCluster; ++q)
+        if (q < ctas) {
+          const uint4 v = ld_cluster_u32x4(cluster_map_shared(at_c, q));
+          c4[0] += v.x, c4[1] += v.y, c4[2] += v.z, c4[3] += v.w;
         }
-        m[j] = (hi << 16) + lo;
-      }
-      cs += cn[j], ms += m[j];
-    }
-    uint32_t cb = cs;
-    uint64_t mb = ms;
-    block_scan(s, cb, mb, ca, ma);
-    cb -= cs, mb -= ms;
+      if (masses) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int i = tid * per + j;
-      cb += cn[j], mb += m[j];
-      if (j < per && i < share) run_count[i] = cb, run_mass[i] = mb;
-    }
-    if (tid == 0) {
-      s.total_count = ca, s.total_mass = ma;
-      s.found = -1;
-    }
-    sync();                                      // every CTA's running sums are complete
-    uint32_t qc[kMaxCluster];
-    uint64_t qm[kMaxCluster], all = 0;
+        for (int q = 0; q < kMaxCluster; ++q)
+          if (q < ctas) {
+            const uint4 v = ld_cluster_u32x4(cluster_map_shared(at_h, q)), w = ld_cluster_u32x4(cluster_map_shared(at_l, q));
+            m4[0] += ((uint64_t)v.x << 16) + w.x, m4[1] += ((uint64_t)v.y << 16) + w.y;
+            m4[2] += ((uint64_t)v.z << 16) + w.z, m4[3] += ((uint64_t)v.w << 16) + w.w;
+          }
+      }
 #pragma unroll
-    for (int q = 0; q < kMaxCluster; ++q) {
-      qc[q] = 0, qm[q] = 0;
-      if (q < ctas) {
-        qc[q] = ld_cluster_u32(peer(&s.total_count, q));
-        qm[q] = ld_cluster_u64(peer(&s.total_mass, q));
-      }
-      all += qm[q];
-    }
-    if (aim_p > 0.) aim_mass = fmax(aim_p * (double)all, 1.);
-    uint64_t base_c = count0, base_m = mass0;
-    int at = -1;
+      for (int j = 0; j < 4; ++j) c_sum += c4[j], m_sum += m4[j];
+      ci = c_sum, mi = m_sum;
 #pragma unroll
-    for (int q = 0; q < kMaxCluster; ++q) {
-      if (at < 0 && q < ctas) {
-        if (by_mass ? (double)(base_m + qm[q]) >= aim_mass : base_c + qc[q] >= aim_count) at = q;
-        else base_c += qc[q], base_m += qm[q];
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t c = __shfl_up_sync(kFull, ci, o);
+        const uint64_t m = __shfl_up_sync(kFull, mi, o);
+        if (lane >= o) ci += c, mi += m;
       }
+      if (lane == 31) s.warp_count[warp] = ci, s.warp_mass[warp] = mi;
+      if (tid == 0) s.found = -1;
     }
-    if (at >= 0)
-      for (int i = tid; i < share; i += kSampleThreads) {
-        const uint64_t c1 = base_c + ld_cluster_u32(peer(&run_count[i], at));
-        const uint64_t m1 = base_m + ld_cluster_u64(peer(&run_mass[i], at));
-        const uint64_t c0 = i ? base_c + ld_cluster_u32(peer(&run_count[i - 1], at)) : base_c;
-        const uint64_t m0 = i ? base_m + ld_cluster_u64(peer(&run_mass[i - 1], at)) : base_m;
-        const bool after = by_mass ? (double)m1 >= aim_mass : c1 >= aim_count;
-        const bool before = by_mass ? !((double)m0 >= aim_mass) : c0 < aim_count;
-        if (after && before) {
-          s.found = at * share + i;
-          s.found_before_count = (uint32_t)c0, s.found_before_mass = m0;
-          s.found_count = (uint32_t)(c1 - c0), s.found_mass = m1 - m0;
-        }
-      }
     __syncthreads();
-  }
-  __device__ uint64_t whole_mass() const {       // after a find
-    uint64_t all = 0;
-    for (int q = 0; q < ctas; ++q) all += ld_cluster_u64(peer(&s.total_mass, q));
-    return all;
+    if (tid < kThreads) {
+      uint32_t run_c = count0 + ci - c_sum;
+      uint64_t run_m = mass0 + mi - m_sum, all = 0;
+#pragma unroll
+      for (int q = 0; q < kThreads / 32; ++q) {
+        const uint64_t m = s.warp_mass[q];
+        if (q < warp) run_c += s.warp_count[q], run_m += m;
+        all += m;
+      }
+      if (p > 0.) aim = aim_of(p, all);
+      if (tid == 0) s.total_mass = all, s.aim = aim;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t c1 = run_c + c4[j];
+        const uint64_t m1 = run_m + m4[j];
+        if ((by_mass ? m1 : c1) >= aim && (by_mass ? run_m : run_c) < aim) {
+          s.found = tid * 4 + j;
+          s.found_before_count = run_c, s.found_before_mass = run_m;
+          s.found_count = c4[j], s.found_mass = m4[j];
+        }
+        run_c = c1, run_m = m1;
+      }
+    }
+    __syncthreads();
   }
   // Largest and smallest key (of the row) among this CTA's kmax / kmin.
   __device__ void key_range(uint32_t &kmax, uint32_t &kmin) const {
@@ -276,69 +351,60 @@ struct Row {
       s.key_max = kmax, s.key_min = kmin;
     }
     sync();
-    for (int q = 0; q < ctas; ++q) {
-      const uint32_t a = ld_cluster_u32(peer(&s.key_max, q)), b = ld_cluster_u32(peer(&s.key_min, q));
-      kmax = q ? max(kmax, a) : a;
-      kmin = q ? min(kmin, b) : b;
-    }
+    kmax = __reduce_max_sync(kFull, lane32(&s.key_max));
+    kmin = __reduce_min_sync(kFull, (tid & 31) < ctas ? lane32(&s.key_min) : 0xffffffffu);
     sync();                                      // (read before the next call writes them)
   }
   // The exact cut within the bin that find() gave for the aim, by the whole cluster.
-  __device__ Cut cut(bool by_mass, uint64_t aim_count, double aim_mass) const {
+  __device__ Cut cut(bool by_mass, uint64_t aim) const {
     Cut k;
-    k.depth = 2, k.b1 = s.found;
-    uint64_t count = s.found_before_count, mass = s.found_before_mass;
-    __syncthreads();                             // (before the histogram's next use)
-    sync();
+    const int b1 = s.found;
+    uint32_t count = s.found_before_count;
+    uint64_t mass = s.found_before_mass;
+    sync();                                      // (before the histogram's next use)
     clear();                                     // parts of the bin
-    for (int i = tid; i < n; i += kSampleThreads) {
-      const float l = logit(i), f = place_of(l, c);
-      if (has_bin(f) && (int)f == k.b1) add(part_of(f, k.b1), weight_of(x_of(l, c)));
-    }
-    __syncthreads();
-    find(by_mass, count, mass, aim_count, aim_mass);
-    k.b2 = s.found;
+    histogram<true, true>([&](float l) {
+      const float f = place_of(l, c);
+      return has_bin(f) && (int)f == b1 ? part_of(f, b1) : -1;
+    });
+    find(by_mass, true, count, mass, aim);
+    const int b2 = s.found;
+    k.end = (float)b1 + (float)(b2 + 1) * (1.f / kBins);
     k.mass = s.found_before_mass + s.found_mass;
     count = s.found_before_count, mass = s.found_before_mass;
-    if (s.found_count == 1 || (!by_mass && count + s.found_count == aim_count)) return k;
+    if (s.found_count == 1 || (!by_mass && count + s.found_count == aim)) return k;
     // values of l within the part, until one is left
+    const float begin = (float)b1 + (float)b2 * (1.f / kBins);
     uint32_t lo = 0, hi = 0xffffffffu;
     for (;;) {
       uint32_t kmax = 0, kmin = 0xffffffffu;
-      for (int i = tid; i < n; i += kSampleThreads) {
-        const float l = logit(i), f = place_of(l, c);
-        if (has_bin(f) && (int)f == k.b1 && part_of(f, k.b1) == k.b2) {
-          const uint32_t key = key_of(l);
-          if (key >= lo && key <= hi) kmax = max(kmax, key), kmin = min(kmin, key);
+      each([&](const Vec<T> &x) {
+#pragma unroll
+        for (int j = 0; j < kN; ++j) {
+          const float f = place_of(x.l[j], c);
+          const uint32_t key = key_of(x.l[j]);
+          if (f >= begin && f < k.end && key >= lo && key <= hi) kmax = max(kmax, key), kmin = min(kmin, key);
         }
-      }
+      });
       key_range(kmax, kmin);
       int shift = 0;
       while (((kmax - kmin) >> shift) >= (uint32_t)kBins) ++shift;
       clear();
-      for (int i = tid; i < n; i += kSampleThreads) {
-        const float l = logit(i), f = place_of(l, c);
-        if (has_bin(f) && (int)f == k.b1 && part_of(f, k.b1) == k.b2) {
-          const uint32_t key = key_of(l);
-          if (key >= kmin && key <= kmax) add((int)((kmax - key) >> shift), weight_of(x_of(l, c)));
-        }
-      }
-      __syncthreads();
-      find(by_mass, count, mass, aim_count, aim_mass);
+      histogram<true, true>([&](float l) {
+        const float f = place_of(l, c);
+        const uint32_t key = key_of(l);
+        return f >= begin && f < k.end && key >= kmin && key <= kmax ? (int)((kmax - key) >> shift) : -1;
+      });
+      find(by_mass, true, count, mass, aim);
       count = s.found_before_count, mass = s.found_before_mass;
       const uint32_t bin = (uint32_t)s.found;
       if (shift == 0) {                          // one value, held by s.found_count tokens
-        k.depth = 3, k.key = kmax - bin;
+        const uint32_t key = kmax - bin;
         const uint64_t many = s.found_count, w = s.found_mass / many;
-        uint64_t keep = many;
-        if (!by_mass) {
-          keep = aim_count - count;
-        } else if (w > 0) {
-          const double want = ceil((aim_mass - (double)mass) / (double)w);
-          keep = want < 1. ? 1 : want > (double)many ? many : (uint64_t)want;
-          while (keep > 1 && (double)(mass + (keep - 1) * w) >= aim_mass) --keep;
-          while (keep < many && (double)(mass + keep * w) < aim_mass) ++keep;
-        }
+        // (by weight: the fewest whose weights reach the aim; the bin's own do, so w > 0)
+        const uint64_t keep = by_mass ? (aim - mass + w - 1) / w : aim - count;
+        k.by_value = true;
+        k.value = __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xffffffffu));
         k.ties = (uint32_t)keep;
         k.by_index = keep < many;
         k.mass = mass + keep * w;
@@ -349,188 +415,190 @@ struct Row {
       lo = kmax - kmin < down ? kmin : kmax - down;
     }
   }
-  // Weight of logit i if the cut and min_p keep it (tie: it is one of the cut's equal tokens, of which
-  // the caller keeps the first by index).
-  __device__ __forceinline__ uint32_t kept(const Cut &k, double least, int i, bool &tie) const {
-    const float l = logit(i), f = place_of(l, c);
-    tie = false;
-    if (!has_bin(f)) return 0;
-    if (k.depth > 0) {
-      const int b = (int)f;
-      if (b > k.b1) return 0;
-      if (b == k.b1) {
-        const int part = part_of(f, b);
-        if (part > k.b2) return 0;
-        if (part == k.b2 && k.depth > 2) {
-          const uint32_t key = key_of(l);
-          if (key < k.key) return 0;
-          tie = k.by_index && key == k.key;
-        }
-      }
+  // Weights of a vector's logits that the cut and min_p keep (tie: one of the cut's equal tokens, of
+  // which the caller keeps the first by index).
+  __device__ __forceinline__ void kept(const Cut &k, uint32_t least, const Vec<T> &x, uint32_t (&w)[kN],
+                                       bool (&tie)[kN]) const {
+#pragma unroll
+    for (int j = 0; j < kN; ++j) {
+      const float l = x.l[j];
+      w[j] = weight_of(x_of(l, c));
+      const bool in = k.by_value ? l >= k.value : !(place_of(l, c) >= k.end);
+      if (!in || w[j] < least) w[j] = 0;
+      tie[j] = k.by_index && l == k.value;
     }
-    const uint32_t w = weight_of(x_of(l, c));
-    return (double)w < least ? 0 : w;
   }
-  // The warps' stretches of the slice, in index order.
-  __device__ __forceinline__ void stretch(int &i0, int &i1) const {
-    const int each = (n + kSampleWarps * 32 - 1) / (kSampleWarps * 32) * 32;
-    i0 = min(n, (tid >> 5) * each);
-    i1 = min(n, i0 + each);
+  // The warps' stretches of the vectors, in index order: a step is 32 vectors, one a lane.
+  __device__ __forceinline__ void stretch(int &v0, int &v1) const {
+    const int per = (vecs + kSampleWarps * 32 - 1) / (kSampleWarps * 32) * 32;
+    v0 = min(vecs, (tid >> 5) * per);
+    v1 = min(vecs, v0 + per);
+  }
+  // Sum over the warps before this one, and over the CTAs before this one, of a number a warp (all:
+  // over the row).
+  __device__ uint32_t before_me(uint32_t mine, uint32_t &all) const {
+    const int lane = tid & 31, warp = tid >> 5;
+    if (lane == 0) s.warp_ties[warp] = mine;
+    __syncthreads();
+    const uint32_t v = lane < kSampleWarps ? s.warp_ties[lane] : 0u;
+    const uint32_t cta = sum8(v), warps = sum8(lane < warp ? v : 0u);
+    if (tid == 0) s.ties = cta;
+    sync();
+    const uint32_t q = lane32(&s.ties);
+    all = sum8(q);
+    return warps + sum8(lane < rank ? q : 0u);
   }
   // Lists the tokens up to bin `last` in the first CTA, by index, if they are at most kList; their
   // number over the row.
   __device__ uint32_t list(int last) const {
-    const int lane = tid & 31, warp = tid >> 5;
+    const int lane = tid & 31;
     const float end = (float)(last + 1);         // (last < 2047: a token up to it has a bin)
-    int i0, i1;
-    stretch(i0, i1);
-    uint32_t many = 0;
-    for (int i = i0 + lane; i < i1; i += 32) many += place_of(logit(i), c) < end;
+    int v0, v1;
+    stretch(v0, v1);
+    uint32_t many = 0, all;
+#pragma unroll 2
+    for (int v = v0 + lane; v < v1; v += 32) {
+      const Vec<T> x(data[v]);
+#pragma unroll
+      for (int j = 0; j < kN; ++j) many += place_of(x.l[j], c) < end;
+    }
     many = __reduce_add_sync(kFull, many);
-    if (lane == 0) s.warp_ties[warp] = many;
-    __syncthreads();
-    if (tid == 0) {
-      uint32_t all = 0;
-      for (int q = 0; q < kSampleWarps; ++q) all += s.warp_ties[q];
-      s.ties = all;
-    }
-    sync();
-    uint32_t at = 0, all = 0;
-    for (int q = 0; q < ctas; ++q) {
-      const uint32_t v = ld_cluster_u32(peer(&s.ties, q));
-      if (q < rank) at += v;
-      all += v;
-    }
+    uint32_t at = before_me(many, all);
     if (all > (uint32_t)kList) return all;
-    for (int q = 0; q < warp; ++q) at += s.warp_ties[q];
     if (many) {
-      const uint32_t to_l = peer(s.list_l, 0), to_i = peer(s.list_i, 0);
-      for (int i = i0; i < i1; i += 32) {
-        const float l = i + lane < i1 ? logit(i + lane) : -INFINITY;
-        const bool in = i + lane < i1 && place_of(l, c) < end;
-        const uint32_t who = __ballot_sync(kFull, in);
-        if (in) {
-          const uint32_t to = at + __popc(who & ((1u << lane) - 1u));
-          st_cluster_u32(to_l + 4 * to, __float_as_uint(l));
-          st_cluster_u32(to_i + 4 * to, (uint32_t)(begin + i + lane));
+      const uint32_t to_l = peer(s.list_l, 0), to_i = peer(s.list_i, 0), below = (1u << lane) - 1u;
+      for (int v = v0; v < v1; v += 32) {
+        const Vec<T> x(v + lane < v1 ? data[v + lane] : Vec<T>::none());
+        bool in[kN], any = false;
+#pragma unroll
+        for (int j = 0; j < kN; ++j) in[j] = place_of(x.l[j], c) < end, any |= in[j];
+        if (!__any_sync(kFull, any)) continue;
+        uint32_t mine = at, step = 0;
+#pragma unroll
+        for (int j = 0; j < kN; ++j) {
+          const uint32_t who = __ballot_sync(kFull, in[j]);
+          mine += __popc(who & below);
+          step += __popc(who);
         }
-        at += __popc(who);
+#pragma unroll
+        for (int j = 0; j < kN; ++j)
+          if (in[j]) {
+            st_cluster_u32(to_l + 4 * mine, __float_as_uint(x.l[j]));
+            st_cluster_u32(to_i + 4 * mine, (uint32_t)(first_index + (v + lane) * kN + j));
+            ++mine;
+          }
+        at += step;
       }
     }
     sync();
     return all;
   }
+  // Sorts the first `many` of the 64-bit keys where the logits were (ascending; a bitonic network).
+  __device__ void sort(uint64_t *key, int many) const {
+    int n = 32;
+    while (n < many) n *= 2;
+    for (int i = many + tid; i < n; i += kSampleThreads) key[i] = ~0ull;
+    __syncthreads();
+    for (int size = 2; size <= n; size *= 2)
+      for (int step = size / 2; step > 0; step /= 2) {
+        for (int q = tid; q < n / 2; q += kSampleThreads) {
+          const int i = 2 * q - (q & (step - 1)), o = i + step;
+          const uint64_t x = key[i], y = key[o];
+          if ((x > y) == ((i & size) == 0)) key[i] = y, key[o] = x;
+        }
+        if (n <= 64) __syncwarp();               // (the first warp's own)
+        else __syncthreads();
+      }
+    __syncthreads();
+  }
   // The choice among the first CTA's list of `all` tokens (up to bin `last`), by that CTA alone.
   // k > 0: top-k cuts in bin `last`, before which the list holds `before` tokens.  p >= 0: top-p, of the
   // weight `row_mass` (0: of the list's, after top-k).
   __device__ void choose(const SampleArgs &a, int row, uint32_t all, int last, uint32_t before, int k, double p,
-                         uint64_t row_mass, double least) const {
+                         uint64_t row_mass, uint32_t least) const {
     constexpr int kPer = kList / kSampleThreads;
+    uint64_t *key = reinterpret_cast<uint64_t *>(data);  // (the logits are not needed any more)
     // each thread: kPer neighbouring tokens of the list
-    float l[kPer];
     uint32_t w[kPer];
     int bin[kPer];
-    uint32_t *members = s.h.count;               // (the histogram's counts are not needed here)
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
       const uint32_t i = tid * kPer + j;
-      l[j] = i < all ? s.list_l[i] : -INFINITY;
-      bin[j] = i < all ? (int)place_of(l[j], c) : kBins;
-      w[j] = i < all ? weight_of(x_of(l[j], c)) : 0;
+      const float l = i < all ? s.list_l[i] : -INFINITY;
+      bin[j] = i < all ? (int)place_of(l, c) : kBins;
+      w[j] = i < all ? weight_of(x_of(l, c)) : 0;
     }
-    // the bin's tokens that `which` picks, listed in any order: each then counts those before it
-    auto collect = [&](int b, auto which) {
-      __syncthreads();
+    s.h.low[tid] = s.h.high[tid] = 0;
+    // the keys of bin b's tokens with any weight, in order: by l, largest first, equal ones by place in
+    // the list
+    auto in_order = [&](int b) {
       if (tid == 0) s.members = 0;
       __syncthreads();
 #pragma unroll
       for (int j = 0; j < kPer; ++j)
-        if (bin[j] == b && which(j)) members[atomicAdd(&s.members, 1)] = tid * kPer + j;
-      __syncthreads();
-    };
-    auto earlier = [&](uint32_t o, float lo, uint32_t i, float li) { return lo > li || (lo == li && o < i); };
-    if (k > 0 && all > (uint32_t)k) {            // of bin `last`, the first k - before
-      collect(last, [](int) { return true; });
-      const int m = s.members;
-#pragma unroll
-      for (int j = 0; j < kPer; ++j)
-        if (bin[j] == last) {
-          uint32_t rank_in = 0;
-          for (int q = 0; q < m; ++q) {
-            const uint32_t o = members[q];
-            rank_in += earlier(o, s.list_l[o], tid * kPer + j, l[j]);
-          }
-          if (before + rank_in >= (uint32_t)k) w[j] = 0;
+        if (bin[j] == b && w[j]) {
+          const uint32_t i = tid * kPer + j;
+          key[atomicAdd(&s.members, 1)] = ((uint64_t)~key_of(s.list_l[i]) << 32) | i;
         }
+      __syncthreads();
+      const int m = s.members;
+      sort(key, m);
+      return m;
+    };
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) s.list_w[tid * kPer + j] = w[j];
+    if (k > 0 && all > (uint32_t)k) {            // of bin `last`, the first k - before
+      const int m = in_order(last);
+      for (int i = tid; i < m; i += kSampleThreads)
+        if (before + i >= (uint32_t)k) s.list_w[(uint32_t)key[i]] = 0;
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) w[j] = s.list_w[tid * kPer + j];
     }
-    uint64_t mass = 0;
+    uint64_t mass = 0, whole = row_mass;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) mass += w[j];
-    uint32_t none = 0, none_all;
-    uint64_t sum = mass, whole;
-    block_scan(s, none, sum, none_all, whole);
     if (p >= 0.) {
-      const double aim = fmax(p * (double)(row_mass ? row_mass : whole), 1.);
-      for (int i = tid; i < kBins; i += kSampleThreads) s.h.low[i] = s.h.high[i] = 0;
-      if (tid == 0) s.found = -1;
+      if (!row_mass) block_scan(s, mass, whole);
+      if (tid == 0) s.aim = aim_of(p, whole);
       __syncthreads();
+      const uint64_t aim = s.aim;
 #pragma unroll
       for (int j = 0; j < kPer; ++j)
         if (w[j]) add_mass(bin[j], w[j]);
       __syncthreads();
-      uint64_t m[kBins / kSampleThreads], ms = 0;
-#pragma unroll
-      for (int j = 0; j < kBins / kSampleThreads; ++j) {
-        const int b = tid * (kBins / kSampleThreads) + j;
-        m[j] = ((uint64_t)s.h.high[b] << 16) + s.h.low[b];
-        ms += m[j];
-      }
-      uint64_t run = ms, run_all;
-      block_scan(s, none, run, none_all, run_all);
-      run -= ms;
-#pragma unroll
-      for (int j = 0; j < kBins / kSampleThreads; ++j) {
-        if (!((double)run >= aim) && (double)(run + m[j]) >= aim) {
-          s.found = tid * (kBins / kSampleThreads) + j;
-          s.found_before_mass = run;
-        }
-        run += m[j];
+      const uint64_t m = ((uint64_t)s.h.high[tid] << 16) + s.h.low[tid];  // a thread a bin
+      uint64_t run_all;
+      const uint64_t run = block_scan(s, m, run_all);
+      if (run >= aim && run - m < aim) {         // (one thread: the list's weights reach the aim)
+        s.found = tid;
+        s.found_before_mass = run - m;
       }
       __syncthreads();
       const int b = s.found;
-      const uint64_t mass0 = s.found_before_mass;
-      collect(b, [&](int j) { return w[j] > 0; });
-      const int many = s.members;
-      uint32_t gone = 0;
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) {
-        if (bin[j] == b && w[j]) {
-          uint64_t run_in = mass0;
-          for (int q = 0; q < many; ++q) {
-            const uint32_t o = members[q];
-            const float lo = s.list_l[o];
-            if (earlier(o, lo, tid * kPer + j, l[j])) run_in += weight_of(x_of(lo, c));
-          }
-          if ((double)run_in >= aim) gone |= 1u << j;
-        } else if (bin[j] > b) {
-          gone |= 1u << j;
-        }
+      uint64_t at = s.found_before_mass;
+      const int many = in_order(b);
+      for (int i0 = 0; i0 < many; i0 += kSampleThreads) {
+        const uint32_t i = i0 + tid < many ? (uint32_t)key[i0 + tid] : 0u, v = i0 + tid < many ? s.list_w[i] : 0u;
+        uint64_t part;
+        const uint64_t upto = at + block_scan(s, v, part);
+        if (v && upto - v >= aim) s.list_w[i] = 0;
+        at += part;
       }
+      __syncthreads();
 #pragma unroll
-      for (int j = 0; j < kPer; ++j)
-        if (gone >> j & 1u) w[j] = 0;
+      for (int j = 0; j < kPer; ++j) w[j] = bin[j] > b ? 0 : s.list_w[tid * kPer + j];
     }
     mass = 0;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-      if ((double)w[j] < least) w[j] = 0;
+      if (w[j] < least) w[j] = 0;
       mass += w[j];
     }
-    sum = mass;
-    block_scan(s, none, sum, none_all, whole);
-    const double u = fmin(fmax((double)a.u[row], 0.), 1.);   // (a NaN becomes 0)
-    uint64_t aim = (uint64_t)floor(u * (double)whole);
-    if (aim >= whole) aim = whole - 1;
+    uint64_t sum = block_scan(s, mass, whole);
+    if (tid == 0) s.aim = pick(a.u[row], whole);
+    __syncthreads();
+    const uint64_t aim = s.aim;
     sum -= mass;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
@@ -541,12 +609,16 @@ struct Row {
       sum += w[j];
     }
   }
+  // floor(u S), below S
+  static __device__ uint64_t pick(float u, uint64_t whole) {
+    const double v = fmin(fmax((double)u, 0.), 1.);  // (a NaN becomes 0)
+    const uint64_t aim = (uint64_t)floor(v * (double)whole);
+    return aim >= whole ? whole - 1 : aim;
+  }
 };
 
-// Bytes of shared memory before the logits: SampleShared and the running sums of a share of the bins.
-__host__ __device__ constexpr int sample_fixed(int ctas) {
-  return (int)(sizeof(SampleShared) + 15) / 16 * 16 + kBins / ctas * 12;
-}
+constexpr int kSampleFixed = (int)(sizeof(SampleShared) + 15) / 16 * 16;  // shared memory before the logits
+static_assert(kBins == kSampleThreads, "a thread a bin");
 
 template <typename T>
 __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a) {
@@ -554,9 +626,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
   SampleShared &s = *reinterpret_cast<SampleShared *>(smem_raw);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int ctas = gridDim.x, rank = blockIdx.x, row = blockIdx.y;
-  uint64_t *run_mass = reinterpret_cast<uint64_t *>(smem_raw + (sizeof(SampleShared) + 15) / 16 * 16);
-  uint32_t *run_count = reinterpret_cast<uint32_t *>(run_mass + kBins / ctas);
-  T *store = reinterpret_cast<T *>(smem_raw + sample_fixed(ctas));
+  uint4 *store = reinterpret_cast<uint4 *>(smem_raw + kSampleFixed);
   const int begin = min(a.vocab, rank * a.slice), n = min(a.vocab, begin + a.slice) - begin;
   for (int i = tid; i < kBins; i += kSampleThreads) s.h.count[i] = s.h.low[i] = s.h.high[i] = 0;
   grid_dependency_wait();
@@ -564,194 +634,201 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
   const float temperature = a.temperature ? a.temperature[row] : 1.f;
   const int k = a.top_k ? a.top_k[row] : 0;
   const float p = a.top_p ? a.top_p[row] : 1.f;
+  const float min_p = a.min_p ? a.min_p[row] : 0.f;
   // ---- the row's slice to shared memory at its own 16-byte phase, and the largest logit
   const T *src = static_cast<const T *>(a.logits) + (int64_t)row * a.vocab + begin;
-  constexpr int kVec = 16 / (int)sizeof(T), kAtOnce = 8;
+  constexpr int kVec = Vec<T>::kN, kAtOnce = 8;
   const int phase = (int)(((uintptr_t)src & 15u) / sizeof(T));
-  T *data = store + phase;
+  const int vecs = n > 0 ? (phase + n + kVec - 1) / kVec : 0;
+  const int whole0 = phase ? 1 : 0, whole1 = (phase + n) / kVec;   // vectors inside the slice
+  const uint4 *from = reinterpret_cast<const uint4 *>(src - phase);  // (read from whole0 on)
   float best = -INFINITY;
-  const int head = min(n, phase ? kVec - phase : 0), vecs = (n - head) / kVec;
-  const uint4 *from = reinterpret_cast<const uint4 *>(src + head);
-  uint4 *to = reinterpret_cast<uint4 *>(data + head);
-  for (int i0 = tid; i0 < vecs; i0 += kAtOnce * kSampleThreads) {
+  for (int i0 = whole0 + tid; i0 < whole1; i0 += kAtOnce * kSampleThreads) {
     uint4 v[kAtOnce];
 #pragma unroll
     for (int j = 0; j < kAtOnce; ++j)
-      if (i0 + j * kSampleThreads < vecs) v[j] = __ldcs(from + i0 + j * kSampleThreads);
+      if (i0 + j * kSampleThreads < whole1) v[j] = __ldcs(from + i0 + j * kSampleThreads);
 #pragma unroll
     for (int j = 0; j < kAtOnce; ++j)
-      if (i0 + j * kSampleThreads < vecs) {
-        to[i0 + j * kSampleThreads] = v[j];
-        const T *e = reinterpret_cast<const T *>(&v[j]);
-#pragma unroll
-        for (int q = 0; q < kVec; ++q) best = fmaxf(best, load_logit(e + q));  // (fmaxf passes over NaN)
+      if (i0 + j * kSampleThreads < whole1) {
+        store[i0 + j * kSampleThreads] = Vec<T>::clean_of(v[j], best);
       }
   }
-  for (int j = tid; j < n - vecs * kVec; j += kSampleThreads) {  // the ends
-    const int i = j < head ? j : j + vecs * kVec;
-    data[i] = src[i];
-    best = fmaxf(best, load_logit(src + i));
+  if (tid < 2 * kVec) {                          // the first and the last vector, where they stick out
+    const int v = tid < kVec ? 0 : vecs - 1, i = v * kVec + tid % kVec - phase;
+    if (vecs > 0 && (v < whole0 || v >= whole1)) {
+      const float x = i >= 0 && i < n ? clean(load_logit(src + i)) : -INFINITY;
+      best = fmaxf(best, x);
+      T *to = reinterpret_cast<T *>(store) + v * kVec + tid % kVec;
+      if constexpr (sizeof(T) == 4) *to = x;
+      else *to = (T)(__float_as_uint(x) >> 16);
+    }
   }
   best = warp_max_f32(best);
   if (lane == 0) s.warp_best[warp] = best;
   __syncthreads();
-  for (int q = 0; q < kSampleWarps; ++q) best = fmaxf(best, s.warp_best[q]);
+  best = warp_max_f32(lane < kSampleWarps ? s.warp_best[lane] : -INFINITY);
   if (tid == 0) s.best = best;
-  Row<T> r{s, run_mass, run_count, data, begin, n, ctas, rank, tid, Scale{}};
+  Row<T> r{s, store, begin - phase, vecs, ctas, rank, tid, Scale{}};
   r.sync();
-  for (int q = 0; q < ctas; ++q) best = fmaxf(best, __uint_as_float(ld_cluster_u32(peer(&s.best, q))));
-  best = clean(best);
+  best = warp_max_f32(lane < ctas ? __uint_as_float(r.lane32(&s.best)) : -INFINITY);
   const bool greedy = !(temperature > 0.f);
   r.c = scale_of(best, greedy ? 1.f : temperature);
   if (best == -INFINITY || greedy) {             // (the same in every CTA of the cluster)
     int first = INT32_MAX;
     if (best != -INFINITY)
-      for (int i = tid; i < n && first == INT32_MAX; i += kSampleThreads)
-        if (r.logit(i) == best) first = begin + i;
+      for (int v = tid; v < vecs && first == INT32_MAX; v += kSampleThreads) {
+        const Vec<T> x(store[v]);
+#pragma unroll
+        for (int j = kVec - 1; j >= 0; --j)
+          if (x.l[j] == best) first = r.first_index + v * kVec + j;
+      }
     first = __reduce_min_sync(kFull, first);
     if (lane == 0) s.warp_ties[warp] = (uint32_t)first;
     __syncthreads();
-    if (tid == 0) {
-      for (int q = 1; q < kSampleWarps; ++q) first = min(first, (int)s.warp_ties[q]);
-      s.first = first;
-    }
+    first = __reduce_min_sync(kFull, lane < kSampleWarps ? (int)s.warp_ties[lane] : INT32_MAX);
+    if (tid == 0) s.first = first;
     r.sync();
-    if (rank == 0 && tid == 0) {
-      for (int q = 0; q < ctas; ++q) first = min(first, (int)ld_cluster_u32(peer(&s.first, q)));
+    if (rank == 0 && warp == 0) {
+      first = __reduce_min_sync(kFull, lane < ctas ? (int)r.lane32(&s.first) : INT32_MAX);
       const bool none = best == -INFINITY;
-      a.tokens[row] = none ? -1 : first;
-      if (a.probs) a.probs[row] = none ? 0.f : 1.f;
+      if (lane == 0) {
+        a.tokens[row] = none ? -1 : first;
+        if (a.probs) a.probs[row] = none ? 0.f : 1.f;
+      }
     }
     r.sync();
     return;
   }
   const bool by_k = k > 0 && k < a.vocab, by_p = p < 1.f;
   const double share = by_p ? fmax((double)p, 0x1p-80) : 1.;  // (at least the likeliest token)
-  const double least = (a.min_p ? (double)fminf(a.min_p[row], 1.f) : 0.) * (double)kFine;
+  // w >= min_p 2^31 for whole w (the product is exact in fp32): at least the whole number above
+  const uint32_t least = min_p > 0.f ? (uint32_t)ceilf(fminf(min_p, 1.f) * kFine) : 0u;
   Cut cut;
   if (by_k || by_p) {
-    // counts if top-k comes first, else weights
-#pragma unroll 4
-    for (int i = tid; i < n; i += kSampleThreads) {
-      const float l = r.logit(i), f = place_of(l, r.c);
-      if (has_bin(f)) {
-        if (by_k) atomicAdd(&s.h.count[(int)f], 1u);
-        else r.add_mass((int)f, weight_of(x_of(l, r.c)));
-      }
-    }
-    __syncthreads();
-    r.find(!by_k, 0, 0, (uint64_t)k, 0., share);
-    // (fewer than k tokens have any weight: the last bin closes the list)
-    const int last = s.found < 0 ? kBins - 2 : s.found;
-    const uint32_t before = s.found < 0 ? 0 : s.found_before_count;
-    const bool all_in = s.found < 0;
-    const uint64_t whole = r.whole_mass();
-    const uint32_t all = r.list(last);
+    const auto bins = [&](float l) { return r.bin_of(l); };
+    if (by_k) r.template histogram<true, false>(bins);   // counts if top-k comes first
+    else r.template histogram<true, true>(bins);
+    r.find(!by_k, !by_k, 0, 0, (uint64_t)k, by_k ? 0. : share);
+    const bool all_in = s.found < 0;             // fewer than k tokens have any weight
+    const int last = all_in ? kBins - 2 : s.found;
+    const uint32_t before = all_in ? 0 : s.found_before_count;
+    const uint64_t whole = by_k ? 0 : s.total_mass;
+    uint64_t aim = s.aim;
+    const uint32_t all = all_in ? kList : before + s.found_count;
     if (all <= (uint32_t)kList) {
-      if (rank == 0) r.choose(a, row, all, last, before, by_k && !all_in ? k : 0, by_p ? share : -1.,
-                              by_k ? 0 : whole, least);
-      return;                                    // (no shared memory of a peer is read from here on)
-    }
-    double aim = fmax(share * (double)whole, 1.);
-    auto histogram = [&](bool counts) {
-      r.sync();
-      r.clear();
-      for (int i = tid; i < n; i += kSampleThreads) {
-        const float l = r.logit(i), f = place_of(l, r.c);
-        if (!has_bin(f)) continue;
-        if (counts) atomicAdd(&s.h.count[(int)f], 1u);
-        r.add_mass((int)f, weight_of(x_of(l, r.c)));
+      const uint32_t listed = r.list(last);
+      if (listed <= (uint32_t)kList) {           // (all_in: known only now)
+        if (rank == 0) r.choose(a, row, listed, last, before, by_k && !all_in ? k : 0, by_p ? share : -1., whole, least);
+        return;                                  // (no shared memory of a peer is read from here on)
       }
-      __syncthreads();
-    };
+    }
     if (by_k) {
       if (by_p) {                                // (top-p wants the weight that top-k keeps)
-        histogram(true);
-        r.find(false, 0, 0, (uint64_t)k, 0.);
+        r.sync();
+        r.clear();
+        r.template histogram<true, true>(bins);
+        r.find(false, true, 0, 0, (uint64_t)k);
       }
-      if (!all_in) cut = r.cut(false, (uint64_t)k, 0.);
+      if (!all_in) cut = r.cut(false, (uint64_t)k);
       if (by_p) {
-        aim = fmax(share * (double)(all_in ? r.whole_mass() : cut.mass), 1.);
-        histogram(false);
-        r.find(true, 0, 0, 0, aim);
+        aim = Row<T>::aim_of(share, all_in ? s.total_mass : cut.mass);
+        r.sync();
+        r.clear();
+        r.template histogram<true, true>(bins);
+        r.find(true, true, 0, 0, aim);
       }
     }
-    if (by_p) cut = r.cut(true, 0, aim);
+    if (by_p) cut = r.cut(true, aim);
   }
   // ---- the kept weights of each warp's stretch of the slice, in index order
-  int i0, i1;
-  r.stretch(i0, i1);
+  int v0, v1;
+  r.stretch(v0, v1);
   uint32_t ties_before = 0;
   if (cut.by_index) {
-    uint32_t ties = 0;
-    for (int i = i0 + lane; i < i1; i += 32) {
-      bool tie;
-      r.kept(cut, least, i, tie);
-      ties += tie;
+    uint32_t ties = 0, all;
+    for (int v = v0 + lane; v < v1; v += 32) {
+      const Vec<T> x(store[v]);
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) ties += x.l[j] == cut.value;
     }
     ties = __reduce_add_sync(kFull, ties);
     r.sync();                                    // (s.ties: its last readers are done)
-    if (lane == 0) s.warp_ties[warp] = ties;
-    __syncthreads();
-    if (tid == 0) {
-      uint32_t all = 0;
-      for (int q = 0; q < kSampleWarps; ++q) all += s.warp_ties[q];
-      s.ties = all;
-    }
-    r.sync();
-    for (int q = 0; q < rank; ++q) ties_before += ld_cluster_u32(peer(&s.ties, q));
-    for (int q = 0; q < warp; ++q) ties_before += s.warp_ties[q];
+    ties_before = r.before_me(ties, all);
   }
-  // one step of 32 tokens: this lane's kept weight (ties: those before this step)
-  auto step = [&](int i, uint32_t &ties) -> uint32_t {
-    bool tie = false;
-    uint32_t w = i < i1 ? r.kept(cut, least, i, tie) : 0u;
+  // one step of 32 vectors: this lane's kept weights (ties: those before this step)
+  auto step = [&](int v, uint32_t &ties, uint32_t (&w)[kVec]) {
+    const Vec<T> x(v < v1 ? store[v] : Vec<T>::none());
+    bool tie[kVec];
+    r.kept(cut, least, x, w, tie);
     if (cut.by_index) {
-      const uint32_t all = __ballot_sync(kFull, tie);
-      if (tie && ties + __popc(all & ((1u << lane) - 1u)) >= cut.ties) w = 0;
-      ties += __popc(all);
+      uint32_t mine = ties;
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) {
+        const uint32_t who = __ballot_sync(kFull, tie[j]);
+        mine += __popc(who & ((1u << lane) - 1u));
+        ties += __popc(who);
+      }
+#pragma unroll
+      for (int j = 0; j < kVec; ++j)
+        if (tie[j] && mine++ >= cut.ties) w[j] = 0;
     }
-    return w;
   };
   uint64_t sum = 0;
   uint32_t ties = ties_before;
-#pragma unroll 4
-  for (int i = i0; i < i1; i += 32) sum += step(i + lane, ties);
+  for (int v = v0; v < v1; v += 32) {
+    uint32_t w[kVec];
+    step(v + lane, ties, w);
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) sum += w[j];
+  }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kFull, sum, o);
   if (lane == 0) s.warp_kept[warp] = sum;
   __syncthreads();
-  if (tid == 0) {
-    uint64_t all = 0;
-    for (int q = 0; q < kSampleWarps; ++q) all += s.warp_kept[q];
-    s.kept = all;
+  uint64_t warps = 0, cta = 0;
+#pragma unroll
+  for (int q = 0; q < kSampleWarps; ++q) {
+    const uint64_t v = s.warp_kept[q];
+    if (q < warp) warps += v;
+    cta += v;
   }
+  if (tid == 0) s.kept = cta;
   r.sync();
-  uint64_t before = 0, total = 0;
-  for (int q = 0; q < ctas; ++q) {
-    const uint64_t v = ld_cluster_u64(peer(&s.kept, q));
-    if (q < rank) before += v;
-    total += v;
+  const uint64_t theirs = r.lane64(&s.kept), total = sum8(theirs);
+  uint64_t before = warps + sum8(lane < rank ? theirs : (uint64_t)0);
+  if (warp == 0) {
+    const uint64_t v = Row<T>::pick(a.u[row], total);
+    if (lane == 0) s.aim = v;
   }
-  for (int q = 0; q < warp; ++q) before += s.warp_kept[q];
-  const double u = fmin(fmax((double)a.u[row], 0.), 1.);   // (a NaN becomes 0)
-  uint64_t aim = (uint64_t)floor(u * (double)total);
-  if (aim >= total) aim = total - 1;
+  __syncthreads();
+  const uint64_t aim = s.aim;
   if (before <= aim && aim < before + sum) {     // one warp of the cluster
     ties = ties_before;
-    for (int i = i0; i < i1; i += 32) {
-      const uint32_t w = step(i + lane, ties);
-      uint64_t run = w;
+    for (int v = v0; v < v1; v += 32) {
+      uint32_t w[kVec];
+      step(v + lane, ties, w);
+      uint64_t mine = 0;
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) mine += w[j];
+      uint64_t run = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const uint64_t v = __shfl_up_sync(kFull, run, o);
-        if (lane >= o) run += v;
+        const uint64_t u = __shfl_up_sync(kFull, run, o);
+        if (lane >= o) run += u;
       }
       const uint32_t over = __ballot_sync(kFull, before + run > aim);
       if (over) {
         if (lane == __ffs(over) - 1) {
-          a.tokens[row] = begin + i + lane;
-          if (a.probs) a.probs[row] = (float)((double)w / (double)total);
+          uint64_t at = before + run - mine;
+#pragma unroll
+          for (int j = 0; j < kVec; ++j) {
+            if (at <= aim && aim < at + w[j]) {
+              a.tokens[row] = r.first_index + (v + lane) * kVec + j;
+              if (a.probs) a.probs[row] = (float)((double)w[j] / (double)total);
+            }
+            at += w[j];
+          }
         }
         break;
       }
@@ -769,7 +846,8 @@ cudaError_t launch_sample(SampleArgs a, int rows, cudaStream_t stream) {
   // the fewest CTAs a row that leave room for two on an SM; more while all rows' CTAs find an SM each
   int ctas = 1;
   auto bytes = [&](int c) {
-    return ((a.vocab + c - 1) / c + 7) / 8 * 8 * (int)sizeof(T) + 16 + sample_fixed(c);
+    // (the choice sorts up to kList 64-bit keys where the logits were)
+    return std::max(((a.vocab + c - 1) / c + 7) / 8 * 8 * (int)sizeof(T) + 32, kList * 8) + kSampleFixed;
   };
   while (ctas < kMaxCluster && (bytes(ctas) > kSampleSmem2 ||
                                 ((int64_t)rows * ctas * 2 <= device_sms() && a.vocab > 2048 * ctas)))
