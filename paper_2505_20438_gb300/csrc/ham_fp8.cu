@@ -33,7 +33,7 @@ struct ham_fp8_weight {
   uint8_t *scales = nullptr;   // [tiles][parts][sk]
   int32_t *err = nullptr;      // device error word
   int32_t *host_err = nullptr; // pinned
-  CUtensorMap map;             // codes as [tiles * kbs * parts * 128][128] bytes, boxes of a block
+  CUtensorMap map;             // codes as [tiles * kbs * parts * 128][128] bytes, boxes of half a block
 };
 
 namespace ham {
@@ -111,8 +111,7 @@ __device__ __forceinline__ void store4(const ProductArgs &a, int64_t row, int c,
 // requested before the dependency wait: nothing on the stream writes them.
 constexpr int kStreamThreads = 256;
 constexpr int kStreamSf = 4;            // scale slots (of four K blocks each)
-constexpr int kStreamSmem = 200 * 1024; // ring budget, one CTA an SM
-constexpr int kStreamSmem2 = 104 * 1024; // ... where two CTAs share an SM
+constexpr int kStreamSmem = 104 * 1024; // of a CTA: two share an SM
 
 constexpr int kStreamStages = 12;       // at most
 constexpr int kStreamBars = (2 * kStreamStages + 2 * kStreamSf + 1) * 8;
@@ -340,11 +339,14 @@ __global__ void __launch_bounds__(kStreamThreads)
 // ------------------------------------------------------------------------------------
 // A pair of CTAs (cta_group::2) computes 256 rows of X by two weight tiles (a gated weight: the gate's
 // and the up's tile of the same features): each CTA holds 128 of the rows (its lanes of tensor memory)
-// and loads its rows and one of the two weight tiles, so that every byte of an operand is read from
-// L2 once a pair.  The pairs are persistent.  The two accumulators (256 columns each) share 64 columns,
-// which leaves the columns 448.. for the scales: a tile's epilogue empties the shared columns first,
-// and the next tile's products begin when it has.
-constexpr int kPairThreads = 256;       // warps: copies, products, scales, -, 4 x epilogue
+// and loads its rows and one of the two weight tiles.  A pair takes 64 bytes a clock an SM from L2 at
+// the products' full rate (512 clocks a K block), which one pair alone gets and 76 pairs do not: so
+// clusters of two pairs (kPairs = 2) take the same weight tiles for neighbouring row tiles, each pair
+// loading half of them into both (multicast), 48 bytes a clock.  The clusters are persistent.  The two
+// accumulators (256 columns each) share 64 columns, which leaves the columns 448.. for the scales: a
+// tile's epilogue takes the shared columns into registers first, and the next tile's products begin when
+// it has.
+constexpr int kPairThreads = 384;       // warps: copies, products, scales, -, 8 x epilogue
 constexpr int kPairStages = 6;
 constexpr int kPairStageBytes = 2 * kBlockBytes;
 constexpr int kPairSf = 4;
@@ -352,35 +354,65 @@ constexpr int kPairSfBytes = 3 * 512;   // the CTA's 128 rows, both weight tiles
 constexpr int kPairBuf1 = 192, kPairSfCol = 448;
 constexpr int kPairSmem = smem_floor(512);
 static_assert(kPairSmem >= 1024 + kPairStages * kPairStageBytes + kPairSf * kPairSfBytes + 256 &&
-                  kPairSmem <= 227 * 1024, "shared memory");
+                  kPairSmem <= 226 * 1024, "shared memory");
 
-template <bool kGated>
+// 32 accumulator columns of one row (from column c of n) to the output.
+__device__ __forceinline__ void store32(const ProductArgs &a, int row, int c, const uint32_t *v, bool wide) {
+  const float *f = reinterpret_cast<const float *>(v);
+  if (wide && c + 32 <= a.n) {
+    char *dst = static_cast<char *>(a.out) + ((int64_t)row * a.n + c) * (a.f32 ? 4 : 2);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (a.f32) {
+        uint32_t w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = v[8 * q + j];
+        st_global_32(dst + 32 * q, w);
+      } else if (q < 2) {
+        uint32_t w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = pack_bf16x2(f[16 * q + 2 * j], f[16 * q + 2 * j + 1]);
+        st_global_32(dst + 32 * q, w);
+      }
+    }
+    return;
+  }
+#pragma unroll
+  for (int q = 0; q < 8; ++q)
+    if (c + 4 * q < a.n) store4(a, row, c + 4 * q, make_float4(f[4 * q], f[4 * q + 1], f[4 * q + 2], f[4 * q + 3]));
+}
+
+template <bool kGated, int kPairs>
 __global__ void __launch_bounds__(kPairThreads, 1)
     fp8_pair_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ CUtensorMap tw,
                     ProductArgs a, int row_tiles, int col_tiles) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t *sf = ring + kPairStages * kPairStageBytes;
-  uint64_t *full = reinterpret_cast<uint64_t *>(sf + kPairSf * kPairSfBytes);  // of the first CTA
-  uint64_t *empty = full + kPairStages;
-  uint64_t *sf_full = empty + kPairStages;     // of the first CTA: an arrival a CTA
+  // full, sf_full and acc_shared_free: the ones of a pair's first CTA are used
+  uint64_t *full = reinterpret_cast<uint64_t *>(sf + kPairSf * kPairSfBytes);
+  uint64_t *empty = full + kPairStages;        // a commit a pair of the cluster
+  uint64_t *sf_full = empty + kPairStages;     // an arrival a CTA
   uint64_t *sf_empty = sf_full + kPairSf;
   uint64_t *acc_full = sf_empty + kPairSf;     // [2]
-  uint64_t *acc_shared_free = acc_full + 2;    // of the first CTA: an arrival an epilogue warp
+  uint64_t *acc_shared_free = acc_full + 2;    // an arrival an epilogue warp of the pair
   uint64_t *drained = acc_shared_free + 1;     // every product issued is complete (after an abort)
   static_assert((2 * kPairStages + 2 * kPairSf + 4) * 8 <= 256, "barriers");
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_shared;
+  __shared__ float row_max[2][128];            // gated: largest magnitude of a row's half
   volatile int *abort_flag = &abort_shared;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int rank = (int)cluster_rank();
-  const int pairs = gridDim.x / 2, pair = blockIdx.x / 2;
-  const int total = row_tiles * col_tiles;
+  const int rank = (int)cluster_rank(), side = rank & 1, pair = rank >> 1, first = rank & ~1;
+  const uint32_t pair_mask = 3u << first, all_mask = (1u << (2 * kPairs)) - 1;
+  const int clusters = gridDim.x / (2 * kPairs), cluster = blockIdx.x / (2 * kPairs);
+  // a cluster's tiles: kPairs neighbouring row tiles (the last may lie past the rows) of one column tile
+  const int row_groups = (row_tiles + kPairs - 1) / kPairs, total = row_groups * col_tiles;
   if (tid == 0) {
     for (int s = 0; s < kPairStages; ++s) {
       mbar_init(&full[s], 1);
-      mbar_init(&empty[s], 1);
+      mbar_init(&empty[s], kPairs);
     }
     for (int s = 0; s < kPairSf; ++s) {
       mbar_init(&sf_full[s], 2);
@@ -388,7 +420,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     }
     mbar_init(&acc_full[0], 1);
     mbar_init(&acc_full[1], 1);
-    mbar_init(acc_shared_free, 8);
+    mbar_init(acc_shared_free, 16);
     mbar_init(drained, 1);
     abort_shared = 0;
     fence_mbar_init();
@@ -411,11 +443,11 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       grid_dependency_wait();
       bool ok = true;
       int it = 0;
-      for (int w = pair; w < total && ok; w += pairs) {
-        const int rt = w % row_tiles, ct = w / row_tiles;
-        const int x_row = rt * 256 + rank * 128;
-        // the laid-out weight's rows of K block 0 of this CTA's tile
-        const int64_t block = kGated ? (int64_t)ct * a.kbs * 2 + rank : ((int64_t)ct * 2 + rank) * a.kbs;
+      for (int w = cluster; w < total && ok; w += clusters) {
+        const int rt = w % row_groups * kPairs + pair, ct = w / row_groups;
+        const int x_row = rt * 256 + side * 128;
+        // K block 0 of this CTA's weight tile in the laid-out weight
+        const int64_t block = kGated ? (int64_t)ct * a.kbs * 2 + side : ((int64_t)ct * 2 + side) * a.kbs;
         for (int kb = 0; kb < a.kbs; ++kb, ++it) {
           const int s = it % kPairStages;
           if (it >= kPairStages &&
@@ -423,12 +455,18 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             ok = false;
             break;
           }
-          if (rank == 0) mbar_arrive_tx(&full[s], 2 * kPairStageBytes);  // both CTAs' copies
-          const uint32_t bar = cluster_map_shared(smem_u32(&full[s]), 0);
+          if (side == 0) mbar_arrive_tx(&full[s], 2 * kPairStageBytes);  // what lands in both CTAs
+          const uint32_t bar = cluster_map_shared(smem_u32(&full[s]), first);
           uint8_t *dst = ring + s * kPairStageBytes;
+          const int w_row = (int)((block + (int64_t)kb * (kGated ? 2 : 1)) * 128);
           tma_load_2d_pair(dst, &tx, kb * kFp8Block, x_row, bar, pol);
-          tma_load_2d_pair(dst + kBlockBytes, &tw, 0, (int)((block + (int64_t)kb * (kGated ? 2 : 1)) * 128), bar,
-                           pol);
+          if constexpr (kPairs == 1) {
+            tma_load_2d_pair(dst + kBlockBytes, &tw, 0, w_row, bar, pol);
+            tma_load_2d_pair(dst + kBlockBytes + kBlockBytes / 2, &tw, 0, w_row + 64, bar, pol);
+          } else {  // this pair's half of the tile, for both
+            tma_load_2d_pair_multicast(dst + kBlockBytes + pair * (kBlockBytes / 2), &tw, 0, w_row + pair * 64, bar,
+                                       5u << side, pol);
+          }
           issued = it + 1;
         }
       }
@@ -438,26 +476,26 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       }
     }
   } else if (warp == 1) {
-    // ------------------------------------------------------------ products (first CTA)
-    if (rank == 0) {
+    // ------------------------------------------------------------ products (a pair's first CTA)
+    if (side == 0) {
       bool ok = true;
       int it = 0, gi = 0, n = 0;
-      for (int w = pair; w < total && ok; w += pairs, ++n) {
+      for (int w = cluster; w < total && ok; w += clusters, ++n) {
         const uint32_t acc = tmem + (uint32_t)((n & 1) * kPairBuf1);
         if (n > 0 && !warp_wait_cluster(acc_shared_free, (uint32_t)(n - 1) & 1u, abort_flag)) { ok = false; break; }
         for (int kb = 0; kb < a.kbs; ++kb, ++it) {
           const int s = it % kPairStages;
-          const bool first = (kb & 3) == 0;
+          const bool new_word = (kb & 3) == 0;
           const uint32_t sft = tmem + kPairSfCol + (uint32_t)((gi & 1) * 16);
-          if (first && !warp_wait_cluster(&sf_full[gi % kPairSf], (uint32_t)(gi / kPairSf) & 1u, abort_flag)) { ok = false; break; }
+          if (new_word && !warp_wait_cluster(&sf_full[gi % kPairSf], (uint32_t)(gi / kPairSf) & 1u, abort_flag)) { ok = false; break; }
           if (!warp_wait_cluster(&full[s], (uint32_t)(it / kPairStages) & 1u, abort_flag)) { ok = false; break; }
           if (elect_one()) {
             tc_fence_after();
-            if (first) {
+            if (new_word) {
               const uint32_t from = smem_u32(sf + (gi % kPairSf) * kPairSfBytes);
 #pragma unroll
               for (int p = 0; p < 3; ++p) tc_copy_scales<2>(sft + p * 4, from + p * 512);
-              tc_commit_pair(&sf_empty[gi % kPairSf]);
+              tc_commit_pair(&sf_empty[gi % kPairSf], pair_mask);
             }
             const uint32_t xa = smem_u32(ring + s * kPairStageBytes), wa = xa + kBlockBytes;
             const uint32_t idesc = idesc_mx(256, 256, kb & 3);
@@ -465,8 +503,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             for (int kk = 0; kk < 4; ++kk)
               tc_mma_mx<2>(acc, smem_desc_sw128(xa + kk * 32, 16, 1024), smem_desc_sw128(wa + kk * 32, 16, 1024),
                            idesc, sft, sft + 4, kb > 0 || kk > 0);
-            tc_commit_pair(&empty[s]);
-            if (kb == a.kbs - 1) tc_commit_pair(&acc_full[n & 1]);
+            tc_commit_pair(&empty[s], all_mask);
+            if (kb == a.kbs - 1) tc_commit_pair(&acc_full[n & 1], pair_mask);
           }
           __syncwarp();
           if ((kb & 3) == 3 || kb == a.kbs - 1) ++gi;
@@ -479,7 +517,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         }
         __syncwarp();
         if (elect_one()) {
-          tc_commit_pair(drained);
+          tc_commit_pair(drained, pair_mask);
           thread_wait(drained, 0u, abort_flag, false);
         }
         __syncwarp();
@@ -492,9 +530,9 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     const int groups = (a.kbs + 3) / 4;
     bool ok = true;
     int gi = 0;
-    for (int w = pair; w < total && ok; w += pairs) {
-      const int rt = w % row_tiles, ct = w / row_tiles;
-      const int x_row = rt * 256 + rank * 128;
+    for (int w = cluster; w < total && ok; w += clusters) {
+      const int rt = w % row_groups * kPairs + pair, ct = w / row_groups;
+      const int x_row = rt * 256 + side * 128;
       for (int g = 0; g < groups; ++g, ++gi) {
         const int slot = gi % kPairSf;
         uint32_t x[4], ws[2];
@@ -520,7 +558,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         dst[64] = make_uint4(ws[1], ws[1], ws[1], ws[1]);
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(cluster_map_shared(smem_u32(&sf_full[slot]), 0));
+        if (lane == 0) mbar_arrive_cluster(cluster_map_shared(smem_u32(&sf_full[slot]), first));
       }
     }
     if (!ok && lane == 0 && !*abort_flag) {
@@ -528,110 +566,111 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       *abort_flag = 1;
     }
   } else if (warp >= 4) {
-    // ------------------------------------------------------------ epilogue: a thread a row
-    const int quarter = warp & 3;
-    const uint32_t free_bar = cluster_map_shared(smem_u32(acc_shared_free), 0);
-    bool ok = true;
+    // ------------------------------------------------------------ epilogue: two threads a row
+    // The first four warps take the columns 0..127 of a plain product (features 0..63 of the gate and
+    // of the up of a gated one), the last four the rest.  The shared columns are the last 64 of the first
+    // accumulator and the first 64 of the second: the warps that have them load them before all else.
+    const int quarter = warp & 3, half = (warp - 4) >> 2, lane_row = quarter * 32 + lane;
+    const uint32_t free_bar = cluster_map_shared(smem_u32(acc_shared_free), first);
+    const bool wide = kGated ? (a.n & 31) == 0 && ((uintptr_t)a.out & 31u) == 0
+                             : (a.n & (a.f32 ? 7 : 15)) == 0 && ((uintptr_t)a.out & 31u) == 0;
     int n = 0;
-    for (int w = pair; w < total && ok; w += pairs, ++n) {
-      const int rt = w % row_tiles, ct = w / row_tiles, buf = n & 1;
-      const int row = rt * 256 + rank * 128 + quarter * 32 + lane;
+    for (int w = cluster; w < total; w += clusters, ++n) {
+      const int rt = w % row_groups * kPairs + pair, ct = w / row_groups, buf = n & 1;
+      const int row = rt * 256 + side * 128 + lane_row;
       const uint32_t acc = tmem + (uint32_t)(buf * kPairBuf1) + ((uint32_t)(quarter * 32) << 16);
-      if (!warp_wait_cluster(&acc_full[buf], (uint32_t)(n >> 1) & 1u, abort_flag)) {
-        if (lane == 0 && !*abort_flag) {
-          record_error(a.err, HAM_DEVERR_TIMEOUT);
-          *abort_flag = 1;
-        }
-        ok = false;
-        break;
+      bool ok = warp_wait_cluster(&acc_full[buf], (uint32_t)(n >> 1) & 1u, abort_flag);
+      if (!ok && lane == 0 && !*abort_flag) {
+        record_error(a.err, HAM_DEVERR_TIMEOUT);
+        *abort_flag = 1;
       }
+      if (kGated) ok = named_barrier_and(1 + quarter, 64, ok);  // (they meet below: both go on or neither)
+      if (!ok) break;
       tc_fence_after();
+      // Each warp arrives once a tile: when it has taken the shared columns that it has, and has long
+      // taken the tile before.
+      auto release = [&] {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(free_bar);
+      };
+      const bool shared = half != buf;           // this warp has shared columns
+      if (!shared) release();
       if constexpr (!kGated) {
-        const int c0 = ct * 256, first = buf ? 0 : 6;  // the shared 64 columns first
-        const bool vec = (a.n & 7) == 0;
+        // 64 columns at a time: half 0 upwards, half 1 downwards, so that shared ones come first
+        uint32_t v[32], u[32];
 #pragma unroll 1
-        for (int i = 0; i < 8; ++i) {
-          const int ch = (first + i) & 7;
-          uint32_t v[32];
-          tmem_ld32(acc + ch * 32, v);
+        for (int i = 0; i < 2; ++i) {
+          const int col = half * 128 + (i ^ half) * 64;
+          tmem_ld32(acc + col, v);
+          tmem_ld32(acc + col + 32, u);
           tmem_wait_ld();
-          if (i == 1) {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(free_bar);
-          }
-          const int c = c0 + ch * 32;
-          if (row < a.rows && c < a.n) {
-            if (vec && c + 32 <= a.n && !a.f32) {
-              uint4 *dst = reinterpret_cast<uint4 *>(static_cast<uint16_t *>(a.out) + (int64_t)row * a.n + c);
-#pragma unroll
-              for (int q = 0; q < 4; ++q) {
-                const float *f = reinterpret_cast<const float *>(v) + 8 * q;
-                dst[q] = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]),
-                                    pack_bf16x2(f[6], f[7]));
-              }
-            } else {
-#pragma unroll
-              for (int q = 0; q < 8; ++q)
-                if (c + 4 * q < a.n)
-                  store4(a, row, c + 4 * q, make_float4(__uint_as_float(v[4 * q]), __uint_as_float(v[4 * q + 1]),
-                                                        __uint_as_float(v[4 * q + 2]), __uint_as_float(v[4 * q + 3])));
-            }
+          if (i == 0 && shared) release();
+          if (row < a.rows) {
+            const int c = ct * 256 + col;
+            if (c < a.n) store32(a, row, c, v, wide);
+            if (c + 32 < a.n) store32(a, row, c + 32, u, wide);
           }
         }
       } else {
-        // features in two halves of 64, the one that lies in the shared columns first
-        float h[2][64];
-        const int first = buf ? 0 : 1;
+        // gate columns half * 64 .., up columns 128 + half * 64 ..; shared: the up's of half 1 in the
+        // first accumulator, the gate's of half 0 in the second (silu is taken of the gate)
+        float h[64];
+        const int early = half ? 128 : 0, late = half ? 0 : 128;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) tmem_ld32(acc + early + half * 64 + j * 32, *reinterpret_cast<uint32_t(*)[32]>(h + j * 32));
+        tmem_wait_ld();
+        if (shared) release();
         float m = 0.f;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int half = first ^ i;
+        for (int j = 0; j < 2; ++j) {
+          uint32_t o[32];
+          tmem_ld32(acc + late + half * 64 + j * 32, o);
+          tmem_wait_ld();
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            uint32_t g[32], u[32];
-            tmem_ld32(acc + half * 64 + j * 32, g);
-            tmem_ld32(acc + 128 + half * 64 + j * 32, u);
-            tmem_wait_ld();
-#pragma unroll
-            for (int q = 0; q < 32; ++q) {
-              h[i][j * 32 + q] = silu_mul(__uint_as_float(g[q]), __uint_as_float(u[q]));
-              m = fmaxf(m, fabsf(h[i][j * 32 + q]));
-            }
-          }
-          if (i == 0) {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(free_bar);
+          for (int q = 0; q < 32; ++q) {
+            const float x = h[j * 32 + q], y = __uint_as_float(o[q]);
+            const float v = half ? silu_mul(y, x) : silu_mul(x, y);
+            h[j * 32 + q] = v;
+            m = fmaxf(m, fabsf(v));
           }
         }
+        row_max[half][lane_row] = m;             // a block's scale is that of both halves
+        named_barrier(1 + quarter, 64);
+        m = fmaxf(m, row_max[half ^ 1][lane_row]);
+        named_barrier(1 + quarter, 64);          // (read before the next tile's is written)
         const int e = fp8_exponent(m);
         const float p = fp8_pow2(-e);
+        const int c = ct * kTile + half * 64;
         if (row < a.rows) {
-          uint8_t *dst = static_cast<uint8_t *>(a.out) + (int64_t)row * a.n;
+          uint32_t code[16];
 #pragma unroll
-          for (int i = 0; i < 2; ++i)
+          for (int q = 0; q < 16; ++q) code[q] = fp8_codes4(h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3], p);
+          uint8_t *dst = static_cast<uint8_t *>(a.out) + (int64_t)row * a.n + c;
+          if (wide && c + 64 <= a.n) {
+            st_global_32(dst, *reinterpret_cast<uint32_t(*)[8]>(code));
+            st_global_32(dst + 32, *reinterpret_cast<uint32_t(*)[8]>(code + 8));
+          } else {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const int c = ct * kTile + (first ^ i) * 64 + q * 16;
-              const float *f = h[i] + q * 16;
-              if (c < a.n)  // (n is a multiple of 16)
-                *reinterpret_cast<uint4 *>(dst + c) =
-                    make_uint4(fp8_codes4(f[0], f[1], f[2], f[3], p), fp8_codes4(f[4], f[5], f[6], f[7], p),
-                               fp8_codes4(f[8], f[9], f[10], f[11], p), fp8_codes4(f[12], f[13], f[14], f[15], p));
-            }
-          uint8_t *s = a.out_scales + (int64_t)row * a.out_sk;
-          s[ct] = (uint8_t)(e + 127);
-          if (ct == a.tiles - 1)
-            for (int b = a.tiles; b < a.out_sk; ++b) s[b] = 127;  // padding
+            for (int q = 0; q < 4; ++q)
+              if (c + 16 * q < a.n)              // (n is a multiple of 16)
+                *reinterpret_cast<uint4 *>(dst + 16 * q) =
+                    make_uint4(code[4 * q], code[4 * q + 1], code[4 * q + 2], code[4 * q + 3]);
+          }
+          if (half == 0) {
+            uint8_t *s = a.out_scales + (int64_t)row * a.out_sk;
+            s[ct] = (uint8_t)(e + 127);
+            if (ct == a.tiles - 1)
+              for (int b = a.tiles; b < a.out_sk; ++b) s[b] = 127;  // padding
+          }
         }
       }
     }
     tc_fence_before();
   }
   __syncwarp();
-  if (warp == 0 && lane == 0 && rank == 0 && *abort_flag)
-    // after an abort the pair's copies (all count at this CTA's barriers) land before either CTA exits
+  if (warp == 0 && lane == 0 && side == 0 && *abort_flag)
+    // after an abort the pair's copies (they count at this CTA's barriers) land before a CTA exits
     for (int t = max(0, issued - kPairStages); t < issued; ++t)
       thread_wait(&full[t % kPairStages], (uint32_t)(t / kPairStages) & 1u, abort_flag, false);
   __syncwarp();
@@ -653,25 +692,25 @@ cudaError_t allow_smem(K kernel, int bytes, bool (&done)[64], int dev) {
   return e;
 }
 
-// Pairs of CTAs that are resident at once (a pair lies within one group of SMs, and an odd group
-// leaves an SM without a partner); a persistent grid is no larger.
+// Clusters of `ctas` CTAs that are resident at once (a cluster lies within one group of SMs, which need
+// not hold a whole number of them); a persistent grid is no larger.
 template <typename K>
-int resident_pairs(K kernel, int (&known)[64], int dev) {
+int resident_clusters(K kernel, int ctas, int (&known)[64], int dev) {
   if (dev >= 0 && dev < 64 && known[dev] > 0) return known[dev];
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(device_sms() / 2 * 2));
+  cfg.gridDim = dim3((unsigned)(device_sms() / ctas * ctas));
   cfg.blockDim = dim3(kPairThreads);
   cfg.dynamicSmemBytes = (size_t)kPairSmem;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.x = (unsigned)ctas;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   int n = 0;
   if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
     cudaGetLastError();
-    n = device_sms() / 2;
+    n = device_sms() / ctas;
   }
   if (dev >= 0 && dev < 64) known[dev] = n;
   return n;
@@ -683,11 +722,10 @@ cudaError_t launch_stream(const CUtensorMap &tx, ProductArgs a, int dev, cudaStr
   const int sms = device_sms();
   const int zt = (a.rows + a.nt - 1) / a.nt;
   int splits = 1;
-  while (splits < 8 && splits * 2 <= a.kbs && (int64_t)a.tiles * zt * splits * 2 <= sms) splits *= 2;
+  while (splits < 8 && splits * 2 <= a.kbs && (int64_t)a.tiles * zt * splits <= sms) splits *= 2;
   a.stage_bytes = kParts * kBlockBytes + a.nt * 128;
   const int per = (a.kbs + splits - 1) / splits;      // K blocks of a CTA
-  const int budget = (int64_t)a.tiles * zt * splits > sms ? kStreamSmem2 : kStreamSmem;
-  a.stages = std::min(std::min(per, kStreamStages), (budget - stream_fixed(kParts)) / a.stage_bytes);
+  a.stages = std::min(std::min(per, kStreamStages), (kStreamSmem - stream_fixed(kParts)) / a.stage_bytes);
   const int acc = kParts * a.nt * kTile * 4;          // the epilogue's, in the ring
   a.stages = std::max(std::max(a.stages, 2), (acc + a.stage_bytes - 1) / a.stage_bytes);
   int cols = 32;
@@ -700,17 +738,33 @@ cudaError_t launch_stream(const CUtensorMap &tx, ProductArgs a, int dev, cudaStr
                       dim3(kStreamThreads), (size_t)smem, dim3(1, (unsigned)splits, 1), stream, tx, a);
 }
 
+template <bool kGated, int kPairs>
+cudaError_t prepare_pair(int dev, int &clusters) {
+  static bool done[64] = {};
+  static int resident[64] = {};
+  const cudaError_t e = allow_smem(fp8_pair_kernel<kGated, kPairs>, kPairSmem, done, dev);
+  if (e == cudaSuccess) clusters = resident_clusters(fp8_pair_kernel<kGated, kPairs>, 2 * kPairs, resident, dev);
+  return e;
+}
+
 template <bool kGated>
 cudaError_t launch_pair(const CUtensorMap &tx, const CUtensorMap &tw, const ProductArgs &a, int dev,
                         cudaStream_t stream) {
-  static bool done[64] = {};
-  static int resident[64] = {};
   const int row_tiles = (a.rows + 255) / 256, col_tiles = kGated ? a.tiles : (a.tiles + 1) / 2;
-  cudaError_t e = allow_smem(fp8_pair_kernel<kGated>, kPairSmem, done, dev);
+  int one = 0, two = 0;
+  cudaError_t e = prepare_pair<kGated, 1>(dev, one);
+  if (e == cudaSuccess) e = prepare_pair<kGated, 2>(dev, two);
   if (e != cudaSuccess) return e;
-  const int pairs = std::min(resident_pairs(fp8_pair_kernel<kGated>, resident, dev), row_tiles * col_tiles);
-  return launch_after(fp8_pair_kernel<kGated>, dim3((unsigned)(2 * pairs)), dim3(kPairThreads), (size_t)kPairSmem,
-                      dim3(2, 1, 1), stream, tx, tw, a, row_tiles, col_tiles);
+  // Tiles that the busiest pair computes, with one pair a cluster and with two; the two share their
+  // weight tiles' loads and are a sixth faster a tile.
+  const int64_t work1 = ((int64_t)row_tiles * col_tiles + one - 1) / one;
+  const int64_t groups = (int64_t)((row_tiles + 1) / 2) * col_tiles, work2 = (groups + two - 1) / two;
+  if (work2 * 5 <= work1 * 6)
+    return launch_after(fp8_pair_kernel<kGated, 2>, dim3((unsigned)(4 * std::min<int64_t>(two, groups))), dim3(kPairThreads),
+                        (size_t)kPairSmem, dim3(4, 1, 1), stream, tx, tw, a, row_tiles, col_tiles);
+  return launch_after(fp8_pair_kernel<kGated, 1>,
+                      dim3((unsigned)(2 * std::min<int64_t>(one, (int64_t)row_tiles * col_tiles))), dim3(kPairThreads),
+                      (size_t)kPairSmem, dim3(2, 1, 1), stream, tx, tw, a, row_tiles, col_tiles);
 }
 
 int run_product(ham_fp8_weight *w, const void *x_codes, const void *x_scales, int32_t rows, void *out,
@@ -830,7 +884,7 @@ int ham_fp8_weight_alloc(int32_t n, int32_t k, const void *codes, const void *sc
   }
   if (e == cudaSuccess) e = cudaMemset(w->err, 0, 4);
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
-  if (e != cudaSuccess || ham::make_bytes_tensor_map(&w->map, w->codes, blocks * w->parts * 128, 128, 128, 128,
+  if (e != cudaSuccess || ham::make_bytes_tensor_map(&w->map, w->codes, blocks * w->parts * 128, 128, 128, 64,
                                                      false) != 0) {
     cudaGetLastError();
     ham_fp8_weight_free(w);

@@ -80,13 +80,13 @@ __device__ __forceinline__ void tmem_dealloc_n(uint32_t taddr, uint32_t cols) {
   asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(cols)
                : "memory");
 }
-// The barrier at the same place in both CTAs receives one arrival once every tcgen05 operation that
-// this thread issued so far is complete.
-__device__ __forceinline__ void tc_commit_pair(uint64_t *bar) {
+// The barrier at the same place in every CTA of `mask` (a bit a cluster rank) receives one arrival once
+// every tcgen05 operation that this thread issued so far is complete.
+__device__ __forceinline__ void tc_commit_pair(uint64_t *bar, uint32_t mask) {
   asm volatile(
       "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
           smem_u32(bar)),
-      "h"((uint16_t)3)
+      "h"((uint16_t)mask)
       : "memory");
 }
 // Arrive on a barrier of a CTA of the cluster (a shared::cluster address), releasing at cluster scope.
@@ -125,6 +125,37 @@ __device__ __forceinline__ void tma_load_2d_pair(void *dst, const CUtensorMap *m
       ".L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;" ::"r"(smem_u32(dst)),
       "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar), "l"(policy)
       : "memory");
+}
+
+// The same into every CTA of `mask`, at the same place in each; the bytes count at the first CTA of each
+// one's pair.
+__device__ __forceinline__ void tma_load_2d_pair_multicast(void *dst, const CUtensorMap *map, int x, int y,
+                                                           uint32_t bar, uint32_t mask, uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      ".multicast::cluster.L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5, %6;" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar), "h"((uint16_t)mask), "l"(policy)
+      : "memory");
+}
+// 32 bytes to global memory (32-byte aligned): a whole sector a thread.
+__device__ __forceinline__ void st_global_32(void *p, const uint32_t (&v)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]),
+               "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
+// A barrier of `threads` threads that also tells whether `ok` held in all of them.
+__device__ __forceinline__ bool named_barrier_and(int id, int threads, bool ok) {
+  uint32_t all;
+  asm volatile(
+      "{\n .reg .pred p, q;\n setp.ne.u32 p, %3, 0;\n bar.red.and.pred q, %1, %2, p;\n"
+      " selp.u32 %0, 1, 0, q;\n}"
+      : "=r"(all)
+      : "r"(id), "r"(threads), "r"((uint32_t)ok)
+      : "memory");
+  return all != 0;
+}
+__device__ __forceinline__ void named_barrier(int id, int threads) {
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
 
 }  // namespace
