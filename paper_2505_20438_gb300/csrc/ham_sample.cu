@@ -14,13 +14,12 @@
 // never sorted.  A histogram over 512 bins of (max - l) / T, which grows as the order goes on, of counts
 // (for top-k) or of counts and weights (top-p alone) finds the bin in which the order is cut: every CTA
 // adds up the cluster's histograms for itself, 16 bytes a load, so that this costs one cluster barrier
-// (of 2048 bins, added up by shares and read back, it took 8500 cycles against 3000).  Then
+// (2048 bins, added up by shares and read back, took 8500 cycles against 3000).  Then
 //  - where at most 2048 tokens lie up to that bin (the usual case) they are listed, in index order, in
-//    the first CTA's shared memory, and that CTA makes the exact cuts, sorting only the tokens of the
-//    cuts' bins, and picks the token;
-//  - otherwise the cluster goes on as a whole: histograms over 512 parts of the bin, then over the
-//    values of l in the part until one is left, whose equal tokens are kept by index; then the sums of
-//    the kept weights by stretches of the index.
+//    the first CTA's shared memory; that CTA sorts them, makes the exact cuts and picks the token;
+//  - otherwise the bin's own tokens are listed in every CTA, which finds the exact cut among them (where
+//    they too are more than 2048: histograms over 512 parts of the bin, then over the values of l in the
+//    part until one is left); then the cluster sums the kept weights by stretches of the index.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -38,9 +37,9 @@ constexpr int kSampleThreads = 512, kSampleWarps = kSampleThreads / 32;
 constexpr int kBins = 512;
 constexpr int kList = 2048;             // tokens that one CTA ranks by itself
 constexpr float kFine = 2147483648.f;   // 2^31
-constexpr float kLeast = -21.49f;       // below -31 log 2 = -21.4876 a weight is 0
 constexpr float kLastBin = 511.f;
-constexpr float kBinsPerX = 23.78f;     // bins of x = (l - max) / T: 511 reach to -21.4886
+constexpr float kBinsPerX = 23.78f;     // bins of x = (l - max) / T: 511 reach to -21.4886, and below
+                                        // -31 log 2 = -21.4876 a weight is 0
 constexpr int kSampleMaxVocab = 1 << 18;
 constexpr int kMaxCluster = 8;           // (8 CTAs hold the largest vocabulary in fp32)
 constexpr int kSampleSmem = 220 * 1024, kSampleSmem2 = 112 * 1024;  // one and two CTAs an SM
@@ -61,9 +60,10 @@ struct __align__(16) Histogram { uint32_t count[kBins], low[kBins], high[kBins];
 // What a CTA shares with its cluster beside the logits.
 struct SampleShared {
   Histogram h;
-  float list_l[kList];                    // first CTA: the listed tokens, by index
+  float list_l[kList];                    // the row's listed tokens, by index
   int32_t list_i[kList];
-  uint32_t list_w[kList];
+  uint32_t own[kList];                    // this CTA's: their places among its logits
+  uint64_t sorted[kList];
   uint64_t total_mass, warp_mass[kSampleWarps];
   uint32_t warp_count[kSampleWarps];
   float best, warp_best[kSampleWarps];
@@ -73,7 +73,9 @@ struct SampleShared {
   int first;                              // first index of the largest logit
   uint64_t found_before_mass, found_mass, aim;
   uint32_t found_before_count, found_count;
-  int found, members;
+  int found;
+  float cut_value;
+  uint32_t cut_ties, cut_by_index;
 };
 
 __device__ __forceinline__ float load_logit(const float *p) { return *p; }
@@ -106,8 +108,7 @@ __device__ __forceinline__ float x_of(float l, const Scale &c) {
   return l == c.best ? 0.f : __fdiv_rn(a, c.t);
 }
 __device__ __forceinline__ uint32_t weight_of(float x) {
-  const uint32_t w = (uint32_t)(expf(x) * kFine);
-  return x >= kLeast ? w : 0u;
+  return (uint32_t)(expf(x) * kFine);  // (NaN: 0)
 }
 // Where l lies in the order, in bins (the fraction: the part of the bin); it grows as l falls, so bins
 // and parts follow the order.  From kLastBin on weights are 0 and the token is left out.
@@ -128,26 +129,38 @@ __device__ __forceinline__ uint64_t ld_cluster_u64(uint32_t a) {
   asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a));
   return v;
 }
-__device__ __forceinline__ void st_cluster_u32(uint32_t a, uint32_t v) {
-  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory");
-}
 __device__ __forceinline__ uint4 ld_cluster_u32x4(uint32_t a) {
   uint4 v;
   asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
   return v;
 }
+__device__ __forceinline__ void cluster_arrive() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+template <typename T>
+__device__ __forceinline__ float ld_cluster_logit(uint32_t a) {
+  if constexpr (sizeof(T) == 4) return __uint_as_float(ld_cluster_u32(a));
+  uint16_t v;
+  asm volatile("ld.shared::cluster.u16 %0, [%1];" : "=h"(v) : "r"(a));
+  return __uint_as_float((uint32_t)v << 16);
+}
 template <typename T>
 __device__ __forceinline__ uint32_t peer(const T *p, int rank) { return cluster_map_shared(smem_u32(p), (uint32_t)rank); }
 
-// Where the order is cut: kept are the tokens whose place is below `end` (a part is 2^-9 of a bin, so
-// that an end between parts is a number of 18 bits), or, with `by_value`, those with logits above
-// `value` and the first `ties` by index of the ones equal to it.
+// Where the order is cut: kept are the logits above `value` and, of the ones equal to it, all or (with
+// by_index) the first `ties` by index.
 struct Cut {
-  float end = INFINITY, value = -INFINITY;
-  bool by_value = false, by_index = false;  // by_index: some of the equal tokens are cut off
+  float value = -INFINITY;
+  bool by_index = false;
   uint32_t ties = 0;
   uint64_t mass = 0;       // weight of what is kept
 };
+__device__ __forceinline__ float logit_of(uint32_t key) {
+  return __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xffffffffu));
+}
 
 // Inclusive running sums of a weight over the block's threads, in thread order; `all`: their sum.
 __device__ __forceinline__ uint64_t block_scan(SampleShared &s, uint64_t mass, uint64_t &all) {
@@ -213,8 +226,8 @@ struct Row {
   static constexpr int kN = Vec<T>::kN;
   SampleShared &s;
   uint4 *data;             // this CTA's logits, cleaned (-inf before and after them)
-  int first_index;         // index of the first vector's first element
-  int vecs, ctas, rank, tid;
+  int first_index;         // index of the first vector's first element (slice further on in the next CTA)
+  int slice, vecs, ctas, rank, tid;
   Scale c;
 
   __device__ void sync() const {
@@ -230,11 +243,19 @@ struct Row {
     const int q = tid & 31;
     return q < ctas ? ld_cluster_u64(peer(p, q)) : 0ull;
   }
-  // f(vector) for every vector of this CTA's logits, in any order.
+  // The warps' stretches of the vectors, in index order: a step is 32 vectors, one a lane.
+  __device__ __forceinline__ void stretch(int &v0, int &v1) const {
+    const int per = (vecs + kSampleWarps * 32 - 1) / (kSampleWarps * 32) * 32;
+    v0 = min(vecs, (tid >> 5) * per);
+    v1 = min(vecs, v0 + per);
+  }
+  // f(vector) for every vector of this lane.
   template <typename F>
   __device__ __forceinline__ void each(F f) const {
+    int v0, v1;
+    stretch(v0, v1);
 #pragma unroll 2
-    for (int v = tid; v < vecs; v += kSampleThreads) f(Vec<T>(data[v]));
+    for (int v = v0 + (tid & 31); v < v1; v += 32) f(Vec<T>(data[v]));
   }
   // The histogram of the logits in range by the bins of `where` (negative: left out), counts and / or
   // weights.  Computed for the whole vector first: a vector's chains of arithmetic overlap.
@@ -277,33 +298,31 @@ struct Row {
   // must stand until their next barrier.
   __device__ void find(bool by_mass, bool masses, uint32_t count0, uint64_t mass0, uint64_t aim, double p = 0.) const {
     sync();                                      // every CTA's histogram is complete
-    constexpr int kThreads = kBins / 4;          // four bins a thread
-    static_assert(kThreads % 32 == 0 && kThreads <= kSampleThreads, "threads");
-    const int lane = tid & 31, warp = tid >> 5;
+    constexpr int kThreads = kBins / 4;          // four bins a thread; a group of threads a histogram
+    static_assert(kThreads % 32 == 0 && 3 * kThreads <= kSampleThreads && 2 * kBins <= kList, "threads");
+    const int lane = tid & 31, warp = tid >> 5, group = tid / kThreads, quad = tid % kThreads;
+    uint64_t m4[4] = {0, 0, 0, 0}, m_sum = 0, mi = 0;
     uint32_t c4[4], c_sum = 0, ci = 0;
-    uint64_t m4[4], m_sum = 0, mi = 0;
-    if (tid < kThreads) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) c4[j] = 0, m4[j] = 0;
-      const uint32_t at_c = smem_u32(&s.h.count[tid * 4]), at_h = smem_u32(&s.h.high[tid * 4]);
-      const uint32_t at_l = smem_u32(&s.h.low[tid * 4]);
+    if (group == 0 || (masses && group < 3)) {
+      const uint32_t at = smem_u32((group == 0 ? s.h.count : group == 1 ? s.h.high : s.h.low) + quad * 4);
+      uint4 v[kMaxCluster];
 #pragma unroll
       for (int q = 0; q < kMaxCluster; ++q)
-        if (q < ctas) {
-          const uint4 v = ld_cluster_u32x4(cluster_map_shared(at_c, q));
-          c4[0] += v.x, c4[1] += v.y, c4[2] += v.z, c4[3] += v.w;
-        }
-      if (masses) {
+        v[q] = q < ctas ? ld_cluster_u32x4(cluster_map_shared(at, q)) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int q = 0; q < kMaxCluster; ++q)
-          if (q < ctas) {
-            const uint4 v = ld_cluster_u32x4(cluster_map_shared(at_h, q)), w = ld_cluster_u32x4(cluster_map_shared(at_l, q));
-            m4[0] += ((uint64_t)v.x << 16) + w.x, m4[1] += ((uint64_t)v.y << 16) + w.y;
-            m4[2] += ((uint64_t)v.z << 16) + w.z, m4[3] += ((uint64_t)v.w << 16) + w.w;
-          }
+      for (int q = 0; q < kMaxCluster; ++q) m4[0] += v[q].x, m4[1] += v[q].y, m4[2] += v[q].z, m4[3] += v[q].w;
+      if (group)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s.sorted[(group - 1) * kBins + quad * 4 + j] = m4[j];
+    }
+    if (masses) __syncthreads();
+    if (tid < kThreads) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        c4[j] = (uint32_t)m4[j], c_sum += c4[j];
+        m4[j] = masses ? (s.sorted[quad * 4 + j] << 16) + s.sorted[kBins + quad * 4 + j] : 0;
+        m_sum += m4[j];
       }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) c_sum += c4[j], m_sum += m4[j];
       ci = c_sum, mi = m_sum;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -355,8 +374,8 @@ struct Row {
     kmin = __reduce_min_sync(kFull, (tid & 31) < ctas ? lane32(&s.key_min) : 0xffffffffu);
     sync();                                      // (read before the next call writes them)
   }
-  // The exact cut within the bin that find() gave for the aim, by the whole cluster.
-  __device__ Cut cut(bool by_mass, uint64_t aim) const {
+  // The exact cut within the bin that find() gave for the aim, by histograms of the whole cluster.
+  __device__ Cut cut_by_bins(bool by_mass, uint64_t aim) const {
     Cut k;
     const int b1 = s.found;
     uint32_t count = s.found_before_count;
@@ -369,12 +388,10 @@ struct Row {
     });
     find(by_mass, true, count, mass, aim);
     const int b2 = s.found;
-    k.end = (float)b1 + (float)(b2 + 1) * (1.f / kBins);
-    k.mass = s.found_before_mass + s.found_mass;
     count = s.found_before_count, mass = s.found_before_mass;
-    if (s.found_count == 1 || (!by_mass && count + s.found_count == aim)) return k;
     // values of l within the part, until one is left
-    const float begin = (float)b1 + (float)b2 * (1.f / kBins);
+    // (a part is 2^-9 of a bin, so that its ends are numbers of 18 bits)
+    const float begin = (float)b1 + (float)b2 * (1.f / kBins), end = begin + 1.f / kBins;
     uint32_t lo = 0, hi = 0xffffffffu;
     for (;;) {
       uint32_t kmax = 0, kmin = 0xffffffffu;
@@ -383,7 +400,7 @@ struct Row {
         for (int j = 0; j < kN; ++j) {
           const float f = place_of(x.l[j], c);
           const uint32_t key = key_of(x.l[j]);
-          if (f >= begin && f < k.end && key >= lo && key <= hi) kmax = max(kmax, key), kmin = min(kmin, key);
+          if (f >= begin && f < end && key >= lo && key <= hi) kmax = max(kmax, key), kmin = min(kmin, key);
         }
       });
       key_range(kmax, kmin);
@@ -393,7 +410,7 @@ struct Row {
       histogram<true, true>([&](float l) {
         const float f = place_of(l, c);
         const uint32_t key = key_of(l);
-        return f >= begin && f < k.end && key >= kmin && key <= kmax ? (int)((kmax - key) >> shift) : -1;
+        return f >= begin && f < end && key >= kmin && key <= kmax ? (int)((kmax - key) >> shift) : -1;
       });
       find(by_mass, true, count, mass, aim);
       count = s.found_before_count, mass = s.found_before_mass;
@@ -403,8 +420,7 @@ struct Row {
         const uint64_t many = s.found_count, w = s.found_mass / many;
         // (by weight: the fewest whose weights reach the aim; the bin's own do, so w > 0)
         const uint64_t keep = by_mass ? (aim - mass + w - 1) / w : aim - count;
-        k.by_value = true;
-        k.value = __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xffffffffu));
+        k.value = logit_of(key);
         k.ties = (uint32_t)keep;
         k.by_index = keep < many;
         k.mass = mass + keep * w;
@@ -415,24 +431,14 @@ struct Row {
       lo = kmax - kmin < down ? kmin : kmax - down;
     }
   }
-  // Weights of a vector's logits that the cut and min_p keep (tie: one of the cut's equal tokens, of
-  // which the caller keeps the first by index).
-  __device__ __forceinline__ void kept(const Cut &k, uint32_t least, const Vec<T> &x, uint32_t (&w)[kN],
-                                       bool (&tie)[kN]) const {
+  // Weights of a vector's logits that the cut and min_p keep (those equal to the cut's value too: where
+  // some of them are cut off, the caller keeps the first by index).
+  __device__ __forceinline__ void kept(const Cut &k, uint32_t least, const Vec<T> &x, uint32_t (&w)[kN]) const {
 #pragma unroll
     for (int j = 0; j < kN; ++j) {
-      const float l = x.l[j];
-      w[j] = weight_of(x_of(l, c));
-      const bool in = k.by_value ? l >= k.value : !(place_of(l, c) >= k.end);
-      if (!in || w[j] < least) w[j] = 0;
-      tie[j] = k.by_index && l == k.value;
+      const uint32_t v = weight_of(x_of(x.l[j], c));
+      w[j] = x.l[j] >= k.value && v >= least ? v : 0u;
     }
-  }
-  // The warps' stretches of the vectors, in index order: a step is 32 vectors, one a lane.
-  __device__ __forceinline__ void stretch(int &v0, int &v1) const {
-    const int per = (vecs + kSampleWarps * 32 - 1) / (kSampleWarps * 32) * 32;
-    v0 = min(vecs, (tid >> 5) * per);
-    v1 = min(vecs, v0 + per);
   }
   // Sum over the warps before this one, and over the CTAs before this one, of a number a warp (all:
   // over the row).
@@ -448,158 +454,199 @@ struct Row {
     all = sum8(q);
     return warps + sum8(lane < rank ? q : 0u);
   }
-  // Lists the tokens up to bin `last` in the first CTA, by index, if they are at most kList; their
-  // number over the row.
-  __device__ uint32_t list(int last) const {
-    const int lane = tid & 31;
-    const float end = (float)(last + 1);         // (last < 2047: a token up to it has a bin)
+  // Lists this CTA's tokens of the bins first .. last, by index; the row's number of them.  If that is at
+  // most kList, pull() then makes the row's list.
+  __device__ uint32_t list(int first, int last) const {
+    const int lane = tid & 31, warp = tid >> 5;
+    const float begin = (float)first, end = (float)(last + 1);  // (last < 511: a token up to it has a bin)
     int v0, v1;
     stretch(v0, v1);
-    uint32_t many = 0, all;
+    uint32_t many = 0;
 #pragma unroll 2
     for (int v = v0 + lane; v < v1; v += 32) {
       const Vec<T> x(data[v]);
 #pragma unroll
-      for (int j = 0; j < kN; ++j) many += place_of(x.l[j], c) < end;
+      for (int j = 0; j < kN; ++j) {
+        const float f = place_of(x.l[j], c);
+        many += f < end && f >= begin;
+      }
     }
+    const uint32_t who_has = __ballot_sync(kFull, many > 0);
     many = __reduce_add_sync(kFull, many);
-    uint32_t at = before_me(many, all);
-    if (all > (uint32_t)kList) return all;
-    if (many) {
-      const uint32_t to_l = peer(s.list_l, 0), to_i = peer(s.list_i, 0), below = (1u << lane) - 1u;
+    if (lane == 0) s.warp_ties[warp] = many;
+    __syncthreads();
+    const uint32_t others = lane < kSampleWarps ? s.warp_ties[lane] : 0u;
+    const uint32_t cta = sum8(others);
+    uint32_t at = sum8(lane < warp ? others : 0u);
+    if (tid == 0) s.ties = cta;
+    if (who_has && cta <= (uint32_t)kList) {
+      const uint32_t below = (1u << lane) - 1u;
       for (int v = v0; v < v1; v += 32) {
-        const Vec<T> x(v + lane < v1 ? data[v + lane] : Vec<T>::none());
+        const Vec<T> x((who_has >> lane & 1u) && v + lane < v1 ? data[v + lane] : Vec<T>::none());
         bool in[kN], any = false;
 #pragma unroll
-        for (int j = 0; j < kN; ++j) in[j] = place_of(x.l[j], c) < end, any |= in[j];
+        for (int j = 0; j < kN; ++j) {
+          const float f = place_of(x.l[j], c);
+          in[j] = f < end && f >= begin, any |= in[j];
+        }
         if (!__any_sync(kFull, any)) continue;
-        uint32_t mine = at, step = 0;
+        uint32_t mine = at;
 #pragma unroll
         for (int j = 0; j < kN; ++j) {
           const uint32_t who = __ballot_sync(kFull, in[j]);
           mine += __popc(who & below);
-          step += __popc(who);
+          at += __popc(who);
         }
 #pragma unroll
         for (int j = 0; j < kN; ++j)
           if (in[j]) {
-            st_cluster_u32(to_l + 4 * mine, __float_as_uint(x.l[j]));
-            st_cluster_u32(to_i + 4 * mine, (uint32_t)(first_index + (v + lane) * kN + j));
-            ++mine;
+            s.own[mine++] = (v + lane) * kN + j;
           }
-        at += step;
       }
     }
     sync();
-    return all;
+    return sum8(lane32(&s.ties));
   }
-  // Sorts the first `many` of the 64-bit keys where the logits were (ascending; a bitonic network).
-  __device__ void sort(uint64_t *key, int many) const {
+  // The CTAs' lists of list(), one after the other.
+  __device__ void pull(uint32_t all) const {
+    uint32_t upto = lane32(&s.ties);             // lane q: the tokens of CTAs 0 .. q
+#pragma unroll
+    for (int o = 1; o < kMaxCluster; o <<= 1) {
+      const uint32_t v = __shfl_up_sync(kFull, upto, o);
+      if ((tid & 31) >= o) upto += v;
+    }
+    for (uint32_t i0 = 0; i0 < all; i0 += kSampleThreads) {
+      const uint32_t i = i0 + tid;
+      int q = 0;
+      uint32_t before = 0;
+#pragma unroll
+      for (int p = 0; p < kMaxCluster - 1; ++p) {
+        const uint32_t v = __shfl_sync(kFull, upto, p);
+        if (p < ctas - 1 && i >= v) q = p + 1, before = v;
+      }
+      if (i < all) {
+        const uint32_t place = ld_cluster_u32(peer(&s.own[i - before], q));
+        s.list_l[i] = ld_cluster_logit<T>(peer(data, q) + place * (uint32_t)sizeof(T));
+        s.list_i[i] = first_index + (q - rank) * slice + (int)place;
+      }
+    }
+    __syncthreads();
+  }
+  // s.sorted: the first `many` listed tokens in order, as (key of l, inverted; place in the list), by
+  // a bitonic network: distances below a warp in registers, the others in shared memory.
+  __device__ void sort_list(int many) const {
+    uint64_t *key = s.sorted;
     int n = 32;
     while (n < many) n *= 2;
-    for (int i = many + tid; i < n; i += kSampleThreads) key[i] = ~0ull;
-    __syncthreads();
-    for (int size = 2; size <= n; size *= 2)
-      for (int step = size / 2; step > 0; step /= 2) {
+    for (int i = tid; i < n; i += kSampleThreads)
+      key[i] = i < many ? ((uint64_t)~key_of(s.list_l[i]) << 32) | (uint32_t)i : ~0ull;
+    for (int size = 32; size <= n; size *= 2) {
+      for (int step = size / 2; step >= 32; step /= 2) {
+        __syncthreads();
         for (int q = tid; q < n / 2; q += kSampleThreads) {
           const int i = 2 * q - (q & (step - 1)), o = i + step;
           const uint64_t x = key[i], y = key[o];
           if ((x > y) == ((i & size) == 0)) key[i] = y, key[o] = x;
         }
-        if (n <= 64) __syncwarp();               // (the first warp's own)
-        else __syncthreads();
       }
+      __syncthreads();
+      for (int i = tid; i < n; i += kSampleThreads) {  // (whole warps)
+        uint64_t x = key[i];
+        for (int sub = size == 32 ? 2 : size; sub <= size; sub *= 2)
+          for (int step = min(sub / 2, 16); step > 0; step /= 2) {
+            const uint64_t y = __shfl_xor_sync(kFull, x, step);
+            const bool low = (i & step) == 0, up = (i & sub) == 0;
+            if ((x > y) == (low == up)) x = y;
+          }
+        key[i] = x;
+      }
+    }
     __syncthreads();
   }
-  // The choice among the first CTA's list of `all` tokens (up to bin `last`), by that CTA alone.
-  // k > 0: top-k cuts in bin `last`, before which the list holds `before` tokens.  p >= 0: top-p, of the
-  // weight `row_mass` (0: of the list's, after top-k).
-  __device__ void choose(const SampleArgs &a, int row, uint32_t all, int last, uint32_t before, int k, double p,
-                         uint64_t row_mass, uint32_t least) const {
-    constexpr int kPer = kList / kSampleThreads;
-    uint64_t *key = reinterpret_cast<uint64_t *>(data);  // (the logits are not needed any more)
-    // each thread: kPer neighbouring tokens of the list
-    uint32_t w[kPer];
-    int bin[kPer];
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const uint32_t i = tid * kPer + j;
-      const float l = i < all ? s.list_l[i] : -INFINITY;
-      bin[j] = i < all ? (int)place_of(l, c) : kBins;
-      w[j] = i < all ? weight_of(x_of(l, c)) : 0;
-    }
-    s.h.low[tid] = s.h.high[tid] = 0;
-    // the keys of bin b's tokens with any weight, in order: by l, largest first, equal ones by place in
-    // the list
-    auto in_order = [&](int b) {
-      if (tid == 0) s.members = 0;
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j < kPer; ++j)
-        if (bin[j] == b && w[j]) {
-          const uint32_t i = tid * kPer + j;
-          key[atomicAdd(&s.members, 1)] = ((uint64_t)~key_of(s.list_l[i]) << 32) | i;
+  __device__ __forceinline__ uint32_t sorted_weight(uint64_t key) const {
+    return weight_of(x_of(logit_of(~(uint32_t)(key >> 32)), c));
+  }
+  // The exact cut within the bin that find() gave for the aim.
+  __device__ Cut cut(bool by_mass, uint64_t aim) const {
+    if (s.found_count > (uint32_t)kList) return cut_by_bins(by_mass, aim);
+    const uint32_t count = s.found_before_count;
+    const uint64_t mass = s.found_before_mass;
+    const int bin = s.found;
+    __syncthreads();
+    const int many = (int)list(bin, bin);
+    pull(many);
+    sort_list(many);
+    uint64_t at = mass;
+    for (int i0 = 0; i0 < many; i0 += kSampleThreads) {
+      const int i = i0 + tid;
+      const uint64_t key = i < many ? s.sorted[i] : ~0ull;
+      const uint64_t w = i < many ? sorted_weight(key) : 0;
+      uint64_t part;
+      const uint64_t upto = at + block_scan(s, w, part);
+      // the last token kept, and how many of its equals are kept with it
+      if (i < many && (by_mass ? upto >= aim && upto - w < aim : count + i + 1 == aim)) {
+        const uint32_t l = (uint32_t)(key >> 32);
+        int from = 0, to = i;                    // the first of the equal ones
+        while (from < to) {
+          const int mid = (from + to) / 2;
+          if ((uint32_t)(s.sorted[mid] >> 32) < l) from = mid + 1;
+          else to = mid;
         }
-      __syncthreads();
-      const int m = s.members;
-      sort(key, m);
-      return m;
-    };
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) s.list_w[tid * kPer + j] = w[j];
-    if (k > 0 && all > (uint32_t)k) {            // of bin `last`, the first k - before
-      const int m = in_order(last);
-      for (int i = tid; i < m; i += kSampleThreads)
-        if (before + i >= (uint32_t)k) s.list_w[(uint32_t)key[i]] = 0;
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) w[j] = s.list_w[tid * kPer + j];
-    }
-    uint64_t mass = 0, whole = row_mass;
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) mass += w[j];
-    if (p >= 0.) {
-      if (!row_mass) block_scan(s, mass, whole);
-      if (tid == 0) s.aim = aim_of(p, whole);
-      __syncthreads();
-      const uint64_t aim = s.aim;
-#pragma unroll
-      for (int j = 0; j < kPer; ++j)
-        if (w[j]) add_mass(bin[j], w[j]);
-      __syncthreads();
-      const uint64_t m = ((uint64_t)s.h.high[tid] << 16) + s.h.low[tid];  // a thread a bin
-      uint64_t run_all;
-      const uint64_t run = block_scan(s, m, run_all);
-      if (run >= aim && run - m < aim) {         // (one thread: the list's weights reach the aim)
-        s.found = tid;
-        s.found_before_mass = run - m;
+        s.cut_value = logit_of(~l);
+        s.cut_ties = i - from + 1;
+        s.cut_by_index = i + 1 < many && (uint32_t)(s.sorted[i + 1] >> 32) == l;
+        s.found_mass = upto;
       }
-      __syncthreads();
-      const int b = s.found;
-      uint64_t at = s.found_before_mass;
-      const int many = in_order(b);
-      for (int i0 = 0; i0 < many; i0 += kSampleThreads) {
-        const uint32_t i = i0 + tid < many ? (uint32_t)key[i0 + tid] : 0u, v = i0 + tid < many ? s.list_w[i] : 0u;
-        uint64_t part;
-        const uint64_t upto = at + block_scan(s, v, part);
-        if (v && upto - v >= aim) s.list_w[i] = 0;
-        at += part;
-      }
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) w[j] = bin[j] > b ? 0 : s.list_w[tid * kPer + j];
+      at += part;
     }
-    mass = 0;
+    __syncthreads();
+    Cut k;
+    k.value = s.cut_value;
+    k.ties = s.cut_ties;
+    k.by_index = s.cut_by_index;
+    k.mass = s.found_mass;
+    return k;
+  }
+  // The choice among the first CTA's list of `all` tokens, by that CTA alone: kPer tokens a thread.
+  // k > 0: top-k.  p >= 0: top-p, of the weight `row_mass` (0: of the list's, after top-k).
+  template <int kPer>
+  __device__ void choose(const SampleArgs &a, int row, int all, int k, double p, uint64_t row_mass, uint32_t least) const {
+    uint32_t *list_w = s.own;                  // (its places are pulled)
+    sort_list(all);
+    if (k <= 0 || k > all) k = all;
+    uint64_t key[kPer], mass = 0, whole;
+    uint32_t w[kPer];
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-      if (w[j] < least) w[j] = 0;
+      const int i = tid * kPer + j;
+      key[j] = i < all ? s.sorted[i] : ~0ull;
+      w[j] = i < k ? sorted_weight(key[j]) : 0;
       mass += w[j];
     }
-    uint64_t sum = block_scan(s, mass, whole);
+    uint64_t run = block_scan(s, mass, whole) - mass, aim = ~0ull;
+    if (p >= 0.) {
+      if (tid == 0) s.aim = aim_of(p, row_mass ? row_mass : whole);
+      __syncthreads();
+      aim = s.aim;
+    }
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int i = tid * kPer + j;
+      if (i < all) list_w[(uint32_t)key[j]] = run < aim && w[j] >= least ? w[j] : 0u;
+      run += w[j];
+    }
+    __syncthreads();
+    mass = 0;                                    // from here on by index
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int i = tid * kPer + j;
+      w[j] = i < all ? list_w[i] : 0u;
+      mass += w[j];
+    }
+    uint64_t sum = block_scan(s, mass, whole) - mass;
     if (tid == 0) s.aim = pick(a.u[row], whole);
     __syncthreads();
-    const uint64_t aim = s.aim;
-    sum -= mass;
+    aim = s.aim;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
       if (sum <= aim && aim < sum + w[j]) {
@@ -669,7 +716,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
   __syncthreads();
   best = warp_max_f32(lane < kSampleWarps ? s.warp_best[lane] : -INFINITY);
   if (tid == 0) s.best = best;
-  Row<T> r{s, store, begin - phase, vecs, ctas, rank, tid, Scale{}};
+  Row<T> r{s, store, rank * a.slice - phase, a.slice, vecs, ctas, rank, tid, Scale{}};
   r.sync();
   best = warp_max_f32(lane < ctas ? __uint_as_float(r.lane32(&s.best)) : -INFINITY);
   const bool greedy = !(temperature > 0.f);
@@ -717,10 +764,18 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
     uint64_t aim = s.aim;
     const uint32_t all = all_in ? kList : before + s.found_count;
     if (all <= (uint32_t)kList) {
-      const uint32_t listed = r.list(last);
+      const uint32_t listed = r.list(0, last);
       if (listed <= (uint32_t)kList) {           // (all_in: known only now)
-        if (rank == 0) r.choose(a, row, listed, last, before, by_k && !all_in ? k : 0, by_p ? share : -1., whole, least);
-        return;                                  // (no shared memory of a peer is read from here on)
+        if (rank == 0) r.pull(listed);
+        if (ctas > 1) cluster_arrive();          // (the others' lists are pulled)
+        if (rank == 0) {
+          const int n_k = by_k ? k : 0;
+          const double n_p = by_p ? share : -1.;
+          if (listed <= (uint32_t)kSampleThreads) r.template choose<1>(a, row, listed, n_k, n_p, whole, least);
+          else r.template choose<kList / kSampleThreads>(a, row, listed, n_k, n_p, whole, least);
+        }
+        if (ctas > 1) cluster_wait();
+        return;
       }
     }
     if (by_k) {
@@ -759,19 +814,18 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
   // one step of 32 vectors: this lane's kept weights (ties: those before this step)
   auto step = [&](int v, uint32_t &ties, uint32_t (&w)[kVec]) {
     const Vec<T> x(v < v1 ? store[v] : Vec<T>::none());
-    bool tie[kVec];
-    r.kept(cut, least, x, w, tie);
+    r.kept(cut, least, x, w);
     if (cut.by_index) {
       uint32_t mine = ties;
 #pragma unroll
       for (int j = 0; j < kVec; ++j) {
-        const uint32_t who = __ballot_sync(kFull, tie[j]);
+        const uint32_t who = __ballot_sync(kFull, x.l[j] == cut.value);
         mine += __popc(who & ((1u << lane) - 1u));
         ties += __popc(who);
       }
 #pragma unroll
       for (int j = 0; j < kVec; ++j)
-        if (tie[j] && mine++ >= cut.ties) w[j] = 0;
+        if (x.l[j] == cut.value && mine++ >= cut.ties) w[j] = 0;
     }
   };
   uint64_t sum = 0;
@@ -843,14 +897,14 @@ cudaError_t launch_sample(SampleArgs a, int rows, cudaStream_t stream) {
   static bool done[64] = {};
   int dev = 0;
   cudaGetDevice(&dev);
-  // the fewest CTAs a row that leave room for two on an SM; more while all rows' CTAs find an SM each
+  // the fewest CTAs a row that leave room for two on an SM; more while all rows' CTAs
+  // still find room at once
   int ctas = 1;
   auto bytes = [&](int c) {
-    // (the choice sorts up to kList 64-bit keys where the logits were)
-    return std::max(((a.vocab + c - 1) / c + 7) / 8 * 8 * (int)sizeof(T) + 32, kList * 8) + kSampleFixed;
+    return ((a.vocab + c - 1) / c + 7) / 8 * 8 * (int)sizeof(T) + 32 + kSampleFixed;
   };
   while (ctas < kMaxCluster && (bytes(ctas) > kSampleSmem2 ||
-                                ((int64_t)rows * ctas * 2 <= device_sms() && a.vocab > 2048 * ctas)))
+                                ((int64_t)rows * ctas <= device_sms() && a.vocab > 2048 * ctas)))
     ctas *= 2;
   a.slice = ((a.vocab + ctas - 1) / ctas + 7) / 8 * 8;
   if (dev < 0 || dev >= 64 || !done[dev]) {
