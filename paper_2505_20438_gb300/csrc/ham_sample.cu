@@ -16,7 +16,7 @@
 // adds up the cluster's histograms for itself, 16 bytes a load, so that this costs one cluster barrier
 // (2048 bins, added up by shares and read back, took 8500 cycles against 3000).  Then
 //  - where at most 2048 tokens lie up to that bin (the usual case) they are listed, in index order, in
-//    the first CTA's shared memory; that CTA sorts them, makes the exact cuts and picks the token;
+//    the first CTA's shared memory; that CTA makes the exact cuts and picks the token;
 //  - otherwise the bin's own tokens are listed in every CTA, which finds the exact cut among them (where
 //    they too are more than 2048: histograms over 512 parts of the bin, then over the values of l in the
 //    part until one is left); then the cluster sums the kept weights by stretches of the index.
@@ -73,7 +73,7 @@ struct SampleShared {
   int first;                              // first index of the largest logit
   uint64_t found_before_mass, found_mass, aim;
   uint32_t found_before_count, found_count;
-  int found;
+  int found, members, cut_at;
   float cut_value;
   uint32_t cut_ties, cut_by_index;
 };
@@ -532,24 +532,28 @@ struct Row {
     }
     __syncthreads();
   }
-  // s.sorted: the first `many` listed tokens in order, as (key of l, inverted; place in the list), by
-  // a bitonic network: distances below a warp in registers, the others in shared memory.
-  __device__ void sort_list(int many) const {
+  __device__ __forceinline__ uint64_t sort_key(int i) const {
+    return ((uint64_t)~key_of(s.list_l[i]) << 32) | (uint32_t)i;
+  }
+  __device__ __forceinline__ float sorted_logit(uint64_t key) const { return logit_of(~(uint32_t)(key >> 32)); }
+  __device__ __forceinline__ uint32_t listed_weight(int i) const { return weight_of(x_of(s.list_l[i], c)); }
+  // Sorts the first `many` keys of s.sorted (by l, largest first, equal ones by place in the list): a
+  // bitonic network, distances below a warp in registers, the others in shared memory.
+  __device__ void sort(int many) const {
     uint64_t *key = s.sorted;
     int n = 32;
     while (n < many) n *= 2;
-    for (int i = tid; i < n; i += kSampleThreads)
-      key[i] = i < many ? ((uint64_t)~key_of(s.list_l[i]) << 32) | (uint32_t)i : ~0ull;
+    for (int i = many + tid; i < n; i += kSampleThreads) key[i] = ~0ull;
+    __syncthreads();
     for (int size = 32; size <= n; size *= 2) {
       for (int step = size / 2; step >= 32; step /= 2) {
-        __syncthreads();
         for (int q = tid; q < n / 2; q += kSampleThreads) {
           const int i = 2 * q - (q & (step - 1)), o = i + step;
           const uint64_t x = key[i], y = key[o];
           if ((x > y) == ((i & size) == 0)) key[i] = y, key[o] = x;
         }
+        __syncthreads();
       }
-      __syncthreads();
       for (int i = tid; i < n; i += kSampleThreads) {  // (whole warps)
         uint64_t x = key[i];
         for (int sub = size == 32 ? 2 : size; sub <= size; sub *= 2)
@@ -560,31 +564,62 @@ struct Row {
           }
         key[i] = x;
       }
+      __syncthreads();
+    }
+  }
+  // The exact cut among the `n` listed tokens, by this CTA alone: a histogram over 512 bins (`bins`; else
+  // the cut is known to lie in bin `bin`), one over the 512 parts of the cut's bin, then the part's tokens
+  // sorted.  count0, mass0: those of the tokens before bin `bin`; weight(i): of listed token i.  s.sorted
+  // holds the part's tokens in order, s.cut_at the last one kept, s.members their number.
+  template <typename W>
+  __device__ Cut cut_list(int n, bool bins, int bin, bool by_mass, uint64_t aim, uint32_t count0, uint64_t mass0,
+                          W weight) const {
+    float base = (float)bin, mult = bins ? 1.f : (float)kBins;
+    for (;;) {
+      clear();
+      for (int i = tid; i < n; i += kSampleThreads) {
+        const float at = (place_of(s.list_l[i], c) - base) * mult;  // (exact)
+        if (at >= 0.f && at < (float)kBins) {
+          atomicAdd(&s.h.count[(int)at], 1u);
+          add_mass((int)at, weight(i));
+        }
+      }
+      __syncthreads();
+      // (at most 2^11 tokens of 2^31: count and weight in one number)
+      const uint64_t mine = ((uint64_t)s.h.count[tid] << 48) + ((uint64_t)s.h.high[tid] << 16) + s.h.low[tid];
+      uint64_t all;
+      const uint64_t run = block_scan(s, mine, all), ran = run - mine;
+      constexpr uint64_t kMass = (1ull << 48) - 1;
+      const uint64_t upto = by_mass ? mass0 + (run & kMass) : count0 + (run >> 48);
+      const uint64_t before = by_mass ? mass0 + (ran & kMass) : count0 + (ran >> 48);
+      if (upto >= aim && before < aim) {
+        s.found = tid;
+        s.found_before_count = count0 + (uint32_t)(ran >> 48), s.found_before_mass = mass0 + (ran & kMass);
+      }
+      if (tid == 0) s.members = 0;
+      __syncthreads();
+      base += (float)s.found / mult;
+      count0 = s.found_before_count, mass0 = s.found_before_mass;
+      if (mult > 1.f) break;
+      mult = (float)kBins;
+      __syncthreads();
+    }
+    const float end = base + 1.f / kBins;
+    for (int i = tid; i < n; i += kSampleThreads) {
+      const float f = place_of(s.list_l[i], c);
+      if (f >= base && f < end) s.sorted[atomicAdd(&s.members, 1)] = sort_key(i);
     }
     __syncthreads();
-  }
-  __device__ __forceinline__ uint32_t sorted_weight(uint64_t key) const {
-    return weight_of(x_of(logit_of(~(uint32_t)(key >> 32)), c));
-  }
-  // The exact cut within the bin that find() gave for the aim.
-  __device__ Cut cut(bool by_mass, uint64_t aim) const {
-    if (s.found_count > (uint32_t)kList) return cut_by_bins(by_mass, aim);
-    const uint32_t count = s.found_before_count;
-    const uint64_t mass = s.found_before_mass;
-    const int bin = s.found;
-    __syncthreads();
-    const int many = (int)list(bin, bin);
-    pull(many);
-    sort_list(many);
-    uint64_t at = mass;
+    const int many = s.members;
+    sort(many);
+    uint64_t at = mass0;
     for (int i0 = 0; i0 < many; i0 += kSampleThreads) {
       const int i = i0 + tid;
-      const uint64_t key = i < many ? s.sorted[i] : ~0ull;
-      const uint64_t w = i < many ? sorted_weight(key) : 0;
+      const uint64_t key = i < many ? s.sorted[i] : ~0ull, w = i < many ? weight((int)(uint32_t)key) : 0;
       uint64_t part;
       const uint64_t upto = at + block_scan(s, w, part);
       // the last token kept, and how many of its equals are kept with it
-      if (i < many && (by_mass ? upto >= aim && upto - w < aim : count + i + 1 == aim)) {
+      if (i < many && (by_mass ? upto >= aim && upto - w < aim : (uint64_t)count0 + i + 1 == aim)) {
         const uint32_t l = (uint32_t)(key >> 32);
         int from = 0, to = i;                    // the first of the equal ones
         while (from < to) {
@@ -592,6 +627,7 @@ struct Row {
           if ((uint32_t)(s.sorted[mid] >> 32) < l) from = mid + 1;
           else to = mid;
         }
+        s.cut_at = i;
         s.cut_value = logit_of(~l);
         s.cut_ties = i - from + 1;
         s.cut_by_index = i + 1 < many && (uint32_t)(s.sorted[i + 1] >> 32) == l;
@@ -607,46 +643,77 @@ struct Row {
     k.mass = s.found_mass;
     return k;
   }
-  // The choice among the first CTA's list of `all` tokens, by that CTA alone: kPer tokens a thread.
-  // k > 0: top-k.  p >= 0: top-p, of the weight `row_mass` (0: of the list's, after top-k).
-  template <int kPer>
-  __device__ void choose(const SampleArgs &a, int row, int all, int k, double p, uint64_t row_mass, uint32_t least) const {
-    uint32_t *list_w = s.own;                  // (its places are pulled)
-    sort_list(all);
-    if (k <= 0 || k > all) k = all;
-    uint64_t key[kPer], mass = 0, whole;
+  // The exact cut within the bin that find() gave for the aim, the same in every CTA of the cluster.
+  __device__ Cut cut(bool by_mass, uint64_t aim) const {
+    if (s.found_count > (uint32_t)kList) return cut_by_bins(by_mass, aim);
+    const uint32_t count = s.found_before_count;
+    const uint64_t mass = s.found_before_mass;
+    const int bin = s.found;
+    __syncthreads();
+    const int many = (int)list(bin, bin);
+    pull(many);
+    sync();                                      // (the histograms' and the lists' last readers are done)
+    return cut_list(many, false, bin, by_mass, aim, count, mass, [&](int i) { return listed_weight(i); });
+  }
+  // The choice among the first CTA's list of `all` tokens up to bin `last`, by that CTA alone.  k > 0:
+  // top-k, which cuts in bin `last`, before which lie `before` tokens.  p >= 0: top-p, of the weight
+  // `row_mass` (0: of the list's, after top-k).  Up to a token a thread are sorted; of more, only the
+  // cuts' parts are.
+  __device__ void choose(const SampleArgs &a, int row, int all, int last, uint32_t before, int k, double p,
+                         uint64_t row_mass, uint32_t least) const {
+    constexpr int kPer = kList / kSampleThreads;
+    uint32_t *list_w = s.own;                    // (its places are pulled)
+    uint64_t whole = row_mass;
+    if (k > all) k = 0;
+    if (all <= kSampleThreads) {
+      if (tid < all) s.sorted[tid] = sort_key(tid);
+      sort(all);
+      const uint64_t key = tid < all ? s.sorted[tid] : ~0ull;
+      const uint32_t w = tid < all && (k <= 0 || tid < k) ? weight_of(x_of(sorted_logit(key), c)) : 0;
+      uint64_t sum, aim = ~0ull;
+      const uint64_t run = block_scan(s, w, sum) - w;
+      if (p >= 0.) {
+        if (tid == 0) s.aim = aim_of(p, row_mass ? row_mass : sum);
+        __syncthreads();
+        aim = s.aim;
+      }
+      if (tid < all) list_w[(uint32_t)key] = run < aim ? w : 0u;
+    } else {
+      for (int i = tid; i < all; i += kSampleThreads) list_w[i] = listed_weight(i);
+      __syncthreads();
+      const auto weight = [&](int i) { return list_w[i]; };
+      const auto drop = [&](const Cut &x) {      // what the cut leaves out
+        for (int i = tid; i < all; i += kSampleThreads)
+          if (s.list_l[i] < x.value) list_w[i] = 0;
+        for (int i = s.cut_at + 1 + tid; i < s.members; i += kSampleThreads) list_w[(uint32_t)s.sorted[i]] = 0;
+        __syncthreads();
+      };
+      if (k > 0) drop(cut_list(all, false, last, false, (uint64_t)k, before, 0, weight));
+      if (p >= 0.) {
+        if (!row_mass) {
+          uint64_t mine = 0;
+          for (int i = tid; i < all; i += kSampleThreads) mine += list_w[i];
+          block_scan(s, mine, whole);
+        }
+        if (tid == 0) s.aim = aim_of(p, whole);
+        __syncthreads();
+        drop(cut_list(all, true, 0, true, s.aim, 0, 0, weight));
+      }
+    }
+    __syncthreads();
+    uint64_t mass = 0;
     uint32_t w[kPer];
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
       const int i = tid * kPer + j;
-      key[j] = i < all ? s.sorted[i] : ~0ull;
-      w[j] = i < k ? sorted_weight(key[j]) : 0;
-      mass += w[j];
-    }
-    uint64_t run = block_scan(s, mass, whole) - mass, aim = ~0ull;
-    if (p >= 0.) {
-      if (tid == 0) s.aim = aim_of(p, row_mass ? row_mass : whole);
-      __syncthreads();
-      aim = s.aim;
-    }
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int i = tid * kPer + j;
-      if (i < all) list_w[(uint32_t)key[j]] = run < aim && w[j] >= least ? w[j] : 0u;
-      run += w[j];
-    }
-    __syncthreads();
-    mass = 0;                                    // from here on by index
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int i = tid * kPer + j;
       w[j] = i < all ? list_w[i] : 0u;
+      if (w[j] < least) w[j] = 0;
       mass += w[j];
     }
     uint64_t sum = block_scan(s, mass, whole) - mass;
     if (tid == 0) s.aim = pick(a.u[row], whole);
     __syncthreads();
-    aim = s.aim;
+    const uint64_t aim = s.aim;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
       if (sum <= aim && aim < sum + w[j]) {
@@ -768,12 +835,8 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
       if (listed <= (uint32_t)kList) {           // (all_in: known only now)
         if (rank == 0) r.pull(listed);
         if (ctas > 1) cluster_arrive();          // (the others' lists are pulled)
-        if (rank == 0) {
-          const int n_k = by_k ? k : 0;
-          const double n_p = by_p ? share : -1.;
-          if (listed <= (uint32_t)kSampleThreads) r.template choose<1>(a, row, listed, n_k, n_p, whole, least);
-          else r.template choose<kList / kSampleThreads>(a, row, listed, n_k, n_p, whole, least);
-        }
+        if (rank == 0)
+          r.choose(a, row, listed, last, before, by_k && !all_in ? k : 0, by_p ? share : -1., whole, least);
         if (ctas > 1) cluster_wait();
         return;
       }
