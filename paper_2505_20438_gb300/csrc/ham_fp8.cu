@@ -111,7 +111,8 @@ __device__ __forceinline__ void store4(const ProductArgs &a, int64_t row, int c,
 // requested before the dependency wait: nothing on the stream writes them.
 constexpr int kStreamThreads = 256;
 constexpr int kStreamSf = 4;            // scale slots (of four K blocks each)
-constexpr int kStreamSmem = 104 * 1024; // of a CTA: two share an SM
+constexpr int kStreamSmem2 = 104 * 1024; // shared memory of a CTA: two share an SM
+constexpr int kStreamSmem3 = 72 * 1024;  // ... three
 
 constexpr int kStreamStages = 12;       // at most
 constexpr int kStreamBars = (2 * kStreamStages + 2 * kStreamSf + 1) * 8;
@@ -724,13 +725,19 @@ cudaError_t launch_stream(const CUtensorMap &tx, ProductArgs a, int dev, cudaStr
   int splits = 1;
   while (splits < 8 && splits * 2 <= a.kbs && (int64_t)a.tiles * zt * splits <= sms) splits *= 2;
   a.stage_bytes = kParts * kBlockBytes + a.nt * 128;
-  const int per = (a.kbs + splits - 1) / splits;      // K blocks of a CTA
-  a.stages = std::min(std::min(per, kStreamStages), (kStreamSmem - stream_fixed(kParts)) / a.stage_bytes);
-  const int acc = kParts * a.nt * kTile * 4;          // the epilogue's, in the ring
-  a.stages = std::max(std::max(a.stages, 2), (acc + a.stage_bytes - 1) / a.stage_bytes);
   int cols = 32;
   while (cols < kParts * a.nt + 2 * (kParts + 1) * 4) cols *= 2;
   a.tmem_cols = cols;
+  const int per = (a.kbs + splits - 1) / splits;      // K blocks of a CTA
+  // A grid of one wave runs fastest with the deepest rings that leave two CTAs an SM; over several waves
+  // a third CTA covers the others' beginnings and ends (head of 128256 features, 64 rows: 94 us with
+  // two an SM, 85 with three; 16384 + 16384 features of 8 rows: 22.7 with either; a second projection
+  // of 16384 in 4096 features: 14.1 with two, 14.8 with three).
+  const bool three = (int64_t)a.tiles * zt * splits > 2 * sms && 3 * cols <= 512;
+  const int budget = three ? kStreamSmem3 : kStreamSmem2;
+  a.stages = std::min(std::min(per, kStreamStages), (budget - stream_fixed(kParts)) / a.stage_bytes);
+  const int acc = kParts * a.nt * kTile * 4;          // the epilogue's, in the ring
+  a.stages = std::max(std::max(a.stages, 2), (acc + a.stage_bytes - 1) / a.stage_bytes);
   const int smem = std::max(a.stages * a.stage_bytes + stream_fixed(kParts), splits > 1 ? smem_floor(cols) : 0);
   cudaError_t e = allow_smem(fp8_stream_kernel<kParts>, 226 * 1024, done, dev);
   if (e != cudaSuccess) return e;
@@ -788,7 +795,8 @@ int run_product(ham_fp8_weight *w, const void *x_codes, const void *x_scales, in
   a.f32 = f32;
   const int64_t tiles = (int64_t)((rows + 255) / 256) * (w->parts == 2 ? w->tiles : (w->tiles + 1) / 2);
   const bool pair = rows > 128 && tiles * 2 >= device_sms();
-  a.nt = std::min(128, (rows + 15) / 16 * 16);
+  const int row_parts = (rows + 127) / 128;           // the streaming kernel's, of equal size
+  a.nt = ((rows + row_parts - 1) / row_parts + 15) / 16 * 16;
   CUtensorMap tx;
   int rc = HAM_OK;
   if (make_bytes_tensor_map(&tx, x_codes, rows, w->k, kFp8Block, pair ? 128 : a.nt, true) != 0) {
