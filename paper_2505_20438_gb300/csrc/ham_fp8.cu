@@ -154,12 +154,17 @@ __global__ void __launch_bounds__(kStreamThreads)
     fence_mbar_init();
   }
   if (warp == 0 && lane == 0) prefetch_tensormap(&tx);
-  if (warp == 1) tmem_alloc_n(&tmem_slot, (uint32_t)a.tmem_cols);
-  tc_fence_before();
   __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = tmem_slot;
-  const uint32_t sf_tmem = tmem + kParts * a.nt;      // two buffers of (kParts + 1) * 4 columns
+  // Tensor memory is taken before the dependency wait (after it, 1.3 us of a call of 6.5 were spent on
+  // it) and before the next kernel may start: a kernel that holds columns and waits for this one while
+  // this one still wants some would keep both waiting.  Of the kernels that may still run before this
+  // one, those that take columns do so before they let anything start, or fill their SMs' shared memory.
+  if (warp > 0) {
+    if (warp == 1) tmem_alloc_n(&tmem_slot, (uint32_t)a.tmem_cols);
+    tc_fence_before();
+    named_barrier(1, kStreamThreads - 32);
+    tc_fence_after();
+  }
   int issued = 0;
 
   if (warp == 0) {
@@ -193,6 +198,8 @@ __global__ void __launch_bounds__(kStreamThreads)
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------ products
+    const uint32_t tmem = *const_cast<volatile uint32_t *>(&tmem_slot);
+    const uint32_t sf_tmem = tmem + kParts * a.nt;    // two buffers of (kParts + 1) * 4 columns
     bool ok = true;
     for (int t = 0; t < nk; ++t) {
       const int s = t % stages, kb = kb0 + t, g = (kb >> 2) - g0;
@@ -272,6 +279,7 @@ __global__ void __launch_bounds__(kStreamThreads)
   __syncwarp();
   bool ok = warp_wait(acc_full, 0u, abort_flag);
   ok = ok && !__any_sync(kFull, *abort_flag != 0);
+  const uint32_t tmem = *const_cast<volatile uint32_t *>(&tmem_slot);
   float *acc = reinterpret_cast<float *>(ring);
   if (ok) {
     tc_fence_after();
@@ -430,11 +438,14 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     prefetch_tensormap(&tx);
     prefetch_tensormap(&tw);
   }
-  if (warp == 1) tmem_alloc_pair<512>(&tmem_slot);
-  tc_fence_before();
   cluster_sync_all();
-  tc_fence_after();
-  const uint32_t tmem = tmem_slot;
+  if (warp > 0) {  // (tensor memory: as in the streaming kernel)
+    if (warp == 1) tmem_alloc_pair<512>(&tmem_slot);
+    tc_fence_before();
+    named_barrier(5, kPairThreads - 32);
+    tc_fence_after();
+  }
+  const uint32_t tmem = *const_cast<volatile uint32_t *>(&tmem_slot);  // (not warp 0's)
   int issued = 0;
 
   if (warp == 0) {
