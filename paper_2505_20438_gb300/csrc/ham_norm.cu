@@ -39,7 +39,13 @@ struct NormArgs {
   uint8_t *scales;         // with codes: [rows][sk]
   int hidden, vecs, blocks, sk;   // vecs = hidden / 8, blocks = ceil(hidden / 128)
   float eps;
+  int far;                 // the outputs pass L2: nothing is gained by keeping them there
 };
+template <typename V>
+__device__ __forceinline__ void put(V *p, const V &v, int far) {
+  if (far) __stcs(p, v);
+  else *p = v;
+}
 
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
@@ -67,7 +73,7 @@ __device__ __forceinline__ uint2 encode8(const float (&y)[8], uint32_t &scale) {
 
 // A block is one row, a thread the groups tid, tid + threads, ... of 8 elements.
 template <int kGroups>
-__global__ void __launch_bounds__(kGroups == 4 ? 1024 : 512) add_norm_kernel(NormArgs a) {
+__global__ void __launch_bounds__(kGroups >= 4 ? 1024 : 512) add_norm_kernel(NormArgs a) {
   __shared__ float part[32];
   const int tid = threadIdx.x, threads = blockDim.x;
   const int64_t row = blockIdx.x;
@@ -101,7 +107,7 @@ __global__ void __launch_bounds__(kGroups == 4 ? 1024 : 512) add_norm_kernel(Nor
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) {
       const int v = tid + g * threads;
-      if (v < a.vecs) a.sum[at + v] = pack8(h[g]);
+      if (v < a.vecs) put(a.sum + at + v, pack8(h[g]), a.far);
     }
   }
   uint4 vw[kGroups];
@@ -125,12 +131,12 @@ __global__ void __launch_bounds__(kGroups == 4 ? 1024 : 512) add_norm_kernel(Nor
     unpack8(vw[g], w);
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = h[g][i] * inv * w[i];
-    if (a.out && v < a.vecs) a.out[at + v] = pack8(y);
+    if (a.out && v < a.vecs) put(a.out + at + v, pack8(y), a.far);
     if (a.codes) {  // (whole warps take part in the shuffles)
       uint32_t scale;
       const uint2 c = encode8(y, scale);
       if (v < a.vecs) {
-        a.codes[at + v] = c;
+        put(a.codes + at + v, c, a.far);
         if ((tid & 15) == 0) a.scales[row * a.sk + (v >> 4)] = (uint8_t)scale;
       }
     }
@@ -247,8 +253,13 @@ int ham_add_norm(const void *x, const void *residual, const void *weight, float 
   a.blocks = (hidden + ham::kFp8Block - 1) / ham::kFp8Block;
   a.sk = ham::fp8_scale_bytes(hidden);
   a.eps = eps;
+  a.far = 2 * e * (!!sum_out + !!out) + e * !!codes > ((size_t)64 << 20);
+  // Few rows: short chains a thread.  Many: more of a row a thread, so that more rows are in flight an SM
+  // (16384 rows of 4096, residual and 8-bit output: 76 us with 512 threads a row, 70 with 256, 68 with
+  // streaming stores).
+  const int most = rows >= 4 * ham::device_sms() ? 256 : 512;
   int groups = 1;
-  while (groups < 4 && a.vecs > groups * 512) groups *= 2;
+  while (groups < 4 && a.vecs > groups * most) groups *= 2;
   const int threads = ((a.vecs + groups - 1) / groups + 31) / 32 * 32;
   auto kernel = groups == 1 ? ham::add_norm_kernel<1> : groups == 2 ? ham::add_norm_kernel<2> : ham::add_norm_kernel<4>;
   const cudaError_t ce = ham::launch_after(kernel, dim3((unsigned)rows), dim3((unsigned)threads), 0,
