@@ -68,7 +68,7 @@ struct SampleShared {
   uint32_t warp_count[kSampleWarps];
   float best, warp_best[kSampleWarps];
   uint32_t key_max, key_min, warp_max[kSampleWarps], warp_min[kSampleWarps];
-  uint64_t kept, warp_kept[kSampleWarps];
+  uint64_t kept;
   uint32_t ties, warp_ties[kSampleWarps];
   int first;                              // first index of the largest logit
   uint64_t found_before_mass, found_mass, aim;
@@ -243,19 +243,37 @@ struct Row {
     const int q = tid & 31;
     return q < ctas ? ld_cluster_u64(peer(p, q)) : 0ull;
   }
-  // The warps' stretches of the vectors, in index order: a step is 32 vectors, one a lane.
-  __device__ __forceinline__ void stretch(int &v0, int &v1) const {
-    const int per = (vecs + kSampleWarps * 32 - 1) / (kSampleWarps * 32) * 32;
-    v0 = min(vecs, (tid >> 5) * per);
-    v1 = min(vecs, v0 + per);
-  }
-  // f(vector) for every vector of this lane.
+  // f(vector) for every vector of this CTA's logits, in any order.
   template <typename F>
   __device__ __forceinline__ void each(F f) const {
+#pragma unroll 2
+    for (int v = tid; v < vecs; v += kSampleThreads) f(Vec<T>(data[v]));
+  }
+  // This thread's stretch of the vectors: the threads' stretches follow one another in index order.  (An
+  // odd number of vectors each, so that a warp's loads of 16 bytes fall on different banks.)
+  __device__ __forceinline__ void stretch(int &v0, int &v1) const {
+    const int per = ((vecs + kSampleThreads - 1) / kSampleThreads) | 1;
+    v0 = min(vecs, tid * per);
+    v1 = min(vecs, v0 + per);
+  }
+  // The vectors of this thread's stretch (bit i: vector v0 + i) that hold a logit for which pred(l); their
+  // number of such logits.
+  template <typename P>
+  __device__ __forceinline__ uint32_t which(P pred, uint32_t &many) const {
     int v0, v1;
     stretch(v0, v1);
+    uint32_t mask = 0;
+    many = 0;
 #pragma unroll 2
-    for (int v = v0 + (tid & 31); v < v1; v += 32) f(Vec<T>(data[v]));
+    for (int v = v0; v < v1; ++v) {
+      const Vec<T> x(data[v]);
+      uint32_t n = 0;
+#pragma unroll
+      for (int j = 0; j < kN; ++j) n += pred(x.l[j]);
+      many += n;
+      mask |= (uint32_t)(n > 0) << (v - v0);
+    }
+    return mask;
   }
   // The histogram of the logits in range by the bins of `where` (negative: left out), counts and / or
   // weights.  Computed for the whole vector first: a vector's chains of arithmetic overlap.
@@ -431,77 +449,34 @@ struct Row {
       lo = kmax - kmin < down ? kmin : kmax - down;
     }
   }
-  // Weights of a vector's logits that the cut and min_p keep (those equal to the cut's value too: where
-  // some of them are cut off, the caller keeps the first by index).
-  __device__ __forceinline__ void kept(const Cut &k, uint32_t least, const Vec<T> &x, uint32_t (&w)[kN]) const {
-#pragma unroll
-    for (int j = 0; j < kN; ++j) {
-      const uint32_t v = weight_of(x_of(x.l[j], c));
-      w[j] = x.l[j] >= k.value && v >= least ? v : 0u;
-    }
-  }
-  // Sum over the warps before this one, and over the CTAs before this one, of a number a warp (all:
-  // over the row).
-  __device__ uint32_t before_me(uint32_t mine, uint32_t &all) const {
-    const int lane = tid & 31, warp = tid >> 5;
-    if (lane == 0) s.warp_ties[warp] = mine;
-    __syncthreads();
-    const uint32_t v = lane < kSampleWarps ? s.warp_ties[lane] : 0u;
-    const uint32_t cta = sum8(v), warps = sum8(lane < warp ? v : 0u);
-    if (tid == 0) s.ties = cta;
-    sync();
-    const uint32_t q = lane32(&s.ties);
-    all = sum8(q);
-    return warps + sum8(lane < rank ? q : 0u);
+  // Weight of l if the cut and min_p keep it (those equal to the cut's value too: where some of them are
+  // cut off, the caller keeps the first by index).
+  __device__ __forceinline__ uint32_t kept(const Cut &k, uint32_t least, float l) const {
+    const uint32_t v = weight_of(x_of(l, c));
+    return l >= k.value && v >= least ? v : 0u;
   }
   // Lists this CTA's tokens of the bins first .. last, by index; the row's number of them.  If that is at
   // most kList, pull() then makes the row's list.
   __device__ uint32_t list(int first, int last) const {
-    const int lane = tid & 31, warp = tid >> 5;
     const float begin = (float)first, end = (float)(last + 1);  // (last < 511: a token up to it has a bin)
-    int v0, v1;
-    stretch(v0, v1);
-    uint32_t many = 0;
-#pragma unroll 2
-    for (int v = v0 + lane; v < v1; v += 32) {
-      const Vec<T> x(data[v]);
-#pragma unroll
-      for (int j = 0; j < kN; ++j) {
-        const float f = place_of(x.l[j], c);
-        many += f < end && f >= begin;
-      }
-    }
-    const uint32_t who_has = __ballot_sync(kFull, many > 0);
-    many = __reduce_add_sync(kFull, many);
-    if (lane == 0) s.warp_ties[warp] = many;
-    __syncthreads();
-    const uint32_t others = lane < kSampleWarps ? s.warp_ties[lane] : 0u;
-    const uint32_t cta = sum8(others);
-    uint32_t at = sum8(lane < warp ? others : 0u);
-    if (tid == 0) s.ties = cta;
-    if (who_has && cta <= (uint32_t)kList) {
-      const uint32_t below = (1u << lane) - 1u;
-      for (int v = v0; v < v1; v += 32) {
-        const Vec<T> x((who_has >> lane & 1u) && v + lane < v1 ? data[v + lane] : Vec<T>::none());
-        bool in[kN], any = false;
-#pragma unroll
-        for (int j = 0; j < kN; ++j) {
-          const float f = place_of(x.l[j], c);
-          in[j] = f < end && f >= begin, any |= in[j];
-        }
-        if (!__any_sync(kFull, any)) continue;
-        uint32_t mine = at;
-#pragma unroll
-        for (int j = 0; j < kN; ++j) {
-          const uint32_t who = __ballot_sync(kFull, in[j]);
-          mine += __popc(who & below);
-          at += __popc(who);
-        }
+    const auto in = [&](float l) {
+      const float f = place_of(l, c);
+      return f < end && f >= begin;
+    };
+    uint32_t many;
+    uint32_t mask = which(in, many);
+    uint64_t cta;
+    uint32_t at = (uint32_t)block_scan(s, many, cta) - many;
+    if (tid == 0) s.ties = (uint32_t)cta;
+    if (cta <= kList) {
+      int v0, v1;
+      stretch(v0, v1);
+      for (; mask; mask &= mask - 1) {
+        const int v = v0 + __ffs(mask) - 1;
+        const Vec<T> x(data[v]);
 #pragma unroll
         for (int j = 0; j < kN; ++j)
-          if (in[j]) {
-            s.own[mine++] = (v + lane) * kN + j;
-          }
+          if (in(x.l[j])) s.own[at++] = v * kN + j;
       }
     }
     sync();
@@ -859,97 +834,81 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
     }
     if (by_p) cut = r.cut(true, aim);
   }
-  // ---- the kept weights of each warp's stretch of the slice, in index order
+  // ---- the kept weights of each thread's stretch of the slice, in index order
+  uint32_t ties_before = 0, mine, ties_all;
+  if (cut.by_index) {
+    r.which([&](float l) { return l == cut.value; }, mine);
+    uint64_t cta;
+    ties_before = (uint32_t)block_scan(s, mine, cta) - mine;
+    r.sync();                                    // (s.ties: its last readers are done)
+    if (tid == 0) s.ties = (uint32_t)cta;
+    r.sync();
+    ties_all = r.lane32(&s.ties);
+    ties_before += sum8(lane < rank ? ties_all : 0u);
+  }
   int v0, v1;
   r.stretch(v0, v1);
-  uint32_t ties_before = 0;
-  if (cut.by_index) {
-    uint32_t ties = 0, all;
-    for (int v = v0 + lane; v < v1; v += 32) {
+  uint64_t sum = 0;
+  if (cut.value == -INFINITY) {
+    for (int v = v0; v < v1; ++v) {
       const Vec<T> x(store[v]);
 #pragma unroll
-      for (int j = 0; j < kVec; ++j) ties += x.l[j] == cut.value;
+      for (int j = 0; j < kVec; ++j) sum += r.kept(cut, least, x.l[j]);
     }
-    ties = __reduce_add_sync(kFull, ties);
-    r.sync();                                    // (s.ties: its last readers are done)
-    ties_before = r.before_me(ties, all);
-  }
-  // one step of 32 vectors: this lane's kept weights (ties: those before this step)
-  auto step = [&](int v, uint32_t &ties, uint32_t (&w)[kVec]) {
-    const Vec<T> x(v < v1 ? store[v] : Vec<T>::none());
-    r.kept(cut, least, x, w);
-    if (cut.by_index) {
-      uint32_t mine = ties;
+  } else {                                       // (few of a long row's: only their vectors are weighed)
+    uint32_t ties = ties_before;
+    for (uint32_t mask = r.which([&](float l) { return l >= cut.value; }, mine); mask; mask &= mask - 1) {
+      const Vec<T> x(store[v0 + __ffs(mask) - 1]);
 #pragma unroll
       for (int j = 0; j < kVec; ++j) {
-        const uint32_t who = __ballot_sync(kFull, x.l[j] == cut.value);
-        mine += __popc(who & ((1u << lane) - 1u));
-        ties += __popc(who);
+        const uint32_t w = r.kept(cut, least, x.l[j]);
+        if (!(cut.by_index && x.l[j] == cut.value && ties++ >= cut.ties)) sum += w;
       }
-#pragma unroll
-      for (int j = 0; j < kVec; ++j)
-        if (x.l[j] == cut.value && mine++ >= cut.ties) w[j] = 0;
     }
-  };
-  uint64_t sum = 0;
-  uint32_t ties = ties_before;
-  for (int v = v0; v < v1; v += 32) {
-    uint32_t w[kVec];
-    step(v + lane, ties, w);
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) sum += w[j];
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kFull, sum, o);
-  if (lane == 0) s.warp_kept[warp] = sum;
-  __syncthreads();
-  uint64_t warps = 0, cta = 0;
-#pragma unroll
-  for (int q = 0; q < kSampleWarps; ++q) {
-    const uint64_t v = s.warp_kept[q];
-    if (q < warp) warps += v;
-    cta += v;
-  }
+  uint64_t cta;
+  uint64_t before = block_scan(s, sum, cta) - sum;
   if (tid == 0) s.kept = cta;
   r.sync();
   const uint64_t theirs = r.lane64(&s.kept), total = sum8(theirs);
-  uint64_t before = warps + sum8(lane < rank ? theirs : (uint64_t)0);
+  before += sum8(lane < rank ? theirs : (uint64_t)0);
   if (warp == 0) {
     const uint64_t v = Row<T>::pick(a.u[row], total);
     if (lane == 0) s.aim = v;
   }
   __syncthreads();
   const uint64_t aim = s.aim;
-  if (before <= aim && aim < before + sum) {     // one warp of the cluster
-    ties = ties_before;
-    for (int v = v0; v < v1; v += 32) {
-      uint32_t w[kVec];
-      step(v + lane, ties, w);
-      uint64_t mine = 0;
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) mine += w[j];
-      uint64_t run = mine;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const uint64_t u = __shfl_up_sync(kFull, run, o);
-        if (lane >= o) run += u;
+  // one thread of the cluster has the token in its stretch: its warp looks for it, a lane a logit
+  const uint32_t owner = __ballot_sync(kFull, before <= aim && aim < before + sum);
+  if (owner) {
+    const int o = __ffs(owner) - 1;
+    const int from = __shfl_sync(kFull, v0, o) * kVec, to = __shfl_sync(kFull, v1, o) * kVec;
+    uint64_t at = __shfl_sync(kFull, before, o);
+    uint32_t ties = __shfl_sync(kFull, ties_before, o);
+    const T *logits = reinterpret_cast<const T *>(store);
+    for (int i0 = from; i0 < to; i0 += 32) {
+      const float l = i0 + lane < to ? load_logit(logits + i0 + lane) : -INFINITY;
+      uint32_t w = r.kept(cut, least, l);
+      if (cut.by_index) {
+        const uint32_t equal = __ballot_sync(kFull, l == cut.value);
+        if (l == cut.value && ties + __popc(equal & ((1u << lane) - 1u)) >= cut.ties) w = 0;
+        ties += __popc(equal);
       }
-      const uint32_t over = __ballot_sync(kFull, before + run > aim);
+      uint64_t run = w;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const uint64_t v = __shfl_up_sync(kFull, run, d);
+        if (lane >= d) run += v;
+      }
+      const uint32_t over = __ballot_sync(kFull, at + run > aim);
       if (over) {
         if (lane == __ffs(over) - 1) {
-          uint64_t at = before + run - mine;
-#pragma unroll
-          for (int j = 0; j < kVec; ++j) {
-            if (at <= aim && aim < at + w[j]) {
-              a.tokens[row] = r.first_index + (v + lane) * kVec + j;
-              if (a.probs) a.probs[row] = (float)((double)w[j] / (double)total);
-            }
-            at += w[j];
-          }
+          a.tokens[row] = r.first_index + i0 + lane;
+          if (a.probs) a.probs[row] = (float)((double)w / (double)total);
         }
         break;
       }
-      before += __shfl_sync(kFull, run, 31);
+      at += __shfl_sync(kFull, run, 31);
     }
   }
   r.sync();  // (a peer may still read this CTA's sums)
