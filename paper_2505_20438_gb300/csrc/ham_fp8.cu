@@ -33,7 +33,7 @@ struct ham_fp8_weight {
   uint8_t *scales = nullptr;   // [tiles][parts][sk]
   int32_t *err = nullptr;      // device error word
   int32_t *host_err = nullptr; // pinned
-  CUtensorMap map;             // codes as [tiles * kbs * parts * 128][128] bytes, boxes of half a block
+  CUtensorMap map;             // codes as one stretch, boxes of half a block
 };
 
 namespace ham {
@@ -355,40 +355,74 @@ __global__ void __launch_bounds__(kStreamThreads)
 // accumulators (256 columns each) share 64 columns, which leaves the columns 448.. for the scales: a
 // tile's epilogue takes the shared columns into registers first, and the next tile's products begin when
 // it has.
-constexpr int kPairThreads = 384;       // warps: copies, products, scales, -, 8 x epilogue
+constexpr int kPairThreads = 384;       // warps: copies, products, 2 x scales, 8 x epilogue
 constexpr int kPairStages = 6;
 constexpr int kPairStageBytes = 2 * kBlockBytes;
 constexpr int kPairSf = 4;
 constexpr int kPairSfBytes = 3 * 512;   // the CTA's 128 rows, both weight tiles
 constexpr int kPairBuf1 = 192, kPairSfCol = 448;
-constexpr int kPairSmem = smem_floor(512);
-static_assert(kPairSmem >= 1024 + kPairStages * kPairStageBytes + kPairSf * kPairSfBytes + 256 &&
-                  kPairSmem <= 226 * 1024, "shared memory");
+constexpr int kTurn = 17;               // floats a row of a warp's turning space: 16 columns, padded
+constexpr int kPairUsed = 1024 + kPairStages * kPairStageBytes + kPairSf * kPairSfBytes + 256 + 8 * 32 * kTurn * 4;
+constexpr int kPairSmem = kPairUsed > smem_floor(512) ? kPairUsed : smem_floor(512);
+static_assert(kPairSmem <= 226 * 1024, "shared memory");
 
-// 32 accumulator columns of one row (from column c of n) to the output.
-__device__ __forceinline__ void store32(const ProductArgs &a, int row, int c, const uint32_t *v, bool wide) {
+// 32 accumulator columns (from column c of n) of a warp's 32 rows, a row a lane, to the output: `bytes` at a
+// time a lane where rows begin at multiples of 32 or 16 bytes, and else turned in shared memory so that
+// 16 lanes write neighbours (a value at a time, 32 rows an instruction: 164 us for 3000 x 5003 outputs
+// of 2000 columns, against 27 us for 5008).
+__device__ __forceinline__ void store32(const ProductArgs &a, int row0, int c, const uint32_t (&v)[32], int bytes,
+                                        float *turn) {
   const float *f = reinterpret_cast<const float *>(v);
-  if (wide && c + 32 <= a.n) {
-    char *dst = static_cast<char *>(a.out) + ((int64_t)row * a.n + c) * (a.f32 ? 4 : 2);
+  const int lane = threadIdx.x & 31, row = row0 + lane;
+  if (c >= a.n) return;
+  if (bytes == 0) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      if (a.f32) {
-        uint32_t w[8];
+    for (int h = 0; h < 2; ++h) {
+      __syncwarp();
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = v[8 * q + j];
-        st_global_32(dst + 32 * q, w);
-      } else if (q < 2) {
-        uint32_t w[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = pack_bf16x2(f[16 * q + 2 * j], f[16 * q + 2 * j + 1]);
-        st_global_32(dst + 32 * q, w);
+      for (int j = 0; j < 16; ++j) turn[lane * kTurn + j] = f[16 * h + j];
+      __syncwarp();
+      const int col = c + 16 * h + (lane & 15);
+#pragma unroll 4
+      for (int i = 0; i < 16; ++i) {
+        const int r = 2 * i + (lane >> 4);
+        if (row0 + r < a.rows && col < a.n) {
+          const float x = turn[r * kTurn + (lane & 15)];
+          const int64_t at = (int64_t)(row0 + r) * a.n + col;
+          if (a.f32) static_cast<float *>(a.out)[at] = x;
+          else static_cast<__nv_bfloat16 *>(a.out)[at] = __float2bfloat16_rn(x);
+        }
       }
     }
     return;
   }
+  if (row >= a.rows) return;
+  char *dst = static_cast<char *>(a.out) + ((int64_t)row * a.n + c) * (a.f32 ? 4 : 2);
+  // 32 bytes (from column `at` of the 32), or their two halves where the row ends between them
+  auto put = [&](int at, int each, const uint32_t (&w)[8]) {
+    char *to = dst + at * (32 / (2 * each));
+    if (bytes == 32) {
+      if (c + at < a.n) st_global_32(to, w);
+    } else {
+      if (c + at < a.n) *reinterpret_cast<uint4 *>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+      if (c + at + each < a.n) *reinterpret_cast<uint4 *>(to + 16) = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+  };
+  if (a.f32) {
 #pragma unroll
-  for (int q = 0; q < 8; ++q)
-    if (c + 4 * q < a.n) store4(a, row, c + 4 * q, make_float4(f[4 * q], f[4 * q + 1], f[4 * q + 2], f[4 * q + 3]));
+    for (int q = 0; q < 4; ++q) {
+      const uint32_t w[8] = {v[8 * q], v[8 * q + 1], v[8 * q + 2], v[8 * q + 3], v[8 * q + 4], v[8 * q + 5], v[8 * q + 6], v[8 * q + 7]};
+      put(8 * q, 4, w);
+    }
+  } else {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      uint32_t w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = pack_bf16x2(f[16 * q + 2 * j], f[16 * q + 2 * j + 1]);
+      put(16 * q, 8, w);
+    }
+  }
 }
 
 template <bool kGated, int kPairs>
@@ -407,6 +441,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   uint64_t *acc_shared_free = acc_full + 2;    // an arrival an epilogue warp of the pair
   uint64_t *drained = acc_shared_free + 1;     // every product issued is complete (after an abort)
   static_assert((2 * kPairStages + 2 * kPairSf + 4) * 8 <= 256, "barriers");
+  float *turn = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(full) + 256);  // [8 warps][32][kTurn]
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_shared;
   __shared__ float row_max[2][128];            // gated: largest magnitude of a row's half
@@ -470,13 +505,13 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           if (side == 0) mbar_arrive_tx(&full[s], 2 * kPairStageBytes);  // what lands in both CTAs
           const uint32_t bar = cluster_map_shared(smem_u32(&full[s]), first);
           uint8_t *dst = ring + s * kPairStageBytes;
-          const int w_row = (int)((block + (int64_t)kb * (kGated ? 2 : 1)) * 128);
+          const int w_row = (int)((block + (int64_t)kb * (kGated ? 2 : 1)) * (kBlockBytes / 2048));
           tma_load_2d_pair(dst, &tx, kb * kFp8Block, x_row, bar, pol);
           if constexpr (kPairs == 1) {
             tma_load_2d_pair(dst + kBlockBytes, &tw, 0, w_row, bar, pol);
-            tma_load_2d_pair(dst + kBlockBytes + kBlockBytes / 2, &tw, 0, w_row + 64, bar, pol);
+            tma_load_2d_pair(dst + kBlockBytes + kBlockBytes / 2, &tw, 0, w_row + kBlockBytes / 4096, bar, pol);
           } else {  // this pair's half of the tile, for both
-            tma_load_2d_pair_multicast(dst + kBlockBytes + pair * (kBlockBytes / 2), &tw, 0, w_row + pair * 64, bar,
+            tma_load_2d_pair_multicast(dst + kBlockBytes + pair * (kBlockBytes / 2), &tw, 0, w_row + pair * (kBlockBytes / 4096), bar,
                                        5u << side, pol);
           }
           issued = it + 1;
@@ -535,47 +570,56 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         __syncwarp();
       }
     }
-  } else if (warp == 2) {
+  } else if (warp < 4) {
     // ------------------------------------------------------------ scale words
+    // Two warps take turns at the words (of four K blocks each), and each loads its next before it
+    // passes one on: the passing on, released at cluster scope, takes about as long as four K blocks'
+    // products do (with one warp it set the pace: 16384 columns, 4096 x 4096, 199 us against 163).
     grid_dependency_wait();
-    grid_launch_dependents();
-    const int groups = (a.kbs + 3) / 4;
-    bool ok = true;
-    int gi = 0;
-    for (int w = cluster; w < total && ok; w += clusters) {
-      const int rt = w % row_groups * kPairs + pair, ct = w / row_groups;
-      const int x_row = rt * 256 + side * 128;
-      for (int g = 0; g < groups; ++g, ++gi) {
-        const int slot = gi % kPairSf;
-        uint32_t x[4], ws[2];
+    if (warp == 2) grid_launch_dependents();
+    const int groups = (a.kbs + 3) / 4, turn = warp - 2;
+    uint32_t x[4], ws[2];
+    auto load = [&](int w, int g) {
+      const int rt = w % row_groups * kPairs + pair, ct = w / row_groups, x_row = rt * 256 + side * 128;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int r = x_row + lane + 32 * j;
-          x[j] = r < a.rows ? __ldg(reinterpret_cast<const uint32_t *>(a.xs + (int64_t)r * a.sk) + g) : 0x7f7f7f7fu;
-        }
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {  // the tile's scale rows: [tile][part]
-          const int row = ct * 2 + p;
-          ws[p] = kGated || row < a.tiles
-                      ? __ldg(reinterpret_cast<const uint32_t *>(a.ws + (int64_t)row * a.sk) + g)
-                      : 0x7f7f7f7fu;
-        }
-        if (gi >= kPairSf && !warp_wait(&sf_empty[slot], (uint32_t)(gi / kPairSf - 1) & 1u, abort_flag)) {
-          ok = false;
-          break;
-        }
-        uint4 *dst = reinterpret_cast<uint4 *>(sf + slot * kPairSfBytes) + lane;
-        dst[0] = make_uint4(x[0], x[1], x[2], x[3]);
-        dst[32] = make_uint4(ws[0], ws[0], ws[0], ws[0]);
-        dst[64] = make_uint4(ws[1], ws[1], ws[1], ws[1]);
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(cluster_map_shared(smem_u32(&sf_full[slot]), first));
+      for (int j = 0; j < 4; ++j) {
+        const int r = x_row + lane + 32 * j;
+        x[j] = r < a.rows ? __ldg(reinterpret_cast<const uint32_t *>(a.xs + (int64_t)r * a.sk) + g) : 0x7f7f7f7fu;
       }
-    }
-    if (!ok && lane == 0 && !*abort_flag) {
-      record_error(a.err, HAM_DEVERR_TIMEOUT);
-      *abort_flag = 1;
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {  // the tile's scale rows: [tile][part]
+        const int row = ct * 2 + p;
+        ws[p] = kGated || row < a.tiles
+                    ? __ldg(reinterpret_cast<const uint32_t *>(a.ws + (int64_t)row * a.sk) + g)
+                    : 0x7f7f7f7fu;
+      }
+    };
+    // the gi-th word of this cluster's tiles is word g of tile w
+    int w = cluster, g = turn;
+    auto settle = [&] {
+      while (g >= groups) g -= groups, w += clusters;
+    };
+    settle();
+    if (w < total) load(w, g);
+    for (int gi = turn; w < total; gi += 2) {
+      const int slot = gi % kPairSf;
+      if (gi >= kPairSf && !warp_wait(&sf_empty[slot], (uint32_t)(gi / kPairSf - 1) & 1u, abort_flag)) {
+        if (lane == 0 && !*abort_flag) {
+          record_error(a.err, HAM_DEVERR_TIMEOUT);
+          *abort_flag = 1;
+        }
+        break;
+      }
+      uint4 *dst = reinterpret_cast<uint4 *>(sf + slot * kPairSfBytes) + lane;
+      dst[0] = make_uint4(x[0], x[1], x[2], x[3]);
+      dst[32] = make_uint4(ws[0], ws[0], ws[0], ws[0]);
+      dst[64] = make_uint4(ws[1], ws[1], ws[1], ws[1]);
+      g += 2;
+      settle();
+      if (w < total) load(w, g);
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(cluster_map_shared(smem_u32(&sf_full[slot]), first));
     }
   } else if (warp >= 4) {
     // ------------------------------------------------------------ epilogue: two threads a row
@@ -584,8 +628,9 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     // accumulator and the first 64 of the second: the warps that have them load them before all else.
     const int quarter = warp & 3, half = (warp - 4) >> 2, lane_row = quarter * 32 + lane;
     const uint32_t free_bar = cluster_map_shared(smem_u32(acc_shared_free), first);
-    const bool wide = kGated ? (a.n & 31) == 0 && ((uintptr_t)a.out & 31u) == 0
-                             : (a.n & (a.f32 ? 7 : 15)) == 0 && ((uintptr_t)a.out & 31u) == 0;
+    // bytes a lane may write at once: a row begins at a multiple of them
+    const int row_bytes = a.n * (kGated ? 1 : a.f32 ? 4 : 2);
+    const int bytes = (row_bytes & 31) == 0 && ((uintptr_t)a.out & 31u) == 0 ? 32 : (row_bytes & 15) == 0 ? 16 : 0;
     int n = 0;
     for (int w = cluster; w < total; w += clusters, ++n) {
       const int rt = w % row_groups * kPairs + pair, ct = w / row_groups, buf = n & 1;
@@ -604,7 +649,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       auto release = [&] {
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(free_bar);
+        if (lane == 0) mbar_arrive_cluster_relaxed(free_bar);
       };
       const bool shared = half != buf;           // this warp has shared columns
       if (!shared) release();
@@ -618,11 +663,9 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           tmem_ld32(acc + col + 32, u);
           tmem_wait_ld();
           if (i == 0 && shared) release();
-          if (row < a.rows) {
-            const int c = ct * 256 + col;
-            if (c < a.n) store32(a, row, c, v, wide);
-            if (c + 32 < a.n) store32(a, row, c + 32, u, wide);
-          }
+          const int c = ct * 256 + col;
+          store32(a, row - lane, c, v, bytes, turn + (warp - 4) * 32 * kTurn);
+          store32(a, row - lane, c + 32, u, bytes, turn + (warp - 4) * 32 * kTurn);
         }
       } else {
         // gate columns half * 64 .., up columns 128 + half * 64 ..; shared: the up's of half 1 in the
@@ -659,7 +702,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
 #pragma unroll
           for (int q = 0; q < 16; ++q) code[q] = fp8_codes4(h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3], p);
           uint8_t *dst = static_cast<uint8_t *>(a.out) + (int64_t)row * a.n + c;
-          if (wide && c + 64 <= a.n) {
+          if (bytes == 32 && c + 64 <= a.n) {
             st_global_32(dst, *reinterpret_cast<uint32_t(*)[8]>(code));
             st_global_32(dst + 32, *reinterpret_cast<uint32_t(*)[8]>(code + 8));
           } else {
@@ -773,11 +816,13 @@ cudaError_t launch_pair(const CUtensorMap &tx, const CUtensorMap &tw, const Prod
   cudaError_t e = prepare_pair<kGated, 1>(dev, one);
   if (e == cudaSuccess) e = prepare_pair<kGated, 2>(dev, two);
   if (e != cudaSuccess) return e;
-  // Tiles that the busiest pair computes, with one pair a cluster and with two; the two share their
-  // weight tiles' loads and are a sixth faster a tile.
+  // Tiles that the busiest pair computes, with one pair a cluster and with two: at the same number the two,
+  // which share their weight tiles' loads, are up to a tenth faster (1024 rows, 16384 features of 4096: 47
+  // to 50 us against 52); else one, of which more are resident (gated, 4096 rows, 16384 features: 29 tiles
+  // and 319 us with two, 27 and 306 to 315 with one).
   const int64_t work1 = ((int64_t)row_tiles * col_tiles + one - 1) / one;
   const int64_t groups = (int64_t)((row_tiles + 1) / 2) * col_tiles, work2 = (groups + two - 1) / two;
-  if (work2 * 5 <= work1 * 6)
+  if (work2 <= work1)
     return launch_after(fp8_pair_kernel<kGated, 2>, dim3((unsigned)(4 * std::min<int64_t>(two, groups))), dim3(kPairThreads),
                         (size_t)kPairSmem, dim3(4, 1, 1), stream, tx, tw, a, row_tiles, col_tiles);
   return launch_after(fp8_pair_kernel<kGated, 1>,
@@ -903,8 +948,8 @@ int ham_fp8_weight_alloc(int32_t n, int32_t k, const void *codes, const void *sc
   }
   if (e == cudaSuccess) e = cudaMemset(w->err, 0, 4);
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
-  if (e != cudaSuccess || ham::make_bytes_tensor_map(&w->map, w->codes, blocks * w->parts * 128, 128, 128, 64,
-                                                     false) != 0) {
+  if (e != cudaSuccess || ham::make_stretch_tensor_map(&w->map, w->codes, blocks * w->parts * ham::kBlockBytes,
+                                                       ham::kBlockBytes / 2) != 0) {
     cudaGetLastError();
     ham_fp8_weight_free(w);
     return op_fail(HAM_ECUDA, "weight layout: %s", cudaGetErrorString(e));

@@ -89,9 +89,15 @@ __device__ __forceinline__ void tc_commit_pair(uint64_t *bar, uint32_t mask) {
       "h"((uint16_t)mask)
       : "memory");
 }
-// Arrive on a barrier of a CTA of the cluster (a shared::cluster address), releasing at cluster scope.
+// Arrive on a barrier of a CTA of the cluster (a shared::cluster address).  With `release` at cluster
+// scope the thread's earlier writes are ordered before it, which costs a round trip to L2 (about a
+// microsecond under load).  Without, it orders execution alone: enough for tensor-memory operations
+// behind tcgen05.fence::before_thread_sync.
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t addr) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
 }
 __device__ __forceinline__ bool mbar_test_cluster(uint64_t *bar, uint32_t parity) {
   uint32_t ok;

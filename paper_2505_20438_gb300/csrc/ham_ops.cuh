@@ -53,6 +53,10 @@ int device_sms();
 int make_bytes_tensor_map(CUtensorMap *map, const void *base, int64_t rows, int64_t cols,
                           int box_cols, int box_rows, bool swizzle);
 
+// TMA map of a stretch of `bytes` of memory (a multiple of 2048) as rows of 2048 bytes, with a box of
+// box_bytes of them one after the other; boxes past the end read zeros.  Returns a CUresult.
+int make_stretch_tensor_map(CUtensorMap *map, const void *base, int64_t bytes, int box_bytes);
+
 // Launch `kernel` so that it may be scheduled before the kernel before it on the stream has ended.
 // Every kernel launched this way waits (griddepcontrol.wait) before it reads anything that an
 // earlier kernel may have written and before it writes, and lets its own successor start only after

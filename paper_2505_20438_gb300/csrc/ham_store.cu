@@ -478,6 +478,19 @@ int make_bytes_tensor_map(CUtensorMap *map, const void *base, int64_t rows, int6
                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
+int make_stretch_tensor_map(CUtensorMap *map, const void *base, int64_t bytes, int box_bytes) {
+  EncodeTiled encode = tensor_map_encoder();
+  if (!encode) return -1;
+  const cuuint64_t dims[2] = {256, (cuuint64_t)(bytes / 2048)};
+  const cuuint64_t strides[1] = {2048};
+  const cuuint32_t box[2] = {256, (cuuint32_t)(box_bytes / 2048)};
+  const cuuint32_t estride[2] = {1, 1};
+  return (int)encode(map, CU_TENSOR_MAP_DATA_TYPE_INT64, 2, const_cast<void *>(base), dims,
+                     strides, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                     CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+
 int make_pool_tensor_map(CUtensorMap *map, const void *pool, int64_t rows, int head_dim) {
   EncodeTiled encode = tensor_map_encoder();
   if (!encode) return -1;
