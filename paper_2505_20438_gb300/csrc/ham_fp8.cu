@@ -74,7 +74,7 @@ struct ProductArgs {
   uint8_t *out_scales;     // gated: [rows][out_sk]
   int32_t *err;
   int rows, n, kbs, sk, out_sk;
-  int nt;                  // rows (of X) a CTA of the streaming kernel takes, a multiple of 16
+  int nt, box;             // the streaming kernel: rows of X a CTA takes (a multiple of 16), rows it loads
   int stages, stage_bytes, tmem_cols;
   int tiles;               // weight tiles
   int f32;                 // fp32 output
@@ -135,7 +135,10 @@ __global__ void __launch_bounds__(kStreamThreads)
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int tile = blockIdx.x, splits = gridDim.y, rank = blockIdx.y;  // a cluster: the splits
-  const int n0 = blockIdx.z * a.nt;
+  // The CTA's rows begin at row n0 and are loaded from row x0 on: a part that would pass the last row
+  // begins earlier instead, since a copy's rows past the end cost more than others (gated, 16384
+  // features of 4096: 300 rows took 67 us, 512 rows 50).
+  const int n0 = blockIdx.z * a.nt, x0 = min(n0, a.rows - a.box);
   const int kb0 = (int)((int64_t)rank * a.kbs / splits), kb1 = (int)((int64_t)(rank + 1) * a.kbs / splits);
   const int nk = kb1 - kb0, stages = a.stages;
   const int g0 = kb0 >> 2;                            // first scale word
@@ -172,7 +175,7 @@ __global__ void __launch_bounds__(kStreamThreads)
     if (lane == 0) {
       const uint64_t pol_x = policy_evict_last();
       const uint8_t *src = a.w + ((int64_t)tile * a.kbs + kb0) * (kParts * kBlockBytes);
-      const int xbytes = a.nt * 128;
+      const int xbytes = a.box * 128;
       auto load_w = [&](int t, int s) {
         mbar_arrive_tx(&full[s], (uint32_t)(kParts * kBlockBytes + xbytes));
         bulk_load(ring + s * a.stage_bytes, src + (int64_t)t * (kParts * kBlockBytes),
@@ -187,7 +190,7 @@ __global__ void __launch_bounds__(kStreamThreads)
           if (!thread_wait(&empty[s], (uint32_t)(t / stages - 1) & 1u, abort_flag, true)) break;
           load_w(t, s);
         }
-        tma_load_2d(ring + s * a.stage_bytes + kParts * kBlockBytes, &tx, (kb0 + t) * kFp8Block, n0, &full[s],
+        tma_load_2d(ring + s * a.stage_bytes + kParts * kBlockBytes, &tx, (kb0 + t) * kFp8Block, x0, &full[s],
                     pol_x);
         issued = t + 1;
       }
@@ -249,8 +252,8 @@ __global__ void __launch_bounds__(kStreamThreads)
       for (int j = 0; j < 4; ++j) {
         const int r = lane + 32 * j;
         x[j] = 0x7f7f7f7fu;
-        if (r < a.nt && n0 + r < a.rows)
-          x[j] = __ldg(reinterpret_cast<const uint32_t *>(a.xs + (int64_t)(n0 + r) * a.sk) + g0 + g);
+        if (r < a.box)
+          x[j] = __ldg(reinterpret_cast<const uint32_t *>(a.xs + (int64_t)(x0 + r) * a.sk) + g0 + g);
       }
 #pragma unroll
       for (int p = 0; p < kParts; ++p)
@@ -302,10 +305,9 @@ __global__ void __launch_bounds__(kStreamThreads)
     tc_fence_after();
     tmem_dealloc_n(tmem, (uint32_t)a.tmem_cols);
   }
-  const int live = min(a.nt, a.rows - n0);
   if (ok) {
     const uint32_t base = smem_u32(acc) + lane * 16;
-    for (int r = rank * 8 + warp; r < live; r += splits * 8) {
+    for (int r = n0 - x0 + rank * 8 + warp; r < a.box; r += splits * 8) {
       float4 v[kParts];
 #pragma unroll
       for (int p = 0; p < kParts; ++p) {
@@ -322,16 +324,16 @@ __global__ void __launch_bounds__(kStreamThreads)
       }
       const int c = tile * kTile + lane * 4;
       if constexpr (kParts == 1) {
-        if (c < a.n) store4(a, n0 + r, c, v[0]);
+        if (c < a.n) store4(a, x0 + r, c, v[0]);
       } else {
         const float h[4] = {silu_mul(v[0].x, v[1].x), silu_mul(v[0].y, v[1].y), silu_mul(v[0].z, v[1].z),
                             silu_mul(v[0].w, v[1].w)};
         const float m = warp_max_f32(fmaxf(fmaxf(fabsf(h[0]), fabsf(h[1])), fmaxf(fabsf(h[2]), fabsf(h[3]))));
         const int e = fp8_exponent(m);
         if (c < a.n)  // (n is a multiple of 16; features past it are zeros)
-          *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(a.out) + (int64_t)(n0 + r) * a.n + c) =
+          *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(a.out) + (int64_t)(x0 + r) * a.n + c) =
               fp8_codes4(h[0], h[1], h[2], h[3], fp8_pow2(-e));
-        uint8_t *s = a.out_scales + (int64_t)(n0 + r) * a.out_sk;
+        uint8_t *s = a.out_scales + (int64_t)(x0 + r) * a.out_sk;
         if (lane == 0) s[tile] = (uint8_t)(e + 127);
         else if (tile == a.tiles - 1 && lane < a.out_sk - tile) s[tile + lane] = 127;  // padding
       }
@@ -366,12 +368,12 @@ constexpr int kPairUsed = 1024 + kPairStages * kPairStageBytes + kPairSf * kPair
 constexpr int kPairSmem = kPairUsed > smem_floor(512) ? kPairUsed : smem_floor(512);
 static_assert(kPairSmem <= 226 * 1024, "shared memory");
 
-// 32 accumulator columns (from column c of n) of a warp's 32 rows, a row a lane, to the output: `bytes` at a
+// 32 accumulator columns (from column c of n) of a warp's 32 rows (those from own0 on), a row a lane, to the output: `bytes` at a
 // time a lane where rows begin at multiples of 32 or 16 bytes, and else turned in shared memory so that
 // 16 lanes write neighbours (a value at a time, 32 rows an instruction: 164 us for 3000 x 5003 outputs
 // of 2000 columns, against 27 us for 5008).
-__device__ __forceinline__ void store32(const ProductArgs &a, int row0, int c, const uint32_t (&v)[32], int bytes,
-                                        float *turn) {
+__device__ __forceinline__ void store32(const ProductArgs &a, int row0, int own0, int c, const uint32_t (&v)[32],
+                                        int bytes, float *turn) {
   const float *f = reinterpret_cast<const float *>(v);
   const int lane = threadIdx.x & 31, row = row0 + lane;
   if (c >= a.n) return;
@@ -386,7 +388,7 @@ __device__ __forceinline__ void store32(const ProductArgs &a, int row0, int c, c
 #pragma unroll 4
       for (int i = 0; i < 16; ++i) {
         const int r = 2 * i + (lane >> 4);
-        if (row0 + r < a.rows && col < a.n) {
+        if (row0 + r >= own0 && col < a.n) {
           const float x = turn[r * kTurn + (lane & 15)];
           const int64_t at = (int64_t)(row0 + r) * a.n + col;
           if (a.f32) static_cast<float *>(a.out)[at] = x;
@@ -396,7 +398,7 @@ __device__ __forceinline__ void store32(const ProductArgs &a, int row0, int c, c
     }
     return;
   }
-  if (row >= a.rows) return;
+  if (row < own0) return;
   char *dst = static_cast<char *>(a.out) + ((int64_t)row * a.n + c) * (a.f32 ? 4 : 2);
   // 32 bytes (from column `at` of the 32), or their two halves where the row ends between them
   auto put = [&](int at, int each, const uint32_t (&w)[8]) {
@@ -453,6 +455,10 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   const int clusters = gridDim.x / (2 * kPairs), cluster = blockIdx.x / (2 * kPairs);
   // a cluster's tiles: kPairs neighbouring row tiles (the last may lie past the rows) of one column tile
   const int row_groups = (row_tiles + kPairs - 1) / kPairs, total = row_groups * col_tiles;
+  // This CTA's 128 rows of row tile rt: the tile's, but none past the last (as in the streaming kernel,
+  // a tile that would pass it begins earlier); an odd last weight tile has no second, so its own is loaded
+  // twice.
+  auto row_of = [&](int rt) { return min(rt * 256 + side * 128, a.rows - 128); };
   if (tid == 0) {
     for (int s = 0; s < kPairStages; ++s) {
       mbar_init(&full[s], 1);
@@ -492,9 +498,10 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       int it = 0;
       for (int w = cluster; w < total && ok; w += clusters) {
         const int rt = w % row_groups * kPairs + pair, ct = w / row_groups;
-        const int x_row = rt * 256 + side * 128;
+        const int x_row = row_of(rt);
         // K block 0 of this CTA's weight tile in the laid-out weight
-        const int64_t block = kGated ? (int64_t)ct * a.kbs * 2 + side : ((int64_t)ct * 2 + side) * a.kbs;
+        const int64_t block = kGated ? (int64_t)ct * a.kbs * 2 + side
+                                     : (int64_t)min(ct * 2 + side, a.tiles - 1) * a.kbs;
         for (int kb = 0; kb < a.kbs; ++kb, ++it) {
           const int s = it % kPairStages;
           if (it >= kPairStages &&
@@ -580,18 +587,14 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     const int groups = (a.kbs + 3) / 4, turn = warp - 2;
     uint32_t x[4], ws[2];
     auto load = [&](int w, int g) {
-      const int rt = w % row_groups * kPairs + pair, ct = w / row_groups, x_row = rt * 256 + side * 128;
+      const int rt = w % row_groups * kPairs + pair, ct = w / row_groups, x_row = row_of(rt);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int r = x_row + lane + 32 * j;
-        x[j] = r < a.rows ? __ldg(reinterpret_cast<const uint32_t *>(a.xs + (int64_t)r * a.sk) + g) : 0x7f7f7f7fu;
-      }
+      for (int j = 0; j < 4; ++j)
+        x[j] = __ldg(reinterpret_cast<const uint32_t *>(a.xs + (int64_t)(x_row + lane + 32 * j) * a.sk) + g);
 #pragma unroll
       for (int p = 0; p < 2; ++p) {  // the tile's scale rows: [tile][part]
-        const int row = ct * 2 + p;
-        ws[p] = kGated || row < a.tiles
-                    ? __ldg(reinterpret_cast<const uint32_t *>(a.ws + (int64_t)row * a.sk) + g)
-                    : 0x7f7f7f7fu;
+        const int row = kGated ? ct * 2 + p : min(ct * 2 + p, a.tiles - 1);
+        ws[p] = __ldg(reinterpret_cast<const uint32_t *>(a.ws + (int64_t)row * a.sk) + g);
       }
     };
     // the gi-th word of this cluster's tiles is word g of tile w
@@ -634,7 +637,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     int n = 0;
     for (int w = cluster; w < total; w += clusters, ++n) {
       const int rt = w % row_groups * kPairs + pair, ct = w / row_groups, buf = n & 1;
-      const int row = rt * 256 + side * 128 + lane_row;
+      const int row0 = row_of(rt) + quarter * 32, row = row0 + lane, own0 = rt * 256 + side * 128;
       const uint32_t acc = tmem + (uint32_t)(buf * kPairBuf1) + ((uint32_t)(quarter * 32) << 16);
       bool ok = warp_wait_cluster(&acc_full[buf], (uint32_t)(n >> 1) & 1u, abort_flag);
       if (!ok && lane == 0 && !*abort_flag) {
@@ -664,8 +667,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           tmem_wait_ld();
           if (i == 0 && shared) release();
           const int c = ct * 256 + col;
-          store32(a, row - lane, c, v, bytes, turn + (warp - 4) * 32 * kTurn);
-          store32(a, row - lane, c + 32, u, bytes, turn + (warp - 4) * 32 * kTurn);
+          store32(a, row0, own0, c, v, bytes, turn + (warp - 4) * 32 * kTurn);
+          store32(a, row0, own0, c + 32, u, bytes, turn + (warp - 4) * 32 * kTurn);
         }
       } else {
         // gate columns half * 64 .., up columns 128 + half * 64 ..; shared: the up's of half 1 in the
@@ -697,7 +700,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         const int e = fp8_exponent(m);
         const float p = fp8_pow2(-e);
         const int c = ct * kTile + half * 64;
-        if (row < a.rows) {
+        if (row >= own0) {
           uint32_t code[16];
 #pragma unroll
           for (int q = 0; q < 16; ++q) code[q] = fp8_codes4(h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3], p);
@@ -850,12 +853,13 @@ int run_product(ham_fp8_weight *w, const void *x_codes, const void *x_scales, in
   a.tiles = w->tiles;
   a.f32 = f32;
   const int64_t tiles = (int64_t)((rows + 255) / 256) * (w->parts == 2 ? w->tiles : (w->tiles + 1) / 2);
-  const bool pair = rows > 128 && tiles * 2 >= device_sms();
+  const bool pair = rows > 128 && tiles * 8 >= device_sms();
   const int row_parts = (rows + 127) / 128;           // the streaming kernel's, of equal size
   a.nt = ((rows + row_parts - 1) / row_parts + 15) / 16 * 16;
+  a.box = std::min(a.nt, rows);
   CUtensorMap tx;
   int rc = HAM_OK;
-  if (make_bytes_tensor_map(&tx, x_codes, rows, w->k, kFp8Block, pair ? 128 : a.nt, true) != 0) {
+  if (make_bytes_tensor_map(&tx, x_codes, rows, w->k, kFp8Block, pair ? 128 : a.box, true) != 0) {
     rc = op_fail(HAM_ECUDA, "tensor map of the rows");
   } else {
     cudaStream_t s = static_cast<cudaStream_t>(stream);
