@@ -798,7 +798,7 @@ cudaError_t launch_stream(const CUtensorMap &tx, ProductArgs a, int dev, cudaStr
   const int smem = std::max(a.stages * a.stage_bytes + stream_fixed(kParts), splits > 1 ? smem_floor(cols) : 0);
   cudaError_t e = allow_smem(fp8_stream_kernel<kParts>, 226 * 1024, done, dev);
   if (e != cudaSuccess) return e;
-  return launch_after(fp8_stream_kernel<kParts>, dim3((unsigned)a.tiles, (unsigned)splits, (unsigned)zt),
+  return launch_after<fp8_stream_kernel<kParts>>(dim3((unsigned)a.tiles, (unsigned)splits, (unsigned)zt),
                       dim3(kStreamThreads), (size_t)smem, dim3(1, (unsigned)splits, 1), stream, tx, a);
 }
 
@@ -826,9 +826,9 @@ cudaError_t launch_pair(const CUtensorMap &tx, const CUtensorMap &tw, const Prod
   const int64_t work1 = ((int64_t)row_tiles * col_tiles + one - 1) / one;
   const int64_t groups = (int64_t)((row_tiles + 1) / 2) * col_tiles, work2 = (groups + two - 1) / two;
   if (work2 <= work1)
-    return launch_after(fp8_pair_kernel<kGated, 2>, dim3((unsigned)(4 * std::min<int64_t>(two, groups))), dim3(kPairThreads),
+    return launch_after<fp8_pair_kernel<kGated, 2>>(dim3((unsigned)(4 * std::min<int64_t>(two, groups))), dim3(kPairThreads),
                         (size_t)kPairSmem, dim3(4, 1, 1), stream, tx, tw, a, row_tiles, col_tiles);
-  return launch_after(fp8_pair_kernel<kGated, 1>,
+  return launch_after<fp8_pair_kernel<kGated, 1>>(
                       dim3((unsigned)(2 * std::min<int64_t>(one, (int64_t)row_tiles * col_tiles))), dim3(kPairThreads),
                       (size_t)kPairSmem, dim3(2, 1, 1), stream, tx, tw, a, row_tiles, col_tiles);
 }

@@ -261,9 +261,11 @@ int ham_add_norm(const void *x, const void *residual, const void *weight, float 
   int groups = 1;
   while (groups < 4 && a.vecs > groups * most) groups *= 2;
   const int threads = ((a.vecs + groups - 1) / groups + 31) / 32 * 32;
-  auto kernel = groups == 1 ? ham::add_norm_kernel<1> : groups == 2 ? ham::add_norm_kernel<2> : ham::add_norm_kernel<4>;
-  const cudaError_t ce = ham::launch_after(kernel, dim3((unsigned)rows), dim3((unsigned)threads), 0,
-                                           dim3(1), static_cast<cudaStream_t>(stream), a);
+  const dim3 grid((unsigned)rows), block((unsigned)threads);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const cudaError_t ce = groups == 1   ? ham::launch_after<ham::add_norm_kernel<1>>(grid, block, 0, dim3(1), s, a)
+                         : groups == 2 ? ham::launch_after<ham::add_norm_kernel<2>>(grid, block, 0, dim3(1), s, a)
+                                       : ham::launch_after<ham::add_norm_kernel<4>>(grid, block, 0, dim3(1), s, a);
   return ce == cudaSuccess ? HAM_OK : op_fail(HAM_ECUDA, "norm launch: %s", cudaGetErrorString(ce));
 }
 
@@ -282,8 +284,8 @@ int ham_fp8_encode(const void *x, int32_t rows, int32_t k, void *codes, void *sc
     return op_fail(HAM_EINVAL, "x, codes and scales must not overlap");
   const int64_t grid = ((int64_t)rows * sk * 16 + 255) / 256;
   if (grid > INT32_MAX) return op_fail(HAM_EINVAL, "rows * k is too large");
-  const cudaError_t ce = ham::launch_after(
-      ham::encode_kernel, dim3((unsigned)grid), dim3(256), 0, dim3(1), static_cast<cudaStream_t>(stream),
+  const cudaError_t ce = ham::launch_after<ham::encode_kernel>(
+      dim3((unsigned)grid), dim3(256), 0, dim3(1), static_cast<cudaStream_t>(stream),
       static_cast<const uint4 *>(x), static_cast<uint2 *>(codes), static_cast<uint8_t *>(scales),
       (int64_t)rows, k / 8, sk);
   return ce == cudaSuccess ? HAM_OK : op_fail(HAM_ECUDA, "encode launch: %s", cudaGetErrorString(ce));
@@ -303,8 +305,8 @@ int ham_fp8_encode_weight(const void *w, int32_t n, int32_t k, void *codes, void
   if (op_overlap(w, 2 * e, codes, e) || op_overlap(w, 2 * e, scales, sb) || op_overlap(codes, e, scales, sb))
     return op_fail(HAM_EINVAL, "w, codes and scales must not overlap");
   // one block a scale byte, the padding's too (no elements there: scale 1)
-  const cudaError_t ce = ham::launch_after(
-      ham::encode_weight_kernel, dim3((unsigned)sk, (unsigned)nb), dim3(256), 0, dim3(1),
+  const cudaError_t ce = ham::launch_after<ham::encode_weight_kernel>(
+      dim3((unsigned)sk, (unsigned)nb), dim3(256), 0, dim3(1),
       static_cast<cudaStream_t>(stream), static_cast<const uint4 *>(w), static_cast<uint2 *>(codes),
       static_cast<uint8_t *>(scales), n, k / 8, sk);
   return ce == cudaSuccess ? HAM_OK : op_fail(HAM_ECUDA, "encode launch: %s", cudaGetErrorString(ce));

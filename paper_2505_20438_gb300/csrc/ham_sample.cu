@@ -934,7 +934,7 @@ cudaError_t launch_sample(SampleArgs a, int rows, cudaStream_t stream) {
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) done[dev] = true;
   }
-  return launch_after(sample_kernel<T>, dim3((unsigned)ctas, (unsigned)rows), dim3(kSampleThreads),
+  return launch_after<sample_kernel<T>>(dim3((unsigned)ctas, (unsigned)rows), dim3(kSampleThreads),
                       (size_t)bytes(ctas), dim3((unsigned)ctas), stream, a);
 }
 

@@ -131,8 +131,8 @@ int fp8_unsupported(const ham_kv *kv, const char *call) {
 //    it on the stream starts only when everything before that call has completed: of the noted calls
 //    only the last one may still run.
 // That call writes only its layer's state, its outputs and its handle's scratch, which a following
-// kernel touches after its wait; calls that are not noted (the embedder, ham_decode_attn_noalloc)
-// write no handle's state.  The library remembers, per stream (and per stream capture), the last noted
+// kernel touches after its wait; calls that are not noted (the embedder, ham_decode_attn_noalloc,
+// the norm, products and sampling after the attention) write no handle's state.  The library remembers, per stream (and per stream capture), the last noted
 // call and which (handle, layer) state it writes, and allows the early start only when that call is
 // known and leaves this layer alone.  Kernels of other code in between are harmless: they cannot write
 // a handle's state (only these calls do), and an unknown predecessor means no early start.
@@ -380,6 +380,18 @@ EncodeTiled tensor_map_encoder() {
   return encode;
 }
 }  // namespace
+
+DriverLaunch driver_launch() {
+  static const DriverLaunch launch = [] {
+    void *fn = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuLaunchKernelEx", &fn, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess)
+      return DriverLaunch(nullptr);
+    return reinterpret_cast<DriverLaunch>(fn);
+  }();
+  return launch;
+}
 
 int make_rows_tensor_map(CUtensorMap *map, const void *base, int64_t rows, int heads,
                          int head_dim, int box_heads, int box_rows) {
