@@ -76,46 +76,37 @@ struct SampleShared {
   int found, members, cut_at;
   float cut_value;
   uint32_t cut_ties, cut_by_index;
+  uint64_t cut_mass;
 };
 
 __device__ __forceinline__ float load_logit(const float *p) { return *p; }
 __device__ __forceinline__ float load_logit(const uint16_t *p) { return __uint_as_float((uint32_t)*p << 16); }
-// NaN counts as ruled out; -0 as 0.
-__device__ __forceinline__ float clean(float l) { return l != l ? -INFINITY : l + 0.f; }
-// Keys in the order of the (cleaned) logits.
+// Keys in the order of the logits (-0 as 0).
 __device__ __forceinline__ uint32_t key_of(float l) {
-  const uint32_t b = __float_as_uint(l);
+  const uint32_t b = __float_as_uint(l + 0.f);
   return b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u);
 }
-// A row's temperature, and x = (l - best) / t rounded to nearest as a division is: with r the rounded
-// reciprocal of t, q = a r and its remainder a - q t (exact in a fused multiply-add), q + rem r rounds
-// to the quotient (Markstein, IBM J. Res. Dev. 34, 1990).  Where a step leaves fp32's range the weight
-// is right all the same: an x that underflows is one whose exponential is 1, an overflow makes x NaN or
-// -inf, and both weigh 0.  Rows with an infinite largest logit or an extreme t divide instead.
+
+// A row's largest logit and temperature.  -x = (best - l) / t rounded to nearest as a division is: with r
+// the rounded reciprocal of t, q = d r and its remainder d - q t (exact in a fused multiply-add), q + rem r
+// rounds to the quotient (Markstein, IBM J. Res. Dev. 34, 1990).  Where a step leaves fp32's range the
+// weight is right all the same: an x that underflows is one whose exponential is 1, and an overflow
+// makes it NaN or -inf, which weigh 0, as a NaN logit does.
 struct Scale {
   float best, t, r, bins;   // bins = kBinsPerX / t
-  bool plain;
 };
 __device__ __forceinline__ Scale scale_of(float best, float t) {
-  return Scale{best, t, __frcp_rn(t), __fdiv_rn(kBinsPerX, t), t > 0x1p-60f && t < 0x1p60f && best < INFINITY};
+  t = fminf(fmaxf(t, 0x1p-60f), 0x1p60f);
+  return Scale{best, t, __frcp_rn(t), __fdiv_rn(kBinsPerX, t)};
 }
-__device__ __forceinline__ float x_of(float l, const Scale &c) {
-  const float a = __fsub_rn(l, c.best);
-  if (c.plain) {
-    const float q = __fmul_rn(a, c.r);
-    return __fmaf_rn(__fmaf_rn(-q, c.t, a), c.r, q);
-  }
-  return l == c.best ? 0.f : __fdiv_rn(a, c.t);
-}
-__device__ __forceinline__ uint32_t weight_of(float x) {
-  return (uint32_t)(expf(x) * kFine);  // (NaN: 0)
+__device__ __forceinline__ uint32_t weight_of(float l, const Scale &c) {
+  const float d = __fsub_rn(c.best, l), q = __fmul_rn(d, c.r);
+  const float x = __fmaf_rn(__fmaf_rn(-q, c.t, d), c.r, q);
+  return (uint32_t)(expf(-x) * kFine);           // (NaN: 0)
 }
 // Where l lies in the order, in bins (the fraction: the part of the bin); it grows as l falls, so bins
-// and parts follow the order.  From kLastBin on weights are 0 and the token is left out.
-__device__ __forceinline__ float place_of(float l, const Scale &c) {
-  const float f = __fmul_rn(__fsub_rn(c.best, l), c.bins);
-  return c.plain || l != c.best ? f : 0.f;
-}
+// and parts follow the order.  From kLastBin on weights are 0 and the token is left out, as is NaN.
+__device__ __forceinline__ float place_of(float l, const Scale &c) { return __fmul_rn(__fsub_rn(c.best, l), c.bins); }
 __device__ __forceinline__ bool has_bin(float place) { return place < kLastBin; }
 __device__ __forceinline__ int part_of(float place, int bin) { return (int)((place - (float)bin) * (float)kBins); }
 
@@ -200,24 +191,18 @@ struct Vec {
 #pragma unroll
     for (int j = 0; j < kN; ++j) l[j] = load_logit(e + j);
   }
-  // A vector of ruled-out logits.
-  static __device__ __forceinline__ uint4 none() {
-    const uint32_t v = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
-    return make_uint4(v, v, v, v);
-  }
-  // The vector with NaN as -inf and -0 as 0; `best`: the largest logit so far.
-  static __device__ __forceinline__ uint4 clean_of(const uint4 &v, float &best) {
-    uint4 o;
-    const T *e = reinterpret_cast<const T *>(&v);
-    T *d = reinterpret_cast<T *>(&o);
+  // (fmaxf and fminf pass over NaN)
+  __device__ __forceinline__ float largest() const {
+    float m = l[0];
 #pragma unroll
-    for (int j = 0; j < kN; ++j) {
-      const float f = clean(load_logit(e + j));
-      best = fmaxf(best, f);
-      if constexpr (sizeof(T) == 4) d[j] = f;
-      else d[j] = (T)(__float_as_uint(f) >> 16);
-    }
-    return o;
+    for (int j = 1; j < kN; ++j) m = fmaxf(m, l[j]);
+    return m;
+  }
+  __device__ __forceinline__ float smallest() const {
+    float m = l[0];
+#pragma unroll
+    for (int j = 1; j < kN; ++j) m = fminf(m, l[j]);
+    return m;
   }
 };
 
@@ -225,7 +210,7 @@ template <typename T>
 struct Row {
   static constexpr int kN = Vec<T>::kN;
   SampleShared &s;
-  uint4 *data;             // this CTA's logits, cleaned (-inf before and after them)
+  uint4 *data;             // this CTA's logits (-inf before and after them)
   int first_index;         // index of the first vector's first element (slice further on in the next CTA)
   int slice, vecs, ctas, rank, tid;
   Scale c;
@@ -256,55 +241,47 @@ struct Row {
     v0 = min(vecs, tid * per);
     v1 = min(vecs, v0 + per);
   }
-  // The vectors of this thread's stretch (bit i: vector v0 + i) that hold a logit for which pred(l); their
-  // number of such logits.
+  // The vectors of this thread's stretch (bit i: vector v0 + i) for which pred(vector).
   template <typename P>
-  __device__ __forceinline__ uint32_t which(P pred, uint32_t &many) const {
+  __device__ __forceinline__ uint32_t which(P pred) const {
     int v0, v1;
     stretch(v0, v1);
     uint32_t mask = 0;
-    many = 0;
 #pragma unroll 2
-    for (int v = v0; v < v1; ++v) {
-      const Vec<T> x(data[v]);
-      uint32_t n = 0;
-#pragma unroll
-      for (int j = 0; j < kN; ++j) n += pred(x.l[j]);
-      many += n;
-      mask |= (uint32_t)(n > 0) << (v - v0);
-    }
+    for (int v = v0; v < v1; ++v) mask |= (uint32_t)pred(Vec<T>(data[v])) << (v - v0);
     return mask;
   }
-  // The histogram of the logits in range by the bins of `where` (negative: left out), counts and / or
-  // weights.  Computed for the whole vector first: a vector's chains of arithmetic overlap.
-  template <bool kCounts, bool kMasses, typename W>
-  __device__ __forceinline__ void histogram(W where) const {
+  // The histogram of the logits by bin(place, l) where in(place, l), of counts and / or weights.
+  // Computed for the whole vector first: a vector's chains of arithmetic overlap.
+  template <bool kMasses, typename I, typename B>
+  __device__ __forceinline__ void histogram(I in, B bin) const {
     each([&](const Vec<T> &x) {
-      int bin[kN];
+      float f[kN];
       uint32_t w[kN];
 #pragma unroll
       for (int j = 0; j < kN; ++j) {
-        bin[j] = where(x.l[j]);
-        if (kMasses) w[j] = weight_of(x_of(x.l[j], c));
+        f[j] = place_of(x.l[j], c);
+        if (kMasses) w[j] = weight_of(x.l[j], c);
       }
 #pragma unroll
       for (int j = 0; j < kN; ++j)
-        if (bin[j] >= 0) {
-          if (kCounts) atomicAdd(&s.h.count[bin[j]], 1u);
-          if (kMasses) add_mass(bin[j], w[j]);
+        if (in(f[j], x.l[j])) {
+          const int b = bin(f[j], x.l[j]);
+          atomicAdd(&s.h.count[b], 1u);
+          if (kMasses) add_mass(b, w[j]);
         }
     });
   }
-  __device__ __forceinline__ int bin_of(float l) const {
-    const float f = place_of(l, c);
-    return has_bin(f) ? (int)f : -1;
+  template <bool kMasses>
+  __device__ __forceinline__ void histogram_of_bins() const {
+    histogram<kMasses>([](float f, float) { return has_bin(f); }, [](float f, float) { return (int)f; });
   }
   __device__ void clear() const {
     for (int i = tid; i < kBins; i += kSampleThreads) s.h.count[i] = s.h.low[i] = s.h.high[i] = 0;
     __syncthreads();
   }
   __device__ __forceinline__ void add_mass(int bin, uint32_t w) const {
-    if (w & 0xffffu) atomicAdd(&s.h.low[bin], w & 0xffffu);
+    atomicAdd(&s.h.low[bin], w & 0xffffu);
     if (w >> 16) atomicAdd(&s.h.high[bin], w >> 16);
   }
   // The share of a row's weight that top-p reaches for: whole numbers from here on (a sum reaches the
@@ -400,10 +377,8 @@ struct Row {
     uint64_t mass = s.found_before_mass;
     sync();                                      // (before the histogram's next use)
     clear();                                     // parts of the bin
-    histogram<true, true>([&](float l) {
-      const float f = place_of(l, c);
-      return has_bin(f) && (int)f == b1 ? part_of(f, b1) : -1;
-    });
+    histogram<true>([&](float f, float) { return has_bin(f) && (int)f == b1; },
+                    [&](float f, float) { return part_of(f, b1); });
     find(by_mass, true, count, mass, aim);
     const int b2 = s.found;
     count = s.found_before_count, mass = s.found_before_mass;
@@ -425,11 +400,9 @@ struct Row {
       int shift = 0;
       while (((kmax - kmin) >> shift) >= (uint32_t)kBins) ++shift;
       clear();
-      histogram<true, true>([&](float l) {
-        const float f = place_of(l, c);
-        const uint32_t key = key_of(l);
-        return f >= begin && f < end && key >= kmin && key <= kmax ? (int)((kmax - key) >> shift) : -1;
-      });
+      histogram<true>(
+          [&](float f, float l) { return f >= begin && f < end && key_of(l) >= kmin && key_of(l) <= kmax; },
+          [&](float, float l) { return (int)((kmax - key_of(l)) >> shift); });
       find(by_mass, true, count, mass, aim);
       count = s.found_before_count, mass = s.found_before_mass;
       const uint32_t bin = (uint32_t)s.found;
@@ -452,33 +425,40 @@ struct Row {
   // Weight of l if the cut and min_p keep it (those equal to the cut's value too: where some of them are
   // cut off, the caller keeps the first by index).
   __device__ __forceinline__ uint32_t kept(const Cut &k, uint32_t least, float l) const {
-    const uint32_t v = weight_of(x_of(l, c));
+    const uint32_t v = weight_of(l, c);
     return l >= k.value && v >= least ? v : 0u;
   }
   // Lists this CTA's tokens of the bins first .. last, by index; the row's number of them.  If that is at
   // most kList, pull() then makes the row's list.
   __device__ uint32_t list(int first, int last) const {
     const float begin = (float)first, end = (float)(last + 1);  // (last < 511: a token up to it has a bin)
+    // the vectors that may hold some, by their largest and smallest logits; then their tokens
+    const uint32_t mask =
+        first == 0 ? which([&](const Vec<T> &x) { return place_of(x.largest(), c) < end; })
+                   : which([&](const Vec<T> &x) { return place_of(x.largest(), c) < end && place_of(x.smallest(), c) >= begin; });
+    int v0, v1;
+    stretch(v0, v1);
     const auto in = [&](float l) {
       const float f = place_of(l, c);
       return f < end && f >= begin;
     };
-    uint32_t many;
-    uint32_t mask = which(in, many);
+    uint32_t many = 0;
+    for (uint32_t m = mask; m; m &= m - 1) {
+      const Vec<T> x(data[v0 + __ffs(m) - 1]);
+#pragma unroll
+      for (int j = 0; j < kN; ++j) many += in(x.l[j]);
+    }
     uint64_t cta;
     uint32_t at = (uint32_t)block_scan(s, many, cta) - many;
     if (tid == 0) s.ties = (uint32_t)cta;
-    if (cta <= kList) {
-      int v0, v1;
-      stretch(v0, v1);
-      for (; mask; mask &= mask - 1) {
-        const int v = v0 + __ffs(mask) - 1;
+    if (many && cta <= kList)
+      for (uint32_t m = mask; m; m &= m - 1) {
+        const int v = v0 + __ffs(m) - 1;
         const Vec<T> x(data[v]);
 #pragma unroll
         for (int j = 0; j < kN; ++j)
           if (in(x.l[j])) s.own[at++] = v * kN + j;
       }
-    }
     sync();
     return sum8(lane32(&s.ties));
   }
@@ -511,7 +491,7 @@ struct Row {
     return ((uint64_t)~key_of(s.list_l[i]) << 32) | (uint32_t)i;
   }
   __device__ __forceinline__ float sorted_logit(uint64_t key) const { return logit_of(~(uint32_t)(key >> 32)); }
-  __device__ __forceinline__ uint32_t listed_weight(int i) const { return weight_of(x_of(s.list_l[i], c)); }
+  __device__ __forceinline__ uint32_t listed_weight(int i) const { return weight_of(s.list_l[i], c); }
   // Sorts the first `many` keys of s.sorted (by l, largest first, equal ones by place in the list): a
   // bitonic network, distances below a warp in registers, the others in shared memory.
   __device__ void sort(int many) const {
@@ -606,7 +586,7 @@ struct Row {
         s.cut_value = logit_of(~l);
         s.cut_ties = i - from + 1;
         s.cut_by_index = i + 1 < many && (uint32_t)(s.sorted[i + 1] >> 32) == l;
-        s.found_mass = upto;
+        s.cut_mass = upto;
       }
       at += part;
     }
@@ -615,10 +595,10 @@ struct Row {
     k.value = s.cut_value;
     k.ties = s.cut_ties;
     k.by_index = s.cut_by_index;
-    k.mass = s.found_mass;
+    k.mass = s.cut_mass;
     return k;
   }
-  // The exact cut within the bin that find() gave for the aim, the same in every CTA of the cluster.
+  // The exact cut within the bin that find() gave for the aim, made by the first CTA for the cluster.
   __device__ Cut cut(bool by_mass, uint64_t aim) const {
     if (s.found_count > (uint32_t)kList) return cut_by_bins(by_mass, aim);
     const uint32_t count = s.found_before_count;
@@ -626,9 +606,17 @@ struct Row {
     const int bin = s.found;
     __syncthreads();
     const int many = (int)list(bin, bin);
-    pull(many);
-    sync();                                      // (the histograms' and the lists' last readers are done)
-    return cut_list(many, false, bin, by_mass, aim, count, mass, [&](int i) { return listed_weight(i); });
+    if (rank == 0) {
+      pull(many);
+      cut_list(many, false, bin, by_mass, aim, count, mass, [&](int i) { return listed_weight(i); });
+    }
+    sync();
+    Cut k;
+    k.value = __uint_as_float(ld_cluster_u32(peer(&s.cut_value, 0)));
+    k.ties = ld_cluster_u32(peer(&s.cut_ties, 0));
+    k.by_index = ld_cluster_u32(peer(&s.cut_by_index, 0));
+    k.mass = ld_cluster_u64(peer(&s.cut_mass, 0));
+    return k;
   }
   // The choice among the first CTA's list of `all` tokens up to bin `last`, by that CTA alone.  k > 0:
   // top-k, which cuts in bin `last`, before which lie `before` tokens.  p >= 0: top-p, of the weight
@@ -644,7 +632,7 @@ struct Row {
       if (tid < all) s.sorted[tid] = sort_key(tid);
       sort(all);
       const uint64_t key = tid < all ? s.sorted[tid] : ~0ull;
-      const uint32_t w = tid < all && (k <= 0 || tid < k) ? weight_of(x_of(sorted_logit(key), c)) : 0;
+      const uint32_t w = tid < all && (k <= 0 || tid < k) ? weight_of(sorted_logit(key), c) : 0;
       uint64_t sum, aim = ~0ull;
       const uint64_t run = block_scan(s, w, sum) - w;
       if (p >= 0.) {
@@ -740,13 +728,14 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
 #pragma unroll
     for (int j = 0; j < kAtOnce; ++j)
       if (i0 + j * kSampleThreads < whole1) {
-        store[i0 + j * kSampleThreads] = Vec<T>::clean_of(v[j], best);
+        store[i0 + j * kSampleThreads] = v[j];
+        best = fmaxf(best, Vec<T>(v[j]).largest());
       }
   }
   if (tid < 2 * kVec) {                          // the first and the last vector, where they stick out
     const int v = tid < kVec ? 0 : vecs - 1, i = v * kVec + tid % kVec - phase;
     if (vecs > 0 && (v < whole0 || v >= whole1)) {
-      const float x = i >= 0 && i < n ? clean(load_logit(src + i)) : -INFINITY;
+      const float x = i >= 0 && i < n ? load_logit(src + i) : -INFINITY;
       best = fmaxf(best, x);
       T *to = reinterpret_cast<T *>(store) + v * kVec + tid % kVec;
       if constexpr (sizeof(T) == 4) *to = x;
@@ -762,6 +751,16 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
   r.sync();
   best = warp_max_f32(lane < ctas ? __uint_as_float(r.lane32(&s.best)) : -INFINITY);
   const bool greedy = !(temperature > 0.f);
+  if (best == INFINITY) {                        // as likely as one another, and nothing else is
+    best = 0.f;
+    T *l = reinterpret_cast<T *>(store);
+    for (int i = tid; i < vecs * kVec; i += kSampleThreads) {
+      const uint32_t to = load_logit(l + i) == INFINITY ? 0u : 0xff800000u;
+      if constexpr (sizeof(T) == 4) l[i] = __uint_as_float(to);
+      else l[i] = (T)(to >> 16);
+    }
+    __syncthreads();
+  }
   r.c = scale_of(best, greedy ? 1.f : temperature);
   if (best == -INFINITY || greedy) {             // (the same in every CTA of the cluster)
     int first = INT32_MAX;
@@ -795,9 +794,8 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
   const uint32_t least = min_p > 0.f ? (uint32_t)ceilf(fminf(min_p, 1.f) * kFine) : 0u;
   Cut cut;
   if (by_k || by_p) {
-    const auto bins = [&](float l) { return r.bin_of(l); };
-    if (by_k) r.template histogram<true, false>(bins);   // counts if top-k comes first
-    else r.template histogram<true, true>(bins);
+    if (by_k) r.template histogram_of_bins<false>();     // counts alone if top-k comes first
+    else r.template histogram_of_bins<true>();
     r.find(!by_k, !by_k, 0, 0, (uint64_t)k, by_k ? 0. : share);
     const bool all_in = s.found < 0;             // fewer than k tokens have any weight
     const int last = all_in ? kBins - 2 : s.found;
@@ -820,7 +818,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
       if (by_p) {                                // (top-p wants the weight that top-k keeps)
         r.sync();
         r.clear();
-        r.template histogram<true, true>(bins);
+        r.template histogram_of_bins<true>();
         r.find(false, true, 0, 0, (uint64_t)k);
       }
       if (!all_in) cut = r.cut(false, (uint64_t)k);
@@ -828,23 +826,29 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
         aim = Row<T>::aim_of(share, all_in ? s.total_mass : cut.mass);
         r.sync();
         r.clear();
-        r.template histogram<true, true>(bins);
+        r.template histogram_of_bins<true>();
         r.find(true, true, 0, 0, aim);
       }
     }
     if (by_p) cut = r.cut(true, aim);
   }
   // ---- the kept weights of each thread's stretch of the slice, in index order
-  uint32_t ties_before = 0, mine, ties_all;
+  uint32_t ties_before = 0, ties_mine = 0;
   if (cut.by_index) {
-    r.which([&](float l) { return l == cut.value; }, mine);
+    int v0, v1;
+    r.stretch(v0, v1);
+    for (int v = v0; v < v1; ++v) {
+      const Vec<T> x(store[v]);
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) ties_mine += x.l[j] == cut.value;
+    }
     uint64_t cta;
-    ties_before = (uint32_t)block_scan(s, mine, cta) - mine;
+    ties_before = (uint32_t)block_scan(s, ties_mine, cta) - ties_mine;
     r.sync();                                    // (s.ties: its last readers are done)
     if (tid == 0) s.ties = (uint32_t)cta;
     r.sync();
-    ties_all = r.lane32(&s.ties);
-    ties_before += sum8(lane < rank ? ties_all : 0u);
+    const uint32_t theirs = r.lane32(&s.ties);
+    ties_before += sum8(lane < rank ? theirs : 0u);
   }
   int v0, v1;
   r.stretch(v0, v1);
@@ -853,11 +857,14 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
     for (int v = v0; v < v1; ++v) {
       const Vec<T> x(store[v]);
 #pragma unroll
-      for (int j = 0; j < kVec; ++j) sum += r.kept(cut, least, x.l[j]);
+      for (int j = 0; j < kVec; ++j) {
+        const uint32_t w = weight_of(x.l[j], r.c);
+        sum += w >= least ? w : 0u;
+      }
     }
   } else {                                       // (few of a long row's: only their vectors are weighed)
     uint32_t ties = ties_before;
-    for (uint32_t mask = r.which([&](float l) { return l >= cut.value; }, mine); mask; mask &= mask - 1) {
+    for (uint32_t mask = r.which([&](const Vec<T> &x) { return x.largest() >= cut.value; }); mask; mask &= mask - 1) {
       const Vec<T> x(store[v0 + __ffs(mask) - 1]);
 #pragma unroll
       for (int j = 0; j < kVec; ++j) {
