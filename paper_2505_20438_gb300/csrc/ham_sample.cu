@@ -10,21 +10,40 @@
 // Sums are of whole numbers, so that neither the order of the additions nor the launch's shape can
 // change an answer.  Weights are below one part in 2^31 of the likeliest token's where they are 0.
 //
-// A row is held in the shared memory of a cluster of CTAs and read from global memory once.  A row is
-// never sorted.  A histogram over 512 bins of (max - l) / T, which grows as the order goes on, of counts
-// (for top-k) or of counts and weights (top-p alone) finds the bin in which the order is cut: every CTA
-// adds up the cluster's histograms for itself, 16 bytes a load, so that this costs one cluster barrier
-// (2048 bins, added up by shares and read back, took 8500 cycles against 3000).  Then
-//  - where at most 2048 tokens lie up to that bin (the usual case) they are listed, in index order, in
-//    the first CTA's shared memory; that CTA makes the exact cuts and picks the token;
-//  - otherwise the bin's own tokens are listed in every CTA, which finds the exact cut among them (where
-//    they too are more than 2048: histograms over 512 parts of the bin, then over the values of l in the
-//    part until one is left); then the cluster sums the kept weights by stretches of the index.
+// A row is never sorted: histograms find where the order is cut, and the tokens next to the cut are listed
+// and cut exactly.  Two kernels do this; the launch takes the second where many rows wait on one another.
+//
+// Few rows (sample_kernel): a row is held in the shared memory of a cluster of CTAs and read from global
+// memory once.  A histogram over 512 bins of (max - l) / T, which grows as the order goes on, of counts (for
+// top-k) or of counts and weights (top-p alone) finds the bin of the cut: every CTA adds up the cluster's
+// histograms for itself, 16 bytes a load, so that this costs one cluster barrier (2048 bins, added up by
+// shares and read back, took 8500 cycles against 3000).  Then
+//  - where at most 2048 tokens lie up to that bin they are listed, in index order, in the first CTA's
+//    shared memory; that CTA makes the exact cuts and picks the token;
+//  - otherwise the bin's own tokens are listed there and the first CTA finds the cut among them for all
+//    (where they too are more than 2048: histograms over 512 parts of the bin, then over the values of l
+//    in the part until one is left); then the cluster sums the kept weights by stretches of the index.
+// One row of 128256 fp32 logits takes 11.9 us, of which the reads are less than one: the rest is a chain of
+// some ten barriers and shared-memory steps.
+//
+// Many rows (sample_alone_kernel): a CTA a row, two an SM, so that no row waits for a place in shared memory
+// and no step for a cluster.  The first pass over the row, which the memory's rate bounds (23 us for 256 rows
+// of 128256 in fp32, 19 at the rate of a copy), leaves the largest logit of each group of 128 (or 256)
+// tokens; what comes after reads the groups that matter, from the L2 where they are still there:
+//  - top-k: the groups whose largest logit is among the k largest of them, in whose bins the k tokens lie
+//    (k = 50: 33 us in all, where the clusters took 106);
+//  - larger k, and top-p alone: the first pass also counts tokens by finer bins, on a scale that does not need
+//    the maximum.  For k they give the tokens to list (60 to 88 us; the shared atomics take 0.8 us a million).
+//    For top-p they bound each bin's weight, which leaves the cut to a few bins, and one more pass sums
+//    weights and lists the bins' tokens (86 us; clusters 195; histograms of all weights took 150);
+//  - no cut: one more pass of exponentials, whose instructions bound it (52 us; clusters 77).
+// A bound that does not hold is seen, exactly, and the row goes the way of the other kernel's steps.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cstddef>
 #include <cmath>
 
 #include "ham_mx.cuh"
@@ -57,13 +76,23 @@ struct SampleArgs {
 // half's sum within 32 bits.
 struct __align__(16) Histogram { uint32_t count[kBins], low[kBins], high[kBins]; };
 
+// Groups of a row that one CTA reads by itself: a vector a lane of a warp.  (The row's first vector may
+// begin before the row.)
+constexpr int kGroups = kSampleMaxVocab / 4 / 32 + 1;
+constexpr int kCopies = 8;               // histograms of such a CTA, one for two warps
+constexpr int kPart = 256;               // tokens that a warp of it lists at once
+constexpr int kFineBins = 4096, kFineCopies = 3, kFineEach = kFineBins / 2 / kSampleThreads;
+constexpr float kFinePerX = 4.f * kBinsPerX;
+constexpr int kQuad = 4;                 // groups that a warp of it has on their way, and takes together
+constexpr int kQuads = (kGroups + kQuad - 1) / kQuad;
+
 // What a CTA shares with its cluster beside the logits.
 struct SampleShared {
   Histogram h;
-  float list_l[kList];                    // the row's listed tokens, by index
+  __align__(16) float list_l[kList];      // the row's listed tokens, by index
   int32_t list_i[kList];
-  uint32_t own[kList];                    // this CTA's: their places among its logits
-  uint64_t sorted[kList];
+  uint32_t own[kGroups];                  // this CTA's: their places among its logits
+  uint64_t sorted[kGroups];
   uint64_t total_mass, warp_mass[kSampleWarps];
   uint32_t warp_count[kSampleWarps];
   float best, warp_best[kSampleWarps];
@@ -77,6 +106,19 @@ struct SampleShared {
   float cut_value;
   uint32_t cut_ties, cut_by_index;
   uint64_t cut_mass;
+};
+static_assert(kFineBins * kFineCopies * 4 <= sizeof(Histogram) * kCopies, "finer histogram");
+static_assert(kQuads * 8 + kSampleWarps * kPart * 4 <= sizeof(Histogram) * kCopies, "lists");
+static_assert(offsetof(SampleShared, sorted) + sizeof(SampleShared::sorted) - offsetof(SampleShared, list_l) >=
+                  kSampleWarps * kQuad * 512, "the groups on their way");
+static_assert(kQuad * 32 * 8 <= kSampleWarps * kPart, "a quad's tokens");
+static_assert(kGroups >= kList && kGroups * 2 >= kSampleWarps * kPart, "lists");
+
+// What a CTA that reads a row by itself has beside it.
+struct RowShared {
+  Histogram h[kCopies];
+  uint32_t group_max[kGroups];            // keys of the groups' largest logits
+  uint4 edge[2];                          // the first and the last vector, where they stick out of the row
 };
 
 __device__ __forceinline__ float load_logit(const float *p) { return *p; }
@@ -124,6 +166,14 @@ __device__ __forceinline__ uint4 ld_cluster_u32x4(uint32_t a) {
   uint4 v;
   asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
   return v;
+}
+__device__ __forceinline__ void cp_async16(uint4 *to, const uint4 *from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
 }
 __device__ __forceinline__ void cluster_arrive() {
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
@@ -206,7 +256,9 @@ struct Vec {
   }
 };
 
-template <typename T>
+constexpr float kWhole = 12582912.f;     // 1.5 2^23
+
+template <typename T, bool kAlone>
 struct Row {
   static constexpr int kN = Vec<T>::kN;
   SampleShared &s;
@@ -214,6 +266,11 @@ struct Row {
   int first_index;         // index of the first vector's first element (slice further on in the next CTA)
   int slice, vecs, ctas, rank, tid;
   Scale c;
+  // kAlone: the row stays in global memory, and this CTA reads it in groups, a warp a run of them
+  RowShared *w;
+  const uint4 *from;       // the row's vectors, of which whole0 .. whole1 - 1 lie in it whole
+  int whole0, whole1, groups, g0, g1;
+  bool infinite;           // the largest logit is: those like it are as likely as one another, nothing else is
 
   __device__ void sync() const {
     if (ctas > 1) cluster_sync_all();
@@ -228,11 +285,108 @@ struct Row {
     const int q = tid & 31;
     return q < ctas ? ld_cluster_u64(peer(p, q)) : 0ull;
   }
-  // f(vector) for every vector of this CTA's logits, in any order.
+  __device__ __forceinline__ Histogram &hist() const {
+    if constexpr (kAlone) return w->h[tid >> 6];
+    return s.h;
+  }
+  __device__ __forceinline__ uint4 vector(int v) const {
+    if (v >= whole0 && v < whole1) return __ldg(from + v);
+    const uint32_t none = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+    return v < vecs ? w->edge[v > 0] : make_uint4(none, none, none, none);
+  }
+  __device__ __forceinline__ Vec<T> logits(const uint4 &v) const {
+    Vec<T> x(v);
+    if (infinite)
+#pragma unroll
+      for (int j = 0; j < kN; ++j) x.l[j] = x.l[j] == INFINITY ? 0.f : -INFINITY;
+    return x;
+  }
+  __device__ __forceinline__ float logit_at(int place) const {
+    const int v = place / kN;
+    const uint4 *x = v >= whole0 && v < whole1 ? from + v : &w->edge[v > 0];
+    const float l = load_logit(reinterpret_cast<const T *>(x) + place % kN);
+    return !infinite ? l : l == INFINITY ? 0.f : -INFINITY;
+  }
+  // For this warp's quads of groups, any of which has want(group): f(group, vector) for the four, then
+  // end(quad); all lanes together.  The groups come through shared memory (the lists' place), a quad on
+  // its way and each lane's vector by itself.  Every other pass goes down: what was read last is still in
+  // the L2.
+  template <bool kDown, typename P, typename F, typename E>
+  __device__ __forceinline__ void run(P want, F f, E end) const {
+    const int lane = tid & 31;
+    uint4 *ring = reinterpret_cast<uint4 *>(s.list_l) + (tid >> 5) * kQuad * 32 + lane;
+    int b = kDown ? (g1 - g0 + 31) / 32 * 32 : -32;   // of the next quad: its window of 32 groups,
+    uint32_t mask = 0;                                // and the window's quads from it on
+    const auto next = [&]() {
+      while (!mask) {
+        b += kDown ? -32 : 32;
+        if (kDown ? b < 0 : b >= g1 - g0) return -1;
+        const int g = g0 + b + lane;
+        mask = __ballot_sync(kFull, g < g1 && want(g));
+        mask = (mask | mask >> 1 | mask >> 2 | mask >> 3) & 0x11111111u;
+      }
+      const int at = kDown ? 31 - __clz(mask) : __ffs(mask) - 1;
+      mask ^= 1u << at;
+      return g0 + b + at;
+    };
+    const auto load = [&](int g, int i) {
+      if (g >= 0) {
+        const int v = (g + i) * 32 + lane;
+        if (v >= whole0 && v < whole1) cp_async16(ring + i * 32, from + v);
+        else ring[i * 32] = vector(v);
+      }
+      cp_async_commit();
+    };
+    int g = next();
+#pragma unroll
+    for (int i = 0; i < kQuad; ++i) load(g, kDown ? kQuad - 1 - i : i);
+    while (g >= 0) {
+      const int then = next();
+#pragma unroll
+      for (int n = 0; n < kQuad; ++n) {
+        const int i = kDown ? kQuad - 1 - n : n;
+        cp_async_wait<kQuad - 1>();
+        f(g + i, logits(ring[i * 32]));
+        load(then, i);
+      }
+      end(g / kQuad);
+      g = then;
+    }
+    cp_async_wait<0>();
+  }
+  // f(group, vector) for the few of this warp's groups for which want(group), four at once; the lists
+  // stay as they are.
+  template <typename P, typename F>
+  __device__ __forceinline__ void run_few(P want, F f) const {
+    const int lane = tid & 31;
+    for (int b = 0; b < g1 - g0; b += 32) {
+      const int mine = g0 + b + lane;
+      uint32_t mask = __ballot_sync(kFull, mine < g1 && want(mine));
+      while (mask) {
+        constexpr int kAtOnce = 4;
+        int g[kAtOnce];
+        uint4 v[kAtOnce];
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j, mask &= mask - 1) g[j] = mask ? g0 + b + __ffs(mask) - 1 : -1;
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j)
+          if (g[j] >= 0) v[j] = vector(g[j] * 32 + lane);
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j)
+          if (g[j] >= 0) f(g[j], logits(v[j]));
+      }
+    }
+  }
+  __device__ __forceinline__ float max_of(int g) const { return logit_of(w->group_max[g]); }
+  // f(vector) for every vector of this CTA's logits that has a weight, in any order.
   template <typename F>
   __device__ __forceinline__ void each(F f) const {
+    if constexpr (kAlone) {
+      run<true>([&](int g) { return has_bin(place_of(max_of(g), c)); }, [&](int, const Vec<T> &x) { f(x); }, [](int) {});
+    } else {
 #pragma unroll 2
-    for (int v = tid; v < vecs; v += kSampleThreads) f(Vec<T>(data[v]));
+      for (int v = tid; v < vecs; v += kSampleThreads) f(Vec<T>(data[v]));
+    }
   }
   // This thread's stretch of the vectors: the threads' stretches follow one another in index order.  (An
   // odd number of vectors each, so that a warp's loads of 16 bytes fall on different banks.)
@@ -255,6 +409,7 @@ struct Row {
   // Computed for the whole vector first: a vector's chains of arithmetic overlap.
   template <bool kMasses, typename I, typename B>
   __device__ __forceinline__ void histogram(I in, B bin) const {
+    Histogram &h = hist();
     each([&](const Vec<T> &x) {
       float f[kN];
       uint32_t w[kN];
@@ -267,8 +422,8 @@ struct Row {
       for (int j = 0; j < kN; ++j)
         if (in(f[j], x.l[j])) {
           const int b = bin(f[j], x.l[j]);
-          atomicAdd(&s.h.count[b], 1u);
-          if (kMasses) add_mass(b, w[j]);
+          atomicAdd(&h.count[b], 1u);
+          if (kMasses) add_mass(h, b, w[j]);
         }
     });
   }
@@ -276,13 +431,18 @@ struct Row {
   __device__ __forceinline__ void histogram_of_bins() const {
     histogram<kMasses>([](float f, float) { return has_bin(f); }, [](float f, float) { return (int)f; });
   }
-  __device__ void clear() const {
-    for (int i = tid; i < kBins; i += kSampleThreads) s.h.count[i] = s.h.low[i] = s.h.high[i] = 0;
+  __device__ void clear(Histogram *h, int many) const {
+    uint4 *p = reinterpret_cast<uint4 *>(h);
+    for (int i = tid; i < many * (int)(sizeof(Histogram) / 16); i += kSampleThreads) p[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
   }
-  __device__ __forceinline__ void add_mass(int bin, uint32_t w) const {
-    atomicAdd(&s.h.low[bin], w & 0xffffu);
-    if (w >> 16) atomicAdd(&s.h.high[bin], w >> 16);
+  __device__ void clear() const {
+    if constexpr (kAlone) clear(w->h, kCopies);
+    else clear(&s.h, 1);
+  }
+  __device__ __forceinline__ void add_mass(Histogram &h, int bin, uint32_t w) const {
+    atomicAdd(&h.low[bin], w & 0xffffu);
+    if (w >> 16) atomicAdd(&h.high[bin], w >> 16);
   }
   // The share of a row's weight that top-p reaches for: whole numbers from here on (a sum reaches the
   // fp64 product if it reaches the whole number above).
@@ -299,11 +459,14 @@ struct Row {
     uint64_t m4[4] = {0, 0, 0, 0}, m_sum = 0, mi = 0;
     uint32_t c4[4], c_sum = 0, ci = 0;
     if (group == 0 || (masses && group < 3)) {
-      const uint32_t at = smem_u32((group == 0 ? s.h.count : group == 1 ? s.h.high : s.h.low) + quad * 4);
+      static_assert(kCopies == kMaxCluster, "histograms of a row");
+      const int offset = (group == 0 ? 0 : group == 1 ? 2 : 1) * kBins + quad * 4;  // count, high, low
       uint4 v[kMaxCluster];
 #pragma unroll
-      for (int q = 0; q < kMaxCluster; ++q)
-        v[q] = q < ctas ? ld_cluster_u32x4(cluster_map_shared(at, q)) : make_uint4(0, 0, 0, 0);
+      for (int q = 0; q < kMaxCluster; ++q) {
+        if constexpr (kAlone) v[q] = *reinterpret_cast<const uint4 *>(w->h[q].count + offset);
+        else v[q] = q < ctas ? ld_cluster_u32x4(peer(s.h.count + offset, q)) : make_uint4(0, 0, 0, 0);
+      }
 #pragma unroll
       for (int q = 0; q < kMaxCluster; ++q) m4[0] += v[q].x, m4[1] += v[q].y, m4[2] += v[q].z, m4[3] += v[q].w;
       if (group)
@@ -432,38 +595,100 @@ struct Row {
   // most kList, pull() then makes the row's list.
   __device__ uint32_t list(int first, int last) const {
     const float begin = (float)first, end = (float)(last + 1);  // (last < 511: a token up to it has a bin)
-    // the vectors that may hold some, by their largest and smallest logits; then their tokens
-    const uint32_t mask =
-        first == 0 ? which([&](const Vec<T> &x) { return place_of(x.largest(), c) < end; })
-                   : which([&](const Vec<T> &x) { return place_of(x.largest(), c) < end && place_of(x.smallest(), c) >= begin; });
-    int v0, v1;
-    stretch(v0, v1);
     const auto in = [&](float l) {
       const float f = place_of(l, c);
       return f < end && f >= begin;
     };
-    uint32_t many = 0;
-    for (uint32_t m = mask; m; m &= m - 1) {
-      const Vec<T> x(data[v0 + __ffs(m) - 1]);
-#pragma unroll
-      for (int j = 0; j < kN; ++j) many += in(x.l[j]);
-    }
-    uint64_t cta;
-    uint32_t at = (uint32_t)block_scan(s, many, cta) - many;
-    if (tid == 0) s.ties = (uint32_t)cta;
-    if (many && cta <= kList)
+    if constexpr (kAlone) {
+      return list_alone([&](int g) { return place_of(max_of(g), c) < end; }, in);
+    } else {
+      // the vectors that may hold some, by their largest and smallest logits; then their tokens
+      const uint32_t mask =
+          first == 0 ? which([&](const Vec<T> &x) { return place_of(x.largest(), c) < end; })
+                     : which([&](const Vec<T> &x) { return place_of(x.largest(), c) < end && place_of(x.smallest(), c) >= begin; });
+      int v0, v1;
+      stretch(v0, v1);
+      uint32_t many = 0;
       for (uint32_t m = mask; m; m &= m - 1) {
-        const int v = v0 + __ffs(m) - 1;
-        const Vec<T> x(data[v]);
+        const Vec<T> x(data[v0 + __ffs(m) - 1]);
+#pragma unroll
+        for (int j = 0; j < kN; ++j) many += in(x.l[j]);
+      }
+      uint64_t cta;
+      uint32_t at = (uint32_t)block_scan(s, many, cta) - many;
+      if (tid == 0) s.ties = (uint32_t)cta;
+      if (many && cta <= kList)
+        for (uint32_t m = mask; m; m &= m - 1) {
+          const int v = v0 + __ffs(m) - 1;
+          const Vec<T> x(data[v]);
+#pragma unroll
+          for (int j = 0; j < kN; ++j)
+            if (in(x.l[j])) s.own[at++] = v * kN + j;
+        }
+      sync();
+      return sum8(lane32(&s.ties));
+    }
+  }
+  // The same by one CTA: its row's list at once, where it has at most kList.  A warp notes the places of
+  // its groups' tokens (from kPart on: finds them again when it knows where they go).
+  template <typename P, typename I>
+  __device__ uint32_t list_alone(P want, I in) const {
+    const int lane = tid & 31, warp = tid >> 5;
+    uint32_t *part = reinterpret_cast<uint32_t *>(s.sorted) + warp * kPart;
+    uint32_t many = 0;                           // of the warp
+    const auto note = [&](int g, const Vec<T> &x, auto to) {
+      uint32_t mine = 0;
+#pragma unroll
+      for (int j = 0; j < kN; ++j) mine += in(x.l[j]);
+      if (!__any_sync(kFull, mine)) return;
+      uint32_t upto = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t v = __shfl_up_sync(kFull, upto, o);
+        if (lane >= o) upto += v;
+      }
+      uint32_t at = many + upto - mine;
+      if (mine)
 #pragma unroll
         for (int j = 0; j < kN; ++j)
-          if (in(x.l[j])) s.own[at++] = v * kN + j;
+          if (in(x.l[j])) to(at++, (uint32_t)((g * 32 + lane) * kN + j), x.l[j]);
+      many += __shfl_sync(kFull, upto, 31);
+    };
+    run_few(want, [&](int g, const Vec<T> &x) {
+      note(g, x, [&](uint32_t at, uint32_t place, float) {
+        if (at < (uint32_t)kPart) part[at] = place;
+      });
+    });
+    __syncthreads();                             // (the counts' last readers are done)
+    if (lane == 0) s.warp_count[warp] = many;
+    __syncthreads();
+    uint32_t all = 0, before = 0;
+    for (int q = 0; q < kSampleWarps; ++q) {
+      if (q < warp) before += s.warp_count[q];
+      all += s.warp_count[q];
+    }
+    if (all > (uint32_t)kList) return all;
+    if (many <= (uint32_t)kPart) {
+      for (uint32_t i = lane; i < many; i += 32) {
+        const uint32_t place = part[i];
+        s.list_l[before + i] = logit_at((int)place);
+        s.list_i[before + i] = first_index + (int)place;
       }
-    sync();
-    return sum8(lane32(&s.ties));
+    } else {
+      many = before;
+      run_few(want, [&](int g, const Vec<T> &x) {
+        note(g, x, [&](uint32_t at, uint32_t place, float l) {
+          s.list_l[at] = l;
+          s.list_i[at] = first_index + (int)place;
+        });
+      });
+    }
+    __syncthreads();
+    return all;
   }
   // The CTAs' lists of list(), one after the other.
   __device__ void pull(uint32_t all) const {
+    if (kAlone) return;
     uint32_t upto = lane32(&s.ties);             // lane q: the tokens of CTAs 0 .. q
 #pragma unroll
     for (int o = 1; o < kMaxCluster; o <<= 1) {
@@ -531,12 +756,12 @@ struct Row {
                           W weight) const {
     float base = (float)bin, mult = bins ? 1.f : (float)kBins;
     for (;;) {
-      clear();
+      clear(&s.h, 1);
       for (int i = tid; i < n; i += kSampleThreads) {
         const float at = (place_of(s.list_l[i], c) - base) * mult;  // (exact)
         if (at >= 0.f && at < (float)kBins) {
           atomicAdd(&s.h.count[(int)at], 1u);
-          add_mass((int)at, weight(i));
+          add_mass(s.h, (int)at, weight(i));
         }
       }
       __syncthreads();
@@ -619,7 +844,7 @@ struct Row {
     return k;
   }
   // The choice among the first CTA's list of `all` tokens up to bin `last`, by that CTA alone.  k > 0:
-  // top-k, which cuts in bin `last`, before which lie `before` tokens.  p >= 0: top-p, of the weight
+  // top-k, which cuts in bin `last` (-1: not known), before which lie `before` tokens.  p >= 0: top-p, of the weight
   // `row_mass` (0: of the list's, after top-k).  Up to a token a thread are sorted; of more, only the
   // cuts' parts are.
   __device__ void choose(const SampleArgs &a, int row, int all, int last, uint32_t before, int k, double p,
@@ -651,7 +876,7 @@ struct Row {
         for (int i = s.cut_at + 1 + tid; i < s.members; i += kSampleThreads) list_w[(uint32_t)s.sorted[i]] = 0;
         __syncthreads();
       };
-      if (k > 0) drop(cut_list(all, false, last, false, (uint64_t)k, before, 0, weight));
+      if (k > 0) drop(cut_list(all, last < 0, max(last, 0), false, (uint64_t)k, before, 0, weight));
       if (p >= 0.) {
         if (!row_mass) {
           uint64_t mine = 0;
@@ -686,6 +911,293 @@ struct Row {
       sum += w[j];
     }
   }
+  // Turns the quads' numbers into the running sums before them; their sum.
+  template <typename N>
+  __device__ uint64_t sum_before(N *of) const {
+    const int quads = (groups + kQuad - 1) / kQuad, per = (quads + kSampleThreads - 1) / kSampleThreads;
+    const int i0 = min(quads, tid * per), i1 = min(quads, i0 + per);
+    uint64_t mine = 0, all;
+    for (int i = i0; i < i1; ++i) mine += of[i];
+    uint64_t at = block_scan(s, mine, all) - mine;
+    for (int i = i0; i < i1; ++i) {
+      const N v = of[i];
+      of[i] = (N)at;
+      at += v;
+    }
+    __syncthreads();
+    return all;
+  }
+  // The quad in which the running sum of `mass` passes the aim of u, left in s.first, and the sum before
+  // it; `mass` is turned into running sums.
+  __device__ uint64_t find_quad(const SampleArgs &a, int row, uint64_t *mass, uint64_t &total) const {
+    const int quads = (groups + kQuad - 1) / kQuad;
+    total = sum_before(mass);
+    if (tid == 0) s.aim = pick(a.u[row], total), s.first = 0;
+    __syncthreads();
+    const uint64_t aim = s.aim;
+    for (int q = tid; q < quads; q += kSampleThreads)
+      if (mass[q] <= aim && aim < (q + 1 < quads ? mass[q + 1] : total)) s.first = q;
+    __syncthreads();
+    return mass[s.first];
+  }
+  // A warp's sum of numbers below 2^36: two parts that 32 lanes add up in 32 bits.
+  static __device__ __forceinline__ uint64_t warp_sum(uint64_t lanes) {
+    const uint32_t low = __reduce_add_sync(kFull, (uint32_t)lanes & 0xffffffu);
+    const uint32_t high = __reduce_add_sync(kFull, (uint32_t)(lanes >> 24));
+    return ((uint64_t)high << 24) + low;
+  }
+  // The token of that quad, by one warp; weigh(group, vector, to): the kept weights of a lane's logits.
+  template <typename W>
+  __device__ void pick_of_quad(const SampleArgs &a, int row, uint64_t before, uint64_t total, W weigh) const {
+    const int lane = tid & 31;
+    const uint64_t aim = s.aim;
+    uint4 v[kQuad];
+#pragma unroll
+    for (int i = 0; i < kQuad; ++i) v[i] = vector((s.first * kQuad + i) * 32 + lane);
+#pragma unroll
+    for (int i = 0; i < kQuad; ++i) {
+      const int g = s.first * kQuad + i;
+      uint32_t to[kN];
+      weigh(g, logits(v[i]), to);
+      uint64_t sum = 0;
+#pragma unroll
+      for (int j = 0; j < kN; ++j) sum += to[j];
+      uint64_t at = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint64_t u = __shfl_up_sync(kFull, at, o);
+        if (lane >= o) at += u;
+      }
+      const uint64_t upto = before + __shfl_sync(kFull, at, 31);
+      at += before - sum;
+#pragma unroll
+      for (int j = 0; j < kN; ++j) {
+        if (at <= aim && aim < at + to[j]) {
+          a.tokens[row] = first_index + (g * 32 + lane) * kN + j;
+          if (a.probs) a.probs[row] = (float)((double)to[j] / (double)total);
+        }
+        at += to[j];
+      }
+      before = upto;
+    }
+  }
+  // Which of the finer bins l lies in, on a scale that needs no row's maximum: the nearest whole number,
+  // up to 2^22, in the low bits of a float (and itself, less 1.5 2^23).
+  __device__ __forceinline__ static float fine_place(float l, float fine_bins) { return __fmaf_rn(l, fine_bins, kWhole); }
+  // Tokens of the finer bin n below that of the largest logit (where they lie too low for a weight, those
+  // may count as higher ones: the bins take turns).
+  __device__ __forceinline__ uint32_t fine_count(float top, int n) const {
+    const uint32_t *fine = reinterpret_cast<const uint32_t *>(w->h);
+    uint32_t many = 0;
+    for (int q = 0; q < kFineCopies; ++q) many += fine[q * kFineBins + ((__float_as_int(top) - n) & (kFineBins - 1))];
+    return many;
+  }
+  __device__ __forceinline__ bool has_fine_bins(float fine_bins) const { return fabsf(c.best * fine_bins) < 0x1p21f; }
+  // The first of the block's numbers, a thread's, whose running sum reaches k; which one, and the sum
+  // before it, in s.found and s.found_before_count, and with it in s.found_count.
+  __device__ void first_to_reach(uint32_t k, uint32_t mine, uint32_t before) const {
+    uint64_t all;
+    const uint32_t upto = before + (uint32_t)block_scan(s, mine, all);
+    if (tid == 0) s.found = -1;
+    __syncthreads();
+    if (upto >= k && upto - mine < k) s.found = tid, s.found_before_count = upto - mine, s.found_count = upto;
+    __syncthreads();
+  }
+  // Lists the row's tokens up to the finer bin of the k-th, or up to a 512th of it; their number.
+  // 0: the bins do not tell it, or it is too many.
+  __device__ uint32_t list_first(uint32_t k, float fine_bins) const {
+    if (!has_fine_bins(fine_bins) || k > (uint32_t)kList) return 0;
+    const float top = fine_place(c.best, fine_bins);
+    uint32_t count[kFineEach], sum = 0;
+#pragma unroll
+    for (int j = 0; j < kFineEach; ++j) sum += count[j] = fine_count(top, kFineEach * tid + j);
+    first_to_reach(k, sum, 0);
+    if (s.found == tid) {
+      uint32_t upto = s.found_before_count;
+      bool found = false;
+#pragma unroll
+      for (int j = 0; j < kFineEach; ++j) {
+        if (!found && upto + count[j] >= k) {
+          found = true;
+          s.members = kFineEach * tid + j;
+          s.found_before_count = upto, s.found_count = upto + count[j];
+        }
+        upto += count[j];
+      }
+    }
+    __syncthreads();
+    // (the last bins may hold tokens that have no place among the others)
+    if (s.found < 0 || s.members >= kFineBins / 2 - 8) return 0;
+    const float bin = top - (float)s.members;
+    uint32_t listed;
+    if (s.found_count <= (uint32_t)kList) {
+      const auto in = [&](float l) { return fine_place(l, fine_bins) >= bin; };
+      listed = list_alone([&](int g) { return in(max_of(g)); }, in);
+    } else {
+      const uint32_t before = s.found_before_count;
+      const float at = kWhole - bin;             // l's part of the bin: -1/2 .. 1/2
+      const auto part = [&](float l) { return __fmaf_rn(l, fine_bins, at); };
+      clear(&s.h, 1);
+      run<true>([&](int g) { return fine_place(max_of(g), fine_bins) >= bin; }, [&](int, const Vec<T> &x) {
+#pragma unroll
+        for (int j = 0; j < kN; ++j)
+          if (fine_place(x.l[j], fine_bins) == bin) atomicAdd(&s.h.count[min(max((int)((0.5f - part(x.l[j])) * (float)kBins), 0), kBins - 1)], 1u);
+      }, [](int) {});
+      __syncthreads();
+      first_to_reach(k, s.h.count[tid], before);
+      if (s.found < 0 || s.found_count > (uint32_t)kList) return 0;
+      const float least = 0.5f - (float)(s.found + 1) / (float)kBins;
+      const auto in = [&](float l) { return part(l) >= least; };
+      listed = list_alone([&](int g) { return in(max_of(g)); }, in);
+    }
+    return listed >= k && listed <= (uint32_t)kList ? listed : 0u;
+  }
+  // Top-p alone.  The counts of the finer bins, taken as the row was read, bound each bin's weight from
+  // both sides (by its ends' weights, 1.1% apart), and so the share of the row's weight up to each bin:
+  // they leave the cut to a few bins.  One pass then sums the weights of the row, of its groups' tokens
+  // above those bins, and lists the bins' own, among which the cut is made.  False, with nothing chosen:
+  // the bounds do not hold the cut (fine_place out of range), or hold too many tokens.
+  __device__ bool top_p(const SampleArgs &a, int row, double p, uint32_t least, float fine_bins) const {
+    const int lane = tid & 31, warp = tid >> 5;
+    if (!has_fine_bins(fine_bins)) return false;
+    const float top = fine_place(c.best, fine_bins), over = __fmaf_rn(c.best, fine_bins, kWhole - top);
+    // ---- the bounds
+    float lo[kFineEach], hi[kFineEach], sum_lo = 0.f, sum_hi = 0.f;
+#pragma unroll
+    for (int j = 0; j < kFineEach; ++j) {
+      const int n = kFineEach * tid + j;
+      const uint32_t many = fine_count(top, n);
+      const float d = (float)n + over + 0.5f;    // of the bin's far end
+      sum_lo = lo[j] = sum_lo + (float)many * expf(-d / kFinePerX);
+      sum_hi = hi[j] = sum_hi + (float)many * expf(-fmaxf(d - 1.f, 0.f) / kFinePerX);
+    }
+    float run_lo = sum_lo, run_hi = sum_hi;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const float x = __shfl_up_sync(kFull, run_lo, o), y = __shfl_up_sync(kFull, run_hi, o);
+      if (lane >= o) run_lo += x, run_hi += y;
+    }
+    if (lane == 31) s.warp_max[warp] = __float_as_uint(run_lo), s.warp_min[warp] = __float_as_uint(run_hi);
+    if (tid == 0) s.key_min = s.key_max = kFineBins / 2 - 1;
+    __syncthreads();
+    float all_lo = 0.f, all_hi = 0.f;
+    run_lo -= sum_lo, run_hi -= sum_hi;
+    for (int q = 0; q < kSampleWarps; ++q) {
+      const float x = __uint_as_float(s.warp_max[q]), y = __uint_as_float(s.warp_min[q]);
+      if (q < warp) run_lo += x, run_hi += y;
+      all_lo += x, all_hi += y;
+    }
+    constexpr float kSlack = 4e-6f;              // for these sums' rounding
+#pragma unroll
+    for (int j = kFineEach - 1; j >= 0; --j) {
+      const float l = run_lo + lo[j], h = run_hi + hi[j];
+      if (h >= ((float)p - kSlack) * (h + fmaxf(all_lo - l, 0.f))) atomicMin(&s.key_min, (uint32_t)(kFineEach * tid + j));
+      if (l >= ((float)p + kSlack) * (l + fmaxf(all_hi - h, 0.f))) atomicMin(&s.key_max, (uint32_t)(kFineEach * tid + j));
+    }
+    __syncthreads();                             // (and the bins are read)
+    const float above = top - (float)s.key_min + 1.f, from_bin = top - (float)s.key_max;
+    // ---- the pass; a warp's list is filled from its end, as its groups go down
+    uint64_t *mass = reinterpret_cast<uint64_t *>(w->h);
+    uint32_t *part = reinterpret_cast<uint32_t *>(mass + kQuads) + warp * kPart;
+    for (int q = tid; q < kQuads; q += kSampleThreads) mass[q] = 0;
+    __syncthreads();
+    uint64_t whole = 0, upper = 0, sum = 0;
+    uint32_t many = 0;
+    run<true>([&](int g) { return weight_of(max_of(g), c) > 0; }, [&](int g, const Vec<T> &x) {
+      uint32_t mine = 0;
+#pragma unroll
+      for (int j = 0; j < kN; ++j) {
+        const uint32_t v = weight_of(x.l[j], c);
+        const float f = fine_place(x.l[j], fine_bins);
+        whole += v;
+        if (f >= above) {
+          upper += v;
+          if (v >= least) sum += v;
+        } else {
+          mine += f >= from_bin;
+        }
+      }
+      if (!__any_sync(kFull, mine)) return;
+      uint32_t after = mine;                     // of this lane and those after it
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t v = __shfl_down_sync(kFull, after, o);
+        if (lane + o < 32) after += v;
+      }
+      uint32_t at = many + after;
+      if (mine)
+#pragma unroll
+        for (int j = 0; j < kN; ++j) {
+          const float f = fine_place(x.l[j], fine_bins);
+          if (f < above && f >= from_bin) {
+            if (at <= (uint32_t)kPart) part[kPart - at] = (uint32_t)((g * 32 + lane) * kN + j);
+            --at;
+          }
+        }
+      many += __shfl_sync(kFull, after, 0);
+    }, [&](int q) {
+      const uint64_t all = warp_sum(sum);
+      if (lane == 0) mass[q] = all;
+      sum = 0;
+    });
+    // ---- the row's list, and its sums
+    if (lane == 0) s.warp_count[warp] = many;
+    uint64_t row_mass, upper_mass;
+    block_scan(s, whole, row_mass);
+    block_scan(s, upper, upper_mass);
+    uint32_t all = 0, before = 0, longest = 0;
+    for (int q = 0; q < kSampleWarps; ++q) {
+      const uint32_t v = s.warp_count[q];
+      if (q < warp) before += v;
+      all += v;
+      longest = max(longest, v);
+    }
+    if (longest > (uint32_t)kPart || all > (uint32_t)kList) return false;
+    uint32_t *list_w = s.own;
+    uint64_t listed = 0;
+    for (uint32_t i = lane; i < many; i += 32) {
+      const uint32_t place = part[kPart - many + i];
+      const float l = logit_at((int)place);
+      const uint32_t v = weight_of(l, c);
+      s.list_l[before + i] = l;
+      s.list_i[before + i] = (int)place;
+      list_w[before + i] = v;
+      listed += v;
+    }
+    uint64_t list_mass;
+    block_scan(s, listed, list_mass);
+    const uint64_t aim = aim_of(p, row_mass);
+    if (upper_mass >= aim || upper_mass + list_mass < aim) return false;
+    __syncthreads();
+    const Cut cut = cut_list((int)all, true, 0, true, aim, 0, upper_mass, [&](int i) { return list_w[i]; });
+    for (int i = tid; i < (int)all; i += kSampleThreads)
+      if (s.list_l[i] < cut.value || list_w[i] < least) list_w[i] = 0;
+    for (int i = s.cut_at + 1 + tid; i < s.members; i += kSampleThreads) list_w[(uint32_t)s.sorted[i]] = 0;
+    __syncthreads();
+    constexpr int kTokens = kQuad * 32 * kN;
+    for (int i = tid; i < (int)all; i += kSampleThreads)
+      if (list_w[i]) atomicAdd(reinterpret_cast<unsigned long long *>(mass + s.list_i[i] / kTokens), (unsigned long long)list_w[i]);
+    __syncthreads();
+    // ---- the quad, and in it the token
+    uint64_t total;
+    const uint64_t ahead = find_quad(a, row, mass, total);
+    uint32_t *of_quad = part - warp * kPart;     // the listed ones of the quad
+    for (int i = tid; i < kTokens; i += kSampleThreads) of_quad[i] = 0;
+    __syncthreads();
+    for (int i = tid; i < (int)all; i += kSampleThreads)
+      if (s.list_i[i] / kTokens == s.first) of_quad[s.list_i[i] % kTokens] = list_w[i];
+    __syncthreads();
+    if (warp == 0)
+      pick_of_quad(a, row, ahead, total, [&](int g, const Vec<T> &x, uint32_t (&to)[kN]) {
+#pragma unroll
+        for (int j = 0; j < kN; ++j) {
+          const uint32_t v = weight_of(x.l[j], c);
+          to[j] = fine_place(x.l[j], fine_bins) >= above ? v >= least ? v : 0u
+                                                         : of_quad[(g % kQuad * 32 + lane) * kN + j];
+        }
+      });
+    return true;
+  }
   // floor(u S), below S
   static __device__ uint64_t pick(float u, uint64_t whole) {
     const double v = fmin(fmax((double)u, 0.), 1.);  // (a NaN becomes 0)
@@ -696,6 +1208,8 @@ struct Row {
 
 constexpr int kSampleFixed = (int)(sizeof(SampleShared) + 15) / 16 * 16;  // shared memory before the logits
 static_assert(kBins == kSampleThreads, "a thread a bin");
+constexpr int kAloneSmem = kSampleFixed + (int)sizeof(RowShared);
+static_assert(kAloneSmem <= kSampleSmem2, "two CTAs an SM");
 
 template <typename T>
 __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a) {
@@ -747,7 +1261,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
   __syncthreads();
   best = warp_max_f32(lane < kSampleWarps ? s.warp_best[lane] : -INFINITY);
   if (tid == 0) s.best = best;
-  Row<T> r{s, store, rank * a.slice - phase, a.slice, vecs, ctas, rank, tid, Scale{}};
+  Row<T, false> r{s, store, rank * a.slice - phase, a.slice, vecs, ctas, rank, tid, Scale{}, nullptr, nullptr, 0, 0, 0, 0, 0, false};
   r.sync();
   best = warp_max_f32(lane < ctas ? __uint_as_float(r.lane32(&s.best)) : -INFINITY);
   const bool greedy = !(temperature > 0.f);
@@ -823,7 +1337,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
       }
       if (!all_in) cut = r.cut(false, (uint64_t)k);
       if (by_p) {
-        aim = Row<T>::aim_of(share, all_in ? s.total_mass : cut.mass);
+        aim = Row<T, false>::aim_of(share, all_in ? s.total_mass : cut.mass);
         r.sync();
         r.clear();
         r.template histogram_of_bins<true>();
@@ -880,7 +1394,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
   const uint64_t theirs = r.lane64(&s.kept), total = sum8(theirs);
   before += sum8(lane < rank ? theirs : (uint64_t)0);
   if (warp == 0) {
-    const uint64_t v = Row<T>::pick(a.u[row], total);
+    const uint64_t v = Row<T, false>::pick(a.u[row], total);
     if (lane == 0) s.aim = v;
   }
   __syncthreads();
@@ -921,6 +1435,235 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
   r.sync();  // (a peer may still read this CTA's sums)
 }
 
+// The same choice with a row a CTA, two of them an SM.
+template <typename T>
+__global__ void __launch_bounds__(kSampleThreads, 2) sample_alone_kernel(SampleArgs a) {
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  SampleShared &s = *reinterpret_cast<SampleShared *>(smem_raw);
+  RowShared &w = *reinterpret_cast<RowShared *>(smem_raw + kSampleFixed);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, row = blockIdx.x;
+  constexpr int kVec = Vec<T>::kN;
+  {
+    uint4 *p = reinterpret_cast<uint4 *>(w.h);
+    for (int i = tid; i < (int)sizeof(w.h) / 16; i += kSampleThreads) p[i] = make_uint4(0, 0, 0, 0);
+  }
+  grid_dependency_wait();
+  grid_launch_dependents();
+  const T *src = static_cast<const T *>(a.logits) + (int64_t)row * a.vocab;
+  const int phase = (int)(((uintptr_t)src & 15u) / sizeof(T));
+  const int vecs = (phase + a.vocab + kVec - 1) / kVec, groups = (vecs + 31) / 32;
+  const int per = (groups + kSampleWarps * kQuad - 1) / (kSampleWarps * kQuad) * kQuad;  // (whole quads)
+  const int g0 = min(groups, warp * per), g1 = min(groups, g0 + per);
+  Row<T, true> r{s, nullptr, -phase, 0, vecs, 1, 0, tid, Scale{}, &w, reinterpret_cast<const uint4 *>(src - phase),
+                 phase ? 1 : 0, (phase + a.vocab) / kVec, groups, g0, g1, false};
+  // the vectors that stick out of the row, by the warps that read them
+  for (int e = 0; e < 2; ++e) {
+    const int v = e ? vecs - 1 : 0, g = v / 32, i = v * kVec + lane - phase;
+    if (g >= g0 && g < g1 && lane < kVec) {
+      const float x = i >= 0 && i < a.vocab ? load_logit(src + i) : -INFINITY;
+      T *to = reinterpret_cast<T *>(&w.edge[e]) + lane;
+      if constexpr (sizeof(T) == 4) *to = x;
+      else *to = (T)(__float_as_uint(x) >> 16);
+    }
+  }
+  const float temperature = a.temperature ? a.temperature[row] : 1.f;
+  const int k = a.top_k ? a.top_k[row] : 0;
+  const float p = a.top_p ? a.top_p[row] : 1.f;
+  const float min_p = a.min_p ? a.min_p[row] : 0.f;
+  const bool greedy = !(temperature > 0.f), by_k = k > 0 && k < a.vocab, by_p = p < 1.f;
+  const bool fine = !greedy && (by_k ? 4 * (int64_t)k > groups : by_p);
+  const float fine_bins = fine ? __fdiv_rn(kFinePerX, scale_of(0.f, temperature).t) : 0.f;
+  uint32_t *const fine_counts = reinterpret_cast<uint32_t *>(w.h) + warp % kFineCopies * kFineBins;
+  __syncthreads();
+  // ---- the groups' largest logits, and the row's
+  uint32_t most = 0;
+  r.template run<false>([](int) { return true; }, [&](int g, const Vec<T> &x) {
+    if (g >= groups) return;
+    const uint32_t m = __reduce_max_sync(kFull, key_of(fmaxf(x.largest(), -INFINITY)));
+    if (lane == 0) w.group_max[g] = m;
+    most = max(most, m);
+    if (fine) {                                  // (what lies too far below the largest so far has no weight)
+      const float least_place = Row<T, true>::fine_place(logit_of(most), fine_bins) - (float)(kFineBins / 2);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        const float f = Row<T, true>::fine_place(x.l[i], fine_bins);
+        if (f >= least_place) atomicAdd(fine_counts + (__float_as_int(f) & (kFineBins - 1)), 1u);
+      }
+    }
+  }, [](int) {});
+  if (lane == 0) s.warp_max[warp] = most;
+  __syncthreads();
+  most = __reduce_max_sync(kFull, lane < kSampleWarps ? s.warp_max[lane] : 0u);
+  float best = logit_of(most);
+  if (best == INFINITY) {                        // as likely as one another, and nothing else is
+    best = 0.f;
+    r.infinite = true;
+    for (int g = tid; g < groups; g += kSampleThreads)
+      w.group_max[g] = key_of(w.group_max[g] == most ? 0.f : -INFINITY);
+    __syncthreads();
+  }
+  const bool none = best == -INFINITY;
+  r.c = scale_of(best, greedy ? 1.f : temperature);
+  if (none || greedy) {
+    if (tid == 0) s.first = groups;
+    __syncthreads();
+    for (int g = tid; g < groups; g += kSampleThreads)
+      if (logit_of(w.group_max[g]) == best) {
+        atomicMin(&s.first, g);
+        break;
+      }
+    __syncthreads();
+    if (warp == 0) {
+      int first = INT32_MAX;
+      const Vec<T> x = r.logits(r.vector(s.first * 32 + lane));
+#pragma unroll
+      for (int j = kVec - 1; j >= 0; --j)
+        if (x.l[j] == best) first = (s.first * 32 + lane) * kVec + j - phase;
+      first = __reduce_min_sync(kFull, first);
+      if (lane == 0) {
+        a.tokens[row] = none ? -1 : first;
+        if (a.probs) a.probs[row] = none ? 0.f : 1.f;
+      }
+    }
+    return;
+  }
+  const double share = by_p ? fmax((double)p, 0x1p-80) : 1.;  // (at least the likeliest token)
+  const uint32_t least = min_p > 0.f ? (uint32_t)ceilf(fminf(min_p, 1.f) * kFine) : 0u;
+  Cut cut;
+  if (by_k && !fine) {
+    // k groups' largest logits are k tokens: what the row's k-th place is, or before it
+    for (int g = tid; g < groups; g += kSampleThreads) {
+      const float f = place_of(logit_of(w.group_max[g]), r.c);
+      if (has_bin(f)) atomicAdd(&w.h[0].count[(int)f], 1u);
+    }
+    r.find(false, false, 0, 0, (uint64_t)k);
+    if (s.found >= 0) {
+      const uint32_t listed = r.list(0, s.found);
+      if (listed <= (uint32_t)kList) {
+        r.choose(a, row, (int)listed, -1, 0, k, by_p ? share : -1., 0, least);
+        return;
+      }
+    }
+    r.clear();
+  }
+  if (fine) {
+    if (by_k) {
+      const uint32_t listed = r.infinite ? 0u : r.list_first((uint32_t)k, fine_bins);
+      if (listed) {
+        r.choose(a, row, (int)listed, -1, 0, k, by_p ? share : -1., 0, least);
+        return;
+      }
+    } else if (!r.infinite && r.top_p(a, row, share, least, fine_bins)) {
+      return;
+    }
+    __syncthreads();
+    r.clear();
+  }
+  if (by_k || by_p) {
+    if (by_k) r.template histogram_of_bins<false>();
+    else r.template histogram_of_bins<true>();
+    r.find(!by_k, !by_k, 0, 0, (uint64_t)k, by_k ? 0. : share);
+    const bool all_in = s.found < 0;             // fewer than k tokens have any weight
+    const int last = all_in ? kBins - 2 : s.found;
+    const uint32_t before = all_in ? 0 : s.found_before_count;
+    const uint64_t whole = by_k ? 0 : s.total_mass;
+    uint64_t aim = s.aim;
+    const uint32_t all = all_in ? kList : before + s.found_count;
+    if (all <= (uint32_t)kList) {
+      const uint32_t listed = r.list(0, last);
+      if (listed <= (uint32_t)kList) {           // (all_in: known only now)
+        r.choose(a, row, listed, last, before, by_k && !all_in ? k : 0, by_p ? share : -1., whole, least);
+        return;
+      }
+    }
+    if (by_k) {
+      if (by_p) {                                // (top-p wants the weight that top-k keeps)
+        __syncthreads();
+        r.clear();
+        r.template histogram_of_bins<true>();
+        r.find(false, true, 0, 0, (uint64_t)k);
+      }
+      if (!all_in) cut = r.cut(false, (uint64_t)k);
+      if (by_p) {
+        aim = Row<T, true>::aim_of(share, all_in ? s.total_mass : cut.mass);
+        __syncthreads();
+        r.clear();
+        r.template histogram_of_bins<true>();
+        r.find(true, true, 0, 0, aim);
+      }
+    }
+    if (by_p) cut = r.cut(true, aim);
+  }
+  // ---- the kept weights of each quad
+  __syncthreads();                               // (what was here was read)
+  uint64_t *mass = reinterpret_cast<uint64_t *>(w.h);
+  uint32_t *ties = reinterpret_cast<uint32_t *>(mass + kQuads);
+  const auto wanted = [&](int g) {
+    const float m = r.max_of(g);
+    return m >= cut.value && weight_of(m, r.c) >= max(least, 1u);
+  };
+  for (int q = tid; q < kQuads; q += kSampleThreads) mass[q] = 0, ties[q] = 0;
+  __syncthreads();
+  uint64_t sum = 0;
+  const auto leave = [&](int q) {
+    const uint64_t all = Row<T, true>::warp_sum(sum);
+    if (lane == 0) mass[q] = all;
+    sum = 0;
+  };
+  uint32_t tied = 0;                             // equals of the cut's value before the group
+  const auto weigh = [&](int g, const Vec<T> &x, uint32_t (&to)[kVec]) {
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) to[j] = r.kept(cut, least, x.l[j]);
+    if (cut.by_index) {                          // (all but the first of those by index are left out)
+      uint32_t mine = 0;
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) mine += x.l[j] == cut.value;
+      uint32_t upto = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t v = __shfl_up_sync(kFull, upto, o);
+        if (lane >= o) upto += v;
+      }
+      if (g % kQuad == 0) tied = ties[g / kQuad];
+      uint32_t at = tied + upto - mine;
+#pragma unroll
+      for (int j = 0; j < kVec; ++j)
+        if (x.l[j] == cut.value && at++ >= cut.ties) to[j] = 0;
+      tied += __shfl_sync(kFull, upto, 31);
+    }
+  };
+  if (cut.value == -INFINITY && !least) {
+    r.template run<true>(wanted, [&](int, const Vec<T> &x) {
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) sum += weight_of(x.l[j], r.c);
+    }, leave);
+  } else {
+    if (cut.by_index) {
+      r.template run<false>(wanted, [&](int, const Vec<T> &x) {
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) tied += x.l[j] == cut.value;
+      }, [&](int q) {
+        tied = __reduce_add_sync(kFull, tied);
+        if (lane == 0) ties[q] = tied;
+        tied = 0;
+      });
+      __syncthreads();
+      r.sum_before(ties);
+    }
+    r.template run<false>(wanted, [&](int g, const Vec<T> &x) {
+      uint32_t to[kVec];
+      weigh(g, x, to);
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) sum += to[j];
+    }, leave);
+  }
+  __syncthreads();
+  // the quad in which the running sum passes the aim, and in it the token
+  uint64_t total;
+  const uint64_t before = r.find_quad(a, row, mass, total);
+  if (warp == 0) r.pick_of_quad(a, row, before, total, weigh);
+}
+
 template <typename T>
 cudaError_t launch_sample(SampleArgs a, int rows, cudaStream_t stream) {
   static bool done[64] = {};
@@ -937,10 +1680,18 @@ cudaError_t launch_sample(SampleArgs a, int rows, cudaStream_t stream) {
     ctas *= 2;
   a.slice = ((a.vocab + ctas - 1) / ctas + 7) / 8 * 8;
   if (dev < 0 || dev >= 64 || !done[dev]) {
-    const cudaError_t e = cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSampleSmem);
+    cudaError_t e = cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSampleSmem);
+    if (e == cudaSuccess)
+      e = cudaFuncSetAttribute(sample_alone_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAloneSmem);
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) done[dev] = true;
   }
+  // A CTA a row where the clusters' CTAs would take turns: from one and a half times what the SMs hold at
+  // once.  (fp32 rows of 128256: at 48, 384 CTAs, clusters / alone took 17 / 29 us without cuts, 26 / 20
+  // with k = 50, 45 / 54 with p = 0.9; at 96 they took 31 / 32, 44 / 23 and 79 / 57.  A row that one CTA
+  // holds waits for no other, and is read once: 1000 rows of 32000 in bf16, 40 / 53, 58 / 61, 105 / 115.)
+  if (ctas > 1 && rows * ctas > 3 * device_sms())
+    return launch_after<sample_alone_kernel<T>>(dim3((unsigned)rows), dim3(kSampleThreads), (size_t)kAloneSmem, dim3(1), stream, a);
   return launch_after<sample_kernel<T>>(dim3((unsigned)ctas, (unsigned)rows), dim3(kSampleThreads),
                       (size_t)bytes(ctas), dim3((unsigned)ctas), stream, a);
 }

@@ -192,3 +192,42 @@ def test_no_rows_and_refusals():
     with pytest.raises(ham.HamError, match="vocab") as e:
         ham.ham_sample(torch.zeros(1, 262145, device="cuda"), u[:1], tok[:1])
     assert e.value.status == ham.HAM_EUNSUPPORTED
+
+
+# Many rows of more logits than one CTA's shared memory holds: a CTA a row.  What its bounds may not hold, and
+# lists that come near their 2048 tokens or pass them, beside the settings of the others.
+MANY = SETTINGS + [(0.8, 300, 1.0, 0.0), (0.8, 2047, 1.0, 0.0), (1.5, 2045, 0.6, 0.0), (1.0, 5000, 0.9, 0.0),
+                   (1.0, 0, 0.9999, 0.0), (1.0, 0, 0.99999, 0.05), (1.0, 0, 0.5, 0.2), (30.0, 0, 0.8, 0.0),
+                   (1.0, 0, 1.0, 1e-5), (1e-6, 0, 0.9, 0.0), (1e6, 100, 0.9, 0.0)]
+
+
+@pytest.mark.parametrize("b,v,f32", [(240, 20011, True), (160, 50001, True), (60, 262144, True), (240, 40003, False),
+                                     (120, 130001, False)])
+def test_many_rows(b, v, f32):
+    rng = np.random.default_rng(b + v)
+    for spread in (0.3, 2.5):
+        pick = np.arange(b) % len(MANY)
+        t, k, p, m = (np.array([MANY[i][j] for i in pick]) for j in range(4))
+        check_exact(_logits(rng, b, v, spread, f32), rng.random(b).astype(np.float32), t.astype(np.float32),
+                    np.minimum(k, 2 ** 30).astype(np.int32), p.astype(np.float32), m.astype(np.float32))
+
+
+@pytest.mark.parametrize("f32", [True, False])
+def test_many_rows_of_few_values(f32):
+    """Equal, stepped, sorted, near-equal, ruled-out, infinite and missing logits, a row each."""
+    import torch
+    v = 40003
+    rng = np.random.default_rng(21)
+    at = np.arange(v)
+    kinds = [np.zeros(v), np.where(at % 3 == 0, 1.0, 0.0), (at % 11) * 0.25, np.full(v, -np.inf),
+             np.where(at < v - 1, -np.inf, 2.0), np.full(v, np.nan), np.where(at % 2 == 0, np.nan, at % 7),
+             np.where((at > 100) & (at < 5000), np.inf, 1.0), np.where(at == 7, np.inf, rng.standard_normal(v)),
+             8 - at * 1e-3, at * 1e-3 - 8, rng.standard_normal(v) * 1e6, rng.standard_normal(v) * 1e-6 + 1000,
+             np.float32(5) + rng.integers(0, 5000, v) * np.float32(2.0 ** -21), np.where(at % 500 == 0, 0.0, -1e30)]
+    settings = MANY + [(1.0, v // 2, 1.0, 0.0), (1.0, v // 2 + 1, 0.73, 0.0), (1.0, v - 1, 1.0, 0.0)]
+    rows = [(x, s) for x in kinds for s in settings]
+    assert len(rows) >= 240
+    l = torch.from_numpy(np.stack([x for x, _ in rows]).astype(np.float32)).cuda()
+    t, k, p, m = (np.array([s[j] for _, s in rows]) for j in range(4))
+    check_exact(l if f32 else l.bfloat16(), rng.random(len(rows)).astype(np.float32), t.astype(np.float32),
+                np.minimum(k, 2 ** 30).astype(np.int32), p.astype(np.float32), m.astype(np.float32))
