@@ -558,6 +558,7 @@ int ham_fp8_weight_status(ham_fp8_weight *w, void *stream, int32_t *device_code)
  *   floor(u S), S their whole sum;  prob = w_token / S
  * The weights are whole numbers and their sums exact, so the token does not depend on batch, launch
  * shape or the order of additions.  T <= 0 (or NaN) takes the largest logit, ties to the lowest index.
+ * (A positive T is taken within 2^-60 .. 2^60.)
  * k <= 0 or k >= vocab, p >= 1 and m <= 0 keep all; the likeliest token is always kept.  A NaN logit
  * counts as -inf (ruled out); a row with nothing but those gives token -1 and prob 0.
  * logits       device [rows][vocab], bf16 or f32 (logits_dtype), 16-byte aligned; vocab at most 2^18
