@@ -23,7 +23,7 @@
 //  - otherwise the bin's own tokens are listed there and the first CTA finds the cut among them for all
 //    (where they too are more than 2048: histograms over 512 parts of the bin, then over the values of l
 //    in the part until one is left); then the cluster sums the kept weights by stretches of the index.
-// One row of 128256 fp32 logits takes 11.9 us, of which the reads are less than one: the rest is a chain of
+// One row of 128256 fp32 logits takes 10.9 us (top-k and top-p), of which the reads are less than one: the rest is a chain of
 // some ten barriers and shared-memory steps.
 //
 // Many rows (sample_alone_kernel): a CTA a row, two an SM, so that no row waits for a place in shared memory
@@ -31,7 +31,7 @@
 // of 128256 in fp32, 19 at the rate of a copy), leaves the largest logit of each group of 128 (or 256)
 // tokens; what comes after reads the groups that matter, from the L2 where they are still there:
 //  - top-k: the groups whose largest logit is among the k largest of them, in whose bins the k tokens lie
-//    (k = 50: 33 us in all, where the clusters took 106);
+//    (k = 50: 31 us in all, where the clusters took 106);
 //  - larger k, and top-p alone: the first pass also counts tokens by finer bins, on a scale that does not need
 //    the maximum.  For k they give the tokens to list (60 to 88 us; the shared atomics take 0.8 us a million).
 //    For top-p they bound each bin's weight, which leaves the cut to a few bins, and one more pass sums
@@ -54,7 +54,8 @@ namespace {
 
 constexpr int kSampleThreads = 512, kSampleWarps = kSampleThreads / 32;
 constexpr int kBins = 512;
-constexpr int kList = 2048;             // tokens that one CTA ranks by itself
+constexpr int kList = 2048;             // tokens that one CTA takes by itself
+constexpr int kRanked = 128;            // ... that it compares with one another
 constexpr float kFine = 2147483648.f;   // 2^31
 constexpr float kLastBin = 511.f;
 constexpr float kBinsPerX = 23.78f;     // bins of x = (l - max) / T: 511 reach to -21.4886, and below
@@ -712,11 +713,40 @@ struct Row {
     }
     __syncthreads();
   }
+  // A listed token's place in the order: by l, largest first, equal ones by index; and which one it is.
+  static_assert(kList <= 1 << 11 && kSampleMaxVocab <= 1 << 18, "keys");
   __device__ __forceinline__ uint64_t sort_key(int i) const {
-    return ((uint64_t)~key_of(s.list_l[i]) << 32) | (uint32_t)i;
+    return ((uint64_t)~key_of(s.list_l[i]) << 32) | (uint32_t)(s.list_i[i] << 11 | i);
   }
-  __device__ __forceinline__ float sorted_logit(uint64_t key) const { return logit_of(~(uint32_t)(key >> 32)); }
+  static __device__ __forceinline__ int listed_of(uint64_t key) { return (int)key & 2047; }
   __device__ __forceinline__ uint32_t listed_weight(int i) const { return weight_of(s.list_l[i], c); }
+  // For a few listed tokens: how many come before each in the order and their weights (of list_w), by comparing
+  // it with every other; as many threads a token as there are, of which the first has the token `i` and
+  // the sums (else i = -1).  (Top-k 50 of one row: 10.5 us, 11.5 if they are sorted; top-k 200: the same.)
+  struct Rank {
+    int i;
+    uint32_t count;
+    uint64_t mass;
+  };
+  __device__ Rank rank_of(int n, const uint32_t *list_w) const {
+    if (tid < n) s.sorted[tid] = sort_key(tid);
+    __syncthreads();
+    int lanes = 1;
+    while (lanes < 32 && 2 * lanes * n <= kSampleThreads) lanes *= 2;
+    const int i = tid / lanes, part = tid & (lanes - 1);
+    Rank r{part || i >= n ? -1 : i, 0, 0};
+    if (i < n) {
+      const uint64_t key = s.sorted[i];
+      for (int j = part; j < n; j += lanes) {
+        if (s.sorted[j] < key) ++r.count, r.mass += list_w[j];
+      }
+    }
+    for (int o = lanes / 2; o > 0; o >>= 1) {
+      r.count += __shfl_xor_sync(kFull, r.count, o);
+      r.mass += __shfl_xor_sync(kFull, r.mass, o);
+    }
+    return r;
+  }
   // Sorts the first `many` keys of s.sorted (by l, largest first, equal ones by place in the list): a
   // bitonic network, distances below a warp in registers, the others in shared memory.
   __device__ void sort(int many) const {
@@ -795,7 +825,7 @@ struct Row {
     uint64_t at = mass0;
     for (int i0 = 0; i0 < many; i0 += kSampleThreads) {
       const int i = i0 + tid;
-      const uint64_t key = i < many ? s.sorted[i] : ~0ull, w = i < many ? weight((int)(uint32_t)key) : 0;
+      const uint64_t key = i < many ? s.sorted[i] : ~0ull, w = i < many ? weight(listed_of(key)) : 0;
       uint64_t part;
       const uint64_t upto = at + block_scan(s, w, part);
       // the last token kept, and how many of its equals are kept with it
@@ -845,8 +875,8 @@ struct Row {
   }
   // The choice among the first CTA's list of `all` tokens up to bin `last`, by that CTA alone.  k > 0:
   // top-k, which cuts in bin `last` (-1: not known), before which lie `before` tokens.  p >= 0: top-p, of the weight
-  // `row_mass` (0: of the list's, after top-k).  Up to a token a thread are sorted; of more, only the
-  // cuts' parts are.
+  // `row_mass` (0: of the list's, after top-k).  Up to a token a thread are ranked or sorted; of more,
+  // only the cuts' parts are.
   __device__ void choose(const SampleArgs &a, int row, int all, int last, uint32_t before, int k, double p,
                          uint64_t row_mass, uint32_t least) const {
     constexpr int kPer = kList / kSampleThreads;
@@ -854,18 +884,28 @@ struct Row {
     uint64_t whole = row_mass;
     if (k > all) k = 0;
     if (all <= kSampleThreads) {
-      if (tid < all) s.sorted[tid] = sort_key(tid);
-      sort(all);
-      const uint64_t key = tid < all ? s.sorted[tid] : ~0ull;
-      const uint32_t w = tid < all && (k <= 0 || tid < k) ? weight_of(sorted_logit(key), c) : 0;
+      if (tid < all) list_w[tid] = listed_weight(tid);
+      Rank r;
+      if (all <= kRanked) {
+        r = rank_of(all, list_w);
+      } else {
+        if (tid < all) s.sorted[tid] = sort_key(tid);
+        sort(all);
+        r.i = tid < all ? listed_of(s.sorted[tid]) : -1;
+        r.count = (uint32_t)tid;
+        const uint32_t w = r.i >= 0 ? list_w[r.i] : 0;
+        uint64_t sum;
+        r.mass = block_scan(s, w, sum) - w;
+      }
+      const uint32_t w = r.i >= 0 && (k <= 0 || (int)r.count < k) ? list_w[r.i] : 0;
       uint64_t sum, aim = ~0ull;
-      const uint64_t run = block_scan(s, w, sum) - w;
+      block_scan(s, w, sum);
       if (p >= 0.) {
         if (tid == 0) s.aim = aim_of(p, row_mass ? row_mass : sum);
         __syncthreads();
         aim = s.aim;
       }
-      if (tid < all) list_w[(uint32_t)key] = run < aim ? w : 0u;
+      if (r.i >= 0) list_w[r.i] = r.mass < aim ? w : 0u;
     } else {
       for (int i = tid; i < all; i += kSampleThreads) list_w[i] = listed_weight(i);
       __syncthreads();
@@ -873,7 +913,7 @@ struct Row {
       const auto drop = [&](const Cut &x) {      // what the cut leaves out
         for (int i = tid; i < all; i += kSampleThreads)
           if (s.list_l[i] < x.value) list_w[i] = 0;
-        for (int i = s.cut_at + 1 + tid; i < s.members; i += kSampleThreads) list_w[(uint32_t)s.sorted[i]] = 0;
+        for (int i = s.cut_at + 1 + tid; i < s.members; i += kSampleThreads) list_w[listed_of(s.sorted[i])] = 0;
         __syncthreads();
       };
       if (k > 0) drop(cut_list(all, last < 0, max(last, 0), false, (uint64_t)k, before, 0, weight));
@@ -1172,7 +1212,7 @@ struct Row {
     const Cut cut = cut_list((int)all, true, 0, true, aim, 0, upper_mass, [&](int i) { return list_w[i]; });
     for (int i = tid; i < (int)all; i += kSampleThreads)
       if (s.list_l[i] < cut.value || list_w[i] < least) list_w[i] = 0;
-    for (int i = s.cut_at + 1 + tid; i < s.members; i += kSampleThreads) list_w[(uint32_t)s.sorted[i]] = 0;
+    for (int i = s.cut_at + 1 + tid; i < s.members; i += kSampleThreads) list_w[listed_of(s.sorted[i])] = 0;
     __syncthreads();
     constexpr int kTokens = kQuad * 32 * kN;
     for (int i = tid; i < (int)all; i += kSampleThreads)
