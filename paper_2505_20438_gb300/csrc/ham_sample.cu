@@ -103,10 +103,10 @@ struct SampleShared {
   int first;                              // first index of the largest logit
   uint64_t found_before_mass, found_mass, aim;
   uint32_t found_before_count, found_count;
-  int found, members, cut_at;
+  int found, members;
   float cut_value;
-  uint32_t cut_ties, cut_by_index;
-  uint64_t cut_mass;
+  uint32_t cut_ties, cut_same;
+  uint64_t cut_key, cut_mass;
 };
 static_assert(kFineBins * kFineCopies * 4 <= sizeof(Histogram) * kCopies, "finer histogram");
 static_assert(kQuads * 8 + kSampleWarps * kPart * 4 <= sizeof(Histogram) * kCopies, "lists");
@@ -720,26 +720,27 @@ struct Row {
   }
   static __device__ __forceinline__ int listed_of(uint64_t key) { return (int)key & 2047; }
   __device__ __forceinline__ uint32_t listed_weight(int i) const { return weight_of(s.list_l[i], c); }
-  // For a few listed tokens: how many come before each in the order and their weights (of list_w), by comparing
-  // it with every other; as many threads a token as there are, of which the first has the token `i` and
-  // the sums (else i = -1).  (Top-k 50 of one row: 10.5 us, 11.5 if they are sorted; top-k 200: the same.)
+  // For a few keys of s.sorted: how many come before each in the order and their weights (s.own, of the list),
+  // by comparing it with every other; as many threads a key as there are, of which the first has the key's
+  // token `i` and the sums (else i = -1).  (Top-k 50 of one row: 10.5 us, 11.5 if they are sorted; top-k
+  // 200: the same.)
   struct Rank {
     int i;
     uint32_t count;
-    uint64_t mass;
+    uint64_t mass, key;
   };
-  __device__ Rank rank_of(int n, const uint32_t *list_w) const {
-    if (tid < n) s.sorted[tid] = sort_key(tid);
-    __syncthreads();
+  __device__ Rank rank_of(int n) const {
     int lanes = 1;
     while (lanes < 32 && 2 * lanes * n <= kSampleThreads) lanes *= 2;
     const int i = tid / lanes, part = tid & (lanes - 1);
-    Rank r{part || i >= n ? -1 : i, 0, 0};
+    Rank r{-1, 0, 0, 0};
     if (i < n) {
-      const uint64_t key = s.sorted[i];
+      r.key = s.sorted[i];
       for (int j = part; j < n; j += lanes) {
-        if (s.sorted[j] < key) ++r.count, r.mass += list_w[j];
+        const uint64_t other = s.sorted[j];
+        if (other < r.key) ++r.count, r.mass += s.own[listed_of(other)];
       }
+      if (part == 0) r.i = listed_of(r.key);
     }
     for (int o = lanes / 2; o > 0; o >>= 1) {
       r.count += __shfl_xor_sync(kFull, r.count, o);
@@ -779,11 +780,9 @@ struct Row {
   }
   // The exact cut among the `n` listed tokens, by this CTA alone: a histogram over 512 bins (`bins`; else
   // the cut is known to lie in bin `bin`), one over the 512 parts of the cut's bin, then the part's tokens
-  // sorted.  count0, mass0: those of the tokens before bin `bin`; weight(i): of listed token i.  s.sorted
-  // holds the part's tokens in order, s.cut_at the last one kept, s.members their number.
-  template <typename W>
-  __device__ Cut cut_list(int n, bool bins, int bin, bool by_mass, uint64_t aim, uint32_t count0, uint64_t mass0,
-                          W weight) const {
+  // ranked or sorted.  count0, mass0: those of the tokens before bin `bin`; s.own: the list's weights.
+  // s.cut_key: the last token kept.
+  __device__ Cut cut_list(int n, bool bins, int bin, bool by_mass, uint64_t aim, uint32_t count0, uint64_t mass0) const {
     float base = (float)bin, mult = bins ? 1.f : (float)kBins;
     for (;;) {
       clear(&s.h, 1);
@@ -791,7 +790,7 @@ struct Row {
         const float at = (place_of(s.list_l[i], c) - base) * mult;  // (exact)
         if (at >= 0.f && at < (float)kBins) {
           atomicAdd(&s.h.count[(int)at], 1u);
-          add_mass(s.h, (int)at, weight(i));
+          add_mass(s.h, (int)at, s.own[i]);
         }
       }
       __syncthreads();
@@ -821,37 +820,42 @@ struct Row {
     }
     __syncthreads();
     const int many = s.members;
-    sort(many);
-    uint64_t at = mass0;
-    for (int i0 = 0; i0 < many; i0 += kSampleThreads) {
-      const int i = i0 + tid;
-      const uint64_t key = i < many ? s.sorted[i] : ~0ull, w = i < many ? weight(listed_of(key)) : 0;
-      uint64_t part;
-      const uint64_t upto = at + block_scan(s, w, part);
-      // the last token kept, and how many of its equals are kept with it
-      if (i < many && (by_mass ? upto >= aim && upto - w < aim : (uint64_t)count0 + i + 1 == aim)) {
-        const uint32_t l = (uint32_t)(key >> 32);
-        int from = 0, to = i;                    // the first of the equal ones
-        while (from < to) {
-          const int mid = (from + to) / 2;
-          if ((uint32_t)(s.sorted[mid] >> 32) < l) from = mid + 1;
-          else to = mid;
-        }
-        s.cut_at = i;
-        s.cut_value = logit_of(~l);
-        s.cut_ties = i - from + 1;
-        s.cut_by_index = i + 1 < many && (uint32_t)(s.sorted[i + 1] >> 32) == l;
-        s.cut_mass = upto;
+    const auto cut_at = [&](uint64_t key, uint32_t w, uint64_t before, uint64_t mass) {
+      if (before < aim && before + (by_mass ? w : 1u) >= aim) s.cut_key = key, s.cut_mass = mass + w;
+    };
+    if (many <= kRanked) {
+      const Rank r = rank_of(many);
+      if (r.i >= 0) cut_at(r.key, s.own[r.i], by_mass ? mass0 + r.mass : (uint64_t)count0 + r.count, mass0 + r.mass);
+    } else {
+      sort(many);
+      uint64_t at = mass0;
+      for (int i0 = 0; i0 < many; i0 += kSampleThreads) {
+        const int i = i0 + tid;
+        const uint64_t key = i < many ? s.sorted[i] : ~0ull;
+        const uint32_t w = i < many ? s.own[listed_of(key)] : 0u;
+        uint64_t part;
+        const uint64_t before = at + block_scan(s, w, part) - w;
+        if (i < many) cut_at(key, w, by_mass ? before : (uint64_t)count0 + i, before);
+        at += part;
       }
-      at += part;
     }
+    if (tid == 0) s.cut_ties = s.cut_same = 0;
     __syncthreads();
-    Cut k;
-    k.value = s.cut_value;
-    k.ties = s.cut_ties;
-    k.by_index = s.cut_by_index;
-    k.mass = s.cut_mass;
-    return k;
+    const uint64_t key = s.cut_key;              // its equals, and how many of them are kept
+    for (int i = tid; i < many; i += kSampleThreads)
+      if ((s.sorted[i] ^ key) >> 32 == 0) {
+        atomicAdd(&s.cut_same, 1u);
+        if (s.sorted[i] <= key) atomicAdd(&s.cut_ties, 1u);
+      }
+    if (tid == 0) s.cut_value = logit_of(~(uint32_t)(key >> 32));
+    __syncthreads();
+    return Cut{s.cut_value, s.cut_ties < s.cut_same, s.cut_ties, s.cut_mass};
+  }
+  // Leaves the listed tokens after the cut's without a weight.
+  __device__ void drop(int n) const {
+    for (int i = tid; i < n; i += kSampleThreads)
+      if (sort_key(i) > s.cut_key) s.own[i] = 0;
+    __syncthreads();
   }
   // The exact cut within the bin that find() gave for the aim, made by the first CTA for the cluster.
   __device__ Cut cut(bool by_mass, uint64_t aim) const {
@@ -863,13 +867,14 @@ struct Row {
     const int many = (int)list(bin, bin);
     if (rank == 0) {
       pull(many);
-      cut_list(many, false, bin, by_mass, aim, count, mass, [&](int i) { return listed_weight(i); });
+      for (int i = tid; i < many; i += kSampleThreads) s.own[i] = listed_weight(i);  // (its places are pulled)
+      cut_list(many, false, bin, by_mass, aim, count, mass);
     }
     sync();
     Cut k;
     k.value = __uint_as_float(ld_cluster_u32(peer(&s.cut_value, 0)));
     k.ties = ld_cluster_u32(peer(&s.cut_ties, 0));
-    k.by_index = ld_cluster_u32(peer(&s.cut_by_index, 0));
+    k.by_index = k.ties < ld_cluster_u32(peer(&s.cut_same, 0));
     k.mass = ld_cluster_u64(peer(&s.cut_mass, 0));
     return k;
   }
@@ -885,11 +890,12 @@ struct Row {
     if (k > all) k = 0;
     if (all <= kSampleThreads) {
       if (tid < all) list_w[tid] = listed_weight(tid);
+      if (tid < all) s.sorted[tid] = sort_key(tid);
+      __syncthreads();
       Rank r;
       if (all <= kRanked) {
-        r = rank_of(all, list_w);
+        r = rank_of(all);
       } else {
-        if (tid < all) s.sorted[tid] = sort_key(tid);
         sort(all);
         r.i = tid < all ? listed_of(s.sorted[tid]) : -1;
         r.count = (uint32_t)tid;
@@ -909,14 +915,10 @@ struct Row {
     } else {
       for (int i = tid; i < all; i += kSampleThreads) list_w[i] = listed_weight(i);
       __syncthreads();
-      const auto weight = [&](int i) { return list_w[i]; };
-      const auto drop = [&](const Cut &x) {      // what the cut leaves out
-        for (int i = tid; i < all; i += kSampleThreads)
-          if (s.list_l[i] < x.value) list_w[i] = 0;
-        for (int i = s.cut_at + 1 + tid; i < s.members; i += kSampleThreads) list_w[listed_of(s.sorted[i])] = 0;
-        __syncthreads();
-      };
-      if (k > 0) drop(cut_list(all, last < 0, max(last, 0), false, (uint64_t)k, before, 0, weight));
+      if (k > 0) {
+        cut_list(all, last < 0, max(last, 0), false, (uint64_t)k, before, 0);
+        drop(all);
+      }
       if (p >= 0.) {
         if (!row_mass) {
           uint64_t mine = 0;
@@ -925,7 +927,8 @@ struct Row {
         }
         if (tid == 0) s.aim = aim_of(p, whole);
         __syncthreads();
-        drop(cut_list(all, true, 0, true, s.aim, 0, 0, weight));
+        cut_list(all, true, 0, true, s.aim, 0, 0);
+        drop(all);
       }
     }
     __syncthreads();
@@ -1209,14 +1212,12 @@ struct Row {
     const uint64_t aim = aim_of(p, row_mass);
     if (upper_mass >= aim || upper_mass + list_mass < aim) return false;
     __syncthreads();
-    const Cut cut = cut_list((int)all, true, 0, true, aim, 0, upper_mass, [&](int i) { return list_w[i]; });
-    for (int i = tid; i < (int)all; i += kSampleThreads)
-      if (s.list_l[i] < cut.value || list_w[i] < least) list_w[i] = 0;
-    for (int i = s.cut_at + 1 + tid; i < s.members; i += kSampleThreads) list_w[listed_of(s.sorted[i])] = 0;
-    __syncthreads();
+    cut_list((int)all, true, 0, true, aim, 0, upper_mass);
+    drop((int)all);
     constexpr int kTokens = kQuad * 32 * kN;
     for (int i = tid; i < (int)all; i += kSampleThreads)
-      if (list_w[i]) atomicAdd(reinterpret_cast<unsigned long long *>(mass + s.list_i[i] / kTokens), (unsigned long long)list_w[i]);
+      if (list_w[i] >= max(least, 1u))
+        atomicAdd(reinterpret_cast<unsigned long long *>(mass + s.list_i[i] / kTokens), (unsigned long long)list_w[i]);
     __syncthreads();
     // ---- the quad, and in it the token
     uint64_t total;
@@ -1225,7 +1226,7 @@ struct Row {
     for (int i = tid; i < kTokens; i += kSampleThreads) of_quad[i] = 0;
     __syncthreads();
     for (int i = tid; i < (int)all; i += kSampleThreads)
-      if (s.list_i[i] / kTokens == s.first) of_quad[s.list_i[i] % kTokens] = list_w[i];
+      if (s.list_i[i] / kTokens == s.first && list_w[i] >= least) of_quad[s.list_i[i] % kTokens] = list_w[i];
     __syncthreads();
     if (warp == 0)
       pick_of_quad(a, row, ahead, total, [&](int g, const Vec<T> &x, uint32_t (&to)[kN]) {
