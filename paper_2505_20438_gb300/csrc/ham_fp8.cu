@@ -385,53 +385,68 @@ constexpr int kPairUsed = 1024 + kPairStages * kPairStageBytes + kPairSf * kPair
 constexpr int kPairSmem = kPairUsed > smem_floor(512) ? kPairUsed : smem_floor(512);
 static_assert(kPairSmem <= 226 * 1024, "shared memory");
 
-// 32 accumulator columns (from column c of n) of a warp's 32 rows (those from own0 on), a row a lane, to the output: `bytes` at a
-// time a lane where rows begin at multiples of 32 or 16 bytes, and else turned in shared memory so that
-// 16 lanes write neighbours (a value at a time, 32 rows an instruction: 164 us for 3000 x 5003 outputs
-// of 2000 columns, against 27 us for 5008).
+// 32 accumulator columns (from column c of n) of a warp's 32 rows (those from own0 on), a row a lane, to the
+// output through shared memory, 16 columns at a time, so that neighbouring lanes write neighbours, kEach
+// elements each: what n is a multiple of, up to 16 bytes.  (3344 rows, K 544, some 15550 features, which the
+// outputs bound: bf16 35 us straight, turned 48 with 8 elements, 55 with 4, 62 with 2, 88 with 1; fp32 53, and
+// 68, 84, 94 with 4, 2, 1.  16 bytes a lane straight from the registers took 57 and 117; a value at
+// a time, a row a lane, 164 for 3000 x 5003 outputs of 2000 columns that take 38 turned.)
+template <int kEach>
+__device__ __forceinline__ void store_turned(const ProductArgs &a, int row0, int own0, int c, const float *f, float *turn) {
+  constexpr int kLanes = 16 / kEach;             // a row's
+  const int lane = threadIdx.x & 31, at = lane % kLanes * kEach;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 16; ++j) turn[lane * kTurn + j] = f[16 * h + j];
+    __syncwarp();
+    const int col = c + 16 * h + at;
+#pragma unroll 4
+    for (int i = 0; i < 16 / kEach; ++i) {
+      const int r = i * 2 * kEach + lane / kLanes;
+      if (row0 + r < own0 || col >= a.n) continue;
+      const float *x = turn + r * kTurn + at;
+      const int64_t to = (int64_t)(row0 + r) * a.n + col;
+      if (a.f32) {
+        float *y = static_cast<float *>(a.out) + to;
+        if constexpr (kEach == 1) *y = x[0];
+        if constexpr (kEach == 2) *reinterpret_cast<float2 *>(y) = make_float2(x[0], x[1]);
+        if constexpr (kEach == 4) *reinterpret_cast<float4 *>(y) = make_float4(x[0], x[1], x[2], x[3]);
+      } else {
+        __nv_bfloat16 *y = static_cast<__nv_bfloat16 *>(a.out) + to;
+        if constexpr (kEach == 1) *y = __float2bfloat16_rn(x[0]);
+        if constexpr (kEach == 2) *reinterpret_cast<uint32_t *>(y) = pack_bf16x2(x[0], x[1]);
+        if constexpr (kEach == 4)
+          *reinterpret_cast<uint2 *>(y) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+        if constexpr (kEach == 8)
+          *reinterpret_cast<uint4 *>(y) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
+                                                     pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+      }
+    }
+  }
+}
+// The same straight from the registers, 32 bytes at a time a lane, where rows begin at multiples of them
+// (`straight`); else turned.
 __device__ __forceinline__ void store32(const ProductArgs &a, int row0, int own0, int c, const uint32_t (&v)[32],
-                                        int bytes, float *turn) {
+                                        bool straight, float *turn) {
   const float *f = reinterpret_cast<const float *>(v);
   const int lane = threadIdx.x & 31, row = row0 + lane;
   if (c >= a.n) return;
-  if (bytes == 0) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      __syncwarp();
-#pragma unroll
-      for (int j = 0; j < 16; ++j) turn[lane * kTurn + j] = f[16 * h + j];
-      __syncwarp();
-      const int col = c + 16 * h + (lane & 15);
-#pragma unroll 4
-      for (int i = 0; i < 16; ++i) {
-        const int r = 2 * i + (lane >> 4);
-        if (row0 + r >= own0 && col < a.n) {
-          const float x = turn[r * kTurn + (lane & 15)];
-          const int64_t at = (int64_t)(row0 + r) * a.n + col;
-          if (a.f32) static_cast<float *>(a.out)[at] = x;
-          else static_cast<__nv_bfloat16 *>(a.out)[at] = __float2bfloat16_rn(x);
-        }
-      }
-    }
+  if (!straight) {
+    if ((a.n & 7) == 0 && !a.f32) store_turned<8>(a, row0, own0, c, f, turn);
+    else if ((a.n & 3) == 0) store_turned<4>(a, row0, own0, c, f, turn);
+    else if ((a.n & 1) == 0) store_turned<2>(a, row0, own0, c, f, turn);
+    else store_turned<1>(a, row0, own0, c, f, turn);
     return;
   }
   if (row < own0) return;
   char *dst = static_cast<char *>(a.out) + ((int64_t)row * a.n + c) * (a.f32 ? 4 : 2);
-  // 32 bytes (from column `at` of the 32), or their two halves where the row ends between them
-  auto put = [&](int at, int each, const uint32_t (&w)[8]) {
-    char *to = dst + at * (32 / (2 * each));
-    if (bytes == 32) {
-      if (c + at < a.n) st_global_32(to, w);
-    } else {
-      if (c + at < a.n) *reinterpret_cast<uint4 *>(to) = make_uint4(w[0], w[1], w[2], w[3]);
-      if (c + at + each < a.n) *reinterpret_cast<uint4 *>(to + 16) = make_uint4(w[4], w[5], w[6], w[7]);
-    }
-  };
   if (a.f32) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const uint32_t w[8] = {v[8 * q], v[8 * q + 1], v[8 * q + 2], v[8 * q + 3], v[8 * q + 4], v[8 * q + 5], v[8 * q + 6], v[8 * q + 7]};
-      put(8 * q, 4, w);
+      if (c + 8 * q < a.n) st_global_32(dst + 32 * q, w);
     }
   } else {
 #pragma unroll
@@ -439,7 +454,7 @@ __device__ __forceinline__ void store32(const ProductArgs &a, int row0, int own0
       uint32_t w[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) w[j] = pack_bf16x2(f[16 * q + 2 * j], f[16 * q + 2 * j + 1]);
-      put(16 * q, 8, w);
+      if (c + 16 * q < a.n) st_global_32(dst + 32 * q, w);
     }
   }
 }
@@ -648,9 +663,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     // accumulator and the first 64 of the second: the warps that have them load them before all else.
     const int quarter = warp & 3, half = (warp - 4) >> 2, lane_row = quarter * 32 + lane;
     const uint32_t free_bar = cluster_map_shared(smem_u32(acc_shared_free), first);
-    // bytes a lane may write at once: a row begins at a multiple of them
-    const int row_bytes = a.n * (kGated ? 1 : a.f32 ? 4 : 2);
-    const int bytes = (row_bytes & 31) == 0 && ((uintptr_t)a.out & 31u) == 0 ? 32 : (row_bytes & 15) == 0 ? 16 : 0;
+    // rows begin at multiples of 32 bytes
+    const bool straight = (a.n * (kGated ? 1 : a.f32 ? 4 : 2) & 31) == 0 && ((uintptr_t)a.out & 31u) == 0;
     int n = 0;
     for (int w = cluster; w < total; w += clusters, ++n) {
       const int rt = w % row_groups * kPairs + pair, ct = w / row_groups, buf = n & 1;
@@ -684,8 +698,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           tmem_wait_ld();
           if (i == 0 && shared) release();
           const int c = ct * 256 + col;
-          store32(a, row0, own0, c, v, bytes, turn + (warp - 4) * 32 * kTurn);
-          store32(a, row0, own0, c + 32, u, bytes, turn + (warp - 4) * 32 * kTurn);
+          store32(a, row0, own0, c, v, straight, turn + (warp - 4) * 32 * kTurn);
+          store32(a, row0, own0, c + 32, u, straight, turn + (warp - 4) * 32 * kTurn);
         }
       } else {
         // gate columns half * 64 .., up columns 128 + half * 64 ..; shared: the up's of half 1 in the
@@ -722,7 +736,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
 #pragma unroll
           for (int q = 0; q < 16; ++q) code[q] = fp8_codes4(h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3], p);
           uint8_t *dst = static_cast<uint8_t *>(a.out) + (int64_t)row * a.n + c;
-          if (bytes == 32 && c + 64 <= a.n) {
+          if (straight && c + 64 <= a.n) {
             st_global_32(dst, *reinterpret_cast<uint32_t(*)[8]>(code));
             st_global_32(dst + 32, *reinterpret_cast<uint32_t(*)[8]>(code + 8));
           } else {

@@ -75,6 +75,26 @@ def test_gated_pairs_match_oracle(t, k, f):
     _gated(t, k, f)
 
 
+@pytest.mark.parametrize("n", [2496, 2504, 2500, 2502, 2503])
+@pytest.mark.parametrize("f32", [False, True])
+def test_linear_pairs_write_at_every_alignment(n, f32):
+    """Rows that begin at multiples of 32 down to 2 bytes, an output that begins at one of 16 alone, and what lies
+    around it left as it is."""
+    import torch
+    t, k = 300, 272
+    rng = np.random.default_rng(n)
+    x, w = random_codes(rng, t, k), random_codes(rng, n, k, weight=True)
+    x64, w64 = ops.decode_rows(*x), ops.decode_weight(*w)
+    handle = alloc_weight(n, k, w)
+    dtype = torch.float32 if f32 else torch.bfloat16
+    for first in (0, 4 if f32 else 8):
+        room = torch.full((first + t * n + 64,), 7.0, dtype=dtype, device="cuda")
+        y = room[first:first + t * n].view(t, n)
+        ham.ham_fp8_linear(handle, dev(x[0]), dev(x[1]), y)
+        check_bf16(y, x64 @ w64.T, product_slack(x64, w64))
+        assert (room[:first] == 7).all() and (room[first + t * n:] == 7).all()
+
+
 def test_scales_over_their_range():
     """Each operand's scales from 2^-124 to 2^119 (their products within fp32)."""
     import torch
