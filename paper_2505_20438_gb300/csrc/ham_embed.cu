@@ -21,15 +21,19 @@
 //     one token its embedding bit for bit; a token count outside 1..max_patch (or rows outside
 //     the call's tokens) gives zeros and sets the error word.
 // Every launch is a programmatic dependent launch of the one before (the next call's
-// projection included): it is scheduled while its predecessor runs, reads only inputs and
-// weights until its dependency wait, writes nothing before it, and does not end without it (in at
-// least one thread), so that a wait always covers everything before it on the stream; the four are a
-// chain of short latency-bound steps, so the overlap is most of the gain.
+// projection included): it is scheduled while its predecessor runs, reads only weights, the
+// handle's tables and the offsets until its dependency wait, writes nothing before it, and does not end
+// without it (in at least one thread), so that a wait always covers everything before it on the stream;
+// the four are a chain of short latency-bound steps, so the overlap is most of the gain.
 // The weights (4 H^2 bf16) dominate the bytes of a call: memory-bound at decoding batches,
 // where the token rows are far fewer than the weight rows.
 // With token ids (ham_embed_tokens) step 1 is a lookup: the projections of every vocabulary
 // entry, [W_q; W_k; W_v] E[v], are tabulated once in fp32, and the fusion kernel reads the rows
 // of the ids.  A call then reads W_o (H^2 bf16) and 12 H bytes per token instead of 4 H^2.
+// The ids may be what the kernel before is still to write (ham_sample lets its successor start before it
+// has chosen a token), so the fusion kernel, then the call's first, waits before it reads ids or offsets,
+// and lets the projection start only after that wait: when the finish kernel runs, everything before the
+// call has ended, and it may read both before its own wait.
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -89,13 +93,17 @@ __global__ void __launch_bounds__(256) fuse_kernel(const float *__restrict__ qkv
                                                    const int32_t *__restrict__ ids, int vocab,
                                                    int batch, int total, int H, int n_heads,
                                                    int max_patch, float scale) {
+  // With ids everything is read after the wait, and the output projection is let start after it too (batch
+  // 64, H 2048: 13.6 us a call; with the projection let start before the wait, and the finish kernel's
+  // reads after its own, 13.7; 21.0 and 21.7 after a sampling).
+  if (ids) grid_dependency_wait();
   // the output projection may be scheduled now: it reads only its weights until its dependency
   // wait, which waits for this whole grid
   grid_launch_dependents();
-  // Everything before the dependency wait reads only the call's inputs and the handle's tables, and
-  // nothing is written before it.  A warp without a patch ends at once (its block's place goes to one
-  // that has; with every warp waiting the call took 24.3 us, not 23.5), but warp 0 waits in any case, so
-  // that the grid's end means the end of everything before it on the stream.
+  // Without ids, what is read before the dependency wait is the offsets (no kernel of the library writes
+  // them) and the handle's tables, and nothing is written before it.  A warp without a patch ends at once
+  // (its block's place goes to one that has; with every warp waiting the call took 24.3 us, not 23.5), but
+  // warp 0 waits in any case, so that the grid's end means the end of everything before it on the stream.
   const int warp = (int)((blockIdx.x * (int64_t)blockDim.x + threadIdx.x) >> 5);
   const int lane = threadIdx.x & 31;
   if (warp >= batch * n_heads) return;
@@ -140,8 +148,7 @@ __global__ void __launch_bounds__(256) fuse_kernel(const float *__restrict__ qkv
       vv[i][e] = in ? pp[H + 32 * e] : 0.f;
     }
   }
-  // the projection's parts after the wait; tabulated rows before it, and the wait before o is written
-  if (!tabulated) grid_dependency_wait();
+  if (!tabulated) grid_dependency_wait();  // the projection's parts
   for (int sp = 0; sp < nparts; ++sp) {
     const float *base = qkv + sp * part + col;
 #pragma unroll
@@ -189,7 +196,6 @@ __global__ void __launch_bounds__(256) fuse_kernel(const float *__restrict__ qkv
     den += s[i];
   }
   const float inv = 1.f / den;
-  if (tabulated) grid_dependency_wait();
 #pragma unroll
   for (int e = 0; e < kPer; ++e) {
     float acc = 0.f;
@@ -214,7 +220,8 @@ __global__ void finish_kernel(const float *__restrict__ part, int nparts,
                               int H, int max_patch) {
   // the next call's projection may be scheduled now (it waits for this grid before its first
   // read of anything a call writes); launched dependent on the output projection, this kernel
-  // reads the offsets and ids first; every thread waits before it reads anything else, writes or ends
+  // reads the offsets and ids first (with ids, the fusion kernel has waited for whatever wrote them
+  // before it let the projection start); every thread waits before it reads anything else, writes or ends
   grid_launch_dependents();
   const int b = blockIdx.y;
   const int j = 8 * (blockIdx.x * blockDim.x + threadIdx.x);

@@ -125,14 +125,17 @@ int fp8_unsupported(const ham_kv *kv, const char *call) {
 //    arrival count), which starts after its own pass has waited: only that pass may still run, and it
 //    touches none of these.
 //  - Several kernels let their successor start before their own wait (the combine; the embedder's
-//    projections, fusion and finish), so a kernel may start while several before it still run.  But
+//    projections and finish, and its fusion where it has no token ids), so a kernel may start while several before it still run.  But
 //    the first kernel of every call noted below lets its successor start only after its own wait, or
 //    was launched in full stream order (the prefill's plan, the fills, set_lengths).  What comes after
 //    it on the stream starts only when everything before that call has completed: of the noted calls
 //    only the last one may still run.
 // That call writes only its layer's state, its outputs and its handle's scratch, which a following
 // kernel touches after its wait; calls that are not noted (the embedder, ham_decode_attn_noalloc,
-// the norm, products and sampling after the attention) write no handle's state.  The library remembers, per stream (and per stream capture), the last noted
+// the norm, products and sampling after the attention) write no handle's state.  What a caller's buffers
+// hold is read after the wait as well, for any of them may be the output of the call before (the token
+// ids that ham_sample writes and ham_embed_tokens takes among them), but for what no call writes: the
+// embedder's offsets, and weights.  The library remembers, per stream (and per stream capture), the last noted
 // call and which (handle, layer) state it writes, and allows the early start only when that call is
 // known and leaves this layer alone.  Kernels of other code in between are harmless: they cannot write
 // a handle's state (only these calls do), and an unknown predecessor means no early start.
