@@ -39,7 +39,7 @@ struct ham_fp8_weight {
   uint8_t *scales = nullptr;   // [tiles][parts][sk]
   int32_t *err = nullptr;      // device error word
   int32_t *host_err = nullptr; // pinned
-  CUtensorMap map;             // codes as one stretch, boxes of half a block
+  CUtensorMap map;             // codes as one stretch, boxes of a block
 };
 
 namespace ham {
@@ -361,19 +361,19 @@ __global__ void __launch_bounds__(kStreamThreads)
 // ------------------------------------------------------------------------------------
 // A pair of CTAs (cta_group::2) computes 256 rows of X by two weight tiles (a gated weight: the gate's
 // and the up's tile of the same features): each CTA holds 128 of the rows (its lanes of tensor memory)
-// and loads its rows and one of the two weight tiles.  A pair takes 64 bytes a clock an SM from L2 at
-// the products' full rate (512 clocks a K block), which one pair alone gets and 76 pairs do not: so
-// clusters of two pairs (kPairs = 2) take the same weight tiles for neighbouring row tiles, each pair
-// loading half of them into both (multicast), 48 bytes a clock.  The clusters are persistent.  The two
-// accumulators (256 columns each) share 64 columns, which leaves the columns 448.. for the scales: a
-// tile's epilogue takes the shared columns into registers first, and the next tile's products begin when
-// it has.
+// and loads its rows and one of the two weight tiles, both into its own shared memory alone (the library
+// is also what every rank of a job on several GPUs loads, so no load here is a cluster multicast).  The
+// pairs are persistent.  The two accumulators (256 columns each) share 64 columns, which leaves the columns
+// 448.. for the scales: a tile's epilogue takes the shared columns into registers first, and the next
+// tile's products begin when it has.
 //
 // Bound by the tensor cores: 8192 rows, K 4096, 6144 features 119 us (3.46 PFLOP/s, 90% of twice the measured
-// bf16 rate), 4096 rows, K 16384, 4096 features 162 us (89%), gated 4096 rows of 4096 in 16384 features
-// 313 us (91%); run without a break the card's power limit makes that 191 and 355 us.  Few tiles leave pairs
-// without work in the last round, and the first tile's loads and the last one's epilogue stand alone
-// (2048 rows, 4096 x 4096: 25 us, 71%).
+// bf16 rate), 4096 rows, K 16384, 4096 features 169 us (85%), gated 4096 rows of 4096 in 16384 features
+// 300 us (95%); run without a break the card's power limit makes that 139, 193 and 357 us.  Few tiles leave
+// pairs without work in the last round, and the first tile's loads and the last one's epilogue stand alone
+// (2048 rows, 4096 x 4096: 26.5 us, 67%).  A pair takes 64 bytes a clock an SM from L2 at the products' full
+// rate; with two pairs a cluster, each loading half of their weight tiles into both, 48, and these cases
+// took 119, 164 and 300 us, 139, 192 and 356.
 constexpr int kPairThreads = 384;       // warps: copies, products, 2 x scales, 8 x epilogue
 constexpr int kPairStages = 6;
 constexpr int kPairStageBytes = 2 * kBlockBytes;
@@ -459,7 +459,7 @@ __device__ __forceinline__ void store32(const ProductArgs &a, int row0, int own0
   }
 }
 
-template <bool kGated, int kPairs>
+template <bool kGated>
 __global__ void __launch_bounds__(kPairThreads, 1)
     fp8_pair_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ CUtensorMap tw,
                     ProductArgs a, int row_tiles, int col_tiles) {
@@ -468,7 +468,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   uint8_t *sf = ring + kPairStages * kPairStageBytes;
   // full, sf_full and acc_shared_free: the ones of a pair's first CTA are used
   uint64_t *full = reinterpret_cast<uint64_t *>(sf + kPairSf * kPairSfBytes);
-  uint64_t *empty = full + kPairStages;        // a commit a pair of the cluster
+  uint64_t *empty = full + kPairStages;
   uint64_t *sf_full = empty + kPairStages;     // an arrival a CTA
   uint64_t *sf_empty = sf_full + kPairSf;
   uint64_t *acc_full = sf_empty + kPairSf;     // [2]
@@ -482,11 +482,9 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   volatile int *abort_flag = &abort_shared;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int rank = (int)cluster_rank(), side = rank & 1, pair = rank >> 1, first = rank & ~1;
-  const uint32_t pair_mask = 3u << first, all_mask = (1u << (2 * kPairs)) - 1;
-  const int clusters = gridDim.x / (2 * kPairs), cluster = blockIdx.x / (2 * kPairs);
-  // a cluster's tiles: kPairs neighbouring row tiles (the last may lie past the rows) of one column tile
-  const int row_groups = (row_tiles + kPairs - 1) / kPairs, total = row_groups * col_tiles;
+  const int side = (int)cluster_rank();
+  const uint32_t both = 3u;
+  const int clusters = gridDim.x / 2, cluster = blockIdx.x / 2, total = row_tiles * col_tiles;
   // This CTA's 128 rows of row tile rt: the tile's, but none past the last (as in the streaming kernel,
   // a tile that would pass it begins earlier); an odd last weight tile has no second, so its own is loaded
   // twice.
@@ -494,7 +492,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   if (tid == 0) {
     for (int s = 0; s < kPairStages; ++s) {
       mbar_init(&full[s], 1);
-      mbar_init(&empty[s], kPairs);
+      mbar_init(&empty[s], 1);
     }
     for (int s = 0; s < kPairSf; ++s) {
       mbar_init(&sf_full[s], 2);
@@ -529,7 +527,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       bool ok = true;
       int it = 0;
       for (int w = cluster; w < total && ok; w += clusters) {
-        const int rt = w % row_groups * kPairs + pair, ct = w / row_groups;
+        const int rt = w % row_tiles, ct = w / row_tiles;
         const int x_row = row_of(rt);
         // K block 0 of this CTA's weight tile in the laid-out weight
         const int64_t block = kGated ? (int64_t)ct * a.kbs * 2 + side
@@ -542,17 +540,11 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             break;
           }
           if (side == 0) mbar_arrive_tx(&full[s], 2 * kPairStageBytes);  // what lands in both CTAs
-          const uint32_t bar = cluster_map_shared(smem_u32(&full[s]), first);
+          const uint32_t bar = cluster_map_shared(smem_u32(&full[s]), 0);
           uint8_t *dst = ring + s * kPairStageBytes;
           const int w_row = (int)((block + (int64_t)kb * (kGated ? 2 : 1)) * (kBlockBytes / 2048));
           tma_load_2d_pair(dst, &tx, kb * kFp8Block, x_row, bar, pol);
-          if constexpr (kPairs == 1) {
-            tma_load_2d_pair(dst + kBlockBytes, &tw, 0, w_row, bar, pol);
-            tma_load_2d_pair(dst + kBlockBytes + kBlockBytes / 2, &tw, 0, w_row + kBlockBytes / 4096, bar, pol);
-          } else {  // this pair's half of the tile, for both
-            tma_load_2d_pair_multicast(dst + kBlockBytes + pair * (kBlockBytes / 2), &tw, 0, w_row + pair * (kBlockBytes / 4096), bar,
-                                       5u << side, pol);
-          }
+          tma_load_2d_pair(dst + kBlockBytes, &tw, 0, w_row, bar, pol);
           issued = it + 1;
         }
       }
@@ -581,7 +573,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
               const uint32_t from = smem_u32(sf + (gi % kPairSf) * kPairSfBytes);
 #pragma unroll
               for (int p = 0; p < 3; ++p) tc_copy_scales<2>(sft + p * 4, from + p * 512);
-              tc_commit_pair(&sf_empty[gi % kPairSf], pair_mask);
+              tc_commit_pair(&sf_empty[gi % kPairSf], both);
             }
             const uint32_t xa = smem_u32(ring + s * kPairStageBytes), wa = xa + kBlockBytes;
             const uint32_t idesc = idesc_mx(256, 256, kb & 3);
@@ -589,8 +581,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             for (int kk = 0; kk < 4; ++kk)
               tc_mma_mx<2>(acc, smem_desc_sw128(xa + kk * 32, 16, 1024), smem_desc_sw128(wa + kk * 32, 16, 1024),
                            idesc, sft, sft + 4, kb > 0 || kk > 0);
-            tc_commit_pair(&empty[s], all_mask);
-            if (kb == a.kbs - 1) tc_commit_pair(&acc_full[n & 1], pair_mask);
+            tc_commit_pair(&empty[s], both);
+            if (kb == a.kbs - 1) tc_commit_pair(&acc_full[n & 1], both);
           }
           __syncwarp();
           if ((kb & 3) == 3 || kb == a.kbs - 1) ++gi;
@@ -603,7 +595,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         }
         __syncwarp();
         if (elect_one()) {
-          tc_commit_pair(drained, pair_mask);
+          tc_commit_pair(drained, both);
           thread_wait(drained, 0u, abort_flag, false);
         }
         __syncwarp();
@@ -619,7 +611,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     const int groups = (a.kbs + 3) / 4, turn = warp - 2;
     uint32_t x[4], ws[2];
     auto load = [&](int w, int g) {
-      const int rt = w % row_groups * kPairs + pair, ct = w / row_groups, x_row = row_of(rt);
+      const int rt = w % row_tiles, ct = w / row_tiles, x_row = row_of(rt);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         x[j] = __ldg(reinterpret_cast<const uint32_t *>(a.xs + (int64_t)(x_row + lane + 32 * j) * a.sk) + g);
@@ -654,7 +646,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       if (w < total) load(w, g);
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(cluster_map_shared(smem_u32(&sf_full[slot]), first));
+      if (lane == 0) mbar_arrive_cluster(cluster_map_shared(smem_u32(&sf_full[slot]), 0));
     }
   } else if (warp >= 4) {
     // ------------------------------------------------------------ epilogue: two threads a row
@@ -662,12 +654,12 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     // of the up of a gated one), the last four the rest.  The shared columns are the last 64 of the first
     // accumulator and the first 64 of the second: the warps that have them load them before all else.
     const int quarter = warp & 3, half = (warp - 4) >> 2, lane_row = quarter * 32 + lane;
-    const uint32_t free_bar = cluster_map_shared(smem_u32(acc_shared_free), first);
+    const uint32_t free_bar = cluster_map_shared(smem_u32(acc_shared_free), 0);
     // rows begin at multiples of 32 bytes
     const bool straight = (a.n * (kGated ? 1 : a.f32 ? 4 : 2) & 31) == 0 && ((uintptr_t)a.out & 31u) == 0;
     int n = 0;
     for (int w = cluster; w < total; w += clusters, ++n) {
-      const int rt = w % row_groups * kPairs + pair, ct = w / row_groups, buf = n & 1;
+      const int rt = w % row_tiles, ct = w / row_tiles, buf = n & 1;
       const int row0 = row_of(rt) + quarter * 32, row = row0 + lane, own0 = rt * 256 + side * 128;
       const uint32_t acc = tmem + (uint32_t)(buf * kPairBuf1) + ((uint32_t)(quarter * 32) << 16);
       bool ok = warp_wait_cluster(&acc_full[buf], (uint32_t)(n >> 1) & 1u, abort_flag);
@@ -781,25 +773,25 @@ cudaError_t allow_smem(K kernel, int bytes, bool (&done)[64], int dev) {
   return e;
 }
 
-// Clusters of `ctas` CTAs that are resident at once (a cluster lies within one group of SMs, which need
-// not hold a whole number of them); a persistent grid is no larger.
+// Pairs that are resident at once (a pair lies within one group of SMs, which need not hold a whole number
+// of them); a persistent grid is no larger.
 template <typename K>
-int resident_clusters(K kernel, int ctas, int (&known)[64], int dev) {
+int resident_pairs(K kernel, int (&known)[64], int dev) {
   if (dev >= 0 && dev < 64 && known[dev] > 0) return known[dev];
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(device_sms() / ctas * ctas));
+  cfg.gridDim = dim3((unsigned)(device_sms() / 2 * 2));
   cfg.blockDim = dim3(kPairThreads);
   cfg.dynamicSmemBytes = (size_t)kPairSmem;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = (unsigned)ctas;
+  attr[0].val.clusterDim.x = 2;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   int n = 0;
   if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
     cudaGetLastError();
-    n = device_sms() / ctas;
+    n = device_sms() / 2;
   }
   if (dev >= 0 && dev < 64) known[dev] = n;
   return n;
@@ -833,35 +825,17 @@ cudaError_t launch_stream(const CUtensorMap &tx, ProductArgs a, int dev, cudaStr
                       dim3(kStreamThreads), (size_t)smem, dim3(1, (unsigned)splits, 1), stream, tx, a);
 }
 
-template <bool kGated, int kPairs>
-cudaError_t prepare_pair(int dev, int &clusters) {
-  static bool done[64] = {};
-  static int resident[64] = {};
-  const cudaError_t e = allow_smem(fp8_pair_kernel<kGated, kPairs>, kPairSmem, done, dev);
-  if (e == cudaSuccess) clusters = resident_clusters(fp8_pair_kernel<kGated, kPairs>, 2 * kPairs, resident, dev);
-  return e;
-}
-
 template <bool kGated>
 cudaError_t launch_pair(const CUtensorMap &tx, const CUtensorMap &tw, const ProductArgs &a, int dev,
                         cudaStream_t stream) {
+  static bool done[64] = {};
+  static int resident[64] = {};
   const int row_tiles = (a.rows + 255) / 256, col_tiles = kGated ? a.tiles : (a.tiles + 1) / 2;
-  int one = 0, two = 0;
-  cudaError_t e = prepare_pair<kGated, 1>(dev, one);
-  if (e == cudaSuccess) e = prepare_pair<kGated, 2>(dev, two);
+  const cudaError_t e = allow_smem(fp8_pair_kernel<kGated>, kPairSmem, done, dev);
   if (e != cudaSuccess) return e;
-  // Tiles that the busiest pair computes, with one pair a cluster and with two: at the same number the two,
-  // which share their weight tiles' loads, are up to a tenth faster (1024 rows, 16384 features of 4096: 47
-  // to 50 us against 52); else one, of which more are resident (gated, 4096 rows, 16384 features: 29 tiles
-  // and 319 us with two, 27 and 306 to 315 with one).
-  const int64_t work1 = ((int64_t)row_tiles * col_tiles + one - 1) / one;
-  const int64_t groups = (int64_t)((row_tiles + 1) / 2) * col_tiles, work2 = (groups + two - 1) / two;
-  if (work2 <= work1)
-    return launch_after<fp8_pair_kernel<kGated, 2>>(dim3((unsigned)(4 * std::min<int64_t>(two, groups))), dim3(kPairThreads),
-                        (size_t)kPairSmem, dim3(4, 1, 1), stream, tx, tw, a, row_tiles, col_tiles);
-  return launch_after<fp8_pair_kernel<kGated, 1>>(
-                      dim3((unsigned)(2 * std::min<int64_t>(one, (int64_t)row_tiles * col_tiles))), dim3(kPairThreads),
-                      (size_t)kPairSmem, dim3(2, 1, 1), stream, tx, tw, a, row_tiles, col_tiles);
+  const int64_t pairs = std::min<int64_t>(resident_pairs(fp8_pair_kernel<kGated>, resident, dev), (int64_t)row_tiles * col_tiles);
+  return launch_after<fp8_pair_kernel<kGated>>(dim3((unsigned)(2 * pairs)), dim3(kPairThreads), (size_t)kPairSmem,
+                      dim3(2, 1, 1), stream, tx, tw, a, row_tiles, col_tiles);
 }
 
 int run_product(ham_fp8_weight *w, const void *x_codes, const void *x_scales, int32_t rows, void *out,
@@ -984,7 +958,7 @@ int ham_fp8_weight_alloc(int32_t n, int32_t k, const void *codes, const void *sc
   if (e == cudaSuccess) e = cudaMemset(w->err, 0, 4);
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
   if (e != cudaSuccess || ham::make_stretch_tensor_map(&w->map, w->codes, blocks * w->parts * ham::kBlockBytes,
-                                                       ham::kBlockBytes / 2) != 0) {
+                                                       ham::kBlockBytes) != 0) {
     cudaGetLastError();
     ham_fp8_weight_free(w);
     return op_fail(HAM_ECUDA, "weight layout: %s", cudaGetErrorString(e));

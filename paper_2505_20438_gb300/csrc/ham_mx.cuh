@@ -133,16 +133,6 @@ __device__ __forceinline__ void tma_load_2d_pair(void *dst, const CUtensorMap *m
       : "memory");
 }
 
-// The same into every CTA of `mask`, at the same place in each; the bytes count at the first CTA of each
-// one's pair.
-__device__ __forceinline__ void tma_load_2d_pair_multicast(void *dst, const CUtensorMap *map, int x, int y,
-                                                           uint32_t bar, uint32_t mask, uint64_t policy) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-      ".multicast::cluster.L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5, %6;" ::"r"(smem_u32(dst)),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar), "h"((uint16_t)mask), "l"(policy)
-      : "memory");
-}
 // 32 bytes to global memory (32-byte aligned): a whole sector a thread.
 __device__ __forceinline__ void st_global_32(void *p, const uint32_t (&v)[8]) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]),
