@@ -6,16 +6,17 @@
 //   H[t][f] = silu(G[t][f]) U[t][f],  G = X W_g^T, U = X W_u^T,  encoded as 8-bit rows
 //
 // The scales are E8M0 bytes, so tcgen05 kind::mxf8f6f4 applies them inside the product (its scale
-// blocks are 32 elements of K: four products of a 128-block use the same byte) and a whole sum stays
-// in one fp32 accumulator in tensor memory.  Four consecutive blocks' bytes are one 32-bit word of a
-// row; a word serves four K steps, the instruction descriptor selecting the byte, so that the scales
-// of an operand tile are copied to tensor memory (512 bytes a copy) once every four steps.
+// blocks are 32 elements of K: four products of a 128-block use the same byte) and sums stay in fp32
+// accumulators in tensor memory.  Four consecutive blocks' bytes are one 32-bit word of a row; a word serves
+// four K steps, the instruction descriptor selecting the byte, so that the scales of an operand tile are
+// copied to tensor memory (512 bytes a copy) once every four steps.
 //
-// The tensor cores add 32 terms of K exactly to the fp32 sum and cut the result off at its last place, which
-// grows with K and with the sum's parts: measured against 64-bit sums, relative to the outputs' norm, 7e-8 at
-// K 4096 and 1.1 to 1.3e-6 at 14512 to 16384 in one accumulator (toward zero), 1.2 to 2.3e-7 where the stream
-// kernel cuts K over a cluster.  Adding parts of K in registers would bring the former down too, but a tile of
-// the pair kernel is 128 KB of sums a CTA, as much as all its registers.
+// The tensor cores add 32 terms of K exactly to the fp32 sum and cut the result off at its last place, toward
+// zero, so that one accumulator's error is a bias that grows with K: measured against 64-bit sums, relative to
+// the outputs' norm, 5.9e-8 at K 1024, 1.1e-7 at 2048, 2.3e-7 at 4096, 1.3e-6 at 16384 (a plain fp32 product:
+// 4.1e-8, 5.9e-8, 8.6e-8, 2.0e-7).  So an accumulator takes kSumBlocks blocks of K, 2048 terms (kSumMost where
+// more accumulators would cost the streaming kernel a CTA an SM), and the parts are added in fp32, in order:
+// 1.1 to 1.2e-7 at every K from 2048 on (2.4e-7).
 //
 // Weights are laid out once (ham_fp8_weight_alloc) as [tile of 128 rows][K block][128 x 128], each
 // block 16 KiB in the shared-memory layout of the 128-byte swizzle, so that a weight tile's K range is
@@ -39,13 +40,14 @@ struct ham_fp8_weight {
   uint8_t *scales = nullptr;   // [tiles][parts][sk]
   int32_t *err = nullptr;      // device error word
   int32_t *host_err = nullptr; // pinned
-  CUtensorMap map;             // codes as one stretch, boxes of a block
+  CUtensorMap map;             // codes as one stretch, boxes of half a block
 };
 
 namespace ham {
 namespace {
 
 constexpr int kTile = 128;             // weight rows of a tile
+constexpr int kSumBlocks = 16, kSumMost = 32;  // K blocks of one accumulator
 constexpr int kBlockBytes = 128 * 128; // a tile's K block
 
 // One thread per 16-byte piece of the laid-out weight.
@@ -80,6 +82,8 @@ struct ProductArgs {
   uint8_t *out_scales;     // gated: [rows][out_sk]
   int32_t *err;
   int rows, n, kbs, sk, out_sk;
+  int part;                // K blocks that one accumulator takes
+  int sums;                // the streaming kernel: accumulators
   int nt, box;             // the streaming kernel: rows of X a CTA takes (a multiple of 16), rows it loads
   int stages, stage_bytes, tmem_cols;
   int tiles;               // weight tiles
@@ -129,6 +133,10 @@ constexpr int kStreamStages = 12;       // at most
 constexpr int kStreamBars = (2 * kStreamStages + 2 * kStreamSf + 1) * 8;
 // Bytes of a scale slot (the weight tiles', the rows') and of everything beside the ring.
 __host__ __device__ constexpr int stream_sf_bytes(int parts) { return (parts + 1) * 512; }
+constexpr int stream_sf_columns(int parts) { return 2 * (parts + 1) * 4; }
+// Accumulators that `columns` of tensor memory hold beside the scales.
+constexpr int stream_sums(int parts, int nt, int columns) { return (columns - stream_sf_columns(parts)) / (parts * nt); }
+constexpr int kMaxSplits = 8;
 constexpr int stream_fixed(int parts) { return 1024 + kStreamSf * stream_sf_bytes(parts) + kStreamBars; }
 
 template <int kParts>
@@ -213,7 +221,9 @@ __global__ void __launch_bounds__(kStreamThreads)
   } else if (warp == 1) {
     // ------------------------------------------------------------ products
     const uint32_t tmem = *const_cast<volatile uint32_t *>(&tmem_slot);
-    const uint32_t sf_tmem = tmem + kParts * a.nt;    // two buffers of (kParts + 1) * 4 columns
+    const uint32_t sf_tmem = tmem + a.sums * kParts * a.nt;  // two buffers of (kParts + 1) * 4 columns
+    uint32_t acc = tmem;
+    int in = 0;                                       // blocks of the accumulator so far
     bool ok = true;
     for (int t = 0; t < nk; ++t) {
       const int s = t % stages, kb = kb0 + t, g = (kb >> 2) - g0;
@@ -235,12 +245,13 @@ __global__ void __launch_bounds__(kStreamThreads)
         for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
           for (int p = 0; p < kParts; ++p)
-            tc_mma_mx<1>(tmem + p * a.nt, smem_desc_sw128(wa + p * kBlockBytes + kk * 32, 16, 1024),
+            tc_mma_mx<1>(acc + p * a.nt, smem_desc_sw128(wa + p * kBlockBytes + kk * 32, 16, 1024),
                          smem_desc_sw128(xa + kk * 32, 16, 1024), idesc, sft + p * 4, sft + kParts * 4,
-                         t > 0 || kk > 0);
+                         in > 0 || kk > 0);
         tc_commit(&empty[s]);
       }
       __syncwarp();
+      if (++in == a.part) in = 0, acc += kParts * a.nt;
     }
     if (!ok && lane == 0 && !*abort_flag) {
       record_error(a.err, HAM_DEVERR_TIMEOUT);
@@ -297,14 +308,21 @@ __global__ void __launch_bounds__(kStreamThreads)
   float *acc = reinterpret_cast<float *>(ring);
   if (ok) {
     tc_fence_after();
-    const int quarter = warp & 3;
+    const int quarter = warp & 3, sums = (nk + a.part - 1) / a.part;  // accumulators in use
     const uint32_t t_row = tmem + ((uint32_t)(quarter * 32) << 16);
     for (int c = (warp >> 2) * 16; c < kParts * a.nt; c += 32) {
-      uint32_t v[16];
-      tmem_ld16(t_row + c, v);
+      float v[16];
+      tmem_ld16(t_row + c, *reinterpret_cast<uint32_t(*)[16]>(v));
       tmem_wait_ld();
+      for (int i = 1; i < sums; ++i) {
+        float u[16];
+        tmem_ld16(t_row + i * kParts * a.nt + c, *reinterpret_cast<uint32_t(*)[16]>(u));
+        tmem_wait_ld();
 #pragma unroll
-      for (int j = 0; j < 16; ++j) acc[(c + j) * kTile + quarter * 32 + lane] = __uint_as_float(v[j]);
+        for (int j = 0; j < 16; ++j) v[j] += u[j];
+      }
+#pragma unroll
+      for (int j = 0; j < 16; ++j) acc[(c + j) * kTile + quarter * 32 + lane] = v[j];
     }
   }
   tc_fence_before();
@@ -361,25 +379,35 @@ __global__ void __launch_bounds__(kStreamThreads)
 // ------------------------------------------------------------------------------------
 // A pair of CTAs (cta_group::2) computes 256 rows of X by two weight tiles (a gated weight: the gate's
 // and the up's tile of the same features): each CTA holds 128 of the rows (its lanes of tensor memory)
-// and loads its rows and one of the two weight tiles, both into its own shared memory alone (the library
-// is also what every rank of a job on several GPUs loads, so no load here is a cluster multicast).  The
-// pairs are persistent.  The two accumulators (256 columns each) share 64 columns, which leaves the columns
-// 448.. for the scales: a tile's epilogue takes the shared columns into registers first, and the next
-// tile's products begin when it has.
+// and loads its rows and half of the weight rows, into its own shared memory alone (the library is also what
+// every rank of a job on several GPUs loads, so no load here is a cluster multicast).  The pairs are
+// persistent.
 //
-// Bound by the tensor cores: 8192 rows, K 4096, 6144 features 119 us (3.46 PFLOP/s, 90% of twice the measured
-// bf16 rate), 4096 rows, K 16384, 4096 features 169 us (85%), gated 4096 rows of 4096 in 16384 features
-// 300 us (95%); run without a break the card's power limit makes that 139, 193 and 357 us.  Few tiles leave
-// pairs without work in the last round, and the first tile's loads and the last one's epilogue stand alone
-// (2048 rows, 4096 x 4096: 26.5 us, 67%).  A pair takes 64 bytes a clock an SM from L2 at the products' full
-// rate; with two pairs a cluster, each loading half of their weight tiles into both, 48, and these cases
-// took 119, 164 and 300 us, 139, 192 and 356.
+// The tile's sums are two accumulators of 128 columns each, of three in tensor memory: one takes a group of
+// two K blocks, then the other takes them, so that a part of K ends in the first a group's products before it
+// ends in the second, the first of the next part has an accumulator of its own at once, and the second takes
+// the one that the epilogue has emptied meanwhile.  With one accumulator of 256 columns, two of which share
+// 64, a part cost 0.6 to 0.9 us more.  (Groups of four blocks, which hold most of the ring, took 4096 x 16384
+// x 4096 from 172 to 205 us.)  The epilogue holds the sums of the parts before in registers.
+//
+// Bound by the tensor cores: 8192 rows, K 4096, 6144 features 120 us (3.44 PFLOP/s, 89% of twice the measured
+// bf16 rate), 4096 rows, K 16384, 4096 features 172 us (83%), gated 4096 rows of 4096 in 16384 features
+// 305 to 310 us (92 to 94%); run without a break the card's power limit makes that 141, 196 and 362 us.  Few
+// tiles leave pairs without work in the last round, and the first tile's loads and the last one's epilogue
+// stand alone (2048 rows, 4096 x 4096: 27 us, 66%).  With one accumulator for all of K these took 119, 169,
+// 302 and 26.5 us; a pair takes 64 bytes a clock an SM from L2 at the products' full rate.
 constexpr int kPairThreads = 384;       // warps: copies, products, 2 x scales, 8 x epilogue
+// Registers a thread: the launch's, and from the roles on those of the first four warps and of the epilogue's
+// eight, which hold a tile's sums in 128 of them.  Together they are what the launch has: a kernel compiled
+// to fewer would wait for the rest forever, so the host looks before it launches one.
+constexpr int kLaunchRegs = 168, kFewRegs = 56, kManyRegs = 224;
+static_assert(4 * kFewRegs + 8 * kManyRegs <= 12 * kLaunchRegs && kPairThreads == 384, "registers");
 constexpr int kPairStages = 6;
 constexpr int kPairStageBytes = 2 * kBlockBytes;
 constexpr int kPairSf = 4;
-constexpr int kPairSfBytes = 3 * 512;   // the CTA's 128 rows, both weight tiles
-constexpr int kPairBuf1 = 192, kPairSfCol = 448;
+constexpr int kPairSfBytes = 3 * 512;   // the CTA's 128 rows, the weight rows of both halves
+constexpr int kPairSums = 3, kPairSfCol = 448;  // accumulators of 128 columns, then the scales
+constexpr int kGroup = 2;               // K blocks that one accumulator takes, then the other
 constexpr int kTurn = 17;               // floats a row of a warp's turning space: 16 columns, padded
 constexpr int kPairUsed = 1024 + kPairStages * kPairStageBytes + kPairSf * kPairSfBytes + 256 + 8 * 32 * kTurn * 4;
 constexpr int kPairSmem = kPairUsed > smem_floor(512) ? kPairUsed : smem_floor(512);
@@ -387,13 +415,15 @@ static_assert(kPairSmem <= 226 * 1024, "shared memory");
 
 // 32 accumulator columns (from column c of n) of a warp's 32 rows (those from own0 on), a row a lane, to the
 // output through shared memory, 16 columns at a time, so that neighbouring lanes write neighbours, kEach
-// elements each: what n is a multiple of, up to 16 bytes.  (3344 rows, K 544, some 15550 features, which the
-// outputs bound: bf16 35 us straight, turned 48 with 8 elements, 55 with 4, 62 with 2, 88 with 1; fp32 53, and
-// 68, 84, 94 with 4, 2, 1.  16 bytes a lane straight from the registers took 57 and 117; a value at
-// a time, a row a lane, 164 for 3000 x 5003 outputs of 2000 columns that take 38 turned.)
-template <int kEach>
+// elements each: what n is a multiple of, up to 16 bytes.  Loads from shared memory are issued four at a time,
+// before their stores.  (3344 rows, K 544, some 15550 features, which the outputs bound: bf16 35 us straight,
+// turned 50 with 8 elements, 60 with 4, 71 with 1 (89 with the loads one by one); fp32 53, and 55 with 4.
+// 16 bytes a lane straight from the registers took 57 and 117; a value at a time, a row a lane, 164 for 3000 x
+// 5003 outputs of 2000 columns that take 38 turned.)
+template <int kEach, bool kF32>
 __device__ __forceinline__ void store_turned(const ProductArgs &a, int row0, int own0, int c, const float *f, float *turn) {
   constexpr int kLanes = 16 / kEach;             // a row's
+  constexpr int kSteps = 16 / kEach, kAtOnce = kSteps < 4 ? kSteps : 4;
   const int lane = threadIdx.x & 31, at = lane % kLanes * kEach;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -402,50 +432,61 @@ __device__ __forceinline__ void store_turned(const ProductArgs &a, int row0, int
     for (int j = 0; j < 16; ++j) turn[lane * kTurn + j] = f[16 * h + j];
     __syncwarp();
     const int col = c + 16 * h + at;
-#pragma unroll 4
-    for (int i = 0; i < 16 / kEach; ++i) {
-      const int r = i * 2 * kEach + lane / kLanes;
-      if (row0 + r < own0 || col >= a.n) continue;
-      const float *x = turn + r * kTurn + at;
-      const int64_t to = (int64_t)(row0 + r) * a.n + col;
-      if (a.f32) {
-        float *y = static_cast<float *>(a.out) + to;
-        if constexpr (kEach == 1) *y = x[0];
-        if constexpr (kEach == 2) *reinterpret_cast<float2 *>(y) = make_float2(x[0], x[1]);
-        if constexpr (kEach == 4) *reinterpret_cast<float4 *>(y) = make_float4(x[0], x[1], x[2], x[3]);
-      } else {
-        __nv_bfloat16 *y = static_cast<__nv_bfloat16 *>(a.out) + to;
-        if constexpr (kEach == 1) *y = __float2bfloat16_rn(x[0]);
-        if constexpr (kEach == 2) *reinterpret_cast<uint32_t *>(y) = pack_bf16x2(x[0], x[1]);
-        if constexpr (kEach == 4)
-          *reinterpret_cast<uint2 *>(y) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
-        if constexpr (kEach == 8)
-          *reinterpret_cast<uint4 *>(y) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
-                                                     pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+#pragma unroll
+    for (int i0 = 0; i0 < kSteps; i0 += kAtOnce) {
+      const int r0 = i0 * 2 * kEach + lane / kLanes;
+      float x[kAtOnce][kEach];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) x[i][j] = turn[(r0 + i * 2 * kEach) * kTurn + at + j];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int row = row0 + r0 + i * 2 * kEach;
+        if (row < own0 || col >= a.n) continue;
+        const int64_t to = (int64_t)row * a.n + col;
+        if constexpr (kF32) {
+          float *y = static_cast<float *>(a.out) + to;
+          if constexpr (kEach == 1) *y = x[i][0];
+          if constexpr (kEach == 2) *reinterpret_cast<float2 *>(y) = make_float2(x[i][0], x[i][1]);
+          if constexpr (kEach == 4) *reinterpret_cast<float4 *>(y) = make_float4(x[i][0], x[i][1], x[i][2], x[i][3]);
+        } else {
+          __nv_bfloat16 *y = static_cast<__nv_bfloat16 *>(a.out) + to;
+          if constexpr (kEach == 1) *y = __float2bfloat16_rn(x[i][0]);
+          if constexpr (kEach == 2) *reinterpret_cast<uint32_t *>(y) = pack_bf16x2(x[i][0], x[i][1]);
+          if constexpr (kEach == 4)
+            *reinterpret_cast<uint2 *>(y) = make_uint2(pack_bf16x2(x[i][0], x[i][1]), pack_bf16x2(x[i][2], x[i][3]));
+          if constexpr (kEach == 8)
+            *reinterpret_cast<uint4 *>(y) = make_uint4(pack_bf16x2(x[i][0], x[i][1]), pack_bf16x2(x[i][2], x[i][3]),
+                                                       pack_bf16x2(x[i][4], x[i][5]), pack_bf16x2(x[i][6], x[i][7]));
+        }
       }
     }
   }
 }
-// The same straight from the registers, 32 bytes at a time a lane, where rows begin at multiples of them
-// (`straight`); else turned.
-__device__ __forceinline__ void store32(const ProductArgs &a, int row0, int own0, int c, const uint32_t (&v)[32],
-                                        bool straight, float *turn) {
-  const float *f = reinterpret_cast<const float *>(v);
-  const int lane = threadIdx.x & 31, row = row0 + lane;
-  if (c >= a.n) return;
-  if (!straight) {
-    if ((a.n & 7) == 0 && !a.f32) store_turned<8>(a, row0, own0, c, f, turn);
-    else if ((a.n & 3) == 0) store_turned<4>(a, row0, own0, c, f, turn);
-    else if ((a.n & 1) == 0) store_turned<2>(a, row0, own0, c, f, turn);
-    else store_turned<1>(a, row0, own0, c, f, turn);
-    return;
+// The same in units of what n is a multiple of.
+__device__ __forceinline__ void store_turned(const ProductArgs &a, int row0, int own0, int c, const float *f, float *turn) {
+  if (a.f32) {
+    if ((a.n & 3) == 0) store_turned<4, true>(a, row0, own0, c, f, turn);
+    else if ((a.n & 1) == 0) store_turned<2, true>(a, row0, own0, c, f, turn);
+    else store_turned<1, true>(a, row0, own0, c, f, turn);
+  } else {
+    if ((a.n & 7) == 0) store_turned<8, false>(a, row0, own0, c, f, turn);
+    else if ((a.n & 3) == 0) store_turned<4, false>(a, row0, own0, c, f, turn);
+    else if ((a.n & 1) == 0) store_turned<2, false>(a, row0, own0, c, f, turn);
+    else store_turned<1, false>(a, row0, own0, c, f, turn);
   }
+}
+// The same straight from the registers, 32 bytes at a time a lane, where rows begin at multiples of them.
+__device__ __forceinline__ void store_straight(const ProductArgs &a, int row, int own0, int c, const float *f) {
   if (row < own0) return;
   char *dst = static_cast<char *>(a.out) + ((int64_t)row * a.n + c) * (a.f32 ? 4 : 2);
   if (a.f32) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const uint32_t w[8] = {v[8 * q], v[8 * q + 1], v[8 * q + 2], v[8 * q + 3], v[8 * q + 4], v[8 * q + 5], v[8 * q + 6], v[8 * q + 7]};
+      uint32_t w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(f[8 * q + j]);
       if (c + 8 * q < a.n) st_global_32(dst + 32 * q, w);
     }
   } else {
@@ -459,22 +500,24 @@ __device__ __forceinline__ void store32(const ProductArgs &a, int row0, int own0
   }
 }
 
-template <bool kGated>
+// kMore: K may be several accumulators' (a plain product of one needs no registers for sums, and stores
+// straight from the accumulator; a gated one holds its 128 values a thread in any case).
+template <bool kGated, bool kMore>
 __global__ void __launch_bounds__(kPairThreads, 1)
     fp8_pair_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ CUtensorMap tw,
                     ProductArgs a, int row_tiles, int col_tiles) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t *sf = ring + kPairStages * kPairStageBytes;
-  // full, sf_full and acc_shared_free: the ones of a pair's first CTA are used
+  // full, sf_full and sum_free: the ones of a pair's first CTA are used
   uint64_t *full = reinterpret_cast<uint64_t *>(sf + kPairSf * kPairSfBytes);
   uint64_t *empty = full + kPairStages;
   uint64_t *sf_full = empty + kPairStages;     // an arrival a CTA
   uint64_t *sf_empty = sf_full + kPairSf;
-  uint64_t *acc_full = sf_empty + kPairSf;     // [2]
-  uint64_t *acc_shared_free = acc_full + 2;    // an arrival an epilogue warp of the pair
-  uint64_t *drained = acc_shared_free + 1;     // every product issued is complete (after an abort)
-  static_assert((2 * kPairStages + 2 * kPairSf + 4) * 8 <= 256, "barriers");
+  uint64_t *sum_full = sf_empty + kPairSf;     // [half][every other part of K]
+  uint64_t *sum_free = sum_full + 4;           // the same: an arrival a warp of the pair that takes the half
+  uint64_t *drained = sum_free + 4;            // every product issued is complete (after an abort)
+  static_assert((2 * kPairStages + 2 * kPairSf + 9) * 8 <= 256, "barriers");
   float *turn = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(full) + 256);  // [8 warps][32][kTurn]
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_shared;
@@ -498,9 +541,10 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       mbar_init(&sf_full[s], 2);
       mbar_init(&sf_empty[s], 1);
     }
-    mbar_init(&acc_full[0], 1);
-    mbar_init(&acc_full[1], 1);
-    mbar_init(acc_shared_free, 16);
+    for (int s = 0; s < 4; ++s) {
+      mbar_init(&sum_full[s], 1);
+      mbar_init(&sum_free[s], 8);
+    }
     mbar_init(drained, 1);
     abort_shared = 0;
     fence_mbar_init();
@@ -518,231 +562,300 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   }
   const uint32_t tmem = *const_cast<volatile uint32_t *>(&tmem_slot);  // (not warp 0's)
   int issued = 0;
-
-  if (warp == 0) {
-    // ------------------------------------------------------------ copies
-    if (lane == 0) {
-      const uint64_t pol = policy_evict_last();
-      grid_dependency_wait();
-      bool ok = true;
-      int it = 0;
-      for (int w = cluster; w < total && ok; w += clusters) {
-        const int rt = w % row_tiles, ct = w / row_tiles;
-        const int x_row = row_of(rt);
-        // K block 0 of this CTA's weight tile in the laid-out weight
-        const int64_t block = kGated ? (int64_t)ct * a.kbs * 2 + side
-                                     : (int64_t)min(ct * 2 + side, a.tiles - 1) * a.kbs;
-        for (int kb = 0; kb < a.kbs; ++kb, ++it) {
-          const int s = it % kPairStages;
-          if (it >= kPairStages &&
-              !thread_wait(&empty[s], (uint32_t)(it / kPairStages - 1) & 1u, abort_flag, true)) {
-            ok = false;
-            break;
-          }
-          if (side == 0) mbar_arrive_tx(&full[s], 2 * kPairStageBytes);  // what lands in both CTAs
-          const uint32_t bar = cluster_map_shared(smem_u32(&full[s]), 0);
-          uint8_t *dst = ring + s * kPairStageBytes;
-          const int w_row = (int)((block + (int64_t)kb * (kGated ? 2 : 1)) * (kBlockBytes / 2048));
-          tma_load_2d_pair(dst, &tx, kb * kFp8Block, x_row, bar, pol);
-          tma_load_2d_pair(dst + kBlockBytes, &tw, 0, w_row, bar, pol);
-          issued = it + 1;
-        }
-      }
-      if (!ok && !*abort_flag) {
-        record_error(a.err, HAM_DEVERR_TIMEOUT);
-        *abort_flag = 1;
-      }
-    }
-  } else if (warp == 1) {
-    // ------------------------------------------------------------ products (a pair's first CTA)
-    if (side == 0) {
-      bool ok = true;
-      int it = 0, gi = 0, n = 0;
-      for (int w = cluster; w < total && ok; w += clusters, ++n) {
-        const uint32_t acc = tmem + (uint32_t)((n & 1) * kPairBuf1);
-        if (n > 0 && !warp_wait_cluster(acc_shared_free, (uint32_t)(n - 1) & 1u, abort_flag)) { ok = false; break; }
-        for (int kb = 0; kb < a.kbs; ++kb, ++it) {
-          const int s = it % kPairStages;
-          const bool new_word = (kb & 3) == 0;
-          const uint32_t sft = tmem + kPairSfCol + (uint32_t)((gi & 1) * 16);
-          if (new_word && !warp_wait_cluster(&sf_full[gi % kPairSf], (uint32_t)(gi / kPairSf) & 1u, abort_flag)) { ok = false; break; }
-          if (!warp_wait_cluster(&full[s], (uint32_t)(it / kPairStages) & 1u, abort_flag)) { ok = false; break; }
-          if (elect_one()) {
-            tc_fence_after();
-            if (new_word) {
-              const uint32_t from = smem_u32(sf + (gi % kPairSf) * kPairSfBytes);
+  if (warp < 4) {
+    if constexpr (kMore) setmaxnreg_dec<kFewRegs>();
+    if (warp == 0) {
+      // ------------------------------------------------------------ copies
+      if (lane == 0) {
+        const uint64_t pol = policy_evict_last();
+        grid_dependency_wait();
+        bool ok = true;
+        int it = 0;
+        for (int w = cluster; w < total && ok; w += clusters) {
+          const int rt = w % row_tiles, ct = w / row_tiles;
+          const int x_row = row_of(rt);
+          // K block 0 of the weight's two stretches of 64 rows that this CTA takes, one a half of the sums: plain,
+          // its half of each tile (so that a half of the sums is a tile); gated, of the gate's or the up's tile
+          int from[2];
 #pragma unroll
-              for (int p = 0; p < 3; ++p) tc_copy_scales<2>(sft + p * 4, from + p * 512);
-              tc_commit_pair(&sf_empty[gi % kPairSf], both);
+          for (int h = 0; h < 2; ++h)
+            from[h] = kGated ? (int)(((int64_t)ct * a.kbs * 2 + side) * (kBlockBytes / 2048)) + h * (kBlockBytes / 4096)
+                             : (int)((int64_t)min(ct * 2 + h, a.tiles - 1) * a.kbs * (kBlockBytes / 2048)) + side * (kBlockBytes / 4096);
+          for (int kb = 0; kb < a.kbs; ++kb, ++it) {
+            const int s = it % kPairStages;
+            if (it >= kPairStages &&
+                !thread_wait(&empty[s], (uint32_t)(it / kPairStages - 1) & 1u, abort_flag, true)) {
+              ok = false;
+              break;
             }
-            const uint32_t xa = smem_u32(ring + s * kPairStageBytes), wa = xa + kBlockBytes;
-            const uint32_t idesc = idesc_mx(256, 256, kb & 3);
+            if (side == 0) mbar_arrive_tx(&full[s], 2 * kPairStageBytes);  // what lands in both CTAs
+            const uint32_t bar = cluster_map_shared(smem_u32(&full[s]), 0);
+            uint8_t *dst = ring + s * kPairStageBytes;
+            tma_load_2d_pair(dst, &tx, kb * kFp8Block, x_row, bar, pol);
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk)
-              tc_mma_mx<2>(acc, smem_desc_sw128(xa + kk * 32, 16, 1024), smem_desc_sw128(wa + kk * 32, 16, 1024),
-                           idesc, sft, sft + 4, kb > 0 || kk > 0);
-            tc_commit_pair(&empty[s], both);
-            if (kb == a.kbs - 1) tc_commit_pair(&acc_full[n & 1], both);
+            for (int h = 0; h < 2; ++h)
+              tma_load_2d_pair(dst + kBlockBytes + h * (kBlockBytes / 2), &tw, 0,
+                               from[h] + kb * (kGated ? 2 : 1) * (kBlockBytes / 2048), bar, pol);
+            issued = it + 1;
           }
-          __syncwarp();
-          if ((kb & 3) == 3 || kb == a.kbs - 1) ++gi;
         }
-      }
-      if (!ok) {
-        if (lane == 0 && !*abort_flag) {
+        if (!ok && !*abort_flag) {
           record_error(a.err, HAM_DEVERR_TIMEOUT);
           *abort_flag = 1;
         }
-        __syncwarp();
-        if (elect_one()) {
+      }
+    } else if (warp == 1) {
+      // ------------------------------------------------------------ products (a pair's first CTA)
+      // One thread waits and issues: what it does between two blocks' products is on their way (a division a
+      // block took 4096 x 16384 x 4096 from 185 to 215 us).
+      if (side == 0 && elect_one()) {
+        const uint64_t blocks = smem_desc_sw128(smem_u32(ring), 16, 1024), words = smem_desc_plain(smem_u32(sf), 0, 128);
+        constexpr uint32_t kNextByte = idesc_mx(256, 128, 1) - idesc_mx(256, 128, 0);
+        const int tiles = (total - cluster + clusters - 1) / clusters;
+        bool ok = true;
+        int s = 0, slot = 0, sum = 0;            // of the block, of the scale word, of the first half's accumulator
+        uint32_t phase = 0, word_phase = 0, n = 0, which = 0;
+        for (int t = 0; t < tiles && ok; ++t) {
+          for (int g = 0, in = 0; g < a.kbs; g += kGroup) {   // in: blocks of this part so far
+            const bool two = g + 1 < a.kbs, ends = g + kGroup >= a.kbs || in + kGroup >= a.part;
+            const int s1 = s + 1 == kPairStages ? 0 : s + 1;
+            if ((g & 3) == 0) {
+              ok = ok && thread_wait_cluster(&sf_full[slot], word_phase, abort_flag);
+              which ^= 16;
+            }
+            ok = ok && thread_wait_cluster(&full[s], phase, abort_flag);
+            // (the accumulator three before: the other half's, two or one parts before)
+            if (in == 0 && n >= 2) ok = ok && thread_wait_cluster(&sum_free[2 + (n & 1)], (n - 2) >> 1 & 1u, abort_flag);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t sft = tmem + kPairSfCol + which;
+            if ((g & 3) == 0) {
+#pragma unroll
+              for (int p = 0; p < 3; ++p)
+                tc_copy_scales_of<2>(sft + p * 4, words + (uint32_t)(slot * (kPairSfBytes / 16) + p * 32));
+              tc_commit_pair(&sf_empty[slot], both);
+              if (++slot == kPairSf) slot = 0, word_phase ^= 1;
+            }
+            const uint32_t idesc = idesc_mx(256, 128, 0) + (g & 3) * kNextByte;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              if (h && in == 0 && n >= 1) {
+                if (!thread_wait_cluster(&sum_free[(n - 1) & 1], (n - 1) >> 1 & 1u, abort_flag)) { ok = false; break; }
+                tc_fence_after();
+              }
+              const uint32_t acc = tmem + (uint32_t)((sum + h) % kPairSums * 128);
+#pragma unroll
+              for (int j = 0; j < kGroup; ++j) {
+                if (j && !two) break;
+                const int st = j ? s1 : s;
+                if (j && !h) {
+                  ok = thread_wait_cluster(&full[s1], phase ^ (s1 == 0), abort_flag);
+                  if (!ok) break;
+                  tc_fence_after();
+                }
+                const uint64_t x = blocks + (uint32_t)(st * (kPairStageBytes / 16)), wt = x + (uint32_t)(kBlockBytes + h * 64 * 128) / 16;
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk)
+                  tc_mma_mx<2>(acc, x + kk * 2, wt + kk * 2, idesc + j * kNextByte, sft, sft + 4 + 4 * h, in + j + kk > 0);
+                if (h) tc_commit_pair(&empty[st], both);
+              }
+              if (!ok) break;
+              if (ends) tc_commit_pair(&sum_full[h * 2 + (n & 1)], both);
+            }
+            if (!ok) break;
+            s += two ? 2 : 1;
+            if (s >= kPairStages) s -= kPairStages, phase ^= 1;
+            in += kGroup;
+            if (ends) {
+              in = 0, ++n;
+              sum = sum == 0 ? 2 : sum - 1;      // (two further on, of three)
+            }
+          }
+        }
+        if (!ok) {
+          if (!*abort_flag) {
+            record_error(a.err, HAM_DEVERR_TIMEOUT);
+            *abort_flag = 1;
+          }
           tc_commit_pair(drained, both);
           thread_wait(drained, 0u, abort_flag, false);
         }
+      }
+      __syncwarp();
+    } else {
+      // ------------------------------------------------------------ scale words
+      // Two warps take turns at the words (of four K blocks each), and each loads its next before it
+      // passes one on: the passing on, released at cluster scope, takes about as long as four K blocks'
+      // products do (with one warp it set the pace: 16384 columns, 4096 x 4096, 199 us against 163).
+      grid_dependency_wait();
+      if (warp == 2) grid_launch_dependents();
+      const int groups = (a.kbs + 3) / 4, turn = warp - 2;
+      uint32_t x[4], ws[2];
+      auto load = [&](int w, int g) {
+        const int rt = w % row_tiles, ct = w / row_tiles, x_row = row_of(rt);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          x[j] = __ldg(reinterpret_cast<const uint32_t *>(a.xs + (int64_t)(x_row + lane + 32 * j) * a.sk) + g);
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {  // the tile's scale rows: [tile][part]
+          const int row = kGated ? ct * 2 + p : min(ct * 2 + p, a.tiles - 1);
+          ws[p] = __ldg(reinterpret_cast<const uint32_t *>(a.ws + (int64_t)row * a.sk) + g);
+        }
+      };
+      // the gi-th word of this cluster's tiles is word g of tile w
+      int w = cluster, g = turn;
+      auto settle = [&] {
+        while (g >= groups) g -= groups, w += clusters;
+      };
+      settle();
+      if (w < total) load(w, g);
+      for (int gi = turn; w < total; gi += 2) {
+        const int slot = gi % kPairSf;
+        if (gi >= kPairSf && !warp_wait(&sf_empty[slot], (uint32_t)(gi / kPairSf - 1) & 1u, abort_flag)) {
+          if (lane == 0 && !*abort_flag) {
+            record_error(a.err, HAM_DEVERR_TIMEOUT);
+            *abort_flag = 1;
+          }
+          break;
+        }
+        uint4 *dst = reinterpret_cast<uint4 *>(sf + slot * kPairSfBytes) + lane;
+        dst[0] = make_uint4(x[0], x[1], x[2], x[3]);
+        dst[32] = make_uint4(ws[0], ws[0], ws[kGated], ws[kGated]);
+        dst[64] = make_uint4(ws[!kGated], ws[!kGated], ws[1], ws[1]);
+        g += 2;
+        settle();
+        if (w < total) load(w, g);
+        fence_proxy_async_smem();
         __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(cluster_map_shared(smem_u32(&sf_full[slot]), 0));
       }
     }
-  } else if (warp < 4) {
-    // ------------------------------------------------------------ scale words
-    // Two warps take turns at the words (of four K blocks each), and each loads its next before it
-    // passes one on: the passing on, released at cluster scope, takes about as long as four K blocks'
-    // products do (with one warp it set the pace: 16384 columns, 4096 x 4096, 199 us against 163).
-    grid_dependency_wait();
-    if (warp == 2) grid_launch_dependents();
-    const int groups = (a.kbs + 3) / 4, turn = warp - 2;
-    uint32_t x[4], ws[2];
-    auto load = [&](int w, int g) {
-      const int rt = w % row_tiles, ct = w / row_tiles, x_row = row_of(rt);
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        x[j] = __ldg(reinterpret_cast<const uint32_t *>(a.xs + (int64_t)(x_row + lane + 32 * j) * a.sk) + g);
-#pragma unroll
-      for (int p = 0; p < 2; ++p) {  // the tile's scale rows: [tile][part]
-        const int row = kGated ? ct * 2 + p : min(ct * 2 + p, a.tiles - 1);
-        ws[p] = __ldg(reinterpret_cast<const uint32_t *>(a.ws + (int64_t)row * a.sk) + g);
-      }
-    };
-    // the gi-th word of this cluster's tiles is word g of tile w
-    int w = cluster, g = turn;
-    auto settle = [&] {
-      while (g >= groups) g -= groups, w += clusters;
-    };
-    settle();
-    if (w < total) load(w, g);
-    for (int gi = turn; w < total; gi += 2) {
-      const int slot = gi % kPairSf;
-      if (gi >= kPairSf && !warp_wait(&sf_empty[slot], (uint32_t)(gi / kPairSf - 1) & 1u, abort_flag)) {
+  } else {
+    if constexpr (kMore) setmaxnreg_inc<kManyRegs>();
+    // ------------------------------------------------------------ epilogue: two threads a row
+    // Four warps take one half's sums, four the other's: a weight tile's, or 64 features of the gate and of the
+    // up of a gated one.
+    const int quarter = warp & 3, half = (warp - 4) >> 2, lane_row = quarter * 32 + lane;
+    const uint32_t free_bar = cluster_map_shared(smem_u32(sum_free + half * 2), 0);
+    // rows begin at multiples of 32 bytes
+    const bool straight = (a.n * (kGated ? 1 : a.f32 ? 4 : 2) & 31) == 0 && ((uintptr_t)a.out & 31u) == 0;
+    const int parts = (a.kbs + a.part - 1) / a.part;
+    int n = 0, sum = half;                       // parts of K so far; the accumulator
+    // The half's next accumulator, complete (false: the wait ran out), and its release.
+    const auto take = [&](uint32_t &acc) {
+      if (!warp_wait_cluster(&sum_full[half * 2 + (n & 1)], (uint32_t)(n >> 1) & 1u, abort_flag)) {
         if (lane == 0 && !*abort_flag) {
           record_error(a.err, HAM_DEVERR_TIMEOUT);
           *abort_flag = 1;
         }
-        break;
+        return false;
       }
-      uint4 *dst = reinterpret_cast<uint4 *>(sf + slot * kPairSfBytes) + lane;
-      dst[0] = make_uint4(x[0], x[1], x[2], x[3]);
-      dst[32] = make_uint4(ws[0], ws[0], ws[0], ws[0]);
-      dst[64] = make_uint4(ws[1], ws[1], ws[1], ws[1]);
-      g += 2;
-      settle();
-      if (w < total) load(w, g);
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(cluster_map_shared(smem_u32(&sf_full[slot]), 0));
-    }
-  } else if (warp >= 4) {
-    // ------------------------------------------------------------ epilogue: two threads a row
-    // The first four warps take the columns 0..127 of a plain product (features 0..63 of the gate and
-    // of the up of a gated one), the last four the rest.  The shared columns are the last 64 of the first
-    // accumulator and the first 64 of the second: the warps that have them load them before all else.
-    const int quarter = warp & 3, half = (warp - 4) >> 2, lane_row = quarter * 32 + lane;
-    const uint32_t free_bar = cluster_map_shared(smem_u32(acc_shared_free), 0);
-    // rows begin at multiples of 32 bytes
-    const bool straight = (a.n * (kGated ? 1 : a.f32 ? 4 : 2) & 31) == 0 && ((uintptr_t)a.out & 31u) == 0;
-    int n = 0;
-    for (int w = cluster; w < total; w += clusters, ++n) {
-      const int rt = w % row_tiles, ct = w / row_tiles, buf = n & 1;
-      const int row0 = row_of(rt) + quarter * 32, row = row0 + lane, own0 = rt * 256 + side * 128;
-      const uint32_t acc = tmem + (uint32_t)(buf * kPairBuf1) + ((uint32_t)(quarter * 32) << 16);
-      bool ok = warp_wait_cluster(&acc_full[buf], (uint32_t)(n >> 1) & 1u, abort_flag);
-      if (!ok && lane == 0 && !*abort_flag) {
-        record_error(a.err, HAM_DEVERR_TIMEOUT);
-        *abort_flag = 1;
-      }
-      if (kGated) ok = named_barrier_and(1 + quarter, 64, ok);  // (they meet below: both go on or neither)
-      if (!ok) break;
       tc_fence_after();
-      // Each warp arrives once a tile: when it has taken the shared columns that it has, and has long
-      // taken the tile before.
-      auto release = [&] {
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_cluster_relaxed(free_bar);
+      acc = tmem + (uint32_t)(sum * 128) + ((uint32_t)(quarter * 32) << 16);
+      sum = sum == 0 ? 2 : sum - 1;              // (two further on, of three)
+      return true;
+    };
+    const auto release = [&] {
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster_relaxed(free_bar + (n & 1) * 8);
+      ++n;
+    };
+    for (int w = cluster; w < total; w += clusters) {
+      const int rt = w % row_tiles, ct = w / row_tiles;
+      const int row0 = row_of(rt) + quarter * 32, row = row0 + lane, own0 = rt * 256 + side * 128;
+      // 32 columns of a plain product
+      const auto store = [&](int c, const float *f) {
+        if (c >= a.n) return;
+        if (straight) store_straight(a, row, own0, c, f);
+        else store_turned(a, row0, own0, c, f, turn + (warp - 4) * 32 * kTurn);
       };
-      const bool shared = half != buf;           // this warp has shared columns
-      if (!shared) release();
-      if constexpr (!kGated) {
-        // 64 columns at a time: half 0 upwards, half 1 downwards, so that shared ones come first
-        uint32_t v[32], u[32];
+      if constexpr (!kMore) {                    // 64 columns at a time, no sums to hold
+        uint32_t acc;
+        if (!take(acc)) break;
 #pragma unroll 1
         for (int i = 0; i < 2; ++i) {
-          const int col = half * 128 + (i ^ half) * 64;
-          tmem_ld32(acc + col, v);
-          tmem_ld32(acc + col + 32, u);
+          float f[64];
+#pragma unroll
+          for (int q = 0; q < 2; ++q) tmem_ld32(acc + i * 64 + q * 32, *reinterpret_cast<uint32_t(*)[32]>(f + q * 32));
           tmem_wait_ld();
-          if (i == 0 && shared) release();
-          const int c = ct * 256 + col;
-          store32(a, row0, own0, c, v, straight, turn + (warp - 4) * 32 * kTurn);
-          store32(a, row0, own0, c + 32, u, straight, turn + (warp - 4) * 32 * kTurn);
+          if (i == 1) release();
+#pragma unroll
+          for (int q = 0; q < 2; ++q) store(ct * 256 + half * 128 + i * 64 + q * 32, f + q * 32);
         }
       } else {
-        // gate columns half * 64 .., up columns 128 + half * 64 ..; shared: the up's of half 1 in the
-        // first accumulator, the gate's of half 0 in the second (silu is taken of the gate)
-        float h[64];
-        const int early = half ? 128 : 0, late = half ? 0 : 128;
+        float v[128];                              // the tile's sums, part after part of K
+        if constexpr (!kGated)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) tmem_ld32(acc + early + half * 64 + j * 32, *reinterpret_cast<uint32_t(*)[32]>(h + j * 32));
-        tmem_wait_ld();
-        if (shared) release();
-        float m = 0.f;
+          for (int j = 0; j < 128; ++j) v[j] = 0.f;
+        bool ok = true;
+#pragma unroll 1
+        for (int c = 0; c < parts; ++c) {
+          uint32_t acc;
+          ok = take(acc);
+          if (!ok) break;
+          if (kGated && c == 0) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          uint32_t o[32];
-          tmem_ld32(acc + late + half * 64 + j * 32, o);
-          tmem_wait_ld();
-#pragma unroll
-          for (int q = 0; q < 32; ++q) {
-            const float x = h[j * 32 + q], y = __uint_as_float(o[q]);
-            const float v = half ? silu_mul(y, x) : silu_mul(x, y);
-            h[j * 32 + q] = v;
-            m = fmaxf(m, fabsf(v));
-          }
-        }
-        row_max[half][lane_row] = m;             // a block's scale is that of both halves
-        named_barrier(1 + quarter, 64);
-        m = fmaxf(m, row_max[half ^ 1][lane_row]);
-        named_barrier(1 + quarter, 64);          // (read before the next tile's is written)
-        const int e = fp8_exponent(m);
-        const float p = fp8_pow2(-e);
-        const int c = ct * kTile + half * 64;
-        if (row >= own0) {
-          uint32_t code[16];
-#pragma unroll
-          for (int q = 0; q < 16; ++q) code[q] = fp8_codes4(h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3], p);
-          uint8_t *dst = static_cast<uint8_t *>(a.out) + (int64_t)row * a.n + c;
-          if (straight && c + 64 <= a.n) {
-            st_global_32(dst, *reinterpret_cast<uint32_t(*)[8]>(code));
-            st_global_32(dst + 32, *reinterpret_cast<uint32_t(*)[8]>(code + 8));
+            for (int q = 0; q < 4; ++q) tmem_ld32(acc + q * 32, *reinterpret_cast<uint32_t(*)[32]>(v + q * 32));
+            tmem_wait_ld();
           } else {
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-              if (c + 16 * q < a.n)              // (n is a multiple of 16)
-                *reinterpret_cast<uint4 *>(dst + 16 * q) =
-                    make_uint4(code[4 * q], code[4 * q + 1], code[4 * q + 2], code[4 * q + 3]);
+            for (int q = 0; q < 2; ++q) {
+              float t[64];
+              tmem_ld32(acc + q * 64, *reinterpret_cast<uint32_t(*)[32]>(t));
+              tmem_ld32(acc + q * 64 + 32, *reinterpret_cast<uint32_t(*)[32]>(t + 32));
+              tmem_wait_ld();
+#pragma unroll
+              for (int j = 0; j < 64; ++j) v[q * 64 + j] += t[j];
+            }
           }
-          if (half == 0) {
-            uint8_t *s = a.out_scales + (int64_t)row * a.out_sk;
-            s[ct] = (uint8_t)(e + 127);
-            if (ct == a.tiles - 1)
-              for (int b = a.tiles; b < a.out_sk; ++b) s[b] = 127;  // padding
+          release();
+        }
+        if (kGated) ok = named_barrier_and(1 + quarter, 64, ok);  // (they meet below: both go on or neither)
+        if (!ok) break;
+        if constexpr (!kGated) {
+#pragma unroll 1
+          for (int q = 0; q < 4; ++q) {
+            float u[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) u[j] = q < 2 ? (q == 0 ? v[j] : v[32 + j]) : (q == 2 ? v[64 + j] : v[96 + j]);
+            store(ct * 256 + half * 128 + q * 32, u);
+          }
+        } else {
+          float h[64], m = 0.f;
+#pragma unroll
+          for (int j = 0; j < 64; ++j) {
+            h[j] = silu_mul(v[j], v[64 + j]);
+            m = fmaxf(m, fabsf(h[j]));
+          }
+          row_max[half][lane_row] = m;             // a block's scale is that of both halves
+          named_barrier(1 + quarter, 64);
+          m = fmaxf(m, row_max[half ^ 1][lane_row]);
+          named_barrier(1 + quarter, 64);          // (read before the next tile's is written)
+          const int e = fp8_exponent(m);
+          const float p = fp8_pow2(-e);
+          const int c = ct * kTile + half * 64;
+          if (row >= own0) {
+            uint32_t code[16];
+#pragma unroll
+            for (int q = 0; q < 16; ++q) code[q] = fp8_codes4(h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3], p);
+            uint8_t *dst = static_cast<uint8_t *>(a.out) + (int64_t)row * a.n + c;
+            if (straight && c + 64 <= a.n) {
+              st_global_32(dst, *reinterpret_cast<uint32_t(*)[8]>(code));
+              st_global_32(dst + 32, *reinterpret_cast<uint32_t(*)[8]>(code + 8));
+            } else {
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+                if (c + 16 * q < a.n)              // (n is a multiple of 16)
+                  *reinterpret_cast<uint4 *>(dst + 16 * q) =
+                      make_uint4(code[4 * q], code[4 * q + 1], code[4 * q + 2], code[4 * q + 3]);
+            }
+            if (half == 0) {
+              uint8_t *s = a.out_scales + (int64_t)row * a.out_sk;
+              s[ct] = (uint8_t)(e + 127);
+              if (ct == a.tiles - 1)
+                for (int b = a.tiles; b < a.out_sk; ++b) s[b] = 127;  // padding
+            }
           }
         }
       }
@@ -803,16 +916,31 @@ cudaError_t launch_stream(const CUtensorMap &tx, ProductArgs a, int dev, cudaStr
   const int sms = device_sms();
   const int zt = (a.rows + a.nt - 1) / a.nt;
   int splits = 1;
-  while (splits < 8 && splits * 2 <= a.kbs && (int64_t)a.tiles * zt * splits <= sms) splits *= 2;
+  while (splits < kMaxSplits && splits * 2 <= a.kbs && (int64_t)a.tiles * zt * splits <= sms) splits *= 2;
   a.stage_bytes = kParts * kBlockBytes + a.nt * 128;
-  int cols = 32;
-  while (cols < kParts * a.nt + 2 * (kParts + 1) * 4) cols *= 2;
-  a.tmem_cols = cols;
-  const int per = (a.kbs + splits - 1) / splits;      // K blocks of a CTA
+  // Accumulators of at most kSumBlocks blocks, as far as the columns of three CTAs an SM go (over one wave,
+  // of two), of kSumMost in any case: with more columns, then with more splits, if that is what it takes.
+  // (Head of 128256 features of 4096 for 64 rows: 87 us with accumulators of 32 blocks, 98 with two CTAs an SM
+  // and 16, 101 with two splits and 16; 8 rows of 16384 in 32768 features: 82 with 16 of 19 columns each or
+  // with one of 128 blocks, 99 with eight splits.)
+  int per, cols;
+  for (;; splits *= 2) {
+    per = (a.kbs + splits - 1) / splits;              // K blocks of a CTA
+    const int want = (per + kSumBlocks - 1) / kSumBlocks, least = (per + kSumMost - 1) / kSumMost;
+    const bool last = splits == kMaxSplits || splits * 2 > a.kbs, waves = (int64_t)a.tiles * zt * splits > 2 * sms;
+    int room = stream_sums(kParts, a.nt, waves ? 128 : 256);
+    if (room < least) room = stream_sums(kParts, a.nt, 256);
+    if (room < least && last) room = stream_sums(kParts, a.nt, 512);
+    a.sums = std::min(want, std::max(room, 1));
+    if (a.sums >= least || last) break;
+  }
+  a.part = (per + a.sums - 1) / a.sums;
+  for (cols = 32; cols < a.sums * kParts * a.nt + stream_sf_columns(kParts);) cols *= 2;
   // A grid of one wave runs fastest with the deepest rings that leave two CTAs an SM; over several waves
   // a third CTA covers the others' beginnings and ends (head of 128256 features, 64 rows: 94 us with
   // two an SM, 85 with three; 16384 + 16384 features of 8 rows: 22.7 with either; a second projection
   // of 16384 in 4096 features: 14.1 with two, 14.8 with three).
+  a.tmem_cols = cols;
   const bool three = (int64_t)a.tiles * zt * splits > 2 * sms && 3 * cols <= 512;
   const int budget = three ? kStreamSmem3 : kStreamSmem2;
   a.stages = std::min(std::min(per, kStreamStages), (budget - stream_fixed(kParts)) / a.stage_bytes);
@@ -825,17 +953,24 @@ cudaError_t launch_stream(const CUtensorMap &tx, ProductArgs a, int dev, cudaStr
                       dim3(kStreamThreads), (size_t)smem, dim3(1, (unsigned)splits, 1), stream, tx, a);
 }
 
-template <bool kGated>
+template <bool kGated, bool kMore>
 cudaError_t launch_pair(const CUtensorMap &tx, const CUtensorMap &tw, const ProductArgs &a, int dev,
                         cudaStream_t stream) {
   static bool done[64] = {};
   static int resident[64] = {};
   const int row_tiles = (a.rows + 255) / 256, col_tiles = kGated ? a.tiles : (a.tiles + 1) / 2;
-  const cudaError_t e = allow_smem(fp8_pair_kernel<kGated>, kPairSmem, done, dev);
+  constexpr auto kKernel = fp8_pair_kernel<kGated, kMore>;
+  if (kMore && (dev < 0 || dev >= 64 || !done[dev])) {
+    cudaFuncAttributes f;
+    const cudaError_t e = cudaFuncGetAttributes(&f, kKernel);
+    if (e != cudaSuccess) return e;
+    if (f.numRegs < kLaunchRegs) return cudaErrorLaunchOutOfResources;
+  }
+  const cudaError_t e = allow_smem(kKernel, kPairSmem, done, dev);
   if (e != cudaSuccess) return e;
-  const int64_t pairs = std::min<int64_t>(resident_pairs(fp8_pair_kernel<kGated>, resident, dev), (int64_t)row_tiles * col_tiles);
-  return launch_after<fp8_pair_kernel<kGated>>(dim3((unsigned)(2 * pairs)), dim3(kPairThreads), (size_t)kPairSmem,
-                      dim3(2, 1, 1), stream, tx, tw, a, row_tiles, col_tiles);
+  const int64_t pairs = std::min<int64_t>(resident_pairs(kKernel, resident, dev), (int64_t)row_tiles * col_tiles);
+  return launch_after<kKernel>(dim3((unsigned)(2 * pairs)), dim3(kPairThreads), (size_t)kPairSmem, dim3(2, 1, 1),
+                               stream, tx, tw, a, row_tiles, col_tiles);
 }
 
 int run_product(ham_fp8_weight *w, const void *x_codes, const void *x_scales, int32_t rows, void *out,
@@ -859,7 +994,14 @@ int run_product(ham_fp8_weight *w, const void *x_codes, const void *x_scales, in
   a.f32 = f32;
   const int64_t tiles = (int64_t)((rows + 255) / 256) * (w->parts == 2 ? w->tiles : (w->tiles + 1) / 2);
   const bool pair = rows > 128 && tiles * 8 >= device_sms();
-  const int row_parts = (rows + 127) / 128;           // the streaming kernel's, of equal size
+  const int sums = (w->kbs + kSumBlocks - 1) / kSumBlocks;  // the pair kernel's, of equal size (in whole scale words)
+  a.part = ((w->kbs + sums - 1) / sums + 3) / 4 * 4;
+  // the streaming kernel's row parts, of equal size: 128 rows at most, fewer where K is so long that a CTA needs
+  // several accumulators even with every split (gated from 32768 on, plain from 98304)
+  const int blocks = (w->kbs + kMaxSplits - 1) / kMaxSplits, needs = (blocks + kSumMost - 1) / kSumMost;
+  int most = 128;
+  while (most > 16 && stream_sums(w->parts, most, 512) < needs) most -= 16;
+  const int row_parts = (rows + most - 1) / most;
   a.nt = ((rows + row_parts - 1) / row_parts + 15) / 16 * 16;
   a.box = std::min(a.nt, rows);
   CUtensorMap tx;
@@ -868,8 +1010,8 @@ int run_product(ham_fp8_weight *w, const void *x_codes, const void *x_scales, in
     rc = op_fail(HAM_ECUDA, "tensor map of the rows");
   } else {
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = pair ? (w->parts == 2 ? launch_pair<true>(tx, w->map, a, w->device, s)
-                                                : launch_pair<false>(tx, w->map, a, w->device, s))
+    const cudaError_t e = pair ? (w->parts == 2 ? launch_pair<true, true>(tx, w->map, a, w->device, s)
+                                                : a.part < a.kbs ? launch_pair<false, true>(tx, w->map, a, w->device, s) : launch_pair<false, false>(tx, w->map, a, w->device, s))
                                : (w->parts == 2 ? launch_stream<2>(tx, a, w->device, s)
                                                 : launch_stream<1>(tx, a, w->device, s));
     if (e != cudaSuccess) rc = op_fail(HAM_ECUDA, "product launch: %s", cudaGetErrorString(e));
@@ -958,7 +1100,7 @@ int ham_fp8_weight_alloc(int32_t n, int32_t k, const void *codes, const void *sc
   if (e == cudaSuccess) e = cudaMemset(w->err, 0, 4);
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
   if (e != cudaSuccess || ham::make_stretch_tensor_map(&w->map, w->codes, blocks * w->parts * ham::kBlockBytes,
-                                                       ham::kBlockBytes) != 0) {
+                                                       ham::kBlockBytes / 2) != 0) {
     cudaGetLastError();
     ham_fp8_weight_free(w);
     return op_fail(HAM_ECUDA, "weight layout: %s", cudaGetErrorString(e));

@@ -42,12 +42,15 @@ __device__ __forceinline__ void tc_mma_mx(uint32_t d_tmem, uint64_t a_desc, uint
 // the 32 rows copied to every lane quarter (of both CTAs for kCtas = 2, each from its own shared
 // memory).  In order with the products the same thread issues.
 template <int kCtas>
-__device__ __forceinline__ void tc_copy_scales(uint32_t tmem, uint32_t smem_addr) {
-  const uint64_t desc = smem_desc_plain(smem_addr, 0, 128);
+__device__ __forceinline__ void tc_copy_scales_of(uint32_t tmem, uint64_t desc) {
   if constexpr (kCtas == 1)
     asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
   else
     asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+template <int kCtas>
+__device__ __forceinline__ void tc_copy_scales(uint32_t tmem, uint32_t smem_addr) {
+  tc_copy_scales_of<kCtas>(tmem, smem_desc_plain(smem_addr, 0, 128));
 }
 
 // ---- pairs of CTAs (cta_group::2) ----------------------------------------------------------
@@ -122,6 +125,15 @@ __device__ __forceinline__ bool warp_wait_cluster(uint64_t *bar, uint32_t parity
       return false;
   }
 }
+// The same by one thread.
+__device__ __forceinline__ bool thread_wait_cluster(uint64_t *bar, uint32_t parity, volatile int *abort_flag) {
+  if (mbar_test_cluster(bar, parity)) return true;
+  const uint64_t t0 = global_timer_ns();
+#pragma unroll 1
+  for (uint32_t n = 1; !mbar_test_cluster(bar, parity); ++n)
+    if ((n & 15u) == 0 && (*abort_flag != 0 || global_timer_ns() - t0 > kWaitLimitNs)) return false;
+  return true;
+}
 // Rank-2 tiled TMA copy into this CTA's shared memory whose bytes count at a barrier of the pair's
 // first CTA (`bar`: its shared::cluster address).
 __device__ __forceinline__ void tma_load_2d_pair(void *dst, const CUtensorMap *map, int x, int y,
@@ -133,6 +145,15 @@ __device__ __forceinline__ void tma_load_2d_pair(void *dst, const CUtensorMap *m
       : "memory");
 }
 
+// Registers of this warpgroup's threads from here on (all four warps).
+template <int kRegs>
+__device__ __forceinline__ void setmaxnreg_inc() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs));
+}
+template <int kRegs>
+__device__ __forceinline__ void setmaxnreg_dec() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs));
+}
 // 32 bytes to global memory (32-byte aligned): a whole sector a thread.
 __device__ __forceinline__ void st_global_32(void *p, const uint32_t (&v)[8]) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]),
