@@ -40,6 +40,7 @@ struct ham_fp8_weight {
   uint8_t *scales = nullptr;   // [tiles][parts][sk]
   int32_t *err = nullptr;      // device error word
   int32_t *host_err = nullptr; // pinned
+  uint64_t wait_ns = ham::kWaitLimitNs;  // limit of the kernels' waits
   CUtensorMap map;             // codes as one stretch, boxes of half a block
 };
 
@@ -87,6 +88,7 @@ struct ProductArgs {
   int nt, box;             // the streaming kernel: rows of X a CTA takes (a multiple of 16), rows it loads
   int stages, stage_bytes, tmem_cols;
   int tiles;               // weight tiles
+  uint64_t wait_ns;        // limit of the waits that may be shortened (the others end with them)
   int f32;                 // fp32 output
 };
 
@@ -206,7 +208,7 @@ __global__ void __launch_bounds__(kStreamThreads)
       for (int t = 0; t < nk; ++t) {
         const int s = t % stages;
         if (t >= pre) {
-          if (!thread_wait(&empty[s], (uint32_t)(t / stages - 1) & 1u, abort_flag, true)) break;
+          if (!thread_wait(&empty[s], (uint32_t)(t / stages - 1) & 1u, abort_flag, true, a.wait_ns)) break;
           load_w(t, s);
         }
         tma_load_2d(ring + s * a.stage_bytes + kParts * kBlockBytes, &tx, (kb0 + t) * kFp8Block, x0, &full[s],
@@ -229,8 +231,8 @@ __global__ void __launch_bounds__(kStreamThreads)
       const int s = t % stages, kb = kb0 + t, g = (kb >> 2) - g0;
       const bool first = t == 0 || (kb & 3) == 0;     // a new scale word
       const uint32_t sft = sf_tmem + (uint32_t)((g & 1) * (kParts + 1) * 4);
-      if (first && !warp_wait(&sf_full[g % kStreamSf], (uint32_t)(g / kStreamSf) & 1u, abort_flag)) { ok = false; break; }
-      if (!warp_wait(&full[s], (uint32_t)(t / stages) & 1u, abort_flag)) { ok = false; break; }
+      if (first && !warp_wait(&sf_full[g % kStreamSf], (uint32_t)(g / kStreamSf) & 1u, abort_flag, a.wait_ns)) { ok = false; break; }
+      if (!warp_wait(&full[s], (uint32_t)(t / stages) & 1u, abort_flag, a.wait_ns)) { ok = false; break; }
       if (elect_one()) {
         tc_fence_after();
         if (first) {
@@ -281,7 +283,7 @@ __global__ void __launch_bounds__(kStreamThreads)
       for (int p = 0; p < kParts; ++p)
         w[p] = __ldg(reinterpret_cast<const uint32_t *>(a.ws + ((int64_t)tile * kParts + p) * a.sk) + g0 + g);
       if (g >= kStreamSf &&
-          !warp_wait(&sf_empty[slot], (uint32_t)(g / kStreamSf - 1) & 1u, abort_flag)) {
+          !warp_wait(&sf_empty[slot], (uint32_t)(g / kStreamSf - 1) & 1u, abort_flag, a.wait_ns)) {
         if (lane == 0 && !*abort_flag) {
           record_error(a.err, HAM_DEVERR_TIMEOUT);
           *abort_flag = 1;
@@ -302,7 +304,11 @@ __global__ void __launch_bounds__(kStreamThreads)
   // Accumulators -> shared memory [part][row][128 features] (the ring, free by now), then each CTA of
   // the cluster adds its share of the rows: a warp a row, a lane four features.
   __syncwarp();
-  bool ok = warp_wait(acc_full, 0u, abort_flag);
+  bool ok = warp_wait(acc_full, 0u, abort_flag);  // (ends with the others, whose limit may be shorter)
+  if (!ok && lane == 0 && !*abort_flag) {
+    record_error(a.err, HAM_DEVERR_TIMEOUT);
+    *abort_flag = 1;
+  }
   ok = ok && !__any_sync(kFull, *abort_flag != 0);
   const uint32_t tmem = *const_cast<volatile uint32_t *>(&tmem_slot);
   float *acc = reinterpret_cast<float *>(ring);
@@ -516,11 +522,11 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   uint64_t *sf_empty = sf_full + kPairSf;
   uint64_t *sum_full = sf_empty + kPairSf;     // [half][every other part of K]
   uint64_t *sum_free = sum_full + 4;           // the same: an arrival a warp of the pair that takes the half
-  uint64_t *drained = sum_free + 4;            // every product issued is complete (after an abort)
+  uint64_t *drained = sum_free + 4;            // every product issued is complete
   static_assert((2 * kPairStages + 2 * kPairSf + 9) * 8 <= 256, "barriers");
   float *turn = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(full) + 256);  // [8 warps][32][kTurn]
   __shared__ uint32_t tmem_slot;
-  __shared__ int abort_shared;
+  __shared__ int abort_shared, issued_shared;
   __shared__ float row_max[2][128];            // gated: largest magnitude of a row's half
   volatile int *abort_flag = &abort_shared;
 
@@ -532,6 +538,41 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   // a tile that would pass it begins earlier); an odd last weight tile has no second, so its own is loaded
   // twice.
   auto row_of = [&](int rt) { return min(rt * 256 + side * 128, a.rows - 128); };
+  // A wait ran out (or the pair has given up already): both CTAs stop.
+  const auto give_up = [&] {
+    if (*abort_flag) return;
+    record_error(a.err, HAM_DEVERR_TIMEOUT);
+    *abort_flag = 1;
+    st_cluster_u32(cluster_map_shared(smem_u32(&abort_shared), side ^ 1), 1u);
+  };
+  // Where tile w begins: this CTA's rows, and K block 0 of the weight's two stretches of 64 rows that it takes, one
+  // a half of the sums: plain, its half of each tile (so that a half of the sums is a tile); gated, of the gate's
+  // or the up's tile.
+  struct Source { int x, w0, w1; };
+  const auto source_of = [&](int w) {
+    constexpr int kRows = kBlockBytes / 2048;    // of a block in the map
+    const int ct = w / row_tiles;
+    Source from{row_of(w % row_tiles), 0, 0};
+    if constexpr (kGated) {
+      from.w0 = (ct * a.kbs * 2 + side) * kRows;
+      from.w1 = from.w0 + kRows / 2;
+    } else {
+      from.w0 = min(ct * 2, a.tiles - 1) * a.kbs * kRows + side * (kRows / 2);
+      from.w1 = min(ct * 2 + 1, a.tiles - 1) * a.kbs * kRows + side * (kRows / 2);
+    }
+    return from;
+  };
+  // Request a tile's K block kb for stage s; the bytes of both CTAs count at the first one's barrier.
+  const auto request = [&](int s, const Source &from, int kb) {
+    const uint64_t pol = policy_evict_last();
+    if (side == 0) mbar_arrive_tx(&full[s], 2 * kPairStageBytes);
+    const uint32_t bar = cluster_map_shared(smem_u32(&full[s]), 0);
+    uint8_t *dst = ring + s * kPairStageBytes;
+    const int down = kb * (kGated ? 2 : 1) * (kBlockBytes / 2048);
+    tma_load_2d_pair(dst, &tx, kb * kFp8Block, from.x, bar, pol);
+    tma_load_2d_pair(dst + kBlockBytes, &tw, 0, from.w0 + down, bar, pol);
+    tma_load_2d_pair(dst + kBlockBytes + kBlockBytes / 2, &tw, 0, from.w1 + down, bar, pol);
+  };
   if (tid == 0) {
     for (int s = 0; s < kPairStages; ++s) {
       mbar_init(&full[s], 1);
@@ -567,47 +608,27 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     if (warp == 0) {
       // ------------------------------------------------------------ copies
       if (lane == 0) {
-        const uint64_t pol = policy_evict_last();
         grid_dependency_wait();
         bool ok = true;
         int it = 0;
         for (int w = cluster; w < total && ok; w += clusters) {
-          const int rt = w % row_tiles, ct = w / row_tiles;
-          const int x_row = row_of(rt);
-          // K block 0 of the weight's two stretches of 64 rows that this CTA takes, one a half of the sums: plain,
-          // its half of each tile (so that a half of the sums is a tile); gated, of the gate's or the up's tile
-          int from[2];
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-            from[h] = kGated ? (int)(((int64_t)ct * a.kbs * 2 + side) * (kBlockBytes / 2048)) + h * (kBlockBytes / 4096)
-                             : (int)((int64_t)min(ct * 2 + h, a.tiles - 1) * a.kbs * (kBlockBytes / 2048)) + side * (kBlockBytes / 4096);
+          const Source from = source_of(w);
           for (int kb = 0; kb < a.kbs; ++kb, ++it) {
-            const int s = it % kPairStages;
-            if (it >= kPairStages &&
-                !thread_wait(&empty[s], (uint32_t)(it / kPairStages - 1) & 1u, abort_flag, true)) {
+            if (it >= kPairStages && !thread_wait(&empty[it % kPairStages], (uint32_t)(it / kPairStages - 1) & 1u, abort_flag,
+                                                  true, a.wait_ns)) {
               ok = false;
               break;
             }
-            if (side == 0) mbar_arrive_tx(&full[s], 2 * kPairStageBytes);  // what lands in both CTAs
-            const uint32_t bar = cluster_map_shared(smem_u32(&full[s]), 0);
-            uint8_t *dst = ring + s * kPairStageBytes;
-            tma_load_2d_pair(dst, &tx, kb * kFp8Block, x_row, bar, pol);
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-              tma_load_2d_pair(dst + kBlockBytes + h * (kBlockBytes / 2), &tw, 0,
-                               from[h] + kb * (kGated ? 2 : 1) * (kBlockBytes / 2048), bar, pol);
+            request(it % kPairStages, from, kb);
             issued = it + 1;
           }
         }
-        if (!ok && !*abort_flag) {
-          record_error(a.err, HAM_DEVERR_TIMEOUT);
-          *abort_flag = 1;
-        }
+        if (!ok) give_up();
       }
     } else if (warp == 1) {
       // ------------------------------------------------------------ products (a pair's first CTA)
       // One thread waits and issues: what it does between two blocks' products is on their way (a division a
-      // block took 4096 x 16384 x 4096 from 185 to 215 us).
+      // block took 4096 x 16384 x 4096 from 185 to 215 us, waits with a limit of their own from 173 to 184).
       if (side == 0 && elect_one()) {
         const uint64_t blocks = smem_desc_sw128(smem_u32(ring), 16, 1024), words = smem_desc_plain(smem_u32(sf), 0, 128);
         constexpr uint32_t kNextByte = idesc_mx(256, 128, 1) - idesc_mx(256, 128, 0);
@@ -672,14 +693,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             }
           }
         }
-        if (!ok) {
-          if (!*abort_flag) {
-            record_error(a.err, HAM_DEVERR_TIMEOUT);
-            *abort_flag = 1;
-          }
-          tc_commit_pair(drained, both);
-          thread_wait(drained, 0u, abort_flag, false);
-        }
+        if (!ok) give_up();
+        tc_commit_pair(drained, both);
       }
       __syncwarp();
     } else {
@@ -711,11 +726,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       if (w < total) load(w, g);
       for (int gi = turn; w < total; gi += 2) {
         const int slot = gi % kPairSf;
-        if (gi >= kPairSf && !warp_wait(&sf_empty[slot], (uint32_t)(gi / kPairSf - 1) & 1u, abort_flag)) {
-          if (lane == 0 && !*abort_flag) {
-            record_error(a.err, HAM_DEVERR_TIMEOUT);
-            *abort_flag = 1;
-          }
+        if (gi >= kPairSf && !warp_wait(&sf_empty[slot], (uint32_t)(gi / kPairSf - 1) & 1u, abort_flag, a.wait_ns)) {
+          if (lane == 0) give_up();
           break;
         }
         uint4 *dst = reinterpret_cast<uint4 *>(sf + slot * kPairSfBytes) + lane;
@@ -741,13 +753,10 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     const bool straight = (a.n * (kGated ? 1 : a.f32 ? 4 : 2) & 31) == 0 && ((uintptr_t)a.out & 31u) == 0;
     const int parts = (a.kbs + a.part - 1) / a.part;
     int n = 0, sum = half;                       // parts of K so far; the accumulator
-    // The half's next accumulator, complete (false: the wait ran out), and its release.
+    // The half's next accumulator, complete (false: the wait ran out, or another one), and its release.
     const auto take = [&](uint32_t &acc) {
       if (!warp_wait_cluster(&sum_full[half * 2 + (n & 1)], (uint32_t)(n >> 1) & 1u, abort_flag)) {
-        if (lane == 0 && !*abort_flag) {
-          record_error(a.err, HAM_DEVERR_TIMEOUT);
-          *abort_flag = 1;
-        }
+        if (lane == 0) give_up();
         return false;
       }
       tc_fence_after();
@@ -863,12 +872,25 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     tc_fence_before();
   }
   __syncwarp();
-  if (warp == 0 && lane == 0 && side == 0 && *abort_flag)
-    // after an abort the pair's copies (they count at this CTA's barriers) land before a CTA exits
-    for (int t = max(0, issued - kPairStages); t < issued; ++t)
-      thread_wait(&full[t % kPairStages], (uint32_t)(t / kPairStages) & 1u, abort_flag, false);
+  if (tid == 0) issued_shared = issued;
+  cluster_sync_all();                            // (the roles of both CTAs have ended)
+  if (warp < 2 && lane == 0) thread_wait(drained, 0u, abort_flag, false);
   __syncwarp();
-  cluster_sync_all();
+  if (*abort_flag) {
+    // Both stages of a block count at the first CTA's barrier: the CTA that has requested fewer requests what
+    // it lacks (nothing reads the stages any more), and the first waits for the last of them to land.
+    if (tid == 0) {
+      const int theirs = (int)ld_cluster_u32(cluster_map_shared(smem_u32(&issued_shared), side ^ 1));
+      for (; issued < theirs; ++issued)
+        request(issued % kPairStages, source_of(cluster + issued / a.kbs * clusters), issued % a.kbs);
+    }
+    cluster_sync_all();
+    if (tid == 0 && side == 0)
+      for (int t = max(0, issued - kPairStages); t < issued; ++t)
+        thread_wait(&full[t % kPairStages], (uint32_t)(t / kPairStages) & 1u, abort_flag, false);
+    __syncwarp();
+    cluster_sync_all();
+  }
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc_pair<512>(tmem);
@@ -992,6 +1014,7 @@ int run_product(ham_fp8_weight *w, const void *x_codes, const void *x_scales, in
   a.out_sk = fp8_scale_bytes(w->n);
   a.tiles = w->tiles;
   a.f32 = f32;
+  a.wait_ns = w->wait_ns;
   const int64_t tiles = (int64_t)((rows + 255) / 256) * (w->parts == 2 ? w->tiles : (w->tiles + 1) / 2);
   const bool pair = rows > 128 && tiles * 8 >= device_sms();
   const int sums = (w->kbs + kSumBlocks - 1) / kSumBlocks;  // the pair kernel's, of equal size (in whole scale words)
@@ -1138,6 +1161,15 @@ int ham_fp8_gated(ham_fp8_weight *w, const void *x_codes, const void *x_scales, 
       op_overlap(scales, sb, x_codes, xb) || op_overlap(scales, sb, x_scales, xsb) || op_overlap(codes, ob, scales, sb))
     return op_fail(HAM_EINVAL, "inputs and outputs must not overlap");
   return ham::run_product(w, x_codes, x_scales, rows, codes, scales, 0, stream);
+}
+
+int ham_fp8_weight_set_wait_limit_ns(ham_fp8_weight *w, uint64_t ns) {
+  if (!w) return op_fail(HAM_EINVAL, "null handle");
+  if (ns > ham::kWaitLimitNs)
+    return op_fail(HAM_EINVAL, "limit %llu ns above the default %llu", (unsigned long long)ns,
+                   (unsigned long long)ham::kWaitLimitNs);
+  w->wait_ns = ns ? ns : ham::kWaitLimitNs;
+  return HAM_OK;
 }
 
 int ham_fp8_weight_status(ham_fp8_weight *w, void *stream, int32_t *device_code) {

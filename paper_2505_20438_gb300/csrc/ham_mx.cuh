@@ -134,6 +134,14 @@ __device__ __forceinline__ bool thread_wait_cluster(uint64_t *bar, uint32_t pari
     if ((n & 15u) == 0 && (*abort_flag != 0 || global_timer_ns() - t0 > kWaitLimitNs)) return false;
   return true;
 }
+__device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ void st_cluster_u32(uint32_t a, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory");
+}
 // Rank-2 tiled TMA copy into this CTA's shared memory whose bytes count at a barrier of the pair's
 // first CTA (`bar`: its shared::cluster address).
 __device__ __forceinline__ void tma_load_2d_pair(void *dst, const CUtensorMap *map, int x, int y,

@@ -153,11 +153,6 @@ __device__ __forceinline__ float place_of(float l, const Scale &c) { return __fm
 __device__ __forceinline__ bool has_bin(float place) { return place < kLastBin; }
 __device__ __forceinline__ int part_of(float place, int bin) { return (int)((place - (float)bin) * (float)kBins); }
 
-__device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t a) {
-  uint32_t v;
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a));
-  return v;
-}
 __device__ __forceinline__ uint64_t ld_cluster_u64(uint32_t a) {
   uint64_t v;
   asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a));

@@ -109,6 +109,7 @@ _SIGNATURES = {
     "ham_fp8_linear": [_vp, _vp, _vp, _i32, _vp, _i32, _vp],
     "ham_fp8_gated": [_vp, _vp, _vp, _i32, _vp, _vp, _vp],
     "ham_fp8_weight_status": [_vp, _vp, ctypes.POINTER(_i32)],
+    "ham_fp8_weight_set_wait_limit_ns": [_vp, ctypes.c_uint64],
     "ham_sample": [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp],
 }
 _lib = None
@@ -663,6 +664,12 @@ def ham_fp8_weight_status(w: Fp8Weight, stream=None) -> int:
     if rc not in (HAM_OK, HAM_EDEVICE):
         _check(rc)
     return code.value
+
+
+def ham_fp8_weight_set_wait_limit_ns(w: Fp8Weight, ns: int):
+    """Limit of the waits of the products with this weight (0: the default 2 s); a testing aid for the failure
+    path."""
+    _check(lib().ham_fp8_weight_set_wait_limit_ns(w, int(ns)))
 
 
 def ham_sample(logits, u, tokens, temperature=None, top_k=None, top_p=None, min_p=None, probs=None,
