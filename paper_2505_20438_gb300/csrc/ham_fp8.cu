@@ -188,6 +188,7 @@ __global__ void __launch_bounds__(kStreamThreads)
     tc_fence_before();
     named_barrier(1, kStreamThreads - 32);
     tc_fence_after();
+    grid_dependency_wait();  // (bounded waits count from here: the kernel before may still have run long)
   }
   int issued = 0;
 
@@ -267,7 +268,6 @@ __global__ void __launch_bounds__(kStreamThreads)
     uint32_t w[kParts];
 #pragma unroll
     for (int p = 0; p < kParts; ++p) w[p] = 0;
-    grid_dependency_wait();
     grid_launch_dependents();
     for (int g = 0; g < ng; ++g) {
       const int slot = g % kStreamSf;
@@ -600,6 +600,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     tc_fence_before();
     named_barrier(5, kPairThreads - 32);
     tc_fence_after();
+    grid_dependency_wait();
   }
   const uint32_t tmem = *const_cast<volatile uint32_t *>(&tmem_slot);  // (not warp 0's)
   int issued = 0;
@@ -702,7 +703,6 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       // Two warps take turns at the words (of four K blocks each), and each loads its next before it
       // passes one on: the passing on, released at cluster scope, takes about as long as four K blocks'
       // products do (with one warp it set the pace: 16384 columns, 4096 x 4096, 199 us against 163).
-      grid_dependency_wait();
       if (warp == 2) grid_launch_dependents();
       const int groups = (a.kbs + 3) / 4, turn = warp - 2;
       uint32_t x[4], ws[2];

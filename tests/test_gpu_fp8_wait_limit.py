@@ -56,3 +56,30 @@ def test_wait_limit_above_the_default_is_rejected():
     with pytest.raises(ham.HamError, match="above the default") as e:
         ham.ham_fp8_weight_set_wait_limit_ns(w, 3_000_000_000)
     assert e.value.status == ham.HAM_EINVAL
+
+
+def test_the_call_before_does_not_count():
+    """A product's CTAs may start while the call before still runs (a sampling lets them at its beginning, and its
+    256 CTAs leave room on some SMs): its waits begin when that call has ended."""
+    import torch
+    rng = np.random.default_rng(1)
+    x = [dev(a) for a in random_codes(rng, 8, 4096)]
+    w = alloc_weight(512, 4096, random_codes(rng, 512, 4096, True))
+    y = torch.empty(8, 512, device="cuda")
+    logits = torch.randn((256, 128256), device="cuda")
+    u, p = torch.rand(256, device="cuda"), torch.full((256,), 0.9, device="cuda")
+    tokens = torch.empty(256, dtype=torch.int32, device="cuda")
+
+    def calls():
+        ham.ham_sample(logits, u, tokens, top_p=p)      # some 90 us
+        ham.ham_fp8_linear(w, *x, y)                    # some 6
+    calls()
+    torch.cuda.synchronize()
+    want = y.clone()
+    ham.ham_fp8_weight_set_wait_limit_ns(w, 25_000)
+    torch.cuda._sleep(2_000_000)
+    for _ in range(10):
+        calls()
+    torch.cuda.synchronize()
+    assert ham.ham_fp8_weight_status(w) == ham.HAM_DEVERR_NONE
+    assert torch.equal(y, want)
