@@ -1737,6 +1737,7 @@ cudaError_t launch_sample(SampleArgs a, int rows, cudaStream_t stream) {
 
 using ham::op_aligned;
 using ham::op_fail;
+using ham::op_overlap;
 
 extern "C" int ham_sample(const void *logits, int32_t logits_dtype, int32_t rows, int32_t vocab, const float *u,
                           const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
@@ -1754,6 +1755,14 @@ extern "C" int ham_sample(const void *logits, int32_t logits_dtype, int32_t rows
   for (const void *p : {(const void *)u, (const void *)temperature, (const void *)top_k, (const void *)top_p,
                         (const void *)min_p, (const void *)tokens, (const void *)probs})
     if (!op_aligned(p, 4)) return op_fail(HAM_EINVAL, "the per-row arrays must be 4-byte aligned");
+  const size_t each = 4 * (size_t)rows, all = (size_t)rows * vocab * (logits_dtype == HAM_DTYPE_F32 ? 4 : 2);
+  for (const void *out : {(const void *)tokens, (const void *)probs}) {
+    for (const void *in : {(const void *)u, (const void *)temperature, (const void *)top_k, (const void *)top_p,
+                           (const void *)min_p})
+      if (op_overlap(out, each, in, each)) return op_fail(HAM_EINVAL, "an output overlaps an input");
+    if (op_overlap(out, each, logits, all)) return op_fail(HAM_EINVAL, "an output overlaps an input");
+  }
+  if (op_overlap(tokens, each, probs, each)) return op_fail(HAM_EINVAL, "two outputs overlap");
   ham::SampleArgs a;
   a.logits = logits;
   a.u = u;
