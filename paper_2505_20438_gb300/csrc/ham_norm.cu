@@ -72,6 +72,19 @@ __device__ __forceinline__ uint2 encode8(const float (&y)[8], uint32_t &scale) {
   return make_uint2(fp8_codes4(y[0], y[1], y[2], y[3], p), fp8_codes4(y[4], y[5], y[6], y[7], p));
 }
 
+// A number's sum over the block; `part`: its warps' sums.
+__device__ __forceinline__ float block_sum(float s, float *part) {
+  const int tid = threadIdx.x;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
+  if ((tid & 31) == 0) part[tid >> 5] = s;
+  __syncthreads();
+  s = (tid & 31) < (blockDim.x >> 5) ? part[tid & 31] : 0.f;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
+  return s;
+}
+
 // A block is one row, a thread the groups tid, tid + threads, ... of 8 elements.  Many rows are bound by
 // memory (16384 rows of 4096, residual in, sum and 8-bit rows out: 67.7 us, 6.9 TB/s counted at the bytes
 // of the operands), few by the chain of launch, reads and the row's sum (8 rows: 1.65 us).
@@ -119,14 +132,23 @@ __global__ void __launch_bounds__(kGroups >= 4 ? 1024 : 512) add_norm_kernel(Nor
     const int v = tid + g * threads;
     vw[g] = v < a.vecs ? __ldg(a.w + v) : make_uint4(0, 0, 0, 0);
   }
+  float mean = block_sum(s, part) / (float)a.hidden + a.eps;
+  // Where the squares leave fp32's range (elements from some 1e18 on; a row below 1e-15 with next to no eps) they
+  // are summed again, and the row normed, in another unit, a power of two.
+  if (__builtin_expect(!(mean >= 0x1p-100f && mean <= 0x1p126f), 0)) {
+    const float unit = mean < 1.f ? 0x1p80f : 0x1p-80f;
+    s = 0.f;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
-  if ((tid & 31) == 0) part[tid >> 5] = s;
-  __syncthreads();
-  s = (tid & 31) < (threads >> 5) ? part[tid & 31] : 0.f;
+    for (int g = 0; g < kGroups; ++g)
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
-  const float inv = rsqrtf(s / (float)a.hidden + a.eps);
+      for (int i = 0; i < 8; ++i) {
+        h[g][i] *= unit;
+        s = fmaf(h[g][i], h[g][i], s);
+      }
+    __syncthreads();                             // (the sums are read)
+    mean = block_sum(s, part) / (float)a.hidden + a.eps * unit * unit;
+  }
+  const float inv = rsqrtf(mean);
 #pragma unroll
   for (int g = 0; g < kGroups; ++g) {
     const int v = tid + g * threads;
