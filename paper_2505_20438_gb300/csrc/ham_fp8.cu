@@ -937,8 +937,11 @@ cudaError_t launch_stream(const CUtensorMap &tx, ProductArgs a, int dev, cudaStr
   static bool done[64] = {};
   const int sms = device_sms();
   const int zt = (a.rows + a.nt - 1) / a.nt;
+  // K is cut over a cluster until there are more CTAs than SMs, at least two blocks each.  (8 rows, us with 1, 2, 4, 8
+  // CTAs a tile: K 4096 with 8 tiles 16.4, 10.2, 6.8, 5.6, 32 tiles 16.9, 10.5, 7.9, 7.6, 64 tiles 16.9, 11.8, 9.8, 14.1,
+  // 128 tiles 18.2, 14.5, 19.1, 22.4, 192 tiles 20.3, 19.2, 23.6, 31.6; 32 tiles with K 1024 5.9, 4.9, 4.6, 5.6.)
   int splits = 1;
-  while (splits < kMaxSplits && splits * 2 <= a.kbs && (int64_t)a.tiles * zt * splits <= sms) splits *= 2;
+  while (splits < kMaxSplits && splits * 4 <= a.kbs && (int64_t)a.tiles * zt * splits <= sms) splits *= 2;
   a.stage_bytes = kParts * kBlockBytes + a.nt * 128;
   // Accumulators of at most kSumBlocks blocks, as far as the columns of three CTAs an SM go (over one wave,
   // of two), of kSumMost in any case: with more columns, then with more splits, if that is what it takes.
@@ -949,7 +952,7 @@ cudaError_t launch_stream(const CUtensorMap &tx, ProductArgs a, int dev, cudaStr
   for (;; splits *= 2) {
     per = (a.kbs + splits - 1) / splits;              // K blocks of a CTA
     const int want = (per + kSumBlocks - 1) / kSumBlocks, least = (per + kSumMost - 1) / kSumMost;
-    const bool last = splits == kMaxSplits || splits * 2 > a.kbs, waves = (int64_t)a.tiles * zt * splits > 2 * sms;
+    const bool last = splits == kMaxSplits || splits * 4 > a.kbs, waves = (int64_t)a.tiles * zt * splits > 2 * sms;
     int room = stream_sums(kParts, a.nt, waves ? 128 : 256);
     if (room < least) room = stream_sums(kParts, a.nt, 256);
     if (room < least && last) room = stream_sums(kParts, a.nt, 512);
@@ -959,9 +962,9 @@ cudaError_t launch_stream(const CUtensorMap &tx, ProductArgs a, int dev, cudaStr
   a.part = (per + a.sums - 1) / a.sums;
   for (cols = 32; cols < a.sums * kParts * a.nt + stream_sf_columns(kParts);) cols *= 2;
   // A grid of one wave runs fastest with the deepest rings that leave two CTAs an SM; over several waves
-  // a third CTA covers the others' beginnings and ends (head of 128256 features, 64 rows: 94 us with
-  // two an SM, 85 with three; 16384 + 16384 features of 8 rows: 22.7 with either; a second projection
-  // of 16384 in 4096 features: 14.1 with two, 14.8 with three).
+  // a third CTA covers the others' beginnings and ends (head of 128256 features, 64 rows: 96 us with
+  // two an SM, 85 with three; 40960 features of 8 rows: 40 and 28; 28672 + 28672 features of 8 rows: 38.3 with either;
+  // a second projection of 16384 in 4096 features: 14.1 with two, 14.8 with three).
   a.tmem_cols = cols;
   const bool three = (int64_t)a.tiles * zt * splits > 2 * sms && 3 * cols <= 512;
   const int budget = three ? kStreamSmem3 : kStreamSmem2;
@@ -1016,7 +1019,13 @@ int run_product(ham_fp8_weight *w, const void *x_codes, const void *x_scales, in
   a.f32 = f32;
   a.wait_ns = w->wait_ns;
   const int64_t tiles = (int64_t)((rows + 255) / 256) * (w->parts == 2 ? w->tiles : (w->tiles + 1) / 2);
-  const bool pair = rows > 128 && tiles * 8 >= device_sms();
+  // The pair kernel where its tiles (of 256 x 256; a tile takes 43 us at K 16384, whoever else is idle) occupy an
+  // eighth of the SMs, gated ones a sixteenth.  Stream / pair kernel, us: 16 tiles (512 x 2048) 8.6 / 6.4 at K 512,
+  // 10.4 / 10.1 at 2048, 12.8 / 15.7 at 4096, 25.5 / 43 at 16384; 21 tiles (768 x 1792) 7.9 / 6.7, 11.1 / 10.4,
+  // 15.6 / 15.7, 45 / 43; 64 tiles (300 x 8192) 8.0 / 7.2, 14.5 / 11.7, 23 / 17, 76 / 54.  Gated, whose stream kernel
+  // fills an SM's tensor memory with 128 rows: 8 tiles (129 x 1024) 9.5 / 10.0 at K 1024, 12.3 / 16.6 at 4096; 12 tiles
+  // (640 x 512) 19 / 10, 24 / 17, 39 / 45 at 16384; 16 tiles (256 x 2048) 29 / 10, 36 / 18, 59 / 46.
+  const bool pair = rows > 128 && tiles * (w->parts == 2 ? 16 : 8) >= device_sms();
   const int sums = (w->kbs + kSumBlocks - 1) / kSumBlocks;  // the pair kernel's, of equal size (in whole scale words)
   a.part = ((w->kbs + sums - 1) / sums + 3) / 4 * 4;
   // the streaming kernel's row parts, of equal size: 128 rows at most, fewer where K is so long that a CTA needs

@@ -75,6 +75,7 @@ struct SampleArgs {
 
 // Weights are added in two halves (weight = high 2^16 + low): at most 2^16 tokens of a CTA keep each
 // half's sum within 32 bits.
+constexpr int kSliceMost = 1 << 16;
 struct __align__(16) Histogram { uint32_t count[kBins], low[kBins], high[kBins]; };
 
 // Groups of a row that one CTA reads by itself: a vector a lane of a warp.  (The row's first vector may
@@ -1507,7 +1508,10 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_alone_kernel(SampleA
   const float p = a.top_p ? a.top_p[row] : 1.f;
   const float min_p = a.min_p ? a.min_p[row] : 0.f;
   const bool greedy = !(temperature > 0.f), by_k = k > 0 && k < a.vocab, by_p = p < 1.f;
-  const bool fine = !greedy && (by_k ? 4 * (int64_t)k > groups : by_p);
+  // Top-k by the groups' largest logits or by the finer counts: 256 rows of 128256 fp32 logits (1002 groups), k = 50 34 /
+  // 42 us, 250 47 / 52, 400 54 / 58, 600 63 / 62, 1000 132 / 69 (the list too long); in bf16 (501 groups), k = 200 39 / 46,
+  // 400 50 / 54, 500 98 / 56.
+  const bool fine = !greedy && (by_k ? 2 * (int64_t)k > groups : by_p);
   const float fine_bins = fine ? __fdiv_rn(kFinePerX, scale_of(0.f, temperature).t) : 0.f;
   uint32_t *const fine_counts = reinterpret_cast<uint32_t *>(w.h) + warp % kFineCopies * kFineBins;
   __syncthreads();
@@ -1705,15 +1709,19 @@ cudaError_t launch_sample(SampleArgs a, int rows, cudaStream_t stream) {
   static bool done[64] = {};
   int dev = 0;
   cudaGetDevice(&dev);
-  // the fewest CTAs a row that leave room for two on an SM; more while all rows' CTAs
-  // still find room at once
-  int ctas = 1;
+  // As many CTAs a row as find an SM each at once (of more than 1024 logits); where there are none that hold the
+  // row, the fewest that leave room for two on an SM.  (us with 1, 2, 4, 8 CTAs a row: 8 x 32000 fp32, k 50, 11.3,
+  // 10.5, 9.4, 9.3; 24 x 50001 fp32, p 0.9, -, 21.9, 18.9, 23.8; 40 x 50001 bf16, p 0.9 and flat, -, 27.0, 30.8, 42.2;
+  // 76 x 32000 fp32, no cut, 9.4, 8.3, 12.7, 13.9; 100 x 32000 bf16, p 0.9, 22.4, 25.6, 33.0, 30.9; 20 x 128256 fp32, p
+  // 0.9, four 24.6, eight 28.2.)
   auto bytes = [&](int c) {
     return ((a.vocab + c - 1) / c + 7) / 8 * 8 * (int)sizeof(T) + 32 + kSampleFixed;
   };
-  while (ctas < kMaxCluster && (bytes(ctas) > kSampleSmem2 ||
-                                ((int64_t)rows * ctas <= device_sms() && a.vocab > 2048 * ctas)))
-    ctas *= 2;
+  const int sms = device_sms();
+  int ctas = kMaxCluster;
+  while (ctas > 1 && ((int64_t)rows * ctas > sms || a.vocab <= 1024 * ctas)) ctas /= 2;
+  if (rows * ctas > sms || bytes(ctas) > kSampleSmem || a.vocab > kSliceMost * ctas)
+    for (ctas = 1; ctas < kMaxCluster && bytes(ctas) > kSampleSmem2;) ctas *= 2;
   a.slice = ((a.vocab + ctas - 1) / ctas + 7) / 8 * 8;
   if (dev < 0 || dev >= 64 || !done[dev]) {
     cudaError_t e = cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSampleSmem);
@@ -1725,8 +1733,10 @@ cudaError_t launch_sample(SampleArgs a, int rows, cudaStream_t stream) {
   // A CTA a row where the clusters' CTAs would take turns: from one and a half times what the SMs hold at
   // once.  (fp32 rows of 128256: at 48, 384 CTAs, clusters / alone took 17 / 29 us without cuts, 26 / 20
   // with k = 50, 45 / 54 with p = 0.9; at 96 they took 31 / 32, 44 / 23 and 79 / 57.  A row that one CTA
-  // holds waits for no other, and is read once: 1000 rows of 32000 in bf16, 40 / 53, 58 / 61, 105 / 115.)
-  if (ctas > 1 && rows * ctas > 3 * device_sms())
+  // holds waits for no other, and is read once: 1000 rows of 32000 in bf16, 40 / 53, 58 / 61, 105 / 115.  Rows of 50001
+  // in fp32 and bf16: at 80, 160 CTAs, 15 / 18 and 13 / 21, 22 / 16 and 17 / 18, 35 / 34 and 34 / 37; at 160, 320 CTAs, 23 /
+  // 25 and 18 / 24, 33 / 19 and 27 / 22, 52 / 47 and 49 / 47.)
+  if (ctas > 1 && rows * ctas > 3 * sms)
     return launch_after<sample_alone_kernel<T>>(dim3((unsigned)rows), dim3(kSampleThreads), (size_t)kAloneSmem, dim3(1), stream, a);
   return launch_after<sample_kernel<T>>(dim3((unsigned)ctas, (unsigned)rows), dim3(kSampleThreads),
                       (size_t)bytes(ctas), dim3((unsigned)ctas), stream, a);
