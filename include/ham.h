@@ -505,7 +505,8 @@ int ham_embed_tokens(ham_embedder *e, const int32_t *ids, const int32_t *offsets
 /* Residual addition and root-mean-square norm:
  *   h = x + residual,  y = h / sqrt(mean_k(h_k^2) + eps) * weight
  *   sum_out = bf16(h),  out = bf16(y),  codes and scales = the 8-bit row of y
- * in fp32 from the bf16 inputs (the norm takes the unrounded h), each output rounded once.
+ * in fp32 from the bf16 inputs (the norm takes the unrounded h), each output rounded once.  (Squares that
+ * leave fp32's range are summed in another unit: rows of any finite size are normed.)
  * x, residual (nullable: 0)  device bf16 [rows][hidden];  weight  device bf16 [hidden]
  * sum_out, out (nullable)    device bf16 [rows][hidden]; each may be x or residual itself
  * codes, scales (nullable, together)  an 8-bit output as above; out or codes is required
@@ -523,7 +524,9 @@ int ham_fp8_encode_weight(const void *w, int32_t n, int32_t k, void *codes, void
 typedef struct ham_fp8_weight ham_fp8_weight; /* opaque handle: a weight laid out for the products */
 
 /* Copy a weight (device codes [n][k] and scales, as above) into the products' layout, on the current
- * CUDA device (synchronous; the caller may free its copy).  With codes_up and scales_up the handle is
+ * CUDA device (synchronous; the caller may free its copy).  It reads them on the legacy default stream: what
+ * wrote them on a stream that does not wait for that one must have ended.  n at most 2^22, k a multiple of 16 and
+ * at most 2^20.  With codes_up and scales_up the handle is
  * a gated weight for ham_fp8_gated: codes the gate's projection, codes_up the up projection, both
  * [n][k], n a multiple of 16.  Host errors: HAM_EINVAL, HAM_EUNSUPPORTED (the padded size passes
  * 2^31 rows of 128), HAM_ENOMEM, HAM_ECUDA; *out is NULL on failure. */
@@ -544,7 +547,8 @@ int ham_fp8_linear(ham_fp8_weight *w, const void *x_codes, const void *x_scales,
 
 /* The first half of a gated feed-forward block, one kernel: G = X W_gate^T, U = X W_up^T (fp32),
  * H = G / (1 + exp(-G)) * U, encoded as 8-bit rows (codes [rows][n], scales), the input of the second
- * projection.  Host errors: HAM_EINVAL (also for a weight without an up part), HAM_ECUDA. */
+ * projection.  rows at most 2^24; the sums as ham_fp8_linear's.  Host errors: HAM_EINVAL (also for a weight
+ * without an up part), HAM_ECUDA. */
 int ham_fp8_gated(ham_fp8_weight *w, const void *x_codes, const void *x_scales, int32_t rows, void *codes,
                   void *scales, void *stream);
 
@@ -561,22 +565,25 @@ int ham_fp8_weight_set_wait_limit_ns(ham_fp8_weight *w, uint64_t ns);
 
 /* One token for each row of logits, from a given random number.  For a row l with settings T, k, p, m
  * and the random number u:
- *   w_i = trunc(2^31 exp((l_i - max l) / T)), x = (l_i - max l) / T in fp32 (0 where l_i = max l)
+ *   w_i = trunc(2^31 exp(x_i)), x_i = (l_i - max l) / T in fp32 (0 where l_i = max l), exp in fp32 as
+ *   CUDA's expf gives it (within two units of its last place)
  *   tokens are ordered by l, largest first, equal ones by index; kept are the first k of them (top-k),
  *   of these the shortest prefix whose weights reach p times the weights of the k (top-p), of these
  *   the ones with w_i >= m 2^31 (min-p: m times the likeliest token's weight)
  *   token = the first index, in index order, at which the running sum of the kept weights exceeds
  *   floor(u S), S their whole sum;  prob = w_token / S
- * The weights are whole numbers and their sums exact, so the token does not depend on batch, launch
- * shape or the order of additions.  T <= 0 (or NaN) takes the largest logit, ties to the lowest index.
+ * The weights are whole numbers and their sums exact: with these weights the token is the formula's, and it
+ * does not depend on batch, launch shape or the order of additions.  T <= 0 (or NaN) takes the largest logit, ties to the lowest index.
  * (A positive T is taken within 2^-60 .. 2^60.)
  * k <= 0 or k >= vocab, p >= 1 and m <= 0 keep all; the likeliest token is always kept.  A NaN logit
  * counts as -inf (ruled out); a row with nothing but those gives token -1 and prob 0.
- * logits       device [rows][vocab], bf16 or f32 (logits_dtype), 16-byte aligned; vocab at most 2^18
+ * logits       device [rows][vocab], bf16 or f32 (logits_dtype), 16-byte aligned; vocab at most 2^18, rows at
+ *              most 65535
  * u            device f32 [rows], in [0, 1)
  * temperature, top_p, min_p  nullable device f32 [rows];  top_k  nullable device int32 [rows]
  *              (NULL: temperature 1, the others off)
  * tokens       device int32 [rows];  probs  nullable device f32 [rows]
+ * Outputs must not overlap inputs or each other.
  * Host errors: HAM_EINVAL, HAM_EUNSUPPORTED (vocab above 2^18), HAM_ECUDA. */
 int ham_sample(const void *logits, int32_t logits_dtype, int32_t rows, int32_t vocab, const float *u,
                const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,

@@ -1038,7 +1038,7 @@ int run_product(ham_fp8_weight *w, const void *x_codes, const void *x_scales, in
   a.box = std::min(a.nt, rows);
   CUtensorMap tx;
   int rc = HAM_OK;
-  if (make_bytes_tensor_map(&tx, x_codes, rows, w->k, kFp8Block, pair ? 128 : a.box, true) != 0) {
+  if (make_bytes_tensor_map(&tx, x_codes, rows, w->k, kFp8Block, pair ? 128 : a.box) != 0) {
     rc = op_fail(HAM_ECUDA, "tensor map of the rows");
   } else {
     cudaStream_t s = static_cast<cudaStream_t>(stream);

@@ -48,10 +48,10 @@ inline bool op_overlap(const void *a, size_t na, const void *b, size_t nb) {
 int device_sms();
 
 // TMA map of a row-major [rows][cols] matrix of bytes (cols a multiple of 16) with a box of
-// {box_cols, box_rows}, with the 128-byte swizzle or none; boxes past the end read zeros.
+// {box_cols, box_rows}, with the 128-byte swizzle; boxes past the end read zeros.
 // Returns a CUresult.
 int make_bytes_tensor_map(CUtensorMap *map, const void *base, int64_t rows, int64_t cols,
-                          int box_cols, int box_rows, bool swizzle);
+                          int box_cols, int box_rows);
 
 // TMA map of a stretch of `bytes` of memory (a multiple of 2048) as rows of 2048 bytes, with a box of
 // box_bytes of them one after the other; boxes past the end read zeros.  Returns a CUresult.

@@ -480,7 +480,7 @@ int make_fp8_v_tensor_map(CUtensorMap *map, const void *v_codes, int64_t rows_d,
 }
 
 int make_bytes_tensor_map(CUtensorMap *map, const void *base, int64_t rows, int64_t cols,
-                          int box_cols, int box_rows, bool swizzle) {
+                          int box_cols, int box_rows) {
   EncodeTiled encode = tensor_map_encoder();
   if (!encode) return -1;
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
@@ -489,8 +489,8 @@ int make_bytes_tensor_map(CUtensorMap *map, const void *base, int64_t rows, int6
   const cuuint32_t estride[2] = {1, 1};
   return (int)encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims,
                      strides, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                     swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
-                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                     CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
 int make_stretch_tensor_map(CUtensorMap *map, const void *base, int64_t bytes, int box_bytes) {
