@@ -556,8 +556,8 @@ int ham_fp8_gated(ham_fp8_weight *w, const void *x_codes, const void *x_scales, 
  * synchronizes `stream`).  Returns HAM_EDEVICE if it was set, with the code in *device_code. */
 int ham_fp8_weight_status(ham_fp8_weight *w, void *stream, int32_t *device_code);
 
-/* Limit, in nanoseconds, of the products' waits for stages and scale words to be freed and, with few rows,
- * to be filled; it counts from the end of the call before.  0 restores the default, 2 s (the largest value accepted).  A wait that runs out records
+/* Limit, in nanoseconds, of the products' waits for scale words to be freed and, with few rows, for stages to
+ * be freed and filled; it counts from the end of the call before.  0 restores the default, 2 s (the largest value accepted).  A wait that runs out records
  * HAM_DEVERR_TIMEOUT (read by ham_fp8_weight_status), ends the kernel's other waits and leaves that call's
  * output undefined; the kernel still waits for the copies and products it started before it ends.  A testing
  * aid, as ham_kv_set_wait_limit_ns is.  Host errors: HAM_EINVAL. */

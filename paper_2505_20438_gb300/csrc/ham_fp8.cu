@@ -563,8 +563,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     return from;
   };
   // Request a tile's K block kb for stage s; the bytes of both CTAs count at the first one's barrier.
-  const auto request = [&](int s, const Source &from, int kb) {
-    const uint64_t pol = policy_evict_last();
+  const auto request = [&](int s, const Source &from, int kb, uint64_t pol) {
     if (side == 0) mbar_arrive_tx(&full[s], 2 * kPairStageBytes);
     const uint32_t bar = cluster_map_shared(smem_u32(&full[s]), 0);
     uint8_t *dst = ring + s * kPairStageBytes;
@@ -609,18 +608,19 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     if (warp == 0) {
       // ------------------------------------------------------------ copies
       if (lane == 0) {
+        const uint64_t pol = policy_evict_last();
         grid_dependency_wait();
         bool ok = true;
         int it = 0;
         for (int w = cluster; w < total && ok; w += clusters) {
           const Source from = source_of(w);
           for (int kb = 0; kb < a.kbs; ++kb, ++it) {
-            if (it >= kPairStages && !thread_wait(&empty[it % kPairStages], (uint32_t)(it / kPairStages - 1) & 1u, abort_flag,
-                                                  true, a.wait_ns)) {
+            if (it >= kPairStages &&
+                !thread_wait(&empty[it % kPairStages], (uint32_t)(it / kPairStages - 1) & 1u, abort_flag, true)) {
               ok = false;
               break;
             }
-            request(it % kPairStages, from, kb);
+            request(it % kPairStages, from, kb, pol);
             issued = it + 1;
           }
         }
@@ -629,7 +629,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     } else if (warp == 1) {
       // ------------------------------------------------------------ products (a pair's first CTA)
       // One thread waits and issues: what it does between two blocks' products is on their way (a division a
-      // block took 4096 x 16384 x 4096 from 185 to 215 us, waits with a limit of their own from 173 to 184).
+      // block took 4096 x 16384 x 4096 from 185 to 215 us, waits with a limit of their own from 173 to 184, and
+      // those of the copies from 170 to 175).
       if (side == 0 && elect_one()) {
         const uint64_t blocks = smem_desc_sw128(smem_u32(ring), 16, 1024), words = smem_desc_plain(smem_u32(sf), 0, 128);
         constexpr uint32_t kNextByte = idesc_mx(256, 128, 1) - idesc_mx(256, 128, 0);
@@ -882,7 +883,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     if (tid == 0) {
       const int theirs = (int)ld_cluster_u32(cluster_map_shared(smem_u32(&issued_shared), side ^ 1));
       for (; issued < theirs; ++issued)
-        request(issued % kPairStages, source_of(cluster + issued / a.kbs * clusters), issued % a.kbs);
+        request(issued % kPairStages, source_of(cluster + issued / a.kbs * clusters), issued % a.kbs, policy_evict_last());
     }
     cluster_sync_all();
     if (tid == 0 && side == 0)

@@ -2,9 +2,9 @@
 keeps working afterwards.
 
 The waits are made to run out on a healthy GPU by shortening their limit to a nanosecond
-(ham_fp8_weight_set_wait_limit_ns): every CTA has more blocks of K than stages, and the first stage is not
-free again by the first poll, so it gives up, with copies and products on their way.  The kernel waits for
-those, frees its tensor memory and ends.  No fault, trap or endless loop is involved.
+(ham_fp8_weight_set_wait_limit_ns): every CTA has more blocks of K than stages or scale words, and finds one
+that is not free again by the first poll, so it gives up, with copies and products on their way.  The kernel
+waits for those, frees its tensor memory and ends.  No fault, trap or endless loop is involved.
 """
 import numpy as np
 import pytest
@@ -16,8 +16,8 @@ pytestmark = pytest.mark.gpu
 
 
 # the stream kernel's CTAs alone and in clusters that share K; the pair kernel with one part of K and with several
-@pytest.mark.parametrize("t,k,n", [(8, 4096, 40000), (8, 16400, 136), (200, 2064, 300), (2304, 1280, 2304),
-                                   (2304, 4112, 2304), (5000, 1280, 4096)])
+@pytest.mark.parametrize("t,k,n", [(8, 4096, 40000), (8, 16400, 136), (200, 2064, 300), (5900, 1280, 4096),
+                                   (2304, 16400, 2304), (2304, 8208, 4000)])
 @pytest.mark.parametrize("gated", [False, True])
 def test_a_wait_runs_out_and_the_weight_recovers(t, k, n, gated):
     import torch
