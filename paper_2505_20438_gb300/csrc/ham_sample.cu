@@ -1712,15 +1712,20 @@ cudaError_t launch_sample(SampleArgs a, int rows, cudaStream_t stream) {
   // As many CTAs a row as find an SM each at once (of more than 1024 logits); where there are none that hold the
   // row, the fewest that leave room for two on an SM.  (us with 1, 2, 4, 8 CTAs a row: 8 x 32000 fp32, k 50, 11.3,
   // 10.5, 9.4, 9.3; 24 x 50001 fp32, p 0.9, -, 21.9, 18.9, 23.8; 40 x 50001 bf16, p 0.9 and flat, -, 27.0, 30.8, 42.2;
-  // 76 x 32000 fp32, no cut, 9.4, 8.3, 12.7, 13.9; 100 x 32000 bf16, p 0.9, 22.4, 25.6, 33.0, 30.9; 20 x 128256 fp32, p
-  // 0.9, four 24.6, eight 28.2.)
+  // 76 x 32000 fp32, no cut, 9.4, 8.3, 12.7, 13.9; 100 x 32000 bf16, p 0.9, 22.4, 25.6, 33.0, 30.9; 32 x 128256 fp32, p
+  // 0.9, four 25.3, eight 29.0; 38 rows, four 46.1, eight 42.3.)
   auto bytes = [&](int c) {
     return ((a.vocab + c - 1) / c + 7) / 8 * 8 * (int)sizeof(T) + 32 + kSampleFixed;
   };
   const int sms = device_sms();
+  // (With a CTA an SM, clusters of four or eight find fewer places than there are SMs: a cluster lies within one group
+  // of them.)
+  const auto at_once = [&](int c) {
+    return c <= 2 || bytes(c) <= kSampleSmem2 ? (int64_t)rows * c <= sms : (int64_t)rows * c * 16 <= sms * 15;
+  };
   int ctas = kMaxCluster;
-  while (ctas > 1 && ((int64_t)rows * ctas > sms || a.vocab <= 1024 * ctas)) ctas /= 2;
-  if (rows * ctas > sms || bytes(ctas) > kSampleSmem || a.vocab > kSliceMost * ctas)
+  while (ctas > 1 && (!at_once(ctas) || a.vocab <= 1024 * ctas)) ctas /= 2;
+  if (!at_once(ctas) || bytes(ctas) > kSampleSmem || a.vocab > kSliceMost * ctas)
     for (ctas = 1; ctas < kMaxCluster && bytes(ctas) > kSampleSmem2;) ctas *= 2;
   a.slice = ((a.vocab + ctas - 1) / ctas + 7) / 8 * 8;
   if (dev < 0 || dev >= 64 || !done[dev]) {
