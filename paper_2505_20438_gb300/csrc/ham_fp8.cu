@@ -15,8 +15,9 @@
 // zero, so that one accumulator's error is a bias that grows with K: measured against 64-bit sums, relative to
 // the outputs' norm, 5.9e-8 at K 1024, 1.1e-7 at 2048, 2.3e-7 at 4096, 1.3e-6 at 16384 (a plain fp32 product:
 // 4.1e-8, 5.9e-8, 8.6e-8, 2.0e-7).  So an accumulator takes kSumBlocks blocks of K, 2048 terms (kSumMost where
-// more accumulators would cost the streaming kernel a CTA an SM), and the parts are added in fp32, in order:
-// 1.1 to 1.2e-7 at every K from 2048 on (2.4e-7).
+// more accumulators would cost the streaming kernel a CTA an SM; kSumNext after the pair kernel's first), and the
+// parts are added in fp32, in order: 0.9 to 1.1e-7 at every K from 2048 on with the pair kernel, 1.1 to 1.4e-7 with the
+// streaming one (2.4e-7).
 //
 // Weights are laid out once (ham_fp8_weight_alloc) as [tile of 128 rows][K block][128 x 128], each
 // block 16 KiB in the shared-memory layout of the 128-byte swizzle, so that a weight tile's K range is
@@ -48,7 +49,7 @@ namespace ham {
 namespace {
 
 constexpr int kTile = 128;             // weight rows of a tile
-constexpr int kSumBlocks = 16, kSumMost = 32;  // K blocks of one accumulator
+constexpr int kSumBlocks = 16, kSumNext = 8, kSumMost = 32;  // K blocks of one accumulator
 constexpr int kBlockBytes = 128 * 128; // a tile's K block
 
 // One thread per 16-byte piece of the laid-out weight.
@@ -83,7 +84,7 @@ struct ProductArgs {
   uint8_t *out_scales;     // gated: [rows][out_sk]
   int32_t *err;
   int rows, n, kbs, sk, out_sk;
-  int part;                // K blocks that one accumulator takes
+  int part, first_part;    // K blocks that one accumulator takes; of the pair kernel's first one in a tile
   int sums;                // the streaming kernel: accumulators
   int nt, box;             // the streaming kernel: rows of X a CTA takes (a multiple of 16), rows it loads
   int stages, stage_bytes, tmem_cols;
@@ -394,7 +395,9 @@ __global__ void __launch_bounds__(kStreamThreads)
 // ends in the second, the first of the next part has an accumulator of its own at once, and the second takes
 // the one that the epilogue has emptied meanwhile.  With one accumulator of 256 columns, two of which share
 // 64, a part cost 0.6 to 0.9 us more.  (Groups of four blocks, which hold most of the ring, took 4096 x 16384
-// x 4096 from 172 to 205 us.)  The epilogue holds the sums of the parts before in registers.
+// x 4096 from 172 to 205 us.)  The epilogue holds the sums of the parts before in registers.  A tile's first part is
+// the longer one, since the epilogue of the tile before still runs beside it: with parts of 12 and 8 blocks the
+// gated 4096 x 4096 x 16384 took 320 us instead of 306, with 8 alone 344, with 16 alone 305.
 //
 // Bound by the tensor cores: 8192 rows, K 4096, 6144 features 120 us (3.44 PFLOP/s, 89% of twice the measured
 // bf16 rate), 4096 rows, K 16384, 4096 features 172 us (83%), gated 4096 rows of 4096 in 16384 features
@@ -639,8 +642,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         int s = 0, slot = 0, sum = 0;            // of the block, of the scale word, of the first half's accumulator
         uint32_t phase = 0, word_phase = 0, n = 0, which = 0;
         for (int t = 0; t < tiles && ok; ++t) {
-          for (int g = 0, in = 0; g < a.kbs; g += kGroup) {   // in: blocks of this part so far
-            const bool two = g + 1 < a.kbs, ends = g + kGroup >= a.kbs || in + kGroup >= a.part;
+          for (int g = 0, in = 0, most = a.first_part; g < a.kbs; g += kGroup) {  // in: blocks of this part so far
+            const bool two = g + 1 < a.kbs, ends = g + kGroup >= a.kbs || in + kGroup >= most;
             const int s1 = s + 1 == kPairStages ? 0 : s + 1;
             if ((g & 3) == 0) {
               ok = ok && thread_wait_cluster(&sf_full[slot], word_phase, abort_flag);
@@ -691,6 +694,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             in += kGroup;
             if (ends) {
               in = 0, ++n;
+              most = a.part;
               sum = sum == 0 ? 2 : sum - 1;      // (two further on, of three)
             }
           }
@@ -752,7 +756,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     const uint32_t free_bar = cluster_map_shared(smem_u32(sum_free + half * 2), 0);
     // rows begin at multiples of 32 bytes
     const bool straight = (a.n * (kGated ? 1 : a.f32 ? 4 : 2) & 31) == 0 && ((uintptr_t)a.out & 31u) == 0;
-    const int parts = (a.kbs + a.part - 1) / a.part;
+    const int parts = 1 + (max(a.kbs - a.first_part, 0) + a.part - 1) / a.part;
     int n = 0, sum = half;                       // parts of K so far; the accumulator
     // The half's next accumulator, complete (false: the wait ran out, or another one), and its release.
     const auto take = [&](uint32_t &acc) {
@@ -1027,8 +1031,8 @@ int run_product(ham_fp8_weight *w, const void *x_codes, const void *x_scales, in
   // fills an SM's tensor memory with 128 rows: 8 tiles (129 x 1024) 9.5 / 10.0 at K 1024, 12.3 / 16.6 at 4096; 12 tiles
   // (640 x 512) 19 / 10, 24 / 17, 39 / 45 at 16384; 16 tiles (256 x 2048) 29 / 10, 36 / 18, 59 / 46.
   const bool pair = rows > 128 && tiles * (w->parts == 2 ? 16 : 8) >= device_sms();
-  const int sums = (w->kbs + kSumBlocks - 1) / kSumBlocks;  // the pair kernel's, of equal size (in whole scale words)
-  a.part = ((w->kbs + sums - 1) / sums + 3) / 4 * 4;
+  a.first_part = kSumBlocks;                          // the pair kernel's parts
+  a.part = kSumNext;
   // the streaming kernel's row parts, of equal size: 128 rows at most, fewer where K is so long that a CTA needs
   // several accumulators even with every split (gated from 32768 on, plain from 98304)
   const int blocks = (w->kbs + kMaxSplits - 1) / kMaxSplits, needs = (blocks + kSumMost - 1) / kSumMost;
@@ -1044,7 +1048,7 @@ int run_product(ham_fp8_weight *w, const void *x_codes, const void *x_scales, in
   } else {
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const cudaError_t e = pair ? (w->parts == 2 ? launch_pair<true, true>(tx, w->map, a, w->device, s)
-                                                : a.part < a.kbs ? launch_pair<false, true>(tx, w->map, a, w->device, s) : launch_pair<false, false>(tx, w->map, a, w->device, s))
+                                                : a.first_part < a.kbs ? launch_pair<false, true>(tx, w->map, a, w->device, s) : launch_pair<false, false>(tx, w->map, a, w->device, s))
                                : (w->parts == 2 ? launch_stream<2>(tx, a, w->device, s)
                                                 : launch_stream<1>(tx, a, w->device, s));
     if (e != cudaSuccess) rc = op_fail(HAM_ECUDA, "product launch: %s", cudaGetErrorString(e));

@@ -290,9 +290,11 @@ int ham_add_norm(const void *x, const void *residual, const void *weight, float 
   a.sk = ham::fp8_scale_bytes(hidden);
   a.eps = eps;
   a.far = 2 * e * (!!sum_out + !!out) + e * !!codes > ((size_t)64 << 20);
-  // Few rows: short chains a thread.  Many: more of a row a thread, so that more rows are in flight an SM
-  // (16384 rows of 4096, residual and 8-bit output: 76 us with 512 threads a row, 70 with 256, 68 with
-  // streaming stores).
+  // Few rows: short chains a thread.  Many: more of a row a thread, so that more rows are in flight an SM.  (At most
+  // 256 / 512 threads a row, us, inputs from memory: 16384 rows of 4096 73 / 79 with residual and 8-bit output, 49 / 60 of
+  // x alone to bf16; of 3008 38 / 46, of 5136 65 / 69, of 8192 89 / 101; 1333 rows of 4096 6.1 / 7.2, of 5136 7.6 / 8.2 (with
+  // residual 11.0 / 10.5); 608 of 4096 3.8 / 3.5, of 5136 4.3 / 3.9, of 8192 5.2 / 6.2; 400 of 5136 3.8 / 3.5, with residual
+  // 5.7 / 5.0; from 12288 on both are the same kernel.)
   const int most = rows >= 4 * ham::device_sms() ? 256 : 512;
   int groups = 1;
   while (groups < 4 && a.vecs > groups * most) groups *= 2;
