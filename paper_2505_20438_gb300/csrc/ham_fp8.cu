@@ -14,10 +14,10 @@
 // The tensor cores add 32 terms of K exactly to the fp32 sum and cut the result off at its last place, toward
 // zero, so that one accumulator's error is a bias that grows with K: measured against 64-bit sums, relative to
 // the outputs' norm, 5.9e-8 at K 1024, 1.1e-7 at 2048, 2.3e-7 at 4096, 1.3e-6 at 16384 (a plain fp32 product:
-// 4.1e-8, 5.9e-8, 8.6e-8, 2.0e-7).  So an accumulator takes kSumBlocks blocks of K, 2048 terms (kSumMost where
-// more accumulators would cost the streaming kernel a CTA an SM; kSumNext after the pair kernel's first), and the
-// parts are added in fp32, in order: 0.9 to 1.1e-7 at every K from 2048 on with the pair kernel, 1.1 to 1.4e-7 with the
-// streaming one (2.4e-7).
+// 4.1e-8, 5.9e-8, 8.6e-8, 2.0e-7).  So an accumulator takes kSumNext blocks of K, 1024 terms (the pair kernel's first
+// in a tile kSumFirst; the streaming kernel's up to kSumMost where more accumulators would cost a CTA an SM), and the
+// parts are added in fp32, in order: 0.9 to 1.1e-7 at every K from 2048 on with the pair kernel, 0.5 to 0.9e-7 with the
+// streaming one (up to 2.4e-7 where its accumulators are few).
 //
 // Weights are laid out once (ham_fp8_weight_alloc) as [tile of 128 rows][K block][128 x 128], each
 // block 16 KiB in the shared-memory layout of the 128-byte swizzle, so that a weight tile's K range is
@@ -49,7 +49,7 @@ namespace ham {
 namespace {
 
 constexpr int kTile = 128;             // weight rows of a tile
-constexpr int kSumBlocks = 16, kSumNext = 8, kSumMost = 32;  // K blocks of one accumulator
+constexpr int kSumFirst = 16, kSumNext = 8, kSumMost = 32;  // K blocks of one accumulator
 constexpr int kBlockBytes = 128 * 128; // a tile's K block
 
 // One thread per 16-byte piece of the laid-out weight.
@@ -948,15 +948,15 @@ cudaError_t launch_stream(const CUtensorMap &tx, ProductArgs a, int dev, cudaStr
   int splits = 1;
   while (splits < kMaxSplits && splits * 4 <= a.kbs && (int64_t)a.tiles * zt * splits <= sms) splits *= 2;
   a.stage_bytes = kParts * kBlockBytes + a.nt * 128;
-  // Accumulators of at most kSumBlocks blocks, as far as the columns of three CTAs an SM go (over one wave,
-  // of two), of kSumMost in any case: with more columns, then with more splits, if that is what it takes.
-  // (Head of 128256 features of 4096 for 64 rows: 87 us with accumulators of 32 blocks, 98 with two CTAs an SM
-  // and 16, 101 with two splits and 16; 8 rows of 16384 in 32768 features: 82 with 16 of 19 columns each or
-  // with one of 128 blocks, 99 with eight splits.)
+  // Accumulators of kSumNext blocks, as far as the columns of three CTAs an SM go (over one wave, of two), of
+  // kSumMost at most in any case: with more columns, then with more splits, if that is what it takes.  (Head of
+  // 128256 features of 4096 for 64 rows: 87 us with one accumulator, 98 with two of 16 blocks and two CTAs an SM, 101
+  // with two splits of 16; 8 rows of 16384 in 32768 features: 81 with seven of 19 or with one of 128 blocks, 99 with
+  // eight splits.)
   int per, cols;
   for (;; splits *= 2) {
     per = (a.kbs + splits - 1) / splits;              // K blocks of a CTA
-    const int want = (per + kSumBlocks - 1) / kSumBlocks, least = (per + kSumMost - 1) / kSumMost;
+    const int want = (per + kSumNext - 1) / kSumNext, least = (per + kSumMost - 1) / kSumMost;
     const bool last = splits == kMaxSplits || splits * 4 > a.kbs, waves = (int64_t)a.tiles * zt * splits > 2 * sms;
     int room = stream_sums(kParts, a.nt, waves ? 128 : 256);
     if (room < least) room = stream_sums(kParts, a.nt, 256);
@@ -1031,7 +1031,7 @@ int run_product(ham_fp8_weight *w, const void *x_codes, const void *x_scales, in
   // fills an SM's tensor memory with 128 rows: 8 tiles (129 x 1024) 9.5 / 10.0 at K 1024, 12.3 / 16.6 at 4096; 12 tiles
   // (640 x 512) 19 / 10, 24 / 17, 39 / 45 at 16384; 16 tiles (256 x 2048) 29 / 10, 36 / 18, 59 / 46.
   const bool pair = rows > 128 && tiles * (w->parts == 2 ? 16 : 8) >= device_sms();
-  a.first_part = kSumBlocks;                          // the pair kernel's parts
+  a.first_part = kSumFirst;                           // the pair kernel's parts
   a.part = kSumNext;
   // the streaming kernel's row parts, of equal size: 128 rows at most, fewer where K is so long that a CTA needs
   // several accumulators even with every split (gated from 32768 on, plain from 98304)
