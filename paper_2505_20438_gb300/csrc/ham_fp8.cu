@@ -124,8 +124,8 @@ __device__ __forceinline__ void store4(const ProductArgs &a, int64_t row, int c,
 // requested before the dependency wait: nothing on the stream writes them.
 //
 // Bound by the weights' bytes where there are enough of them: the head of 128256 features of 4096 for 64 rows
-// takes 84.6 us (97% of the copy rate), a gated half of 16384 features for 8 rows 22.9 (87%), 14.3 for
-// 8 rows of 16384 in 4096 (69%).  A 4096 x 4096 weight, 16 MB, takes 8 us against 2.5 at that rate: the chain
+// takes 85.6 us (96% of the copy rate), a gated half of 16384 features for 8 rows 23.4 to 24.4 (82 to 85%), 14.9
+// for 8 rows of 16384 in 4096 (66%).  A 4096 x 4096 weight, 16 MB, takes 7.1 us against 2.5 at that rate: the chain
 // of launch, first blocks, products, the cluster's sums and stores stands alone.
 constexpr int kStreamThreads = 256;
 constexpr int kStreamSf = 4;            // scale slots (of four K blocks each)

@@ -86,7 +86,7 @@ __device__ __forceinline__ float block_sum(float s, float *part) {
 }
 
 // A block is one row, a thread the groups tid, tid + threads, ... of 8 elements.  Many rows are bound by
-// memory (16384 rows of 4096, residual in, sum and 8-bit rows out: 67.7 us, 6.9 TB/s counted at the bytes
+// memory (16384 rows of 4096, residual in, sum and 8-bit rows out: 68.1 us, 6.9 TB/s counted at the bytes
 // of the operands), few by the chain of launch, reads and the row's sum (8 rows: 1.65 us).
 template <int kGroups>
 __global__ void __launch_bounds__(kGroups >= 4 ? 1024 : 512) add_norm_kernel(NormArgs a) {

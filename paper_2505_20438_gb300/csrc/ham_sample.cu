@@ -37,7 +37,8 @@
 //    For top-p they bound each bin's weight, which leaves the cut to a few bins, and one more pass sums
 //    weights and lists the bins' tokens (86 us; clusters 195; histograms of all weights took 150);
 //  - no cut: one more pass of exponentials, whose instructions bound it (52 us; clusters 77).
-// A bound that does not hold is seen, exactly, and the row goes the way of the other kernel's steps.
+// A bound that does not hold is seen, exactly, and the row goes the way of the other kernel's steps.  (Two CTAs an SM
+// leave 64 registers a thread, of which 64 bytes spill in fp32 and 132 in bf16, as ptxas reports them.)
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
