@@ -38,7 +38,7 @@
 //    weights and lists the bins' tokens (86 us; clusters 195; histograms of all weights took 150);
 //  - no cut: one more pass of exponentials, whose instructions bound it (52 us; clusters 77).
 // A bound that does not hold is seen, exactly, and the row goes the way of the other kernel's steps.  (Two CTAs an SM
-// leave 64 registers a thread, of which 64 bytes spill in fp32 and 132 in bf16, as ptxas reports them.)
+// leave 64 registers a thread, of which 88 bytes spill in fp32 and 136 in bf16, as ptxas reports them.)
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -951,6 +951,48 @@ struct Row {
       sum += w[j];
     }
   }
+  // Top-k (k > 0) and top-p (p >= 0) by the histograms of the bins, which are clear.  True: the tokens up to the cut are
+  // few, and the first CTA has chosen among them; else where the order is cut.
+  __device__ bool cuts(const SampleArgs &a, int row, int k, double p, uint32_t least, Cut &cut_at) const {
+    const bool by_k = k > 0, by_p = p >= 0.;
+    if (by_k) histogram_of_bins<false>();        // counts alone if top-k comes first
+    else histogram_of_bins<true>();
+    find(!by_k, !by_k, 0, 0, (uint64_t)k, by_k ? 0. : p);
+    const bool all_in = s.found < 0;             // fewer than k tokens have any weight
+    const int last = all_in ? kBins - 2 : s.found;
+    const uint32_t before = all_in ? 0 : s.found_before_count;
+    const uint64_t whole = by_k ? 0 : s.total_mass;
+    uint64_t aim = s.aim;
+    const uint32_t all = all_in ? kList : before + s.found_count;
+    if (all <= (uint32_t)kList) {
+      const uint32_t listed = list(0, last);
+      if (listed <= (uint32_t)kList) {           // (all_in: known only now)
+        if (rank == 0) pull(listed);
+        if (ctas > 1) cluster_arrive();          // (the others' lists are pulled)
+        if (rank == 0) choose(a, row, (int)listed, last, before, all_in ? 0 : k, p, whole, least);
+        if (ctas > 1) cluster_wait();
+        return true;
+      }
+    }
+    if (by_k) {
+      if (by_p) {                                // (top-p wants the weight that top-k keeps)
+        sync();
+        clear();
+        histogram_of_bins<true>();
+        find(false, true, 0, 0, (uint64_t)k);
+      }
+      if (!all_in) cut_at = cut(false, (uint64_t)k);
+      if (by_p) {
+        aim = aim_of(p, all_in ? s.total_mass : cut_at.mass);
+        sync();
+        clear();
+        histogram_of_bins<true>();
+        find(true, true, 0, 0, aim);
+      }
+    }
+    if (by_p) cut_at = cut(true, aim);
+    return false;
+  }
   // Turns the quads' numbers into the running sums before them; their sum.
   template <typename N>
   __device__ uint64_t sum_before(N *of) const {
@@ -1345,45 +1387,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
   // w >= min_p 2^31 for whole w (the product is exact in fp32): at least the whole number above
   const uint32_t least = min_p > 0.f ? (uint32_t)ceilf(fminf(min_p, 1.f) * kFine) : 0u;
   Cut cut;
-  if (by_k || by_p) {
-    if (by_k) r.template histogram_of_bins<false>();     // counts alone if top-k comes first
-    else r.template histogram_of_bins<true>();
-    r.find(!by_k, !by_k, 0, 0, (uint64_t)k, by_k ? 0. : share);
-    const bool all_in = s.found < 0;             // fewer than k tokens have any weight
-    const int last = all_in ? kBins - 2 : s.found;
-    const uint32_t before = all_in ? 0 : s.found_before_count;
-    const uint64_t whole = by_k ? 0 : s.total_mass;
-    uint64_t aim = s.aim;
-    const uint32_t all = all_in ? kList : before + s.found_count;
-    if (all <= (uint32_t)kList) {
-      const uint32_t listed = r.list(0, last);
-      if (listed <= (uint32_t)kList) {           // (all_in: known only now)
-        if (rank == 0) r.pull(listed);
-        if (ctas > 1) cluster_arrive();          // (the others' lists are pulled)
-        if (rank == 0)
-          r.choose(a, row, listed, last, before, by_k && !all_in ? k : 0, by_p ? share : -1., whole, least);
-        if (ctas > 1) cluster_wait();
-        return;
-      }
-    }
-    if (by_k) {
-      if (by_p) {                                // (top-p wants the weight that top-k keeps)
-        r.sync();
-        r.clear();
-        r.template histogram_of_bins<true>();
-        r.find(false, true, 0, 0, (uint64_t)k);
-      }
-      if (!all_in) cut = r.cut(false, (uint64_t)k);
-      if (by_p) {
-        aim = Row<T, false>::aim_of(share, all_in ? s.total_mass : cut.mass);
-        r.sync();
-        r.clear();
-        r.template histogram_of_bins<true>();
-        r.find(true, true, 0, 0, aim);
-      }
-    }
-    if (by_p) cut = r.cut(true, aim);
-  }
+  if ((by_k || by_p) && r.cuts(a, row, by_k ? k : 0, by_p ? share : -1., least, cut)) return;
   // ---- the kept weights of each thread's stretch of the slice, in index order
   uint32_t ties_before = 0, ties_mine = 0;
   if (cut.by_index) {
@@ -1600,41 +1604,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_alone_kernel(SampleA
     __syncthreads();
     r.clear();
   }
-  if (by_k || by_p) {
-    if (by_k) r.template histogram_of_bins<false>();
-    else r.template histogram_of_bins<true>();
-    r.find(!by_k, !by_k, 0, 0, (uint64_t)k, by_k ? 0. : share);
-    const bool all_in = s.found < 0;             // fewer than k tokens have any weight
-    const int last = all_in ? kBins - 2 : s.found;
-    const uint32_t before = all_in ? 0 : s.found_before_count;
-    const uint64_t whole = by_k ? 0 : s.total_mass;
-    uint64_t aim = s.aim;
-    const uint32_t all = all_in ? kList : before + s.found_count;
-    if (all <= (uint32_t)kList) {
-      const uint32_t listed = r.list(0, last);
-      if (listed <= (uint32_t)kList) {           // (all_in: known only now)
-        r.choose(a, row, listed, last, before, by_k && !all_in ? k : 0, by_p ? share : -1., whole, least);
-        return;
-      }
-    }
-    if (by_k) {
-      if (by_p) {                                // (top-p wants the weight that top-k keeps)
-        __syncthreads();
-        r.clear();
-        r.template histogram_of_bins<true>();
-        r.find(false, true, 0, 0, (uint64_t)k);
-      }
-      if (!all_in) cut = r.cut(false, (uint64_t)k);
-      if (by_p) {
-        aim = Row<T, true>::aim_of(share, all_in ? s.total_mass : cut.mass);
-        __syncthreads();
-        r.clear();
-        r.template histogram_of_bins<true>();
-        r.find(true, true, 0, 0, aim);
-      }
-    }
-    if (by_p) cut = r.cut(true, aim);
-  }
+  if ((by_k || by_p) && r.cuts(a, row, by_k ? k : 0, by_p ? share : -1., least, cut)) return;
   // ---- the kept weights of each quad
   __syncthreads();                               // (what was here was read)
   uint64_t *mass = reinterpret_cast<uint64_t *>(w.h);
