@@ -37,10 +37,9 @@ struct ham_fp8_weight {
   int32_t n = 0, k = 0, parts = 1;   // parts: 2 for a gated weight (gate, up)
   int32_t tiles = 0, kbs = 0, sk = 0;
   int device = 0;
-  uint8_t *codes = nullptr;    // [tiles][kbs][parts][128 x 128 swizzled]
+  uint8_t *codes = nullptr;    // [tiles][kbs][parts][128 x 128 swizzled], and behind them in the same allocation
   uint8_t *scales = nullptr;   // [tiles][parts][sk]
-  int32_t *err = nullptr;      // device error word
-  int32_t *host_err = nullptr; // pinned
+  int32_t *err = nullptr;      // the device error word
   uint64_t wait_ns = ham::kWaitLimitNs;  // limit of the kernels' waits
   CUtensorMap map;             // codes as one stretch, boxes of half a block
 };
@@ -1082,9 +1081,6 @@ int ham_fp8_weight_free(ham_fp8_weight *w) {
   cudaGetDevice(&dev);
   cudaSetDevice(w->device);
   cudaFree(w->codes);
-  cudaFree(w->scales);
-  cudaFree(w->err);
-  cudaFreeHost(w->host_err);
   cudaSetDevice(dev);
   delete w;
   return HAM_OK;
@@ -1115,15 +1111,15 @@ int ham_fp8_weight_alloc(int32_t n, int32_t k, const void *codes, const void *sc
     delete w;
     return op_fail(HAM_EUNSUPPORTED, "weight of %d x %d is too large", n, k);
   }
-  cudaError_t e = cudaMalloc(reinterpret_cast<void **>(&w->codes), (size_t)blocks * w->parts * ham::kBlockBytes);
-  if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void **>(&w->scales), (size_t)w->tiles * w->parts * w->sk);
-  if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void **>(&w->err), 4);
-  if (e == cudaSuccess) e = cudaMallocHost(reinterpret_cast<void **>(&w->host_err), 4);
+  const size_t code_bytes = (size_t)blocks * w->parts * ham::kBlockBytes, scale_bytes = (size_t)w->tiles * w->parts * w->sk;
+  cudaError_t e = cudaMalloc(reinterpret_cast<void **>(&w->codes), code_bytes + scale_bytes + 4);
   if (e != cudaSuccess) {
     cudaGetLastError();
     ham_fp8_weight_free(w);
     return op_fail(HAM_ENOMEM, "weight of %d x %d: %s", n, k, cudaGetErrorString(e));
   }
+  w->scales = w->codes + code_bytes;             // (whole words)
+  w->err = reinterpret_cast<int32_t *>(w->scales + scale_bytes);
   const int64_t pieces = blocks * (ham::kBlockBytes / 16);
   for (int p = 0; p < w->parts && e == cudaSuccess; ++p) {
     ham::lay_out_weight_kernel<<<(unsigned)((pieces + 255) / 256), 256>>>(
@@ -1189,12 +1185,13 @@ int ham_fp8_weight_set_wait_limit_ns(ham_fp8_weight *w, uint64_t ns) {
 int ham_fp8_weight_status(ham_fp8_weight *w, void *stream, int32_t *device_code) {
   if (!w) return op_fail(HAM_EINVAL, "null handle");
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  cudaError_t ce = cudaMemcpyAsync(w->host_err, w->err, 4, cudaMemcpyDeviceToHost, s);
+  int32_t code = 0;
+  cudaError_t ce = cudaMemcpyAsync(&code, w->err, 4, cudaMemcpyDeviceToHost, s);
   if (ce == cudaSuccess) ce = cudaMemsetAsync(w->err, 0, 4, s);
   if (ce == cudaSuccess) ce = cudaStreamSynchronize(s);
   if (ce != cudaSuccess) return op_fail(HAM_ECUDA, "status read: %s", cudaGetErrorString(ce));
-  if (device_code) *device_code = *w->host_err;
-  if (*w->host_err != 0) return op_fail(HAM_EDEVICE, "device error word = %d", *w->host_err);
+  if (device_code) *device_code = code;
+  if (code != 0) return op_fail(HAM_EDEVICE, "device error word = %d", code);
   return HAM_OK;
 }
 
