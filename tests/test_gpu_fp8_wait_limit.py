@@ -76,7 +76,7 @@ def test_the_call_before_does_not_count():
     calls()
     torch.cuda.synchronize()
     want = y.clone()
-    ham.ham_fp8_weight_set_wait_limit_ns(w, 25_000)
+    ham.ham_fp8_weight_set_wait_limit_ns(w, 40_000)
     torch.cuda._sleep(2_000_000)
     for _ in range(10):
         calls()
