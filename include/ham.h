@@ -53,7 +53,8 @@ enum {
   HAM_DEVERR_NTOK = 2,      /* token count < 1 for a new slot */
   HAM_DEVERR_PAGE = 3,      /* page-table entry outside [0, pool_pages) */
   HAM_DEVERR_SLOTS = 4,     /* slot counter outside [0, max_slots_per_seq] */
-  HAM_DEVERR_TIMEOUT = 5    /* a bounded wait inside a kernel ran out */
+  HAM_DEVERR_TIMEOUT = 5,   /* a bounded wait inside a kernel ran out */
+  HAM_DEVERR_ROUTE = 6      /* an experts' call: offsets that are no grouping, or an order entry out of range */
 };
 
 /* Position given to a new slot when ham_kv_append gets pos == NULL (Sec. 3.2). */
@@ -588,6 +589,82 @@ int ham_fp8_weight_set_wait_limit_ns(ham_fp8_weight *w, uint64_t ns);
 int ham_sample(const void *logits, int32_t logits_dtype, int32_t rows, int32_t vocab, const float *u,
                const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
                int32_t *tokens, float *probs, void *stream);
+
+/* ------------------------------------------------------------------------------------
+ * A feed-forward block made of experts
+ * ------------------------------------------------------------------------------------
+ * Where the base model's block is E gated blocks of which each row takes a few, the calls between the norm and
+ * the next residual are, with 8-bit rows and weights as above:
+ *   ham_fp8_linear (the router's logits, f32) -> ham_route -> ham_fp8_experts_gated -> ham_fp8_experts_linear
+ *   -> ham_experts_combine
+ * A SLOT is one (row, expert) pair that was chosen.  Slots are numbered by expert, within an expert by row: the
+ * slots of expert e are offsets[e] .. offsets[e + 1] - 1, and there are at most rows * top_k.  The counts stay on
+ * the device: nothing here waits for the host, and a capture replays with other counts. */
+
+enum { HAM_SCORE_SOFTMAX = 0, HAM_SCORE_SIGMOID = 1 };
+
+/* The experts of each row, and the grouping of the chosen pairs by expert.  For a row l of logits:
+ *   s_e = exp(l_e) / sum exp(l)  (HAM_SCORE_SOFTMAX)  or  1 / (1 + exp(-max(l_e, -80)))  (HAM_SCORE_SIGMOID)
+ *   v_e = s_e + bias_e  (bias nullable: 0)
+ *   experts lie in `groups` groups of experts / groups neighbours; a group's value is the sum of its two largest
+ *   v; the top_groups largest groups stay (equal ones: the lower index)
+ *   chosen: of the experts that stay the top_k largest v, largest first (equal ones: the lower index; without a
+ *   bias experts are compared by l)
+ *   weight = scale * s_e, divided by the sum of the chosen experts' s if renorm
+ * The choice is that of exact scores: where values in fp32 lie too near to one another to tell, the row's are computed
+ * again in fp64.  Weights are computed in fp32, off by at most 2^-18 of
+ * themselves.
+ * A logit of -inf or NaN, or a value v that is, rules its expert out; +inf counts as the largest finite number.  A
+ * place that no expert is left for gets expert -1, weight 0 and no slot: a padding row is a row of -inf.
+ * logits  device [rows][experts], bf16 or f32 (logits_dtype);  bias  nullable device f32 [experts]
+ * experts 1..512;  top_k 1..32, at most experts / groups * top_groups;  groups 1..32, a divisor of experts;
+ * top_groups 1..groups;  rows at most 2^24
+ * expert  device int32 [rows][top_k];  weight  device f32 [rows][top_k]
+ * offsets device int32 [experts + 1]: offsets[0] = 0, offsets[experts] the number of slots
+ * order   device int32 [rows * top_k]: the slots' pairs, row * top_k + place; -1 from offsets[experts] on
+ * place   device int32 [rows][top_k]: the pairs' slots; -1 where there is no expert
+ * Pointers 4-byte aligned (bf16 logits: 2).  Outputs must not overlap inputs or each other.  One launch, or two.
+ * Host errors: HAM_EINVAL, HAM_ECUDA. */
+int ham_route(const void *logits, int32_t logits_dtype, const float *bias, int32_t rows, int32_t experts,
+              int32_t top_k, int32_t score, int32_t groups, int32_t top_groups, int32_t renorm, float scale,
+              int32_t *expert, float *weight, int32_t *offsets, int32_t *order, int32_t *place, void *stream);
+
+/* Copy the weights of `experts` experts (codes [experts][n][k], scales [experts][ceil(n / 128)][4 * ceil(k / 512)])
+ * into the products' layout; with codes_up and scales_up the gated ones, n a multiple of 16.  As
+ * ham_fp8_weight_alloc in everything else; ham_fp8_weight_free, ham_fp8_weight_status and
+ * ham_fp8_weight_set_wait_limit_ns serve this handle too.  experts 1..512; HAM_EUNSUPPORTED where the padded
+ * weights pass 2^42 bytes. */
+int ham_fp8_experts_alloc(int32_t experts, int32_t n, int32_t k, const void *codes, const void *scales,
+                          const void *codes_up, const void *scales_up, ham_fp8_weight **out);
+
+/* The first half of the experts' gated blocks.  Slot i of expert e takes row t = order[i] / top_k of the 8-bit rows X:
+ *   G = X[t] W_gate,e^T, U = X[t] W_up,e^T (fp32),  H = G / (1 + exp(-G)) * U, encoded as an 8-bit row:
+ * codes [rows * top_k][n], scales [rows * top_k][..], in slot order.  Rows from offsets[experts] on are left as they
+ * were.  Sums as ham_fp8_linear's with parts of at most 2048 terms; a slot's result does not depend on the others.
+ * x_codes [rows][k], x_scales; rows at most 2^24, rows * top_k at most 2^26; offsets, order as ham_route gives them.
+ * Offsets that decrease or leave 0..rows * top_k set the device error word (HAM_DEVERR_ROUTE) and the call writes
+ * nothing; an order entry of a slot outside 0..rows * top_k - 1 sets it and counts as entry 0.
+ * Host errors: HAM_EINVAL, HAM_ECUDA. */
+int ham_fp8_experts_gated(ham_fp8_weight *w, const void *x_codes, const void *x_scales, int32_t rows,
+                          const int32_t *offsets, const int32_t *order, int32_t top_k, void *codes, void *scales,
+                          void *stream);
+
+/* out[i] = X[i] W_e^T for the slots i of each expert e: 8-bit rows X [slots][k] in slot order (what
+ * ham_fp8_experts_gated leaves), out [slots][n] in out_dtype (HAM_DTYPE_BF16 or HAM_DTYPE_F32).  slots is the
+ * buffers' number of rows, at most 2^26; rows from offsets[experts] on are neither read nor written.  Sums, offsets and
+ * errors as ham_fp8_experts_gated's. */
+int ham_fp8_experts_linear(ham_fp8_weight *w, const void *x_codes, const void *x_scales, int32_t slots,
+                           const int32_t *offsets, void *out, int32_t out_dtype, void *stream);
+
+/* The weighted sum of a row's results:
+ *   out[t] = add[t] + sum_j weight[t][j] * y[place[t][j]]
+ * in fp32, j in order, rounded once to bf16; a place outside 0..rows * top_k - 1 (ham_route's -1) adds nothing.
+ * y  device [rows * top_k][n], bf16 or f32 (y_dtype);  add  nullable device bf16 [rows][n] (a shared expert's result,
+ * or the residual; it may be out itself);  weight  device f32, place  device int32 [rows][top_k]
+ * out  device bf16 [rows][n].  rows at most 2^24, top_k 1..32, n at most 2^20; y, add and out 16-byte aligned.
+ * Host errors: HAM_EINVAL, HAM_ECUDA. */
+int ham_experts_combine(const void *y, int32_t y_dtype, const float *weight, const int32_t *place, const void *add,
+                        int32_t rows, int32_t top_k, int32_t n, void *out, void *stream);
 
 #ifdef __cplusplus
 }

@@ -30,26 +30,10 @@
 #include <cstring>
 #include <new>
 
-#include "ham_mx.cuh"
-#include "ham_ops.cuh"
-
-struct ham_fp8_weight {
-  int32_t n = 0, k = 0, parts = 1;   // parts: 2 for a gated weight (gate, up)
-  int32_t tiles = 0, kbs = 0, sk = 0;
-  int device = 0;
-  uint8_t *codes = nullptr;    // [tiles][kbs][parts][128 x 128 swizzled], and behind them in the same allocation
-  uint8_t *scales = nullptr;   // [tiles][parts][sk]
-  int32_t *err = nullptr;      // the device error word
-  uint64_t wait_ns = ham::kWaitLimitNs;  // limit of the kernels' waits
-  CUtensorMap map;             // codes as one stretch, boxes of half a block
-};
+#include "ham_fp8.cuh"
 
 namespace ham {
 namespace {
-
-constexpr int kTile = 128;             // weight rows of a tile
-constexpr int kSumFirst = 16, kSumNext = 8, kSumMost = 32;  // K blocks of one accumulator
-constexpr int kBlockBytes = 128 * 128; // a tile's K block
 
 // One thread per 16-byte piece of the laid-out weight.
 __global__ void lay_out_weight_kernel(const uint8_t *__restrict__ codes, int n, int k, int part, int parts,
@@ -70,12 +54,6 @@ __global__ void lay_out_scales_kernel(const uint8_t *__restrict__ scales, int ti
   if (i < tiles * sk) dst[((int64_t)(i / sk) * parts + part) * sk + i % sk] = scales[i];
 }
 
-// Shared memory that a CTA with `cols` columns of tensor memory asks for at least, in kernels whose CTAs
-// wait for one another: an SM's 228 KB then run out before its 512 columns do, so that no CTA of a
-// cluster ever waits for columns that a CTA of another cluster holds (two clusters could otherwise each
-// hold what the other waits for).
-constexpr int smem_floor(int cols) { return (228 * 1024 * (cols / 32) + 16) / 17; }
-
 struct ProductArgs {
   const uint8_t *w, *ws;   // the handle's layout
   const uint8_t *xs;       // [rows][sk]
@@ -91,8 +69,6 @@ struct ProductArgs {
   uint64_t wait_ns;        // limit of the waits that may be shortened (the others end with them)
   int f32;                 // fp32 output
 };
-
-__device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.f + expf(-g)) * u; }
 
 // Four neighbouring outputs of one row from column c (a multiple of 4), within the row's n.
 __device__ __forceinline__ void store4(const ProductArgs &a, int64_t row, int c, float4 v) {
@@ -404,12 +380,6 @@ __global__ void __launch_bounds__(kStreamThreads)
 // tiles leave pairs without work in the last round, and the first tile's loads and the last one's epilogue
 // stand alone (2048 rows, 4096 x 4096: 27 us, 66%).  With one accumulator for all of K these took 119, 169,
 // 302 and 26.5 us; a pair takes 64 bytes a clock an SM from L2 at the products' full rate.
-constexpr int kPairThreads = 384;       // warps: copies, products, 2 x scales, 8 x epilogue
-// Registers a thread: the launch's, and from the roles on those of the first four warps and of the epilogue's
-// eight, which hold a tile's sums in 128 of them.  Together they are what the launch has: a kernel compiled
-// to fewer would wait for the rest forever, so the host looks before it launches one.
-constexpr int kLaunchRegs = 168, kFewRegs = 56, kManyRegs = 224;
-static_assert(4 * kFewRegs + 8 * kManyRegs <= 12 * kLaunchRegs && kPairThreads == 384, "registers");
 constexpr int kPairStages = 6;
 constexpr int kPairStageBytes = 2 * kBlockBytes;
 constexpr int kPairSf = 4;
@@ -904,38 +874,6 @@ __global__ void __launch_bounds__(kPairThreads, 1)
 // ------------------------------------------------------------------------------------
 // Host side
 // ------------------------------------------------------------------------------------
-template <typename K>
-cudaError_t allow_smem(K kernel, int bytes, bool (&done)[64], int dev) {
-  if (dev >= 0 && dev < 64 && done[dev]) return cudaSuccess;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e == cudaSuccess && dev >= 0 && dev < 64) done[dev] = true;
-  return e;
-}
-
-// Pairs that are resident at once (a pair lies within one group of SMs, which need not hold a whole number
-// of them); a persistent grid is no larger.
-template <typename K>
-int resident_pairs(K kernel, int (&known)[64], int dev) {
-  if (dev >= 0 && dev < 64 && known[dev] > 0) return known[dev];
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(device_sms() / 2 * 2));
-  cfg.blockDim = dim3(kPairThreads);
-  cfg.dynamicSmemBytes = (size_t)kPairSmem;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = 2;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  int n = 0;
-  if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
-    cudaGetLastError();
-    n = device_sms() / 2;
-  }
-  if (dev >= 0 && dev < 64) known[dev] = n;
-  return n;
-}
-
 template <int kParts>
 cudaError_t launch_stream(const CUtensorMap &tx, ProductArgs a, int dev, cudaStream_t stream) {
   static bool done[64] = {};
@@ -997,7 +935,7 @@ cudaError_t launch_pair(const CUtensorMap &tx, const CUtensorMap &tw, const Prod
   }
   const cudaError_t e = allow_smem(kKernel, kPairSmem, done, dev);
   if (e != cudaSuccess) return e;
-  const int64_t pairs = std::min<int64_t>(resident_pairs(kKernel, resident, dev), (int64_t)row_tiles * col_tiles);
+  const int64_t pairs = std::min<int64_t>(resident_pairs(kKernel, kPairSmem, resident, dev), (int64_t)row_tiles * col_tiles);
   return launch_after<kKernel>(dim3((unsigned)(2 * pairs)), dim3(kPairThreads), (size_t)kPairSmem, dim3(2, 1, 1),
                                stream, tx, tw, a, row_tiles, col_tiles);
 }
@@ -1058,6 +996,7 @@ int run_product(ham_fp8_weight *w, const void *x_codes, const void *x_scales, in
 
 int check_product(const ham_fp8_weight *w, const void *xc, const void *xs, int32_t rows, const void *out) {
   if (!w) return op_fail(HAM_EINVAL, "null handle");
+  if (w->experts) return op_fail(HAM_EINVAL, "experts' weights serve ham_fp8_experts_gated and ham_fp8_experts_linear");
   if (rows < 0 || rows > (1 << 24)) return op_fail(HAM_EINVAL, "rows %d outside 0..2^24", rows);
   if (rows == 0) return HAM_OK;
   if (!xc || !xs || !out) return op_fail(HAM_EINVAL, "codes, scales and the output are required");

@@ -1,0 +1,79 @@
+// What the products with 8-bit weights share (ham_fp8.cu, ham_experts.cu): the handle and its layouts, the sums'
+// parts, the launches' helpers.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include "ham_mx.cuh"
+#include "ham_ops.cuh"
+
+// One weight: codes [tile][K block][part][128 x 128].  Some experts': blocks of 128 x 128 too, as ham_experts.cu says.
+struct ham_fp8_weight {
+  int32_t n = 0, k = 0, parts = 1;   // parts: 2 for a gated weight (gate, up)
+  int32_t experts = 0;               // 0: one weight
+  int32_t tiles = 0, kbs = 0, sk = 0;
+  int device = 0;
+  uint8_t *codes = nullptr;    // 128 x 128 swizzled blocks, and behind them in the same allocation
+  uint8_t *scales = nullptr;   // [(experts)][tiles][parts][sk]
+  int32_t *err = nullptr;      // the device error word
+  uint64_t wait_ns = ham::kWaitLimitNs;  // limit of the kernels' waits
+  CUtensorMap map;             // codes as one stretch, boxes of half a block (experts: a block)
+};
+
+namespace ham {
+namespace {
+
+constexpr int kTile = 128;             // weight rows of a tile
+constexpr int kSumFirst = 16, kSumNext = 8, kSumMost = 32;  // K blocks of one accumulator
+constexpr int kBlockBytes = 128 * 128; // a tile's K block
+
+__device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.f + expf(-g)) * u; }
+
+// Shared memory that a CTA with `cols` columns of tensor memory asks for at least, in kernels whose CTAs
+// wait for one another: an SM's 228 KB then run out before its 512 columns do, so that no CTA of a
+// cluster ever waits for columns that a CTA of another cluster holds (two clusters could otherwise each
+// hold what the other waits for).
+constexpr int smem_floor(int cols) { return (228 * 1024 * (cols / 32) + 16) / 17; }
+
+// Registers a thread of the pair kernels: the launch's, and from the roles on those of the first four warps and of
+// the epilogue's eight, which hold a tile's sums in 128 of them.  Together they are what the launch has: a kernel
+// compiled to fewer would wait for the rest forever, so the host looks before it launches one.
+constexpr int kPairThreads = 384;       // warps: copies, products, 2 x scales, 8 x epilogue
+constexpr int kLaunchRegs = 168, kFewRegs = 56, kManyRegs = 224;
+static_assert(4 * kFewRegs + 8 * kManyRegs <= 12 * kLaunchRegs && kPairThreads == 384, "registers");
+
+template <typename K>
+cudaError_t allow_smem(K kernel, int bytes, bool (&done)[64], int dev) {
+  if (dev >= 0 && dev < 64 && done[dev]) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && dev >= 0 && dev < 64) done[dev] = true;
+  return e;
+}
+
+// Pairs that are resident at once (a pair lies within one group of SMs, which need not hold a whole number
+// of them); a persistent grid is no larger.
+template <typename K>
+int resident_pairs(K kernel, int smem, int (&known)[64], int dev) {
+  if (dev >= 0 && dev < 64 && known[dev] > 0) return known[dev];
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(device_sms() / 2 * 2));
+  cfg.blockDim = dim3(kPairThreads);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int n = 0;
+  if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
+    cudaGetLastError();
+    n = device_sms() / 2;
+  }
+  if (dev >= 0 && dev < 64) known[dev] = n;
+  return n;
+}
+
+}  // namespace
+}  // namespace ham

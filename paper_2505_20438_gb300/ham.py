@@ -24,10 +24,11 @@ HAM_OK, HAM_EINVAL, HAM_ENOMEM, HAM_ECAPACITY, HAM_ECUDA, HAM_EDEVICE, HAM_EUNSU
 STATUS_NAMES = {0: "HAM_OK", 1: "HAM_EINVAL", 2: "HAM_ENOMEM", 3: "HAM_ECAPACITY",
                 4: "HAM_ECUDA", 5: "HAM_EDEVICE", 6: "HAM_EUNSUPPORTED"}
 (HAM_DEVERR_NONE, HAM_DEVERR_CAPACITY, HAM_DEVERR_NTOK, HAM_DEVERR_PAGE, HAM_DEVERR_SLOTS,
- HAM_DEVERR_TIMEOUT) = range(6)
+ HAM_DEVERR_TIMEOUT, HAM_DEVERR_ROUTE) = range(7)
 HAM_POS_SLOT, HAM_POS_TOKEN = 0, 1
 HAM_DTYPE_BF16, HAM_DTYPE_F32 = 0, 1
 HAM_KV_BF16, HAM_KV_E4M3 = 0, 1
+HAM_SCORE_SOFTMAX, HAM_SCORE_SIGMOID = 0, 1
 
 
 class HamError(RuntimeError):
@@ -111,6 +112,12 @@ _SIGNATURES = {
     "ham_fp8_weight_status": [_vp, _vp, ctypes.POINTER(_i32)],
     "ham_fp8_weight_set_wait_limit_ns": [_vp, ctypes.c_uint64],
     "ham_sample": [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp],
+    "ham_route": [_vp, _i32, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _i32, ctypes.c_float, _vp, _vp, _vp, _vp, _vp,
+                  _vp],
+    "ham_fp8_experts_alloc": [_i32, _i32, _i32, _vp, _vp, _vp, _vp, ctypes.POINTER(_vp)],
+    "ham_fp8_experts_gated": [_vp, _vp, _vp, _i32, _vp, _vp, _i32, _vp, _vp, _vp],
+    "ham_fp8_experts_linear": [_vp, _vp, _vp, _i32, _vp, _vp, _i32, _vp],
+    "ham_experts_combine": [_vp, _i32, _vp, _vp, _vp, _i32, _i32, _i32, _vp, _vp],
 }
 _lib = None
 
@@ -596,10 +603,11 @@ def ham_fp8_encode_weight(w, codes, scales, stream=None):
 
 
 class Fp8Weight:
-    """Owning handle of one weight laid out for the 8-bit products (ham_fp8_weight*)."""
+    """Owning handle of one weight, or of some experts', laid out for the 8-bit products (ham_fp8_weight*)."""
 
-    def __init__(self, ptr: int, n: int, k: int, gated: bool):
+    def __init__(self, ptr: int, n: int, k: int, gated: bool, experts: int = 0):
         self.ptr, self.n, self.k, self.gated = ptr, n, k, gated
+        self.experts = experts      # 0: one weight, for ham_fp8_linear and ham_fp8_gated
 
     @property
     def _as_parameter_(self):
@@ -687,3 +695,75 @@ def ham_sample(logits, u, tokens, temperature=None, top_k=None, top_p=None, min_
         _dev(top_k, row, "i32", "top_k", nullable=True), _dev(top_p, row, "f32", "top_p", nullable=True),
         _dev(min_p, row, "f32", "min_p", nullable=True), _dev(tokens, row, "i32", "tokens"),
         _dev(probs, row, "f32", "probs", nullable=True), _stream_ptr(stream)))
+
+
+# ---------------------------------------------------------------------------------------
+# a feed-forward block made of experts
+# ---------------------------------------------------------------------------------------
+
+def ham_route(logits, expert, weight, offsets, order, place, bias=None, score=HAM_SCORE_SOFTMAX, groups=1,
+              top_groups=1, renorm=True, scale=1.0, stream=None):
+    """Each row's experts and their grouping: from logits [T][E] (bf16 or fp32) the chosen expert int32
+    [T][K] and weight fp32 [T][K], offsets int32 [E + 1] of each expert's slots, order int32 [T * K] (a slot's pair
+    t * K + j) and place int32 [T][K] (a pair's slot)."""
+    import torch
+    T, E = logits.shape if logits is not None and logits.dim() == 2 else (0, 0)
+    K = expert.shape[1] if expert is not None and expert.dim() == 2 else 0
+    f32 = logits is not None and logits.dtype is torch.float32
+    _check(lib().ham_route(
+        _dev(logits, (T, E), "f32" if f32 else "bf16", "logits"), HAM_DTYPE_F32 if f32 else HAM_DTYPE_BF16,
+        _dev(bias, (E,), "f32", "bias", nullable=True), T, E, K, score, groups, top_groups, int(renorm), scale,
+        _dev(expert, (T, K), "i32", "expert"), _dev(weight, (T, K), "f32", "weight"),
+        _dev(offsets, (E + 1,), "i32", "offsets"), _dev(order, (T * K,), "i32", "order"),
+        _dev(place, (T, K), "i32", "place"), _stream_ptr(stream)))
+
+
+def ham_fp8_experts_alloc(experts, n, k, codes, scales, codes_up=None, scales_up=None) -> Fp8Weight:
+    """codes uint8 [experts][n][k] and scales uint8 [experts][ceil(n / 128)][fp8_scale_bytes(k)] on the GPU
+    (copied); with codes_up and scales_up the gated weights (codes the gates' projections)."""
+    import torch
+    shape, sshape = (experts, n, k), (experts, -(-n // 128), fp8_scale_bytes(k))
+    out = ctypes.c_void_p()
+    args = (_dev(codes, shape, "u8", "codes"), _dev(scales, sshape, "u8", "scales"),
+            _dev(codes_up, shape, "u8", "codes_up", nullable=True),
+            _dev(scales_up, sshape, "u8", "scales_up", nullable=True))
+    torch.cuda.current_stream().synchronize()   # (the copy runs on the legacy default stream)
+    _check(lib().ham_fp8_experts_alloc(experts, n, k, *args, ctypes.byref(out)))
+    return Fp8Weight(out.value, n, k, codes_up is not None, experts)
+
+
+def ham_fp8_experts_gated(w: Fp8Weight, x_codes, x_scales, offsets, order, top_k, codes, scales, stream=None):
+    """8-bit rows (codes [T * top_k][n], scales) in slot order of silu(X W_gate^T) * (X W_up^T) with each slot's
+    expert, for 8-bit rows X [T][k]; offsets and order as ham_route leaves them."""
+    T = x_codes.shape[0] if x_codes is not None and x_codes.dim() == 2 else 0
+    S = T * top_k
+    _check(lib().ham_fp8_experts_gated(
+        w, _dev(x_codes, (T, w.k), "u8", "x_codes"), _dev(x_scales, (T, fp8_scale_bytes(w.k)), "u8", "x_scales"), T,
+        _dev(offsets, (w.experts + 1,), "i32", "offsets"), _dev(order, (S,), "i32", "order"), top_k,
+        _dev(codes, (S, w.n), "u8", "codes"), _dev(scales, (S, fp8_scale_bytes(w.n)), "u8", "scales"),
+        _stream_ptr(stream)))
+
+
+def ham_fp8_experts_linear(w: Fp8Weight, x_codes, x_scales, offsets, out, stream=None):
+    """out [S][n] (bf16 or fp32) = X W^T with each slot's expert, for 8-bit rows X [S][k] in slot order."""
+    import torch
+    S = x_codes.shape[0] if x_codes is not None and x_codes.dim() == 2 else 0
+    f32 = out is not None and out.dtype is torch.float32
+    _check(lib().ham_fp8_experts_linear(
+        w, _dev(x_codes, (S, w.k), "u8", "x_codes"), _dev(x_scales, (S, fp8_scale_bytes(w.k)), "u8", "x_scales"), S,
+        _dev(offsets, (w.experts + 1,), "i32", "offsets"), _dev(out, (S, w.n), "f32" if f32 else "bf16", "out"),
+        HAM_DTYPE_F32 if f32 else HAM_DTYPE_BF16, _stream_ptr(stream)))
+
+
+def ham_experts_combine(y, weight, place, out, add=None, stream=None):
+    """out bf16 [T][n] = add + sum_j weight[:, j] * y[place[:, j]] for y [T * K][n] (bf16 or fp32), weight fp32 and
+    place int32 [T][K]; add (bf16 [T][n]) is optional and may be out itself."""
+    import torch
+    T, K = weight.shape if weight is not None and weight.dim() == 2 else (0, 0)
+    n = out.shape[1] if out is not None and out.dim() == 2 else 0
+    f32 = y is not None and y.dtype is torch.float32
+    _check(lib().ham_experts_combine(
+        _dev(y, (T * K, n), "f32" if f32 else "bf16", "y"), HAM_DTYPE_F32 if f32 else HAM_DTYPE_BF16,
+        _dev(weight, (T, K), "f32", "weight"), _dev(place, (T, K), "i32", "place"),
+        _dev(add, (T, n), "bf16", "add", nullable=True), T, K, n, _dev(out, (T, n), "bf16", "out"),
+        _stream_ptr(stream)))
