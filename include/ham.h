@@ -633,7 +633,7 @@ int ham_route(const void *logits, int32_t logits_dtype, const float *bias, int32
  * into the products' layout; with codes_up and scales_up the gated ones, n a multiple of 16.  As
  * ham_fp8_weight_alloc in everything else; ham_fp8_weight_free, ham_fp8_weight_status and
  * ham_fp8_weight_set_wait_limit_ns serve this handle too.  experts 1..512; HAM_EUNSUPPORTED where the padded
- * weights pass 2^42 bytes. */
+ * weights pass 2^41 bytes. */
 int ham_fp8_experts_alloc(int32_t experts, int32_t n, int32_t k, const void *codes, const void *scales,
                           const void *codes_up, const void *scales_up, ham_fp8_weight **out);
 

@@ -49,91 +49,615 @@ __global__ void lay_out_expert_scales_kernel(const uint8_t *__restrict__ scales,
   if (i < rows * sk) dst[(i / sk * parts + part) * sk + i % sk] = scales[i];
 }
 
+// ------------------------------------------------------------------------------------
+// The kernel: pairs of CTAs, 256 rows of weights by up to 256 slots
+// ------------------------------------------------------------------------------------
+// The weights are the product's M: a pair of CTAs (cta_group::2) multiplies two half tiles, one a CTA (128 lanes of its
+// tensor memory), with the N rows of one expert's slots.  N is what the expert has, up to the next multiple of 32, so
+// that a few rows cost a few rows' products and many experts of uneven counts leave no lanes idle.  More than 256 slots
+// are cut into tiles of equal size, more than 128 into two halves of N, each an accumulator of its own.
+//
+// Each CTA copies its half tile's K block (16 KiB, one stretch) and half of the N rows (a gated product's four rows a
+// copy, by index, from where they lie), into its own shared memory alone.  Sums take parts of K as
+// the products of one weight do (ham_fp8.cu): kSumFirst blocks, then kSumNext, in three accumulators of 128 columns that
+// are used in turn; the epilogue adds them in registers.
+//
+// A thread of the epilogue has one feature (a lane) and up to 128 slots (columns).  Plain outputs are neighbours across
+// a warp's lanes.  Of a gated product lanes 0..15 hold the gate and 16..31 the up projection of 16 features: one shuffle
+// each gives the lower lanes the even slots' products, the upper ones the odd slots'.  A slot's largest magnitude over
+// the 128 features of a scale is wanted from both CTAs' warps: 16 bits of each (exponent and seven bits, all that the
+// scale depends on) through shared memory and the pair's.
 struct ExpertArgs {
-  const uint8_t *w, *ws;   // the handle's layout
-  const uint8_t *x, *xs;   // rows
+  const uint8_t *ws;       // the handle's scales
+  const uint8_t *xs;       // the rows'
   const int32_t *offsets, *order;  // order: gated
   void *out;
   uint8_t *out_scales;     // gated
   int32_t *err;
-  int experts, slots, top_k, n, k, kbs, sk, out_sk, tiles, halves, f32;
+  int experts, slots, top_k, n, kbs, sk, out_sk, tiles, f32;
+  uint64_t wait_ns;
 };
 
-__device__ __forceinline__ float code_value(uint32_t byte) {
-  uint32_t lo, hi;
-  e4m3x4_to_f16x2(byte, lo, hi);
-  return __half2float(__ushort_as_half((unsigned short)(lo & 0xffffu)));
+constexpr int kExpertStages = 6;
+constexpr int kExpertStageBytes = 2 * kBlockBytes;  // the weights' block, 64 + 64 rows
+constexpr int kExpertSf = 4;            // scale slots (of four K blocks each)
+constexpr int kExpertSfBytes = 3 * 512; // the CTA's half tile, both halves of N
+constexpr int kSums = 3, kSfCol = 448;  // accumulators of 128 columns, then the scales
+constexpr int kGroup = 2;               // K blocks that one accumulator takes, then the other
+constexpr int kKeyBytes = 2 * 2 * 8 * 128 * 2;   // [half][every other tile][warp of the pair][slot]
+constexpr int kCodeBytes = 2 * 128 * 64;         // [half][slot][feature]
+constexpr int kExpertUsed = 1024 + kExpertStages * kExpertStageBytes + kExpertSf * kExpertSfBytes + 512;
+constexpr int expert_smem(bool gated) {
+  const int used = kExpertUsed + (gated ? kKeyBytes + kCodeBytes + 2 * 128 : 0);
+  return used > smem_floor(512) ? used : smem_floor(512);
 }
-__device__ __forceinline__ float scale_value(uint8_t s) {
-  return s == 255 ? __uint_as_float(0x7fffffffu) : s ? __uint_as_float((uint32_t)s << 23) : 0x1p-127f;
+static_assert(expert_smem(true) + (kMostExperts + 64) * 4 <= 227 * 1024, "shared memory");
+
+// A tile: slots of one expert by one pair of half tiles.
+struct ExpertTile {
+  int expert, ct, slot0, count;
+  int n0, n1;                           // columns of the two halves (multiples of 32; n1 may be 0)
+};
+
+// g / (1 + exp(-g)): the exponential of -|g|, so that nothing overflows, and a reciprocal of a number in 1..2 (the
+// quotient's general form tests for and mends cases that do not occur here).
+__device__ __forceinline__ float silu_of(float g) {
+  const float t = expf(-fabsf(g)), d = 1.f + t;
+  float r;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(d));
+  r = fmaf(r, fmaf(-d, r, 1.f), r);
+  return g * (g < 0.f ? t * r : r);
 }
 
-// A thread a feature, a block 128 features of one slot.
 template <bool kGated>
-__global__ void __launch_bounds__(128) experts_kernel(ExpertArgs a) {
-  __shared__ float x[kFp8Block];
-  __shared__ float top[4];
-  const int slot = blockIdx.x, tile = blockIdx.y, tid = threadIdx.x;
+__global__ void __launch_bounds__(kPairThreads, 1)
+    experts_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ CUtensorMap tw, ExpertArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t *sf = ring + kExpertStages * kExpertStageBytes;
+  // full, sf_full and sum_free: the ones of a pair's first CTA are used
+  uint64_t *full = reinterpret_cast<uint64_t *>(sf + kExpertSf * kExpertSfBytes);
+  uint64_t *empty = full + kExpertStages;
+  uint64_t *sf_full = empty + kExpertStages;   // an arrival a CTA
+  uint64_t *sf_empty = sf_full + kExpertSf;
+  uint64_t *sum_full = sf_empty + kExpertSf;   // [epilogue group][its accumulators in turn]
+  uint64_t *sum_free = sum_full + 2 * kSums;   // [accumulator]: an arrival a warp of the pair that takes it
+  uint64_t *keys_full = sum_free + kSums;      // [half][every other tile]: an arrival a warp of the pair
+  uint64_t *drained = keys_full + 4;           // every product issued is complete
+  static_assert((2 * kExpertStages + 2 * kExpertSf + 3 * kSums + 5) * 8 <= 512, "barriers");
+  uint16_t *keys = reinterpret_cast<uint16_t *>(reinterpret_cast<uint8_t *>(full) + 512);
+  uint8_t *code_rows = reinterpret_cast<uint8_t *>(keys) + kKeyBytes;
+  uint8_t *exponents = code_rows + kCodeBytes; // [half][slot]
+  __shared__ int starts[kMostExperts + 1];     // row tiles of the experts before
+  __shared__ int parts_of[12], bad_shared;
+  __shared__ int4 gathered[2][16];             // gated: the rows of a tile's copies
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_shared, issued_shared;
+  volatile int *abort_flag = &abort_shared;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int side = (int)cluster_rank();
+  const uint32_t both = 3u;
+  const int clusters = gridDim.x / 2, cluster = blockIdx.x / 2;
+  const int cols = kGated ? a.tiles : (a.tiles + 1) / 2;    // pairs of half tiles
+  // A wait ran out (or the pair has given up already): both CTAs stop.
+  const auto give_up = [&] {
+    if (*abort_flag) return;
+    record_error(a.err, HAM_DEVERR_TIMEOUT);
+    *abort_flag = 1;
+    st_cluster_u32(cluster_map_shared(smem_u32(&abort_shared), side ^ 1), 1u);
+  };
+  if (tid == 0) {
+    for (int s = 0; s < kExpertStages; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int s = 0; s < kExpertSf; ++s) {
+      mbar_init(&sf_full[s], 2);
+      mbar_init(&sf_empty[s], 1);
+    }
+    for (int s = 0; s < 2 * kSums; ++s) mbar_init(&sum_full[s], 1);
+    for (int s = 0; s < kSums; ++s) mbar_init(&sum_free[s], 8);
+    for (int s = 0; s < 4; ++s) mbar_init(&keys_full[s], 8);
+    mbar_init(drained, 1);
+    abort_shared = 0;
+    bad_shared = 0;
+    fence_mbar_init();
+  }
+  if (warp == 0 && lane == 0) {
+    prefetch_tensormap(&tx);
+    prefetch_tensormap(&tw);
+  }
+  cluster_sync_all();
+  // Tensor memory is taken before the dependency wait and before the next kernel may start (as in ham_fp8.cu).
+  if (warp == 1) tmem_alloc_pair<512>(&tmem_slot);
+  tc_fence_before();
   grid_dependency_wait();
-  grid_launch_dependents();
-  int expert = -1;
-  for (int e = 0; e < a.experts; ++e) {
-    const int from = a.offsets[e], to = a.offsets[e + 1];
-    if (from < 0 || to > a.slots || from > to) {
-      if (tid == 0) record_error(a.err, HAM_DEVERR_ROUTE);
-      return;
-    }
-    if (slot >= from && slot < to) expert = e;
-  }
-  if (expert < 0) return;
-  int row = slot;
-  if (kGated) {
-    const int o = a.order[slot];
-    if (o < 0 || o >= a.slots) {
-      if (tid == 0) record_error(a.err, HAM_DEVERR_ROUTE);
-      row = 0;
-    } else {
-      row = o / a.top_k;
-    }
-  }
-  const int f = tile * kTile + tid;
-  float sum[2] = {0.f, 0.f};
-  for (int kb = 0; kb < a.kbs; ++kb) {
-    __syncthreads();
-    const int col = kb * kFp8Block + tid;
-    x[tid] = col < a.k ? code_value(a.x[(int64_t)row * a.k + col]) : 0.f;
-    __syncthreads();
-    const float sx = scale_value(a.xs[(int64_t)row * a.sk + kb]);
+  // ---------------------------------------------------------------- the experts' row tiles, added up
+  {
+    int tiles_of[2], sum = 0;
 #pragma unroll
-    for (int p = 0; p < (kGated ? 2 : 1); ++p) {
-      const int half = kGated ? tile * 2 + tid / 64 : tile, r = kGated ? (tid % 64) / 16 * 32 + p * 16 + tid % 16 : tid;
-      const uint8_t *w = a.w + (((int64_t)expert * a.halves + half) * a.kbs + kb) * kBlockBytes + r * 128;
-      float part = 0.f;
-      for (int c = 0; c < 8; ++c) {
-        const uint4 v = *reinterpret_cast<const uint4 *>(w + ((c ^ (r & 7)) << 4));
-        const uint32_t word[4] = {v.x, v.y, v.z, v.w};
-        for (int i = 0; i < 16; ++i) part = fmaf(x[16 * c + i], code_value(word[i / 4] >> 8 * (i % 4) & 0xffu), part);
+    for (int i = 0; i < 2; ++i) {
+      const int e = 2 * tid + i;
+      tiles_of[i] = 0;
+      if (e < a.experts) {
+        const int from = a.offsets[e], to = a.offsets[e + 1];
+        if (from < 0 || to < from || to > a.slots) bad_shared = 1;
+        else tiles_of[i] = (to - from + 255) >> 8;
       }
-      const float sw = scale_value(a.ws[(((int64_t)expert * a.tiles + tile) * (kGated ? 2 : 1) + p) * a.sk + kb]);
-      sum[p] += part * sx * sw;
+      sum += tiles_of[i];
     }
-  }
-  if constexpr (!kGated) {
-    if (f >= a.n) return;
-    const int64_t to = (int64_t)slot * a.n + f;
-    if (a.f32) static_cast<float *>(a.out)[to] = sum[0];
-    else static_cast<__nv_bfloat16 *>(a.out)[to] = __float2bfloat16_rn(sum[0]);
-  } else {
-    const float h = silu_mul(sum[0], sum[1]);
-    const float m = warp_max_f32(fabsf(h));
-    if ((tid & 31) == 0) top[tid >> 5] = m;
+    int run = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(kFull, run, o);
+      if (lane >= o) run += x;
+    }
+    if (lane == 31) parts_of[warp] = run;
     __syncthreads();
-    const int e = fp8_exponent(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
-    if (f < a.n) static_cast<uint8_t *>(a.out)[(int64_t)slot * a.n + f] = (uint8_t)fp8_codes4(h, 0, 0, 0, fp8_pow2(-e));
-    uint8_t *s = a.out_scales + (int64_t)slot * a.out_sk;
-    if (tid == 0) s[tile] = (uint8_t)(e + 127);
-    if (tile == a.tiles - 1 && tid > 0 && tile + tid < a.out_sk) s[tile + tid] = 127;
+    tc_fence_after();
+    for (int w = 0; w < warp; ++w) run += parts_of[w];
+    run -= sum;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (2 * tid + i <= a.experts) starts[2 * tid + i] = run;
+      run += tiles_of[i];
+    }
+    __syncthreads();
   }
+  if (bad_shared && tid == 0) record_error(a.err, HAM_DEVERR_ROUTE);
+  const int64_t total = bad_shared ? 0 : (int64_t)starts[a.experts] * cols;
+  const uint32_t tmem = *const_cast<volatile uint32_t *>(&tmem_slot);
+  // Tile w: an expert's tiles lie together, its row tiles next to one another (they share their weights).
+  const auto tile_of = [&](int64_t w) {
+    int lo = 0, hi = a.experts;                  // starts[lo] * cols <= w < starts[hi] * cols
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if ((int64_t)starts[mid] * cols <= w) lo = mid;
+      else hi = mid;
+    }
+    ExpertTile t;
+    t.expert = lo;
+    const int from = a.offsets[lo], rows = a.offsets[lo + 1] - from, rt = starts[lo + 1] - starts[lo];
+    const int64_t at = w - (int64_t)starts[lo] * cols;
+    int r = 0;
+    t.ct = (int)at;
+    if (rt > 1) t.ct = (int)(at / rt), r = (int)(at % rt);
+    const int each = ((rows + rt - 1) / rt + 31) & ~31;
+    t.slot0 = from + r * each;
+    t.count = min(each, rows - r * each);
+    const int n = (t.count + 31) & ~31;
+    t.n0 = n > 128 ? (n / 2 + 31) & ~31 : n;
+    t.n1 = n - t.n0;
+    return t;
+  };
+  // The row of the tile's slot i (past the last: the last).
+  const auto row_of = [&](const ExpertTile &t, int i) {
+    const int slot = t.slot0 + min(i, t.count - 1);
+    if constexpr (!kGated) return slot;
+    const int o = a.order[slot];
+    if ((uint32_t)o >= (uint32_t)a.slots) {
+      record_error(a.err, HAM_DEVERR_ROUTE);
+      return 0;
+    }
+    return o / a.top_k;
+  };
+  // The copies of a tile by warp 0.  Of each half of N a CTA brings n / 2 rows, as far as the tile has them (what lies in
+  // the others' place does not matter: a row's sums are its own), kRowsEach a copy.
+  constexpr int kRowsEach = kGated ? 4 : 16;
+  struct Source { int w, bytes, copies[2], row[2]; };
+  const auto source_of = [&](int64_t w) {
+    const ExpertTile t = tile_of(w);
+    Source from;
+    from.bytes = 2 * kBlockBytes;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int n = h ? t.n1 : t.n0, base = h ? t.n0 : 0;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const int rows = min(max(t.count - base - s * (n / 2), 0), n / 2), copies = (rows + kRowsEach - 1) / kRowsEach;
+        from.bytes += copies * kRowsEach * 128;
+        if (s == side) from.copies[h] = copies, from.row[h] = t.slot0 + base + s * (n / 2);
+      }
+      if constexpr (kGated)                        // lane l: the rows of copy l
+        if (lane < from.copies[h]) {
+          const int i = base + side * (n / 2) + lane * 4;
+          gathered[h][lane] = make_int4(row_of(t, i), row_of(t, i + 1), row_of(t, i + 2), row_of(t, i + 3));
+        }
+    }
+    __syncwarp();
+    const int half = kGated ? t.ct * 2 + side : min(t.ct * 2 + side, a.tiles - 1);
+    from.w = (t.expert * (a.tiles * (kGated ? 2 : 1)) + half) * a.kbs;
+    return from;
+  };
+  // Request a tile's K block kb for stage s (one thread); the bytes of both CTAs count at the first one's barrier.
+  const auto request = [&](int s, const Source &from, int kb, uint64_t pol) {
+    const uint32_t bar = cluster_map_shared(smem_u32(&full[s]), 0);
+    uint8_t *dst = ring + s * kExpertStageBytes;
+    if (side == 0) mbar_arrive_tx(&full[s], (uint32_t)from.bytes);
+    tma_load_2d_pair(dst, &tw, 0, (from.w + kb) * (kBlockBytes / 2048), bar, pol);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      dst += h ? 64 * 128 : kBlockBytes;
+      if constexpr (kGated) {
+#pragma unroll 1
+        for (int c0 = 0; c0 < from.copies[h]; c0 += 4) {
+          int4 r[4];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) r[c] = gathered[h][c0 + c];
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            if (c0 + c < from.copies[h]) tma_gather4_pair(dst + (c0 + c) * 512, &tx, kb * kFp8Block, r[c], bar, pol);
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (c < from.copies[h]) tma_load_2d_pair(dst + c * 2048, &tx, kb * kFp8Block, from.row[h] + c * 16, bar, pol);
+      }
+    }
+  };
+  int issued = 0;
+  if (warp < 4) {
+    setmaxnreg_dec<kFewRegs>();
+    if (warp == 0) {
+      // ------------------------------------------------------------ copies
+      const uint64_t pol = policy_evict_last();
+      bool ok = true;
+      int it = 0;
+      for (int64_t w = cluster; w < total && ok; w += clusters) {
+        const Source from = source_of(w);
+        for (int kb = 0; kb < a.kbs; ++kb, ++it) {
+          if (it >= kExpertStages &&
+              !warp_wait(&empty[it % kExpertStages], (uint32_t)(it / kExpertStages - 1) & 1u, abort_flag)) {
+            ok = false;
+            break;
+          }
+          if (elect_one()) request(it % kExpertStages, from, kb, pol);
+          __syncwarp();
+          issued = it + 1;
+        }
+      }
+      if (!ok && lane == 0) give_up();
+    } else if (warp == 1) {
+      // ------------------------------------------------------------ products (a pair's first CTA)
+      if (side == 0 && elect_one()) {
+        const uint64_t blocks = smem_desc_sw128(smem_u32(ring), 16, 1024), words = smem_desc_plain(smem_u32(sf), 0, 128);
+        constexpr uint32_t kNextByte = idesc_mx(256, 128, 1) - idesc_mx(256, 128, 0);
+        bool ok = true;
+        int s = 0, slot = 0;                     // of the block, of the scale word
+        uint32_t phase = 0, word_phase = 0, which = 0;
+        uint32_t use = 0, singles = 0, given0 = 0, given1 = 0;  // accumulators, tiles of one half, each group's accumulators so far
+        const auto free_sum = [&](uint32_t u) {
+          return u < kSums || thread_wait_cluster(&sum_free[u % kSums], (u / kSums - 1) & 1u, abort_flag);
+        };
+        for (int64_t w = cluster; w < total && ok; w += clusters) {
+          const ExpertTile t = tile_of(w);
+          const int halves = t.n1 ? 2 : 1;
+          const uint32_t alone = halves == 1 && (singles++ & 1);  // the second group's turn
+          const uint32_t idesc_half[2] = {idesc_mx(256, t.n0, 0), idesc_mx(256, t.n1, 0)};
+          for (int g = 0, in = 0, most = kSumFirst; g < a.kbs; g += kGroup) {  // in: blocks of this part so far
+            const bool two = g + 1 < a.kbs, ends = g + kGroup >= a.kbs || in + kGroup >= most;
+            const int s1 = s + 1 == kExpertStages ? 0 : s + 1;
+            if ((g & 3) == 0) {
+              ok = ok && thread_wait_cluster(&sf_full[slot], word_phase, abort_flag);
+              which ^= 16;
+            }
+            ok = ok && thread_wait_cluster(&full[s], phase, abort_flag);
+            if (in == 0) ok = ok && free_sum(use);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t sft = tmem + kSfCol + which;
+            if ((g & 3) == 0) {
+#pragma unroll
+              for (int p = 0; p < 3; ++p)
+                tc_copy_scales_of<2>(sft + p * 4, words + (uint32_t)(slot * (kExpertSfBytes / 16) + p * 32));
+              tc_commit_pair(&sf_empty[slot], both);
+              if (++slot == kExpertSf) slot = 0, word_phase ^= 1;
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              if (h >= halves) break;
+              if (h && in == 0) {
+                if (!free_sum(use + 1)) { ok = false; break; }
+                tc_fence_after();
+              }
+              const uint32_t acc = tmem + (use + h) % kSums * 128, idesc = idesc_half[h] + (g & 3) * kNextByte;
+#pragma unroll
+              for (int j = 0; j < kGroup; ++j) {
+                if (j && !two) break;
+                const int st = j ? s1 : s;
+                if (j && !h) {
+                  ok = thread_wait_cluster(&full[s1], phase ^ (s1 == 0), abort_flag);
+                  if (!ok) break;
+                  tc_fence_after();
+                }
+                const uint64_t wt = blocks + (uint32_t)(st * (kExpertStageBytes / 16)), x = wt + (uint32_t)(kBlockBytes + h * 64 * 128) / 16;
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk)
+                  tc_mma_mx<2>(acc, wt + kk * 2, x + kk * 2, idesc + j * kNextByte, sft, sft + 4 + 4 * h, in + j + kk > 0);
+                if (h == halves - 1) tc_commit_pair(&empty[st], both);
+              }
+              if (!ok) break;
+              if (ends) {
+                const bool second = h || alone;
+                tc_commit_pair(&sum_full[second ? kSums + given1 % kSums : given0 % kSums], both);
+                if (second) ++given1;
+                else ++given0;
+              }
+            }
+            if (!ok) break;
+            s += two ? 2 : 1;
+            if (s >= kExpertStages) s -= kExpertStages, phase ^= 1;
+            in += kGroup;
+            if (ends) {
+              in = 0;
+              most = kSumNext;
+              use += halves;
+            }
+          }
+        }
+        if (!ok) give_up();
+        tc_commit_pair(drained, both);
+      }
+      __syncwarp();
+    } else {
+      // ------------------------------------------------------------ scale words
+      // Two warps take turns at the words (of four K blocks each), and each loads its next before it passes one on.
+      if (warp == 2) grid_launch_dependents();
+      const int groups = (a.kbs + 3) / 4, turn = warp - 2;
+      uint32_t x[8], ws;
+      int64_t w = cluster, known = -1;           // known: the tile of the rows below
+      int g = turn, rows[8], wrow = 0;
+      const auto load = [&] {
+        if (w != known) {
+          const ExpertTile t = tile_of(w);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int i = lane + 32 * (j & 3), n = j < 4 ? t.n0 : t.n1;
+            rows[j] = i < n ? row_of(t, (j < 4 ? 0 : t.n0) + i) : -1;
+          }
+          wrow = kGated ? (t.expert * a.tiles + t.ct) * 2 + (lane >> 4) : t.expert * a.tiles + min(t.ct * 2 + side, a.tiles - 1);
+          known = w;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          x[j] = rows[j] >= 0 ? __ldg(reinterpret_cast<const uint32_t *>(a.xs + (int64_t)rows[j] * a.sk) + g) : 0x7f7f7f7fu;
+        ws = __ldg(reinterpret_cast<const uint32_t *>(a.ws + (int64_t)wrow * a.sk) + g);
+      };
+      // the gi-th word of this cluster's tiles is word g of tile w
+      const auto settle = [&] {
+        while (g >= groups) g -= groups, w += clusters;
+      };
+      settle();
+      if (w < total) load();
+      for (int64_t gi = turn; w < total; gi += 2) {
+        const int slot = (int)(gi % kExpertSf);
+        if (gi >= kExpertSf && !warp_wait(&sf_empty[slot], (uint32_t)(gi / kExpertSf - 1) & 1u, abort_flag, a.wait_ns)) {
+          if (lane == 0) give_up();
+          break;
+        }
+        uint4 *dst = reinterpret_cast<uint4 *>(sf + slot * kExpertSfBytes) + lane;
+        dst[0] = make_uint4(ws, ws, ws, ws);
+        dst[32] = make_uint4(x[0], x[1], x[2], x[3]);
+        dst[64] = make_uint4(x[4], x[5], x[6], x[7]);
+        g += 2;
+        settle();
+        if (w < total) load();
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(cluster_map_shared(smem_u32(&sf_full[slot]), 0));
+      }
+    }
+  } else {
+    setmaxnreg_inc<kManyRegs>();
+    // ------------------------------------------------------------ epilogue: a feature a thread
+    // Four warps take the first half's sums, four the second's; tiles of one half in turn.
+    const int quarter = warp & 3, group = (warp - 4) >> 2;
+    const uint32_t free_bar = cluster_map_shared(smem_u32(sum_free), 0);
+    const int parts = 1 + (max(a.kbs - kSumFirst, 0) + kSumNext - 1) / kSumNext;
+    uint32_t use = 0, singles = 0;               // accumulators, tiles of one half so far
+    uint32_t got = 0, taken = 0;                 // accumulators, tiles that this group took
+    for (int64_t w = cluster; w < total; w += clusters) {
+      const ExpertTile t = tile_of(w);
+      const int halves = t.n1 ? 2 : 1;
+      int half = group;
+      const uint32_t first = use;
+      use += parts * halves;
+      if (halves == 1) {
+        if ((singles++ & 1) != (uint32_t)group) continue;
+        half = 0;
+      }
+      const int n = half ? t.n1 : t.n0, base = half ? t.n0 : 0;
+      const int live = min(n, t.count - base);   // slots of this half
+      float v[128];                              // a feature's sums, slot after slot
+#pragma unroll
+      for (int j = 0; j < 128; ++j) v[j] = 0.f;
+      bool ok = true;
+#pragma unroll 1
+      for (int c = 0; c < parts; ++c) {
+        const uint32_t u = first + c * halves + half;
+        // (a group waits for accumulators of its own alone, each barrier's phases in order; of them three at most are
+        // full and not yet taken)
+        ok = warp_wait_cluster(&sum_full[group * kSums + got % kSums], (got / kSums) & 1u, abort_flag);
+        ++got;
+        if (!ok) {
+          if (lane == 0) give_up();
+          break;
+        }
+        tc_fence_after();
+        const uint32_t acc = tmem + u % kSums * 128 + ((uint32_t)(quarter * 32) << 16);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (q * 32 < n) {
+            float f[32];
+            tmem_ld32(acc + q * 32, *reinterpret_cast<uint32_t(*)[32]>(f));
+            tmem_wait_ld();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[q * 32 + j] += f[j];
+          }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster_relaxed(free_bar + u % kSums * 8);
+      }
+      const int64_t slot0 = t.slot0 + base;
+      if constexpr (!kGated) {
+        if (!ok) break;
+        const int f = t.ct * 256 + side * 128 + quarter * 32 + lane;
+        if (f < a.n) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            if (q * 32 < live) {
+              if (a.f32) {
+                float *out = static_cast<float *>(a.out) + (slot0 + q * 32) * a.n + f;
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                  if (q * 32 + j < live) out[(int64_t)j * a.n] = v[q * 32 + j];
+              } else {
+                __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(a.out) + (slot0 + q * 32) * a.n + f;
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                  if (q * 32 + j < live) out[(int64_t)j * a.n] = __float2bfloat16_rn(v[q * 32 + j]);
+              }
+            }
+        }
+      } else {
+        const int buffer = group * 2 + (taken & 1);
+        uint16_t *key = keys + buffer * (8 * 128);
+        float h[64];                             // slot 2 i + lane / 16 of feature 16 quarter + lane % 16
+        if (ok) {
+          const bool upper = lane & 16;
+          uint32_t m[32];                          // 16 bits of h[2 i], of h[2 i + 1]
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+#pragma unroll
+            for (int i = 8 * q; i < 8 * q + 8; ++i) m[i] = 0;
+            if (q * 32 >= n) continue;
+#pragma unroll
+            for (int i = 16 * q; i < 16 * q + 16; ++i) {
+              const float other = __shfl_xor_sync(kFull, upper ? v[2 * i] : v[2 * i + 1], 16);
+              const float own = upper ? v[2 * i + 1] : v[2 * i];
+              h[i] = silu_of(upper ? other : own) * (upper ? own : other);
+              const uint32_t u = __float_as_uint(h[i]) & 0x7fffffffu;
+              const uint32_t b = u > 0x7f800000u ? 0u : (u >> 16) | (u != 0u);   // (NaN counts for nothing)
+              m[i / 2] |= i & 1 ? b << 16 : b;
+            }
+          }
+          // the largest over the 16 lanes of a slot: lanes swap what the other half of them will go on with
+#pragma unroll
+          for (int o = 8, c = 16; o > 0; o >>= 1, c >>= 1)
+#pragma unroll
+            for (int i = 0; i < c; ++i) {
+              const bool high = lane & o;
+              const uint32_t got = __shfl_xor_sync(kFull, high ? m[i] : m[c + i], o);
+              m[i] = __vmaxu2(high ? m[c + i] : m[i], got);
+            }
+          // m[0], m[1]: words 2 (bits 3..0 of the lane, the highest first) + 0, 1, each of slots 4 i + lane / 16 and
+          // two further on
+          const int word = (lane & 8 ? 16 : 0) + (lane & 4 ? 8 : 0) + (lane & 2 ? 4 : 0) + (lane & 1 ? 2 : 0);
+          uint16_t *mine = key + (side * 4 + quarter) * 128;
+          const uint32_t theirs = cluster_map_shared(smem_u32(mine), side ^ 1);
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const int slot = 4 * (word + i) + 2 * j + (lane >> 4);
+              const uint16_t b = (uint16_t)(m[i] >> 16 * j);
+              mine[slot] = b;
+              asm volatile("st.shared::cluster.u16 [%0], %1;" ::"r"(theirs + slot * 2), "h"(b) : "memory");
+            }
+          __syncwarp();
+          if (lane < 2) mbar_arrive_cluster(cluster_map_shared(smem_u32(&keys_full[buffer]), lane));
+          ok = warp_wait_cluster(&keys_full[buffer], (taken >> 1) & 1u, abort_flag);
+          if (!ok && lane == 0) give_up();
+        }
+        ++taken;
+        ok = named_barrier_and(1 + group, 128, ok);  // (they meet below: all go on or none)
+        if (!ok) break;
+        const int slot = quarter * 32 + lane;      // a slot's scale a thread
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = max(top, (uint32_t)key[i * 128 + slot]);
+        const int e = fp8_exponent(__uint_as_float(top << 16));
+        uint8_t *exponent = exponents + group * 128;
+        exponent[slot] = (uint8_t)(e + 127);
+        if (side == 0 && slot < live) {
+          uint8_t *s = a.out_scales + (slot0 + slot) * a.out_sk;
+          s[t.ct] = (uint8_t)(e + 127);
+          if (t.ct == a.tiles - 1)
+            for (int b = a.tiles; b < a.out_sk; ++b) s[b] = 127;  // padding
+        }
+        named_barrier(1 + group, 128);
+        uint8_t *codes = code_rows + group * (128 * 64);
+        const int feature = quarter * 16 + (lane & 15);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          if (4 * i < live) {                      // slots 4 i + lane / 16 and two further on
+            const uint32_t es = *reinterpret_cast<const uint32_t *>(exponent + 4 * i) >> (lane & 16 ? 8 : 0);
+            const float p = fp8_pow2(127 - (int)(es & 0xffu)), q = fp8_pow2(127 - (int)(es >> 16 & 0xffu));
+            const uint32_t c = fp8_codes4(h[2 * i] * p, h[2 * i + 1] * q, 0.f, 0.f, 1.f);
+            uint8_t *to = codes + (4 * i + (lane >> 4)) * 64 + feature;
+            to[0] = (uint8_t)c;
+            to[128] = (uint8_t)(c >> 8);
+          }
+        }
+        named_barrier(1 + group, 128);
+        const int c = (slot & 3) * 16, col = t.ct * kTile + side * 64 + c;
+        for (int r = slot >> 2; r < live; r += 32)
+          if (col < a.n)                           // (n is a multiple of 16)
+            *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(a.out) + (slot0 + r) * a.n + col) =
+                *reinterpret_cast<const uint4 *>(codes + r * 64 + c);
+        named_barrier(1 + group, 128);             // (read before the next tile's are written)
+      }
+    }
+    tc_fence_before();
+  }
+  __syncwarp();
+  if (tid == 0) issued_shared = issued;
+  cluster_sync_all();                            // (the roles of both CTAs have ended)
+  if (warp < 2 && lane == 0) thread_wait(drained, 0u, abort_flag, false);
+  __syncwarp();
+  if (*abort_flag) {
+    // The copies of both CTAs count at the first one's barrier: the CTA that has requested fewer requests what it lacks
+    // (nothing reads the stages any more), and the first waits for the last of them to land.
+    if (warp == 0) {
+      const int theirs = (int)ld_cluster_u32(cluster_map_shared(smem_u32(&issued_shared), side ^ 1));
+      for (; issued < theirs; ++issued) {
+        const Source from = source_of(cluster + (int64_t)(issued / a.kbs) * clusters);
+        if (elect_one()) request(issued % kExpertStages, from, issued % a.kbs, policy_evict_last());
+        __syncwarp();
+      }
+    }
+    cluster_sync_all();
+    if (tid == 0 && side == 0)
+      for (int t = max(0, issued - kExpertStages); t < issued; ++t)
+        thread_wait(&full[t % kExpertStages], (uint32_t)(t / kExpertStages) & 1u, abort_flag, false);
+    __syncwarp();
+    cluster_sync_all();
+  }
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc_pair<512>(tmem);
+  }
+}
+
+template <bool kGated>
+cudaError_t launch_experts(const CUtensorMap &tx, const CUtensorMap &tw, const ExpertArgs &a, int dev, cudaStream_t s) {
+  static bool done[64] = {};
+  static int resident[64] = {};
+  constexpr auto kKernel = experts_kernel<kGated>;
+  constexpr int kSmem = expert_smem(kGated);
+  if (dev < 0 || dev >= 64 || !done[dev]) {
+    cudaFuncAttributes f;
+    const cudaError_t e = cudaFuncGetAttributes(&f, kKernel);
+    if (e != cudaSuccess) return e;
+    if (f.numRegs < kLaunchRegs) return cudaErrorLaunchOutOfResources;
+  }
+  const cudaError_t e = allow_smem(kKernel, kSmem, done, dev);
+  if (e != cudaSuccess) return e;
+  const int64_t cols = kGated ? a.tiles : (a.tiles + 1) / 2;
+  const int64_t most = ((int64_t)a.slots / 256 + std::min(a.slots, a.experts)) * cols;  // tiles at most
+  const int64_t pairs = std::min<int64_t>(resident_pairs(kKernel, kSmem, resident, dev), most);
+  return launch_after<kKernel>(dim3((unsigned)(2 * pairs)), dim3(kPairThreads), (size_t)kSmem, dim3(2, 1, 1), s, tx, tw, a);
 }
 
 int check_experts(const ham_fp8_weight *w, const void *xc, const void *xs, int64_t slots, const void *offsets,
@@ -145,26 +669,29 @@ int check_experts(const ham_fp8_weight *w, const void *xc, const void *xs, int64
   return HAM_OK;
 }
 
-int run_experts(ham_fp8_weight *w, ExpertArgs a, void *stream) {
+int run_experts(ham_fp8_weight *w, const void *x_codes, int32_t rows, ExpertArgs a, void *stream) {
   int dev = 0;
   cudaGetDevice(&dev);
   if (dev != w->device) cudaSetDevice(w->device);
-  a.w = w->codes;
   a.ws = w->scales;
   a.err = w->err;
   a.experts = w->experts;
   a.n = w->n;
-  a.k = w->k;
   a.kbs = w->kbs;
   a.sk = w->sk;
   a.out_sk = fp8_scale_bytes(w->n);
   a.tiles = w->tiles;
-  a.halves = w->tiles * w->parts;
-  const dim3 grid((unsigned)a.slots, (unsigned)a.tiles);
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = w->parts == 2 ? launch_after<experts_kernel<true>>(grid, dim3(128), 0, dim3(1), s, a)
-                                      : launch_after<experts_kernel<false>>(grid, dim3(128), 0, dim3(1), s, a);
-  const int rc = e == cudaSuccess ? HAM_OK : op_fail(HAM_ECUDA, "experts launch: %s", cudaGetErrorString(e));
+  a.wait_ns = w->wait_ns;
+  CUtensorMap tx;
+  int rc = HAM_OK;
+  if (make_bytes_tensor_map(&tx, x_codes, rows, w->k, kFp8Block, w->parts == 2 ? 1 : 16) != 0) {
+    rc = op_fail(HAM_ECUDA, "tensor map of the rows");
+  } else {
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const cudaError_t e = w->parts == 2 ? launch_experts<true>(tx, w->map, a, w->device, s)
+                                        : launch_experts<false>(tx, w->map, a, w->device, s);
+    if (e != cudaSuccess) rc = op_fail(HAM_ECUDA, "experts launch: %s", cudaGetErrorString(e));
+  }
   if (dev != w->device) cudaSetDevice(dev);
   return rc;
 }
@@ -202,7 +729,7 @@ int ham_fp8_experts_alloc(int32_t experts, int32_t n, int32_t k, const void *cod
   w->sk = ham::fp8_scale_bytes(k);
   cudaGetDevice(&w->device);
   const int64_t blocks = (int64_t)w->tiles * w->kbs * w->parts;  // of one expert
-  if (blocks > ((int64_t)1 << 42) / ham::kBlockBytes / experts) {
+  if (blocks > ((int64_t)1 << 41) / ham::kBlockBytes / experts) {
     delete w;
     return op_fail(HAM_EUNSUPPORTED, "weights of %d x %d x %d are too large", experts, n, k);
   }
@@ -267,7 +794,6 @@ int ham_fp8_experts_gated(ham_fp8_weight *w, const void *x_codes, const void *x_
       if (op_overlap(o.p, o.n, i.p, i.n)) return op_fail(HAM_EINVAL, "an output overlaps an input");
   if (op_overlap(outs[0].p, outs[0].n, outs[1].p, outs[1].n)) return op_fail(HAM_EINVAL, "two outputs overlap");
   ham::ExpertArgs a{};
-  a.x = static_cast<const uint8_t *>(x_codes);
   a.xs = static_cast<const uint8_t *>(x_scales);
   a.offsets = offsets;
   a.order = order;
@@ -275,7 +801,7 @@ int ham_fp8_experts_gated(ham_fp8_weight *w, const void *x_codes, const void *x_
   a.slots = (int)slots;
   a.out = codes;
   a.out_scales = static_cast<uint8_t *>(scales);
-  return ham::run_experts(w, a, stream);
+  return ham::run_experts(w, x_codes, rows, a, stream);
 }
 
 int ham_fp8_experts_linear(ham_fp8_weight *w, const void *x_codes, const void *x_scales, int32_t slots,
@@ -293,14 +819,13 @@ int ham_fp8_experts_linear(ham_fp8_weight *w, const void *x_codes, const void *x
       op_overlap(out, ob, offsets, 4 * ((size_t)w->experts + 1)))
     return op_fail(HAM_EINVAL, "out overlaps an input");
   ham::ExpertArgs a{};
-  a.x = static_cast<const uint8_t *>(x_codes);
   a.xs = static_cast<const uint8_t *>(x_scales);
   a.offsets = offsets;
   a.top_k = 1;
   a.slots = slots;
   a.out = out;
   a.f32 = f32;
-  return ham::run_experts(w, a, stream);
+  return ham::run_experts(w, x_codes, slots, a, stream);
 }
 
 }  // extern "C"

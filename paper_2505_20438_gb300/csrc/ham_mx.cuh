@@ -1,5 +1,5 @@
 // Inline-PTX wrappers of the block-scaled 8-bit products (tcgen05 kind::mxf8f6f4) and of thread-block
-// pairs (cta_group::2): shared by the kernels of ham_fp8.cu.
+// pairs (cta_group::2): shared by the kernels of ham_fp8.cu and ham_experts.cu.
 #pragma once
 
 #include <cuda.h>
@@ -150,6 +150,17 @@ __device__ __forceinline__ void tma_load_2d_pair(void *dst, const CUtensorMap *m
       "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
       ".L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;" ::"r"(smem_u32(dst)),
       "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar), "l"(policy)
+      : "memory");
+}
+
+// Four rows (r) of the map's matrix, 128 bytes of each from column x on, one after another into this CTA's shared memory
+// (the map's box is one row high); their bytes count at a barrier of the pair's first CTA.
+__device__ __forceinline__ void tma_gather4_pair(void *dst, const CUtensorMap *map, int x, const int4 &r, uint32_t bar,
+                                                 uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes"
+      ".L2::cache_hint [%0], [%1, {%2, %3, %4, %5, %6}], [%7], %8;" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(r.x), "r"(r.y), "r"(r.z), "r"(r.w), "r"(bar), "l"(policy)
       : "memory");
 }
 

@@ -15,7 +15,17 @@ def weights(rng, experts, n, k):
     c, s = random_codes(rng, experts * n, k)
     c = c.reshape(experts, n, k)
     s = rng.integers(113, 130, (experts, -(-n // 128), ops.scale_bytes(k))).astype(np.uint8)
-    return c, s, [ops.decode_weight(c[e], s[e]) for e in range(experts)]
+    return c, s, Values(c, s)
+
+
+class Values:
+    """The experts' weights in fp64, one at a time."""
+
+    def __init__(self, codes, scales):
+        self.codes, self.scales = codes, scales
+
+    def __getitem__(self, e):
+        return ops.decode_weight(self.codes[e], self.scales[e])
 
 
 def alloc(n, k, w, up=None):
@@ -50,8 +60,9 @@ def run_gated(rng, counts, n, k, top_k=2, rows=None, stream=None):
         a, b = offsets[e], offsets[e + 1]
         if a < b:
             mine = x[order[a:b] // top_k]
-            g, u, want = ops.gated(mine, w[2][e], up[2][e])
-            check_codes(codes[a:b], scales[a:b], want, gated_slack(mine, w[2][e], up[2][e], g, u))
+            wg, wu = w[2][e], up[2][e]
+            g, u, want = ops.gated(mine, wg, wu)
+            check_codes(codes[a:b], scales[a:b], want, gated_slack(mine, wg, wu, g, u))
     # rows behind the last slot are left as they were
     assert (codes[total:] == 0x7f).all() and (scales[total:] == 255).all()
     return h, args, codes, scales
@@ -75,7 +86,8 @@ def run_linear(rng, counts, n, k, out="bf16", slots=None, stream=None):
     for e in range(len(counts)):
         a, b = offsets[e], offsets[e + 1]
         if a < b:
-            check_bf16(y[a:b], x[a:b] @ w[2][e].T, product_slack(x[a:b], w[2][e]))
+            we = w[2][e]
+            check_bf16(y[a:b], x[a:b] @ we.T, product_slack(x[a:b], we))
     assert (y[total:] == -7).all()
     return h, args, y
 
@@ -112,6 +124,15 @@ def test_long_sums(k):
     for counts in ([3, 0, 20], [200, 90]):
         run_gated(rng, counts, 128, k)
         run_linear(rng, counts, 256, k, "f32")
+
+
+@pytest.mark.parametrize("counts", ["ones", "mixed", "large"])
+def test_tiles_one_after_another(counts):
+    """Several tiles a pair of CTAs, K in several parts: tiles of one and of two halves in every order."""
+    rng = np.random.default_rng(len(counts))
+    c = {"ones": np.ones(100, int), "mixed": rng.choice([0, 1, 40, 130, 200], 90), "large": rng.choice([3, 128, 256], 80)}[counts]
+    run_gated(rng, c, 256, 2304, top_k=4)
+    run_linear(rng, c, 400, 2304)
 
 
 def test_no_slots_and_rows_behind_the_last():
