@@ -13,6 +13,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <mutex>
 #include <new>
 
 #include "ham_fp8.cuh"
@@ -59,8 +60,8 @@ __global__ void lay_out_expert_scales_kernel(const uint8_t *__restrict__ scales,
 //
 // Each CTA copies its half tile's K block (16 KiB, one stretch) and half of the N rows (a gated product's four rows a
 // copy, by index, from where they lie), into its own shared memory alone.  Sums take parts of K as
-// the products of one weight do (ham_fp8.cu): kSumFirst blocks, then kSumNext, in three accumulators of 128 columns that
-// are used in turn; the epilogue adds them in registers.
+// the products of one weight do (ham_fp8.cu), kExpertPart blocks each, in three accumulators of 128 columns that are used in
+// turn; the epilogue adds them in registers.
 //
 // A thread of the epilogue has one feature (a lane) and up to 128 slots (columns).  Plain outputs are neighbours across
 // a warp's lanes.  Of a gated product lanes 0..15 hold the gate and 16..31 the up projection of 16 features: one shuffle
@@ -70,7 +71,8 @@ __global__ void lay_out_expert_scales_kernel(const uint8_t *__restrict__ scales,
 struct ExpertArgs {
   const uint8_t *ws;       // the handle's scales
   const uint8_t *xs;       // the rows'
-  const int32_t *offsets, *order;  // order: gated
+  const int32_t *offsets, *order;
+  int gather;              // the rows are order's, not the slots' own
   void *out;
   uint8_t *out_scales;     // gated
   int32_t *err;
@@ -78,40 +80,85 @@ struct ExpertArgs {
   uint64_t wait_ns;
 };
 
+constexpr int kSortFrom = 64;           // slots an expert on average from which gathered rows are sorted first
+constexpr int kExpertPart = 16;         // K blocks of one accumulator
 constexpr int kExpertStages = 6;
 constexpr int kExpertStageBytes = 2 * kBlockBytes;  // the weights' block, 64 + 64 rows
 constexpr int kExpertSf = 4;            // scale slots (of four K blocks each)
 constexpr int kExpertSfBytes = 3 * 512; // the CTA's half tile, both halves of N
+constexpr int kExpertFew = 72, kExpertMany = 216;  // registers of the first four warps' threads, of the epilogue's
+static_assert(4 * kExpertFew + 8 * kExpertMany <= 12 * kLaunchRegs, "registers");
 constexpr int kSums = 3, kSfCol = 448;  // accumulators of 128 columns, then the scales
 constexpr int kGroup = 2;               // K blocks that one accumulator takes, then the other
 constexpr int kKeyBytes = 2 * 2 * 8 * 128 * 2;   // [half][every other tile][warp of the pair][slot]
 constexpr int kCodeBytes = 2 * 128 * 64;         // [half][slot][feature]
-constexpr int kExpertUsed = 1024 + kExpertStages * kExpertStageBytes + kExpertSf * kExpertSfBytes + 512;
+constexpr int kPowerBytes = 2 * 128 * 4;         // [half][even slots, odd ones]
+constexpr int kExpertBars = 288;
+constexpr int kExpertUsed = 1024 + kExpertStages * kExpertStageBytes + kExpertSf * kExpertSfBytes + kExpertBars;
+constexpr int kTurnPitch = 144, kTurnBytes = 16 * kTurnPitch;  // plain: a warp's 32 features of 32 slots, slots in pairs
 constexpr int expert_smem(bool gated) {
-  const int used = kExpertUsed + (gated ? kKeyBytes + kCodeBytes + 2 * 128 : 0);
+  const int used = kExpertUsed + (gated ? kKeyBytes + kCodeBytes + kPowerBytes : 8 * kTurnBytes);
   return used > smem_floor(512) ? used : smem_floor(512);
 }
-static_assert(expert_smem(true) + (kMostExperts + 64) * 4 <= 227 * 1024, "shared memory");
+static_assert(expert_smem(true) + (kMostExperts + 1) * 4 + 32 * 16 + 128 <= 227 * 1024, "shared memory");
 
-// A tile: slots of one expert by one pair of half tiles.
+// A tile: slots of one expert by one pair of half tiles.  A CTA brings the rows of (n0 + n1) / 2 neighbouring slots, the
+// first n0 / 2 of them for the first half.
 struct ExpertTile {
   int expert, ct, slot0, count;
   int n0, n1;                           // columns of the two halves (multiples of 32; n1 may be 0)
+  // The tile's slot that is column j of half h: the first CTA's rows, then the second one's.
+  __device__ __forceinline__ int slot_at(int h, int j) const {
+    const int mine = (h ? n1 : n0) / 2, first = h ? n0 / 2 : 0;
+    return first + j + (j < mine ? 0 : (n0 + n1) / 2 - mine);
+  }
 };
 
-// g / (1 + exp(-g)): the exponential of -|g|, so that nothing overflows, and a reciprocal of a number in 1..2 (the
-// quotient's general form tests for and mends cases that do not occur here).
+// The rows of the slots, one after another, for products with more rows than a copy by index keeps up with.
+constexpr int kSortWarps = 8;
+__global__ void __launch_bounds__(kSortWarps * 32) sort_rows_kernel(const uint4 *__restrict__ x, const uint32_t *__restrict__ xs,
+                                                                    const int32_t *order, const int32_t *last, int slots, int top_k,
+                                                                    int vecs, int words, uint4 *codes, uint32_t *scales,
+                                                                    int32_t *err) {
+  const int lane = threadIdx.x & 31;
+  const int64_t slot = (int64_t)blockIdx.x * kSortWarps + (threadIdx.x >> 5);
+  grid_dependency_wait();
+  grid_launch_dependents();
+  if (slot >= min(*last, slots)) return;
+  int64_t row = order[slot];
+  if (row < 0 || row >= slots) {
+    if (lane == 0) record_error(err, HAM_DEVERR_ROUTE);
+    row = 0;
+  }
+  row /= top_k;
+  for (int w = lane; w < words; w += 32) scales[slot * words + w] = xs[row * words + w];
+  int v = lane;
+  for (; v + 7 * 32 < vecs; v += 8 * 32) {
+    uint4 r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = x[row * vecs + v + 32 * i];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) codes[slot * vecs + v + 32 * i] = r[i];
+  }
+  for (; v < vecs; v += 32) codes[slot * vecs + v] = x[row * vecs + v];
+}
+
+// Maps of the rows with boxes of 16, 32, 64 and 128 of them; of rows by index the first alone, with boxes of one.
+struct RowMaps {
+  CUtensorMap of[4];
+};
+
+// g / (1 + exp(-g)) by a reciprocal that is within a unit of its last place (a quotient's general form tests for and
+// mends cases that do not occur: 1 + exp(-g) is never below 1).
 __device__ __forceinline__ float silu_of(float g) {
-  const float t = expf(-fabsf(g)), d = 1.f + t;
   float r;
-  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(d));
-  r = fmaf(r, fmaf(-d, r, 1.f), r);
-  return g * (g < 0.f ? t * r : r);
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + expf(-g)));
+  return g * r;
 }
 
 template <bool kGated>
 __global__ void __launch_bounds__(kPairThreads, 1)
-    experts_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ CUtensorMap tw, ExpertArgs a) {
+    experts_kernel(const __grid_constant__ RowMaps tx, const __grid_constant__ CUtensorMap tw, ExpertArgs a) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t *sf = ring + kExpertStages * kExpertStageBytes;
@@ -124,13 +171,13 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   uint64_t *sum_free = sum_full + 2 * kSums;   // [accumulator]: an arrival a warp of the pair that takes it
   uint64_t *keys_full = sum_free + kSums;      // [half][every other tile]: an arrival a warp of the pair
   uint64_t *drained = keys_full + 4;           // every product issued is complete
-  static_assert((2 * kExpertStages + 2 * kExpertSf + 3 * kSums + 5) * 8 <= 512, "barriers");
-  uint16_t *keys = reinterpret_cast<uint16_t *>(reinterpret_cast<uint8_t *>(full) + 512);
+  static_assert((2 * kExpertStages + 2 * kExpertSf + 3 * kSums + 5) * 8 <= kExpertBars, "barriers");
+  uint16_t *keys = reinterpret_cast<uint16_t *>(reinterpret_cast<uint8_t *>(full) + kExpertBars);
   uint8_t *code_rows = reinterpret_cast<uint8_t *>(keys) + kKeyBytes;
-  uint8_t *exponents = code_rows + kCodeBytes; // [half][slot]
+  float *powers = reinterpret_cast<float *>(code_rows + kCodeBytes);
   __shared__ int starts[kMostExperts + 1];     // row tiles of the experts before
   __shared__ int parts_of[12], bad_shared;
-  __shared__ int4 gathered[2][16];             // gated: the rows of a tile's copies
+  __shared__ int4 gathered[32];                // the rows of a tile's copies by index
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_shared, issued_shared;
   volatile int *abort_flag = &abort_shared;
@@ -165,7 +212,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     fence_mbar_init();
   }
   if (warp == 0 && lane == 0) {
-    prefetch_tensormap(&tx);
+    for (int i = 0; i < (a.gather ? 1 : 4); ++i) prefetch_tensormap(&tx.of[i]);
     prefetch_tensormap(&tw);
   }
   cluster_sync_all();
@@ -234,7 +281,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   // The row of the tile's slot i (past the last: the last).
   const auto row_of = [&](const ExpertTile &t, int i) {
     const int slot = t.slot0 + min(i, t.count - 1);
-    if constexpr (!kGated) return slot;
+    if (!a.gather) return slot;
     const int o = a.order[slot];
     if ((uint32_t)o >= (uint32_t)a.slots) {
       record_error(a.err, HAM_DEVERR_ROUTE);
@@ -242,28 +289,24 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     }
     return o / a.top_k;
   };
-  // The copies of a tile by warp 0.  Of each half of N a CTA brings n / 2 rows, as far as the tile has them (what lies in
-  // the others' place does not matter: a row's sums are its own), kRowsEach a copy.
-  constexpr int kRowsEach = kGated ? 4 : 16;
-  struct Source { int w, bytes, copies[2], row[2]; };
+  // The copies of a tile by warp 0: of a CTA's rows those that the tile has (what lies in the others' place does not
+  // matter: a row's sums are its own), up to the next multiple of 16; by index, of four.
+  struct Source { int w, bytes, copies, row; };
   const auto source_of = [&](int64_t w) {
     const ExpertTile t = tile_of(w);
+    const int n = (t.n0 + t.n1) / 2, each = a.gather ? 4 : 16;
     Source from;
     from.bytes = 2 * kBlockBytes;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int n = h ? t.n1 : t.n0, base = h ? t.n0 : 0;
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const int rows = min(max(t.count - base - s * (n / 2), 0), n / 2), copies = (rows + kRowsEach - 1) / kRowsEach;
-        from.bytes += copies * kRowsEach * 128;
-        if (s == side) from.copies[h] = copies, from.row[h] = t.slot0 + base + s * (n / 2);
-      }
-      if constexpr (kGated)                        // lane l: the rows of copy l
-        if (lane < from.copies[h]) {
-          const int i = base + side * (n / 2) + lane * 4;
-          gathered[h][lane] = make_int4(row_of(t, i), row_of(t, i + 1), row_of(t, i + 2), row_of(t, i + 3));
-        }
+    for (int s = 0; s < 2; ++s) {
+      const int copies = (min(max(t.count - s * n, 0), n) + each - 1) / each;
+      from.bytes += copies * each * 128;
+      if (s == side) from.copies = copies;
+    }
+    from.row = t.slot0 + side * n;
+    if (a.gather && lane < from.copies) {
+      const int i = side * n + lane * 4;
+      gathered[lane] = make_int4(row_of(t, i), row_of(t, i + 1), row_of(t, i + 2), row_of(t, i + 3));
     }
     __syncwarp();
     const int half = kGated ? t.ct * 2 + side : min(t.ct * 2 + side, a.tiles - 1);
@@ -276,29 +319,30 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     uint8_t *dst = ring + s * kExpertStageBytes;
     if (side == 0) mbar_arrive_tx(&full[s], (uint32_t)from.bytes);
     tma_load_2d_pair(dst, &tw, 0, (from.w + kb) * (kBlockBytes / 2048), bar, pol);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      dst += h ? 64 * 128 : kBlockBytes;
-      if constexpr (kGated) {
+    dst += kBlockBytes;
+    if (a.gather) {
 #pragma unroll 1
-        for (int c0 = 0; c0 < from.copies[h]; c0 += 4) {
-          int4 r[4];
+      for (int c0 = 0; c0 < from.copies; c0 += 4) {
+        int4 r[4];
 #pragma unroll
-          for (int c = 0; c < 4; ++c) r[c] = gathered[h][c0 + c];
-#pragma unroll
-          for (int c = 0; c < 4; ++c)
-            if (c0 + c < from.copies[h]) tma_gather4_pair(dst + (c0 + c) * 512, &tx, kb * kFp8Block, r[c], bar, pol);
-        }
-      } else {
+        for (int c = 0; c < 4; ++c) r[c] = gathered[c0 + c];
 #pragma unroll
         for (int c = 0; c < 4; ++c)
-          if (c < from.copies[h]) tma_load_2d_pair(dst + c * 2048, &tx, kb * kFp8Block, from.row[h] + c * 16, bar, pol);
+          if (c0 + c < from.copies) tma_gather4_pair(dst + (c0 + c) * 512, &tx.of[0], kb * kFp8Block, r[c], bar, pol);
       }
+    } else {
+      int done = 0;
+#pragma unroll
+      for (int i = 3; i >= 0; --i)
+        if (from.copies >> i & 1) {
+          tma_load_2d_pair(dst + done * 2048, &tx.of[i], kb * kFp8Block, from.row + done * 16, bar, pol);
+          done += 1 << i;
+        }
     }
   };
   int issued = 0;
   if (warp < 4) {
-    setmaxnreg_dec<kFewRegs>();
+    setmaxnreg_dec<kExpertFew>();
     if (warp == 0) {
       // ------------------------------------------------------------ copies
       const uint64_t pol = policy_evict_last();
@@ -335,8 +379,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           const int halves = t.n1 ? 2 : 1;
           const uint32_t alone = halves == 1 && (singles++ & 1);  // the second group's turn
           const uint32_t idesc_half[2] = {idesc_mx(256, t.n0, 0), idesc_mx(256, t.n1, 0)};
-          for (int g = 0, in = 0, most = kSumFirst; g < a.kbs; g += kGroup) {  // in: blocks of this part so far
-            const bool two = g + 1 < a.kbs, ends = g + kGroup >= a.kbs || in + kGroup >= most;
+          for (int g = 0, in = 0; g < a.kbs; g += kGroup) {  // in: blocks of this part so far
+            const bool two = g + 1 < a.kbs, ends = g + kGroup >= a.kbs || in + kGroup >= kExpertPart;
             const int s1 = s + 1 == kExpertStages ? 0 : s + 1;
             if ((g & 3) == 0) {
               ok = ok && thread_wait_cluster(&sf_full[slot], word_phase, abort_flag);
@@ -371,7 +415,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
                   if (!ok) break;
                   tc_fence_after();
                 }
-                const uint64_t wt = blocks + (uint32_t)(st * (kExpertStageBytes / 16)), x = wt + (uint32_t)(kBlockBytes + h * 64 * 128) / 16;
+                const uint64_t wt = blocks + (uint32_t)(st * (kExpertStageBytes / 16)), x = wt + (uint32_t)(kBlockBytes + (h ? t.n0 / 2 * 128 : 0)) / 16;
 #pragma unroll
                 for (int kk = 0; kk < 4; ++kk)
                   tc_mma_mx<2>(acc, wt + kk * 2, x + kk * 2, idesc + j * kNextByte, sft, sft + 4 + 4 * h, in + j + kk > 0);
@@ -391,7 +435,6 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             in += kGroup;
             if (ends) {
               in = 0;
-              most = kSumNext;
               use += halves;
             }
           }
@@ -413,8 +456,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           const ExpertTile t = tile_of(w);
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const int i = lane + 32 * (j & 3), n = j < 4 ? t.n0 : t.n1;
-            rows[j] = i < n ? row_of(t, (j < 4 ? 0 : t.n0) + i) : -1;
+            const int i = lane + 32 * (j & 3);
+            rows[j] = i < (j < 4 ? t.n0 : t.n1) ? row_of(t, t.slot_at(j >> 2, i)) : -1;
           }
           wrow = kGated ? (t.expert * a.tiles + t.ct) * 2 + (lane >> 4) : t.expert * a.tiles + min(t.ct * 2 + side, a.tiles - 1);
           known = w;
@@ -449,12 +492,12 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       }
     }
   } else {
-    setmaxnreg_inc<kManyRegs>();
+    setmaxnreg_inc<kExpertMany>();
     // ------------------------------------------------------------ epilogue: a feature a thread
     // Four warps take the first half's sums, four the second's; tiles of one half in turn.
     const int quarter = warp & 3, group = (warp - 4) >> 2;
     const uint32_t free_bar = cluster_map_shared(smem_u32(sum_free), 0);
-    const int parts = 1 + (max(a.kbs - kSumFirst, 0) + kSumNext - 1) / kSumNext;
+    const int parts = (a.kbs + kExpertPart - 1) / kExpertPart;
     uint32_t use = 0, singles = 0;               // accumulators, tiles of one half so far
     uint32_t got = 0, taken = 0;                 // accumulators, tiles that this group took
     for (int64_t w = cluster; w < total; w += clusters) {
@@ -467,11 +510,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         if ((singles++ & 1) != (uint32_t)group) continue;
         half = 0;
       }
-      const int n = half ? t.n1 : t.n0, base = half ? t.n0 : 0;
-      const int live = min(n, t.count - base);   // slots of this half
+      const int n = half ? t.n1 : t.n0;
       float v[128];                              // a feature's sums, slot after slot
-#pragma unroll
-      for (int j = 0; j < 128; ++j) v[j] = 0.f;
       bool ok = true;
 #pragma unroll 1
       for (int c = 0; c < parts; ++c) {
@@ -486,85 +526,124 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         }
         tc_fence_after();
         const uint32_t acc = tmem + u % kSums * 128 + ((uint32_t)(quarter * 32) << 16);
+        if (c == 0) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (q * 32 < n) {
-            float f[32];
-            tmem_ld32(acc + q * 32, *reinterpret_cast<uint32_t(*)[32]>(f));
-            tmem_wait_ld();
+          for (int q = 0; q < 4; ++q)
+            if (q * 32 < n) tmem_ld32(acc + q * 32, *reinterpret_cast<uint32_t(*)[32]>(v + q * 32));
+          tmem_wait_ld();
+        } else {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[q * 32 + j] += f[j];
-          }
+          for (int q = 0; q < 4; ++q)
+            if (q * 32 < n) {
+              float f[32];
+              tmem_ld32(acc + q * 32, *reinterpret_cast<uint32_t(*)[32]>(f));
+              tmem_wait_ld();
+#pragma unroll
+              for (int j = 0; j < 32; ++j) v[q * 32 + j] += f[j];
+            }
+        }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster_relaxed(free_bar + u % kSums * 8);
       }
-      const int64_t slot0 = t.slot0 + base;
       if constexpr (!kGated) {
         if (!ok) break;
-        const int f = t.ct * 256 + side * 128 + quarter * 32 + lane;
-        if (f < a.n) {
+        const int f0 = t.ct * 256 + side * 128 + quarter * 32;
+        if (!a.f32 && (a.n & 7) == 0) {
+          // Pairs of slots as words, turned in shared memory: a lane then writes 8 features of two slots.  (Straight from
+          // the registers, 2 bytes a lane, 4096 rows of 8 experts took 248 us.)
+          uint8_t *turn = reinterpret_cast<uint8_t *>(keys) + (warp - 4) * kTurnBytes;
+          const int pair = lane >> 2, c = (lane & 3) * 8;
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
-            if (q * 32 < live) {
-              if (a.f32) {
-                float *out = static_cast<float *>(a.out) + (slot0 + q * 32) * a.n + f;
+          for (int q = 0; q < 4; ++q) {
+            if (q * 32 >= n) continue;
+            __syncwarp();
 #pragma unroll
-                for (int j = 0; j < 32; ++j)
-                  if (q * 32 + j < live) out[(int64_t)j * a.n] = v[q * 32 + j];
-              } else {
-                __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(a.out) + (slot0 + q * 32) * a.n + f;
+            for (int j = 0; j < 16; ++j)
+              *reinterpret_cast<uint32_t *>(turn + j * kTurnPitch + lane * 4) = pack_bf16x2(v[q * 32 + 2 * j], v[q * 32 + 2 * j + 1]);
+            __syncwarp();
 #pragma unroll
-                for (int j = 0; j < 32; ++j)
-                  if (q * 32 + j < live) out[(int64_t)j * a.n] = __float2bfloat16_rn(v[q * 32 + j]);
+            for (int i = 0; i < 2; ++i) {
+              const uint4 x = *reinterpret_cast<const uint4 *>(turn + (pair + 8 * i) * kTurnPitch + c * 4);
+              const uint4 y = *reinterpret_cast<const uint4 *>(turn + (pair + 8 * i) * kTurnPitch + c * 4 + 16);
+              const int slot = t.slot_at(half, q * 32 + 2 * (pair + 8 * i));   // (and the next: 16 columns are neighbours)
+              if (f0 + c < a.n) {
+                __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(a.out) + (int64_t)(t.slot0 + slot) * a.n + f0 + c;
+                if (slot < t.count)
+                  *reinterpret_cast<uint4 *>(out) = make_uint4(__byte_perm(x.x, x.y, 0x5410), __byte_perm(x.z, x.w, 0x5410),
+                                                               __byte_perm(y.x, y.y, 0x5410), __byte_perm(y.z, y.w, 0x5410));
+                if (slot + 1 < t.count)
+                  *reinterpret_cast<uint4 *>(out + a.n) = make_uint4(__byte_perm(x.x, x.y, 0x7632), __byte_perm(x.z, x.w, 0x7632),
+                                                                     __byte_perm(y.x, y.y, 0x7632), __byte_perm(y.z, y.w, 0x7632));
               }
             }
+          }
+        } else if (f0 + lane < a.n) {
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {            // (16 columns are neighbouring slots)
+            const int slot = t.slot_at(half, q * 16), live = q * 16 < n ? t.count - slot : 0;
+            if (live <= 0) continue;
+            const int64_t to = (int64_t)(t.slot0 + slot) * a.n + f0 + lane;
+            if (a.f32) {
+              float *out = static_cast<float *>(a.out) + to;
+#pragma unroll
+              for (int j = 0; j < 16; ++j)
+                if (j < live) out[(int64_t)j * a.n] = v[q * 16 + j];
+            } else {
+              __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(a.out) + to;
+#pragma unroll
+              for (int j = 0; j < 16; ++j)
+                if (j < live) out[(int64_t)j * a.n] = __float2bfloat16_rn(v[q * 16 + j]);
+            }
+          }
         }
       } else {
         const int buffer = group * 2 + (taken & 1);
         uint16_t *key = keys + buffer * (8 * 128);
-        float h[64];                             // slot 2 i + lane / 16 of feature 16 quarter + lane % 16
+        const bool upper = lane & 16;
+        float h[64];                             // column 2 i + lane / 16 of feature 16 quarter + lane % 16
         if (ok) {
-          const bool upper = lane & 16;
-          uint32_t m[32];                          // 16 bits of h[2 i], of h[2 i + 1]
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
+            if (q * 32 < n) {
 #pragma unroll
-            for (int i = 8 * q; i < 8 * q + 8; ++i) m[i] = 0;
-            if (q * 32 >= n) continue;
+              for (int i = 16 * q; i < 16 * q + 16; ++i) {
+                const float other = __shfl_xor_sync(kFull, upper ? v[2 * i] : v[2 * i + 1], 16);
+                const float own = upper ? v[2 * i + 1] : v[2 * i];
+                h[i] = silu_of(upper ? other : own) * (upper ? own : other);
+              }
+            } else {
 #pragma unroll
-            for (int i = 16 * q; i < 16 * q + 16; ++i) {
-              const float other = __shfl_xor_sync(kFull, upper ? v[2 * i] : v[2 * i + 1], 16);
-              const float own = upper ? v[2 * i + 1] : v[2 * i];
-              h[i] = silu_of(upper ? other : own) * (upper ? own : other);
-              const uint32_t u = __float_as_uint(h[i]) & 0x7fffffffu;
-              const uint32_t b = u > 0x7f800000u ? 0u : (u >> 16) | (u != 0u);   // (NaN counts for nothing)
-              m[i / 2] |= i & 1 ? b << 16 : b;
+              for (int i = 16 * q; i < 16 * q + 16; ++i) h[i] = 0.f;
             }
           }
-          // the largest over the 16 lanes of a slot: lanes swap what the other half of them will go on with
+          // the largest over the 16 lanes of a column (NaN counts for nothing): lanes swap what the other half of
+          // them will go on with, and end with those of h[4 (lane % 16)] .. h[4 (lane % 16) + 3]
+          float m[32];
 #pragma unroll
-          for (int o = 8, c = 16; o > 0; o >>= 1, c >>= 1)
+          for (int i = 0; i < 32; ++i) {
+            const bool high = lane & 8;
+            const float other = __shfl_xor_sync(kFull, high ? h[i] : h[32 + i], 8);
+            m[i] = fmaxf(fabsf(high ? h[32 + i] : h[i]), fabsf(other));
+          }
+#pragma unroll
+          for (int o = 4, c = 16; o > 0; o >>= 1, c >>= 1)
 #pragma unroll
             for (int i = 0; i < c; ++i) {
               const bool high = lane & o;
-              const uint32_t got = __shfl_xor_sync(kFull, high ? m[i] : m[c + i], o);
-              m[i] = __vmaxu2(high ? m[c + i] : m[i], got);
+              const float other = __shfl_xor_sync(kFull, high ? m[i] : m[c + i], o);
+              m[i] = fmaxf(high ? m[c + i] : m[i], other);
             }
-          // m[0], m[1]: words 2 (bits 3..0 of the lane, the highest first) + 0, 1, each of slots 4 i + lane / 16 and
-          // two further on
-          const int word = (lane & 8 ? 16 : 0) + (lane & 4 ? 8 : 0) + (lane & 2 ? 4 : 0) + (lane & 1 ? 2 : 0);
           uint16_t *mine = key + (side * 4 + quarter) * 128;
           const uint32_t theirs = cluster_map_shared(smem_u32(mine), side ^ 1);
 #pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const int slot = 4 * (word + i) + 2 * j + (lane >> 4);
-              const uint16_t b = (uint16_t)(m[i] >> 16 * j);
-              mine[slot] = b;
-              asm volatile("st.shared::cluster.u16 [%0], %1;" ::"r"(theirs + slot * 2), "h"(b) : "memory");
-            }
+          for (int i = 0; i < 4; ++i) {
+            const int column = 8 * (lane & 15) + 2 * i + (lane >> 4);
+            const uint32_t u = __float_as_uint(m[i]);
+            const uint16_t b = (uint16_t)(u > 0x7f800000u ? 0u : (u >> 16) | (u != 0u));
+            mine[column] = b;
+            asm volatile("st.shared::cluster.u16 [%0], %1;" ::"r"(theirs + column * 2), "h"(b) : "memory");
+          }
           __syncwarp();
           if (lane < 2) mbar_arrive_cluster(cluster_map_shared(smem_u32(&keys_full[buffer]), lane));
           ok = warp_wait_cluster(&keys_full[buffer], (taken >> 1) & 1u, abort_flag);
@@ -573,39 +652,43 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         ++taken;
         ok = named_barrier_and(1 + group, 128, ok);  // (they meet below: all go on or none)
         if (!ok) break;
-        const int slot = quarter * 32 + lane;      // a slot's scale a thread
-        uint32_t top = 0;
+        float *power = powers + group * 128;
+        {
+          const int column = quarter * 32 + lane, slot = t.slot_at(half, column);  // a slot's scale a thread
+          uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, (uint32_t)key[i * 128 + slot]);
-        const int e = fp8_exponent(__uint_as_float(top << 16));
-        uint8_t *exponent = exponents + group * 128;
-        exponent[slot] = (uint8_t)(e + 127);
-        if (side == 0 && slot < live) {
-          uint8_t *s = a.out_scales + (slot0 + slot) * a.out_sk;
-          s[t.ct] = (uint8_t)(e + 127);
-          if (t.ct == a.tiles - 1)
-            for (int b = a.tiles; b < a.out_sk; ++b) s[b] = 127;  // padding
-        }
-        named_barrier(1 + group, 128);
-        uint8_t *codes = code_rows + group * (128 * 64);
-        const int feature = quarter * 16 + (lane & 15);
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          if (4 * i < live) {                      // slots 4 i + lane / 16 and two further on
-            const uint32_t es = *reinterpret_cast<const uint32_t *>(exponent + 4 * i) >> (lane & 16 ? 8 : 0);
-            const float p = fp8_pow2(127 - (int)(es & 0xffu)), q = fp8_pow2(127 - (int)(es >> 16 & 0xffu));
-            const uint32_t c = fp8_codes4(h[2 * i] * p, h[2 * i + 1] * q, 0.f, 0.f, 1.f);
-            uint8_t *to = codes + (4 * i + (lane >> 4)) * 64 + feature;
-            to[0] = (uint8_t)c;
-            to[128] = (uint8_t)(c >> 8);
+          for (int i = 0; i < 8; ++i) top = max(top, (uint32_t)key[i * 128 + column]);
+          const int e = fp8_exponent(__uint_as_float(top << 16));
+          power[(column & 1) * 64 + (column >> 1)] = fp8_pow2(-e);
+          if (side == 0 && column < n && slot < t.count) {
+            uint8_t *s = a.out_scales + (int64_t)(t.slot0 + slot) * a.out_sk;
+            s[t.ct] = (uint8_t)(e + 127);
+            if (t.ct == a.tiles - 1)
+              for (int b = a.tiles; b < a.out_sk; ++b) s[b] = 127;  // padding
           }
         }
         named_barrier(1 + group, 128);
-        const int c = (slot & 3) * 16, col = t.ct * kTile + side * 64 + c;
-        for (int r = slot >> 2; r < live; r += 32)
-          if (col < a.n)                           // (n is a multiple of 16)
-            *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(a.out) + (slot0 + r) * a.n + col) =
+        uint8_t *codes = code_rows + group * (128 * 64);
+        uint8_t *to = codes + (lane >> 4) * 64 + quarter * 16 + (lane & 15);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (q * 32 < n) {
+#pragma unroll
+            for (int i = 16 * q; i < 16 * q + 16; i += 4) {
+              const float4 p = *reinterpret_cast<const float4 *>(power + (lane >> 4) * 64 + i);
+              const uint32_t c = fp8_codes4(h[i] * p.x, h[i + 1] * p.y, h[i + 2] * p.z, h[i + 3] * p.w, 1.f);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) to[(i + j) * 128] = (uint8_t)(c >> 8 * j);
+            }
+          }
+        named_barrier(1 + group, 128);
+        const int c = (lane & 3) * 16, col = t.ct * kTile + side * 64 + c;
+        for (int r = quarter * 8 + (lane >> 2); r < n; r += 32) {
+          const int slot = t.slot_at(half, r);
+          if (slot < t.count && col < a.n)         // (n is a multiple of 16)
+            *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(a.out) + (int64_t)(t.slot0 + slot) * a.n + col) =
                 *reinterpret_cast<const uint4 *>(codes + r * 64 + c);
+        }
         named_barrier(1 + group, 128);             // (read before the next tile's are written)
       }
     }
@@ -641,7 +724,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
 }
 
 template <bool kGated>
-cudaError_t launch_experts(const CUtensorMap &tx, const CUtensorMap &tw, const ExpertArgs &a, int dev, cudaStream_t s) {
+cudaError_t launch_experts(const RowMaps &tx, const CUtensorMap &tw, const ExpertArgs &a, int dev, cudaStream_t s) {
   static bool done[64] = {};
   static int resident[64] = {};
   constexpr auto kKernel = experts_kernel<kGated>;
@@ -658,6 +741,30 @@ cudaError_t launch_experts(const CUtensorMap &tx, const CUtensorMap &tw, const E
   const int64_t most = ((int64_t)a.slots / 256 + std::min(a.slots, a.experts)) * cols;  // tiles at most
   const int64_t pairs = std::min<int64_t>(resident_pairs(kKernel, kSmem, resident, dev), most);
   return launch_after<kKernel>(dim3((unsigned)(2 * pairs)), dim3(kPairThreads), (size_t)kSmem, dim3(2, 1, 1), s, tx, tw, a);
+}
+
+// The device's pool for sorted rows: ordered by the stream (a captured call's belong to its graph), what it has once
+// been given stays with it.
+cudaMemPool_t row_pool(int dev) {
+  static std::mutex guard;
+  static cudaMemPool_t pools[64] = {};
+  if (dev < 0 || dev >= 64) return nullptr;
+  std::lock_guard<std::mutex> lock(guard);
+  if (!pools[dev]) {
+    cudaMemPoolProps props = {};
+    props.allocType = cudaMemAllocationTypePinned;
+    props.location.type = cudaMemLocationTypeDevice;
+    props.location.id = dev;
+    cudaMemPool_t pool = nullptr;
+    if (cudaMemPoolCreate(&pool, &props) != cudaSuccess) {
+      cudaGetLastError();
+      return nullptr;
+    }
+    uint64_t all = UINT64_MAX;
+    cudaMemPoolSetAttribute(pool, cudaMemPoolAttrReleaseThreshold, &all);
+    pools[dev] = pool;
+  }
+  return pools[dev];
 }
 
 int check_experts(const ham_fp8_weight *w, const void *xc, const void *xs, int64_t slots, const void *offsets,
@@ -682,16 +789,37 @@ int run_experts(ham_fp8_weight *w, const void *x_codes, int32_t rows, ExpertArgs
   a.out_sk = fp8_scale_bytes(w->n);
   a.tiles = w->tiles;
   a.wait_ns = w->wait_ns;
-  CUtensorMap tx;
-  int rc = HAM_OK;
-  if (make_bytes_tensor_map(&tx, x_codes, rows, w->k, kFp8Block, w->parts == 2 ? 1 : 16) != 0) {
-    rc = op_fail(HAM_ECUDA, "tensor map of the rows");
-  } else {
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = w->parts == 2 ? launch_experts<true>(tx, w->map, a, w->device, s)
-                                        : launch_experts<false>(tx, w->map, a, w->device, s);
-    if (e != cudaSuccess) rc = op_fail(HAM_ECUDA, "experts launch: %s", cudaGetErrorString(e));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaError_t e = cudaSuccess;
+  uint8_t *sorted = nullptr;
+  // Copies by index take some 80 clocks for four rows, boxes of neighbouring rows four a row.
+  if (a.gather && a.slots > kSortFrom * a.experts) {
+    const size_t codes = (size_t)a.slots * w->k, scales = (size_t)a.slots * w->sk;
+    cudaMemPool_t pool = row_pool(w->device);
+    if (pool && cudaMallocFromPoolAsync(reinterpret_cast<void **>(&sorted), codes + scales, pool, s) != cudaSuccess) {
+      cudaGetLastError();
+      sorted = nullptr;                            // (by index, then)
+    }
+    if (sorted) {
+      e = launch_after<sort_rows_kernel>(dim3((unsigned)((a.slots + kSortWarps - 1) / kSortWarps)), dim3(kSortWarps * 32), 0, dim3(1), s,
+                                         static_cast<const uint4 *>(x_codes), reinterpret_cast<const uint32_t *>(a.xs), a.order,
+                                         a.offsets + a.experts, a.slots, a.top_k, w->k / 16, w->sk / 4,
+                                         reinterpret_cast<uint4 *>(sorted), reinterpret_cast<uint32_t *>(sorted + codes), a.err);
+      x_codes = sorted;
+      a.xs = sorted + codes;
+      a.gather = 0;
+      rows = a.slots;
+    }
   }
+  RowMaps tx;
+  int rc = HAM_OK;
+  for (int i = 0; i < (a.gather ? 1 : 4); ++i)
+    if (make_bytes_tensor_map(&tx.of[i], x_codes, rows, w->k, kFp8Block, a.gather ? 1 : 16 << i) != 0)
+      rc = op_fail(HAM_ECUDA, "tensor map of the rows");
+  if (rc == HAM_OK && e == cudaSuccess)
+    e = w->parts == 2 ? launch_experts<true>(tx, w->map, a, w->device, s) : launch_experts<false>(tx, w->map, a, w->device, s);
+  if (sorted) cudaFreeAsync(sorted, s);
+  if (rc == HAM_OK && e != cudaSuccess) rc = op_fail(HAM_ECUDA, "experts launch: %s", cudaGetErrorString(e));
   if (dev != w->device) cudaSetDevice(dev);
   return rc;
 }
@@ -797,6 +925,7 @@ int ham_fp8_experts_gated(ham_fp8_weight *w, const void *x_codes, const void *x_
   a.xs = static_cast<const uint8_t *>(x_scales);
   a.offsets = offsets;
   a.order = order;
+  a.gather = 1;
   a.top_k = top_k;
   a.slots = (int)slots;
   a.out = codes;
