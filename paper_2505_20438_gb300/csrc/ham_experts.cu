@@ -51,17 +51,18 @@ __global__ void lay_out_expert_scales_kernel(const uint8_t *__restrict__ scales,
 }
 
 // ------------------------------------------------------------------------------------
-// The kernel: pairs of CTAs, 256 rows of weights by up to 256 slots
+// The kernel: pairs of CTAs, 256 rows of weights by up to 224 slots
 // ------------------------------------------------------------------------------------
 // The weights are the product's M: a pair of CTAs (cta_group::2) multiplies two half tiles, one a CTA (128 lanes of its
 // tensor memory), with the N rows of one expert's slots.  N is what the expert has, up to the next multiple of 32, so
-// that a few rows cost a few rows' products and many experts of uneven counts leave no lanes idle.  More than 256 slots
-// are cut into tiles of equal size, more than 128 into two halves of N, each an accumulator of its own.
+// that a few rows cost a few rows' products and many experts of uneven counts leave no lanes idle.  More than 224 slots
+// are cut into tiles of equal size, more than 128 into two halves of N, each for four warps of the epilogue.
 //
 // Each CTA copies its half tile's K block (16 KiB, one stretch) and half of the N rows (a gated product's four rows a
 // copy, by index, from where they lie), into its own shared memory alone.  Sums take parts of K as
-// the products of one weight do (ham_fp8.cu), kExpertPart blocks each, in three accumulators of 128 columns that are used in
-// turn; the epilogue adds them in registers.
+// the products of one weight do (ham_fp8.cu), kExpertPart blocks each, in two sums of 224 columns in turn, so that a whole
+// tile's products (of two parts) are on their way while the epilogue deals with the tile before; it adds them in
+// registers.
 //
 // A thread of the epilogue has one feature (a lane) and up to 128 slots (columns).  Plain outputs are neighbours across
 // a warp's lanes.  Of a gated product lanes 0..15 hold the gate and 16..31 the up projection of 16 features: one shuffle
@@ -88,7 +89,7 @@ constexpr int kExpertSf = 4;            // scale slots (of four K blocks each)
 constexpr int kExpertSfBytes = 3 * 512; // the CTA's half tile, both halves of N
 constexpr int kExpertFew = 72, kExpertMany = 216;  // registers of the first four warps' threads, of the epilogue's
 static_assert(4 * kExpertFew + 8 * kExpertMany <= 12 * kLaunchRegs, "registers");
-constexpr int kSums = 3, kSfCol = 448;  // accumulators of 128 columns, then the scales
+constexpr int kTileSlots = 224, kSfCol = 448;  // columns of one of the two sums, and behind both the scales
 constexpr int kGroup = 2;               // K blocks that one accumulator takes, then the other
 constexpr int kKeyBytes = 2 * 2 * 8 * 128 * 2;   // [half][every other tile][warp of the pair][slot]
 constexpr int kCodeBytes = 2 * 128 * 64;         // [half][slot][feature]
@@ -167,11 +168,11 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   uint64_t *empty = full + kExpertStages;
   uint64_t *sf_full = empty + kExpertStages;   // an arrival a CTA
   uint64_t *sf_empty = sf_full + kExpertSf;
-  uint64_t *sum_full = sf_empty + kExpertSf;   // [epilogue group][its accumulators in turn]
-  uint64_t *sum_free = sum_full + 2 * kSums;   // [accumulator]: an arrival a warp of the pair that takes it
-  uint64_t *keys_full = sum_free + kSums;      // [half][every other tile]: an arrival a warp of the pair
+  uint64_t *sum_full = sf_empty + kExpertSf;   // [epilogue group][its parts in turn]
+  uint64_t *sum_free = sum_full + 4;           // [sum][half]: an arrival a warp of the pair that takes it
+  uint64_t *keys_full = sum_free + 4;          // [half][every other tile]: an arrival a warp of the pair
   uint64_t *drained = keys_full + 4;           // every product issued is complete
-  static_assert((2 * kExpertStages + 2 * kExpertSf + 3 * kSums + 5) * 8 <= kExpertBars, "barriers");
+  static_assert((2 * kExpertStages + 2 * kExpertSf + 13) * 8 <= kExpertBars, "barriers");
   uint16_t *keys = reinterpret_cast<uint16_t *>(reinterpret_cast<uint8_t *>(full) + kExpertBars);
   uint8_t *code_rows = reinterpret_cast<uint8_t *>(keys) + kKeyBytes;
   float *powers = reinterpret_cast<float *>(code_rows + kCodeBytes);
@@ -203,9 +204,11 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       mbar_init(&sf_full[s], 2);
       mbar_init(&sf_empty[s], 1);
     }
-    for (int s = 0; s < 2 * kSums; ++s) mbar_init(&sum_full[s], 1);
-    for (int s = 0; s < kSums; ++s) mbar_init(&sum_free[s], 8);
-    for (int s = 0; s < 4; ++s) mbar_init(&keys_full[s], 8);
+    for (int s = 0; s < 4; ++s) {
+      mbar_init(&sum_full[s], 1);
+      mbar_init(&sum_free[s], 8);
+      mbar_init(&keys_full[s], 8);
+    }
     mbar_init(drained, 1);
     abort_shared = 0;
     bad_shared = 0;
@@ -230,7 +233,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       if (e < a.experts) {
         const int from = a.offsets[e], to = a.offsets[e + 1];
         if (from < 0 || to < from || to > a.slots) bad_shared = 1;
-        else tiles_of[i] = (to - from + 255) >> 8;
+        else tiles_of[i] = (to - from + kTileSlots - 1) / kTileSlots;
       }
       sum += tiles_of[i];
     }
@@ -370,9 +373,15 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         bool ok = true;
         int s = 0, slot = 0;                     // of the block, of the scale word
         uint32_t phase = 0, word_phase = 0, which = 0;
-        uint32_t use = 0, singles = 0, given0 = 0, given1 = 0;  // accumulators, tiles of one half, each group's accumulators so far
-        const auto free_sum = [&](uint32_t u) {
-          return u < kSums || thread_wait_cluster(&sum_free[u % kSums], (u / kSums - 1) & 1u, abort_flag);
+        uint32_t part = 0, singles = 0, given[2] = {0, 0};  // parts, tiles of one half, each group's parts so far
+        uint32_t used[2][2] = {{0, 0}, {0, 0}};    // [sum][half]: how often
+        // Both halves of a sum are free.
+        const auto free_sum = [&](int b) {
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t n = b ? used[1][h] : used[0][h];
+            if (n && !thread_wait_cluster(&sum_free[b * 2 + h], (n - 1) & 1u, abort_flag)) return false;
+          }
+          return true;
         };
         for (int64_t w = cluster; w < total && ok; w += clusters) {
           const ExpertTile t = tile_of(w);
@@ -387,7 +396,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
               which ^= 16;
             }
             ok = ok && thread_wait_cluster(&full[s], phase, abort_flag);
-            if (in == 0) ok = ok && free_sum(use);
+            if (in == 0) ok = ok && free_sum(part & 1);
             if (!ok) break;
             tc_fence_after();
             const uint32_t sft = tmem + kSfCol + which;
@@ -401,11 +410,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               if (h >= halves) break;
-              if (h && in == 0) {
-                if (!free_sum(use + 1)) { ok = false; break; }
-                tc_fence_after();
-              }
-              const uint32_t acc = tmem + (use + h) % kSums * 128, idesc = idesc_half[h] + (g & 3) * kNextByte;
+              const uint32_t acc = tmem + (part & 1) * kTileSlots + (h ? t.n0 : 0), idesc = idesc_half[h] + (g & 3) * kNextByte;
 #pragma unroll
               for (int j = 0; j < kGroup; ++j) {
                 if (j && !two) break;
@@ -423,10 +428,10 @@ __global__ void __launch_bounds__(kPairThreads, 1)
               }
               if (!ok) break;
               if (ends) {
-                const bool second = h || alone;
-                tc_commit_pair(&sum_full[second ? kSums + given1 % kSums : given0 % kSums], both);
-                if (second) ++given1;
-                else ++given0;
+                if (h || alone) tc_commit_pair(&sum_full[2 + (given[1]++ & 1)], both);
+                else tc_commit_pair(&sum_full[given[0]++ & 1], both);
+                if (part & 1) ++used[1][h];
+                else ++used[0][h];
               }
             }
             if (!ok) break;
@@ -435,7 +440,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             in += kGroup;
             if (ends) {
               in = 0;
-              use += halves;
+              ++part;
             }
           }
         }
@@ -498,14 +503,14 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     const int quarter = warp & 3, group = (warp - 4) >> 2;
     const uint32_t free_bar = cluster_map_shared(smem_u32(sum_free), 0);
     const int parts = (a.kbs + kExpertPart - 1) / kExpertPart;
-    uint32_t use = 0, singles = 0;               // accumulators, tiles of one half so far
-    uint32_t got = 0, taken = 0;                 // accumulators, tiles that this group took
+    uint32_t first = 0, singles = 0;             // parts, tiles of one half so far
+    uint32_t got = 0, taken = 0;                 // parts, tiles that this group took
     for (int64_t w = cluster; w < total; w += clusters) {
       const ExpertTile t = tile_of(w);
       const int halves = t.n1 ? 2 : 1;
       int half = group;
-      const uint32_t first = use;
-      use += parts * halves;
+      const uint32_t sum = first;
+      first += parts;
       if (halves == 1) {
         if ((singles++ & 1) != (uint32_t)group) continue;
         half = 0;
@@ -515,17 +520,17 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       bool ok = true;
 #pragma unroll 1
       for (int c = 0; c < parts; ++c) {
-        const uint32_t u = first + c * halves + half;
-        // (a group waits for accumulators of its own alone, each barrier's phases in order; of them three at most are
-        // full and not yet taken)
-        ok = warp_wait_cluster(&sum_full[group * kSums + got % kSums], (got / kSums) & 1u, abort_flag);
+        const int b = (int)(sum + c & 1);
+        // (a group waits for parts of its own alone, each barrier's phases in order: of them two at most are full and
+        // not yet taken)
+        ok = warp_wait_cluster(&sum_full[group * 2 + (got & 1)], (got >> 1) & 1u, abort_flag);
         ++got;
         if (!ok) {
           if (lane == 0) give_up();
           break;
         }
         tc_fence_after();
-        const uint32_t acc = tmem + u % kSums * 128 + ((uint32_t)(quarter * 32) << 16);
+        const uint32_t acc = tmem + b * kTileSlots + (half ? t.n0 : 0) + ((uint32_t)(quarter * 32) << 16);
         if (c == 0) {
 #pragma unroll
           for (int q = 0; q < 4; ++q)
@@ -544,7 +549,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster_relaxed(free_bar + u % kSums * 8);
+        if (lane == 0) mbar_arrive_cluster_relaxed(free_bar + (b * 2 + half) * 8);
       }
       if constexpr (!kGated) {
         if (!ok) break;
@@ -738,7 +743,7 @@ cudaError_t launch_experts(const RowMaps &tx, const CUtensorMap &tw, const Exper
   const cudaError_t e = allow_smem(kKernel, kSmem, done, dev);
   if (e != cudaSuccess) return e;
   const int64_t cols = kGated ? a.tiles : (a.tiles + 1) / 2;
-  const int64_t most = ((int64_t)a.slots / 256 + std::min(a.slots, a.experts)) * cols;  // tiles at most
+  const int64_t most = ((int64_t)a.slots / kTileSlots + std::min(a.slots, a.experts)) * cols;  // tiles at most
   const int64_t pairs = std::min<int64_t>(resident_pairs(kKernel, kSmem, resident, dev), most);
   return launch_after<kKernel>(dim3((unsigned)(2 * pairs)), dim3(kPairThreads), (size_t)kSmem, dim3(2, 1, 1), s, tx, tw, a);
 }
