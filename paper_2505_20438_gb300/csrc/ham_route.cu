@@ -9,6 +9,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cfloat>
 
 #include "ham_ops.cuh"
@@ -18,12 +19,21 @@ namespace ham {
 namespace {
 
 constexpr int kMostExperts = 512, kMostTop = 32;
-constexpr int kChooseWarps = 8;          // rows of a block
+constexpr int kChooseWarps = 8, kChooseBlocks = 4;  // warps of a block, blocks an SM
+
+template <typename K>
+cudaError_t allow(K kernel, int bytes, bool (&done)[64], int dev) {
+  if (dev >= 0 && dev < 64 && done[dev]) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && dev >= 0 && dev < 64) done[dev] = true;
+  return e;
+}
 
 struct RouteArgs {
   const void *logits;      // [rows][experts] bf16 or f32
   const float *bias;       // nullable
-  int f32, rows, experts, top_k, sigmoid, groups, top_groups, renorm;
+  int f32, wide;           // wide: rows of whole 16 bytes
+  int rows, experts, top_k, sigmoid, groups, top_groups, renorm;
   float scale;
   int32_t *expert;         // [rows][top_k]
   float *weight;
@@ -31,15 +41,14 @@ struct RouteArgs {
 };
 
 // A logit as the formulas take it: -inf rules out (NaN too).
-__device__ __forceinline__ float read_logit(const RouteArgs &a, int64_t at) {
-  float l = a.f32 ? static_cast<const float *>(a.logits)[at]
-                  : __bfloat162float(static_cast<const __nv_bfloat16 *>(a.logits)[at]);
-  if (!(l > -INFINITY)) return -INFINITY;
-  l = fminf(l, FLT_MAX);
-  return a.sigmoid ? fmaxf(l, -80.f) : l;
+__device__ __forceinline__ float a_logit(const RouteArgs &a, float l) {
+  l = l > -INFINITY ? fminf(l, FLT_MAX) : -INFINITY;
+  return a.sigmoid && l > -INFINITY ? fmaxf(l, -80.f) : l;
 }
-__device__ __forceinline__ float exp_of(float x) { return expf(x); }
-__device__ __forceinline__ double exp_of(double x) { return exp(x); }
+__device__ __forceinline__ float read_logit(const RouteArgs &a, int64_t at) {
+  return a_logit(a, a.f32 ? static_cast<const float *>(a.logits)[at]
+                          : __bfloat162float(static_cast<const __nv_bfloat16 *>(a.logits)[at]));
+}
 // exp(l - top), l <= top, the difference's rounding (which a large one would carry over) put right.
 __device__ __forceinline__ float exp_difference(float l, float top) {
   const float x = l - top, part = x - l;
@@ -47,10 +56,11 @@ __device__ __forceinline__ float exp_difference(float l, float top) {
   const float e = expf(x);
   return e > 0.f ? fmaf(e, off, e) : 0.f;
 }
-// A number's place in the order of floats, as an unsigned one; 0: ruled out.
+// A number's place in the order of floats, as an unsigned one; kNoRank: -inf, ruled out.
+constexpr uint32_t kNoRank = 0x007fffffu;
 __device__ __forceinline__ uint32_t rank_of(float x) {
   const uint32_t u = __float_as_uint(x + 0.f);   // (-0 -> +0)
-  return x > -INFINITY ? (u & 0x80000000u ? ~u : u | 0x80000000u) : 0u;
+  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float value_of(uint32_t r) {
   return __uint_as_float(r & 0x80000000u ? r & 0x7fffffffu : ~r);
@@ -62,180 +72,354 @@ __device__ __forceinline__ T warp_sum(T x) {
   return x;
 }
 // The largest x over the warp and the lowest index that has it (-1: every x is -inf).
-__device__ __forceinline__ int warp_best(float x, int index, float &best) {
-  const uint32_t r = rank_of(x), top = __reduce_max_sync(kFull, r);
-  best = top ? value_of(top) : -INFINITY;
-  const int at = __reduce_min_sync(kFull, r == top ? index : INT32_MAX);
-  return top ? at : -1;
-}
-__device__ __forceinline__ int warp_best(double x, int index, double &best) {
+__device__ __forceinline__ int warp_best(double x, int index) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     const double y = __shfl_xor_sync(kFull, x, o);
     const int j = __shfl_xor_sync(kFull, index, o);
     if (y > x || (y == x && j < index)) x = y, index = j;
   }
-  best = x;
   return x > -INFINITY ? index : -1;
 }
 
-// One row's experts by a warp, lane j < top_k getting the j-th (-1: none).  Values in T; in fp32 `unsure` says that
-// two values that a decision lies between are nearer than their errors: the caller then computes the row in fp64.
-//
-// fp32 errors, relative to the row's largest score: of a sigmoid two units of expf, a sum and a quotient, below 2^-21;
-// of a softmax the rounding of l - max (|x| exp(x) <= 0.37 units), expf, 21 additions and a product, below 2^-19.
-// A value adds half a unit of itself.  Equal logits with equal biases are equal exactly, however they are computed.
-template <typename T, int kPer>
-__device__ __forceinline__ int choose_row(const RouteArgs &a, int row, const int (&group)[kPer], T *shared, float &peak,
-                                          T &total, bool &unsure) {
-  constexpr bool kCheck = sizeof(T) == 4;
-  const int lane = threadIdx.x & 31;
+// One row's experts by a warp in fp64, lane j < top_k getting the j-th (-1: none): for the rows in which fp32 cannot tell
+// two values apart.  `shared`: the row's values.
+__device__ __noinline__ int choose_exactly(const RouteArgs &a, int row, double *shared) {
+  const int lane = threadIdx.x & 31, each = a.experts / a.groups;
   const int64_t base = (int64_t)row * a.experts;
-  const T none = -INFINITY;
-  T l[kPer], v[kPer];
-  float m = -INFINITY;
+  double m = -INFINITY, z = 0;
+  for (int e = lane; e < a.experts; e += 32) m = fmax(m, (double)read_logit(a, base + e));
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int e = lane + 32 * i;
-    const float x = e < a.experts ? read_logit(a, base + e) : -INFINITY;
-    m = fmaxf(m, x);
-    l[i] = x;
+  for (int o = 16; o > 0; o >>= 1) m = fmax(m, __shfl_xor_sync(kFull, m, o));
+  if (!a.sigmoid) {
+    for (int e = lane; e < a.experts; e += 32) z += exp((double)read_logit(a, base + e) - m);
+    z = warp_sum(z);
   }
-  m = warp_max_f32(m);
-  peak = m;
-  total = 1;
-  unsure = false;
-  if (!(m > -INFINITY)) return -1;
-  const bool values = a.bias || a.top_groups < a.groups;   // else the logits decide
-  T smax = 0, cmax = 0;
-  if (values || !a.renorm) {
-    if (a.sigmoid) {
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) v[i] = l[i] > none ? T(1) / (T(1) + exp_of(-l[i])) : T(0);
-    } else {
-      T z = 0;
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) z += v[i] = l[i] > none ? exp_of(l[i] - T(m)) : T(0);
-      total = warp_sum(z);
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) v[i] = v[i] / total;
-    }
+  for (int e = lane; e < a.experts; e += 32) {
+    const double l = read_logit(a, base + e);
+    double v = a.sigmoid ? 1 / (1 + exp(-l)) : exp(l - m) / z;
+    if (a.bias) v += a.bias[e];
+    shared[e] = l > -INFINITY && v > -INFINITY ? v : -INFINITY;
   }
-  T tol = 0, group_tol = 0;
-  if (values) {
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int e = lane + 32 * i;
-      if (kCheck) smax = fmax(smax, v[i]);
-      if (a.bias && e < a.experts) v[i] += T(a.bias[e]);
-      if (!(l[i] > none) || !(v[i] > none)) l[i] = v[i] = none;
-      else if (kCheck) cmax = fmax(cmax, fabs(v[i]));
-    }
-    if constexpr (kCheck) {
-      smax = warp_max_f32(smax), cmax = warp_max_f32(cmax);
-      const T off = smax * (a.sigmoid ? 0x1p-21f : 0x1p-19f);
-      tol = 2 * off + cmax * 0x1p-22f;
-      group_tol = 4 * off + cmax * 0x1p-20f;
-    }
-  }
+  __syncwarp();
+  uint32_t stays = kFull;
   if (a.top_groups < a.groups) {
-    // each group's two largest values by a few lanes
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < kPer; ++i)
-      if (lane + 32 * i < a.experts) shared[lane + 32 * i] = v[i];
-    __syncwarp();
-    const int each = a.experts / a.groups;
-    int lanes = 32;
-    while (lanes * a.groups > 32) lanes >>= 1;
-    const int g = lane / lanes, sub = lane % lanes;
-    T first = none, second = none;
-    if (g < a.groups)
-      for (int i = sub; i < each; i += lanes) {
-        const T x = shared[g * each + i];
+    double first = -INFINITY, second = -INFINITY;
+    if (lane < a.groups)
+      for (int i = 0; i < each; ++i) {
+        const double x = shared[lane * each + i];
         if (x > first) second = first, first = x;
         else if (x > second) second = x;
       }
-    for (int o = lanes >> 1; o > 0; o >>= 1) {
-      const T x = __shfl_xor_sync(kFull, first, o), y = __shfl_xor_sync(kFull, second, o);
-      second = fmax(fmin(first, x), fmax(second, y));
-      first = fmax(first, x);
-    }
-    T sum = first > none && second > none ? first + second : first;
-    if (sub) sum = none;
-    uint32_t stays = 0;
-    T last = none;
-    for (int j = 0; j <= a.top_groups; ++j) {
-      T best;
-      const int at = warp_best(sum, g, best);
+    double sum = first > -INFINITY && second > -INFINITY ? first + second : first;
+    stays = 0;
+    for (int j = 0; j < a.top_groups; ++j) {
+      const int at = warp_best(sum, lane);
       if (at < 0) break;
-      if (j < a.top_groups) {
-        stays |= 1u << at;
-        last = best;
-        if (g == at) sum = none;
-      } else if (kCheck && !(last - best > group_tol)) {
-        unsure = true;
-        return -1;
-      }
+      stays |= 1u << at;
+      if (lane == at) sum = -INFINITY;
     }
-#pragma unroll
-    for (int i = 0; i < kPer; ++i)
-      if (!(stays >> group[i] & 1u)) l[i] = v[i] = none;
-  }
-  if (!a.bias) {
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) v[i] = l[i];
   }
   int mine = -1;
-  T value = none, before = none;
-  int at_before = -1;
-  const int rounds = kCheck && a.bias ? a.top_k + 1 : a.top_k;
-  for (int j = 0; j < rounds; ++j) {
-    T x = v[0];
-    int e = lane;
-#pragma unroll
-    for (int i = 1; i < kPer; ++i)
-      if (v[i] > x) x = v[i], e = lane + 32 * i;
-    T best;
-    const int at = warp_best(x, e, best);
+  for (int j = 0; j < a.top_k; ++j) {
+    double x = -INFINITY;
+    int e = INT32_MAX;
+    for (int i = lane; i < a.experts; i += 32)
+      if (stays >> i / each & 1u) {
+        // (without a bias the logits decide; an expert that was taken is ruled out)
+        const double y = a.bias || !(shared[i] > -INFINITY) ? shared[i] : (double)read_logit(a, base + i);
+        if (y > x) x = y, e = i;
+      }
+    const int at = warp_best(x, e);
     if (at < 0) break;
-    if (kCheck && a.bias && j > 0 && !(before - best > tol))
-      unsure = unsure || a.bias[at] != a.bias[at_before] || read_logit(a, base + at) != read_logit(a, base + at_before);
-    if (lane == j && j < a.top_k) mine = at, value = best;
-    before = best, at_before = at;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i)
-      if (lane + 32 * i == at) v[i] = none;
+    if (lane == j) mine = at;
+    if (lane == (at & 31)) shared[at] = -INFINITY;
+    __syncwarp();
   }
+  __syncwarp();
   return mine;
 }
 
+// The warp's rows from lane's experts lane * kPer .. lane * kPer + kPer - 1 of each.
 template <int kPer>
-__device__ __noinline__ int choose_row_again(const RouteArgs &a, int row, const int (&group)[kPer], double *shared,
-                                             float &peak, double &total) {
-  bool unsure;
-  return choose_row<double, kPer>(a, row, group, shared, peak, total, unsure);
-}
+struct Chooser {
+  float bias[kPer];        // this lane's experts'
+  int each, lanes, group;  // experts of a group; the lanes that hold one (0: it does not lie in 2^i whole lanes), this lane's
 
-// A warp a row.
-template <int kPer>
-__global__ void __launch_bounds__(kChooseWarps * 32) choose_kernel(RouteArgs a) {
-  __shared__ double shared[kChooseWarps][kPer * 32];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  int group[kPer];
+  __device__ __forceinline__ explicit Chooser(const RouteArgs &a) {
+    const int lane = threadIdx.x & 31;
+    each = a.experts / a.groups;
+    lanes = each % kPer == 0 ? each / kPer : 0;
+    if (lanes & (lanes - 1)) lanes = 0;
+    group = lane * kPer / each;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) group[i] = min(lane + 32 * i, a.experts - 1) / (a.experts / a.groups);
-  grid_dependency_wait();
-  grid_launch_dependents();
-  for (int row = blockIdx.x * kChooseWarps + warp; row < a.rows; row += gridDim.x * kChooseWarps) {
+    for (int i = 0; i < kPer; ++i) bias[i] = a.bias && lane * kPer + i < a.experts ? a.bias[lane * kPer + i] : 0.f;
+  }
+
+  __device__ __forceinline__ void read(const RouteArgs &a, int row, float (&l)[kPer]) const {
+    const int e0 = (threadIdx.x & 31) * kPer;
+    const int64_t base = (int64_t)row * a.experts + e0;
+    if (kPer >= 4 && a.f32 && a.wide) {
+#pragma unroll
+      for (int i = 0; i < kPer; i += 4) {
+        float4 x = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+        if (e0 + i < a.experts) x = *reinterpret_cast<const float4 *>(static_cast<const float *>(a.logits) + base + i);
+        l[i] = a_logit(a, x.x), l[i + 1] = a_logit(a, x.y), l[i + 2] = a_logit(a, x.z), l[i + 3] = a_logit(a, x.w);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) l[i] = e0 + i < a.experts ? read_logit(a, base + i) : -INFINITY;
+    }
+  }
+
+  // The row's experts, lane j < top_k getting the j-th (-1: none).  `unsure`: two values that a decision lies between are
+  // nearer than their errors.  `shared`: room for the row's values.
+  //
+  // The errors, relative to the row's largest score: of a sigmoid two units of expf, half a unit of a sum and one of a
+  // reciprocal, below 2^-21;
+  // of a softmax the rounding of l - max (|x| exp(x) <= 0.37 units), expf, 21 additions and a quotient, below 2^-19.  A
+  // value adds half a unit of itself.  Equal logits with equal biases are equal exactly, however they are computed.
+  __device__ __forceinline__ int choose(const RouteArgs &a, int row, float *shared, float &peak, float &z, bool &unsure) const {
+    const int lane = threadIdx.x & 31;
+    float l[kPer];
+    read(a, row, l);
+    float m = l[0];
+#pragma unroll
+    for (int i = 1; i < kPer; ++i) m = fmaxf(m, l[i]);
+    m = warp_max_f32(m);
+    peak = m;
+    z = 1.f;
+    unsure = false;
+    if (!(m > -INFINITY)) return -1;
+    const bool grouped = a.top_groups < a.groups;
+    uint32_t k[kPer];                            // the experts' places in the order
+    float tol = 0.f, group_tol = 0.f;
+    if (a.bias || grouped || !(a.renorm || a.sigmoid)) {   // (else the logits decide, and their quotients suffice)
+      float v[kPer];
+      if (a.sigmoid) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(v[i]) : "f"(1.f + expf(-l[i])));  // (0 where ruled out)
+        }
+      } else {
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) sum += v[i] = expf(l[i] - m);
+        z = warp_sum(sum);
+        const float back = 1.f / z;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) v[i] *= back;
+      }
+      if (a.bias || grouped) {
+        float smax = 0.f, cmax = 0.f;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          smax = fmaxf(smax, v[i]);
+          v[i] += bias[i];
+          if (!(l[i] > -INFINITY && v[i] > -INFINITY)) v[i] = -INFINITY;
+          else cmax = fmaxf(cmax, fabsf(v[i]));
+        }
+        smax = warp_max_f32(smax), cmax = warp_max_f32(cmax);
+        const float off = smax * (a.sigmoid ? 0x1p-21f : 0x1p-19f);
+        tol = 2 * off + cmax * 0x1p-22f;
+        group_tol = 4 * off + cmax * 0x1p-20f;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+          if (!(v[i] > -INFINITY)) l[i] = -INFINITY;
+      }
+      if (grouped) {
+        uint32_t stays;
+        if (!keep_groups(a, l, v, shared, group_tol, stays)) {
+          unsure = true;
+          return -1;
+        }
+        if (lanes) {
+          if (!(stays >> group & 1u)) {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) l[i] = v[i] = -INFINITY;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < kPer; ++i)
+            if (!(stays >> (lane * kPer + i) / each & 1u)) l[i] = v[i] = -INFINITY;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) k[i] = rank_of(a.bias ? v[i] : l[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) k[i] = rank_of(l[i]);
+    }
+    // Each lane's experts in order (neighbours change places, so that equal ones keep theirs), then the warp's largest
+    // first one, again and again.
+    uint64_t ids = 0;                            // four bits each
+    uint32_t id[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) id[i] = i;
+#pragma unroll
+    for (int r = 0; r < kPer; ++r)
+#pragma unroll
+      for (int i = r & 1; i + 1 < kPer; i += 2) {
+        const bool swap = k[i] < k[i + 1];
+        const uint32_t x = k[i], y = id[i];
+        k[i] = max(x, k[i + 1]), k[i + 1] = min(x, k[i + 1]);
+        id[i] = swap ? id[i + 1] : y, id[i + 1] = swap ? y : id[i + 1];
+      }
+    uint32_t low = 0, high = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      if (i < 8) low |= id[i] << 4 * i;
+      else high |= id[i] << 4 * (i - 8);
+    }
+    ids = (uint64_t)high << 32 | low;
+    int mine = -1;                               // lane j: the j-th; with a bias the one after the last too
+    uint32_t rank = kNoRank;
+    const int rounds = min(a.top_k + (a.bias ? 1 : 0), 32);
+    for (int j = 0; j < rounds; ++j) {
+      const uint32_t top = __reduce_max_sync(kFull, k[0]);
+      if (top == kNoRank) break;
+      const int owner = __ffs(__ballot_sync(kFull, k[0] == top)) - 1;
+      const int e = owner * kPer + (int)(__shfl_sync(kFull, (uint32_t)ids, owner) & 15u);
+      if (lane == j) mine = e, rank = top;
+      if (lane == owner) {
+#pragma unroll
+        for (int i = 0; i + 1 < kPer; ++i) k[i] = k[i + 1];
+        k[kPer - 1] = kNoRank;
+        ids >>= 4;
+      }
+    }
+    if (a.bias) {
+      uint32_t next = __shfl_down_sync(kFull, rank, 1);
+      int e = __shfl_down_sync(kFull, mine, 1);
+      if (a.top_k == 32) {                       // (a lane for each: the one after the last is still to come)
+        const uint32_t top = __reduce_max_sync(kFull, k[0]);
+        if (lane == 31) next = top, e = -1;
+      }
+      const bool near = lane < a.top_k && next > kNoRank && !(value_of(rank) - value_of(next) > tol);
+      if (__any_sync(kFull, near)) {
+        const int64_t base = (int64_t)row * a.experts;
+        const bool differ = near && (e < 0 || a.bias[mine] != a.bias[e] || read_logit(a, base + mine) != read_logit(a, base + e));
+        if (__any_sync(kFull, differ)) {
+          // A sigmoid's value is its own logit's alone: where what follows is far enough away, the few chosen are put in
+          // order by their exact values.
+          const uint32_t follows = __reduce_max_sync(kFull, k[0]);
+          const bool apart = follows == kNoRank || value_of(__shfl_sync(kFull, rank, rounds - 1)) - value_of(follows) > tol;
+          if (!a.sigmoid || rounds > 31 || !apart) {
+            unsure = true;
+          } else {
+            double exact = -INFINITY;
+            if (mine >= 0) exact = 1 / (1 + exp(-(double)read_logit(a, base + mine))) + a.bias[mine];
+            int at = 0;                            // of this lane's among the others
+            for (int j = 0; j < rounds; ++j) {
+              const double other = __shfl_sync(kFull, exact, j);
+              const int o = __shfl_sync(kFull, mine, j);
+              at += o >= 0 && (other > exact || (other == exact && o < mine));
+            }
+            if (mine < 0) at = 32;
+            int sorted = -1;
+            for (int j = 0; j < rounds; ++j)
+              if (__shfl_sync(kFull, at, j) == lane) sorted = j;
+            const int chosen = __shfl_sync(kFull, mine, max(sorted, 0));
+            mine = sorted >= 0 ? chosen : -1;
+          }
+        }
+      }
+      if (lane >= a.top_k) mine = -1;
+    }
+    return mine;
+  }
+
+  // The top_groups groups of the largest sums of two values, a bit each; false: two sums are too near to one another.
+  __device__ __forceinline__ bool keep_groups(const RouteArgs &a, const float (&l)[kPer], const float (&v)[kPer], float *shared,
+                                              float tol, uint32_t &stays) const {
+    const int lane = threadIdx.x & 31;
+    float first = -INFINITY, second = -INFINITY;
+    int g = group, step = lanes;                 // the group that this lane works at, the lanes that do
+    if (lanes) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        second = fmaxf(second, fminf(first, v[i]));
+        first = fmaxf(first, v[i]);
+      }
+    } else {
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+        if (lane * kPer + i < a.experts) shared[lane * kPer + i] = v[i];
+      __syncwarp();
+      step = 32;
+      while (step * a.groups > 32) step >>= 1;
+      g = lane / step;
+      if (g < a.groups)
+        for (int i = lane % step; i < each; i += step) {
+          const float x = shared[g * each + i];
+          second = fmaxf(second, fminf(first, x));
+          first = fmaxf(first, x);
+        }
+    }
+    for (int o = step >> 1; o > 0; o >>= 1) {
+      const float x = __shfl_xor_sync(kFull, first, o), y = __shfl_xor_sync(kFull, second, o);
+      second = fmaxf(fminf(first, x), fmaxf(second, y));
+      first = fmaxf(first, x);
+    }
+    const float sum = second > -INFINITY ? first + second : first;   // (-inf: no expert is left)
+    int before = 0;                              // groups that come before this one
+    for (int i = 0; i < a.groups; ++i) {
+      const float other = __shfl_sync(kFull, sum, i * step);
+      before += other > sum || (other == sum && i < g);
+    }
+    const bool live = g < a.groups && sum > -INFINITY, kept = live && before < a.top_groups;
+    const uint32_t least = __reduce_min_sync(kFull, kept ? rank_of(sum) : kFull);
+    const uint32_t most = __reduce_max_sync(kFull, live && !kept ? rank_of(sum) : kNoRank);
+    stays = __reduce_or_sync(kFull, kept ? 1u << g : 0u);
+    if (most == kNoRank || value_of(least) - value_of(most) > tol) return true;
+    if (!a.sigmoid || !lanes) return false;
+    // Exactly, a sigmoid's value being its own logit's alone: the values that may be a group's two largest, one a lane at a
+    // time.
+    uint32_t wanted = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (v[i] > -INFINITY && !(v[i] < (second > -INFINITY ? second : first) - tol)) wanted |= 1u << i;
+    double first64 = -INFINITY, second64 = -INFINITY;
+    while (__any_sync(kFull, wanted)) {
+      const int at = __ffs(wanted) - 1;
+      float x = -INFINITY, b = 0.f;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+        if (i == at) x = l[i], b = bias[i];
+      const double exact = at >= 0 ? 1 / (1 + exp(-(double)x)) + b : -INFINITY;
+      second64 = fmax(second64, fmin(first64, exact));
+      first64 = fmax(first64, exact);
+      wanted &= wanted - 1;
+    }
+    for (int o = step >> 1; o > 0; o >>= 1) {
+      const double x = __shfl_xor_sync(kFull, first64, o), y = __shfl_xor_sync(kFull, second64, o);
+      second64 = fmax(fmin(first64, x), fmax(second64, y));
+      first64 = fmax(first64, x);
+    }
+    const double sum64 = second64 > -INFINITY ? first64 + second64 : first64;
+    before = 0;
+    for (int i = 0; i < a.groups; ++i) {
+      const double other = __shfl_sync(kFull, sum64, i * step);
+      before += other > sum64 || (other == sum64 && i < g);
+    }
+    stays = __reduce_or_sync(kFull, live && before < a.top_groups ? 1u << g : 0u);
+    return true;
+  }
+};
+
+// Rows by a warp: first, first + step, ..
+template <int kPer>
+__device__ __forceinline__ void choose_rows(const RouteArgs &a, int first, int step, double *shared) {
+  const int lane = threadIdx.x & 31;
+  const Chooser<kPer> chooser(a);
+  for (int row = first; row < a.rows; row += step) {
     float peak, z;
     bool unsure;
-    int mine = choose_row<float, kPer>(a, row, group, reinterpret_cast<float *>(shared[warp]), peak, z, unsure);
+    int mine = chooser.choose(a, row, reinterpret_cast<float *>(shared), peak, z, unsure);
     if (unsure) {
-      double z64;
       __syncwarp();
-      mine = choose_row_again<kPer>(a, row, group, shared[warp], peak, z64);
-      z = (float)z64;
+      mine = choose_exactly(a, row, shared);
     }
     // the weights, from the chosen experts' logits alone: lane j has the j-th
     float s = 0.f;
@@ -259,90 +443,187 @@ __global__ void __launch_bounds__(kChooseWarps * 32) choose_kernel(RouteArgs a) 
   }
 }
 
+template <int kPer>
+__global__ void __launch_bounds__(kChooseWarps * 32) choose_kernel(const __grid_constant__ RouteArgs a) {
+  __shared__ double shared[kChooseWarps][kPer * 32];
+  const int warp = threadIdx.x >> 5;
+  grid_dependency_wait();
+  grid_launch_dependents();
+  choose_rows<kPer>(a, blockIdx.x * kChooseWarps + warp, gridDim.x * kChooseWarps, shared[warp]);
+}
+
 // ------------------------------------------------------------------------------------
 // Grouping: a stable counting sort of the pairs by expert, by one cluster
 // ------------------------------------------------------------------------------------
-// A warp takes a stretch of the pairs, 32 at a time, and counts each expert's in a histogram of its own (the lanes
-// with equal experts find one another, one of them counts: no atomics, so that every run gives the same order).  The
-// histograms' running sums over warps, then CTAs (through distributed shared memory), then experts are where each
-// warp's pairs of an expert begin; a second walk places them.
-constexpr int kGroupThreads = 1024, kGroupWarps = 32, kGroupCtas = 8;
+// A warp takes a stretch of rows, 32 at a time, and counts each expert's in a histogram of its own.  The
+// histograms' running sums over warps, then CTAs (through distributed shared memory), then experts are where each warp's
+// pairs of an expert begin.  A second walk places them: a row has an expert once at most, so that the rows of 32 that
+// have it are bits of a word (or-ed together in any order), and a pair's place is the bits before its own.  (With the
+// lanes of equal experts finding one another, 32 pairs at a time, 131072 pairs took 27 us.)
+//
+// A CTA that has no more than kStaged pairs puts them in their order in shared memory and writes each expert's one after
+// another; scattered words cost a CTA some 8 us for 16384.
+constexpr int kGroupThreads = 1024, kGroupWarps = 32, kGroupCtas = 8, kStaged = 16384;
+// (Pitch of the histograms: odd, so that four lanes that add up eight warps each of one expert's meet no bank twice.)
+__host__ __device__ constexpr int group_pitch(int experts) { return experts | 1; }
+__host__ __device__ constexpr int group_smem(int experts, bool staged) {
+  return 2 * kGroupWarps * group_pitch(experts) * 4 + (staged ? kStaged * 4 : 0);
+}
+static_assert(group_smem(kMostExperts, true) <= 220 * 1024, "shared memory");
 
-__global__ void __launch_bounds__(kGroupThreads) group_kernel(RouteArgs a, int64_t n) {
-  extern __shared__ int32_t hist[];              // [warps][experts]
-  __shared__ int32_t count[kMostExperts], first[kMostExperts], part[kGroupWarps];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, E = a.experts;
-  const int ctas = gridDim.x, rank = blockIdx.x;
-  int32_t *mine = hist + warp * E;
-  for (int e = lane; e < E; e += 32) mine[e] = 0;
-  const int64_t stretch = ((n + ctas * kGroupWarps - 1) / (ctas * kGroupWarps) + 31) / 32 * 32;
-  const int64_t from = (rank * kGroupWarps + warp) * stretch, to = min(n, from + stretch);
-  grid_dependency_wait();
-  grid_launch_dependents();
+// (Every thread of a block of kGroupThreads, of every block of the cluster; hist: [2][warps][pitch], and the staged pairs.)
+__device__ __forceinline__ void group_pairs(const RouteArgs &a, int32_t *hist, bool staged) {
+  __shared__ int32_t count[kMostExperts], first[kMostExperts], local[kMostExperts], part[2][kGroupWarps];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, E = a.experts, K = a.top_k, pitch = group_pitch(E);
+  const int ctas = gridDim.x, rank = blockIdx.x;   // (one cluster)
+  int32_t *mine = hist + warp * pitch;
+  uint32_t *rows_of = reinterpret_cast<uint32_t *>(hist + (kGroupWarps + warp) * pitch);
+  uint32_t *stage = reinterpret_cast<uint32_t *>(hist + 2 * kGroupWarps * pitch);
+  const int stretch = ((a.rows + ctas * kGroupWarps - 1) / (ctas * kGroupWarps) + 31) & ~31;  // rows of a warp
+  const int64_t row0 = (int64_t)rank * kGroupWarps * stretch;                                // the CTA's first
+  const int64_t from = row0 + (int64_t)warp * stretch, to = min((int64_t)a.rows, from + stretch);
+  for (int e = lane; e < E; e += 32) mine[e] = 0, rows_of[e] = 0;
   __syncwarp();
-  for (int64_t i = from; i < to; i += 32) {
-    const int e = i + lane < to ? a.expert[i + lane] : -1;
-    const uint32_t same = __match_any_sync(kFull, e);
-    if (e >= 0 && lane == __ffs(same) - 1) mine[e] += __popc(same);
-    __syncwarp();
+  for (int64_t i0 = from * K; i0 < to * K; i0 += 8 * 32) {
+    int e[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = i0 + 32 * i + lane < to * K ? a.expert[i0 + 32 * i + lane] : -1;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (e[i] >= 0) atomicAdd(&mine[e[i]], 1);    // (of whole numbers: any order)
   }
   __syncthreads();
-  for (int e = tid; e < E; e += kGroupThreads) {
-    int run = 0;
-    for (int w = 0; w < kGroupWarps; ++w) {
-      const int c = hist[w * E + e];
-      hist[w * E + e] = run;
-      run += c;
+  for (int x = tid >> 2; x < (E + 7) / 8 * 8; x += kGroupThreads / 4) {
+    const int w0 = (tid & 3) * (kGroupWarps / 4);
+    int c[kGroupWarps / 4], run = 0;
+#pragma unroll
+    for (int i = 0; i < kGroupWarps / 4; ++i) {
+      c[i] = run;
+      if (x < E) run += hist[(w0 + i) * pitch + x];
     }
-    count[e] = run;
+    int upto = run;
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) {
+      const int y = __shfl_up_sync(kFull, upto, o, 4);
+      if ((tid & 3) >= o) upto += y;
+    }
+    if (x < E) {
+#pragma unroll
+      for (int i = 0; i < kGroupWarps / 4; ++i) hist[(w0 + i) * pitch + x] = upto - run + c[i];
+      if ((tid & 3) == 3) count[x] = upto;
+    }
   }
   if (ctas > 1) cluster_sync_all();
   else __syncthreads();
-  int before = 0, all = 0;                       // this expert's, of the CTAs before and of all
-  if (tid < E)
-    for (int q = 0; q < ctas; ++q) {
-      uint32_t c;
-      if (ctas > 1) asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(c) : "r"(cluster_map_shared(smem_u32(&count[tid]), q)));
-      else c = (uint32_t)count[tid];
-      if (q < rank) before += (int)c;
-      all += (int)c;
+  int before = 0, all = 0, own = 0;              // this expert's, of the CTAs before, of all, of this one
+  if (tid < E) {
+    own = count[tid];
+    if (ctas > 1) {
+      uint32_t c[kGroupCtas];
+#pragma unroll
+      for (int q = 0; q < kGroupCtas; ++q)
+        asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(c[q]) : "r"(cluster_map_shared(smem_u32(&count[tid]), q)));
+#pragma unroll
+      for (int q = 0; q < kGroupCtas; ++q) {
+        if (q < rank) before += (int)c[q];
+        all += (int)c[q];
+      }
+    } else {
+      all = own;
     }
-  int run = all;                                 // over the experts up to this one
+  }
+  int run = all, own_run = own;                  // over the experts up to this one
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int x = __shfl_up_sync(kFull, run, o);
-    if (lane >= o) run += x;
+    const int x = __shfl_up_sync(kFull, run, o), y = __shfl_up_sync(kFull, own_run, o);
+    if (lane >= o) run += x, own_run += y;
   }
-  if (lane == 31) part[warp] = run;
+  if (lane == 31) part[0][warp] = run, part[1][warp] = own_run;
   if (ctas > 1) cluster_sync_all();              // (the counts have been read)
   else __syncthreads();
-  int lead = 0, total = 0;
-  for (int w = 0; w < kGroupWarps; ++w) {
-    if (w < warp) lead += part[w];
-    total += part[w];
-  }
+  const int warps = (E + 31) / 32;               // that have experts
+  const int all_of = lane < warps ? part[0][lane] : 0, own_of = lane < warps ? part[1][lane] : 0;
+  const int total = __reduce_add_sync(kFull, all_of), owned = __reduce_add_sync(kFull, own_of);
+  const int lead = __reduce_add_sync(kFull, lane < warp ? all_of : 0), own_lead = __reduce_add_sync(kFull, lane < warp ? own_of : 0);
   if (tid < E) {
     first[tid] = lead + run - all + before;
+    local[tid] = own_lead + own_run - own;
     if (rank == 0) {
       a.offsets[tid] = lead + run - all;
       if (tid == 0) a.offsets[E] = total;
     }
   }
   __syncthreads();
-  for (int64_t i = from; i < to; i += 32) {
-    const int e = i + lane < to ? a.expert[i + lane] : -1;
-    const uint32_t same = __match_any_sync(kFull, e);
-    int at = -1;
-    if (e >= 0) {
-      at = first[e] + mine[e] + __popc(same & ((1u << lane) - 1));
-      a.order[at] = (int32_t)(i + lane);
+  const uint32_t one_kth = 65536 / K + 1;          // x / K = x one_kth / 65536 for x < 1024
+  for (int64_t r0 = from; r0 < to; r0 += 32) {     // 32 rows: 32 K pairs, 8 x 32 at a time
+    const int64_t p0 = r0 * K;
+    const int pairs = (int)min((int64_t)32, to - r0) * K;
+    int e[8];
+    const auto read = [&](int i0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) e[i] = i0 + 32 * i + lane < pairs ? a.expert[p0 + i0 + 32 * i + lane] : -1;
+    };
+    for (int i0 = 0; i0 < pairs; i0 += 8 * 32) {
+      read(i0);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (e[i] >= 0) atomicOr(&rows_of[e[i]], 1u << ((i0 + 32 * i + lane) * one_kth >> 16));
     }
-    if (i + lane < to) a.place[i + lane] = at;
     __syncwarp();
-    if (e >= 0 && lane == __ffs(same) - 1) mine[e] += __popc(same);
+    for (int i0 = 0; i0 < pairs; i0 += 8 * 32) {
+      if (pairs > 8 * 32) read(i0);
+      int at[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        at[i] = -1;
+        if (e[i] < 0) continue;
+        const int p = i0 + 32 * i + lane;
+        const int r = mine[e[i]] + __popc(rows_of[e[i]] & ((1u << (p * one_kth >> 16)) - 1));
+        at[i] = first[e[i]] + r;
+        if (staged) stage[local[e[i]] + r] = (uint32_t)((int)(p0 - row0 * K) + p) << 9 | (uint32_t)e[i];
+        else a.order[at[i]] = (int32_t)(p0 + p);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i0 + 32 * i + lane < pairs) a.place[p0 + i0 + 32 * i + lane] = at[i];
+    }
+    __syncwarp();
+    for (int x = lane; x < E; x += 32) {
+      mine[x] += __popc(rows_of[x]);
+      rows_of[x] = 0;
+    }
     __syncwarp();
   }
+  if (staged) {
+    __syncthreads();
+    for (int p = tid; p < owned; p += kGroupThreads) {
+      const uint32_t v = stage[p];
+      const int e = (int)(v & 511u);
+      a.order[first[e] + p - local[e]] = (int32_t)(row0 * K + (v >> 9));
+    }
+  }
+  const int64_t n = (int64_t)a.rows * K;
   for (int64_t i = total + rank * kGroupThreads + tid; i < n; i += ctas * kGroupThreads) a.order[i] = -1;
+}
+
+__global__ void __launch_bounds__(kGroupThreads) group_kernel(const __grid_constant__ RouteArgs a, int staged) {
+  extern __shared__ int32_t hist[];
+  grid_dependency_wait();
+  grid_launch_dependents();
+  group_pairs(a, hist, staged != 0);
+}
+
+// A few rows: the choice and the grouping by one block.
+constexpr int kFewRows = 32, kAloneRows = 1024;
+template <int kPer>
+__global__ void __launch_bounds__(kGroupThreads) route_few_kernel(const __grid_constant__ RouteArgs a) {
+  extern __shared__ int32_t hist[];              // the grouping's, before that [warps][values]
+  grid_dependency_wait();
+  grid_launch_dependents();
+  const int warp = threadIdx.x >> 5;
+  choose_rows<kPer>(a, warp, kGroupWarps, reinterpret_cast<double *>(hist) + warp * (kPer * 32));
+  __syncthreads();
+  group_pairs(a, hist, false);
 }
 
 // ------------------------------------------------------------------------------------
@@ -355,40 +636,97 @@ struct CombineArgs {
   const __nv_bfloat16 *add;  // nullable
   __nv_bfloat16 *out;
   int64_t slots;
-  int top_k, n, f32;
+  int top_k, n;
 };
 
-// kEach neighbouring columns of a row a thread.
-template <int kEach, bool kF32>
-__global__ void __launch_bounds__(256) combine_kernel(CombineArgs a) {
+// kEach neighbouring numbers as they lie in memory, read at once (16 bytes at a time at most).
+template <typename T, int kEach>
+struct alignas(sizeof(T) * kEach < 16 ? sizeof(T) * kEach : 16) Piece {
+  T v[kEach];
+};
+__device__ __forceinline__ float as_float(float x) { return x; }
+__device__ __forceinline__ float as_float(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+
+// kEach neighbouring columns of a row a thread, kGroups times (a block's columns apart).  The results of kTogether
+// places are read before any is added.  (4096 rows of 8 x 4096 in bf16: 62 us where numbers were converted as they were
+// read, so that each read was waited for.)
+constexpr int kTogether = 4;
+template <int kEach, int kGroups, typename Y>
+__global__ void __launch_bounds__(256) combine_kernel(const __grid_constant__ CombineArgs a) {
   const int64_t row = blockIdx.x;
-  const int c = (blockIdx.y * blockDim.x + threadIdx.x) * kEach;
+  const int c0 = (blockIdx.y * kGroups * blockDim.x + threadIdx.x) * kEach;
   grid_dependency_wait();
   grid_launch_dependents();
-  if (c >= a.n) return;
-  float sum[kEach];
+  float sum[kGroups][kEach];
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) sum[i] = a.add ? __bfloat162float(a.add[row * a.n + c + i]) : 0.f;
-  for (int j = 0; j < a.top_k; ++j) {
-    const int64_t at = a.place[row * a.top_k + j];
-    if (at < 0 || at >= a.slots) continue;
-    const float w = a.weight[row * a.top_k + j];
+  for (int g = 0; g < kGroups; ++g) {
+    const int c = c0 + g * (int)blockDim.x * kEach;
+    Piece<uint16_t, kEach> p = {};
+    if (a.add && c < a.n) p = *reinterpret_cast<const Piece<uint16_t, kEach> *>(a.add + row * a.n + c);
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int64_t from = at * a.n + c + i;
-      const float y = kF32 ? static_cast<const float *>(a.y)[from]
-                           : __bfloat162float(static_cast<const __nv_bfloat16 *>(a.y)[from]);
-      sum[i] = fmaf(w, y, sum[i]);
+    for (int i = 0; i < kEach; ++i) sum[g][i] = as_float(p.v[i]);
+  }
+  for (int j0 = 0; j0 < a.top_k; j0 += kTogether) {
+    Piece<Y, kEach> p[kTogether][kGroups];
+    float w[kTogether];
+    bool live[kTogether];
+#pragma unroll
+    for (int j = 0; j < kTogether; ++j) {
+      const int64_t pair = row * a.top_k + j0 + j;
+      const int64_t at = j0 + j < a.top_k ? a.place[pair] : -1;
+      live[j] = at >= 0 && at < a.slots;
+      w[j] = live[j] ? a.weight[pair] : 0.f;
+      const Y *y = static_cast<const Y *>(a.y) + at * a.n + c0;
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g)
+        if (live[j] && c0 + g * (int)blockDim.x * kEach < a.n) p[j][g] = *reinterpret_cast<const Piece<Y, kEach> *>(y + g * (int)blockDim.x * kEach);
     }
+#pragma unroll
+    for (int j = 0; j < kTogether; ++j)
+      if (live[j]) {
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+          for (int i = 0; i < kEach; ++i) sum[g][i] = fmaf(w[j], as_float(p[j][g].v[i]), sum[g][i]);
+      }
   }
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) a.out[row * a.n + c + i] = __float2bfloat16_rn(sum[i]);
+  for (int g = 0; g < kGroups; ++g) {
+    const int c = c0 + g * (int)blockDim.x * kEach;
+    if (c >= a.n) continue;
+    Piece<uint16_t, kEach> p;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) p.v[i] = __bfloat16_as_ushort(__float2bfloat16_rn(sum[g][i]));
+    *reinterpret_cast<Piece<uint16_t, kEach> *>(a.out + row * a.n + c) = p;
+  }
+}
+template <int kEach, int kGroups>
+cudaError_t launch_combine(const CombineArgs &a, int rows, bool f32, cudaStream_t s) {
+  // a row in as few blocks of threads as hold it, of equal shares
+  const int share = (a.n + kEach * kGroups - 1) / (kEach * kGroups), parts = (share + 255) / 256;
+  const dim3 grid((unsigned)rows, (unsigned)parts), block((unsigned)(((share + parts - 1) / parts + 31) / 32 * 32));
+  return f32 ? launch_after<combine_kernel<kEach, kGroups, float>>(grid, block, 0, dim3(1), s, a)
+             : launch_after<combine_kernel<kEach, kGroups, uint16_t>>(grid, block, 0, dim3(1), s, a);
 }
 
+// Launches of Kernel<kPer> for the experts' number.
 template <int kPer>
-cudaError_t launch_choose(const RouteArgs &a, cudaStream_t s) {
-  const int blocks = (a.rows + kChooseWarps - 1) / kChooseWarps;
-  return launch_after<choose_kernel<kPer>>(dim3((unsigned)blocks), dim3(kChooseWarps * 32), 0, dim3(1), s, a);
+cudaError_t launch_route(const RouteArgs &a, cudaStream_t s) {
+  static bool few_done[64] = {}, done[64] = {};
+  int dev = 0;
+  cudaGetDevice(&dev);
+  if (a.rows <= kFewRows) {
+    constexpr int kMost = std::max(kGroupWarps * kPer * 32 * 8, group_smem(kPer * 32, false));
+    const cudaError_t e = allow(route_few_kernel<kPer>, kMost, few_done, dev);
+    return e != cudaSuccess ? e : launch_after<route_few_kernel<kPer>>(dim3(1), dim3(kGroupThreads), (size_t)kMost, dim3(1), s, a);
+  }
+  const int blocks = std::min((a.rows + kChooseWarps - 1) / kChooseWarps, device_sms() * kChooseBlocks);
+  cudaError_t e = launch_after<choose_kernel<kPer>>(dim3((unsigned)blocks), dim3(kChooseWarps * 32), 0, dim3(1), s, a);
+  if (e == cudaSuccess) e = allow(group_kernel, group_smem(kMostExperts, true), done, dev);
+  const unsigned ctas = a.rows <= kAloneRows ? 1 : kGroupCtas;
+  const int stretch = ((a.rows + (int)ctas * kGroupWarps - 1) / ((int)ctas * kGroupWarps) + 31) & ~31;
+  const bool staged = (int64_t)stretch * kGroupWarps * a.top_k <= kStaged;
+  return e != cudaSuccess ? e : launch_after<group_kernel>(dim3(ctas), dim3(kGroupThreads), (size_t)group_smem(a.experts, staged), dim3(ctas), s, a, (int)staged);
 }
 
 }  // namespace
@@ -440,6 +778,7 @@ int ham_route(const void *logits, int32_t logits_dtype, const float *bias, int32
   a.logits = logits;
   a.bias = bias;
   a.f32 = f32;
+  a.wide = f32 && experts % 4 == 0 && op_aligned(logits, 16);
   a.rows = rows;
   a.experts = experts;
   a.top_k = top_k;
@@ -454,26 +793,11 @@ int ham_route(const void *logits, int32_t logits_dtype, const float *bias, int32
   a.order = order;
   a.place = place;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  cudaError_t ce = experts <= 32    ? ham::launch_choose<1>(a, s)
-                   : experts <= 64  ? ham::launch_choose<2>(a, s)
-                   : experts <= 128 ? ham::launch_choose<4>(a, s)
-                   : experts <= 256 ? ham::launch_choose<8>(a, s)
-                                    : ham::launch_choose<16>(a, s);
-  if (ce == cudaSuccess) {
-    static bool done[64] = {};
-    int dev = 0;
-    cudaGetDevice(&dev);
-    if (dev < 0 || dev >= 64 || !done[dev]) {
-      ce = cudaFuncSetAttribute(ham::group_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                ham::kGroupWarps * ham::kMostExperts * 4);
-      if (ce == cudaSuccess && dev >= 0 && dev < 64) done[dev] = true;
-    }
-    const int ctas = pairs <= 8192 ? 1 : ham::kGroupCtas;
-    if (ce == cudaSuccess)
-      ce = ham::launch_after<ham::group_kernel>(dim3((unsigned)ctas), dim3(ham::kGroupThreads),
-                                                (size_t)ham::kGroupWarps * experts * 4, dim3((unsigned)ctas), s, a,
-                                                (int64_t)pairs);
-  }
+  const cudaError_t ce = experts <= 32    ? ham::launch_route<1>(a, s)
+                         : experts <= 64  ? ham::launch_route<2>(a, s)
+                         : experts <= 128 ? ham::launch_route<4>(a, s)
+                         : experts <= 256 ? ham::launch_route<8>(a, s)
+                                          : ham::launch_route<16>(a, s);
   return ce == cudaSuccess ? HAM_OK : op_fail(HAM_ECUDA, "route launch: %s", cudaGetErrorString(ce));
 }
 
@@ -504,11 +828,13 @@ int ham_experts_combine(const void *y, int32_t y_dtype, const float *weight, con
   a.slots = (int64_t)pairs;
   a.top_k = top_k;
   a.n = n;
-  a.f32 = f32;
-  const dim3 grid((unsigned)rows, (unsigned)((n + 255) / 256));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const cudaError_t ce = f32 ? ham::launch_after<ham::combine_kernel<1, true>>(grid, dim3(256), 0, dim3(1), s, a)
-                             : ham::launch_after<ham::combine_kernel<1, false>>(grid, dim3(256), 0, dim3(1), s, a);
+  // Two pieces of 16 bytes a thread for many rows, one for few (us with one / two: 8 rows of 8 x 4096 2.2 / 2.9, 4096 rows 48.8 /
+  // 46.6, 8192 rows of 2 x 4096 44.5 / 37.1, of 4 x 2048 29.7 / 27.4; with four 51.5, 39.2 and 32.9).
+  const cudaError_t ce = n % 8 == 0   ? (rows < 4 * ham::device_sms() ? ham::launch_combine<8, 1>(a, rows, f32, s)
+                                                                      : ham::launch_combine<8, 2>(a, rows, f32, s))
+                         : n % 2 == 0 ? ham::launch_combine<2, 4>(a, rows, f32, s)
+                                      : ham::launch_combine<1, 4>(a, rows, f32, s);
   return ce == cudaSuccess ? HAM_OK : op_fail(HAM_ECUDA, "combine launch: %s", cudaGetErrorString(ce));
 }
 

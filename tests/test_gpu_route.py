@@ -69,7 +69,8 @@ def test_groups(experts, groups, top_groups, k, dtype, sigmoid, with_bias):
     _run(1.5 * rng.standard_normal((41, experts)), k, dtype, sigmoid, bias, groups=groups, top_groups=top_groups)
 
 
-@pytest.mark.parametrize("rows,experts,k", [(1, 64, 8), (5, 64, 8), (1023, 16, 1), (1025, 64, 8), (3001, 256, 5), (9000, 8, 2)])
+@pytest.mark.parametrize("rows,experts,k", [(1, 64, 8), (5, 64, 8), (1023, 16, 1), (1025, 64, 8), (3001, 256, 5), (9000, 8, 2),
+                                            (1024, 512, 32), (16384, 64, 8), (20001, 64, 7), (70000, 300, 3)])
 def test_many_rows(rows, experts, k):
     rng = np.random.default_rng(rows)
     l = rng.standard_normal((rows, experts)) + 2 * rng.standard_normal(experts)  # some experts have most of the rows
@@ -88,6 +89,25 @@ def test_values_that_fp32_cannot_tell_apart(sigmoid):
     assert 0 < np.diff(v).max() < 1e-6
     _run(l, 8, sigmoid=sigmoid, bias=bias)
     _run(l, 8, sigmoid=sigmoid, bias=bias, groups=8, top_groups=3)
+
+
+@pytest.mark.parametrize("k", [1, 2, 7, 31, 32])
+def test_pairs_of_near_values(k):
+    """Here and there two values that differ by less than fp32 tells, among others that lie apart; the last chosen and the
+    first that is not among them."""
+    rng = np.random.default_rng(k)
+    rows, experts = 64, 100
+    l = np.float32(rng.standard_normal((rows, experts))).astype(np.float64)
+    s = np.stack([ox.scores(r, True) for r in l])
+    bias = np.zeros(experts)
+    bias[:50] = 0.25
+    # expert 50 + i of row i: the logit whose score is another's value, rounded to fp32
+    for i in range(rows):
+        v = np.sort(s[i] + bias)[::-1]
+        target = v[min(k - 1 + i % 2, experts - 1)]
+        if target < 0.999:
+            l[i, 50 + i % 50] = np.float32(np.log(target / (1 - target)))
+    _run(l, k, sigmoid=True, bias=bias)
 
 
 def test_equal_logits_and_equal_values():
