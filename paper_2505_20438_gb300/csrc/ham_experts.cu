@@ -73,7 +73,7 @@ struct ExpertArgs {
   const uint8_t *ws;       // the handle's scales
   const uint8_t *xs;       // the rows'
   const int32_t *offsets, *order;
-  int gather;              // the rows are order's, not the slots' own
+  int gather, boxes;       // the rows are order's, not the slots' own; row maps
   void *out;
   uint8_t *out_scales;     // gated
   int32_t *err;
@@ -144,9 +144,11 @@ __global__ void __launch_bounds__(kSortWarps * 32) sort_rows_kernel(const uint4 
   for (; v < vecs; v += 32) codes[slot * vecs + v] = x[row * vecs + v];
 }
 
-// Maps of the rows with boxes of 16, 32, 64 and 128 of them; of rows by index the first alone, with boxes of one.
+// Maps of the rows with boxes of 16, 32 and 64 of them, as far as a CTA's may be that many; of rows by index the first
+// alone, with boxes of one.
+constexpr int kBoxes = 3;
 struct RowMaps {
-  CUtensorMap of[4];
+  CUtensorMap of[kBoxes];
 };
 
 // g / (1 + exp(-g)) by a reciprocal that is within a unit of its last place (a quotient's general form tests for and
@@ -215,7 +217,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     fence_mbar_init();
   }
   if (warp == 0 && lane == 0) {
-    for (int i = 0; i < (a.gather ? 1 : 4); ++i) prefetch_tensormap(&tx.of[i]);
+    for (int i = 0; i < a.boxes; ++i) prefetch_tensormap(&tx.of[i]);
     prefetch_tensormap(&tw);
   }
   cluster_sync_all();
@@ -336,7 +338,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     } else {
       int done = 0;
 #pragma unroll
-      for (int i = 3; i >= 0; --i)
+      for (int i = kBoxes - 1; i >= 0; --i)
         if (from.copies >> i & 1) {
           tma_load_2d_pair(dst + done * 2048, &tx.of[i], kb * kFp8Block, from.row + done * 16, bar, pol);
           done += 1 << i;
@@ -818,7 +820,8 @@ int run_experts(ham_fp8_weight *w, const void *x_codes, int32_t rows, ExpertArgs
   }
   RowMaps tx;
   int rc = HAM_OK;
-  for (int i = 0; i < (a.gather ? 1 : 4); ++i)
+  a.boxes = a.gather || a.slots <= 32 ? 1 : a.slots <= 64 ? 2 : 3;   // (a CTA's rows: half of the slots' next 32, 112 at most)
+  for (int i = 0; i < a.boxes; ++i)
     if (make_bytes_tensor_map(&tx.of[i], x_codes, rows, w->k, kFp8Block, a.gather ? 1 : 16 << i) != 0)
       rc = op_fail(HAM_ECUDA, "tensor map of the rows");
   if (rc == HAM_OK && e == cudaSuccess)
