@@ -151,12 +151,15 @@ struct RowMaps {
   CUtensorMap of[kBoxes];
 };
 
-// g / (1 + exp(-g)) by a reciprocal that is within a unit of its last place (a quotient's general form tests for and
-// mends cases that do not occur: 1 + exp(-g) is never below 1).
+// g / (1 + exp(-g)) from t = exp(-|g|), which never overflows: g t / (1 + t) below zero, g / (1 + t) above; the
+// reciprocal, of a number in 1..2, with one step of Newton's (a quotient's general form tests for and mends cases that do
+// not occur here).
 __device__ __forceinline__ float silu_of(float g) {
+  const float t = expf(-fabsf(g)), d = 1.f + t;
   float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + expf(-g)));
-  return g * r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d));
+  r = fmaf(r, fmaf(-d, r, 1.f), r);
+  return g * (g < 0.f ? t * r : r);
 }
 
 template <bool kGated>

@@ -208,6 +208,45 @@ def test_nan_stays_in_its_row():
     assert torch.equal(y, clean)
 
 
+def test_gates_far_from_zero():
+    """Gates down to -105 (where exp(g) leaves fp32's normal numbers and then fp32) and up to 300, a block each: the
+    values are the formula's, however small."""
+    rng = np.random.default_rng(12)
+    n, k, rows = 128 * 6, 128, 40
+    far = np.repeat([-85.0, -88.0, -95.0, -105.0, 60.0, 300.0], 128)
+    wg, wu = np.zeros((1, n, k)), rng.standard_normal((1, n, k)) * 64
+    wg[0, :, 0] = far / 4
+    (gc, gs), (uc, us) = _exact_codes(wg), _exact_codes(wu)
+    xc = rng.integers(0, 40, (rows, k)).astype(np.uint8)
+    xc[:, 0] = 0x48                          # 4
+    xs = np.full((rows, ops.scale_bytes(k)), 127, np.uint8)
+    h = alloc(n, k, (gc, gs), (uc, us))
+    codes, scales = empty_rows(rows, n)
+    ham.ham_fp8_experts_gated(h, dev(xc), dev(xs), dev(np.int32([0, rows])), dev(np.arange(rows, dtype=np.int32)), 1, codes, scales)
+    x, wg, wu = ops.decode_rows(xc, xs), ops.decode_weight(gc[0], gs[0]), ops.decode_weight(uc[0], us[0])
+    g, u, want = ops.gated(x, wg, wu)
+    assert (np.abs(g - far) <= np.abs(far) / 16).all()
+    # (A gate is one product, exact; the rest as in gated_slack.  2^-149: the exponential's last place, where it is not a
+    # normal number.)
+    silu = np.abs(ops.silu(g))
+    check_codes(codes, scales, want, silu * product_slack(x, wu) + 2.0 ** -20 * silu * np.abs(u) + 2.0 ** -149 * np.abs(g * u))
+
+
+def _exact_codes(w):
+    """e4m3 codes and block scales nearest to weights [experts][n][k] (n, k multiples of 128)."""
+    e, n, k = w.shape
+    b = w.reshape(e, n // 128, 128, k // 128, 128)
+    x = ops.block_exponent(np.abs(b).max(axis=(2, 4)))
+    q = (b * 2.0 ** -x[:, :, None, :, None].astype(float)).reshape(e, n, k)
+    values = ops.code_values()
+    order = np.argsort(np.where(np.isnan(values), np.inf, values))[:254]
+    at = np.clip(np.searchsorted(values[order], q), 1, 253)
+    near = np.where(q - values[order][at - 1] < values[order][at] - q, at - 1, at)
+    s = np.full((e, n // 128, ops.scale_bytes(k)), 127, np.uint8)
+    s[:, :, :k // 128] = x + 127
+    return order[near].astype(np.uint8), s
+
+
 def test_bad_offsets_and_order_are_reported():
     """Offsets that are no grouping compute nothing, an order entry out of range counts as entry 0; both are reported."""
     import torch
