@@ -65,8 +65,9 @@ __global__ void lay_out_expert_scales_kernel(const uint8_t *__restrict__ scales,
 // registers.
 //
 // A thread of the epilogue has one feature (a lane) and up to 128 slots (columns).  Plain outputs are neighbours across
-// a warp's lanes.  Of a gated product lanes 0..15 hold the gate and 16..31 the up projection of 16 features: one shuffle
-// each gives the lower lanes the even slots' products, the upper ones the odd slots'.  A slot's largest magnitude over
+// a warp's lanes.  Of a gated product 16 lanes hold the gate and 16 the up projection of 16 features: half a warp reads
+// both of half the slots, the other half those of the others (with lanes exchanged by shuffles 4096 rows of 8 experts took
+// 474 us).  A slot's largest magnitude over
 // the 128 features of a scale is wanted from both CTAs' warps: 16 bits of each (exponent and seven bits, all that the
 // scale depends on) through shared memory and the pair's.
 struct ExpertArgs {
@@ -151,15 +152,18 @@ struct RowMaps {
   CUtensorMap of[kBoxes];
 };
 
-// g / (1 + exp(-g)) from t = exp(-|g|), which never overflows: g t / (1 + t) below zero, g / (1 + t) above; the
-// reciprocal, of a number in 1..2, with one step of Newton's (a quotient's general form tests for and mends cases that do
-// not occur here).
-__device__ __forceinline__ float silu_of(float g) {
-  const float t = expf(-fabsf(g)), d = 1.f + t;
-  float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d));
-  r = fmaf(r, fmaf(-d, r, 1.f), r);
-  return g * (g < 0.f ? t * r : r);
+// u g / (1 + exp(-g)), of two numbers, from t = exp(-|g|), which never overflows: g t / (1 + t) below zero, g / (1 + t)
+// above; the reciprocal, of a number in 1..2, with one step of Newton's (a quotient's general form tests for and mends
+// cases that do not occur here).
+__device__ __forceinline__ float2 silu_mul2(float2 g, float2 u) {
+  const float2 one = make_float2(1.f, 1.f), t = make_float2(expf(-fabsf(g.x)), expf(-fabsf(g.y)));
+  const float2 d = add2(t, one);
+  float2 r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(d.x));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(d.y));
+  r = fma2(r, fma2(make_float2(-d.x, -d.y), r, one), r);
+  const float2 s = mul2(make_float2(g.x < 0.f ? t.x : 1.f, g.y < 0.f ? t.y : 1.f), r);
+  return mul2(mul2(g, s), u);
 }
 
 template <bool kGated>
@@ -521,7 +525,9 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         half = 0;
       }
       const int n = half ? t.n1 : t.n0;
-      float v[128];                              // a feature's sums, slot after slot
+      // Plain: a feature's sums, slot after slot.  Gated: the gate's of feature 16 quarter + lane % 16 and from 64 on the up
+      // projection's, 16 columns of each 32, the first ones (lanes 0..15) or the others.
+      float v[128];
       bool ok = true;
 #pragma unroll 1
       for (int c = 0; c < parts; ++c) {
@@ -536,20 +542,32 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         }
         tc_fence_after();
         const uint32_t acc = tmem + b * kTileSlots + (half ? t.n0 : 0) + ((uint32_t)(quarter * 32) << 16);
+        const auto load = [&](int q, float *first, float *second) {  // 32 columns: plain; gated: the gate's, the up's
+          if constexpr (kGated) {
+            tmem_ld16x2(acc + q * 32, *reinterpret_cast<uint32_t(*)[16]>(first));
+            tmem_ld16x2(acc + q * 32 + (16u << 16), *reinterpret_cast<uint32_t(*)[16]>(second));
+          } else {
+            tmem_ld32(acc + q * 32, *reinterpret_cast<uint32_t(*)[32]>(first));
+          }
+        };
         if (c == 0) {
 #pragma unroll
           for (int q = 0; q < 4; ++q)
-            if (q * 32 < n) tmem_ld32(acc + q * 32, *reinterpret_cast<uint32_t(*)[32]>(v + q * 32));
+            if (q * 32 < n) load(q, v + q * (kGated ? 16 : 32), v + 64 + q * 16);
           tmem_wait_ld();
         } else {
 #pragma unroll
           for (int q = 0; q < 4; ++q)
             if (q * 32 < n) {
               float f[32];
-              tmem_ld32(acc + q * 32, *reinterpret_cast<uint32_t(*)[32]>(f));
+              load(q, f, f + 16);
               tmem_wait_ld();
 #pragma unroll
-              for (int j = 0; j < 32; ++j) v[q * 32 + j] += f[j];
+              for (int j = 0; j < 32; j += 2) {
+                const int at = !kGated ? q * 32 + j : j < 16 ? q * 16 + j : 48 + q * 16 + j;
+                const float2 s = add2(make_float2(v[at], v[at + 1]), make_float2(f[j], f[j + 1]));
+                v[at] = s.x, v[at + 1] = s.y;
+              }
             }
         }
         tc_fence_before();
@@ -610,17 +628,15 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       } else {
         const int buffer = group * 2 + (taken & 1);
         uint16_t *key = keys + buffer * (8 * 128);
-        const bool upper = lane & 16;
-        float h[64];                             // column 2 i + lane / 16 of feature 16 quarter + lane % 16
+        float h[64];                             // columns 32 (i / 16) + 16 (lane / 16) + i % 16
         if (ok) {
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             if (q * 32 < n) {
 #pragma unroll
-              for (int i = 16 * q; i < 16 * q + 16; ++i) {
-                const float other = __shfl_xor_sync(kFull, upper ? v[2 * i] : v[2 * i + 1], 16);
-                const float own = upper ? v[2 * i + 1] : v[2 * i];
-                h[i] = silu_of(upper ? other : own) * (upper ? own : other);
+              for (int i = 16 * q; i < 16 * q + 16; i += 2) {
+                const float2 s = silu_mul2(make_float2(v[i], v[i + 1]), make_float2(v[64 + i], v[64 + i + 1]));
+                h[i] = s.x, h[i + 1] = s.y;
               }
             } else {
 #pragma unroll
@@ -644,16 +660,17 @@ __global__ void __launch_bounds__(kPairThreads, 1)
               const float other = __shfl_xor_sync(kFull, high ? m[i] : m[c + i], o);
               m[i] = fmaxf(high ? m[c + i] : m[i], other);
             }
-          uint16_t *mine = key + (side * 4 + quarter) * 128;
-          const uint32_t theirs = cluster_map_shared(smem_u32(mine), side ^ 1);
+          uint32_t b[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int column = 8 * (lane & 15) + 2 * i + (lane >> 4);
-            const uint32_t u = __float_as_uint(m[i]);
-            const uint16_t b = (uint16_t)(u > 0x7f800000u ? 0u : (u >> 16) | (u != 0u));
-            mine[column] = b;
-            asm volatile("st.shared::cluster.u16 [%0], %1;" ::"r"(theirs + column * 2), "h"(b) : "memory");
+            const uint32_t bits = __float_as_uint(m[i]);
+            b[i] = bits > 0x7f800000u ? 0u : (bits >> 16) | (bits != 0u);
           }
+          const uint32_t b01 = b[0] | b[1] << 16, b23 = b[2] | b[3] << 16;
+          uint16_t *mine = key + (side * 4 + quarter) * 128 + (lane & 12) * 8 + (lane & 16) + (lane & 3) * 4;
+          *reinterpret_cast<uint2 *>(mine) = make_uint2(b01, b23);
+          asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(cluster_map_shared(smem_u32(mine), side ^ 1)), "r"(b01), "r"(b23)
+                       : "memory");
           __syncwarp();
           if (lane < 2) mbar_arrive_cluster(cluster_map_shared(smem_u32(&keys_full[buffer]), lane));
           ok = warp_wait_cluster(&keys_full[buffer], (taken >> 1) & 1u, abort_flag);
@@ -669,7 +686,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
 #pragma unroll
           for (int i = 0; i < 8; ++i) top = max(top, (uint32_t)key[i * 128 + column]);
           const int e = fp8_exponent(__uint_as_float(top << 16));
-          power[(column & 1) * 64 + (column >> 1)] = fp8_pow2(-e);
+          power[column] = fp8_pow2(-e);
           if (side == 0 && column < n && slot < t.count) {
             uint8_t *s = a.out_scales + (int64_t)(t.slot0 + slot) * a.out_sk;
             s[t.ct] = (uint8_t)(e + 127);
@@ -679,16 +696,20 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         }
         named_barrier(1 + group, 128);
         uint8_t *codes = code_rows + group * (128 * 64);
-        uint8_t *to = codes + (lane >> 4) * 64 + quarter * 16 + (lane & 15);
+        // (rows of an odd 16 change places with their neighbours, or both halves of a warp would write to the same banks)
+        uint8_t *to = codes + (lane & 16) * 64 + quarter * 16 + (lane & 15);
 #pragma unroll
         for (int q = 0; q < 4; ++q)
           if (q * 32 < n) {
 #pragma unroll
-            for (int i = 16 * q; i < 16 * q + 16; i += 4) {
-              const float4 p = *reinterpret_cast<const float4 *>(power + (lane >> 4) * 64 + i);
-              const uint32_t c = fp8_codes4(h[i] * p.x, h[i + 1] * p.y, h[i + 2] * p.z, h[i + 3] * p.w, 1.f);
+            for (int i = 0; i < 16; i += 4) {
+              const float4 p = *reinterpret_cast<const float4 *>(power + q * 32 + (lane & 16) + i);
+              const int at = 16 * q + i;
+              const float2 x = mul2(make_float2(h[at], h[at + 1]), make_float2(p.x, p.y));
+              const float2 y = mul2(make_float2(h[at + 2], h[at + 3]), make_float2(p.z, p.w));
+              const uint32_t c = fp8_codes4(x.x, x.y, y.x, y.y, 1.f);
 #pragma unroll
-              for (int j = 0; j < 4; ++j) to[(i + j) * 128] = (uint8_t)(c >> 8 * j);
+              for (int j = 0; j < 4; ++j) to[(q * 32 + i + (j ^ (lane >> 4))) * 64] = (uint8_t)(c >> 8 * j);
             }
           }
         named_barrier(1 + group, 128);
@@ -697,7 +718,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           const int slot = t.slot_at(half, r);
           if (slot < t.count && col < a.n)         // (n is a multiple of 16)
             *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(a.out) + (int64_t)(t.slot0 + slot) * a.n + col) =
-                *reinterpret_cast<const uint4 *>(codes + r * 64 + c);
+                *reinterpret_cast<const uint4 *>(codes + (r ^ (r >> 4 & 1)) * 64 + c);
         }
         named_barrier(1 + group, 128);             // (read before the next tile's are written)
       }
