@@ -94,12 +94,12 @@ def test_block(t, k, settings):
     b.check(x, k, settings)
 
 
-def test_block_captured():
+@pytest.mark.parametrize("t,k", [(40, 2), (400, 3)])    # rows by index; sorted first
+def test_block_captured(t, k):
     """Every replay routes its own rows; nothing depends on the counts of the capture."""
     import torch
     rng = np.random.default_rng(1)
     b = Block(rng, 256, 8, 128)
-    t, k = 40, 2
     b.buffers(t, k)
     bias = dev(np.float32(0.1 * rng.standard_normal(8)))
     settings = dict(score=ham.HAM_SCORE_SIGMOID, bias=bias)
@@ -138,3 +138,48 @@ def test_a_padded_batch():
     assert int(b.offsets[-1]) == 32
     assert torch.equal(b.out[:16], live[:16]) and torch.equal(b.out[16:], x[16:])
     assert torch.isnan(b.y[32:].float()).all()
+
+
+def test_two_graphs_and_a_stream_at_once():
+    """Two captured blocks of many rows and calls on a third stream share the weights: each has memory of its own for the
+    sorted rows."""
+    import torch
+    rng = np.random.default_rng(3)
+    t, k = 700, 2
+    b = Block(rng, 256, 8, 128)
+    b.buffers(t, k)
+    x = [torch.randn((t, 256), device="cuda").bfloat16() for _ in range(3)]
+    b.run(x[0], k)
+    rows = []
+    for v in x:
+        ham.ham_add_norm(v, b.norm, 1e-5, codes=b.x8[0], scales=b.x8[1])
+        rows.append([a.clone() for a in b.x8])
+    outs = [[torch.zeros_like(a) for a in b.h8] for _ in x]
+
+    def call(i, stream=None):
+        ham.ham_fp8_experts_gated(b.h_gated, *rows[i], b.offsets, b.order, k, *outs[i], stream=stream)
+
+    want = []
+    for i in range(3):
+        call(i)
+        want.append([a.clone() for a in outs[i]])
+    torch.cuda.synchronize()
+    graphs, streams = [], [torch.cuda.Stream() for _ in range(3)]
+    for i in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[i], stream=streams[i]):
+            for _ in range(3):
+                call(i)
+    for o in outs:
+        for a in o:
+            a.zero_()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                graphs[i].replay()
+        call(2, streams[2])
+    torch.cuda.synchronize()
+    for o, w in zip(outs, want):
+        assert all(torch.equal(a, c) for a, c in zip(o, w))
+    assert ham.ham_fp8_weight_status(b.h_gated) == ham.HAM_DEVERR_NONE
