@@ -82,7 +82,6 @@ struct ExpertArgs {
   uint64_t wait_ns;
 };
 
-constexpr int kSortFrom = 64;           // slots an expert on average from which gathered rows are sorted first
 constexpr int kExpertPart = 16;         // K blocks of one accumulator
 constexpr int kExpertStages = 6;
 constexpr int kExpertStageBytes = 2 * kBlockBytes;  // the weights' block, 64 + 64 rows
@@ -823,8 +822,14 @@ int run_experts(ham_fp8_weight *w, const void *x_codes, int32_t rows, ExpertArgs
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;
   uint8_t *sorted = nullptr;
-  // Copies by index take some 80 clocks for four rows, boxes of neighbouring rows four a row.
-  if (a.gather && a.slots > kSortFrom * a.experts) {
+  // Rows by index, or sorted first?  A copy by index takes its thread some 80 clocks for four rows, a box of neighbouring
+  // rows four a row, so that a K block costs some 35 ns more, from 16 slots an expert on 4.5 ns a slot; sorting takes 2.8 us
+  // and the rows' bytes twice.  (us by index / sorted, K 4096, 2048 features of 32 experts, 4, 8, 16, 24, 32, 64, 128 slots
+  // an expert: 94.1 / 89.9, 96.1 / 91.6, 97.5 / 92.2, 103.8 / 92.6, 120.4 / 93.5, 157.6 / 96.8, 234.6 / 104.1; K 1024, 512
+  // features of 16, 16, 32, 64, 96 slots: 11.4 / 14.4, 12.5 / 15.1, 14.4 / 16.2, 16.2 / 17.1.)
+  const int64_t blocks = (int64_t)std::min(a.slots, a.experts) * a.tiles * a.kbs / (device_sms() / 2);  // a pair's
+  const int64_t more_ns = blocks * std::max<int64_t>(35, (int64_t)a.slots * 9 / (2 * a.experts));
+  if (a.gather && more_ns > 2800 + (int64_t)a.slots * w->k / 3400) {
     const size_t codes = (size_t)a.slots * w->k, scales = (size_t)a.slots * w->sk;
     cudaMemPool_t pool = row_pool(w->device);
     if (pool && cudaMallocFromPoolAsync(reinterpret_cast<void **>(&sorted), codes + scales, pool, s) != cudaSuccess) {

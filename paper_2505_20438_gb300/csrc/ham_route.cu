@@ -462,7 +462,7 @@ __global__ void __launch_bounds__(kChooseWarps * 32) choose_kernel(const __grid_
 // lanes of equal experts finding one another, 32 pairs at a time, 131072 pairs took 27 us.)
 //
 // A CTA that has no more than kStaged pairs puts them in their order in shared memory and writes each expert's one after
-// another; scattered words cost a CTA some 8 us for 16384.
+// another (1024 rows of 8: 9.1 us a call against 10.7 with scattered words; 16384 rows 30.6 against 33.1).
 constexpr int kGroupThreads = 1024, kGroupWarps = 32, kGroupCtas = 8, kStaged = 16384;
 // (Pitch of the histograms: odd, so that four lanes that add up eight warps each of one expert's meet no bank twice.)
 __host__ __device__ constexpr int group_pitch(int experts) { return experts | 1; }
@@ -613,8 +613,9 @@ __global__ void __launch_bounds__(kGroupThreads) group_kernel(const __grid_const
   group_pairs(a, hist, staged != 0);
 }
 
-// A few rows: the choice and the grouping by one block.
-constexpr int kFewRows = 32, kAloneRows = 1024;
+// A few rows: the choice and the grouping by one block.  (us with one launch / with two, 64 experts: 8 rows 5.4 / 6.2, 16 rows
+// 5.7 / 5.9, 32 rows 6.6 / 6.1; 256 experts: 6.3 / 7.0 for 8 rows, 8.7 / 7.0 for 32.)
+constexpr int kFewRows = 16;
 template <int kPer>
 __global__ void __launch_bounds__(kGroupThreads) route_few_kernel(const __grid_constant__ RouteArgs a) {
   extern __shared__ int32_t hist[];              // the grouping's, before that [warps][values]
@@ -723,7 +724,9 @@ cudaError_t launch_route(const RouteArgs &a, cudaStream_t s) {
   const int blocks = std::min((a.rows + kChooseWarps - 1) / kChooseWarps, device_sms() * kChooseBlocks);
   cudaError_t e = launch_after<choose_kernel<kPer>>(dim3((unsigned)blocks), dim3(kChooseWarps * 32), 0, dim3(1), s, a);
   if (e == cudaSuccess) e = allow(group_kernel, group_smem(kMostExperts, true), done, dev);
-  const unsigned ctas = a.rows <= kAloneRows ? 1 : kGroupCtas;
+  // (The whole call with one block / a cluster of eight, 64 experts, us: 512 rows 7.5 / 8.2, 1024 rows 9.1 / 9.9, 2048 rows
+  // 13.1 / 10.5; 256 experts: 8.7 / 9.6, 10.7 / 11.7, 15.9 / 12.7.)
+  const unsigned ctas = a.rows <= 1024 ? 1 : kGroupCtas;
   const int stretch = ((a.rows + (int)ctas * kGroupWarps - 1) / ((int)ctas * kGroupWarps) + 31) & ~31;
   const bool staged = (int64_t)stretch * kGroupWarps * a.top_k <= kStaged;
   return e != cudaSuccess ? e : launch_after<group_kernel>(dim3(ctas), dim3(kGroupThreads), (size_t)group_smem(a.experts, staged), dim3(ctas), s, a, (int)staged);
