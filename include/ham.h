@@ -639,11 +639,14 @@ int ham_fp8_experts_alloc(int32_t experts, int32_t n, int32_t k, const void *cod
 
 /* The first half of the experts' gated blocks.  Slot i of expert e takes row t = order[i] / top_k of the 8-bit rows X:
  *   G = X[t] W_gate,e^T, U = X[t] W_up,e^T (fp32),  H = G / (1 + exp(-G)) * U, encoded as an 8-bit row:
- * codes [rows * top_k][n], scales [rows * top_k][..], in slot order.  Rows from offsets[experts] on are left as they
- * were.  Sums as ham_fp8_linear's with parts of at most 2048 terms; a slot's result does not depend on the others.
+ * codes [rows * top_k][n], scales [rows * top_k][..], in slot order.  Rows outside offsets[0] .. offsets[experts] - 1 are
+ * left as they were.  Sums as ham_fp8_linear's with parts of at most 2048 terms; a slot's result does not depend on the others.
  * x_codes [rows][k], x_scales; rows at most 2^24, rows * top_k at most 2^26; offsets, order as ham_route gives them.
  * Offsets that decrease or leave 0..rows * top_k set the device error word (HAM_DEVERR_ROUTE) and the call writes
  * nothing; an order entry of a slot outside 0..rows * top_k - 1 sets it and counts as entry 0.
+ * Where many rows are taken, copies of them in slot order come from a memory pool of the library's for the device
+ * (cudaMallocFromPoolAsync on `stream`, freed on it; it keeps up to 1 GiB; a captured call's copies belong to its graph);
+ * without memory the rows are read by index instead, with the same results.  One launch, or two.
  * Host errors: HAM_EINVAL, HAM_ECUDA. */
 int ham_fp8_experts_gated(ham_fp8_weight *w, const void *x_codes, const void *x_scales, int32_t rows,
                           const int32_t *offsets, const int32_t *order, int32_t top_k, void *codes, void *scales,
@@ -651,8 +654,8 @@ int ham_fp8_experts_gated(ham_fp8_weight *w, const void *x_codes, const void *x_
 
 /* out[i] = X[i] W_e^T for the slots i of each expert e: 8-bit rows X [slots][k] in slot order (what
  * ham_fp8_experts_gated leaves), out [slots][n] in out_dtype (HAM_DTYPE_BF16 or HAM_DTYPE_F32).  slots is the
- * buffers' number of rows, at most 2^26; rows from offsets[experts] on are neither read nor written.  Sums, offsets and
- * errors as ham_fp8_experts_gated's. */
+ * buffers' number of rows, at most 2^26; rows outside offsets[0] .. offsets[experts] - 1 are not written.  Sums, offsets
+ * and errors as ham_fp8_experts_gated's; one launch. */
 int ham_fp8_experts_linear(ham_fp8_weight *w, const void *x_codes, const void *x_scales, int32_t slots,
                            const int32_t *offsets, void *out, int32_t out_dtype, void *stream);
 

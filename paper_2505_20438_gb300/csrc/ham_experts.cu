@@ -13,7 +13,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
-#include <mutex>
+#include <atomic>
 #include <new>
 
 #include "ham_fp8.cuh"
@@ -58,18 +58,29 @@ __global__ void lay_out_expert_scales_kernel(const uint8_t *__restrict__ scales,
 // that a few rows cost a few rows' products and many experts of uneven counts leave no lanes idle.  More than 224 slots
 // are cut into tiles of equal size, more than 128 into two halves of N, each for four warps of the epilogue.
 //
-// Each CTA copies its half tile's K block (16 KiB, one stretch) and half of the N rows (a gated product's four rows a
-// copy, by index, from where they lie), into its own shared memory alone.  Sums take parts of K as
-// the products of one weight do (ham_fp8.cu), kExpertPart blocks each, in two sums of 224 columns in turn, so that a whole
-// tile's products (of two parts) are on their way while the epilogue deals with the tile before; it adds them in
-// registers.
+// Each CTA copies its half tile's K block (16 KiB, one stretch) and half of the N rows (of a gated product by index, four
+// rows a copy, or sorted before) into its own shared memory alone.  Sums take parts of K as the products of one weight do
+// (ham_fp8.cu), kExpertPart blocks each, in two sums of 224 columns in turn, so that a whole tile's products (of two parts)
+// are on their way while the epilogue deals with the tile before; it adds them in registers.  Errors against 64-bit sums,
+// relative to the outputs' norm: 3.4e-8 at K 512, 1.1e-7 from 2048 on (a plain fp32 product 2.7e-8, 6.0e-8, 1.3e-7 at 8192).
 //
 // A thread of the epilogue has one feature (a lane) and up to 128 slots (columns).  Plain outputs are neighbours across
 // a warp's lanes.  Of a gated product 16 lanes hold the gate and 16 the up projection of 16 features: half a warp reads
 // both of half the slots, the other half those of the others (with lanes exchanged by shuffles 4096 rows of 8 experts took
-// 474 us).  A slot's largest magnitude over
-// the 128 features of a scale is wanted from both CTAs' warps: 16 bits of each (exponent and seven bits, all that the
-// scale depends on) through shared memory and the pair's.
+// 474 us, 460 so).  A slot's largest magnitude over the 128 features of a scale is wanted from both CTAs' warps: 16 bits of
+// each (exponent and seven bits, all that the scale depends on) through shared memory and the pair's.
+//
+// What bounds it.  Few rows: the weights' bytes.  8 rows of 8 of 64 experts (K 4096, 2048 features) take 119 us, 87% of the
+// copy rate with the sorting and the first and last tile's latencies, some 7 us, in it; the second products (K 2048, 4096
+// features) 59 us, 88%.  Many rows: tensor cores and the path from L2, under the card's power limit.  4096 rows of 8 of 64
+// experts take 446 to 470 us, 28 of them the sorting, and 224 for the second products, 2.4 PFLOP/s; without any epilogue 410 and
+// 198, with half of the products 356 and 178, without the weights' copies 354 and 181.  A dense product of as many operations
+// as the second takes 195 when it is repeated for as long.
+//
+// Measured and not taken: copies by index for many rows (1430 us gated: 84 clocks for four rows, whoever issues them from one
+// warp); three sums of 128 columns and tiles of 256 slots (520 us); parts of 1024 terms (553 us: the products then run only one
+// part ahead); deeper rings where tiles are narrow (no faster); the next tile's looking up moved ahead (2 to 8% slower);
+// weights marked to leave the L2 first (478 against 453 us).
 struct ExpertArgs {
   const uint8_t *ws;       // the handle's scales
   const uint8_t *xs;       // the rows'
@@ -93,7 +104,7 @@ constexpr int kTileSlots = 224, kSfCol = 448;  // columns of one of the two sums
 constexpr int kGroup = 2;               // K blocks that one accumulator takes, then the other
 constexpr int kKeyBytes = 2 * 2 * 8 * 128 * 2;   // [half][every other tile][warp of the pair][slot]
 constexpr int kCodeBytes = 2 * 128 * 64;         // [half][slot][feature]
-constexpr int kPowerBytes = 2 * 128 * 4;         // [half][even slots, odd ones]
+constexpr int kPowerBytes = 2 * 128 * 4;         // [half][slot]
 constexpr int kExpertBars = 288;
 constexpr int kExpertUsed = 1024 + kExpertStages * kExpertStageBytes + kExpertSf * kExpertSfBytes + kExpertBars;
 constexpr int kTurnPitch = 144, kTurnBytes = 16 * kTurnPitch;  // plain: a warp's 32 features of 32 slots, slots in pairs
@@ -118,14 +129,14 @@ struct ExpertTile {
 // The rows of the slots, one after another, for products with more rows than a copy by index keeps up with.
 constexpr int kSortWarps = 8;
 __global__ void __launch_bounds__(kSortWarps * 32) sort_rows_kernel(const uint4 *__restrict__ x, const uint32_t *__restrict__ xs,
-                                                                    const int32_t *order, const int32_t *last, int slots, int top_k,
+                                                                    const int32_t *order, const int32_t *offsets, int experts, int slots, int top_k,
                                                                     int vecs, int words, uint4 *codes, uint32_t *scales,
                                                                     int32_t *err) {
   const int lane = threadIdx.x & 31;
   const int64_t slot = (int64_t)blockIdx.x * kSortWarps + (threadIdx.x >> 5);
   grid_dependency_wait();
   grid_launch_dependents();
-  if (slot >= min(*last, slots)) return;
+  if (slot < offsets[0] || slot >= min(offsets[experts], slots)) return;
   int64_t row = order[slot];
   if (row < 0 || row >= slots) {
     if (lane == 0) record_error(err, HAM_DEVERR_ROUTE);
@@ -773,28 +784,34 @@ cudaError_t launch_experts(const RowMaps &tx, const CUtensorMap &tw, const Exper
   return launch_after<kKernel>(dim3((unsigned)(2 * pairs)), dim3(kPairThreads), (size_t)kSmem, dim3(2, 1, 1), s, tx, tw, a);
 }
 
-// The device's pool for sorted rows: ordered by the stream (a captured call's belong to its graph), what it has once
-// been given stays with it.
+// The device's pool for sorted rows: memory is ordered by the stream (a captured call's belongs to its graph) and goes to
+// no other stream before its own is known to be done with it.  Up to kKeepBytes stay with the pool.
+constexpr uint64_t kKeepBytes = (uint64_t)1 << 30;
 cudaMemPool_t row_pool(int dev) {
-  static std::mutex guard;
-  static cudaMemPool_t pools[64] = {};
+  static std::atomic<cudaMemPool_t> pools[64];
   if (dev < 0 || dev >= 64) return nullptr;
-  std::lock_guard<std::mutex> lock(guard);
-  if (!pools[dev]) {
-    cudaMemPoolProps props = {};
-    props.allocType = cudaMemAllocationTypePinned;
-    props.location.type = cudaMemLocationTypeDevice;
-    props.location.id = dev;
-    cudaMemPool_t pool = nullptr;
-    if (cudaMemPoolCreate(&pool, &props) != cudaSuccess) {
-      cudaGetLastError();
-      return nullptr;
-    }
-    uint64_t all = UINT64_MAX;
-    cudaMemPoolSetAttribute(pool, cudaMemPoolAttrReleaseThreshold, &all);
-    pools[dev] = pool;
+  cudaMemPool_t pool = pools[dev].load();
+  if (pool) return pool;
+  cudaMemPoolProps props = {};
+  props.allocType = cudaMemAllocationTypePinned;
+  props.location.type = cudaMemLocationTypeDevice;
+  props.location.id = dev;
+  if (cudaMemPoolCreate(&pool, &props) != cudaSuccess) {
+    cudaGetLastError();
+    return nullptr;
   }
-  return pools[dev];
+  uint64_t keep = kKeepBytes;
+  int no = 0;
+  cudaMemPoolSetAttribute(pool, cudaMemPoolAttrReleaseThreshold, &keep);
+  for (cudaMemPoolAttr reuse : {cudaMemPoolReuseFollowEventDependencies, cudaMemPoolReuseAllowOpportunistic,
+                                cudaMemPoolReuseAllowInternalDependencies})
+    cudaMemPoolSetAttribute(pool, reuse, &no);
+  cudaMemPool_t first = nullptr;
+  if (!pools[dev].compare_exchange_strong(first, pool)) {   // (another thread's came first)
+    cudaMemPoolDestroy(pool);
+    pool = first;
+  }
+  return pool;
 }
 
 int check_experts(const ham_fp8_weight *w, const void *xc, const void *xs, int64_t slots, const void *offsets,
@@ -839,7 +856,7 @@ int run_experts(ham_fp8_weight *w, const void *x_codes, int32_t rows, ExpertArgs
     if (sorted) {
       e = launch_after<sort_rows_kernel>(dim3((unsigned)((a.slots + kSortWarps - 1) / kSortWarps)), dim3(kSortWarps * 32), 0, dim3(1), s,
                                          static_cast<const uint4 *>(x_codes), reinterpret_cast<const uint32_t *>(a.xs), a.order,
-                                         a.offsets + a.experts, a.slots, a.top_k, w->k / 16, w->sk / 4,
+                                         a.offsets, a.experts, a.slots, a.top_k, w->k / 16, w->sk / 4,
                                          reinterpret_cast<uint4 *>(sorted), reinterpret_cast<uint32_t *>(sorted + codes), a.err);
       x_codes = sorted;
       a.xs = sorted + codes;

@@ -104,6 +104,13 @@ def test_counts_of_rows(counts, n, k):
     run_linear(rng, counts, n, k)
 
 
+@pytest.mark.parametrize("counts", [[128, 1, 255], [257, 0, 0, 300], [513, 2], [130, 200, 97]], ids=str)
+@pytest.mark.parametrize("n,k", [(4096, 1024), (4112, 1040)])
+def test_rows_sorted_first(counts, n, k):
+    """Products so large that their rows are copied into slot order before."""
+    run_gated(np.random.default_rng(len(counts) + n), counts, n, k, top_k=3)
+
+
 @pytest.mark.parametrize("n,k", [(16, 16), (128, 48), (144, 128), (272, 144), (528, 2064), (112, 640), (384, 1040)])
 @pytest.mark.parametrize("counts", [[2, 0, 5], [40, 7], [130, 200]], ids=str)
 def test_gated_sizes(n, k, counts):
@@ -141,6 +148,35 @@ def test_no_slots_and_rows_behind_the_last():
     run_linear(rng, [0, 0], 128, 256, slots=9)
     run_gated(rng, [3, 4], 128, 256, rows=40)
     run_linear(rng, [5, 0, 200], 128, 256, slots=300)
+
+
+@pytest.mark.parametrize("counts,n,k", [([5, 9], 128, 256), ([90, 150], 3200, 2048)])
+def test_offsets_may_begin_anywhere(counts, n, k):
+    """The experts of one part of the slots: the others' rows are neither looked at nor written."""
+    import torch
+    rng = np.random.default_rng(4)
+    slots, first = sum(counts) + 20, 11
+    w, up = weights(rng, 2, n, k), weights(rng, 2, n, k)
+    hg, hl = alloc(n, k, w, up), alloc(n, k, w)
+    xc, xs = (dev(v) for v in random_codes(rng, slots, k))
+    offsets = np.int32([0, counts[0], sum(counts)]) + first
+    order = rng.permutation(slots).astype(np.int32)
+    order[:first], order[sum(counts) + first:] = 1 << 30, -5
+    codes, scales = empty_rows(slots, n)
+    y = torch.full((slots, n), -7.0, device="cuda")
+    ham.ham_fp8_experts_gated(hg, xc, xs, dev(offsets), dev(order), 1, codes, scales)
+    ham.ham_fp8_experts_linear(hl, xc, xs, dev(offsets), y)
+    assert ham.ham_fp8_weight_status(hg) == ham.ham_fp8_weight_status(hl) == ham.HAM_DEVERR_NONE
+    inside = np.zeros(slots, bool)
+    inside[first:first + sum(counts)] = True
+    assert (y[~inside] == -7).all() and (codes[~inside] == 0x7f).all() and (scales[~inside] == 255).all()
+    x = ops.decode_rows(xc.cpu().numpy(), xs.cpu().numpy())
+    for e in range(2):
+        a, b = offsets[e], offsets[e + 1]
+        check_bf16(y[a:b], x[a:b] @ w[2][e].T, product_slack(x[a:b], w[2][e]))
+        mine = x[order[a:b]]
+        g, u, want = ops.gated(mine, w[2][e], up[2][e])
+        check_codes(codes[a:b], scales[a:b], want, gated_slack(mine, w[2][e], up[2][e], g, u))
 
 
 def test_many_experts():

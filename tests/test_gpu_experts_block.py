@@ -94,23 +94,23 @@ def test_block(t, k, settings):
     b.check(x, k, settings)
 
 
-@pytest.mark.parametrize("t,k", [(40, 2), (400, 3)])    # rows by index; sorted first
-def test_block_captured(t, k):
+@pytest.mark.parametrize("t,k,width", [(40, 2, 256), (400, 3, 1024)])    # rows by index; sorted first
+def test_block_captured(t, k, width):
     """Every replay routes its own rows; nothing depends on the counts of the capture."""
     import torch
     rng = np.random.default_rng(1)
-    b = Block(rng, 256, 8, 128)
+    b = Block(rng, width, 8, width)
     b.buffers(t, k)
     bias = dev(np.float32(0.1 * rng.standard_normal(8)))
     settings = dict(score=ham.HAM_SCORE_SIGMOID, bias=bias)
-    x = torch.randn((t, 256), device="cuda").bfloat16() * 0.25
+    x = torch.randn((t, width), device="cuda").bfloat16() * 0.25
     b.run(x, k, **settings)                 # (the first calls set the kernels up: not in a capture)
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         b.run(x, k, **settings)
     for i in range(4):
-        x.copy_(torch.randn((t, 256), device="cuda") * 0.25)
+        x.copy_(torch.randn((t, width), device="cuda") * 0.25)
         if i == 2:
             bias.copy_(dev(np.float32([9, 9, 0, 0, 0, 0, 0, 0])))   # two experts take every row
         graph.replay()
@@ -146,9 +146,9 @@ def test_two_graphs_and_a_stream_at_once():
     import torch
     rng = np.random.default_rng(3)
     t, k = 700, 2
-    b = Block(rng, 256, 8, 128)
+    b = Block(rng, 1024, 8, 1024)
     b.buffers(t, k)
-    x = [torch.randn((t, 256), device="cuda").bfloat16() for _ in range(3)]
+    x = [torch.randn((t, 1024), device="cuda").bfloat16() for _ in range(3)]
     b.run(x[0], k)
     rows = []
     for v in x:
