@@ -140,6 +140,19 @@ __device__ __noinline__ int choose_exactly(const RouteArgs &a, int row, double *
   return mine;
 }
 
+// ------------------------------------------------------------------------------------
+// The choice: a warp a row
+// ------------------------------------------------------------------------------------
+// A lane has kPer neighbouring experts, in registers: scores, values and the groups' sums (a group that lies in whole
+// lanes takes two shuffles a doubling) need no shared memory.  Each lane sorts its own; then the warp's largest first one
+// is taken top_k times, a reduction, a ballot and a shift of the owner's each.  Deciding in fp32 and only where two values
+// are nearer than their errors in fp64, for those values alone, costs a few comparisons a row: with whole rows computed
+// again 16384 rows of 256 with sigmoid and bias took 48 us, so 24.
+//
+// Bound by instructions, some 1200 a row of 256 experts in 8 groups at 2.8 a clock: 26 us for 16384 rows (with softmax
+// alone 17), where reading the logits takes 2.5.  An eighth of it is the sorting, a fifth the taking, a tenth the weights,
+// the rest the logits and their scores.
+//
 // The warp's rows from lane's experts lane * kPer .. lane * kPer + kPer - 1 of each.
 template <int kPer>
 struct Chooser {
@@ -462,8 +475,8 @@ __global__ void __launch_bounds__(kChooseWarps * 32) choose_kernel(const __grid_
 // lanes of equal experts finding one another, 32 pairs at a time, 131072 pairs took 27 us.)
 //
 // A CTA that has no more than kStaged pairs puts them in their order in shared memory and writes each expert's one after
-// another (1024 rows of 8: 9.1 us a call against 10.7 with scattered words; 16384 rows 30.6 against 33.1).
-constexpr int kGroupThreads = 1024, kGroupWarps = 32, kGroupCtas = 8, kStaged = 16384;
+// another (1024 rows of 8: 9.1 us a call against 10.7 with scattered words; 16384 rows, by eight CTAs, 30.6 against 33.1).
+constexpr int kGroupThreads = 1024, kGroupWarps = 32, kGroupCtas = 16, kStaged = 16384;
 // (Pitch of the histograms: odd, so that four lanes that add up eight warps each of one expert's meet no bank twice.)
 __host__ __device__ constexpr int group_pitch(int experts) { return experts | 1; }
 __host__ __device__ constexpr int group_smem(int experts, bool staged) {
@@ -521,8 +534,11 @@ __device__ __forceinline__ void group_pairs(const RouteArgs &a, int32_t *hist, b
     if (ctas > 1) {
       uint32_t c[kGroupCtas];
 #pragma unroll
-      for (int q = 0; q < kGroupCtas; ++q)
-        asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(c[q]) : "r"(cluster_map_shared(smem_u32(&count[tid]), q)));
+      for (int q = 0; q < kGroupCtas; ++q) {
+        c[q] = 0;
+        if (q < ctas)
+          asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(c[q]) : "r"(cluster_map_shared(smem_u32(&count[tid]), q)));
+      }
 #pragma unroll
       for (int q = 0; q < kGroupCtas; ++q) {
         if (q < rank) before += (int)c[q];
@@ -710,6 +726,29 @@ cudaError_t launch_combine(const CombineArgs &a, int rows, bool f32, cudaStream_
              : launch_after<combine_kernel<kEach, kGroups, uint16_t>>(grid, block, 0, dim3(1), s, a);
 }
 
+// CTAs of a grouping cluster at most: 16 need a group of SMs that holds as many.
+int group_ctas(int dev) {
+  static int known[64] = {};
+  if (dev >= 0 && dev < 64 && known[dev]) return known[dev];
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(kGroupCtas);
+  cfg.blockDim = dim3(kGroupThreads);
+  cfg.dynamicSmemBytes = (size_t)group_smem(kMostExperts, true);
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = kGroupCtas;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int n = 0;
+  const bool fits = cudaFuncSetAttribute(group_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+                    cudaOccupancyMaxActiveClusters(&n, group_kernel, &cfg) == cudaSuccess && n > 0;
+  if (!fits) cudaGetLastError();
+  const int ctas = fits ? kGroupCtas : 8;
+  if (dev >= 0 && dev < 64) known[dev] = ctas;
+  return ctas;
+}
+
 // Launches of Kernel<kPer> for the experts' number.
 template <int kPer>
 cudaError_t launch_route(const RouteArgs &a, cudaStream_t s) {
@@ -724,12 +763,15 @@ cudaError_t launch_route(const RouteArgs &a, cudaStream_t s) {
   const int blocks = std::min((a.rows + kChooseWarps - 1) / kChooseWarps, device_sms() * kChooseBlocks);
   cudaError_t e = launch_after<choose_kernel<kPer>>(dim3((unsigned)blocks), dim3(kChooseWarps * 32), 0, dim3(1), s, a);
   if (e == cudaSuccess) e = allow(group_kernel, group_smem(kMostExperts, true), done, dev);
+  if (e != cudaSuccess) return e;
   // (The whole call with one block / a cluster of eight, 64 experts, us: 512 rows 7.5 / 8.2, 1024 rows 9.1 / 9.9, 2048 rows
-  // 13.1 / 10.5; 256 experts: 8.7 / 9.6, 10.7 / 11.7, 15.9 / 12.7.)
-  const unsigned ctas = a.rows <= 1024 ? 1 : kGroupCtas;
-  const int stretch = ((a.rows + (int)ctas * kGroupWarps - 1) / ((int)ctas * kGroupWarps) + 31) & ~31;
+  // 13.1 / 10.5; 256 experts: 8.7 / 9.6, 10.7 / 11.7, 15.9 / 12.7.  With eight / with sixteen, 256 experts: 2048 rows 12.8 / 13.1,
+  // 4096 rows 15.1 / 15.5, 16384 rows 30.8 / 26.4; 128 experts, 32768 rows 50.5 / 36.5.)
+  const int ctas = a.rows <= 1024 ? 1 : a.rows <= 4096 ? 8 : group_ctas(dev);
+  const int stretch = ((a.rows + ctas * kGroupWarps - 1) / (ctas * kGroupWarps) + 31) & ~31;
   const bool staged = (int64_t)stretch * kGroupWarps * a.top_k <= kStaged;
-  return e != cudaSuccess ? e : launch_after<group_kernel>(dim3(ctas), dim3(kGroupThreads), (size_t)group_smem(a.experts, staged), dim3(ctas), s, a, (int)staged);
+  return launch_after<group_kernel>(dim3((unsigned)ctas), dim3(kGroupThreads), (size_t)group_smem(a.experts, staged),
+                                    dim3((unsigned)ctas), s, a, (int)staged);
 }
 
 }  // namespace
