@@ -949,6 +949,7 @@ int ham_fp8_experts_alloc(int32_t experts, int32_t n, int32_t k, const void *cod
     ham_fp8_weight_free(w);
     return op_fail(HAM_ECUDA, "weight layout: %s", cudaGetErrorString(e));
   }
+  if (codes_up) ham::row_pool(w->device);        // (not first in a call, which may be captured)
   *out = w;
   return HAM_OK;
 }
