@@ -72,10 +72,10 @@ __global__ void lay_out_expert_scales_kernel(const uint8_t *__restrict__ scales,
 //
 // What bounds it.  Few rows: the weights' bytes.  8 rows of 8 of 64 experts (K 4096, 2048 features) take 119 us, 87% of the
 // copy rate with the sorting and the first and last tile's latencies, some 7 us, in it; the second products (K 2048, 4096
-// features) 59 us, 88%.  Many rows: tensor cores and the path from L2, under the card's power limit.  4096 rows of 8 of 64
-// experts take 446 to 470 us, 28 of them the sorting, and 224 for the second products, 2.4 PFLOP/s; without any epilogue 410 and
-// 198, with half of the products 356 and 178, without the weights' copies 354 and 181.  A dense product of as many operations
-// as the second takes 195 when it is repeated for as long.
+// features) 59 us, 88%.  Many rows: the path from L2, and the card's power limit.  4096 rows of 8 of 64 experts take 446 to 470 us,
+// 25 of them the sorting, and 224 for the second products, 2.4 PFLOP/s.  A K block of the usual tile, 171 slots of 512, is 27 KB
+// a CTA in 0.33 us: 83 GB/s an SM, 12.6 TB/s in all, where the dense pair kernel's 32 KB come at 93 and feed 256 rows.  Without any
+// epilogue the calls take 410 and 198, with half of the products 356 and 178, without the weights' copies 354 and 181.
 //
 // Measured and not taken: copies by index for many rows (1430 us gated: 84 clocks for four rows, whoever issues them from one
 // warp); three sums of 128 columns and tiles of 256 slots (520 us); parts of 1024 terms (553 us: the products then run only one
@@ -136,8 +136,9 @@ __global__ void __launch_bounds__(kSortWarps * 32) sort_rows_kernel(const uint4 
   const int64_t slot = (int64_t)blockIdx.x * kSortWarps + (threadIdx.x >> 5);
   grid_dependency_wait();
   grid_launch_dependents();
-  if (slot < offsets[0] || slot >= min(offsets[experts], slots)) return;
-  int64_t row = order[slot];
+  if (slot >= slots) return;
+  int64_t row = order[slot];                     // (on its way with the offsets)
+  if (slot < offsets[0] || slot >= offsets[experts]) return;
   if (row < 0 || row >= slots) {
     if (lane == 0) record_error(err, HAM_DEVERR_ROUTE);
     row = 0;
