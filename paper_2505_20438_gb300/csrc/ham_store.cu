@@ -369,7 +369,7 @@ using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t,
                                  const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
                                  const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeTiled tensor_map_encoder() {
+EncodeTiled driver_encoder() {
   static EncodeTiled encode = nullptr;
   if (!encode) {
     void *fn = nullptr;
@@ -382,6 +382,20 @@ EncodeTiled tensor_map_encoder() {
   }
   return encode;
 }
+// The driver's call wants a context on the calling thread, which the runtime's calls have no need of: a thread whose
+// first call this is gets its current device's.
+CUresult encode_tiled(CUtensorMap *map, CUtensorMapDataType type, cuuint32_t rank, void *base, const cuuint64_t *dims,
+                      const cuuint64_t *strides, const cuuint32_t *box, const cuuint32_t *steps,
+                      CUtensorMapInterleave interleave, CUtensorMapSwizzle swizzle, CUtensorMapL2promotion promotion,
+                      CUtensorMapFloatOOBfill fill) {
+  const EncodeTiled encode = driver_encoder();
+  CUresult r = encode(map, type, rank, base, dims, strides, box, steps, interleave, swizzle, promotion, fill);
+  int dev = 0;
+  if (r == CUDA_ERROR_INVALID_CONTEXT && cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess)
+    r = encode(map, type, rank, base, dims, strides, box, steps, interleave, swizzle, promotion, fill);
+  return r;
+}
+EncodeTiled tensor_map_encoder() { return driver_encoder() ? encode_tiled : nullptr; }
 }  // namespace
 
 DriverLaunch driver_launch() {
