@@ -19,7 +19,7 @@ namespace ham {
 namespace {
 
 constexpr int kMostExperts = 512, kMostTop = 32;
-constexpr int kChooseWarps = 8, kChooseBlocks = 4;  // warps of a block, blocks an SM
+constexpr int kChooseWarps = 4;  // warps (rows) of a block
 
 template <typename K>
 cudaError_t allow(K kernel, int bytes, bool (&done)[64], int dev) {
@@ -144,17 +144,25 @@ __device__ __noinline__ int choose_exactly(const RouteArgs &a, int row, double *
 // The choice: a warp a row
 // ------------------------------------------------------------------------------------
 // A lane has kPer neighbouring experts, in registers: scores, values and the groups' sums (a group that lies in whole
-// lanes takes two shuffles a doubling) need no shared memory.  Each lane sorts its own; then the warp's largest first one
-// is taken top_k times, a reduction, a ballot and a shift of the owner's each.  Deciding in fp32 and only where two values
-// are nearer than their errors in fp64, for those values alone, costs a few comparisons a row: with whole rows computed
-// again 16384 rows of 256 with sigmoid and bias took 48 us, so 24.
+// lanes takes two shuffles a doubling) need no shared memory.  Each lane brings its three largest to its front, in order;
+// then the warp's largest first one is taken top_k times, a reduction, a ballot and a shift of the owner's each, and a lane
+// that runs out brings up one more.  (16384 rows of 256 in 8 groups with one, two, three, four and all of them in order at first:
+// 38.6, 32.4, 31.9, 32.6 and 33.6 us a call, grouping and all; 8192 rows of 512: 31.7, 24.1, 24.1, 25.0, 31.5.)  Deciding in fp32
+// and only where two values are nearer than their errors in fp64, for those values alone, costs a few comparisons a row:
+// with whole rows computed again 16384 rows of 256 with sigmoid and bias took 48 us, so 24.
 //
-// Bound by instructions, some 1200 a row of 256 experts in 8 groups at 2.8 a clock: 26 us for 16384 rows (with softmax
-// alone 17), where reading the logits takes 2.5.  An eighth of it is the sorting, a fifth the taking, a tenth the weights,
-// the rest the logits and their scores.
+// A warp has one row: with blocks that stay and take rows in turn, 4 an SM of 8 warps, the last turn is a third full (16384 rows
+// of 256: 24.8 us a call, so 21.5; in groups 31.9 and 31.1).
 //
-// The warp's rows from lane's experts lane * kPer .. lane * kPer + kPer - 1 of each.
-template <int kPer>
+// Bound by instructions, some 1050 a row of 256 experts in 8 groups (580 with softmax alone): 23 us for 16384 rows by
+// themselves (14), where reading the logits takes 2.5.
+//
+// What is known of a call where its kernel is made: nothing; that the logits decide alone; sigmoid and a bias; these and groups
+// of 2^i whole lanes.  (Asked for in the kernel, the flags cost a tenth of the time: 27.3 instead of
+// 25.7 us a call for 16384 rows of 256 with sigmoid and a bias.)
+enum { kAnyChoice, kByLogits, kSigmoidBias, kSigmoidBiasGroups };
+// Lane's experts: lane * kPer .. lane * kPer + kPer - 1.
+template <int kPer, int kMode>
 struct Chooser {
   float bias[kPer];        // this lane's experts'
   int each, lanes, group;  // experts of a group; the lanes that hold one (0: it does not lie in 2^i whole lanes), this lane's
@@ -204,12 +212,14 @@ struct Chooser {
     z = 1.f;
     unsure = false;
     if (!(m > -INFINITY)) return -1;
-    const bool grouped = a.top_groups < a.groups;
+    constexpr bool kAll = kMode == kSigmoidBiasGroups, kBoth = kAll || kMode == kSigmoidBias;
+    const bool grouped = kAll || (kMode == kAnyChoice && a.top_groups < a.groups);
+    const bool has_bias = kBoth || (kMode == kAnyChoice && a.bias), sigmoid = kBoth || a.sigmoid;
     uint32_t k[kPer];                            // the experts' places in the order
     float tol = 0.f, group_tol = 0.f;
-    if (a.bias || grouped || !(a.renorm || a.sigmoid)) {   // (else the logits decide, and their quotients suffice)
+    if (kMode != kByLogits && (has_bias || grouped || !(a.renorm || sigmoid))) {  // (else the logits' quotients suffice)
       float v[kPer];
-      if (a.sigmoid) {
+      if (sigmoid) {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
           asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(v[i]) : "f"(1.f + expf(-l[i])));  // (0 where ruled out)
@@ -223,7 +233,7 @@ struct Chooser {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) v[i] *= back;
       }
-      if (a.bias || grouped) {
+      if (has_bias || grouped) {
         float smax = 0.f, cmax = 0.f;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
@@ -233,7 +243,7 @@ struct Chooser {
           else cmax = fmaxf(cmax, fabsf(v[i]));
         }
         smax = warp_max_f32(smax), cmax = warp_max_f32(cmax);
-        const float off = smax * (a.sigmoid ? 0x1p-21f : 0x1p-19f);
+        const float off = smax * (sigmoid ? 0x1p-21f : 0x1p-19f);
         tol = 2 * off + cmax * 0x1p-22f;
         group_tol = 4 * off + cmax * 0x1p-20f;
 #pragma unroll
@@ -246,7 +256,7 @@ struct Chooser {
           unsure = true;
           return -1;
         }
-        if (lanes) {
+        if (kAll || lanes) {
           if (!(stays >> group & 1u)) {
 #pragma unroll
             for (int i = 0; i < kPer; ++i) l[i] = v[i] = -INFINITY;
@@ -258,50 +268,51 @@ struct Chooser {
         }
       }
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) k[i] = rank_of(a.bias ? v[i] : l[i]);
+      for (int i = 0; i < kPer; ++i) k[i] = rank_of(has_bias ? v[i] : l[i]);
     } else {
 #pragma unroll
       for (int i = 0; i < kPer; ++i) k[i] = rank_of(l[i]);
     }
-    // Each lane's experts in order (neighbours change places, so that equal ones keep theirs), then the warp's largest
-    // first one, again and again.
-    uint64_t ids = 0;                            // four bits each
+    // Each lane's largest few in order at its front (passes from the back that change neighbours' places, so that equal ones
+    // keep theirs), then the warp's largest first one, again and again; a lane that has no more in order makes all pass once more.
+    constexpr int kFront = kPer < 3 ? kPer : 3;
     uint32_t id[kPer];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) id[i] = i;
+    const auto pass = [&](int from) {
 #pragma unroll
-    for (int r = 0; r < kPer; ++r)
+      for (int i = kPer - 2; i >= 0; --i)
+        if (i >= from) {
+          const bool swap = k[i] < k[i + 1];
+          const uint32_t x = k[i], y = id[i];
+          k[i] = max(x, k[i + 1]), k[i + 1] = min(x, k[i + 1]);
+          id[i] = swap ? id[i + 1] : y, id[i + 1] = swap ? y : id[i + 1];
+        }
+    };
 #pragma unroll
-      for (int i = r & 1; i + 1 < kPer; i += 2) {
-        const bool swap = k[i] < k[i + 1];
-        const uint32_t x = k[i], y = id[i];
-        k[i] = max(x, k[i + 1]), k[i + 1] = min(x, k[i + 1]);
-        id[i] = swap ? id[i + 1] : y, id[i + 1] = swap ? y : id[i + 1];
-      }
-    uint32_t low = 0, high = 0;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      if (i < 8) low |= id[i] << 4 * i;
-      else high |= id[i] << 4 * (i - 8);
-    }
-    ids = (uint64_t)high << 32 | low;
+    for (int i = 0; i < kFront; ++i) pass(i);
+    int front = kFront;                          // in order
     int mine = -1;                               // lane j: the j-th; with a bias the one after the last too
     uint32_t rank = kNoRank;
-    const int rounds = min(a.top_k + (a.bias ? 1 : 0), 32);
+    const int rounds = min(a.top_k + (has_bias ? 1 : 0), 32);
     for (int j = 0; j < rounds; ++j) {
       const uint32_t top = __reduce_max_sync(kFull, k[0]);
       if (top == kNoRank) break;
       const int owner = __ffs(__ballot_sync(kFull, k[0] == top)) - 1;
-      const int e = owner * kPer + (int)(__shfl_sync(kFull, (uint32_t)ids, owner) & 15u);
+      const int e = owner * kPer + (int)__shfl_sync(kFull, id[0], owner);
       if (lane == j) mine = e, rank = top;
       if (lane == owner) {
 #pragma unroll
-        for (int i = 0; i + 1 < kPer; ++i) k[i] = k[i + 1];
-        k[kPer - 1] = kNoRank;
-        ids >>= 4;
+        for (int i = 0; i + 1 < kFront; ++i) k[i] = k[i + 1], id[i] = id[i + 1];
+        k[kFront - 1] = kNoRank;
+        --front;
+      }
+      if (kPer > kFront && __any_sync(kFull, front == 0)) {
+        pass(0);
+        front = min(front + 1, kFront);
       }
     }
-    if (a.bias) {
+    if (has_bias) {
       uint32_t next = __shfl_down_sync(kFull, rank, 1);
       int e = __shfl_down_sync(kFull, mine, 1);
       if (a.top_k == 32) {                       // (a lane for each: the one after the last is still to come)
@@ -317,7 +328,7 @@ struct Chooser {
           // order by their exact values.
           const uint32_t follows = __reduce_max_sync(kFull, k[0]);
           const bool apart = follows == kNoRank || value_of(__shfl_sync(kFull, rank, rounds - 1)) - value_of(follows) > tol;
-          if (!a.sigmoid || rounds > 31 || !apart) {
+          if (!sigmoid || rounds > 31 || !apart) {
             unsure = true;
           } else {
             double exact = -INFINITY;
@@ -348,7 +359,7 @@ struct Chooser {
     const int lane = threadIdx.x & 31;
     float first = -INFINITY, second = -INFINITY;
     int g = group, step = lanes;                 // the group that this lane works at, the lanes that do
-    if (lanes) {
+    if (kMode == kSigmoidBiasGroups || lanes) {
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
         second = fmaxf(second, fminf(first, v[i]));
@@ -386,7 +397,7 @@ struct Chooser {
     const uint32_t most = __reduce_max_sync(kFull, live && !kept ? rank_of(sum) : kNoRank);
     stays = __reduce_or_sync(kFull, kept ? 1u << g : 0u);
     if (most == kNoRank || value_of(least) - value_of(most) > tol) return true;
-    if (!a.sigmoid || !lanes) return false;
+    if (kMode != kSigmoidBiasGroups && (!a.sigmoid || !lanes)) return false;
     // Exactly, a sigmoid's value being its own logit's alone: the values that may be a group's two largest, one a lane at a
     // time.
     uint32_t wanted = 0;
@@ -421,48 +432,47 @@ struct Chooser {
   }
 };
 
-// Rows by a warp: first, first + step, ..
-template <int kPer>
-__device__ __forceinline__ void choose_rows(const RouteArgs &a, int first, int step, double *shared) {
+// A row by a warp.
+template <int kPer, int kMode>
+__device__ __forceinline__ void choose_row(const RouteArgs &a, int row, double *shared) {
   const int lane = threadIdx.x & 31;
-  const Chooser<kPer> chooser(a);
-  for (int row = first; row < a.rows; row += step) {
-    float peak, z;
-    bool unsure;
-    int mine = chooser.choose(a, row, reinterpret_cast<float *>(shared), peak, z, unsure);
-    if (unsure) {
-      __syncwarp();
-      mine = choose_exactly(a, row, shared);
-    }
-    // the weights, from the chosen experts' logits alone: lane j has the j-th
-    float s = 0.f;
-    const float l = mine >= 0 ? read_logit(a, (int64_t)row * a.experts + mine) : -INFINITY;
-    if (a.sigmoid) {
-      if (mine >= 0) s = 1.f / (1.f + expf(-l));
-    } else {
-      const float top = a.renorm ? warp_max_f32(l) : peak;  // (a quotient: any common factor will do)
-      if (mine >= 0) s = exp_difference(l, top);
-      if (!a.renorm) s /= z;
-    }
-    if (a.renorm) {
-      const float sum = warp_sum(s);
-      if (mine >= 0) s /= sum;
-    }
-    if (lane < a.top_k) {
-      const int64_t to = (int64_t)row * a.top_k + lane;
-      a.expert[to] = mine;
-      a.weight[to] = s * a.scale;
-    }
+  const Chooser<kPer, kMode> chooser(a);
+  float peak, z;
+  bool unsure;
+  int mine = chooser.choose(a, row, reinterpret_cast<float *>(shared), peak, z, unsure);
+  if (unsure) {
+    __syncwarp();
+    mine = choose_exactly(a, row, shared);
+  }
+  // the weights, from the chosen experts' logits alone: lane j has the j-th
+  float s = 0.f;
+  const float l = mine >= 0 ? read_logit(a, (int64_t)row * a.experts + mine) : -INFINITY;
+  if (a.sigmoid) {
+    if (mine >= 0) s = 1.f / (1.f + expf(-l));
+  } else {
+    const float top = a.renorm ? warp_max_f32(l) : peak;  // (a quotient: any common factor will do)
+    if (mine >= 0) s = exp_difference(l, top);
+    if (!a.renorm) s /= z;
+  }
+  if (a.renorm) {
+    const float sum = warp_sum(s);
+    if (mine >= 0) s /= sum;
+  }
+  if (lane < a.top_k) {
+    const int64_t to = (int64_t)row * a.top_k + lane;
+    a.expert[to] = mine;
+    a.weight[to] = s * a.scale;
   }
 }
 
-template <int kPer>
+template <int kPer, int kMode>
 __global__ void __launch_bounds__(kChooseWarps * 32) choose_kernel(const __grid_constant__ RouteArgs a) {
   __shared__ double shared[kChooseWarps][kPer * 32];
   const int warp = threadIdx.x >> 5;
   grid_dependency_wait();
   grid_launch_dependents();
-  choose_rows<kPer>(a, blockIdx.x * kChooseWarps + warp, gridDim.x * kChooseWarps, shared[warp]);
+  const int64_t row = (int64_t)blockIdx.x * kChooseWarps + warp;
+  if (row < a.rows) choose_row<kPer, kMode>(a, (int)row, shared[warp]);
 }
 
 // ------------------------------------------------------------------------------------
@@ -482,9 +492,17 @@ __host__ __device__ constexpr int group_pitch(int experts) { return experts | 1;
 __host__ __device__ constexpr int group_smem(int experts, bool staged) {
   return 2 * kGroupWarps * group_pitch(experts) * 4 + (staged ? kStaged * 4 : 0);
 }
+// (Rows of a warp.)
+__host__ __device__ constexpr int group_stretch(int rows, int ctas) {
+  return ((rows + ctas * kGroupWarps - 1) / (ctas * kGroupWarps) + 31) & ~31;
+}
 static_assert(group_smem(kMostExperts, true) <= 220 * 1024, "shared memory");
 
+// kOnce: the stretch is 32 rows, whose bits the first walk finds and counts for both.  (16384 rows of 8 of 64: 15.3 us a call
+// otherwise, so 14.6; 1333 rows of 4 of 60 8.8 and 8.0.  Asked for in the kernel, 65536 rows of 2 of 64 took 30.8 instead of 28.7.)
+//
 // (Every thread of a block of kGroupThreads, of every block of the cluster; hist: [2][warps][pitch], and the staged pairs.)
+template <bool kOnce>
 __device__ __forceinline__ void group_pairs(const RouteArgs &a, int32_t *hist, bool staged) {
   __shared__ int32_t count[kMostExperts], first[kMostExperts], local[kMostExperts], part[2][kGroupWarps];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, E = a.experts, K = a.top_k, pitch = group_pitch(E);
@@ -492,18 +510,33 @@ __device__ __forceinline__ void group_pairs(const RouteArgs &a, int32_t *hist, b
   int32_t *mine = hist + warp * pitch;
   uint32_t *rows_of = reinterpret_cast<uint32_t *>(hist + (kGroupWarps + warp) * pitch);
   uint32_t *stage = reinterpret_cast<uint32_t *>(hist + 2 * kGroupWarps * pitch);
-  const int stretch = ((a.rows + ctas * kGroupWarps - 1) / (ctas * kGroupWarps) + 31) & ~31;  // rows of a warp
+  const int stretch = kOnce ? 32 : group_stretch(a.rows, ctas);
   const int64_t row0 = (int64_t)rank * kGroupWarps * stretch;                                // the CTA's first
   const int64_t from = row0 + (int64_t)warp * stretch, to = min((int64_t)a.rows, from + stretch);
-  for (int e = lane; e < E; e += 32) mine[e] = 0, rows_of[e] = 0;
-  __syncwarp();
-  for (int64_t i0 = from * K; i0 < to * K; i0 += 8 * 32) {
-    int e[8];
+  const uint32_t one_kth = 65536 / K + 1;        // x / K = x one_kth / 65536 for x < 1024
+  int e[8];                                      // experts of 8 x 32 pairs
+  const auto read = [&](int64_t p0, int i0, int pairs) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) e[i] = i0 + 32 * i + lane < to * K ? a.expert[i0 + 32 * i + lane] : -1;
+    for (int i = 0; i < 8; ++i) e[i] = i0 + 32 * i + lane < pairs ? a.expert[p0 + i0 + 32 * i + lane] : -1;
+  };
+  const auto mark = [&](int i0) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (e[i] >= 0) atomicAdd(&mine[e[i]], 1);    // (of whole numbers: any order)
+      if (e[i] >= 0) atomicOr(&rows_of[e[i]], 1u << ((i0 + 32 * i + lane) * one_kth >> 16));
+  };
+  for (int x = lane; x < E; x += 32) mine[x] = 0, rows_of[x] = 0;
+  __syncwarp();
+  const int64_t first_pair = from * K;
+  const int most = to > from ? (int)min((int64_t)stretch, to - from) * K : 0;
+  for (int i0 = 0; i0 < most; i0 += 8 * 32) {
+    read(first_pair, i0, most);
+    if (kOnce) {
+      mark(i0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (e[i] >= 0) atomicAdd(&mine[e[i]], 1);    // (of whole numbers: any order)
+    }
   }
   __syncthreads();
   for (int x = tid >> 2; x < (E + 7) / 8 * 8; x += kGroupThreads / 4) {
@@ -512,7 +545,7 @@ __device__ __forceinline__ void group_pairs(const RouteArgs &a, int32_t *hist, b
 #pragma unroll
     for (int i = 0; i < kGroupWarps / 4; ++i) {
       c[i] = run;
-      if (x < E) run += hist[(w0 + i) * pitch + x];
+      if (x < E) run += kOnce ? __popc((uint32_t)hist[(kGroupWarps + w0 + i) * pitch + x]) : hist[(w0 + i) * pitch + x];
     }
     int upto = run;
 #pragma unroll
@@ -570,24 +603,18 @@ __device__ __forceinline__ void group_pairs(const RouteArgs &a, int32_t *hist, b
     }
   }
   __syncthreads();
-  const uint32_t one_kth = 65536 / K + 1;          // x / K = x one_kth / 65536 for x < 1024
-  for (int64_t r0 = from; r0 < to; r0 += 32) {     // 32 rows: 32 K pairs, 8 x 32 at a time
+  for (int64_t r0 = from; r0 < to; r0 += 32) {
     const int64_t p0 = r0 * K;
     const int pairs = (int)min((int64_t)32, to - r0) * K;
-    int e[8];
-    const auto read = [&](int i0) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) e[i] = i0 + 32 * i + lane < pairs ? a.expert[p0 + i0 + 32 * i + lane] : -1;
-    };
-    for (int i0 = 0; i0 < pairs; i0 += 8 * 32) {
-      read(i0);
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (e[i] >= 0) atomicOr(&rows_of[e[i]], 1u << ((i0 + 32 * i + lane) * one_kth >> 16));
+    if (!kOnce) {
+      for (int i0 = 0; i0 < pairs; i0 += 8 * 32) {
+        read(p0, i0, pairs);
+        mark(i0);
+      }
+      __syncwarp();
     }
-    __syncwarp();
     for (int i0 = 0; i0 < pairs; i0 += 8 * 32) {
-      if (pairs > 8 * 32) read(i0);
+      if (pairs > 8 * 32) read(p0, i0, pairs);
       int at[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -603,6 +630,7 @@ __device__ __forceinline__ void group_pairs(const RouteArgs &a, int32_t *hist, b
       for (int i = 0; i < 8; ++i)
         if (i0 + 32 * i + lane < pairs) a.place[p0 + i0 + 32 * i + lane] = at[i];
     }
+    if (kOnce) break;
     __syncwarp();
     for (int x = lane; x < E; x += 32) {
       mine[x] += __popc(rows_of[x]);
@@ -622,25 +650,27 @@ __device__ __forceinline__ void group_pairs(const RouteArgs &a, int32_t *hist, b
   for (int64_t i = total + rank * kGroupThreads + tid; i < n; i += ctas * kGroupThreads) a.order[i] = -1;
 }
 
+template <bool kOnce>
 __global__ void __launch_bounds__(kGroupThreads) group_kernel(const __grid_constant__ RouteArgs a, int staged) {
   extern __shared__ int32_t hist[];
   grid_dependency_wait();
   grid_launch_dependents();
-  group_pairs(a, hist, staged != 0);
+  group_pairs<kOnce>(a, hist, staged != 0);
 }
 
 // A few rows: the choice and the grouping by one block.  (us with one launch / with two, 64 experts: 8 rows 5.4 / 6.2, 16 rows
 // 5.7 / 5.9, 32 rows 6.6 / 6.1; 256 experts: 6.3 / 7.0 for 8 rows, 8.7 / 7.0 for 32.)
 constexpr int kFewRows = 16;
+static_assert(kFewRows <= kGroupWarps, "a warp has one row");
 template <int kPer>
 __global__ void __launch_bounds__(kGroupThreads) route_few_kernel(const __grid_constant__ RouteArgs a) {
   extern __shared__ int32_t hist[];              // the grouping's, before that [warps][values]
   grid_dependency_wait();
   grid_launch_dependents();
   const int warp = threadIdx.x >> 5;
-  choose_rows<kPer>(a, warp, kGroupWarps, reinterpret_cast<double *>(hist) + warp * (kPer * 32));
+  if (warp < a.rows) choose_row<kPer, kAnyChoice>(a, warp, reinterpret_cast<double *>(hist) + warp * (kPer * 32));
   __syncthreads();
-  group_pairs(a, hist, false);
+  group_pairs<true>(a, hist, false);
 }
 
 // ------------------------------------------------------------------------------------
@@ -740,9 +770,12 @@ int group_ctas(int dev) {
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  int n = 0;
-  const bool fits = cudaFuncSetAttribute(group_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
-                    cudaOccupancyMaxActiveClusters(&n, group_kernel, &cfg) == cudaSuccess && n > 0;
+  const auto fit = [&](auto kernel) {
+    int n = 0;
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+           cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess && n > 0;
+  };
+  const bool fits = fit(group_kernel<true>) && fit(group_kernel<false>);
   if (!fits) cudaGetLastError();
   const int ctas = fits ? kGroupCtas : 8;
   if (dev >= 0 && dev < 64) known[dev] = ctas;
@@ -752,7 +785,7 @@ int group_ctas(int dev) {
 // Launches of Kernel<kPer> for the experts' number.
 template <int kPer>
 cudaError_t launch_route(const RouteArgs &a, cudaStream_t s) {
-  static bool few_done[64] = {}, done[64] = {};
+  static bool few_done[64] = {}, once_done[64] = {}, done[64] = {};
   int dev = 0;
   cudaGetDevice(&dev);
   if (a.rows <= kFewRows) {
@@ -760,18 +793,27 @@ cudaError_t launch_route(const RouteArgs &a, cudaStream_t s) {
     const cudaError_t e = allow(route_few_kernel<kPer>, kMost, few_done, dev);
     return e != cudaSuccess ? e : launch_after<route_few_kernel<kPer>>(dim3(1), dim3(kGroupThreads), (size_t)kMost, dim3(1), s, a);
   }
-  const int blocks = std::min((a.rows + kChooseWarps - 1) / kChooseWarps, device_sms() * kChooseBlocks);
-  cudaError_t e = launch_after<choose_kernel<kPer>>(dim3((unsigned)blocks), dim3(kChooseWarps * 32), 0, dim3(1), s, a);
-  if (e == cudaSuccess) e = allow(group_kernel, group_smem(kMostExperts, true), done, dev);
+  const dim3 grid((unsigned)(((int64_t)a.rows + kChooseWarps - 1) / kChooseWarps)), block(kChooseWarps * 32);
+  const int each = a.experts / a.groups, lanes = each / kPer;
+  const bool grouped = a.top_groups < a.groups;
+  cudaError_t e = !a.bias && !grouped && (a.renorm || a.sigmoid) ? launch_after<choose_kernel<kPer, kByLogits>>(grid, block, 0, dim3(1), s, a)
+                  : a.sigmoid && a.bias && !grouped ? launch_after<choose_kernel<kPer, kSigmoidBias>>(grid, block, 0, dim3(1), s, a)
+                  : a.sigmoid && a.bias && each % kPer == 0 && (lanes & (lanes - 1)) == 0
+                      ? launch_after<choose_kernel<kPer, kSigmoidBiasGroups>>(grid, block, 0, dim3(1), s, a)
+                      : launch_after<choose_kernel<kPer, kAnyChoice>>(grid, block, 0, dim3(1), s, a);
+  if (e == cudaSuccess) e = allow(group_kernel<true>, group_smem(kMostExperts, true), once_done, dev);
+  if (e == cudaSuccess) e = allow(group_kernel<false>, group_smem(kMostExperts, true), done, dev);
   if (e != cudaSuccess) return e;
   // (The whole call with one block / a cluster of eight, 64 experts, us: 512 rows 7.5 / 8.2, 1024 rows 9.1 / 9.9, 2048 rows
   // 13.1 / 10.5; 256 experts: 8.7 / 9.6, 10.7 / 11.7, 15.9 / 12.7.  With eight / with sixteen, 256 experts: 2048 rows 12.8 / 13.1,
   // 4096 rows 15.1 / 15.5, 16384 rows 30.8 / 26.4; 128 experts, 32768 rows 50.5 / 36.5.)
   const int ctas = a.rows <= 1024 ? 1 : a.rows <= 4096 ? 8 : group_ctas(dev);
-  const int stretch = ((a.rows + ctas * kGroupWarps - 1) / (ctas * kGroupWarps) + 31) & ~31;
-  const bool staged = (int64_t)stretch * kGroupWarps * a.top_k <= kStaged;
-  return launch_after<group_kernel>(dim3((unsigned)ctas), dim3(kGroupThreads), (size_t)group_smem(a.experts, staged),
-                                    dim3((unsigned)ctas), s, a, (int)staged);
+  const int stretch = group_stretch(a.rows, ctas);
+  const int staged = (int64_t)stretch * kGroupWarps * a.top_k <= kStaged;
+  const dim3 cluster((unsigned)ctas);
+  const size_t smem = (size_t)group_smem(a.experts, staged);
+  return stretch == 32 ? launch_after<group_kernel<true>>(cluster, dim3(kGroupThreads), smem, cluster, s, a, staged)
+                       : launch_after<group_kernel<false>>(cluster, dim3(kGroupThreads), smem, cluster, s, a, staged);
 }
 
 }  // namespace

@@ -110,6 +110,22 @@ def test_pairs_of_near_values(k):
     _run(l, k, sigmoid=True, bias=bias)
 
 
+@pytest.mark.parametrize("experts", [40, 64, 96, 128, 250, 256, 500, 512])
+@pytest.mark.parametrize("sigmoid,with_bias,groups", [(False, False, 1), (True, False, 1), (False, True, 1), (True, True, 1),
+                                                      (True, True, 2), (False, False, 2)])
+def test_chosen_experts_that_lie_together(experts, sigmoid, with_bias, groups):
+    """The largest logits in one run of neighbours, rising, falling, equal and in few steps: all of a lane's are taken."""
+    rng = np.random.default_rng(experts + groups)
+    l = -3 + 0.5 * rng.integers(-2, 2, (48, experts))
+    for t in range(len(l)):
+        n = int(rng.integers(1, 33))
+        at = int(rng.integers(0, experts - n + 1)) if t % 3 else (0 if t % 2 else experts - n)
+        l[t, at:at + n] = [np.arange(n) / 16, -np.arange(n) / 16, np.zeros(n), rng.integers(0, 4, n) / 4][t % 4]
+    bias = 0.125 * rng.integers(0, 2, experts) if with_bias else None
+    for k in (8, 31, 32):
+        _run(l, min(k, experts // groups), sigmoid=sigmoid, bias=bias, groups=groups, top_groups=1)
+
+
 def test_equal_logits_and_equal_values():
     _run(np.zeros((3, 40)), 6)
     _run(np.zeros((3, 40)), 6, sigmoid=True, bias=np.full(40, 0.25), groups=5, top_groups=2)
