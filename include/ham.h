@@ -553,8 +553,8 @@ int ham_fp8_linear(ham_fp8_weight *w, const void *x_codes, const void *x_scales,
 int ham_fp8_gated(ham_fp8_weight *w, const void *x_codes, const void *x_scales, int32_t rows, void *codes,
                   void *scales, void *stream);
 
-/* Read and clear the weight's device error word (a bounded wait of a product that ran out;
- * synchronizes `stream`).  Returns HAM_EDEVICE if it was set, with the code in *device_code. */
+/* Read and clear the weight's device error word (a bounded wait of a product that ran out, or what an
+ * experts' call found out of range, HAM_DEVERR_ROUTE; synchronizes `stream`).  Returns HAM_EDEVICE if it was set, with the code in *device_code. */
 int ham_fp8_weight_status(ham_fp8_weight *w, void *stream, int32_t *device_code);
 
 /* Limit, in nanoseconds, of the products' waits for scale words to be freed and, with few rows, for stages to

@@ -485,7 +485,7 @@ __global__ void __launch_bounds__(kChooseWarps * 32) choose_kernel(const __grid_
 // lanes of equal experts finding one another, 32 pairs at a time, 131072 pairs took 27 us.)
 //
 // A CTA that has no more than kStaged pairs puts them in their order in shared memory and writes each expert's one after
-// another (1024 rows of 8: 9.1 us a call against 10.7 with scattered words; 16384 rows, by eight CTAs, 30.6 against 33.1).
+// another (1024 rows of 8 of 64: 7.9 us a call against 9.4 with scattered words; 16384 rows of 256 20.1 against 22.1).
 constexpr int kGroupThreads = 1024, kGroupWarps = 32, kGroupCtas = 16, kStaged = 16384;
 // (Pitch of the histograms: odd, so that four lanes that add up eight warps each of one expert's meet no bank twice.)
 __host__ __device__ constexpr int group_pitch(int experts) { return experts | 1; }
@@ -658,8 +658,9 @@ __global__ void __launch_bounds__(kGroupThreads) group_kernel(const __grid_const
   group_pairs<kOnce>(a, hist, staged != 0);
 }
 
-// A few rows: the choice and the grouping by one block.  (us with one launch / with two, 64 experts: 8 rows 5.4 / 6.2, 16 rows
-// 5.7 / 5.9, 32 rows 6.6 / 6.1; 256 experts: 6.3 / 7.0 for 8 rows, 8.7 / 7.0 for 32.)
+// A few rows: the choice and the grouping by one block.  (us with one launch / with two, 64 experts: 8 rows 4.7 / 4.8, 16 rows
+// 5.1 / 5.0, 32 rows 5.9 / 5.2; 256 experts: 5.8 / 5.9 for 8 rows, 6.4 / 6.0 for 16, 7.8 / 6.2 for 32.  Up to 16 for the sake of
+// calls outside graphs, where a launch is two of the host's.)
 constexpr int kFewRows = 16;
 static_assert(kFewRows <= kGroupWarps, "a warp has one row");
 template <int kPer>
@@ -804,10 +805,10 @@ cudaError_t launch_route(const RouteArgs &a, cudaStream_t s) {
   if (e == cudaSuccess) e = allow(group_kernel<true>, group_smem(kMostExperts, true), once_done, dev);
   if (e == cudaSuccess) e = allow(group_kernel<false>, group_smem(kMostExperts, true), done, dev);
   if (e != cudaSuccess) return e;
-  // (The whole call with one block / a cluster of eight, 64 experts, us: 512 rows 7.5 / 8.2, 1024 rows 9.1 / 9.9, 2048 rows
-  // 13.1 / 10.5; 256 experts: 8.7 / 9.6, 10.7 / 11.7, 15.9 / 12.7.  With eight / with sixteen, 256 experts: 2048 rows 12.8 / 13.1,
-  // 4096 rows 15.1 / 15.5, 16384 rows 30.8 / 26.4; 128 experts, 32768 rows 50.5 / 36.5.)
-  const int ctas = a.rows <= 1024 ? 1 : a.rows <= 4096 ? 8 : group_ctas(dev);
+  // (The whole call with one block / a cluster of eight / of sixteen, us, 64 experts: 512 rows 6.3 / 7.1 / 7.2, 1024 rows
+  // 7.9 / 8.7 / 8.8, 2048 rows 12.7 / 9.0 / 9.1, 8192 rows 47 / 11.1 / 11.3, 16384 rows 88 / 19.1 / 14.6; 256 experts: 7.6 / 8.5 /
+  // 8.8, 9.5 / 10.5 / 10.8, 15.5 / 11.2 / 11.5, 59 / 15.4 / 15.9, 110 / 25.4 / 20.1.)
+  const int ctas = a.rows <= 1024 ? 1 : a.rows <= 8192 ? 8 : group_ctas(dev);
   const int stretch = group_stretch(a.rows, ctas);
   const int staged = (int64_t)stretch * kGroupWarps * a.top_k <= kStaged;
   const dim3 cluster((unsigned)ctas);
