@@ -346,6 +346,18 @@ struct Chooser {
             const int chosen = __shfl_sync(kFull, mine, max(sorted, 0));
             mine = sorted >= 0 ? chosen : -1;
           }
+        } else if (__shfl_sync(kFull, near, a.top_k - 1)) {
+          // The one after the last is exactly the last's equal: what is still to come and near may be larger all the same.
+          const int last = __shfl_sync(kFull, mine, a.top_k - 1);
+          const float value = value_of(__shfl_sync(kFull, rank, a.top_k - 1)), b = a.bias[last], x = read_logit(a, base + last);
+          bool other = false;
+#pragma unroll
+          for (int i = 0; i < kPer; ++i)
+            if (k[i] > kNoRank && !(value - value_of(k[i]) > tol)) {
+              const int e = lane * kPer + (int)id[i];
+              other |= a.bias[e] != b || read_logit(a, base + e) != x;
+            }
+          unsure = __any_sync(kFull, other);
         }
       }
       if (lane >= a.top_k) mine = -1;

@@ -110,6 +110,25 @@ def test_pairs_of_near_values(k):
     _run(l, k, sigmoid=True, bias=bias)
 
 
+@pytest.mark.parametrize("experts", [40, 64, 250, 345, 512])
+@pytest.mark.parametrize("sigmoid,groups", [(True, 1), (False, 1), (True, 2)])
+@pytest.mark.parametrize("k", [1, 2, 7, 20])
+def test_a_larger_value_behind_equal_ones(experts, sigmoid, groups, k):
+    """Many equal logits and, anywhere among them, one that is a unit larger: fp32 may give its value a place after all of
+    theirs, or the same."""
+    if experts % groups:
+        groups = 3
+    rng = np.random.default_rng(experts + k)
+    l = np.empty((64, experts), np.float32)
+    for t in range(len(l)):
+        x = np.float32(rng.uniform(-2, 2))
+        l[t] = x - 3
+        some = rng.permutation(experts)[:int(rng.integers(k + 1, min(experts, k + 20)))]
+        l[t, some] = x
+        l[t, some[0]] = np.nextafter(x, np.float32(9))
+    _run(l, min(k, experts // groups), sigmoid=sigmoid, bias=np.full(experts, 0.25), groups=groups, top_groups=1)
+
+
 @pytest.mark.parametrize("experts", [40, 64, 96, 128, 250, 256, 500, 512])
 @pytest.mark.parametrize("sigmoid,with_bias,groups", [(False, False, 1), (True, False, 1), (False, True, 1), (True, True, 1),
                                                       (True, True, 2), (False, False, 2)])
