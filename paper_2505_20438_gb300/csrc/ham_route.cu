@@ -398,17 +398,20 @@ struct Chooser {
       second = fmaxf(fminf(first, x), fmaxf(second, y));
       first = fmaxf(first, x);
     }
-    const float sum = second > -INFINITY ? first + second : first;   // (-inf: no expert is left)
+    // (Whether a group has an expert left is asked of its largest value: a sum of two finite ones may be infinite.)
+    const bool live = g < a.groups && first > -INFINITY;
+    const float sum = second > -INFINITY ? first + second : first;
+    const bool passes = __any_sync(kFull, live && fabsf(sum) == INFINITY);   // fp32's range: the exact sums decide
     int before = 0;                              // groups that come before this one
     for (int i = 0; i < a.groups; ++i) {
       const float other = __shfl_sync(kFull, sum, i * step);
       before += other > sum || (other == sum && i < g);
     }
-    const bool live = g < a.groups && sum > -INFINITY, kept = live && before < a.top_groups;
+    const bool kept = live && before < a.top_groups;
     const uint32_t least = __reduce_min_sync(kFull, kept ? rank_of(sum) : kFull);
     const uint32_t most = __reduce_max_sync(kFull, live && !kept ? rank_of(sum) : kNoRank);
     stays = __reduce_or_sync(kFull, kept ? 1u << g : 0u);
-    if (most == kNoRank || value_of(least) - value_of(most) > tol) return true;
+    if (!passes && (most == kNoRank || value_of(least) - value_of(most) > tol)) return true;
     if (kMode != kSigmoidBiasGroups && (!a.sigmoid || !lanes)) return false;
     // Exactly, a sigmoid's value being its own logit's alone: the values that may be a group's two largest, one a lane at a
     // time.
