@@ -675,7 +675,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const uint32_t bits = __float_as_uint(m[i]);
-            b[i] = bits > 0x7f800000u ? 0u : (bits >> 16) | (bits != 0u);
+            // (infinity's key is infinity: with the bit that keeps small numbers from being none it would be NaN)
+            b[i] = bits > 0x7f800000u ? 0u : min((bits >> 16) | (bits != 0u), 0x7f80u);
           }
           const uint32_t b01 = b[0] | b[1] << 16, b23 = b[2] | b[3] << 16;
           uint16_t *mine = key + (side * 4 + quarter) * 128 + (lane & 12) * 8 + (lane & 16) + (lane & 3) * 4;
