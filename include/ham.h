@@ -640,7 +640,8 @@ int ham_fp8_experts_alloc(int32_t experts, int32_t n, int32_t k, const void *cod
 /* The first half of the experts' gated blocks.  Slot i of expert e takes row t = order[i] / top_k of the 8-bit rows X:
  *   G = X[t] W_gate,e^T, U = X[t] W_up,e^T (fp32),  H = G / (1 + exp(-G)) * U, encoded as an 8-bit row:
  * codes [rows * top_k][n], scales [rows * top_k][..], in slot order.  Rows outside offsets[0] .. offsets[experts] - 1 are
- * left as they were.  Sums as ham_fp8_linear's with parts of at most 2048 terms; a slot's result does not depend on the others.
+ * left as they were.  Sums as ham_fp8_linear's, in parts of at most 1536 terms: of random terms off by some 6e-8 (k 1024) to
+ * 1e-7 (k 8192) of the outputs' norm.  A slot's result does not depend on the others.
  * x_codes [rows][k], x_scales; rows at most 2^24, rows * top_k at most 2^26; offsets, order as ham_route gives them.
  * Offsets that decrease or leave 0..rows * top_k set the device error word (HAM_DEVERR_ROUTE) and the call writes
  * nothing; an order entry of a slot outside 0..rows * top_k - 1 sets it and counts as entry 0.

@@ -60,9 +60,12 @@ __global__ void lay_out_expert_scales_kernel(const uint8_t *__restrict__ scales,
 //
 // Each CTA copies its half tile's K block (16 KiB, one stretch) and half of the N rows (of a gated product by index, four
 // rows a copy, or sorted before) into its own shared memory alone.  Sums take parts of K as the products of one weight do
-// (ham_fp8.cu), kExpertPart blocks each, in two sums of 224 columns in turn, so that a whole tile's products (of two parts)
-// are on their way while the epilogue deals with the tile before; it adds them in registers.  Errors against 64-bit sums,
-// relative to the outputs' norm: 3.4e-8 at K 512, 1.1e-7 from 2048 on (a plain fp32 product 2.7e-8, 6.0e-8, 1.3e-7 at 8192).
+// (ham_fp8.cu), of equal size and at most kExpertPart blocks (or one more, for an even number), in two sums of 224 columns
+// in turn, so that two parts' products are on their way while the epilogue deals with the tile before; it adds them in
+// registers.  Errors against 64-bit sums, relative to the outputs' norm, of K 512, 1024, 1408, 2048, 4096, 8192: 3.4e-8,
+// 6.0e-8, 7.2e-8, 6.5e-8, 8.7e-8, 9.8e-8 (an fp32 product in the usual order 2.7e-8, 4.1e-8, 4.7e-8, 6.0e-8, 8.6e-8, 1.3e-7).
+// With parts of 16 blocks they were 1.1e-7 from K 2048 on, and 4096 rows' gated halves 3 to 5% faster (444 us against 457);
+// of 8, 6.5e-8, 7.2e-8 and 8.2e-8 at 2048, 4096 and 8192, and 507 us.
 //
 // A thread of the epilogue has one feature (a lane) and up to 128 slots (columns).  Plain outputs are neighbours across
 // a warp's lanes.  Of a gated product 16 lanes hold the gate and 16 the up projection of 16 features: half a warp reads
@@ -78,8 +81,7 @@ __global__ void lay_out_expert_scales_kernel(const uint8_t *__restrict__ scales,
 // epilogue the calls take 410 and 198, with half of the products 356 and 178, without the weights' copies 354 and 181.
 //
 // Measured and not taken: copies by index for many rows (1430 us gated: 84 clocks for four rows, whoever issues them from one
-// warp); three sums of 128 columns and tiles of 256 slots (520 us); parts of 1024 terms (553 us: the products then run only one
-// part ahead); deeper rings where tiles are narrow (no faster); the next tile's looking up moved ahead (2 to 8% slower);
+// warp); three sums of 128 columns and tiles of 256 slots (520 us); deeper rings where tiles are narrow (no faster); the next tile's looking up moved ahead (2 to 8% slower);
 // weights marked to leave the L2 first (478 against 453 us).
 struct ExpertArgs {
   const uint8_t *ws;       // the handle's scales
@@ -89,11 +91,11 @@ struct ExpertArgs {
   void *out;
   uint8_t *out_scales;     // gated
   int32_t *err;
-  int experts, slots, top_k, n, kbs, sk, out_sk, tiles, f32;
+  int experts, slots, top_k, n, kbs, part, sk, out_sk, tiles, f32;   // part: K blocks of one accumulator, even
   uint64_t wait_ns;
 };
 
-constexpr int kExpertPart = 16;         // K blocks of one accumulator
+constexpr int kExpertPart = 11;         // K blocks of one accumulator, or one more
 constexpr int kExpertStages = 6;
 constexpr int kExpertStageBytes = 2 * kBlockBytes;  // the weights' block, 64 + 64 rows
 constexpr int kExpertSf = 4;            // scale slots (of four K blocks each)
@@ -409,7 +411,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           const uint32_t alone = halves == 1 && (singles++ & 1);  // the second group's turn
           const uint32_t idesc_half[2] = {idesc_mx(256, t.n0, 0), idesc_mx(256, t.n1, 0)};
           for (int g = 0, in = 0; g < a.kbs; g += kGroup) {  // in: blocks of this part so far
-            const bool two = g + 1 < a.kbs, ends = g + kGroup >= a.kbs || in + kGroup >= kExpertPart;
+            const bool two = g + 1 < a.kbs, ends = g + kGroup >= a.kbs || in + kGroup >= a.part;
             const int s1 = s + 1 == kExpertStages ? 0 : s + 1;
             if ((g & 3) == 0) {
               ok = ok && thread_wait_cluster(&sf_full[slot], word_phase, abort_flag);
@@ -522,7 +524,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     // Four warps take the first half's sums, four the second's; tiles of one half in turn.
     const int quarter = warp & 3, group = (warp - 4) >> 2;
     const uint32_t free_bar = cluster_map_shared(smem_u32(sum_free), 0);
-    const int parts = (a.kbs + kExpertPart - 1) / kExpertPart;
+    const int parts = (a.kbs + a.part - 1) / a.part;
     uint32_t first = 0, singles = 0;             // parts, tiles of one half so far
     uint32_t got = 0, taken = 0;                 // parts, tiles that this group took
     for (int64_t w = cluster; w < total; w += clusters) {
@@ -834,6 +836,8 @@ int run_experts(ham_fp8_weight *w, const void *x_codes, int32_t rows, ExpertArgs
   a.experts = w->experts;
   a.n = w->n;
   a.kbs = w->kbs;
+  const int parts = (w->kbs + kExpertPart - 1) / kExpertPart;   // of equal size
+  a.part = ((w->kbs + parts - 1) / parts + kGroup - 1) / kGroup * kGroup;
   a.sk = w->sk;
   a.out_sk = fp8_scale_bytes(w->n);
   a.tiles = w->tiles;
