@@ -623,7 +623,8 @@ enum { HAM_SCORE_SOFTMAX = 0, HAM_SCORE_SIGMOID = 1 };
  * offsets device int32 [experts + 1]: offsets[0] = 0, offsets[experts] the number of slots
  * order   device int32 [rows * top_k]: the slots' pairs, row * top_k + place; -1 from offsets[experts] on
  * place   device int32 [rows][top_k]: the pairs' slots; -1 where there is no expert
- * Pointers 4-byte aligned (bf16 logits: 2).  Outputs must not overlap inputs or each other.  One launch, or two.
+ * Pointers 4-byte aligned (bf16 logits: 2).  Outputs must not overlap inputs or each other.  One launch, or two; with
+ * rows == 0 none, and where offsets is given zeros are written to it (no slots).
  * Host errors: HAM_EINVAL, HAM_ECUDA. */
 int ham_route(const void *logits, int32_t logits_dtype, const float *bias, int32_t rows, int32_t experts,
               int32_t top_k, int32_t score, int32_t groups, int32_t top_groups, int32_t renorm, float scale,

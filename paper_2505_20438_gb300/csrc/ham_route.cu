@@ -858,7 +858,15 @@ int ham_route(const void *logits, int32_t logits_dtype, const float *bias, int32
   if (top_k < 1 || top_k > ham::kMostTop || top_k > most)
     return op_fail(HAM_EINVAL, "top_k %d outside 1..%d", top_k, most < ham::kMostTop ? most : ham::kMostTop);
   if (!(scale > -INFINITY && scale < INFINITY)) return op_fail(HAM_EINVAL, "scale must be finite");
-  if (rows == 0) return HAM_OK;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (rows == 0) {                               // no slots: what a call before left there is no grouping of this batch
+    const size_t bytes = 4 * ((size_t)experts + 1);
+    if (!offsets) return HAM_OK;
+    if (!op_aligned(offsets, 4)) return op_fail(HAM_EINVAL, "pointers must be 4-byte aligned");
+    if (op_overlap(offsets, bytes, bias, 4 * (size_t)experts)) return op_fail(HAM_EINVAL, "an output overlaps an input");
+    const cudaError_t ce = cudaMemsetAsync(offsets, 0, bytes, s);
+    return ce == cudaSuccess ? HAM_OK : op_fail(HAM_ECUDA, "route: %s", cudaGetErrorString(ce));
+  }
   if (!logits || !expert || !weight || !offsets || !order || !place)
     return op_fail(HAM_EINVAL, "logits and the five outputs are required");
   const int f32 = logits_dtype == HAM_DTYPE_F32;
@@ -895,7 +903,6 @@ int ham_route(const void *logits, int32_t logits_dtype, const float *bias, int32
   a.offsets = offsets;
   a.order = order;
   a.place = place;
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
   const cudaError_t ce = experts <= 32    ? ham::launch_route<1>(a, s)
                          : experts <= 64  ? ham::launch_route<2>(a, s)
                          : experts <= 128 ? ham::launch_route<4>(a, s)
