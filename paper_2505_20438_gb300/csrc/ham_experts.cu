@@ -789,10 +789,12 @@ cudaError_t launch_experts(const RowMaps &tx, const CUtensorMap &tw, const Exper
 }
 
 // The device's pool for sorted rows: memory is ordered by the stream (a captured call's belongs to its graph) and goes to
-// no other stream before its own is known to be done with it.  Up to kKeepBytes stay with the pool.
+// no other stream before its own is known to be done with it.  Up to kKeepBytes stay with the pool, until the last gated
+// weights of the device are freed.
 constexpr uint64_t kKeepBytes = (uint64_t)1 << 30;
+std::atomic<cudaMemPool_t> pools[64];
+std::atomic<int> sorting_weights[64];            // by device
 cudaMemPool_t row_pool(int dev) {
-  static std::atomic<cudaMemPool_t> pools[64];
   if (dev < 0 || dev >= 64) return nullptr;
   cudaMemPool_t pool = pools[dev].load();
   if (pool) return pool;
@@ -885,6 +887,15 @@ int run_experts(ham_fp8_weight *w, const void *x_codes, int32_t rows, ExpertArgs
 }
 
 }  // namespace
+
+void experts_weight_freed(int dev) {
+  if (dev < 0 || dev >= 64 || --sorting_weights[dev] != 0) return;
+  const cudaMemPool_t pool = pools[dev].load();
+  if (!pool) return;
+  // (memory whose use has not ended would stay with the pool)
+  if (cudaDeviceSynchronize() != cudaSuccess || cudaMemPoolTrimTo(pool, 0) != cudaSuccess) cudaGetLastError();
+}
+
 }  // namespace ham
 
 using ham::op_aligned;
@@ -955,7 +966,11 @@ int ham_fp8_experts_alloc(int32_t experts, int32_t n, int32_t k, const void *cod
     ham_fp8_weight_free(w);
     return op_fail(HAM_ECUDA, "weight layout: %s", cudaGetErrorString(e));
   }
-  if (codes_up) ham::row_pool(w->device);        // (not first in a call, which may be captured)
+  if (codes_up && w->device >= 0 && w->device < 64) {
+    ham::row_pool(w->device);                    // (not first in a call, which may be captured)
+    ++ham::sorting_weights[w->device];
+    w->sorts = true;
+  }
   *out = w;
   return HAM_OK;
 }

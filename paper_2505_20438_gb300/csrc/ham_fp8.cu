@@ -1020,6 +1020,7 @@ int ham_fp8_weight_free(ham_fp8_weight *w) {
   cudaGetDevice(&dev);
   cudaSetDevice(w->device);
   cudaFree(w->codes);
+  if (w->sorts) ham::experts_weight_freed(w->device);
   cudaSetDevice(dev);
   delete w;
   return HAM_OK;

@@ -12,6 +12,7 @@
 struct ham_fp8_weight {
   int32_t n = 0, k = 0, parts = 1;   // parts: 2 for a gated weight (gate, up)
   int32_t experts = 0;               // 0: one weight
+  bool sorts = false;                // its calls may take memory of the device's pool for sorted rows
   int32_t tiles = 0, kbs = 0, sk = 0;
   int device = 0;
   uint8_t *codes = nullptr;    // 128 x 128 swizzled blocks, and behind them in the same allocation
@@ -22,6 +23,9 @@ struct ham_fp8_weight {
 };
 
 namespace ham {
+// One weight that `sorts` less on a device: with the last one the pool's memory goes back.
+void experts_weight_freed(int dev);
+
 namespace {
 
 constexpr int kTile = 128;             // weight rows of a tile
