@@ -32,8 +32,6 @@ constexpr int kTile = 128;             // weight rows of a tile
 constexpr int kSumFirst = 16, kSumNext = 8, kSumMost = 32;  // K blocks of one accumulator
 constexpr int kBlockBytes = 128 * 128; // a tile's K block
 
-__device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.f + expf(-g)) * u; }
-
 // Shared memory that a CTA with `cols` columns of tensor memory asks for at least, in kernels whose CTAs
 // wait for one another: an SM's 228 KB then run out before its 512 columns do, so that no CTA of a
 // cluster ever waits for columns that a CTA of another cluster holds (two clusters could otherwise each
