@@ -70,6 +70,8 @@ struct ProductArgs {
   int f32;                 // fp32 output
 };
 
+constexpr int kSumFirst = 16, kSumNext = 8, kSumMost = 32;  // K blocks of one accumulator
+
 // u g / (1 + exp(-g)); from kFarGate down, where exp(-g) may leave fp32 and is all of the sum, u g exp(g).
 constexpr float kFarGate = -88.f;
 __device__ __forceinline__ float silu_mul(float g, float u) {
@@ -387,6 +389,8 @@ __global__ void __launch_bounds__(kStreamThreads)
 // tiles leave pairs without work in the last round, and the first tile's loads and the last one's epilogue
 // stand alone (2048 rows, 4096 x 4096: 27 us, 66%).  With one accumulator for all of K these took 119, 169,
 // 302 and 26.5 us; a pair takes 64 bytes a clock an SM from L2 at the products' full rate.
+constexpr int kFewRegs = 56, kManyRegs = 224;   // registers of the first four warps' threads, of the epilogue's
+static_assert(4 * kFewRegs + 8 * kManyRegs <= 12 * kLaunchRegs && kPairThreads == 384, "registers");
 constexpr int kPairStages = 6;
 constexpr int kPairStageBytes = 2 * kBlockBytes;
 constexpr int kPairSf = 4;

@@ -1,5 +1,6 @@
-// What the products with 8-bit weights share (ham_fp8.cu, ham_experts.cu): the handle and its layouts, the sums'
-// parts, the launches' helpers.
+// What the products with 8-bit weights share (ham_fp8.cu, ham_experts.cu): the handle, the weights' blocks, the pair
+// kernels' launches.  (Each has its own parts of K, and its own order of the same role's code: a mend in one pair kernel's
+// scale words, waits or end is to be looked for in the other's.)
 #pragma once
 
 #include <cuda.h>
@@ -29,7 +30,6 @@ void experts_weight_freed(int dev);
 namespace {
 
 constexpr int kTile = 128;             // weight rows of a tile
-constexpr int kSumFirst = 16, kSumNext = 8, kSumMost = 32;  // K blocks of one accumulator
 constexpr int kBlockBytes = 128 * 128; // a tile's K block
 
 // Shared memory that a CTA with `cols` columns of tensor memory asks for at least, in kernels whose CTAs
@@ -38,20 +38,11 @@ constexpr int kBlockBytes = 128 * 128; // a tile's K block
 // hold what the other waits for).
 constexpr int smem_floor(int cols) { return (228 * 1024 * (cols / 32) + 16) / 17; }
 
-// Registers a thread of the pair kernels: the launch's, and from the roles on those of the first four warps and of
-// the epilogue's eight, which hold a tile's sums in 128 of them.  Together they are what the launch has: a kernel
+// Registers a thread that the pair kernels are launched with.  From the roles on the first four warps' threads have fewer
+// and the epilogue's eight more, which hold a tile's sums in 128 of them; together they are what the launch has: a kernel
 // compiled to fewer would wait for the rest forever, so the host looks before it launches one.
 constexpr int kPairThreads = 384;       // warps: copies, products, 2 x scales, 8 x epilogue
-constexpr int kLaunchRegs = 168, kFewRegs = 56, kManyRegs = 224;
-static_assert(4 * kFewRegs + 8 * kManyRegs <= 12 * kLaunchRegs && kPairThreads == 384, "registers");
-
-template <typename K>
-cudaError_t allow_smem(K kernel, int bytes, bool (&done)[64], int dev) {
-  if (dev >= 0 && dev < 64 && done[dev]) return cudaSuccess;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e == cudaSuccess && dev >= 0 && dev < 64) done[dev] = true;
-  return e;
-}
+constexpr int kLaunchRegs = 168;
 
 // Pairs that are resident at once (a pair lies within one group of SMs, which need not hold a whole number
 // of them); a persistent grid is no larger.

@@ -46,6 +46,14 @@ inline bool op_overlap(const void *a, size_t na, const void *b, size_t nb) {
 }
 // SMs of the current device (cached per device).
 int device_sms();
+// Let `kernel` have `bytes` of dynamic shared memory, once a device.
+template <typename K>
+cudaError_t allow_smem(K kernel, int bytes, bool (&done)[64], int dev) {
+  if (dev >= 0 && dev < 64 && done[dev]) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && dev >= 0 && dev < 64) done[dev] = true;
+  return e;
+}
 
 // TMA map of a row-major [rows][cols] matrix of bytes (cols a multiple of 16) with a box of
 // {box_cols, box_rows}, with the 128-byte swizzle; boxes past the end read zeros.

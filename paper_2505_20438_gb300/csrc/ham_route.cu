@@ -21,14 +21,6 @@ namespace {
 constexpr int kMostExperts = 512, kMostTop = 32;
 constexpr int kChooseWarps = 4;  // warps (rows) of a block
 
-template <typename K>
-cudaError_t allow(K kernel, int bytes, bool (&done)[64], int dev) {
-  if (dev >= 0 && dev < 64 && done[dev]) return cudaSuccess;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e == cudaSuccess && dev >= 0 && dev < 64) done[dev] = true;
-  return e;
-}
-
 struct RouteArgs {
   const void *logits;      // [rows][experts] bf16 or f32
   const float *bias;       // nullable
@@ -806,7 +798,7 @@ cudaError_t launch_route(const RouteArgs &a, cudaStream_t s) {
   cudaGetDevice(&dev);
   if (a.rows <= kFewRows) {
     constexpr int kMost = std::max(kGroupWarps * kPer * 32 * 8, group_smem(kPer * 32, false));
-    const cudaError_t e = allow(route_few_kernel<kPer>, kMost, few_done, dev);
+    const cudaError_t e = allow_smem(route_few_kernel<kPer>, kMost, few_done, dev);
     return e != cudaSuccess ? e : launch_after<route_few_kernel<kPer>>(dim3(1), dim3(kGroupThreads), (size_t)kMost, dim3(1), s, a);
   }
   const dim3 grid((unsigned)(((int64_t)a.rows + kChooseWarps - 1) / kChooseWarps)), block(kChooseWarps * 32);
@@ -817,8 +809,8 @@ cudaError_t launch_route(const RouteArgs &a, cudaStream_t s) {
                   : a.sigmoid && a.bias && each % kPer == 0 && (lanes & (lanes - 1)) == 0
                       ? launch_after<choose_kernel<kPer, kSigmoidBiasGroups>>(grid, block, 0, dim3(1), s, a)
                       : launch_after<choose_kernel<kPer, kAnyChoice>>(grid, block, 0, dim3(1), s, a);
-  if (e == cudaSuccess) e = allow(group_kernel<true>, group_smem(kMostExperts, true), once_done, dev);
-  if (e == cudaSuccess) e = allow(group_kernel<false>, group_smem(kMostExperts, true), done, dev);
+  if (e == cudaSuccess) e = allow_smem(group_kernel<true>, group_smem(kMostExperts, true), once_done, dev);
+  if (e == cudaSuccess) e = allow_smem(group_kernel<false>, group_smem(kMostExperts, true), done, dev);
   if (e != cudaSuccess) return e;
   // (The whole call with one block / a cluster of eight / of sixteen, us, 64 experts: 512 rows 6.3 / 7.1 / 7.2, 1024 rows
   // 7.9 / 8.7 / 8.8, 2048 rows 12.7 / 9.0 / 9.1, 8192 rows 47 / 11.1 / 11.3, 16384 rows 88 / 19.1 / 14.6; 256 experts: 7.6 / 8.5 /
