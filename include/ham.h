@@ -614,8 +614,10 @@ enum { HAM_SCORE_SOFTMAX = 0, HAM_SCORE_SIGMOID = 1 };
  * The choice is that of exact scores: where values in fp32 lie too near to one another to tell, the row's are computed
  * again in fp64.  Weights are computed in fp32, off by at most 2^-18 of themselves, and where they or their scores
  * leave fp32's normal numbers by |scale| 2^-140 + 2^-149 more (a far expert's weight may be 0).
- * A logit of -inf or NaN, or a value v that is, rules its expert out; +inf counts as the largest finite number.  A
- * place that no expert is left for gets expert -1, weight 0 and no slot: a padding row is a row of -inf.
+ * A logit of -inf or NaN, or a value v that is, rules its expert out; +inf counts as the largest finite number.  (To mask
+ * an expert give it a logit or a bias of -inf: biases far beyond the scores, such as the lowest finite number, have every
+ * row computed in fp64, some twenty times as slow.)  A place that no expert is left for gets expert -1, weight 0 and no
+ * slot: a padding row is a row of -inf.
  * logits  device [rows][experts], bf16 or f32 (logits_dtype);  bias  nullable device f32 [experts]
  * experts 1..512;  top_k 1..32, at most experts / groups * top_groups;  groups 1..32, a divisor of experts;
  * top_groups 1..groups;  rows at most 2^24

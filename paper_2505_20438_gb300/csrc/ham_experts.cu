@@ -64,8 +64,10 @@ __global__ void lay_out_expert_scales_kernel(const uint8_t *__restrict__ scales,
 // in turn, so that two parts' products are on their way while the epilogue deals with the tile before; it adds them in
 // registers.  Errors against 64-bit sums, relative to the outputs' norm, of K 512, 1024, 1408, 2048, 4096, 8192: 3.4e-8,
 // 6.0e-8, 7.2e-8, 6.5e-8, 8.7e-8, 9.8e-8 (an fp32 product in the usual order 2.7e-8, 4.1e-8, 4.7e-8, 6.0e-8, 8.6e-8, 1.3e-7).
-// With parts of 16 blocks they were 1.1e-7 from K 2048 on, and 4096 rows' gated halves 3 to 5% faster (444 us against 457);
-// of 8, 6.5e-8, 7.2e-8 and 8.2e-8 at 2048, 4096 and 8192, and 507 us.
+// With parts of 16 blocks they were 1.1e-7 from K 2048 on; the more parts cost gated halves of 64, 128, 192 slots an expert
+// 0.4, 3 and 4% at K 4096, of 512 there 3%, at K 2048 (two parts instead of one) 1, 6 and 9% of 64, 128 and 512, plain
+// products 2% at most.  Parts of 8: 6.5e-8, 7.2e-8 and 8.2e-8 at 2048, 4096 and 8192, and 507 us for 4096 rows' gated halves
+// (parts of 11 457, of 16 444).
 //
 // A thread of the epilogue has one feature (a lane) and up to 128 slots (columns).  Plain outputs are neighbours across
 // a warp's lanes.  Of a gated product 16 lanes hold the gate and 16 the up projection of 16 features: half a warp reads
@@ -75,10 +77,12 @@ __global__ void lay_out_expert_scales_kernel(const uint8_t *__restrict__ scales,
 //
 // What bounds it.  Few rows: the weights' bytes.  8 rows of 8 of 64 experts (K 4096, 2048 features) take 119 us, 87% of the
 // copy rate with the sorting and the first and last tile's latencies, some 7 us, in it; the second products (K 2048, 4096
-// features) 59 us, 88%.  Many rows: the path from L2, and the card's power limit.  4096 rows of 8 of 64 experts take 446 to 470 us,
-// 25 of them the sorting, and 224 for the second products, 2.4 PFLOP/s.  A K block of the usual tile, 171 slots of 512, is 27 KB
-// a CTA in 0.33 us: 83 GB/s an SM, 12.6 TB/s in all, where the dense pair kernel's 32 KB come at 93 and feed 256 rows.  Without any
-// epilogue the calls take 410 and 198, with half of the products 356 and 178, without the weights' copies 354 and 181.
+// features) 59 us, 87%.  Many rows: no one thing.  4096 rows of 8 of 64 experts take 457 to 507 us, 25 of them the sorting, and
+// 226 to 231 for the second products, 2.4 PFLOP/s; a stream of such calls, which the card's power limit slows down, 540 and 265.
+// A K block of the usual tile, 171 slots of 512, is 27 KB a CTA in 0.33 us: 83 GB/s an SM, 12.6 TB/s in all, where the dense pair
+// kernel's 32 KB come at 93 and feed 256 rows.  Without any epilogue the calls took 410 and 198 (of 446 and 224, with parts of 16
+// blocks), with half of the products 356 and 178, without the weights' copies 354 and 181: each alone is an eighth to a fifth.
+// The gated epilogue's sums, results and maxima pass its 216 registers: 180 bytes a thread are spilled (the plain one's none).
 //
 // Measured and not taken: copies by index for many rows (1430 us gated: 84 clocks for four rows, whoever issues them from one
 // warp); three sums of 128 columns and tiles of 256 slots (520 us); deeper rings where tiles are narrow (no faster); the next tile's looking up moved ahead (2 to 8% slower);
@@ -850,8 +854,8 @@ int run_experts(ham_fp8_weight *w, const void *x_codes, int32_t rows, ExpertArgs
   // Rows by index, or sorted first?  A copy by index takes its thread some 80 clocks for four rows, a box of neighbouring
   // rows four a row, so that a K block costs some 35 ns more, from 16 slots an expert on 4.5 ns a slot; sorting takes 2.8 us
   // and the rows' bytes twice.  (us by index / sorted, K 4096, 2048 features of 32 experts, 4, 8, 16, 24, 32, 64, 128 slots
-  // an expert: 94.1 / 89.9, 96.1 / 91.6, 97.5 / 92.2, 103.8 / 92.6, 120.4 / 93.5, 157.6 / 96.8, 234.6 / 104.1; K 1024, 512
-  // features of 16, 16, 32, 64, 96 slots: 11.4 / 14.4, 12.5 / 15.1, 14.4 / 16.2, 16.2 / 17.1.)
+  // an expert in the mean: 88.3 / 84.6, 95.9 / 91.0, 100.5 / 92.7, 113.8 / 93.3, 122.6 / 93.6, 162.3 / 97.5, 237.5 / 111.4; K 1024, 512
+  // features of 16, 16, 32, 64, 96 slots: 11.8 / 14.9, 12.8 / 15.5, 16.0 / 17.0, 17.6 / 17.3.)
   const int64_t blocks = (int64_t)std::min(a.slots, a.experts) * a.tiles * a.kbs / (device_sms() / 2);  // a pair's
   const int64_t more_ns = blocks * std::max<int64_t>(35, (int64_t)a.slots * 9 / (2 * a.experts));
   if (a.gather && more_ns > 2800 + (int64_t)a.slots * w->k / 3400) {

@@ -139,19 +139,20 @@ __device__ __noinline__ int choose_exactly(const RouteArgs &a, int row, double *
 // lanes takes two shuffles a doubling) need no shared memory.  Each lane brings its three largest to its front, in order;
 // then the warp's largest first one is taken top_k times, a reduction, a ballot and a shift of the owner's each, and a lane
 // that runs out brings up one more.  (16384 rows of 256 in 8 groups with one, two, three, four and all of them in order at first:
-// 38.6, 32.4, 31.9, 32.6 and 33.6 us a call, grouping and all; 8192 rows of 512: 31.7, 24.1, 24.1, 25.0, 31.5.)  Deciding in fp32
+// 35.4, 29.8, 29.2, 29.8 and 30.7 us a call, grouping and all; 8192 rows of 512: 26.2, 20.1, 20.0, 20.7, 26.0.)  Deciding in fp32
 // and only where two values are nearer than their errors in fp64, for those values alone, costs a few comparisons a row:
-// with whole rows computed again 16384 rows of 256 with sigmoid and bias took 48 us, so 24.
+// with whole rows computed again 16384 rows of 256 with sigmoid and bias take 47.6 us, so 25.9; in groups 54.3, so 29.2.
 //
-// A warp has one row: with blocks that stay and take rows in turn, 4 an SM of 8 warps, the last turn is a third full (16384 rows
-// of 256: 24.8 us a call, so 21.5; in groups 31.9 and 31.1).
+// A warp has one row: blocks that stay and take rows in turn, 4 an SM of 8 warps, have a last turn that is a third full (an eighth
+// slower when it was tried, on an earlier form).
 //
-// Bound by instructions, some 1050 a row of 256 experts in 8 groups (580 with softmax alone): 23 us for 16384 rows by
-// themselves (14), where reading the logits takes 2.5.
+// Bound by instructions, some 1050 a row of 256 experts in 8 groups: of the 29.2 us that 16384 rows take, 21 are the
+// choice (of 20.0 where the logits alone decide, 11.4), and reading the logits takes 2.5.  bf16 logits, read one by one, cost
+// as much: 30.7 and 20.4 us.
 //
 // What is known of a call where its kernel is made: nothing; that the logits decide alone; sigmoid and a bias; these and groups
-// of 2^i whole lanes.  (Asked for in the kernel, the flags cost a tenth of the time: 27.3 instead of
-// 25.7 us a call for 16384 rows of 256 with sigmoid and a bias.)
+// of 2^i whole lanes.  (Asked for in the kernel, the flags cost 16384 rows of 256 with sigmoid and a bias 27.5 us a call
+// instead of 25.9, where the logits alone decide 23.0 instead of 20.0.)
 enum { kAnyChoice, kByLogits, kSigmoidBias, kSigmoidBiasGroups };
 // Lane's experts: lane * kPer .. lane * kPer + kPer - 1.
 template <int kPer, int kMode>
@@ -191,7 +192,9 @@ struct Chooser {
   // The errors, relative to the row's largest score: of a sigmoid two units of expf, half a unit of a sum and one of a
   // reciprocal, below 2^-21;
   // of a softmax the rounding of l - max (|x| exp(x) <= 0.37 units), expf, 21 additions and a quotient, below 2^-19.  A
-  // value adds half a unit of itself.  Equal logits with equal biases are equal exactly, however they are computed.
+  // value adds half a unit of itself; the bound takes the row's largest for all.  (So a bias far beyond the scores, the lowest
+  // finite number as a mask, has every row decided in fp64: 16384 rows of 256 then take 395 us, in groups 721.  A mask of -inf
+  // costs nothing.)  Equal logits with equal biases are equal exactly, however they are computed.
   __device__ __forceinline__ int choose(const RouteArgs &a, int row, float *shared, float &peak, float &z, bool &unsure) const {
     const int lane = threadIdx.x & 31;
     float l[kPer];
@@ -492,7 +495,7 @@ __global__ void __launch_bounds__(kChooseWarps * 32) choose_kernel(const __grid_
 // lanes of equal experts finding one another, 32 pairs at a time, 131072 pairs took 27 us.)
 //
 // A CTA that has no more than kStaged pairs puts them in their order in shared memory and writes each expert's one after
-// another (1024 rows of 8 of 64: 7.9 us a call against 9.4 with scattered words; 16384 rows of 256 20.1 against 22.1).
+// another (1024 rows of 8 of 64: 7.9 us a call against 9.4 with scattered words; 16384 rows of 256 20.0 against 22.0).
 constexpr int kGroupThreads = 1024, kGroupWarps = 32, kGroupCtas = 16, kStaged = 16384;
 // (Pitch of the histograms: odd, so that four lanes that add up eight warps each of one expert's meet no bank twice.)
 __host__ __device__ constexpr int group_pitch(int experts) { return experts | 1; }
@@ -505,8 +508,8 @@ __host__ __device__ constexpr int group_stretch(int rows, int ctas) {
 }
 static_assert(group_smem(kMostExperts, true) <= 220 * 1024, "shared memory");
 
-// kOnce: the stretch is 32 rows, whose bits the first walk finds and counts for both.  (16384 rows of 8 of 64: 15.3 us a call
-// otherwise, so 14.6; 1333 rows of 4 of 60 8.8 and 8.0.  Asked for in the kernel, 65536 rows of 2 of 64 took 30.8 instead of 28.7.)
+// kOnce: the stretch is 32 rows, whose bits the first walk finds and counts for both.  (16384 rows of 8 of 64: 15.0 us a call
+// otherwise, so 14.2; 1333 rows of 4 of 60 8.0 and 7.2.  Asked for in the kernel, it cost 65536 rows of 2 of 64 7%.)
 //
 // (Every thread of a block of kGroupThreads, of every block of the cluster; hist: [2][warps][pitch], and the staged pairs.)
 template <bool kOnce>
@@ -665,9 +668,10 @@ __global__ void __launch_bounds__(kGroupThreads) group_kernel(const __grid_const
   group_pairs<kOnce>(a, hist, staged != 0);
 }
 
-// A few rows: the choice and the grouping by one block.  (us with one launch / with two, 64 experts: 8 rows 4.7 / 4.8, 16 rows
-// 5.1 / 5.0, 32 rows 5.9 / 5.2; 256 experts: 5.8 / 5.9 for 8 rows, 6.4 / 6.0 for 16, 7.8 / 6.2 for 32.  Up to 16 for the sake of
-// calls outside graphs, where a launch is two of the host's.)
+// A few rows: the choice and the grouping by one block.  (us with one launch / with two, of 2, 8 and 32 choices.  64 experts: 8 rows
+// 4.2 / 4.4, 4.5 / 4.8, 6.1 / 6.3; 16 rows 4.5 / 4.4, 5.0 / 4.9, 7.2 / 7.2; 256 experts: 8 rows 5.3 / 5.2, 5.8 / 5.8, 7.9 / 7.8; 16 rows
+// 5.7 / 5.3, 6.4 / 5.9, 9.6 / 8.8; 32 rows of 8 choices 5.9 / 5.2 and 7.8 / 6.2.  Up to 16 for the sake of calls outside
+// graphs, where a launch is two of the host's.  With more than 256 experts the block's 64 registers a thread spill 204 bytes.)
 constexpr int kFewRows = 16;
 static_assert(kFewRows <= kGroupWarps, "a warp has one row");
 template <int kPer>
@@ -812,9 +816,11 @@ cudaError_t launch_route(const RouteArgs &a, cudaStream_t s) {
   if (e == cudaSuccess) e = allow_smem(group_kernel<true>, group_smem(kMostExperts, true), once_done, dev);
   if (e == cudaSuccess) e = allow_smem(group_kernel<false>, group_smem(kMostExperts, true), done, dev);
   if (e != cudaSuccess) return e;
-  // (The whole call with one block / a cluster of eight / of sixteen, us, 64 experts: 512 rows 6.3 / 7.1 / 7.2, 1024 rows
-  // 7.9 / 8.7 / 8.8, 2048 rows 12.7 / 9.0 / 9.1, 8192 rows 47 / 11.1 / 11.3, 16384 rows 88 / 19.1 / 14.6; 256 experts: 7.6 / 8.5 /
-  // 8.8, 9.5 / 10.5 / 10.8, 15.5 / 11.2 / 11.5, 59 / 15.4 / 15.9, 110 / 25.4 / 20.1.)
+  // The steps lie where a warp would have a second stretch of 32 rows, however many the choices.  (The whole call with one
+  // block / a cluster of eight / of sixteen, us, 64 experts.  2 choices: 1024 rows 5.8 / 6.5 / 6.6, 2048 rows 7.9 / 6.7 / 6.8,
+  // 8192 rows 18 / 8.0 / 8.2, 16384 rows 36 / 12.7 / 10.5; 8: 7.8 / 8.6 / 8.7, 12.4 / 8.9 / 9.0, 47 / 11.1 / 11.2, 87 / 18.7 / 14.3; 32:
+  // 28.4 / 29.4 / 29.4, 54 / 29.7 / 29.8, 196 / 35.4 / 35.5, 380 / 68 / 45.  256 experts, 8 choices: 9.4 / 10.4 / 10.7, 15.3 / 11.2 / 11.6,
+  // 58 / 15.4 / 15.9, 108 / 25.3 / 20.1; 2 and 32 alike.)
   const int ctas = a.rows <= 1024 ? 1 : a.rows <= 8192 ? 8 : group_ctas(dev);
   const int stretch = group_stretch(a.rows, ctas);
   const int staged = (int64_t)stretch * kGroupWarps * a.top_k <= kStaged;
