@@ -533,7 +533,8 @@ typedef struct ham_fp8_weight ham_fp8_weight; /* opaque handle: a weight laid ou
  * 2^31 rows of 128), HAM_ENOMEM, HAM_ECUDA; *out is NULL on failure. */
 int ham_fp8_weight_alloc(int32_t n, int32_t k, const void *codes, const void *scales, const void *codes_up,
                          const void *scales_up, ham_fp8_weight **out);
-int ham_fp8_weight_free(ham_fp8_weight *w); /* synchronizes as cudaFree does; NULL is a no-op */
+int ham_fp8_weight_free(ham_fp8_weight *w); /* synchronizes as cudaFree does, the last gated experts' weights with the
+                                             * whole device; NULL is a no-op */
 
 /* out [rows][n] = X W^T: 8-bit rows X [rows][k], products on the block-scaled tensor cores, summed in
  * fp32 and rounded once to out_dtype (HAM_DTYPE_BF16 or HAM_DTYPE_F32).  The tensor cores take 32 terms of
